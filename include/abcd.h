@@ -401,6 +401,57 @@ ABCD_API int32_t abcd_adam_step(const abcd_adam_group* groups /* host */, int32_
                                 hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Operators of a decoder that turns learned features, one row per Gaussian,
+ * into attributes, and of its training. A block of it is
+ *   x + dropout(ffn(layer_norm(x))).
+ * Matrices are row-major with unit stride along a row; ld* is the distance
+ * between rows in elements (>= the width) and may be odd, and an array needs its
+ * element's alignment only. All arrays of a call hold elements of `dtype`
+ * unless stated; statistics, products and sums are kept in fp32 (in the order
+ * that the launch fixes: the same call gives the same result) and every output
+ * is rounded once, to nearest, from fp32. n >= 0 rows, up to
+ * ABCD_MAX_GAUSSIANS; widths 1..ABCD_MAX_WIDTH. */
+typedef enum { ABCD_F32 = 0, ABCD_F16 = 1, ABCD_BF16 = 2 } abcd_dtype;
+#define ABCD_MAX_WIDTH 65536
+
+/* Layer norm over rows of width d: mean and rstd = 1 / sqrt(var + eps) with
+ * var = mean((x - mean)^2); y = (x - mean) rstd weight + bias. weight and bias
+ * (d elements of type wdtype: dtype or ABCD_F32) may be NULL, then 1 and 0.
+ * mean and rstd (fp32, n each) may be NULL, then not written; the backward needs
+ * them. eps >= 0 (with eps = 0 a constant row gives NaN). y may be x itself. */
+ABCD_API int32_t abcd_layer_norm(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx,
+                                 int32_t wdtype, const void* weight, const void* bias, float eps,
+                                 void* y, int64_t ldy, float* mean, float* rstd,
+                                 hipStream_t stream);
+
+/* Its gradients, with z = (x - mean) rstd and v = dy weight:
+ *   dx = add + rstd (v - mean(v) - z mean(v z));  dweight = sum dy z;  dbias = sum dy
+ * (sums over the rows, written, not added to; type wdtype). add (may be NULL) is
+ * a gradient that reaches x by another path, the residual one. dx, dweight and
+ * dbias may be NULL, then not computed; dx may be dy or add itself. workspace:
+ * at least abcd_layer_norm_bwd_workspace_size bytes, 256-byte aligned. */
+ABCD_API int32_t abcd_layer_norm_bwd_workspace_size(int32_t dtype, int64_t n, int64_t d,
+                                                    size_t* bytes);
+ABCD_API int32_t abcd_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* dy,
+                                     int64_t lddy, const void* x, int64_t ldx, const float* mean,
+                                     const float* rstd, int32_t wdtype, const void* weight,
+                                     const void* add, int64_t ldadd, void* dx, int64_t lddx,
+                                     void* dweight, void* dbias, void* workspace, size_t ws_bytes,
+                                     hipStream_t stream);
+
+/* Dropout: y = residual + keep x / (1 - p), 0 <= p <= 1 (p = 1: nothing is
+ * kept; what is dropped becomes 0, infinities and NaN too). residual may be NULL
+ * (then 0) and y may be x or residual itself. keep is never stored: element
+ * (row, col) takes word col % 4 of the Philox 4x32 block with 7 rounds (Salmon
+ * et al. 2011) of the counter (col / 4, row, offset low, offset high) under the
+ * key (seed low, seed high), and is kept if the word is >= floor(p 2^32). The
+ * gradient is the same call on dy without a residual. Calls whose masks are to
+ * be independent differ in offset. */
+ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx,
+                              const void* residual, int64_t ldr, void* y, int64_t ldy, double p,
+                              uint64_t seed, uint64_t offset, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Helpers. abcd_last_error: message of the last failure on this thread.
  * abcd_timing_*: optional per-kernel HIP-event timing of every launch made by
  * this thread (off by default; enabling it adds two event records per launch
@@ -409,7 +460,8 @@ ABCD_API int32_t abcd_adam_step(const abcd_adam_group* groups /* host */, int32_
  * (names: composite, project, bin_zero, depth_keys, radix_pass, l1_place,
  * l2_count, l2_scatter, bin_small_sort, bin_small_collect, bin_empty, bin_count,
  * render_fwd, loss_l1, zero_fill, bwd_order, render_bwd, project_bwd, adam,
- * render_cache, cache_rect_init). */
+ * render_cache, cache_rect_init, layer_norm, layer_norm_bwd, layer_norm_cols,
+ * sum_parts, dropout). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

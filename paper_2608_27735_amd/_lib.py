@@ -67,6 +67,13 @@ SIGNATURES = {
     "abcd_loss_l1_grad": (_I32, [_I32, _I32, _P, _P, C.POINTER(C.c_float), _P, _P, _P]),
     "abcd_adam_step": (_I32, [C.POINTER(abcd_adam_group), _I32, C.c_float, C.c_float, C.c_float,
                               _I64, _P]),
+    "abcd_layer_norm": (_I32, [_I32, _I64, _I64, _P, _I64, _I32, _P, _P, C.c_float, _P, _I64, _P, _P,
+                               _P]),
+    "abcd_layer_norm_bwd_workspace_size": (_I32, [_I32, _I64, _I64, C.POINTER(_SZ)]),
+    "abcd_layer_norm_bwd": (_I32, [_I32, _I64, _I64, _P, _I64, _P, _I64, _P, _P, _I32, _P, _P, _I64,
+                                   _P, _I64, _P, _P, _P, _SZ, _P]),
+    "abcd_dropout": (_I32, [_I32, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, C.c_double, C.c_uint64,
+                            C.c_uint64, _P]),
     "abcd_last_error": (C.c_char_p, []),
     "abcd_version": (C.c_char_p, []),
     "abcd_status_string": (C.c_char_p, [_I32]),

@@ -324,6 +324,172 @@ def adam_step(params, grads, exp_avg, exp_avg_sq, lr, step, beta1=0.9, beta2=0.9
                                      int(step), _stream()))
 
 
+# ------------------------------------------------------------ decoder: rows
+
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # abcd_dtype
+
+
+def _dtype_of(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _rows(t, name, like=None, shape=None, out=False):
+    """Checks a matrix of rows with unit stride along a row; returns the distance
+    between its rows. like: a tensor whose dtype and device it shares."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must be {like.dtype} on {like.device}, "
+                         f"got {t.dtype} on {t.device}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected "
+                         f"{'(rows, width)' if shape is None else shape}")
+    n, d = t.shape
+    if d == 0:
+        raise ValueError(f"{name} has rows of width 0")
+    s0, s1 = t.stride()
+    if n <= 1:
+        s0 = d
+    if (d > 1 and s1 != 1) or s0 < d:
+        raise ValueError(f"{name} must have unit stride along a row and rows that do not overlap, "
+                         f"got strides {t.stride()}")
+    return s0
+
+
+def _vector(t, name, d, dtype, device):
+    if t is None:
+        return
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (d,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with shape ({d},), got {tuple(t.shape)}")
+
+
+def _param_dtype(x, weight, bias):
+    """The common type of weight and bias: x's or float32."""
+    wt = weight.dtype if weight is not None else bias.dtype if bias is not None else x.dtype
+    if wt != x.dtype and wt != torch.float32:
+        raise ValueError(f"weight and bias must be {x.dtype} or float32, got {wt}")
+    return wt
+
+
+def _workspace(workspace, need, device):
+    if workspace is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    if not workspace.is_cuda or workspace.device != device or workspace.dtype != torch.uint8 \
+            or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
+    return workspace  # its size is checked by the library
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, mean=None, rstd=None):
+    """Layer norm of the rows of x [n, d] (float32, float16 or bfloat16; any row
+    stride): dict(y, mean, rstd), mean and rstd in float32, which
+    layer_norm_bwd takes. weight, bias [d]: of x's type or float32. out, mean,
+    rstd: where to write (out may be x)."""
+    code = _dtype_of(x, "x")
+    ldx = _rows(x, "x")
+    n, d = x.shape
+    wt = _param_dtype(x, weight, bias)
+    _vector(weight, "weight", d, wt, x.device)
+    _vector(bias, "bias", d, wt, x.device)
+    if out is None:
+        out = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    ldy = _rows(out, "out", x, (n, d))
+    if mean is None:
+        mean = _empty((n,), torch.float32, x.device)
+    if rstd is None:
+        rstd = _empty((n,), torch.float32, x.device)
+    _vector(mean, "mean", n, torch.float32, x.device)
+    _vector(rstd, "rstd", n, torch.float32, x.device)
+    check(_lib.load().abcd_layer_norm(code, n, d, x.data_ptr(), ldx, _DTYPES[wt], _ptr(weight),
+                                      _ptr(bias), float(eps), out.data_ptr(), ldy,
+                                      mean.data_ptr(), rstd.data_ptr(), _stream()))
+    return dict(y=out, mean=mean, rstd=rstd)
+
+
+def layer_norm_bwd_workspace_size(n, d, dtype):
+    sz = C.c_size_t(0)
+    check(_lib.load().abcd_layer_norm_bwd_workspace_size(_DTYPES[dtype], n, d, C.byref(sz)))
+    return sz.value
+
+
+def layer_norm_bwd(dy, x, mean, rstd, weight=None, add=None, wdtype=None, workspace=None,
+                   grads=None):
+    """Gradients of layer_norm: dict(x, weight, bias). mean and rstd are the
+    forward's; add [n, d] is added to x's gradient (a residual path's). weight
+    and bias gradients have weight's type (wdtype without a weight). grads: a
+    dict of tensors to write into, where a None leaves that gradient out."""
+    code = _dtype_of(x, "x")
+    ldx = _rows(x, "x")
+    n, d = x.shape
+    dev = x.device
+    lddy = _rows(dy, "dy", x, (n, d))
+    ldadd = 0 if add is None else _rows(add, "add", x, (n, d))
+    _vector(mean, "mean", n, torch.float32, dev)
+    _vector(rstd, "rstd", n, torch.float32, dev)
+    if weight is not None or wdtype is None:
+        wdtype = _param_dtype(x, weight, None)
+    elif wdtype != x.dtype and wdtype != torch.float32:
+        raise ValueError(f"wdtype must be {x.dtype} or float32, got {wdtype}")
+    _vector(weight, "weight", d, wdtype, dev)
+    if grads is None:
+        grads = dict(x=torch.empty((n, d), dtype=x.dtype, device=dev),
+                     weight=_empty((d,), wdtype, dev), bias=_empty((d,), wdtype, dev))
+    dx, dw, db = grads.get("x"), grads.get("weight"), grads.get("bias")
+    lddx = 0 if dx is None else _rows(dx, "grads[x]", x, (n, d))
+    _vector(dw, "grads[weight]", d, wdtype, dev)
+    _vector(db, "grads[bias]", d, wdtype, dev)
+    if dw is not None or db is not None:
+        workspace = _workspace(workspace, layer_norm_bwd_workspace_size(n, d, x.dtype), dev)
+    check(_lib.load().abcd_layer_norm_bwd(
+        code, n, d, dy.data_ptr(), lddy, x.data_ptr(), ldx, _ptr(mean), _ptr(rstd),
+        _DTYPES[wdtype], _ptr(weight), _ptr(add), ldadd, _ptr(dx), lddx, _ptr(dw), _ptr(db),
+        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return grads
+
+
+def _drop_args(p, seed, offset):
+    p, seed, offset = float(p), int(seed), int(offset)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must be in [0, 1], got {p}")
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    return p, seed, offset
+
+
+def dropout(x, p, seed, offset=0, residual=None, out=None):
+    """residual + dropout(x) for x [n, d] (any row stride): an element is kept
+    with probability 1 - p and divided by it. The mask is a function of seed,
+    offset and the element's row and column (see abcd_dropout) and is never
+    stored; calls whose masks are to be independent differ in offset. out may be
+    x or residual."""
+    code = _dtype_of(x, "x")
+    ldx = _rows(x, "x")
+    n, d = x.shape
+    p, seed, offset = _drop_args(p, seed, offset)
+    ldr = 0 if residual is None else _rows(residual, "residual", x, (n, d))
+    if out is None:
+        out = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    ldy = _rows(out, "out", x, (n, d))
+    check(_lib.load().abcd_dropout(code, n, d, x.data_ptr(), ldx, _ptr(residual), ldr,
+                                   out.data_ptr(), ldy, p, seed, offset, _stream()))
+    return out
+
+
+def dropout_bwd(dy, p, seed, offset=0, out=None):
+    """Gradient of dropout's x: the forward's p, seed and offset make its mask
+    again (the residual's gradient is dy itself)."""
+    return dropout(dy, p, seed, offset, out=out)
+
+
 # ---------------------------------------------------------------- collapse
 
 def composite_cache(images, order, n_front, F=None, B=None, accumulate=False, rects=None,
@@ -417,4 +583,5 @@ __all__ = ["AbcdError", "project", "bin_sort", "bin_sort_workspace_size", "rende
            "render_bwd", "render_bwd_workspace_size", "composite_cache", "loss_l1_grad",
            "timing_enable", "timing_reset", "timing_read", "version", "n_tiles", "adam_step",
            "render_cache", "stage_cached", "make_split", "split_workspace_size", "intersections",
-           "render_bwd_noalloc"]
+           "render_bwd_noalloc", "layer_norm", "layer_norm_bwd", "layer_norm_bwd_workspace_size",
+           "dropout", "dropout_bwd"]

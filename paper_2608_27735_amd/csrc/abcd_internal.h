@@ -2,7 +2,7 @@
 //
 // Kernels are written for CDNA4: 64-lane wavefronts, 16x16 pixel tiles mapped
 // to 256-thread workgroups (4 waves), LDS staging, wave-level ballots and
-// shuffles. Nothing here is a dense contraction, so no MFMA is used.
+// shuffles. Nothing in the step is a dense contraction, so it uses no MFMA.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -28,6 +28,14 @@ int32_t hip_fail(hipError_t e, const char* what);
   do {                              \
     const int32_t st_ = (call);     \
     if (st_ != ABCD_OK) return st_; \
+  } while (0)
+
+#define REQUIRE(cond, ...)            \
+  do {                                \
+    if (!(cond)) {                    \
+      abcd::set_error(__VA_ARGS__);   \
+      return ABCD_E_INVALID;          \
+    }                                 \
   } while (0)
 
 #define ABCD_HIP(call)                                   \
@@ -338,5 +346,24 @@ int32_t stage_cached(int width, int height, int k, const uint16_t* const* host_i
 int32_t launch_composite(int width, int height, int k, const uint16_t* images,
                          const int32_t* order, int n_front, const int32_t* rects, float stop_t,
                          float* F, float* B, int accumulate, bool beside, hipStream_t stream);
+
+// dropout.hip, layer_norm.hip, reduce.hip (dtype: abcd_dtype; ld*: elements
+// between rows)
+int32_t launch_dropout(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx,
+                       const void* residual, int64_t ldr, void* y, int64_t ldy, double p,
+                       uint64_t seed, uint64_t offset, hipStream_t stream);
+size_t layer_norm_bwd_workspace_bytes(int32_t dtype, int64_t n, int64_t d);
+int32_t launch_layer_norm(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx,
+                          int32_t wdtype, const void* weight, const void* bias, float eps, void* y,
+                          int64_t ldy, float* mean, float* rstd, hipStream_t stream);
+int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* dy, int64_t lddy,
+                              const void* x, int64_t ldx, const float* mean, const float* rstd,
+                              int32_t wdtype, const void* weight, const void* add, int64_t ldadd,
+                              void* dx, int64_t lddx, void* dweight, void* dbias, void* workspace,
+                              hipStream_t stream);
+// out0[c] = sum over p of part[p][c] for c < split, out1[c - split] for the other
+// columns, rounded to dtype; either may be NULL. No parts: zeros.
+int32_t launch_sum_parts(const float* part, int64_t parts, int64_t cols, int64_t split,
+                         int32_t dtype, void* out0, void* out1, hipStream_t stream);
 
 }  // namespace abcd

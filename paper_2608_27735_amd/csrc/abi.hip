@@ -61,14 +61,6 @@ using namespace abcd;
 
 namespace {
 
-#define REQUIRE(cond, ...)            \
-  do {                                \
-    if (!(cond)) {                    \
-      abcd::set_error(__VA_ARGS__);   \
-      return ABCD_E_INVALID;          \
-    }                                 \
-  } while (0)
-
 int32_t check_camera(const abcd_camera* c) {
   REQUIRE(c != nullptr, "camera is NULL");
   REQUIRE(c->width > 0 && c->height > 0, "image size %dx%d must be positive", c->width, c->height);

@@ -1,0 +1,56 @@
+// reduce.hip -- sums of partial results in a fixed order.
+#include <algorithm>
+
+#include "rows.h"
+
+namespace abcd {
+namespace {
+
+constexpr int kPartWaves = 16;
+
+// out0[c] (c < split) and out1[c - split] = sum over p of part[p][c]: 64 columns
+// per workgroup, the parts dealt to its 16 waves, whose sums LDS joins.
+template <typename T>
+__global__ __launch_bounds__(kPartWaves* kWave) void sum_parts_kernel(const float* part, int64_t parts,
+                                                                     int64_t cols, int64_t split, T* out0,
+                                                                     T* out1) {
+  __shared__ float red[kPartWaves][kWave];
+  const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+  const int64_t c = (int64_t)blockIdx.x * kWave + l;
+  float s = 0.0f;
+  if (c < cols) {
+    int64_t p = w;
+    for (; p + 7 * kPartWaves < parts; p += 8 * kPartWaves) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = part[(p + i * kPartWaves) * cols + c];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
+    for (; p < parts; p += kPartWaves) s += part[p * cols + c];
+  }
+  red[w][l] = s;
+  __syncthreads();
+  if (w != 0 || c >= cols) return;
+  for (int i = 1; i < kPartWaves; ++i) s += red[i][l];
+  if (c < split) {
+    if (out0) out0[c] = (T)s;
+  } else if (out1) {
+    out1[c - split] = (T)s;
+  }
+}
+
+}  // namespace
+
+int32_t launch_sum_parts(const float* part, int64_t parts, int64_t cols, int64_t split, int32_t dtype, void* out0,
+                         void* out1, hipStream_t stream) {
+  return with_type(dtype, [&](auto zero) -> int32_t {
+    typedef decltype(zero) T;
+    ABCD_LAUNCH("sum_parts", (sum_parts_kernel<T>), (cols + kWave - 1) / kWave, kPartWaves * kWave, 0, stream, part,
+                parts, cols, split, static_cast<T*>(out0), static_cast<T*>(out1));
+    ABCD_HIP(hipGetLastError());
+    return ABCD_OK;
+  });
+}
+
+}  // namespace abcd
