@@ -451,6 +451,51 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
                               const void* residual, int64_t ldr, void* y, int64_t ldy, double p,
                               uint64_t seed, uint64_t offset, hipStream_t stream);
 
+/* Gated feed-forward block over rows x[n][d]:
+ *   h = act(x w_gate' + b_gate) * (x w_up' + b_up);  y = residual + dropout(h w_down' + b_down)
+ * with h of width `h` and y of width `o`. Weights are contiguous, one row per
+ * output: w_gate and w_up [h][d], w_down [o][h]; biases [h], [h], [o], each may be
+ * NULL (0). Dropout as in abcd_dropout over y's n rows (p = 0: none). act:
+ * ABCD_ACT_SILU g sigmoid(g), ABCD_ACT_GELU g Phi(g) (Phi the normal distribution,
+ * by the error function), ABCD_ACT_RELU max(g, 0). Products and act are computed
+ * in fp32; the pre-activations, h and the gradients that reach them are rounded
+ * to dtype where they are stored between products. */
+enum { ABCD_ACT_SILU = 0, ABCD_ACT_GELU = 1, ABCD_ACT_RELU = 2 };
+typedef struct abcd_ffn {
+  int32_t dtype, act;
+  int64_t d, h, o;
+  const void *w_gate, *w_up, *w_down;
+  const void *b_gate, *b_up, *b_down;
+  double p;
+  uint64_t seed, offset;
+} abcd_ffn;
+
+/* Forward. residual (may be NULL) and y: [n][o], y may be residual itself. gate,
+ * up, hidden: all NULL, or arrays [n][(h + 7) / 8 * 8] of dtype, 16-byte aligned,
+ * that receive the pre-activations and h for the backward (columns past h: zeros).
+ * workspace: at least abcd_gated_ffn_workspace_size(ffn, n, saved) bytes (saved: 1
+ * if gate, up and hidden are given, else 0), 256-byte aligned. */
+ABCD_API int32_t abcd_gated_ffn_workspace_size(const abcd_ffn* ffn /* host */, int64_t n,
+                                               int32_t saved, size_t* bytes);
+ABCD_API int32_t abcd_gated_ffn(const abcd_ffn* ffn /* host */, int64_t n, const void* x,
+                                int64_t ldx, const void* residual, int64_t ldr, void* y,
+                                int64_t ldy, void* gate, void* up, void* hidden, void* workspace,
+                                size_t ws_bytes, hipStream_t stream);
+
+/* Backward: gradients of x (not counting the residual path, whose gradient is dy
+ * itself) and of every weight and bias, written, of dtype, laid out as what they
+ * belong to; each may be NULL, then not computed. gate, up, hidden: the forward's,
+ * or all NULL: then they are computed again from x (one product more, and no
+ * memory held between the passes). p, seed and offset are the forward's. */
+ABCD_API int32_t abcd_gated_ffn_bwd_workspace_size(const abcd_ffn* ffn /* host */, int64_t n,
+                                                   int32_t saved, size_t* bytes);
+ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, const void* dy,
+                                    int64_t lddy, const void* x, int64_t ldx, const void* gate,
+                                    const void* up, const void* hidden, void* dx, int64_t lddx,
+                                    void* dw_gate, void* dw_up, void* dw_down, void* db_gate,
+                                    void* db_up, void* db_down, void* workspace, size_t ws_bytes,
+                                    hipStream_t stream);
+
 /* ------------------------------------------------------------------------ */
 /* Helpers. abcd_last_error: message of the last failure on this thread.
  * abcd_timing_*: optional per-kernel HIP-event timing of every launch made by
@@ -461,7 +506,8 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
  * l2_count, l2_scatter, bin_small_sort, bin_small_collect, bin_empty, bin_count,
  * render_fwd, loss_l1, zero_fill, bwd_order, render_bwd, project_bwd, adam,
  * render_cache, cache_rect_init, layer_norm, layer_norm_bwd, layer_norm_cols,
- * sum_parts, dropout). */
+ * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
+ * ffn_dweight). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

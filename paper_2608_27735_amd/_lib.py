@@ -42,9 +42,18 @@ class abcd_split(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class abcd_ffn(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("d", C.c_int64), ("h", C.c_int64),
+                ("o", C.c_int64), ("w_gate", C.c_void_p), ("w_up", C.c_void_p),
+                ("w_down", C.c_void_p), ("b_gate", C.c_void_p), ("b_up", C.c_void_p),
+                ("b_down", C.c_void_p), ("p", C.c_double), ("seed", C.c_uint64),
+                ("offset", C.c_uint64)]
+
+
 _P = C.c_void_p  # device pointers travel as integers
 _I32, _I64, _SZ = C.c_int32, C.c_int64, C.c_size_t
 _CAM, _PRM = C.POINTER(abcd_camera), C.POINTER(abcd_raster_params)
+_FFN = C.POINTER(abcd_ffn)
 
 # name -> (restype, argtypes); mirrors include/abcd.h
 SIGNATURES = {
@@ -74,6 +83,11 @@ SIGNATURES = {
                                    _P, _I64, _P, _P, _P, _SZ, _P]),
     "abcd_dropout": (_I32, [_I32, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, C.c_double, C.c_uint64,
                             C.c_uint64, _P]),
+    "abcd_gated_ffn_workspace_size": (_I32, [_FFN, _I64, _I32, C.POINTER(_SZ)]),
+    "abcd_gated_ffn_bwd_workspace_size": (_I32, [_FFN, _I64, _I32, C.POINTER(_SZ)]),
+    "abcd_gated_ffn": (_I32, [_FFN, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _SZ, _P]),
+    "abcd_gated_ffn_bwd": (_I32, [_FFN, _I64, _P, _I64, _P, _I64] + [_P] * 4 + [_I64] + [_P] * 7 +
+                           [_SZ, _P]),
     "abcd_last_error": (C.c_char_p, []),
     "abcd_version": (C.c_char_p, []),
     "abcd_status_string": (C.c_char_p, [_I32]),

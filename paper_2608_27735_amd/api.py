@@ -490,6 +490,124 @@ def dropout_bwd(dy, p, seed, offset=0, out=None):
     return dropout(dy, p, seed, offset, out=out)
 
 
+_ACTS = {"silu": 0, "gelu": 1, "relu": 2}  # ABCD_ACT_*
+FFN_WEIGHTS = ("w_gate", "w_up", "w_down")
+FFN_BIASES = ("b_gate", "b_up", "b_down")
+
+
+def _ffn(x, params, act, p, seed, offset):
+    """The block's description for the library, checked against x [n, d]."""
+    code = _dtype_of(x, "x")
+    ldx = _rows(x, "x")
+    d, dev = x.shape[1], x.device
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}, got {act!r}")
+    for k in params:
+        if k not in FFN_WEIGHTS and k not in FFN_BIASES:
+            raise ValueError(f"unknown parameter {k!r}")
+    for k in FFN_WEIGHTS:
+        if params.get(k) is None:
+            raise ValueError(f"{k} is required")
+    if params["w_gate"].dim() != 2 or params["w_down"].dim() != 2:
+        raise ValueError("w_gate and w_down must be matrices")
+    h, o = params["w_gate"].shape[0], params["w_down"].shape[0]
+    if h == 0 or o == 0:
+        raise ValueError("a weight has no rows")
+    f = _lib.abcd_ffn()
+    f.dtype, f.act, f.d, f.h, f.o = code, _ACTS[act], d, h, o
+    for k, shape in (("w_gate", (h, d)), ("w_up", (h, d)), ("w_down", (o, h)), ("b_gate", (h,)),
+                     ("b_up", (h,)), ("b_down", (o,))):
+        t = params.get(k)
+        if t is None:
+            continue
+        if t.dtype != x.dtype or t.device != dev:
+            raise ValueError(f"{k} must be {x.dtype} on {dev}, got {t.dtype} on {t.device}")
+        if tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{k} must be contiguous with shape {shape}, got {tuple(t.shape)}")
+        setattr(f, k, t.data_ptr())
+    f.p, f.seed, f.offset = _drop_args(p, seed, offset)
+    return f, ldx
+
+
+def _saved_ptrs(saved, n, h, like):
+    """gate, up, hidden of a forward that kept them."""
+    if saved is None:
+        return [None] * 3
+    out = []
+    for k in ("gate", "up", "hidden"):
+        t = saved[k]
+        if t.dtype != like.dtype or t.device != like.device or not t.is_contiguous() \
+                or tuple(t.shape) != (n, (h + 7) // 8 * 8):
+            raise ValueError(f"saved[{k}] must be a contiguous {like.dtype} tensor of shape "
+                             f"({n}, {(h + 7) // 8 * 8}) on {like.device}")
+        out.append(t.data_ptr() if n > 0 else None)
+    return out
+
+
+def gated_ffn(x, params, act="silu", residual=None, p=0.0, seed=0, offset=0, save=False, out=None,
+              workspace=None):
+    """Gated feed-forward block of x [n, d] (float32, float16 or bfloat16; any
+    row stride): residual + dropout(h w_down' + b_down) with
+    h = act(x w_gate' + b_gate) * (x w_up' + b_up). params: dict(w_gate [h, d],
+    w_up [h, d], w_down [o, h][, b_gate [h], b_up [h], b_down [o]]) of x's type.
+    act: "silu", "gelu" or "relu". Dropout as in dropout().
+
+    Returns dict(y [n, o], saved): with save=True what gated_ffn_bwd needs of
+    this pass, else None (it computes that again). out may be residual."""
+    f, ldx = _ffn(x, params, act, p, seed, offset)
+    n, dev = x.shape[0], x.device
+    ldr = 0 if residual is None else _rows(residual, "residual", x, (n, f.o))
+    if out is None:
+        out = torch.empty((n, f.o), dtype=x.dtype, device=dev)
+    ldy = _rows(out, "out", x, (n, f.o))
+    saved = None
+    if save:
+        hp = (f.h + 7) // 8 * 8
+        saved = {k: torch.empty((n, hp), dtype=x.dtype, device=dev) for k in ("gate", "up", "hidden")}
+    lib = _lib.load()
+    sz = C.c_size_t(0)
+    check(lib.abcd_gated_ffn_workspace_size(C.byref(f), n, 1 if save else 0, C.byref(sz)))
+    workspace = _workspace(workspace, sz.value, dev)
+    check(lib.abcd_gated_ffn(C.byref(f), n, x.data_ptr(), ldx, _ptr(residual), ldr, out.data_ptr(),
+                             ldy, *_saved_ptrs(saved, n, f.h, x), workspace.data_ptr(),
+                             workspace.numel(), _stream()))
+    return dict(y=out, saved=saved)
+
+
+def gated_ffn_bwd(dy, x, params, act="silu", saved=None, p=0.0, seed=0, offset=0, grads=None,
+                  workspace=None):
+    """Gradients of gated_ffn for dy [n, o]: dict(x, w_gate, w_up, w_down[, and
+    the biases that params has]); the residual's is dy itself. saved: the
+    forward's, or None to compute it again. p, seed and offset are the forward's.
+    grads: a dict of tensors to write into, where a missing one is left out."""
+    f, ldx = _ffn(x, params, act, p, seed, offset)
+    n, d = x.shape
+    dev = x.device
+    lddy = _rows(dy, "dy", x, (n, f.o))
+    if grads is None:
+        grads = {k: torch.empty_like(params[k]) for k in FFN_WEIGHTS + FFN_BIASES
+                 if params.get(k) is not None}
+        grads["x"] = torch.empty((n, d), dtype=x.dtype, device=dev)
+    for k, shape in (("w_gate", (f.h, d)), ("w_up", (f.h, d)), ("w_down", (f.o, f.h)),
+                     ("b_gate", (f.h,)), ("b_up", (f.h,)), ("b_down", (f.o,))):
+        t = grads.get(k)
+        if t is not None and (t.dtype != x.dtype or t.device != dev or tuple(t.shape) != shape
+                              or not t.is_contiguous()):
+            raise ValueError(f"grads[{k}] must be contiguous {x.dtype} on {dev} with shape {shape}")
+    dx = grads.get("x")
+    lddx = 0 if dx is None else _rows(dx, "grads[x]", x, (n, d))
+    lib = _lib.load()
+    sz = C.c_size_t(0)
+    check(lib.abcd_gated_ffn_bwd_workspace_size(C.byref(f), n, 0 if saved is None else 1,
+                                                C.byref(sz)))
+    workspace = _workspace(workspace, sz.value, dev)
+    check(lib.abcd_gated_ffn_bwd(
+        C.byref(f), n, dy.data_ptr(), lddy, x.data_ptr(), ldx, *_saved_ptrs(saved, n, f.h, x),
+        _ptr(dx), lddx, *[_ptr(grads.get(k)) for k in FFN_WEIGHTS + FFN_BIASES],
+        workspace.data_ptr(), workspace.numel(), _stream()))
+    return grads
+
+
 # ---------------------------------------------------------------- collapse
 
 def composite_cache(images, order, n_front, F=None, B=None, accumulate=False, rects=None,
@@ -584,4 +702,4 @@ __all__ = ["AbcdError", "project", "bin_sort", "bin_sort_workspace_size", "rende
            "timing_enable", "timing_reset", "timing_read", "version", "n_tiles", "adam_step",
            "render_cache", "stage_cached", "make_split", "split_workspace_size", "intersections",
            "render_bwd_noalloc", "layer_norm", "layer_norm_bwd", "layer_norm_bwd_workspace_size",
-           "dropout", "dropout_bwd"]
+           "dropout", "dropout_bwd", "gated_ffn", "gated_ffn_bwd"]

@@ -347,7 +347,7 @@ int32_t launch_composite(int width, int height, int k, const uint16_t* images,
                          const int32_t* order, int n_front, const int32_t* rects, float stop_t,
                          float* F, float* B, int accumulate, bool beside, hipStream_t stream);
 
-// dropout.hip, layer_norm.hip, reduce.hip (dtype: abcd_dtype; ld*: elements
+// dropout.hip, layer_norm.hip (dtype: abcd_dtype; ld*: elements
 // between rows)
 int32_t launch_dropout(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx,
                        const void* residual, int64_t ldr, void* y, int64_t ldy, double p,
@@ -361,7 +361,17 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
                               int32_t wdtype, const void* weight, const void* add, int64_t ldadd,
                               void* dx, int64_t lddx, void* dweight, void* dbias, void* workspace,
                               hipStream_t stream);
-// out0[c] = sum over p of part[p][c] for c < split, out1[c - split] for the other
+// gated_ffn.hip
+size_t gated_ffn_workspace_bytes(const abcd_ffn& f, int64_t n, bool saved, bool backward);
+int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx,
+                         const void* residual, int64_t ldr, void* y, int64_t ldy, void* gate,
+                         void* up, void* hidden, void* workspace, hipStream_t stream);
+int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64_t lddy,
+                             const void* x, int64_t ldx, const void* gate, const void* up,
+                             const void* hidden, void* dx, int64_t lddx, void* dw_gate,
+                             void* dw_up, void* dw_down, void* db_gate, void* db_up, void* db_down,
+                             void* workspace, hipStream_t stream);
+// reduce.hip: out0[c] = sum over p of part[p][c] for c < split, out1[c - split] for the other
 // columns, rounded to dtype; either may be NULL. No parts: zeros.
 int32_t launch_sum_parts(const float* part, int64_t parts, int64_t cols, int64_t split,
                          int32_t dtype, void* out0, void* out1, hipStream_t stream);

@@ -45,9 +45,84 @@ int32_t check_workspace(const void* ws, size_t have, size_t need) {
   return ABCD_OK;
 }
 
+int32_t check_ffn(const abcd_ffn* f, int64_t n) {
+  REQUIRE(f != nullptr, "ffn is NULL");
+  TRY_STATUS(check_rows(f->dtype, n, f->d));
+  TRY_STATUS(check_rows(f->dtype, n, f->h));
+  TRY_STATUS(check_rows(f->dtype, n, f->o));
+  REQUIRE(f->act == ABCD_ACT_SILU || f->act == ABCD_ACT_GELU || f->act == ABCD_ACT_RELU, "unknown act %d", f->act);
+  REQUIRE(f->p >= 0.0 && f->p <= 1.0, "p must be in [0, 1]");
+  return ABCD_OK;
+}
+
+int32_t check_ffn_weights(const abcd_ffn& f) {
+  REQUIRE(f.w_gate && f.w_up && f.w_down, "a weight is NULL");
+  TRY_STATUS(check_vector("w_gate", f.w_gate, f.dtype));
+  TRY_STATUS(check_vector("w_up", f.w_up, f.dtype));
+  TRY_STATUS(check_vector("w_down", f.w_down, f.dtype));
+  TRY_STATUS(check_vector("b_gate", f.b_gate, f.dtype));
+  TRY_STATUS(check_vector("b_up", f.b_up, f.dtype));
+  return check_vector("b_down", f.b_down, f.dtype);
+}
+
+int32_t check_saved(const void* gate, const void* up, const void* hidden) {
+  REQUIRE((gate == nullptr) == (up == nullptr) && (up == nullptr) == (hidden == nullptr),
+          "gate, up and hidden go together");
+  for (const void* p : {gate, up, hidden})
+    REQUIRE((reinterpret_cast<uintptr_t>(p) & 15) == 0, "gate, up and hidden must be 16-byte aligned");
+  return ABCD_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int32_t abcd_gated_ffn_workspace_size(const abcd_ffn* ffn, int64_t n, int32_t saved, size_t* bytes) {
+  TRY_STATUS(check_ffn(ffn, n));
+  REQUIRE(bytes != nullptr, "bytes is NULL");
+  *bytes = gated_ffn_workspace_bytes(*ffn, n, saved != 0, false);
+  return ABCD_OK;
+}
+
+int32_t abcd_gated_ffn_bwd_workspace_size(const abcd_ffn* ffn, int64_t n, int32_t saved, size_t* bytes) {
+  TRY_STATUS(check_ffn(ffn, n));
+  REQUIRE(bytes != nullptr, "bytes is NULL");
+  *bytes = gated_ffn_workspace_bytes(*ffn, n, saved != 0, true);
+  return ABCD_OK;
+}
+
+int32_t abcd_gated_ffn(const abcd_ffn* ffn, int64_t n, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                       void* y, int64_t ldy, void* gate, void* up, void* hidden, void* workspace, size_t ws_bytes,
+                       hipStream_t stream) {
+  TRY_STATUS(check_ffn(ffn, n));
+  const abcd_ffn& f = *ffn;
+  TRY_STATUS(check_ffn_weights(f));
+  TRY_STATUS(check_matrix("x", x, f.dtype, n, f.d, ldx, false));
+  TRY_STATUS(check_matrix("residual", residual, f.dtype, n, f.o, ldr, true));
+  TRY_STATUS(check_matrix("y", y, f.dtype, n, f.o, ldy, false));
+  TRY_STATUS(check_saved(gate, up, hidden));
+  if (n > 0)
+    TRY_STATUS(check_workspace(workspace, ws_bytes, gated_ffn_workspace_bytes(f, n, hidden != nullptr, false)));
+  return launch_gated_ffn(f, n, x, ldx, residual, ldr, y, ldy, gate, up, hidden, workspace, stream);
+}
+
+int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn, int64_t n, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                           const void* gate, const void* up, const void* hidden, void* dx, int64_t lddx,
+                           void* dw_gate, void* dw_up, void* dw_down, void* db_gate, void* db_up, void* db_down,
+                           void* workspace, size_t ws_bytes, hipStream_t stream) {
+  TRY_STATUS(check_ffn(ffn, n));
+  const abcd_ffn& f = *ffn;
+  TRY_STATUS(check_ffn_weights(f));
+  TRY_STATUS(check_matrix("dy", dy, f.dtype, n, f.o, lddy, false));
+  TRY_STATUS(check_matrix("x", x, f.dtype, n, f.d, ldx, false));
+  TRY_STATUS(check_matrix("dx", dx, f.dtype, n, f.d, lddx, true));
+  TRY_STATUS(check_saved(gate, up, hidden));
+  for (const void* g : {dw_gate, dw_up, dw_down, db_gate, db_up, db_down})
+    TRY_STATUS(check_vector("a gradient", g, f.dtype));
+  TRY_STATUS(check_workspace(workspace, ws_bytes, gated_ffn_workspace_bytes(f, n, hidden != nullptr, true)));
+  return launch_gated_ffn_bwd(f, n, dy, lddy, x, ldx, gate, up, hidden, dx, lddx, dw_gate, dw_up, dw_down, db_gate,
+                              db_up, db_down, workspace, stream);
+}
 
 int32_t abcd_layer_norm(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx, int32_t wdtype,
                         const void* weight, const void* bias, float eps, void* y, int64_t ldy, float* mean,

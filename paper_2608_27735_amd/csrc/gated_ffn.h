@@ -1,0 +1,301 @@
+// gated_ffn.h -- the gated feed-forward block's kernels, for one element type
+// (gated_ffn_f32.hip, gated_ffn_f16.hip and gated_ffn_bf16.hip each compile them
+// for theirs).
+//
+//   g = x Wg' + bg, u = x Wu' + bu, h = a(g) u, y = residual + dropout(h Wd' + bd)
+// and, with dz = dropout's gradient of dy,
+//   dh = dz Wd, dg = dh u a'(g), du = dh a(g), dx = dg Wg + du Wu,
+//   dWg = dg' x, dWu = du' x, dWd = dz' h, and the biases' gradients the column sums.
+// Five products: both projections in one (a tile holds the same columns of g and
+// of u, so h is made from the accumulators), the down projection, dh (whose
+// accumulators become dg and du with g and u read back), dx as one product of
+// twice the contraction, and the weights' gradients, split along the rows where
+// the result has too few tiles to fill the GPU. Products accumulate in fp32; g, u,
+// h, dg and du are rounded to the element type between the launches, as the
+// matrix cores read them, and everything else is rounded once.
+#pragma once
+
+#include <algorithm>
+
+#include "gated_ffn_args.h"
+#include "gemm.h"
+
+namespace abcd {
+namespace {
+
+// e^-g by the hardware's base-2 exponential.
+__device__ __forceinline__ float sigmoid(float g) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * g));
+}
+
+// a(g) and, where it is wanted, a'(g). The activation is the same for every lane.
+__device__ __forceinline__ float activate(float g, int act) {
+  if (act == ABCD_ACT_SILU) return g * sigmoid(g);
+  if (act == ABCD_ACT_GELU) return g * (0.5f + 0.5f * erff(0.70710678118654752f * g));
+  return fmaxf(g, 0.0f);
+}
+__device__ __forceinline__ float activate_grad(float g, int act, float& slope) {
+  if (act == ABCD_ACT_SILU) {
+    const float s = sigmoid(g);
+    slope = s * (1.0f + g * (1.0f - s));
+    return g * s;
+  }
+  if (act == ABCD_ACT_GELU) {
+    const float c = 0.5f + 0.5f * erff(0.70710678118654752f * g);
+    slope = c + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
+    return g * c;
+  }
+  slope = g > 0.0f ? 1.0f : 0.0f;
+  return fmaxf(g, 0.0f);
+}
+
+// Tiles: 256 x 256 by 8 waves, each 128 x 64 of it, where there are enough of
+// them; else 128 x 128 by 4 waves of 64 x 64.
+struct Big {
+  static constexpr int TX = 256, TW = 256, WX = 2, WW = 4;
+};
+struct Small {
+  static constexpr int TX = 128, TW = 128, WX = 2, WW = 2;
+};
+
+template <typename T, typename Cfg, bool kXAlong, bool kWAlong, bool kHalves>
+using ProductOf = Product<T, Cfg::TX, Cfg::TW, Cfg::WX, Cfg::WW, kXAlong, kWAlong, kHalves>;
+
+#define ABCD_TILE_LDS(P)                    \
+  __shared__ __align__(16) char tile0[P::kLdsBytes]; \
+  __shared__ __align__(16) char tile1[P::kLdsBytes]; \
+  LdsChar* const lds0 = (LdsChar*)tile0;    \
+  LdsChar* const lds1 = (LdsChar*)tile1
+
+template <typename T>
+__device__ __forceinline__ f32x4 load4(const void* p, int64_t at, int64_t n) {
+  return load_vec<T, 4, false>(static_cast<const T*>(p) + at, n > 4 ? 4 : (int)n);
+}
+
+template <typename T, typename Cfg>
+__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn a) {
+  typedef ProductOf<T, Cfg, true, true, true> P;
+  ABCD_TILE_LDS(P);
+  int tx, tw;
+  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
+  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * (Cfg::TW / 2);
+  P p;
+  p.template run<1>(a.x, a.w, ix, iw, 0, a.d, lds0, lds1);
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int w = 0; w < P::FW / 2; ++w) {
+    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4;
+    if (c >= a.ldh) continue;
+    f32x4 bg = 0.0f, bu = 0.0f;
+    if (a.bg && c < a.h) bg = load4<T>(a.bg, c, a.h - c);
+    if (a.bu && c < a.h) bu = load4<T>(a.bu, c, a.h - c);
+#pragma unroll
+    for (int x = 0; x < P::FX; ++x) {
+      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
+      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
+      if (r >= a.x.len) continue;
+      f32x4 g = p.acc[x][w] + bg, u = p.acc[x][w + P::FW / 2] + bu, h;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
+        h[i] = activate(g[i], a.act) * u[i];
+      }
+      const int64_t at = r * a.ldh + c;
+      store_vec<T, 4, true>(static_cast<T*>(a.hidden) + at, h, 4);
+      if (a.gate) {
+        store_vec<T, 4, true>(static_cast<T*>(a.gate) + at, g, 4);
+        store_vec<T, 4, true>(static_cast<T*>(a.up) + at, u, 4);
+      }
+    }
+  }
+}
+
+template <typename T, typename Cfg>
+__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_out_kernel(FfnOut a) {
+  typedef ProductOf<T, Cfg, true, true, false> P;
+  ABCD_TILE_LDS(P);
+  int tx, tw;
+  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
+  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
+  P p;
+  p.template run<1>(a.hidden, a.w, ix, iw, 0, a.h, lds0, lds1);
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int w = 0; w < P::FW; ++w) {
+    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4, left = a.o - c;
+    if (left <= 0) continue;
+    f32x4 b = 0.0f;
+    if (a.bias) b = load4<T>(a.bias, c, left);
+#pragma unroll
+    for (int x = 0; x < P::FX; ++x) {
+      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
+      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
+      if (r >= a.hidden.len) continue;
+      f32x4 y = drop_vec<4>(p.acc[x][w] + b, a.key, (uint32_t)r, (uint32_t)c);
+      if (a.res) y = load4<T>(a.res, r * a.ldr + c, left) + y;
+      store_vec<T, 4, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, (int)(left > 4 ? 4 : left));
+    }
+  }
+}
+
+template <typename T, typename Cfg>
+__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dhidden_kernel(FfnDHidden a) {
+  typedef ProductOf<T, Cfg, true, false, false> P;
+  ABCD_TILE_LDS(P);
+  int tx, tw;
+  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
+  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
+  P p;
+  p.template run<1>(a.dz, a.w, ix, iw, 0, a.o, lds0, lds1);
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int w = 0; w < P::FW; ++w) {
+    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4;
+    if (c >= a.ldh) continue;
+#pragma unroll
+    for (int x = 0; x < P::FX; ++x) {
+      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
+      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
+      if (r >= a.dz.len) continue;
+      const int64_t at = r * a.ldh + c;
+      const f32x4 g = load_vec<T, 4, true>(static_cast<const T*>(a.gate) + at, 4);
+      const f32x4 u = load_vec<T, 4, true>(static_cast<const T*>(a.up) + at, 4);
+      f32x4 dg, du;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float slope;
+        const float v = activate_grad(g[i], a.act, slope), dh = p.acc[x][w][i];
+        const bool in = c + i < a.h;
+        dg[i] = in ? dh * u[i] * slope : 0.0f;
+        du[i] = in ? dh * v : 0.0f;
+      }
+      store_vec<T, 4, true>(static_cast<T*>(a.dgate) + at, dg, 4);
+      store_vec<T, 4, true>(static_cast<T*>(a.dup) + at, du, 4);
+    }
+  }
+}
+
+template <typename T, typename Cfg>
+__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dx_kernel(FfnDX a) {
+  typedef ProductOf<T, Cfg, true, false, false> P;
+  ABCD_TILE_LDS(P);
+  int tx, tw;
+  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
+  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
+  P p;
+  p.template run<2>(a.dgu, a.w, ix, iw, 0, a.h, lds0, lds1);
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int w = 0; w < P::FW; ++w) {
+    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4, left = a.d - c;
+    if (left <= 0) continue;
+#pragma unroll
+    for (int x = 0; x < P::FX; ++x) {
+      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
+      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
+      if (r < a.dgu.len)
+        store_vec<T, 4, false>(static_cast<T*>(a.dx) + r * a.lddx + c, p.acc[x][w], (int)(left > 4 ? 4 : left));
+    }
+  }
+}
+
+// Weights' gradients: rows are X's index (of half tx >= tiles_x / 2 with two), the
+// contraction runs over rows [blockIdx.y per, + per).
+template <typename T, typename Cfg>
+__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dweight_kernel(FfnDWeight a) {
+  typedef ProductOf<T, Cfg, false, false, false> P;
+  ABCD_TILE_LDS(P);
+  int tx, tw;
+  tile_of(blockIdx.x, a.halves * a.tiles_x, a.tiles_w, tx, tw);
+  const int half = tx >= a.tiles_x ? 1 : 0;
+  const int64_t ix = (int64_t)(tx - half * a.tiles_x) * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
+  const int64_t k0 = blockIdx.y * a.per, k1 = k0 + a.per < a.n ? k0 + a.per : a.n;
+  Side X = a.x;
+  X.p[0] = a.x.p[half];
+  P p;
+  p.template run<1>(X, a.w, ix, iw, k0, k1, lds0, lds1);
+  const int l = threadIdx.x & 63;
+  const int64_t cols = a.w.len, rows = a.x.len;
+#pragma unroll
+  for (int w = 0; w < P::FW; ++w) {
+    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4, left = cols - c;
+    if (left <= 0) continue;
+    const int m = (int)(left > 4 ? 4 : left);
+#pragma unroll
+    for (int x = 0; x < P::FX; ++x) {
+      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
+      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
+      if (r >= rows) continue;
+      if (a.part)
+        store_vec<float, 4, false>(a.part + ((blockIdx.y * a.halves + half) * rows + r) * cols + c, p.acc[x][w], m);
+      else
+        store_vec<T, 4, false>(static_cast<T*>(half ? a.out1 : a.out0) + r * cols + c, p.acc[x][w], m);
+    }
+  }
+}
+
+inline int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
+
+// The big tile where it gives most of the CUs one.
+inline bool use_big(int64_t nx, int64_t nw, int tw) { return tiles(nx, Big::TX) * tiles(nw, tw) >= 192; }
+
+#define ABCD_FFN_LAUNCH(label, kernel, a, nx, nw, half, stream)                                           \
+  do {                                                                                                    \
+    const bool big_ = use_big(nx, nw, Big::TW / (half));                                                  \
+    a.tiles_x = (int)tiles(nx, big_ ? Big::TX : Small::TX);                                               \
+    a.tiles_w = (int)tiles(nw, (big_ ? Big::TW : Small::TW) / (half));                                    \
+    const int64_t grid_ = (int64_t)a.tiles_x * a.tiles_w;                                                 \
+    REQUIRE(grid_ < (int64_t(1) << 31), "too many tiles");                                                \
+    if (big_)                                                                                             \
+      ABCD_LAUNCH(label, (kernel<T, Big>), grid_, Big::WX* Big::WW * 64, 0, stream, a);                   \
+    else                                                                                                  \
+      ABCD_LAUNCH(label, (kernel<T, Small>), grid_, Small::WX* Small::WW * 64, 0, stream, a);             \
+    ABCD_HIP(hipGetLastError());                                                                          \
+  } while (0)
+
+template <typename T>
+int32_t run_in(FfnIn a, hipStream_t stream) {
+  ABCD_FFN_LAUNCH("ffn_in", ffn_in_kernel, a, a.x.len, a.h, 2, stream);
+  return ABCD_OK;
+}
+template <typename T>
+int32_t run_out(FfnOut a, hipStream_t stream) {
+  ABCD_FFN_LAUNCH("ffn_out", ffn_out_kernel, a, a.hidden.len, a.o, 1, stream);
+  return ABCD_OK;
+}
+template <typename T>
+int32_t run_dhidden(FfnDHidden a, hipStream_t stream) {
+  ABCD_FFN_LAUNCH("ffn_dhidden", ffn_dhidden_kernel, a, a.dz.len, a.h, 1, stream);
+  return ABCD_OK;
+}
+template <typename T>
+int32_t run_dx(FfnDX a, hipStream_t stream) {
+  ABCD_FFN_LAUNCH("ffn_dx", ffn_dx_kernel, a, a.dgu.len, a.d, 1, stream);
+  return ABCD_OK;
+}
+template <typename T>
+int32_t run_dweight(FfnDWeight a, int splits, hipStream_t stream) {
+  const bool big = splits == 1 && use_big(a.halves * a.x.len, a.w.len, Big::TW);
+  a.tiles_x = (int)tiles(a.x.len, big ? Big::TX : Small::TX);
+  a.tiles_w = (int)tiles(a.w.len, big ? Big::TW : Small::TW);
+  const dim3 grid(a.halves * a.tiles_x * a.tiles_w, splits);
+  if (big)
+    ABCD_LAUNCH("ffn_dweight", (ffn_dweight_kernel<T, Big>), grid, Big::WX* Big::WW * 64, 0, stream, a);
+  else
+    ABCD_LAUNCH("ffn_dweight", (ffn_dweight_kernel<T, Small>), grid, Small::WX* Small::WW * 64, 0, stream, a);
+  ABCD_HIP(hipGetLastError());
+  return ABCD_OK;
+}
+
+}  // namespace
+
+#define ABCD_FFN_KERNELS(NAME, TYPE)                                                                   \
+  int32_t ffn_in_##NAME(const FfnIn& a, hipStream_t s) { return run_in<TYPE>(a, s); }                  \
+  int32_t ffn_out_##NAME(const FfnOut& a, hipStream_t s) { return run_out<TYPE>(a, s); }               \
+  int32_t ffn_dhidden_##NAME(const FfnDHidden& a, hipStream_t s) { return run_dhidden<TYPE>(a, s); }   \
+  int32_t ffn_dx_##NAME(const FfnDX& a, hipStream_t s) { return run_dx<TYPE>(a, s); }                  \
+  int32_t ffn_dweight_##NAME(const FfnDWeight& a, int splits, hipStream_t s) {                         \
+    return run_dweight<TYPE>(a, splits, s);                                                            \
+  }
+
+}  // namespace abcd

@@ -1,0 +1,275 @@
+// gated_ffn.hip -- the gated feed-forward block: how a call becomes products
+// (gated_ffn.h), copies of what 16-byte loads cannot take, and column sums.
+#include <algorithm>
+
+#include "gated_ffn_args.h"
+
+namespace abcd {
+namespace {
+
+// Copies rows of `cols` elements into rows of ldd, the rest of each zeroed, with
+// dropout where the key says so: what a product reads has to start on 16 bytes,
+// its rows a multiple of that apart, with zeros up to it.
+struct PackArgs {
+  const void* src;
+  void* dst;
+  int64_t ld, ldd, n;
+  int cols, lanes;
+  DropKey key;
+};
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void pack_rows_kernel(PackArgs a) {
+  constexpr int N = kPer16<T>;
+  const int t = threadIdx.x & (a.lanes - 1), rows = kBlock / a.lanes;
+  for (int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / a.lanes; row < a.n;
+       row += (int64_t)gridDim.x * rows) {
+    const T* s = static_cast<const T*>(a.src) + row * a.ld;
+    T* d = static_cast<T*>(a.dst) + row * a.ldd;
+    for (int c = t * N; c < a.ldd; c += a.lanes * N) {
+      Floats<N> v = 0.0f;
+      if (c < a.cols) v = load_vec<T, N, false>(s + c, a.cols - c);
+      store_vec<T, N, true>(d + c, drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c), N);
+    }
+  }
+}
+
+// part[blockIdx.y][c] = sum over rows blockIdx.y, + gridDim.y rows.. of m[row][c].
+// `lanes` threads along a row, the workgroup's other threads on other rows.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void column_sums_kernel(const void* m, int64_t ld, int64_t n, int cols,
+                                                             int lanes, float* part) {
+  constexpr int N = kPer16<T>;
+  __shared__ float red[kBlock * N];
+  const int t = threadIdx.x & (lanes - 1), rows = kBlock / lanes;
+  const int c = ((int)blockIdx.x * lanes + t) * N;
+  Floats<N> s = 0.0f;
+  if (c < cols)
+    for (int64_t row = (int64_t)blockIdx.y * rows + threadIdx.x / lanes; row < n; row += (int64_t)gridDim.y * rows)
+      s += load_vec<T, N, false>(static_cast<const T*>(m) + row * ld + c, cols - c);
+#pragma unroll
+  for (int i = 0; i < N; ++i) red[threadIdx.x * N + i] = s[i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < lanes * N; i += kBlock) {
+    const int64_t at = (int64_t)blockIdx.x * lanes * N + i;
+    if (at >= cols) break;
+    float v = 0.0f;
+    for (int r = 0; r < rows; ++r) v += red[r * lanes * N + i];
+    part[(int64_t)blockIdx.y * cols + at] = v;
+  }
+}
+
+int lanes_for(int nvec) {
+  int l = 1;
+  while (l < kBlock && l < nvec) l *= 2;
+  return l;
+}
+
+int64_t sum_parts_of(int64_t n) { return std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, 256)); }
+
+int32_t pack(int32_t dtype, int64_t n, int64_t cols, const void* src, int64_t ld, void* dst, int64_t ldd,
+             const DropKey& key, hipStream_t stream) {
+  return with_type(dtype, [&](auto z) -> int32_t {
+    typedef decltype(z) T;
+    PackArgs a{src, dst, ld, ldd, n, (int)cols, lanes_for((int)(ldd / kPer16<T>)), key};
+    const int64_t rows = kBlock / a.lanes;
+    ABCD_LAUNCH("pack_rows", (pack_rows_kernel<T>), std::min<int64_t>((n + rows - 1) / rows, 1 << 20), kBlock, 0,
+                stream, a);
+    ABCD_HIP(hipGetLastError());
+    return ABCD_OK;
+  });
+}
+
+// out[c] = sum over the rows of m, rounded to dtype.
+int32_t column_sums(int32_t dtype, int64_t n, int64_t cols, const void* m, int64_t ld, void* out, float* part,
+                    hipStream_t stream) {
+  const int64_t parts = sum_parts_of(n);
+  TRY_STATUS(with_type(dtype, [&](auto z) -> int32_t {
+    typedef decltype(z) T;
+    const int nvec = (int)((cols + kPer16<T> - 1) / kPer16<T>), lanes = std::min(lanes_for(nvec), 64);
+    ABCD_LAUNCH("column_sums", (column_sums_kernel<T>), dim3((nvec + lanes - 1) / lanes, parts), kBlock, 0, stream,
+                m, ld, n, (int)cols, lanes, part);
+    ABCD_HIP(hipGetLastError());
+    return ABCD_OK;
+  }));
+  return launch_sum_parts(part, parts, cols, cols, dtype, out, nullptr, stream);
+}
+
+int64_t up8(int64_t v) { return (v + 7) & ~int64_t(7); }
+
+// Whether products can read rows of `cols` elements at p, ld apart, as they are.
+bool direct(int32_t dtype, const void* p, int64_t cols, int64_t ld) {
+  const size_t sz = type_bytes(dtype);
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * sz) % 16 == 0 && (cols * sz) % 16 == 0 &&
+         ld <= (int64_t(1) << 20);
+}
+
+// Hands out a workspace in 256-byte pieces; with no base it only adds up.
+struct Pieces {
+  char* base;
+  size_t used = 0;
+  void* take(size_t bytes) {
+    char* p = base ? base + used : nullptr;
+    used += align256(bytes);
+    return p;
+  }
+};
+
+struct Scratch {
+  void *x, *wg, *wu, *wd, *dz, *gate, *up, *hidden;
+  float* part;
+  size_t bytes;
+};
+
+// How many ways the rows are split for a weight gradient of `tiles` 128 x 128
+// tiles: about two workgroups per CU, each with at least 512 rows.
+int splits_for(int64_t tiles, int64_t n) {
+  const int64_t want = (512 + tiles - 1) / tiles, most = std::max<int64_t>(1, n / 512);
+  return (int)std::min<int64_t>({want, most, 256});
+}
+int64_t tiles128(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128); }
+int splits_gate_up(const abcd_ffn& f, int64_t n) { return splits_for(2 * tiles128(f.h, f.d), n); }
+int splits_down(const abcd_ffn& f, int64_t n) { return splits_for(tiles128(f.o, f.h), n); }
+
+Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* workspace) {
+  const size_t sz = type_bytes(f.dtype);
+  const int64_t dp = up8(f.d), hp = up8(f.h), op = up8(f.o);
+  Pieces p{static_cast<char*>(workspace)};
+  Scratch s{};
+  s.x = p.take(n * dp * sz);
+  s.wg = p.take(f.h * dp * sz);
+  s.wu = p.take(f.h * dp * sz);
+  s.wd = p.take(f.o * hp * sz);
+  if (!saved) s.hidden = p.take(n * hp * sz);
+  if (backward) {
+    s.dz = p.take(n * op * sz);
+    s.gate = p.take(n * hp * sz);
+    s.up = p.take(n * hp * sz);
+    size_t part = sum_parts_of(n) * std::max(f.h, f.o);
+    const int sg = splits_gate_up(f, n), sd = splits_down(f, n);
+    if (sg > 1) part = std::max<size_t>(part, (size_t)sg * 2 * f.h * f.d);
+    if (sd > 1) part = std::max<size_t>(part, (size_t)sd * f.h * f.o);
+    s.part = static_cast<float*>(p.take(part * sizeof(float)));
+  }
+  s.bytes = p.used;
+  return s;
+}
+
+#define FFN_BY_TYPE(f, fn, ...)                                 \
+  ((f).dtype == ABCD_F32   ? fn##_f32(__VA_ARGS__)              \
+   : (f).dtype == ABCD_F16 ? fn##_f16(__VA_ARGS__)              \
+                           : fn##_bf16(__VA_ARGS__))
+
+// A weight as products read it: itself or its copy.
+int32_t weight(const abcd_ffn& f, const void* w, int64_t rows, int64_t cols, void* copy, Side& s,
+               hipStream_t stream) {
+  s = Side{{w, nullptr}, cols, rows};
+  if (direct(f.dtype, w, cols, cols)) return ABCD_OK;
+  s.p[0] = copy;
+  s.ld = up8(cols);
+  return pack(f.dtype, rows, cols, w, cols, copy, s.ld, DropKey{}, stream);
+}
+
+int32_t rows_of(const abcd_ffn& f, const void* m, int64_t n, int64_t cols, int64_t ld, void* copy, Side& s,
+                hipStream_t stream) {
+  s = Side{{m, nullptr}, ld, n};
+  if (direct(f.dtype, m, cols, ld)) return ABCD_OK;
+  s.p[0] = copy;
+  s.ld = up8(cols);
+  return pack(f.dtype, n, cols, m, ld, copy, s.ld, DropKey{}, stream);
+}
+
+// Both projections as one side of two halves; their copies are laid out alike.
+int32_t gate_up(const abcd_ffn& f, const Scratch& s, Side& w, hipStream_t stream) {
+  const bool both = direct(f.dtype, f.w_gate, f.d, f.d) && direct(f.dtype, f.w_up, f.d, f.d);
+  w = Side{{f.w_gate, f.w_up}, f.d, f.h};
+  if (both) return ABCD_OK;
+  w = Side{{s.wg, s.wu}, up8(f.d), f.h};
+  TRY_STATUS(pack(f.dtype, f.h, f.d, f.w_gate, f.d, s.wg, w.ld, DropKey{}, stream));
+  return pack(f.dtype, f.h, f.d, f.w_up, f.d, s.wu, w.ld, DropKey{}, stream);
+}
+
+}  // namespace
+
+size_t gated_ffn_workspace_bytes(const abcd_ffn& f, int64_t n, bool saved, bool backward) {
+  return layout(f, n, saved, backward, nullptr).bytes;
+}
+
+int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx, const void* residual,
+                         int64_t ldr, void* y, int64_t ldy, void* gate, void* up, void* hidden, void* workspace,
+                         hipStream_t stream) {
+  if (n == 0) return ABCD_OK;
+  const Scratch s = layout(f, n, hidden != nullptr, false, workspace);
+  if (!hidden) hidden = s.hidden;
+  const int64_t hp = up8(f.h);
+  Side xs, w;
+  TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
+  TRY_STATUS(gate_up(f, s, w, stream));
+  const FfnIn in{xs, w, f.b_gate, f.b_up, hidden, gate, up, f.d, f.h, hp, f.act, 0, 0};
+  TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
+  TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, w, stream));
+  const FfnOut out{Side{{hidden, nullptr}, hp, n}, w, f.b_down, residual, y, f.h, f.o, ldr, ldy,
+                   drop_key(f.p, f.seed, f.offset), 0, 0};
+  return FFN_BY_TYPE(f, ffn_out, out, stream);
+}
+
+int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64_t lddy, const void* x,
+                             int64_t ldx, const void* gate, const void* up, const void* hidden, void* dx,
+                             int64_t lddx, void* dw_gate, void* dw_up, void* dw_down, void* db_gate, void* db_up,
+                             void* db_down, void* workspace, hipStream_t stream) {
+  const Scratch s = layout(f, n, hidden != nullptr, true, workspace);
+  const int64_t hp = up8(f.h);
+  Side xs{}, wgu{}, wd{}, dz{};
+  if (n > 0) {
+    TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
+    TRY_STATUS(gate_up(f, s, wgu, stream));
+    TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, wd, stream));
+    if (f.p > 0.0) {
+      dz = Side{{s.dz, nullptr}, up8(f.o), n};
+      TRY_STATUS(pack(f.dtype, n, f.o, dy, lddy, s.dz, dz.ld, drop_key(f.p, f.seed, f.offset), stream));
+    } else {
+      TRY_STATUS(rows_of(f, dy, n, f.o, lddy, s.dz, dz, stream));
+    }
+    if (!hidden) {
+      const FfnIn in{xs, wgu, f.b_gate, f.b_up, s.hidden, s.gate, s.up, f.d, f.h, hp, f.act, 0, 0};
+      TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
+      gate = s.gate;
+      up = s.up;
+      hidden = s.hidden;
+    }
+  }
+  // W side across: its index is h, the contraction o
+  const bool inner = dx || dw_gate || dw_up || db_gate || db_up;
+  if (n > 0 && inner) {
+    const FfnDHidden dh{dz, Side{{wd.p[0], nullptr}, wd.ld, f.h}, gate, up, s.gate, s.up, f.o, f.h, hp, f.act, 0, 0};
+    TRY_STATUS(FFN_BY_TYPE(f, ffn_dhidden, dh, stream));
+  }
+  const Side dgu{{s.gate, s.up}, hp, n};
+  if (n > 0 && dx) {
+    const FfnDX a{dgu, Side{{wgu.p[0], wgu.p[1]}, wgu.ld, f.d}, dx, f.h, f.d, lddx, 0, 0};
+    TRY_STATUS(FFN_BY_TYPE(f, ffn_dx, a, stream));
+  }
+  auto dweight = [&](Side X, Side W, int halves, void* out0, void* out1, int splits) -> int32_t {
+    const int64_t rows = (n + splits - 1) / splits, per = (rows + 63) / 64 * 64;
+    FfnDWeight a{X, W, out0, out1, splits > 1 ? s.part : nullptr, n, per, halves, 0, 0};
+    TRY_STATUS(FFN_BY_TYPE(f, ffn_dweight, a, splits, stream));
+    if (splits > 1)
+      return launch_sum_parts(s.part, splits, halves * X.len * W.len, X.len * W.len, f.dtype, out0, out1, stream);
+    return ABCD_OK;
+  };
+  if (dw_gate || dw_up) {
+    Side X{{dw_gate ? s.gate : s.up, s.up}, hp, f.h};
+    const int halves = dw_gate && dw_up ? 2 : 1;
+    TRY_STATUS(dweight(X, Side{{xs.p[0], nullptr}, xs.ld, f.d}, halves, dw_gate ? dw_gate : dw_up, dw_up,
+                       splits_gate_up(f, n)));
+  }
+  if (dw_down)
+    TRY_STATUS(dweight(Side{{dz.p[0], nullptr}, dz.ld, f.o}, Side{{hidden, nullptr}, hp, f.h}, 1, dw_down, nullptr,
+                       splits_down(f, n)));
+  if (db_gate) TRY_STATUS(column_sums(f.dtype, n, f.h, s.gate, hp, db_gate, s.part, stream));
+  if (db_up) TRY_STATUS(column_sums(f.dtype, n, f.h, s.up, hp, db_up, s.part, stream));
+  if (db_down) TRY_STATUS(column_sums(f.dtype, n, f.o, dz.p[0], dz.ld, db_down, s.part, stream));
+  return ABCD_OK;
+}
+
+}  // namespace abcd

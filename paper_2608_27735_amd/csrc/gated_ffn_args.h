@@ -1,0 +1,75 @@
+// gated_ffn_args.h -- arguments of the gated feed-forward block's products, and
+// their launchers by element type.
+#pragma once
+
+#include "rows.h"
+
+namespace abcd {
+
+// One side of a product. Aligned for 16-byte loads: p and ld * sizeof(T) are
+// multiples of 16, 256 rows are less than 2^31 bytes, and, contracted along, the
+// elements between the contraction's end and the next multiple of 16 bytes are zeros.
+struct Side {
+  const void* p[2];  // the second where there are two segments or two halves
+  int64_t ld;
+  int64_t len;  // of the index that is not contracted (of each half)
+};
+
+// hidden, gate and up: [n][ldh], columns [h, ldh) zero; gate NULL: only hidden
+struct FfnIn {
+  Side x, w;
+  const void* bg;
+  const void* bu;
+  void* hidden;
+  void* gate;
+  void* up;
+  int64_t d, h, ldh;
+  int act, tiles_x, tiles_w;
+};
+struct FfnOut {
+  Side hidden, w;
+  const void* bias;
+  const void* res;
+  void* y;
+  int64_t h, o, ldr, ldy;
+  DropKey key;
+  int tiles_x, tiles_w;
+};
+struct FfnDHidden {
+  Side dz, w;
+  const void* gate;
+  const void* up;
+  void* dgate;  // may be gate and up themselves
+  void* dup;
+  int64_t o, h, ldh;
+  int act, tiles_x, tiles_w;
+};
+struct FfnDX {
+  Side dgu, w;
+  void* dx;
+  int64_t h, d, lddx;
+  int tiles_x, tiles_w;
+};
+// out = X' W over n rows, X of one or two halves; part: [splits][halves][x.len][w.len]
+// fp32 sums over `per` rows each, or NULL for the results themselves
+struct FfnDWeight {
+  Side x, w;
+  void* out0;
+  void* out1;
+  float* part;
+  int64_t n, per;
+  int halves, tiles_x, tiles_w;
+};
+
+#define ABCD_FFN_DECLARE(NAME)                                 \
+  int32_t ffn_in_##NAME(const FfnIn&, hipStream_t);            \
+  int32_t ffn_out_##NAME(const FfnOut&, hipStream_t);          \
+  int32_t ffn_dhidden_##NAME(const FfnDHidden&, hipStream_t);  \
+  int32_t ffn_dx_##NAME(const FfnDX&, hipStream_t);            \
+  int32_t ffn_dweight_##NAME(const FfnDWeight&, int, hipStream_t);
+ABCD_FFN_DECLARE(f32)
+ABCD_FFN_DECLARE(f16)
+ABCD_FFN_DECLARE(bf16)
+#undef ABCD_FFN_DECLARE
+
+}  // namespace abcd

@@ -90,3 +90,49 @@ def act(g, name):
         c = torch.special.ndtr(g)
         return g * c, c + g * torch.exp(-0.5 * g * g) / math.sqrt(2.0 * math.pi)
     return torch.relu(g), (g > 0).to(F64)
+
+
+def ffn(x, w, name, u, res=None, keep=None, p=0.0, dy=None):
+    """The gated feed-forward block and its gradients: name -> (value, magnitude
+    of the fp32 sums' terms, standard deviation that rounding the stored
+    intermediates to unit u leaves, to first order)."""
+    z = lambda k, n: w[k] if w.get(k) is not None else torch.zeros(n, dtype=F64)
+    h, o = w["w_gate"].shape[0], w["w_down"].shape[0]
+    g, up = x @ w["w_gate"].T + z("b_gate", h), x @ w["w_up"].T + z("b_up", h)
+    mg = x.abs() @ w["w_gate"].abs().T + z("b_gate", h).abs()
+    mu = x.abs() @ w["w_up"].abs().T + z("b_up", h).abs()
+    a, da = act(g, name)
+    hid = a * up
+    # fp32 sums reach h too
+    sh = u * hid.abs() + 8 * E32 * (da.abs() * mg * up.abs() + a.abs() * mu + hid.abs())
+    y = hid @ w["w_down"].T + z("b_down", o)
+    my = hid.abs() @ w["w_down"].abs().T + z("b_down", o).abs()
+    sy = (sh ** 2 @ w["w_down"].T ** 2).sqrt()
+    keep = torch.ones_like(y, dtype=torch.bool) if keep is None else keep
+    scale = 1.0 / (1.0 - p) if p < 1.0 else 0.0
+    y, my, sy = (torch.where(keep, v * scale, torch.zeros_like(v)) for v in (y, my, sy))
+    if res is not None:
+        y, my = y + res, my + res.abs()
+    out = dict(y=(y, my, sy))
+    if dy is None:
+        return out
+    dz = torch.where(keep, dy * scale, torch.zeros_like(dy))
+    sdz = u * dz.abs() if p > 0 else torch.zeros_like(dz)
+    dh = dz @ w["w_down"]
+    sdh = (sdz ** 2 @ w["w_down"] ** 2).sqrt() + 8 * E32 * (dz.abs() @ w["w_down"].abs())
+    dg, du = dh * up * da, dh * a
+    sdg = u * (dg.abs() * 2 + (dh * up * g).abs()) + (up * da).abs() * sdh + \
+        8 * E32 * ((dh * da).abs() * mu + (dh * up).abs() * mg)
+    if name == "relu":  # its derivative jumps where the fp32 sum may have either sign
+        sdg = sdg + torch.where(g.abs() <= 16 * E32 * mg, (dh * up).abs(), torch.zeros_like(g))
+    sdu = u * (du.abs() + (dh * da * g).abs()) + a.abs() * sdh + 8 * E32 * dh.abs() * mg * da.abs()
+    both = lambda f: f(dg, sdg, "w_gate") + f(du, sdu, "w_up")
+    out["x"] = (both(lambda v, s, k: v @ w[k]), both(lambda v, s, k: v.abs() @ w[k].abs()),
+                both(lambda v, s, k: s ** 2 @ w[k] ** 2).sqrt())
+    for k, v, s in (("w_gate", dg, sdg), ("w_up", du, sdu)):
+        out[k] = (v.T @ x, v.abs().T @ x.abs(), ((s ** 2).T @ x ** 2).sqrt())
+    out["w_down"] = (dz.T @ hid, dz.abs().T @ hid.abs(),
+                     ((sdz ** 2).T @ hid ** 2 + (dz ** 2).T @ sh ** 2).sqrt())
+    for k, v, s in (("b_gate", dg, sdg), ("b_up", du, sdu), ("b_down", dz, sdz)):
+        out[k] = (v.sum(0), v.abs().sum(0), (s ** 2).sum(0).sqrt())
+    return out

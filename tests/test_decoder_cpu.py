@@ -80,3 +80,56 @@ def test_reference_generator_known_block():
     for j, word in enumerate(c):
         for p in (word / 2.0 ** 32, (word + 1) / 2.0 ** 32):
             assert bool(R.keep_mask(1, 4, p, 0, 0)[0, j]) == (word >= int(p * 2 ** 32))
+
+
+def _ffn(**kw):
+    from paper_2608_27735_amd import _lib
+    f = _lib.abcd_ffn()
+    f.dtype, f.act, f.d, f.h, f.o, f.p = F16, 0, 8, 16, 8, 0.1
+    f.w_gate = f.w_up = f.w_down = FAKE
+    for k, v in kw.items():
+        setattr(f, k, v)
+    return f
+
+
+BAD_FFN = [dict(dtype=3), dict(act=3), dict(act=-1), dict(d=0), dict(h=0), dict(o=0), dict(d=65537), dict(h=65537),
+           dict(p=-0.5), dict(p=1.5), dict(p=float("nan")), dict(w_gate=None), dict(w_up=None), dict(w_down=None),
+           dict(w_up=FAKE + 1), dict(b_gate=FAKE + 1), dict(b_up=FAKE + 1), dict(b_down=FAKE + 1)]
+
+
+def test_gated_ffn_refuses(lib):
+    need = C.c_size_t(0)
+    assert lib.abcd_gated_ffn_workspace_size(C.byref(_ffn()), 4, 0, C.byref(need)) == 0
+    base = [C.byref(_ffn()), 4, FAKE, 8, FAKE, 8, FAKE, 8, FAKE, FAKE, FAKE, FAKE, need.value, None]
+    refuse(base, lib.abcd_gated_ffn,
+           [(0, None), (1, -1), (2, None), (3, 7), (4, FAKE + 1), (5, 7), (6, None), (7, 7), (8, None), (9, None),
+            (10, None), (10, FAKE + 8), (11, None), (11, FAKE + 64), (12, 0)])
+    refuse(base, lib.abcd_gated_ffn, [(0, C.byref(_ffn(**kw))) for kw in BAD_FFN])
+    assert lib.abcd_gated_ffn_workspace_size(None, 4, 0, C.byref(need)) == 1
+    assert lib.abcd_gated_ffn_workspace_size(C.byref(_ffn()), 4, 0, None) == 1
+
+
+def test_gated_ffn_bwd_refuses(lib):
+    need = C.c_size_t(0)
+    assert lib.abcd_gated_ffn_bwd_workspace_size(C.byref(_ffn()), 4, 1, C.byref(need)) == 0
+    base = [C.byref(_ffn()), 4, FAKE, 8, FAKE, 8, FAKE, FAKE, FAKE, FAKE, 8] + [FAKE] * 7 + [need.value, None]
+    refuse(base, lib.abcd_gated_ffn_bwd,
+           [(0, None), (1, -1), (2, None), (3, 7), (4, None), (5, 7), (6, None), (7, FAKE + 8), (8, None), (10, 7)] +
+           [(i, FAKE + 1) for i in range(11, 17)] + [(17, None), (17, FAKE + 8), (18, need.value - 1)])
+    refuse(base, lib.abcd_gated_ffn_bwd, [(0, C.byref(_ffn(**kw))) for kw in BAD_FFN])
+    assert lib.abcd_gated_ffn_bwd_workspace_size(C.byref(_ffn()), -1, 1, C.byref(need)) == 1
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu", "relu"])
+def test_reference_ffn_gradients_are_its_forwards(name):
+    g = torch.Generator().manual_seed(1)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=R.F64)
+    n, d, h, o = 5, 7, 9, 6
+    x, dy, keep = r(n, d), r(n, o), r(n, o) > -0.3
+    w = dict(w_gate=r(h, d), w_up=r(h, d), w_down=r(o, h), b_gate=r(h), b_up=r(h), b_down=r(o))
+    leaves = {k: v.clone().requires_grad_() for k, v in {**w, "x": x}.items()}
+    y = R.ffn(leaves["x"], {k: leaves[k] for k in w}, name, 0.0, None, keep, 0.25)["y"][0]
+    want = dict(zip(leaves, torch.autograd.grad((y * dy).sum(), list(leaves.values()))))
+    got = R.ffn(x, w, name, 0.0, None, keep, 0.25, dy)
+    for k in want:
+        assert torch.allclose(got[k][0], want[k], rtol=1e-10, atol=1e-12), k

@@ -1,0 +1,226 @@
+"""The gated feed-forward block, forward and backward, against its float64
+definition. Tolerances: one rounding of the output, six standard deviations of
+what rounding the stored intermediates leaves, and fp32 roundings of the sums'
+terms (16 of their magnitude)."""
+import pytest
+import torch
+
+import decoder_ref as R
+from test_gpu_decoder_rows import DT, IDS, rand, say
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def api():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2608_27735_amd import api
+    return api
+
+
+def weights(seed, d, h, o, dtype, bias):
+    w = dict(w_gate=rand(seed, h, d, dtype, scale=d ** -0.5), w_up=rand(seed + 1, h, d, dtype, scale=d ** -0.5),
+             w_down=rand(seed + 2, o, h, dtype, scale=h ** -0.5))
+    w = {k: v.contiguous() for k, v in w.items()}
+    if bias:
+        w.update(b_gate=rand(seed + 3, 1, h, dtype, scale=0.3)[0], b_up=rand(seed + 4, 1, h, dtype, scale=0.3)[0],
+                 b_down=rand(seed + 5, 1, o, dtype, scale=0.3)[0])
+    return w
+
+
+def check(name, got, ref):
+    value, mag, sd = ref
+    R.close(name, got, value, mag, extra=6 * sd)
+
+
+def run(api, n, d, h, o, dtype, act, bias, p, pad=0, skip=0, seed=5, offset=9, recompute=False):
+    say("ffn", n, d, h, o, dtype, act, "bias" if bias else "", "p", p, "pad", pad, skip)
+    x, w = rand(1, n, d, dtype, pad, skip), weights(10, d, h, o, dtype, bias)
+    res, dy = rand(2, n, o, dtype, skip, pad), rand(3, n, o, dtype, pad, skip)
+    keep = R.keep_mask(n, o, p, seed, offset) if 0.0 < p < 1.0 else torch.full((n, o), p < 1.0)
+    ref = R.ffn(R.d64(x), {k: R.d64(v) for k, v in w.items()}, act, R.UNIT[dtype], R.d64(res), keep, p, R.d64(dy))
+    f = api.gated_ffn(x, w, act, residual=res, p=p, seed=seed, offset=offset, save=True)
+    check("y", f["y"], ref["y"])
+    plain = api.gated_ffn(x, w, act, residual=res, p=p, seed=seed, offset=offset)
+    assert torch.equal(plain["y"], f["y"]) and plain["saved"] is None
+    grads = api.gated_ffn_bwd(dy, x, w, act, saved=f["saved"], p=p, seed=seed, offset=offset)
+    assert set(grads) == set(w) | {"x"}
+    for k, v in grads.items():
+        check("d" + k, v, ref[k])
+    again = api.gated_ffn_bwd(dy, x, w, act, saved=None, p=p, seed=seed, offset=offset)
+    for k, v in again.items():
+        assert torch.equal(v, grads[k]), k
+    return x, w, res, dy, f, grads
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,d,h,o", [
+    (1, 1, 1, 1), (1, 8, 16, 8), (2, 7, 5, 3), (3, 64, 128, 64), (17, 59, 33, 48), (64, 96, 256, 59), (65, 40, 8, 65),
+    (127, 130, 129, 131), (128, 128, 128, 128), (129, 257, 255, 120), (300, 63, 190, 257), (1100, 72, 136, 48)])
+def test_block_sizes(api, dtype, n, d, h, o):
+    run(api, n, d, h, o, dtype, "silu", True, 0.1)
+    run(api, n, d, h, o, dtype, "gelu", False, 0.0, pad=3, skip=1)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("p", [0.0, 0.5, 1.0])
+def test_activations_and_dropout(api, act, p):
+    run(api, 70, 48, 80, 40, torch.bfloat16, act, True, p)
+    run(api, 70, 48, 80, 40, torch.float32, act, True, p)
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+def test_large_tiles_and_split_rows(api, dtype):
+    """Enough tiles for the large ones in every product; long rows for the splits."""
+    run(api, 6200, 2000, 1216, 2000, dtype, "silu", False, 0.0)
+    run(api, 9001, 24, 40, 16, dtype, "gelu", True, 0.0)
+
+
+@pytest.mark.parametrize("n", [2, 8, 16, 31, 33, 64])
+@pytest.mark.parametrize("d,h,o", [(512, 1376, 512), (1001, 333, 77)])
+def test_few_rows(api, n, d, h, o):
+    run(api, n, d, h, o, torch.float16, "silu", True, 0.1)
+    run(api, n, d, h, o, torch.bfloat16, "gelu", False, 0.0, pad=8)
+    run(api, n, d, h, o, torch.float32, "silu", True, 0.0)
+
+
+def test_no_rows(api):
+    w = weights(1, 16, 24, 8, torch.float32, True)
+    x, dy = torch.empty(0, 16, device="cuda"), torch.empty(0, 8, device="cuda")
+    f = api.gated_ffn(x, w, save=True)
+    assert f["y"].shape == (0, 8)
+    for saved in (f["saved"], None):
+        g = api.gated_ffn_bwd(dy, x, w, saved=saved)
+        assert all((v == 0).all() for v in g.values()) and g["x"].shape == (0, 16)
+
+
+def test_gradient_against_differences(api):
+    n, d, h, o = 9, 21, 34, 11
+    x, w, res, dy, f, g = run(api, n, d, h, o, torch.float32, "gelu", True, 0.0)
+    X, W, DY = R.d64(x), {k: R.d64(v) for k, v in w.items()}, R.d64(dy)
+    loss = lambda X, W: (R.ffn(X, W, "gelu", 0.0)["y"][0] * DY).sum().item()
+    gen = torch.Generator().manual_seed(3)
+    for _ in range(4):
+        vx = torch.randn(X.shape, generator=gen, dtype=R.F64)
+        vw = {k: torch.randn(v.shape, generator=gen, dtype=R.F64) for k, v in W.items()}
+        e = 1e-5
+        diff = (loss(X + e * vx, {k: W[k] + e * vw[k] for k in W}) -
+                loss(X - e * vx, {k: W[k] - e * vw[k] for k in W})) / (2 * e)
+        terms = [R.d64(g["x"]) * vx] + [R.d64(g[k]) * vw[k] for k in W]
+        along, size = sum(t.sum().item() for t in terms), sum(t.abs().sum().item() for t in terms)
+        assert abs(diff - along) <= 1e-5 * size, (diff, along)
+
+
+def test_mask_is_dropouts_own(api):
+    """The block's dropout is api.dropout of its output."""
+    n, d, h, o = 200, 64, 96, 50
+    w, x = weights(4, d, h, o, torch.float32, True), rand(1, n, d, torch.float32)
+    y = api.gated_ffn(x, w)["y"]
+    z = api.gated_ffn(x, w, p=0.4, seed=(1 << 60) + 3, offset=(1 << 40) + 1)["y"]
+    assert torch.equal(z, api.dropout(y, 0.4, (1 << 60) + 3, (1 << 40) + 1))
+
+
+@pytest.mark.parametrize("shape", [(40, 24, 64, 24), (40, 24, 64, 30), (3, 256, 512, 256), (2500, 64, 128, 64)])
+def test_bad_rows_stay_in_their_rows(api, shape):
+    n, d, h, o = shape
+    for dtype in (torch.float32, torch.bfloat16):
+        w, x = weights(4, d, h, o, dtype, True), rand(1, n, d, dtype)
+        clean = api.gated_ffn(x, w)["y"].clone()
+        bad = x.clone()
+        bad[1, 3], bad[n - 1, d - 1] = float("nan"), float("inf")
+        y = api.gated_ffn(bad, w)["y"]
+        keep = torch.ones(n, dtype=torch.bool)
+        keep[[1, n - 1]] = False
+        assert torch.equal(y[keep], clean[keep])
+        assert y[1].isnan().all() and not y[n - 1].isfinite().all()
+
+
+def test_outputs_leave_their_surroundings(api):
+    """Rows written into a wider array leave the columns beside them alone; the
+    residual may be written over."""
+    n, d, h, o = 77, 40, 72, 37
+    for dtype in DT:
+        w, x = weights(4, d, h, o, dtype, True), rand(1, n, d, dtype)
+        wide = torch.full((n, o + 9), 7.0, dtype=dtype, device="cuda")
+        y = api.gated_ffn(x, w, out=wide[:, 4:4 + o])["y"]
+        assert (wide[:, :4] == 7).all() and (wide[:, 4 + o:] == 7).all()
+        assert torch.equal(y, api.gated_ffn(x, w)["y"])
+        res = rand(2, n, o, dtype)
+        want = api.gated_ffn(x, w, residual=res, p=0.3, seed=1)["y"]
+        api.gated_ffn(x, w, residual=res, p=0.3, seed=1, out=res)
+        assert torch.equal(res, want)
+        dx = torch.full((n, d + 5), 7.0, dtype=dtype, device="cuda")
+        api.gated_ffn_bwd(res, x, w, grads=dict(x=dx[:, 2:2 + d]))
+        assert (dx[:, :2] == 7).all() and (dx[:, 2 + d:] == 7).all()
+
+
+def test_partial_gradients(api):
+    n, d, h, o = 90, 40, 72, 24
+    w, x, dy = weights(4, d, h, o, torch.bfloat16, True), rand(1, n, d, torch.bfloat16), rand(2, n, o, torch.bfloat16)
+    full = api.gated_ffn_bwd(dy, x, w)
+    for keys in (["x"], ["w_gate"], ["w_up"], ["w_down"], ["b_gate"], ["b_up"], ["b_down"], ["w_up", "b_gate"], []):
+        some = {k: torch.empty_like(full[k]) for k in keys}
+        api.gated_ffn_bwd(dy, x, w, grads=some)
+        assert all(torch.equal(some[k], full[k]) for k in keys), keys
+
+
+def test_on_a_side_stream_and_in_a_graph(api):
+    n, d, h, o = 600, 64, 128, 64
+    w, x = weights(4, d, h, o, torch.bfloat16, True), rand(1, n, d, torch.bfloat16)
+    dy = rand(2, n, o, torch.bfloat16)
+
+    def step():
+        f = api.gated_ffn(x, w, p=0.2, seed=1, save=True)
+        return {"y": f["y"], **api.gated_ffn_bwd(dy, x, w, saved=f["saved"], p=0.2, seed=1)}
+
+    ref = step()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        out = step()
+    s.synchronize()
+    assert all(torch.equal(out[k], ref[k]) for k in ref)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for i in range(3):
+        x.copy_(rand(20 + i, n, d, torch.bfloat16))
+        want = {k: v.clone() for k, v in step().items()}
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[k], want[k]) for k in want), i
+
+
+def test_refusals(api):
+    n, d, h, o = 8, 16, 24, 12
+    w, x = weights(4, d, h, o, torch.float32, True), rand(1, n, d, torch.float32)
+    dy = rand(2, n, o, torch.float32)
+    saved = api.gated_ffn(x, w, save=True)["saved"]
+    without = lambda k: {a: b for a, b in w.items() if a != k}
+    bad = [
+        lambda: api.gated_ffn(x.cpu(), w),
+        lambda: api.gated_ffn(x.t(), w),
+        lambda: api.gated_ffn(x[:, :8], w),
+        lambda: api.gated_ffn(x, without("w_up")),
+        lambda: api.gated_ffn(x, {**w, "w_up": w["w_up"][:8]}),
+        lambda: api.gated_ffn(x, {**w, "w_down": w["w_down"].half()}),
+        lambda: api.gated_ffn(x, {**w, "w_down": w["w_down"].t()}),
+        lambda: api.gated_ffn(x, {**w, "b_up": w["b_up"][:4]}),
+        lambda: api.gated_ffn(x, {**w, "gain": w["b_up"]}),
+        lambda: api.gated_ffn(x, w, act="tanh"),
+        lambda: api.gated_ffn(x, w, p=2.0),
+        lambda: api.gated_ffn(x, w, residual=x),
+        lambda: api.gated_ffn(x, w, out=torch.empty(n, o, device="cuda").half()),
+        lambda: api.gated_ffn(x, w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")),
+        lambda: api.gated_ffn_bwd(dy[:, :4], x, w),
+        lambda: api.gated_ffn_bwd(dy.half(), x, w),
+        lambda: api.gated_ffn_bwd(dy, x, w, saved={k: v[:4] for k, v in saved.items()}),
+        lambda: api.gated_ffn_bwd(dy, x, w, saved={k: v.half() for k, v in saved.items()}),
+        lambda: api.gated_ffn_bwd(dy, x, w, grads=dict(w_up=torch.empty(h, d + 1, device="cuda"))),
+        lambda: api.gated_ffn_bwd(dy, x, w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, api.AbcdError)):
+            call()
+            print("not refused:", i)
