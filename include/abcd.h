@@ -458,8 +458,8 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
  * NULL (0). Dropout as in abcd_dropout over y's n rows (p = 0: none). act:
  * ABCD_ACT_SILU g sigmoid(g), ABCD_ACT_GELU g Phi(g) (Phi the normal distribution,
  * by the error function), ABCD_ACT_RELU max(g, 0). Products and act are computed
- * in fp32; the pre-activations, h and the gradients that reach them are rounded
- * to dtype where they are stored between products. */
+ * in fp32; h, its derivatives by the pre-activations and the gradients that
+ * reach these are rounded to dtype where they are stored between products. */
 enum { ABCD_ACT_SILU = 0, ABCD_ACT_GELU = 1, ABCD_ACT_RELU = 2 };
 typedef struct abcd_ffn {
   int32_t dtype, act;
@@ -470,28 +470,29 @@ typedef struct abcd_ffn {
   uint64_t seed, offset;
 } abcd_ffn;
 
-/* Forward. residual (may be NULL) and y: [n][o], y may be residual itself. gate,
- * up, hidden: all NULL, or arrays [n][(h + 7) / 8 * 8] of dtype, 16-byte aligned,
- * that receive the pre-activations and h for the backward (columns past h: zeros).
- * workspace: at least abcd_gated_ffn_workspace_size(ffn, n, saved) bytes (saved: 1
- * if gate, up and hidden are given, else 0), 256-byte aligned. */
+/* Forward. residual (may be NULL) and y: [n][o], y may be residual itself. by_gate,
+ * by_up, hidden: all NULL, or arrays [n][(h + 7) / 8 * 8] of dtype, 16-byte
+ * aligned, that receive for the backward h's derivatives by the two
+ * pre-activations and h itself (columns past h: zeros). workspace: at least
+ * abcd_gated_ffn_workspace_size(ffn, n, saved) bytes (saved: 1 if by_gate, by_up
+ * and hidden are given, else 0), 256-byte aligned. */
 ABCD_API int32_t abcd_gated_ffn_workspace_size(const abcd_ffn* ffn /* host */, int64_t n,
                                                int32_t saved, size_t* bytes);
 ABCD_API int32_t abcd_gated_ffn(const abcd_ffn* ffn /* host */, int64_t n, const void* x,
                                 int64_t ldx, const void* residual, int64_t ldr, void* y,
-                                int64_t ldy, void* gate, void* up, void* hidden, void* workspace,
+                                int64_t ldy, void* by_gate, void* by_up, void* hidden, void* workspace,
                                 size_t ws_bytes, hipStream_t stream);
 
 /* Backward: gradients of x (not counting the residual path, whose gradient is dy
  * itself) and of every weight and bias, written, of dtype, laid out as what they
- * belong to; each may be NULL, then not computed. gate, up, hidden: the forward's,
- * or all NULL: then they are computed again from x (one product more, and no
+ * belong to; each may be NULL, then not computed. by_gate, by_up, hidden: the
+ * forward's, or all NULL: then they are computed again from x (one product more, and no
  * memory held between the passes). p, seed and offset are the forward's. */
 ABCD_API int32_t abcd_gated_ffn_bwd_workspace_size(const abcd_ffn* ffn /* host */, int64_t n,
                                                    int32_t saved, size_t* bytes);
 ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, const void* dy,
-                                    int64_t lddy, const void* x, int64_t ldx, const void* gate,
-                                    const void* up, const void* hidden, void* dx, int64_t lddx,
+                                    int64_t lddy, const void* x, int64_t ldx, const void* by_gate,
+                                    const void* by_up, const void* hidden, void* dx, int64_t lddx,
                                     void* dw_gate, void* dw_up, void* dw_down, void* db_gate,
                                     void* db_up, void* db_down, void* workspace, size_t ws_bytes,
                                     hipStream_t stream);

@@ -493,6 +493,7 @@ def dropout_bwd(dy, p, seed, offset=0, out=None):
 _ACTS = {"silu": 0, "gelu": 1, "relu": 2}  # ABCD_ACT_*
 FFN_WEIGHTS = ("w_gate", "w_up", "w_down")
 FFN_BIASES = ("b_gate", "b_up", "b_down")
+FFN_SAVED = ("by_gate", "by_up", "hidden")
 
 
 def _ffn(x, params, act, p, seed, offset):
@@ -530,11 +531,11 @@ def _ffn(x, params, act, p, seed, offset):
 
 
 def _saved_ptrs(saved, n, h, like):
-    """gate, up, hidden of a forward that kept them."""
+    """What a forward kept: h's derivatives by the pre-activations, and h."""
     if saved is None:
         return [None] * 3
     out = []
-    for k in ("gate", "up", "hidden"):
+    for k in FFN_SAVED:
         t = saved[k]
         if t.dtype != like.dtype or t.device != like.device or not t.is_contiguous() \
                 or tuple(t.shape) != (n, (h + 7) // 8 * 8):
@@ -563,7 +564,7 @@ def gated_ffn(x, params, act="silu", residual=None, p=0.0, seed=0, offset=0, sav
     saved = None
     if save:
         hp = (f.h + 7) // 8 * 8
-        saved = {k: torch.empty((n, hp), dtype=x.dtype, device=dev) for k in ("gate", "up", "hidden")}
+        saved = {k: torch.empty((n, hp), dtype=x.dtype, device=dev) for k in FFN_SAVED}
     lib = _lib.load()
     sz = C.c_size_t(0)
     check(lib.abcd_gated_ffn_workspace_size(C.byref(f), n, 1 if save else 0, C.byref(sz)))

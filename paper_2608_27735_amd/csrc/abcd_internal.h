@@ -364,10 +364,10 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
 // gated_ffn.hip
 size_t gated_ffn_workspace_bytes(const abcd_ffn& f, int64_t n, bool saved, bool backward);
 int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx,
-                         const void* residual, int64_t ldr, void* y, int64_t ldy, void* gate,
-                         void* up, void* hidden, void* workspace, hipStream_t stream);
+                         const void* residual, int64_t ldr, void* y, int64_t ldy, void* by_gate,
+                         void* by_up, void* hidden, void* workspace, hipStream_t stream);
 int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64_t lddy,
-                             const void* x, int64_t ldx, const void* gate, const void* up,
+                             const void* x, int64_t ldx, const void* by_gate, const void* by_up,
                              const void* hidden, void* dx, int64_t lddx, void* dw_gate,
                              void* dw_up, void* dw_down, void* db_gate, void* db_up, void* db_down,
                              void* workspace, hipStream_t stream);

@@ -65,11 +65,11 @@ int32_t check_ffn_weights(const abcd_ffn& f) {
   return check_vector("b_down", f.b_down, f.dtype);
 }
 
-int32_t check_saved(const void* gate, const void* up, const void* hidden) {
-  REQUIRE((gate == nullptr) == (up == nullptr) && (up == nullptr) == (hidden == nullptr),
-          "gate, up and hidden go together");
-  for (const void* p : {gate, up, hidden})
-    REQUIRE((reinterpret_cast<uintptr_t>(p) & 15) == 0, "gate, up and hidden must be 16-byte aligned");
+int32_t check_saved(const void* by_gate, const void* by_up, const void* hidden) {
+  REQUIRE((by_gate == nullptr) == (by_up == nullptr) && (by_up == nullptr) == (hidden == nullptr),
+          "by_gate, by_up and hidden go together");
+  for (const void* p : {by_gate, by_up, hidden})
+    REQUIRE((reinterpret_cast<uintptr_t>(p) & 15) == 0, "by_gate, by_up and hidden must be 16-byte aligned");
   return ABCD_OK;
 }
 
@@ -92,7 +92,7 @@ int32_t abcd_gated_ffn_bwd_workspace_size(const abcd_ffn* ffn, int64_t n, int32_
 }
 
 int32_t abcd_gated_ffn(const abcd_ffn* ffn, int64_t n, const void* x, int64_t ldx, const void* residual, int64_t ldr,
-                       void* y, int64_t ldy, void* gate, void* up, void* hidden, void* workspace, size_t ws_bytes,
+                       void* y, int64_t ldy, void* by_gate, void* by_up, void* hidden, void* workspace, size_t ws_bytes,
                        hipStream_t stream) {
   TRY_STATUS(check_ffn(ffn, n));
   const abcd_ffn& f = *ffn;
@@ -100,14 +100,14 @@ int32_t abcd_gated_ffn(const abcd_ffn* ffn, int64_t n, const void* x, int64_t ld
   TRY_STATUS(check_matrix("x", x, f.dtype, n, f.d, ldx, false));
   TRY_STATUS(check_matrix("residual", residual, f.dtype, n, f.o, ldr, true));
   TRY_STATUS(check_matrix("y", y, f.dtype, n, f.o, ldy, false));
-  TRY_STATUS(check_saved(gate, up, hidden));
+  TRY_STATUS(check_saved(by_gate, by_up, hidden));
   if (n > 0)
     TRY_STATUS(check_workspace(workspace, ws_bytes, gated_ffn_workspace_bytes(f, n, hidden != nullptr, false)));
-  return launch_gated_ffn(f, n, x, ldx, residual, ldr, y, ldy, gate, up, hidden, workspace, stream);
+  return launch_gated_ffn(f, n, x, ldx, residual, ldr, y, ldy, by_gate, by_up, hidden, workspace, stream);
 }
 
 int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn, int64_t n, const void* dy, int64_t lddy, const void* x, int64_t ldx,
-                           const void* gate, const void* up, const void* hidden, void* dx, int64_t lddx,
+                           const void* by_gate, const void* by_up, const void* hidden, void* dx, int64_t lddx,
                            void* dw_gate, void* dw_up, void* dw_down, void* db_gate, void* db_up, void* db_down,
                            void* workspace, size_t ws_bytes, hipStream_t stream) {
   TRY_STATUS(check_ffn(ffn, n));
@@ -116,11 +116,11 @@ int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn, int64_t n, const void* dy, int64
   TRY_STATUS(check_matrix("dy", dy, f.dtype, n, f.o, lddy, false));
   TRY_STATUS(check_matrix("x", x, f.dtype, n, f.d, ldx, false));
   TRY_STATUS(check_matrix("dx", dx, f.dtype, n, f.d, lddx, true));
-  TRY_STATUS(check_saved(gate, up, hidden));
+  TRY_STATUS(check_saved(by_gate, by_up, hidden));
   for (const void* g : {dw_gate, dw_up, dw_down, db_gate, db_up, db_down})
     TRY_STATUS(check_vector("a gradient", g, f.dtype));
   TRY_STATUS(check_workspace(workspace, ws_bytes, gated_ffn_workspace_bytes(f, n, hidden != nullptr, true)));
-  return launch_gated_ffn_bwd(f, n, dy, lddy, x, ldx, gate, up, hidden, dx, lddx, dw_gate, dw_up, dw_down, db_gate,
+  return launch_gated_ffn_bwd(f, n, dy, lddy, x, ldx, by_gate, by_up, hidden, dx, lddx, dw_gate, dw_up, dw_down, db_gate,
                               db_up, db_down, workspace, stream);
 }
 

@@ -8,11 +8,14 @@
 //   dWg = dg' x, dWu = du' x, dWd = dz' h, and the biases' gradients the column sums.
 // Five products: both projections in one (a tile holds the same columns of g and
 // of u, so h is made from the accumulators), the down projection, dh (whose
-// accumulators become dg and du with g and u read back), dx as one product of
-// twice the contraction, and the weights' gradients, split along the rows where
-// the result has too few tiles to fill the GPU. Products accumulate in fp32; g, u,
-// h, dg and du are rounded to the element type between the launches, as the
-// matrix cores read them, and everything else is rounded once.
+// accumulators become dg and du by h's derivatives, which the forward kept), dx as
+// one product of twice the contraction, and the weights' gradients, split along
+// the rows where the result has too few tiles to fill the GPU. Products accumulate
+// in fp32. Between the launches h, dg and du are rounded to the element type, as
+// the matrix cores read them, and so are dh/dg = u a'(g) and dh/du = a(g): kept in
+// place of g and u they cost as much memory, dg and du take one rounding from each
+// instead of two or three, and the backward evaluates no activation. dz is dy with
+// zeros, exact; its factor 1 / (1 - p) is applied to the products' fp32 sums.
 #pragma once
 
 #include <algorithm>
@@ -28,13 +31,8 @@ __device__ __forceinline__ float sigmoid(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * g));
 }
 
-// a(g) and, where it is wanted, a'(g). The activation is the same for every lane.
-__device__ __forceinline__ float activate(float g, int act) {
-  if (act == ABCD_ACT_SILU) return g * sigmoid(g);
-  if (act == ABCD_ACT_GELU) return g * (0.5f + 0.5f * erff(0.70710678118654752f * g));
-  return fmaxf(g, 0.0f);
-}
-__device__ __forceinline__ float activate_grad(float g, int act, float& slope) {
+// a(g) and a'(g). The activation is the same for every lane.
+__device__ __forceinline__ float activate(float g, int act, float& slope) {
   if (act == ABCD_ACT_SILU) {
     const float s = sigmoid(g);
     slope = s * (1.0f + g * (1.0f - s));
@@ -94,17 +92,20 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn 
       __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
       const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
       if (r >= a.x.len) continue;
-      f32x4 g = p.acc[x][w] + bg, u = p.acc[x][w + P::FW / 2] + bu, h;
+      f32x4 g = p.acc[x][w] + bg, u = p.acc[x][w + P::FW / 2] + bu, h, hg, hu;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
-        h[i] = activate(g[i], a.act) * u[i];
+        float slope;
+        hu[i] = activate(g[i], a.act, slope);
+        h[i] = hu[i] * u[i];
+        hg[i] = slope * u[i];
       }
       const int64_t at = r * a.ldh + c;
       store_vec<T, 4, true>(static_cast<T*>(a.hidden) + at, h, 4);
-      if (a.gate) {
-        store_vec<T, 4, true>(static_cast<T*>(a.gate) + at, g, 4);
-        store_vec<T, 4, true>(static_cast<T*>(a.up) + at, u, 4);
+      if (a.by_gate) {
+        store_vec<T, 4, true>(static_cast<T*>(a.by_gate) + at, hg, 4);
+        store_vec<T, 4, true>(static_cast<T*>(a.by_up) + at, hu, 4);
       }
     }
   }
@@ -158,16 +159,15 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dhidden_kernel(F
       const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
       if (r >= a.dz.len) continue;
       const int64_t at = r * a.ldh + c;
-      const f32x4 g = load_vec<T, 4, true>(static_cast<const T*>(a.gate) + at, 4);
-      const f32x4 u = load_vec<T, 4, true>(static_cast<const T*>(a.up) + at, 4);
+      const f32x4 hg = load_vec<T, 4, true>(static_cast<const T*>(a.by_gate) + at, 4);
+      const f32x4 hu = load_vec<T, 4, true>(static_cast<const T*>(a.by_up) + at, 4);
       f32x4 dg, du;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float slope;
-        const float v = activate_grad(g[i], a.act, slope), dh = p.acc[x][w][i];
+        const float dh = p.acc[x][w][i] * a.scale;
         const bool in = c + i < a.h;
-        dg[i] = in ? dh * u[i] * slope : 0.0f;
-        du[i] = in ? dh * v : 0.0f;
+        dg[i] = in ? dh * hg[i] : 0.0f;
+        du[i] = in ? dh * hu[i] : 0.0f;
       }
       store_vec<T, 4, true>(static_cast<T*>(a.dgate) + at, dg, 4);
       store_vec<T, 4, true>(static_cast<T*>(a.dup) + at, du, 4);
@@ -227,9 +227,10 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dweight_kernel(F
       const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
       if (r >= rows) continue;
       if (a.part)
-        store_vec<float, 4, false>(a.part + ((blockIdx.y * a.halves + half) * rows + r) * cols + c, p.acc[x][w], m);
+        store_vec<float, 4, false>(a.part + ((blockIdx.y * a.halves + half) * rows + r) * cols + c, p.acc[x][w] * a.scale,
+                                   m);
       else
-        store_vec<T, 4, false>(static_cast<T*>(half ? a.out1 : a.out0) + r * cols + c, p.acc[x][w], m);
+        store_vec<T, 4, false>(static_cast<T*>(half ? a.out1 : a.out0) + r * cols + c, p.acc[x][w] * a.scale, m);
     }
   }
 }

@@ -34,11 +34,12 @@ __global__ __launch_bounds__(kBlock) void pack_rows_kernel(PackArgs a) {
   }
 }
 
-// part[blockIdx.y][c] = sum over rows blockIdx.y, + gridDim.y rows.. of m[row][c].
+// part[blockIdx.y][c] = sum over rows blockIdx.y, + gridDim.y rows.. of m[row][c],
+// times scale.
 // `lanes` threads along a row, the workgroup's other threads on other rows.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void column_sums_kernel(const void* m, int64_t ld, int64_t n, int cols,
-                                                             int lanes, float* part) {
+                                                             int lanes, float scale, float* part) {
   constexpr int N = kPer16<T>;
   __shared__ float red[kBlock * N];
   const int t = threadIdx.x & (lanes - 1), rows = kBlock / lanes;
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(kBlock) void column_sums_kernel(const void* m, int6
     if (at >= cols) break;
     float v = 0.0f;
     for (int r = 0; r < rows; ++r) v += red[r * lanes * N + i];
-    part[(int64_t)blockIdx.y * cols + at] = v;
+    part[(int64_t)blockIdx.y * cols + at] = v * scale;
   }
 }
 
@@ -80,15 +81,15 @@ int32_t pack(int32_t dtype, int64_t n, int64_t cols, const void* src, int64_t ld
   });
 }
 
-// out[c] = sum over the rows of m, rounded to dtype.
-int32_t column_sums(int32_t dtype, int64_t n, int64_t cols, const void* m, int64_t ld, void* out, float* part,
-                    hipStream_t stream) {
+// out[c] = scale times the sum over the rows of m, rounded to dtype.
+int32_t column_sums(int32_t dtype, int64_t n, int64_t cols, const void* m, int64_t ld, float scale, void* out,
+                    float* part, hipStream_t stream) {
   const int64_t parts = sum_parts_of(n);
   TRY_STATUS(with_type(dtype, [&](auto z) -> int32_t {
     typedef decltype(z) T;
     const int nvec = (int)((cols + kPer16<T> - 1) / kPer16<T>), lanes = std::min(lanes_for(nvec), 64);
     ABCD_LAUNCH("column_sums", (column_sums_kernel<T>), dim3((nvec + lanes - 1) / lanes, parts), kBlock, 0, stream,
-                m, ld, n, (int)cols, lanes, part);
+                m, ld, n, (int)cols, lanes, scale, part);
     ABCD_HIP(hipGetLastError());
     return ABCD_OK;
   }));
@@ -196,7 +197,7 @@ size_t gated_ffn_workspace_bytes(const abcd_ffn& f, int64_t n, bool saved, bool 
 }
 
 int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx, const void* residual,
-                         int64_t ldr, void* y, int64_t ldy, void* gate, void* up, void* hidden, void* workspace,
+                         int64_t ldr, void* y, int64_t ldy, void* by_gate, void* by_up, void* hidden, void* workspace,
                          hipStream_t stream) {
   if (n == 0) return ABCD_OK;
   const Scratch s = layout(f, n, hidden != nullptr, false, workspace);
@@ -205,7 +206,7 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
   Side xs, w;
   TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
   TRY_STATUS(gate_up(f, s, w, stream));
-  const FfnIn in{xs, w, f.b_gate, f.b_up, hidden, gate, up, f.d, f.h, hp, f.act, 0, 0};
+  const FfnIn in{xs, w, f.b_gate, f.b_up, hidden, by_gate, by_up, f.d, f.h, hp, f.act, 0, 0};
   TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
   TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, w, stream));
   const FfnOut out{Side{{hidden, nullptr}, hp, n}, w, f.b_down, residual, y, f.h, f.o, ldr, ldy,
@@ -214,11 +215,16 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
 }
 
 int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64_t lddy, const void* x,
-                             int64_t ldx, const void* gate, const void* up, const void* hidden, void* dx,
+                             int64_t ldx, const void* by_gate, const void* by_up, const void* hidden, void* dx,
                              int64_t lddx, void* dw_gate, void* dw_up, void* dw_down, void* db_gate, void* db_up,
                              void* db_down, void* workspace, hipStream_t stream) {
   const Scratch s = layout(f, n, hidden != nullptr, true, workspace);
   const int64_t hp = up8(f.h);
+  // dz is dy with zeros where the forward dropped; the factor of what is kept
+  // multiplies the sums that dz enters
+  DropKey mask = drop_key(f.p, f.seed, f.offset);
+  const float scale = mask.scale;
+  mask.scale = 1.0f;
   Side xs{}, wgu{}, wd{}, dz{};
   if (n > 0) {
     TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
@@ -226,22 +232,22 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, wd, stream));
     if (f.p > 0.0) {
       dz = Side{{s.dz, nullptr}, up8(f.o), n};
-      TRY_STATUS(pack(f.dtype, n, f.o, dy, lddy, s.dz, dz.ld, drop_key(f.p, f.seed, f.offset), stream));
+      TRY_STATUS(pack(f.dtype, n, f.o, dy, lddy, s.dz, dz.ld, mask, stream));
     } else {
       TRY_STATUS(rows_of(f, dy, n, f.o, lddy, s.dz, dz, stream));
     }
     if (!hidden) {
       const FfnIn in{xs, wgu, f.b_gate, f.b_up, s.hidden, s.gate, s.up, f.d, f.h, hp, f.act, 0, 0};
       TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
-      gate = s.gate;
-      up = s.up;
+      by_gate = s.gate;
+      by_up = s.up;
       hidden = s.hidden;
     }
   }
   // W side across: its index is h, the contraction o
   const bool inner = dx || dw_gate || dw_up || db_gate || db_up;
   if (n > 0 && inner) {
-    const FfnDHidden dh{dz, Side{{wd.p[0], nullptr}, wd.ld, f.h}, gate, up, s.gate, s.up, f.o, f.h, hp, f.act, 0, 0};
+    const FfnDHidden dh{dz, Side{{wd.p[0], nullptr}, wd.ld, f.h}, by_gate, by_up, s.gate, s.up, f.o, f.h, hp, scale, 0, 0};
     TRY_STATUS(FFN_BY_TYPE(f, ffn_dhidden, dh, stream));
   }
   const Side dgu{{s.gate, s.up}, hp, n};
@@ -249,9 +255,9 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     const FfnDX a{dgu, Side{{wgu.p[0], wgu.p[1]}, wgu.ld, f.d}, dx, f.h, f.d, lddx, 0, 0};
     TRY_STATUS(FFN_BY_TYPE(f, ffn_dx, a, stream));
   }
-  auto dweight = [&](Side X, Side W, int halves, void* out0, void* out1, int splits) -> int32_t {
+  auto dweight = [&](Side X, Side W, int halves, void* out0, void* out1, int splits, float factor) -> int32_t {
     const int64_t rows = (n + splits - 1) / splits, per = (rows + 63) / 64 * 64;
-    FfnDWeight a{X, W, out0, out1, splits > 1 ? s.part : nullptr, n, per, halves, 0, 0};
+    FfnDWeight a{X, W, out0, out1, splits > 1 ? s.part : nullptr, factor, n, per, halves, 0, 0};
     TRY_STATUS(FFN_BY_TYPE(f, ffn_dweight, a, splits, stream));
     if (splits > 1)
       return launch_sum_parts(s.part, splits, halves * X.len * W.len, X.len * W.len, f.dtype, out0, out1, stream);
@@ -261,14 +267,14 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     Side X{{dw_gate ? s.gate : s.up, s.up}, hp, f.h};
     const int halves = dw_gate && dw_up ? 2 : 1;
     TRY_STATUS(dweight(X, Side{{xs.p[0], nullptr}, xs.ld, f.d}, halves, dw_gate ? dw_gate : dw_up, dw_up,
-                       splits_gate_up(f, n)));
+                       splits_gate_up(f, n), 1.0f));
   }
   if (dw_down)
     TRY_STATUS(dweight(Side{{dz.p[0], nullptr}, dz.ld, f.o}, Side{{hidden, nullptr}, hp, f.h}, 1, dw_down, nullptr,
-                       splits_down(f, n)));
-  if (db_gate) TRY_STATUS(column_sums(f.dtype, n, f.h, s.gate, hp, db_gate, s.part, stream));
-  if (db_up) TRY_STATUS(column_sums(f.dtype, n, f.h, s.up, hp, db_up, s.part, stream));
-  if (db_down) TRY_STATUS(column_sums(f.dtype, n, f.o, dz.p[0], dz.ld, db_down, s.part, stream));
+                       splits_down(f, n), scale));
+  if (db_gate) TRY_STATUS(column_sums(f.dtype, n, f.h, s.gate, hp, 1.0f, db_gate, s.part, stream));
+  if (db_up) TRY_STATUS(column_sums(f.dtype, n, f.h, s.up, hp, 1.0f, db_up, s.part, stream));
+  if (db_down) TRY_STATUS(column_sums(f.dtype, n, f.o, dz.p[0], dz.ld, scale, db_down, s.part, stream));
   return ABCD_OK;
 }
 

@@ -15,14 +15,15 @@ struct Side {
   int64_t len;  // of the index that is not contracted (of each half)
 };
 
-// hidden, gate and up: [n][ldh], columns [h, ldh) zero; gate NULL: only hidden
+// hidden and its derivatives by gate and up: [n][ldh], columns [h, ldh) zero;
+// by_gate NULL: only hidden
 struct FfnIn {
   Side x, w;
   const void* bg;
   const void* bu;
   void* hidden;
-  void* gate;
-  void* up;
+  void* by_gate;
+  void* by_up;
   int64_t d, h, ldh;
   int act, tiles_x, tiles_w;
 };
@@ -35,14 +36,16 @@ struct FfnOut {
   DropKey key;
   int tiles_x, tiles_w;
 };
+// dgate and dup may be by_gate and by_up themselves
 struct FfnDHidden {
   Side dz, w;
-  const void* gate;
-  const void* up;
-  void* dgate;  // may be gate and up themselves
+  const void* by_gate;
+  const void* by_up;
+  void* dgate;
   void* dup;
   int64_t o, h, ldh;
-  int act, tiles_x, tiles_w;
+  float scale;  // of dz
+  int tiles_x, tiles_w;
 };
 struct FfnDX {
   Side dgu, w;
@@ -57,6 +60,7 @@ struct FfnDWeight {
   void* out0;
   void* out1;
   float* part;
+  float scale;  // of the sums
   int64_t n, per;
   int halves, tiles_x, tiles_w;
 };
