@@ -470,6 +470,11 @@ typedef struct abcd_ffn {
   uint64_t seed, offset;
 } abcd_ffn;
 
+/* *keeps = 1 if a training step does best to let the forward keep by_gate, by_up and
+ * hidden for the backward, 0 if the backward makes them again faster than it would
+ * read them (narrow blocks of many rows). Either way both are correct. */
+ABCD_API int32_t abcd_gated_ffn_keeps(const abcd_ffn* ffn /* host */, int64_t n, int32_t* keeps);
+
 /* Forward. residual (may be NULL) and y: [n][o], y may be residual itself. by_gate,
  * by_up, hidden: all NULL, or arrays [n][(h + 7) / 8 * 8] of dtype, 16-byte
  * aligned, that receive for the backward h's derivatives by the two
@@ -508,7 +513,7 @@ ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, c
  * render_fwd, loss_l1, zero_fill, bwd_order, render_bwd, project_bwd, adam,
  * render_cache, cache_rect_init, layer_norm, layer_norm_bwd, layer_norm_cols,
  * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
- * ffn_dweight). */
+ * ffn_dweight, ffn_narrow, ffn_narrow_bwd). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

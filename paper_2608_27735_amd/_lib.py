@@ -83,6 +83,7 @@ SIGNATURES = {
                                    _P, _I64, _P, _P, _P, _SZ, _P]),
     "abcd_dropout": (_I32, [_I32, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, C.c_double, C.c_uint64,
                             C.c_uint64, _P]),
+    "abcd_gated_ffn_keeps": (_I32, [_FFN, _I64, C.POINTER(_I32)]),
     "abcd_gated_ffn_workspace_size": (_I32, [_FFN, _I64, _I32, C.POINTER(_SZ)]),
     "abcd_gated_ffn_bwd_workspace_size": (_I32, [_FFN, _I64, _I32, C.POINTER(_SZ)]),
     "abcd_gated_ffn": (_I32, [_FFN, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _SZ, _P]),

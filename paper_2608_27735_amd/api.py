@@ -553,19 +553,24 @@ def gated_ffn(x, params, act="silu", residual=None, p=0.0, seed=0, offset=0, sav
     w_up [h, d], w_down [o, h][, b_gate [h], b_up [h], b_down [o]]) of x's type.
     act: "silu", "gelu" or "relu". Dropout as in dropout().
 
-    Returns dict(y [n, o], saved): with save=True what gated_ffn_bwd needs of
-    this pass, else None (it computes that again). out may be residual."""
+    Returns dict(y [n, o], saved): with save=True what gated_ffn_bwd takes of
+    this pass, else None; None too where the backward makes it again faster than
+    it would read it (narrow blocks of many rows). out may be residual."""
     f, ldx = _ffn(x, params, act, p, seed, offset)
     n, dev = x.shape[0], x.device
     ldr = 0 if residual is None else _rows(residual, "residual", x, (n, f.o))
     if out is None:
         out = torch.empty((n, f.o), dtype=x.dtype, device=dev)
     ldy = _rows(out, "out", x, (n, f.o))
+    lib = _lib.load()
     saved = None
+    if save:
+        keeps = C.c_int32(0)
+        check(lib.abcd_gated_ffn_keeps(C.byref(f), n, C.byref(keeps)))
+        save = keeps.value != 0
     if save:
         hp = (f.h + 7) // 8 * 8
         saved = {k: torch.empty((n, hp), dtype=x.dtype, device=dev) for k in FFN_SAVED}
-    lib = _lib.load()
     sz = C.c_size_t(0)
     check(lib.abcd_gated_ffn_workspace_size(C.byref(f), n, 1 if save else 0, C.byref(sz)))
     workspace = _workspace(workspace, sz.value, dev)

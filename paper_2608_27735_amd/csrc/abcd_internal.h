@@ -362,6 +362,7 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
                               void* dx, int64_t lddx, void* dweight, void* dbias, void* workspace,
                               hipStream_t stream);
 // gated_ffn.hip
+bool gated_ffn_keeps(const abcd_ffn& f, int64_t n);
 size_t gated_ffn_workspace_bytes(const abcd_ffn& f, int64_t n, bool saved, bool backward);
 int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx,
                          const void* residual, int64_t ldr, void* y, int64_t ldy, void* by_gate,
@@ -371,9 +372,20 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
                              const void* hidden, void* dx, int64_t lddx, void* dw_gate,
                              void* dw_up, void* dw_down, void* db_gate, void* db_up, void* db_down,
                              void* workspace, hipStream_t stream);
-// reduce.hip: out0[c] = sum over p of part[p][c] for c < split, out1[c - split] for the other
-// columns, rounded to dtype; either may be NULL. No parts: zeros.
-int32_t launch_sum_parts(const float* part, int64_t parts, int64_t cols, int64_t split,
-                         int32_t dtype, void* out0, void* out1, hipStream_t stream);
+// reduce.hip: out[i][c - begin[i]] = sum over p of part[p][c], rounded to dtype, for
+// the columns c of [begin[i], begin[i + 1]); an output may be NULL. begin[count]:
+// columns of a part. No parts: zeros.
+struct SumOuts {
+  void* out[6];
+  int64_t begin[7];
+  int count;
+  void add(void* p, int64_t cols) {
+    out[count] = p;
+    begin[count + 1] = begin[count] + cols;
+    ++count;
+  }
+};
+int32_t launch_sum_parts(const float* part, int64_t parts, const SumOuts& outs, int32_t dtype,
+                         hipStream_t stream);
 
 }  // namespace abcd

@@ -77,6 +77,13 @@ int32_t check_saved(const void* by_gate, const void* by_up, const void* hidden) 
 
 extern "C" {
 
+int32_t abcd_gated_ffn_keeps(const abcd_ffn* ffn, int64_t n, int32_t* keeps) {
+  TRY_STATUS(check_ffn(ffn, n));
+  REQUIRE(keeps != nullptr, "keeps is NULL");
+  *keeps = gated_ffn_keeps(*ffn, n) ? 1 : 0;
+  return ABCD_OK;
+}
+
 int32_t abcd_gated_ffn_workspace_size(const abcd_ffn* ffn, int64_t n, int32_t saved, size_t* bytes) {
   TRY_STATUS(check_ffn(ffn, n));
   REQUIRE(bytes != nullptr, "bytes is NULL");

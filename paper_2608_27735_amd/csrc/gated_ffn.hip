@@ -93,7 +93,9 @@ int32_t column_sums(int32_t dtype, int64_t n, int64_t cols, const void* m, int64
     ABCD_HIP(hipGetLastError());
     return ABCD_OK;
   }));
-  return launch_sum_parts(part, parts, cols, cols, dtype, out, nullptr, stream);
+  SumOuts outs{};
+  outs.add(out, cols);
+  return launch_sum_parts(part, parts, outs, dtype, stream);
 }
 
 int64_t up8(int64_t v) { return (v + 7) & ~int64_t(7); }
@@ -132,11 +134,26 @@ int64_t tiles128(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((c
 int splits_gate_up(const abcd_ffn& f, int64_t n) { return splits_for(2 * tiles128(f.h, f.d), n); }
 int splits_down(const abcd_ffn& f, int64_t n) { return splits_for(tiles128(f.o, f.h), n); }
 
+// Whether the narrow kernels take the block: what they hold in registers and LDS,
+// in 16-bit types, and rows enough to share the cost of setting the weights up.
+bool narrow(const abcd_ffn& f, int64_t n) {
+  return f.dtype != ABCD_F32 && f.d <= 64 && f.o <= 64 && f.h <= 128 && n >= 1024;
+}
+constexpr int64_t kCUs = 256;
+int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 127) / 128, 3 * kCUs); }
+int64_t narrow_bwd_blocks(int64_t n) { return std::min<int64_t>((n + 63) / 64, kCUs); }
+int64_t narrow_sums(const abcd_ffn& f) { return 2 * f.h * f.d + f.o * f.h + 2 * f.h + f.o; }
+
 Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* workspace) {
   const size_t sz = type_bytes(f.dtype);
   const int64_t dp = up8(f.d), hp = up8(f.h), op = up8(f.o);
   Pieces p{static_cast<char*>(workspace)};
   Scratch s{};
+  if (!saved && narrow(f, n)) {
+    if (backward) s.part = static_cast<float*>(p.take(narrow_bwd_blocks(n) * narrow_sums(f) * sizeof(float)));
+    s.bytes = p.used;
+    return s;
+  }
   s.x = p.take(n * dp * sz);
   s.wg = p.take(f.h * dp * sz);
   s.wu = p.take(f.h * dp * sz);
@@ -192,6 +209,8 @@ int32_t gate_up(const abcd_ffn& f, const Scratch& s, Side& w, hipStream_t stream
 
 }  // namespace
 
+bool gated_ffn_keeps(const abcd_ffn& f, int64_t n) { return !narrow(f, n); }
+
 size_t gated_ffn_workspace_bytes(const abcd_ffn& f, int64_t n, bool saved, bool backward) {
   return layout(f, n, saved, backward, nullptr).bytes;
 }
@@ -200,6 +219,12 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
                          int64_t ldr, void* y, int64_t ldy, void* by_gate, void* by_up, void* hidden, void* workspace,
                          hipStream_t stream) {
   if (n == 0) return ABCD_OK;
+  if (!hidden && narrow(f, n)) {
+    const FfnNarrow a{x, f.w_gate, f.w_up, f.w_down, f.b_gate, f.b_up, f.b_down, residual, y, n, f.d, f.h, f.o,
+                      ldx, ldr, ldy, drop_key(f.p, f.seed, f.offset), f.act};
+    return f.dtype == ABCD_F16 ? ffn_narrow_f16(a, narrow_blocks(n), stream)
+                               : ffn_narrow_bf16(a, narrow_blocks(n), stream);
+  }
   const Scratch s = layout(f, n, hidden != nullptr, false, workspace);
   if (!hidden) hidden = s.hidden;
   const int64_t hp = up8(f.h);
@@ -225,6 +250,20 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
   DropKey mask = drop_key(f.p, f.seed, f.offset);
   const float scale = mask.scale;
   mask.scale = 1.0f;
+  if (!hidden && narrow(f, n)) {
+    const int64_t blocks = narrow_bwd_blocks(n);
+    const FfnNarrowBwd a{x, dy, f.w_gate, f.w_up, f.w_down, f.b_gate, f.b_up, dx, s.part, n, f.d, f.h, f.o,
+                         ldx, lddy, lddx, narrow_sums(f), mask, scale, f.act};
+    TRY_STATUS(f.dtype == ABCD_F16 ? ffn_narrow_bwd_f16(a, blocks, stream) : ffn_narrow_bwd_bf16(a, blocks, stream));
+    SumOuts outs{};
+    outs.add(dw_gate, f.h * f.d);
+    outs.add(dw_up, f.h * f.d);
+    outs.add(dw_down, f.o * f.h);
+    outs.add(db_gate, f.h);
+    outs.add(db_up, f.h);
+    outs.add(db_down, f.o);
+    return launch_sum_parts(s.part, blocks, outs, f.dtype, stream);
+  }
   Side xs{}, wgu{}, wd{}, dz{};
   if (n > 0) {
     TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
@@ -259,9 +298,11 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     const int64_t rows = (n + splits - 1) / splits, per = (rows + 63) / 64 * 64;
     FfnDWeight a{X, W, out0, out1, splits > 1 ? s.part : nullptr, factor, n, per, halves, 0, 0};
     TRY_STATUS(FFN_BY_TYPE(f, ffn_dweight, a, splits, stream));
-    if (splits > 1)
-      return launch_sum_parts(s.part, splits, halves * X.len * W.len, X.len * W.len, f.dtype, out0, out1, stream);
-    return ABCD_OK;
+    if (splits == 1) return ABCD_OK;
+    SumOuts outs{};
+    outs.add(out0, X.len * W.len);
+    if (halves == 2) outs.add(out1, X.len * W.len);
+    return launch_sum_parts(s.part, splits, outs, f.dtype, stream);
   };
   if (dw_gate || dw_up) {
     Side X{{dw_gate ? s.gate : s.up, s.up}, hp, f.h};

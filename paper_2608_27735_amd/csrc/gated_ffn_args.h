@@ -65,6 +65,30 @@ struct FfnDWeight {
   int halves, tiles_x, tiles_w;
 };
 
+// The narrow block, in one launch each way.
+struct FfnNarrow {
+  const void *x, *w_gate, *w_up, *w_down, *b_gate, *b_up, *b_down;
+  const void* res;
+  void* y;
+  int64_t n, d, h, o, ldx, ldr, ldy;
+  DropKey key;
+  int act;
+};
+// part: [workgroups][sums], the sums laid out as dWg, dWu, dWd, dbg, dbu, dbd
+struct FfnNarrowBwd {
+  const void *x, *dy, *w_gate, *w_up, *w_down, *b_gate, *b_up;
+  void* dx;  // may be NULL
+  float* part;
+  int64_t n, d, h, o, ldx, lddy, lddx, sums;
+  DropKey key;
+  float scale;  // of what the forward kept
+  int act;
+};
+int32_t ffn_narrow_f16(const FfnNarrow&, int64_t blocks, hipStream_t);
+int32_t ffn_narrow_bf16(const FfnNarrow&, int64_t blocks, hipStream_t);
+int32_t ffn_narrow_bwd_f16(const FfnNarrowBwd&, int64_t blocks, hipStream_t);
+int32_t ffn_narrow_bwd_bf16(const FfnNarrowBwd&, int64_t blocks, hipStream_t);
+
 #define ABCD_FFN_DECLARE(NAME)                                 \
   int32_t ffn_in_##NAME(const FfnIn&, hipStream_t);            \
   int32_t ffn_out_##NAME(const FfnOut&, hipStream_t);          \

@@ -1,0 +1,444 @@
+// gated_ffn_narrow.h -- the gated feed-forward block of many narrow rows (one per
+// Gaussian), forward and backward in one launch each, for 16-bit element types.
+//
+// With d and o of a few dozen the products' results outweigh their inputs: h and
+// its derivatives alone would be written and read several times what x and y
+// take. Here nothing but x, dy, y and dx passes through memory. The matrix
+// instruction's result serves as the next one's operand without leaving the
+// registers: a lane of a 16 x 16 result holds four consecutive indexes of one side
+// and one of the other, so two results side by side are eight indexes of a
+// contraction of 32, in an order that the other operand is laid out to match.
+//
+// Forward: a wave takes kRowFrags x 16 rows at a time; weights lie in LDS in
+// fragment order, loaded once per workgroup, and for every 32 columns of h the
+// wave makes g and u, h from them, and adds h's part of y.
+//
+// Backward: a workgroup takes 64 rows at a time, and each of its 8 waves kHB x 16
+// columns of h for all of them, so that its part of the weights stays in its
+// registers, and so do its parts of dWg, dWu and dWd over all rows that the
+// workgroup takes. g, u, dh, dg, du and h are made again in registers; only dg and
+// du go through LDS, to the waves that make dx, one round later. x and dz are read
+// from LDS along for g, u and dh, and across (ds_read_b64_tr_b16) for the weights'
+// gradients. The biases' gradients are products with ones. Workgroups write their
+// sums in fp32, and a second launch adds these in a fixed order.
+#pragma once
+
+#include <algorithm>
+
+#include "activation.h"
+#include "gated_ffn_args.h"
+#include "gemm.h"
+
+namespace abcd {
+namespace {
+
+// 8 elements from p, n of them there (others 0), as they are.
+template <typename T, bool kWhole>
+__device__ __forceinline__ typename Frag<T>::type load_frag(const T* p, int n) {
+  typedef typename Frag<T>::type F;
+  typedef F FU __attribute__((aligned(sizeof(T))));
+  F v = (T)0.0f;
+  if (n >= 8) {
+    v = *reinterpret_cast<const FU*>(p);
+  } else if (!kWhole) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) v[i] = p[i];
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type join(f32x4 a, f32x4 b) {
+  typename Frag<T>::type r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (T)a[i], r[4 + i] = (T)b[i];
+  return r;
+}
+
+// m[row][col], 0 outside rows x cols.
+template <typename T>
+__device__ __forceinline__ T at_or_0(const void* m, int row, int col, int rows, int cols) {
+  return row < rows && col < cols ? static_cast<const T*>(m)[(int64_t)row * cols + col] : (T)0.0f;
+}
+
+constexpr int kNarrowThreads = 256, kNarrowBwdThreads = 512;
+
+// kDF: contractions of 32 that hold d; kOB: 16-column blocks of o; kHC: 32-column
+// chunks of h
+template <typename T, int kDF, int kOB, int kHC, bool kWhole>
+__global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow a) {
+  typedef typename Frag<T>::type F;
+  constexpr int kNarrowWaves = kNarrowThreads / 64, kRowFrags = 2, kRows = kRowFrags * 16;
+  constexpr int kChunk = 4 * kDF + kOB;  // fragments of a chunk: gate, up, down
+  __shared__ __align__(16) F weights[kHC * kChunk * 64];
+  __shared__ __align__(16) float bias[2][kHC * 32];
+  const int d = (int)a.d, h = (int)a.h, o = (int)a.o;
+  for (int s = threadIdx.x; s < kHC * kChunk * 64; s += kNarrowThreads) {
+    const int l = s & 63, f = s / 64 % kChunk, c = s / 64 / kChunk;
+    F v = (T)0.0f;
+    if (f < 4 * kDF) {
+      // gate and up: block f / kDF of (gate 0, gate 1, up 0, up 1), contraction f % kDF
+      const int row = c * 32 + (f / kDF & 1) * 16 + (l & 15), col = f % kDF * 32 + (l >> 4) * 8;
+      const T* w = static_cast<const T*>(f < 2 * kDF ? a.w_gate : a.w_up);
+      if (row < h && col < d) v = load_frag<T, false>(w + (int64_t)row * d + col, d - col);
+    } else {
+      // down: lane quarter q of block b holds columns q kOB 4 + 4 b .. + 3 of y, so
+      // that a lane's blocks are consecutive columns
+      const int i = l & 15, out = (i >> 2) * (kOB * 4) + (f - 4 * kDF) * 4 + (i & 3);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        v[e] = at_or_0<T>(a.w_down, out, c * 32 + (e >> 2) * 16 + (l >> 4) * 4 + (e & 3), o, h);
+    }
+    weights[s] = v;
+  }
+  for (int s = threadIdx.x; s < 2 * kHC * 32; s += kNarrowThreads) {
+    const int c = s % (kHC * 32);
+    const T* b = static_cast<const T*>(s < kHC * 32 ? a.b_gate : a.b_up);
+    bias[s / (kHC * 32)][c] = b && c < h ? (float)b[c] : 0.0f;
+  }
+  __syncthreads();
+  const int l = threadIdx.x & 63, j = l & 15, q = l >> 4;
+  const int64_t step = (int64_t)gridDim.x * kNarrowWaves * kRows;
+  int64_t r0 = ((int64_t)blockIdx.x * kNarrowWaves + (threadIdx.x >> 6)) * kRows;
+  const int chunks = (h + 31) / 32;
+  auto fetch = [&](int64_t from, F (&x)[kRowFrags][kDF]) {
+#pragma unroll
+    for (int x0 = 0; x0 < kRowFrags; ++x0) {
+      const int64_t r = from + x0 * 16 + j;
+#pragma unroll
+      for (int f = 0; f < kDF; ++f) {
+        const int c = f * 32 + q * 8;
+        x[x0][f] = (T)0.0f;
+        if (r < a.n && c < d) x[x0][f] = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + c, d - c);
+      }
+    }
+  };
+  F next[kRowFrags][kDF];
+  fetch(r0, next);
+  for (; r0 < a.n; r0 += step) {
+    F x[kRowFrags][kDF];
+#pragma unroll
+    for (int i = 0; i < kRowFrags; ++i)
+#pragma unroll
+      for (int f = 0; f < kDF; ++f) x[i][f] = next[i][f];
+    fetch(r0 + step, next);
+    f32x4 y[kRowFrags][kOB];
+#pragma unroll
+    for (int i = 0; i < kRowFrags; ++i)
+#pragma unroll
+      for (int b = 0; b < kOB; ++b) y[i][b] = 0.0f;
+    for (int c = 0; c < chunks; ++c) {
+      const F* w = weights + c * kChunk * 64 + l;
+      f32x4 g[kRowFrags][2], u[kRowFrags][2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const f32x4 bg = *reinterpret_cast<const f32x4*>(&bias[0][c * 32 + b * 16 + q * 4]);
+        const f32x4 bu = *reinterpret_cast<const f32x4*>(&bias[1][c * 32 + b * 16 + q * 4]);
+#pragma unroll
+        for (int i = 0; i < kRowFrags; ++i) g[i][b] = bg, u[i][b] = bu;
+#pragma unroll
+        for (int f = 0; f < kDF; ++f) {
+          const F wg = w[(b * kDF + f) * 64], wu = w[((2 + b) * kDF + f) * 64];
+#pragma unroll
+          for (int i = 0; i < kRowFrags; ++i) {
+            g[i][b] = mma(wg, x[i][f], g[i][b]);
+            u[i][b] = mma(wu, x[i][f], u[i][b]);
+          }
+        }
+      }
+      F hid[kRowFrags];
+#pragma unroll
+      for (int i = 0; i < kRowFrags; ++i) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float slope;
+            g[i][b][e] = activate(g[i][b][e], a.act, slope) * u[i][b][e];
+          }
+        hid[i] = join<T>(g[i][0], g[i][1]);
+      }
+#pragma unroll
+      for (int b = 0; b < kOB; ++b) {
+        const F wd = w[(4 * kDF + b) * 64];
+#pragma unroll
+        for (int i = 0; i < kRowFrags; ++i) y[i][b] = mma(wd, hid[i], y[i][b]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRowFrags; ++i) {
+      const int64_t r = r0 + i * 16 + j;
+      if (r >= a.n) continue;
+#pragma unroll
+      for (int b = 0; b < kOB; b += 2) {
+        const int c = q * (kOB * 4) + b * 4, left = o - c;
+        if (left <= 0) continue;
+        Floats<8> v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = y[i][b + e / 4][e % 4];
+        if (a.b_down) v += load_vec<T, 8, false>(static_cast<const T*>(a.b_down) + c, left);
+        v = drop_vec<8>(v, a.key, (uint32_t)r, (uint32_t)c);
+        if (a.res) v = load_vec<T, 8, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left) + v;
+        store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + c, v, left);
+      }
+    }
+  }
+}
+
+// Rows of 128 bytes in LDS (64 elements): where the 8 bytes of elements 4 unit .. + 3
+// of a row lie, so that neither the lanes that read 16 bytes of consecutive rows nor
+// those that read 8 bytes across them meet a bank too often.
+__device__ __forceinline__ int row_at(int row, int unit) { return row * 128 + (((unit >> 1) ^ (row & 7)) * 16) + (unit & 1) * 8; }
+// The same for dg and du, which are written 8 bytes down 16 rows.
+__device__ __forceinline__ int turned_at(int row, int unit) {
+  return row * 128 + ((unit ^ (((row & 3) << 2) | ((row >> 2) & 3))) * 8);
+}
+
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type read_across(LdsChar* lo, LdsChar* hi) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) s16x4 LdsS4;
+  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)lo);
+  const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)hi);
+  return __builtin_bit_cast(typename Frag<T>::type, (s16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// d and o up to 64, h up to kHB * 128
+template <typename T, int kHB, bool kWhole>
+__global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(FfnNarrowBwd a) {
+  typedef typename Frag<T>::type F;
+  constexpr int kTile = 64 * 128, kH = kHB * 128;
+  __shared__ __align__(16) char xs[2][kTile];        // [64 rows][64 columns]
+  __shared__ __align__(16) char zs[2][kTile];
+  __shared__ __align__(16) char turned[2][2 * kH * 128];  // [dg, then du: column of h][64 rows]
+  const int d = (int)a.d, h = (int)a.h, o = (int)a.o;
+  const int l = threadIdx.x & 63, j = l & 15, q = l >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // this wave's columns of h: block b's column j
+  F wg[kHB][2], wu[kHB][2], wd[kHB][2];
+  f32x4 bg[kHB], bu[kHB];
+#pragma unroll
+  for (int b = 0; b < kHB; ++b) {
+    const int col = (wave * kHB + b) * 16 + j;
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const int c = f * 32 + q * 8;
+      wg[b][f] = wu[b][f] = (T)0.0f;
+      if (col < h && c < d) {
+        wg[b][f] = load_frag<T, false>(static_cast<const T*>(a.w_gate) + (int64_t)col * d + c, d - c);
+        wu[b][f] = load_frag<T, false>(static_cast<const T*>(a.w_up) + (int64_t)col * d + c, d - c);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) wd[b][f][e] = at_or_0<T>(a.w_down, c + e, col, o, h);
+    }
+    bg[b] = a.b_gate && col < h ? (float)static_cast<const T*>(a.b_gate)[col] : 0.0f;
+    bu[b] = a.b_up && col < h ? (float)static_cast<const T*>(a.b_up)[col] : 0.0f;
+  }
+  // what it makes of dx: columns xb * 16 .. + 15 of rows xr * 32 .. + 31
+  const int xb = wave & 3, xr = wave >> 2;
+  F wx[2][kH / 32];
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int k = 0; k < kH / 32; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) wx[s][k][e] = at_or_0<T>(s ? a.w_up : a.w_gate, k * 32 + q * 8 + e, xb * 16 + j, h, d);
+  f32x4 dwg[kHB][4], dwu[kHB][4], dwd[kHB][4], sg[kHB], su[kHB], sz = 0.0f;
+#pragma unroll
+  for (int b = 0; b < kHB; ++b) {
+    sg[b] = su[b] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) dwg[b][k] = dwu[b][k] = dwd[b][k] = 0.0f;
+  }
+  F ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (T)1.0f;
+
+  // thread t brings row t / 8, columns (t & 7) 8 .. + 7 of a block's x and dz
+  const int lr = threadIdx.x >> 3, lc = (threadIdx.x & 7) * 8;
+  F nx, nz;
+  auto fetch = [&](int64_t block) {
+    const int64_t r = block * 64 + lr;
+    nx = nz = (T)0.0f;
+    if (r < a.n && lc < d) nx = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + lc, d - lc);
+    if (r < a.n && lc < o) nz = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + r * a.lddy + lc, o - lc);
+  };
+  auto put = [&](int64_t block, int into) {
+    // the mask as it was in the forward; the factor of what is kept comes at the end
+    if (a.key.mode != 0) {
+      const uint32_t r = (uint32_t)(block * 64 + lr);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const uint32_t bits = a.key.mode == 2 ? 0 : drop_bits(a.key, r, lc / 4 + v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!(bits >> e & 1)) nz[4 * v + e] = (T)0.0f;
+      }
+    }
+    *reinterpret_cast<F*>(xs[into] + row_at(lr, lc / 4)) = nx;
+    *reinterpret_cast<F*>(zs[into] + row_at(lr, lc / 4)) = nz;
+  };
+  auto dx_of = [&](int64_t block, int from) {
+    f32x4 acc[2];
+    acc[0] = acc[1] = 0.0f;
+    LdsChar* const t = (LdsChar*)turned[from];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int k = 0; k < kH / 32; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = s * kH + k * 32 + q * 8 + (j >> 2), unit = (xr * 2 + i) * 4 + (j & 3);
+          acc[i] = mma(wx[s][k], read_across<T>(t + turned_at(row, unit), t + turned_at(row + 4, unit)), acc[i]);
+        }
+    const int c = xb * 16 + q * 4, left = d - c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t r = block * 64 + xr * 32 + i * 16 + j;
+      if (a.dx && r < a.n && left > 0)
+        store_vec<T, 4, false>(static_cast<T*>(a.dx) + r * a.lddx + c, acc[i] * a.scale, left);
+    }
+  };
+
+  const int64_t blocks = (a.n + 63) / 64;
+  int64_t block = blockIdx.x, last = -1;
+  int cur = 0;
+  if (block < blocks) {
+    fetch(block);
+    put(block, 0);
+  }
+  for (; block < blocks; block += gridDim.x, cur ^= 1) {
+    const int64_t next = block + gridDim.x;
+    __syncthreads();  // this block's rows are in LDS, and so are the last one's dg and du
+    if (next < blocks) fetch(next);
+    LdsChar* const x = (LdsChar*)xs[cur];
+    LdsChar* const z = (LdsChar*)zs[cur];
+    LdsChar* const t = (LdsChar*)turned[cur];
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {  // 32 rows at a time
+      F dg[kHB], du[kHB], hid[kHB];
+#pragma unroll
+      for (int b = 0; b < kHB; ++b) {
+        f32x4 vg[2], vu[2], vh[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = half * 32 + i * 16 + j;
+          f32x4 g = bg[b], u = bu[b], dh = 0.0f;
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            typedef const __attribute__((address_space(3))) F LdsF;
+            const F ax = *(LdsF*)(x + row_at(row, (f * 32 + q * 8) / 4));
+            const F az = *(LdsF*)(z + row_at(row, (f * 32 + q * 8) / 4));
+            g = mma(ax, wg[b][f], g);
+            u = mma(ax, wu[b][f], u);
+            dh = mma(az, wd[b][f], dh);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float slope;
+            const float v = activate(g[e], a.act, slope);
+            vh[i][e] = v * u[e];
+            vg[i][e] = dh[e] * (u[e] * slope);
+            vu[i][e] = dh[e] * v;
+          }
+        }
+        dg[b] = join<T>(vg[0], vg[1]);
+        du[b] = join<T>(vu[0], vu[1]);
+        hid[b] = join<T>(vh[0], vh[1]);
+        const int col = (wave * kHB + b) * 16 + j;
+        typedef typename VecOf<T, 4>::type V4;
+        typedef __attribute__((address_space(3))) V4 LdsV4;
+        const int unit = half * 8 + q;
+        *(LdsV4*)(t + turned_at(col, unit)) = __builtin_shufflevector(dg[b], dg[b], 0, 1, 2, 3);
+        *(LdsV4*)(t + turned_at(col, unit + 4)) = __builtin_shufflevector(dg[b], dg[b], 4, 5, 6, 7);
+        *(LdsV4*)(t + turned_at(kH + col, unit)) = __builtin_shufflevector(du[b], du[b], 0, 1, 2, 3);
+        *(LdsV4*)(t + turned_at(kH + col, unit + 4)) = __builtin_shufflevector(du[b], du[b], 4, 5, 6, 7);
+        sg[b] = mma(ones, dg[b], sg[b]);
+        su[b] = mma(ones, du[b], su[b]);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // column 16 k + j, rows half 32 + 4 q .. + 3 and 16 further on
+        const int row = half * 32 + q * 4 + (j >> 2), unit = k * 4 + (j & 3);
+        const F ax = read_across<T>(x + row_at(row, unit), x + row_at(row + 16, unit));
+        const F az = read_across<T>(z + row_at(row, unit), z + row_at(row + 16, unit));
+#pragma unroll
+        for (int b = 0; b < kHB; ++b) {
+          dwg[b][k] = mma(ax, dg[b], dwg[b][k]);
+          dwu[b][k] = mma(ax, du[b], dwu[b][k]);
+          dwd[b][k] = mma(az, hid[b], dwd[b][k]);
+        }
+        if (k == (wave & 3)) sz = mma(az, ones, sz);
+      }
+    }
+    if (last >= 0) dx_of(last, cur ^ 1);
+    last = block;
+    if (next < blocks) put(next, cur ^ 1);
+  }
+  __syncthreads();
+  if (last >= 0) dx_of(last, cur ^ 1);
+
+  // sums: [dWg h x d][dWu h x d][dWd o x h][dbg h][dbu h][dbd o]
+  float* const part = a.part + (int64_t)blockIdx.x * a.sums;
+  const int64_t up = (int64_t)h * d, down = 2 * up, biases = down + (int64_t)o * h;
+#pragma unroll
+  for (int b = 0; b < kHB; ++b) {
+    const int col = (wave * kHB + b) * 16 + j;
+    if (col >= h) continue;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = k * 16 + q * 4 + e;
+        if (c < d) {
+          part[(int64_t)col * d + c] = dwg[b][k][e] * a.scale;
+          part[up + (int64_t)col * d + c] = dwu[b][k][e] * a.scale;
+        }
+        if (c < o) part[down + (int64_t)c * h + col] = dwd[b][k][e] * a.scale;
+      }
+    if (q == 0) {
+      part[biases + col] = sg[b][0] * a.scale;
+      part[biases + h + col] = su[b][0] * a.scale;
+    }
+  }
+  if (wave < 4 && j == 0)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = wave * 16 + q * 4 + e;
+      if (c < o) part[biases + 2 * h + c] = sz[e] * a.scale;
+    }
+}
+
+template <typename T>
+int32_t run_narrow(const FfnNarrow& a, int64_t blocks, hipStream_t stream) {
+  const bool whole = a.d % 8 == 0;
+  if (whole)
+    ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, 2, 4, 4, true>), blocks, kNarrowThreads, 0, stream, a);
+  else
+    ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, 2, 4, 4, false>), blocks, kNarrowThreads, 0, stream, a);
+  ABCD_HIP(hipGetLastError());
+  return ABCD_OK;
+}
+
+template <typename T>
+int32_t run_narrow_bwd(const FfnNarrowBwd& a, int64_t blocks, hipStream_t stream) {
+  const bool whole = a.d % 8 == 0 && a.o % 8 == 0;
+  if (whole)
+    ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, 1, true>), blocks, kNarrowBwdThreads, 0, stream, a);
+  else
+    ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, 1, false>), blocks, kNarrowBwdThreads, 0, stream, a);
+  ABCD_HIP(hipGetLastError());
+  return ABCD_OK;
+}
+
+}  // namespace
+
+#define ABCD_FFN_NARROW(NAME, TYPE)                                                                                  \
+  int32_t ffn_narrow_##NAME(const FfnNarrow& a, int64_t blocks, hipStream_t s) { return run_narrow<TYPE>(a, blocks, s); } \
+  int32_t ffn_narrow_bwd_##NAME(const FfnNarrowBwd& a, int64_t blocks, hipStream_t s) {                              \
+    return run_narrow_bwd<TYPE>(a, blocks, s);                                                                       \
+  }
+
+}  // namespace abcd

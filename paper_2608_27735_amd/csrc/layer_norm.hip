@@ -389,7 +389,10 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
     }));
   if (dweight || dbias) {
     const int32_t to = wf32 ? ABCD_F32 : dtype;
-    TRY_STATUS(launch_sum_parts(part, blocks, 2 * d, d, to, dweight, dbias, stream));
+    SumOuts outs{};
+    outs.add(dweight, d);
+    outs.add(dbias, d);
+    TRY_STATUS(launch_sum_parts(part, blocks, outs, to, stream));
   }
   return ABCD_OK;
 }

@@ -8,15 +8,15 @@ namespace {
 
 constexpr int kPartWaves = 16;
 
-// out0[c] (c < split) and out1[c - split] = sum over p of part[p][c]: 64 columns
-// per workgroup, the parts dealt to its 16 waves, whose sums LDS joins.
+// Column c of the parts belongs to the output whose range holds it; out[i] = sum
+// over p of part[p][c]: 64 columns per workgroup, the parts dealt to its 16 waves,
+// whose sums LDS joins.
 template <typename T>
 __global__ __launch_bounds__(kPartWaves* kWave) void sum_parts_kernel(const float* part, int64_t parts,
-                                                                     int64_t cols, int64_t split, T* out0,
-                                                                     T* out1) {
+                                                                     SumOuts outs) {
   __shared__ float red[kPartWaves][kWave];
   const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
-  const int64_t c = (int64_t)blockIdx.x * kWave + l;
+  const int64_t c = (int64_t)blockIdx.x * kWave + l, cols = outs.begin[outs.count];
   float s = 0.0f;
   if (c < cols) {
     int64_t p = w;
@@ -33,21 +33,19 @@ __global__ __launch_bounds__(kPartWaves* kWave) void sum_parts_kernel(const floa
   __syncthreads();
   if (w != 0 || c >= cols) return;
   for (int i = 1; i < kPartWaves; ++i) s += red[i][l];
-  if (c < split) {
-    if (out0) out0[c] = (T)s;
-  } else if (out1) {
-    out1[c - split] = (T)s;
-  }
+  int k = 0;
+  while (c >= outs.begin[k + 1]) ++k;
+  if (outs.out[k]) static_cast<T*>(outs.out[k])[c - outs.begin[k]] = (T)s;
 }
 
 }  // namespace
 
-int32_t launch_sum_parts(const float* part, int64_t parts, int64_t cols, int64_t split, int32_t dtype, void* out0,
-                         void* out1, hipStream_t stream) {
+int32_t launch_sum_parts(const float* part, int64_t parts, const SumOuts& outs, int32_t dtype, hipStream_t stream) {
   return with_type(dtype, [&](auto zero) -> int32_t {
     typedef decltype(zero) T;
+    const int64_t cols = outs.begin[outs.count];
     ABCD_LAUNCH("sum_parts", (sum_parts_kernel<T>), (cols + kWave - 1) / kWave, kPartWaves * kWave, 0, stream, part,
-                parts, cols, split, static_cast<T*>(out0), static_cast<T*>(out1));
+                parts, outs);
     ABCD_HIP(hipGetLastError());
     return ABCD_OK;
   });

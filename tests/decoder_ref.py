@@ -60,20 +60,18 @@ def layer_norm_bwd(dy, x, mean, rstd, w, add):
 
 
 def keep_mask(n, d, p, seed, offset):
-    """Philox 4x32-7 in Python integers (small matrices)."""
-    M = 0xFFFFFFFF
-    thr = math.floor(p * 2 ** 32)
-    keep = np.zeros((n, d), bool)
-    for r in range(n):
-        for q in range((d + 3) // 4):
-            c = [q, r, offset & M, offset >> 32]
-            k0, k1 = seed & M, seed >> 32
-            for _ in range(7):
-                a, b = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
-                c = [(b >> 32) ^ c[1] ^ k0, b & M, (a >> 32) ^ c[3] ^ k1, a & M]
-                k0, k1 = (k0 + 0x9E3779B9) & M, (k1 + 0xBB67AE85) & M
-            for j in range(min(4, d - 4 * q)):
-                keep[r, 4 * q + j] = c[j] >= thr
+    """Philox 4x32-7, its words as unsigned 64-bit integers."""
+    M, S = np.uint64(0xFFFFFFFF), np.uint64(32)
+    quads = (d + 3) // 4
+    c = [np.tile(np.arange(quads, dtype=np.uint64), (n, 1)),
+         np.repeat(np.arange(n, dtype=np.uint64)[:, None], quads, 1),
+         np.full((n, quads), offset & 0xFFFFFFFF, np.uint64), np.full((n, quads), offset >> 32, np.uint64)]
+    k0, k1 = seed & 0xFFFFFFFF, seed >> 32
+    for _ in range(7):
+        a, b = np.uint64(0xD2511F53) * c[0], np.uint64(0xCD9E8D57) * c[2]
+        c = [(b >> S) ^ c[1] ^ np.uint64(k0), b & M, (a >> S) ^ c[3] ^ np.uint64(k1), a & M]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    keep = np.stack(c, 2).reshape(n, 4 * quads)[:, :d] >= np.uint64(math.floor(p * 2 ** 32))
     return torch.from_numpy(keep)
 
 

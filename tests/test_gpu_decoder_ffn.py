@@ -76,6 +76,39 @@ def test_large_tiles_and_split_rows(api, dtype):
     run(api, 9001, 24, 40, 16, dtype, "gelu", True, 0.0)
 
 
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n,d,h,o", [
+    (1024, 64, 128, 64), (1025, 1, 1, 1), (1100, 7, 5, 3), (2049, 33, 100, 48), (3000, 59, 127, 61), (1500, 16, 129, 16),
+    (20011, 64, 128, 64), (70001, 24, 40, 50)])
+def test_narrow_rows(api, dtype, n, d, h, o):
+    run(api, n, d, h, o, dtype, "silu", True, 0.1)
+    run(api, n, d, h, o, dtype, "gelu", False, 0.0, pad=5, skip=1)
+    run(api, n, d, h, o, dtype, "relu", True, 1.0)
+
+
+def test_narrow_kernels_agree_with_the_products(api):
+    """The same block by the tiled products (what the forward keeps is given)."""
+    n, d, h, o = 5000, 64, 128, 64
+    w, x, dy = weights(4, d, h, o, torch.bfloat16, True), rand(1, n, d, torch.bfloat16), rand(2, n, o, torch.bfloat16)
+    import ctypes as C
+    from paper_2608_27735_amd import _lib
+    f, ldx = api._ffn(x, w, "silu", 0.2, 3, 4)
+    saved = [torch.empty((n, h), dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    y = torch.empty((n, o), dtype=torch.bfloat16, device="cuda")
+    lib, sz = _lib.load(), C.c_size_t(0)
+    api.check(lib.abcd_gated_ffn_workspace_size(C.byref(f), n, 1, C.byref(sz)))
+    ws = torch.empty(sz.value, dtype=torch.uint8, device="cuda")
+    api.check(lib.abcd_gated_ffn(C.byref(f), n, x.data_ptr(), ldx, None, 0, y.data_ptr(), o,
+                                 *[t.data_ptr() for t in saved], ws.data_ptr(), ws.numel(), api._stream()))
+    kept = api.gated_ffn_bwd(dy, x, w, saved=dict(zip(api.FFN_SAVED, saved)), p=0.2, seed=3, offset=4)
+    narrow = api.gated_ffn(x, w, p=0.2, seed=3, offset=4, save=True)
+    assert narrow["saved"] is None
+    grads = api.gated_ffn_bwd(dy, x, w, p=0.2, seed=3, offset=4)
+    for k, a, b in [("y", y, narrow["y"])] + [(k, kept[k], grads[k]) for k in grads]:
+        rel = (a.double() - b.double()).norm() / b.double().norm()
+        assert rel <= 8e-3, (k, rel)  # a few roundings of 2^-9
+
+
 @pytest.mark.parametrize("n", [2, 8, 16, 31, 33, 64])
 @pytest.mark.parametrize("d,h,o", [(512, 1376, 512), (1001, 333, 77)])
 def test_few_rows(api, n, d, h, o):
