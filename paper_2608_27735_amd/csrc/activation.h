@@ -1,6 +1,8 @@
 // activation.h -- the gated block's activations and their derivatives.
 #pragma once
 
+#include <type_traits>
+
 #include "abcd_internal.h"
 
 namespace abcd {
@@ -10,20 +12,30 @@ __device__ __forceinline__ float sigmoid(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * g));
 }
 
-// a(g) and a'(g). The activation is the same for every lane.
-__device__ __forceinline__ float activate(float g, int act, float& slope) {
-  if (act == ABCD_ACT_SILU) {
-    const float s = sigmoid(g);
-    slope = s * (1.0f + g * (1.0f - s));
-    return g * s;
+// a(g) and a'(g). The activation is a template argument of the kernels: with a
+// branch at every element no two elements' exponentials overlap.
+template <int kAct>
+__device__ __forceinline__ float activate(float g, float& slope) {
+  if (kAct == ABCD_ACT_SILU) {
+    const float s = sigmoid(g), v = g * s;
+    slope = fmaf(v, 1.0f - s, s);
+    return v;
   }
-  if (act == ABCD_ACT_GELU) {
+  if (kAct == ABCD_ACT_GELU) {
     const float c = 0.5f + 0.5f * erff(0.70710678118654752f * g);
     slope = c + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
     return g * c;
   }
   slope = g > 0.0f ? 1.0f : 0.0f;
   return fmaxf(g, 0.0f);
+}
+
+// Calls f with act as a constant.
+template <typename F>
+int32_t with_act(int act, F f) {
+  if (act == ABCD_ACT_SILU) return f(std::integral_constant<int, ABCD_ACT_SILU>{});
+  if (act == ABCD_ACT_GELU) return f(std::integral_constant<int, ABCD_ACT_GELU>{});
+  return f(std::integral_constant<int, ABCD_ACT_RELU>{});
 }
 
 }  // namespace abcd

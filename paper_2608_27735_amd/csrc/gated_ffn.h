@@ -50,7 +50,7 @@ __device__ __forceinline__ f32x4 load4(const void* p, int64_t at, int64_t n) {
   return load_vec<T, 4, false>(static_cast<const T*>(p) + at, n > 4 ? 4 : (int)n);
 }
 
-template <typename T, typename Cfg>
+template <typename T, typename Cfg, int kAct>
 __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn a) {
   typedef ProductOf<T, Cfg, true, true, true> P;
   ABCD_TILE_LDS(P);
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn 
       for (int i = 0; i < 4; ++i) {
         if (c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
         float slope;
-        hu[i] = activate(g[i], a.act, slope);
+        hu[i] = activate<kAct>(g[i], slope);
         h[i] = hu[i] * u[i];
         hg[i] = slope * u[i];
       }
@@ -220,7 +220,7 @@ inline int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
 // The big tile where it gives most of the CUs one.
 inline bool use_big(int64_t nx, int64_t nw, int tw) { return tiles(nx, Big::TX) * tiles(nw, tw) >= 192; }
 
-#define ABCD_FFN_LAUNCH(label, kernel, a, nx, nw, half, stream)                                           \
+#define ABCD_FFN_LAUNCH(label, kernel, a, nx, nw, half, stream, ...)                                      \
   do {                                                                                                    \
     const bool big_ = use_big(nx, nw, Big::TW / (half));                                                  \
     a.tiles_x = (int)tiles(nx, big_ ? Big::TX : Small::TX);                                               \
@@ -228,16 +228,18 @@ inline bool use_big(int64_t nx, int64_t nw, int tw) { return tiles(nx, Big::TX) 
     const int64_t grid_ = (int64_t)a.tiles_x * a.tiles_w;                                                 \
     REQUIRE(grid_ < (int64_t(1) << 31), "too many tiles");                                                \
     if (big_)                                                                                             \
-      ABCD_LAUNCH(label, (kernel<T, Big>), grid_, Big::WX* Big::WW * 64, 0, stream, a);                   \
+      ABCD_LAUNCH(label, (kernel<T, Big __VA_ARGS__>), grid_, Big::WX* Big::WW * 64, 0, stream, a);       \
     else                                                                                                  \
-      ABCD_LAUNCH(label, (kernel<T, Small>), grid_, Small::WX* Small::WW * 64, 0, stream, a);             \
+      ABCD_LAUNCH(label, (kernel<T, Small __VA_ARGS__>), grid_, Small::WX* Small::WW * 64, 0, stream, a); \
     ABCD_HIP(hipGetLastError());                                                                          \
   } while (0)
 
 template <typename T>
 int32_t run_in(FfnIn a, hipStream_t stream) {
-  ABCD_FFN_LAUNCH("ffn_in", ffn_in_kernel, a, a.x.len, a.h, 2, stream);
-  return ABCD_OK;
+  return with_act(a.act, [&](auto act) -> int32_t {
+    ABCD_FFN_LAUNCH("ffn_in", ffn_in_kernel, a, a.x.len, a.h, 2, stream, , decltype(act)::value);
+    return ABCD_OK;
+  });
 }
 template <typename T>
 int32_t run_out(FfnOut a, hipStream_t stream) {

@@ -32,19 +32,25 @@
 namespace abcd {
 namespace {
 
-// 8 elements from p, n of them there (others 0), as they are.
-template <typename T, bool kWhole>
-__device__ __forceinline__ typename Frag<T>::type load_frag(const T* p, int n) {
+// Where loads of what lies outside an array go: under a condition a load would be
+// waited for by itself, at the end of its branch.
+__device__ uint32_t zeros[4];
+
+// 8 elements from p as they are where `in`, else 0.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type load_whole(const T* p, bool in) {
   typedef typename Frag<T>::type F;
   typedef F FU __attribute__((aligned(sizeof(T))));
-  F v = (T)0.0f;
-  if (n >= 8) {
-    v = *reinterpret_cast<const FU*>(p);
-  } else if (!kWhole) {
+  return *reinterpret_cast<const FU*>(in ? p : reinterpret_cast<const T*>(zeros));
+}
+// The same where only n of them may be there (n <= 0: none).
+template <typename T, bool kWhole>
+__device__ __forceinline__ typename Frag<T>::type load_frag(const T* p, int n) {
+  if (kWhole || n >= 8 || n <= 0) return load_whole(p, n > 0);
+  typename Frag<T>::type v = (T)0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) v[i] = p[i];
-  }
+  for (int i = 0; i < 7; ++i)
+    if (i < n) v[i] = p[i];
   return v;
 }
 
@@ -59,14 +65,15 @@ __device__ __forceinline__ typename Frag<T>::type join(f32x4 a, f32x4 b) {
 // m[row][col], 0 outside rows x cols.
 template <typename T>
 __device__ __forceinline__ T at_or_0(const void* m, int row, int col, int rows, int cols) {
-  return row < rows && col < cols ? static_cast<const T*>(m)[(int64_t)row * cols + col] : (T)0.0f;
+  const bool in = row < rows && col < cols;
+  return *(in ? static_cast<const T*>(m) + (int64_t)row * cols + col : reinterpret_cast<const T*>(zeros));
 }
 
 constexpr int kNarrowThreads = 256, kNarrowBwdThreads = 512;
 
-// kDF: contractions of 32 that hold d; kOB: 16-column blocks of o; kHC: 32-column
+// kWhole: d, h and o are multiples of 8. kDF: contractions of 32 that hold d; kOB: 16-column blocks of o; kHC: 32-column
 // chunks of h
-template <typename T, int kDF, int kOB, int kHC, bool kWhole>
+template <typename T, int kAct, int kDF, int kOB, int kHC, bool kWhole>
 __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow a) {
   typedef typename Frag<T>::type F;
   constexpr int kNarrowWaves = kNarrowThreads / 64, kRowFrags = 2, kRows = kRowFrags * 16;
@@ -74,21 +81,38 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
   __shared__ __align__(16) F weights[kHC * kChunk * 64];
   __shared__ __align__(16) float bias[2][kHC * 32];
   const int d = (int)a.d, h = (int)a.h, o = (int)a.o;
-  for (int s = threadIdx.x; s < kHC * kChunk * 64; s += kNarrowThreads) {
+  constexpr int kTurns = kHC * kChunk * 64 / kNarrowThreads;
+  static_assert(kHC * kChunk * 64 % kNarrowThreads == 0, "every thread sets up as many");
+#pragma unroll 4
+  for (int turn = 0; turn < kTurns; ++turn) {
+    const int s = turn * kNarrowThreads + threadIdx.x;
     const int l = s & 63, f = s / 64 % kChunk, c = s / 64 / kChunk;
-    F v = (T)0.0f;
-    if (f < 4 * kDF) {
-      // gate and up: block f / kDF of (gate 0, gate 1, up 0, up 1), contraction f % kDF
-      const int row = c * 32 + (f / kDF & 1) * 16 + (l & 15), col = f % kDF * 32 + (l >> 4) * 8;
-      const T* w = static_cast<const T*>(f < 2 * kDF ? a.w_gate : a.w_up);
-      if (row < h && col < d) v = load_frag<T, false>(w + (int64_t)row * d + col, d - col);
+    F v;
+    // gate and up: block f / kDF of (gate 0, gate 1, up 0, up 1), contraction f %
+    // kDF; down: lane quarter q of block b holds columns q kOB 4 + 4 b .. + 3 of y,
+    // so that a lane's blocks are consecutive columns
+    const bool in = f < 4 * kDF;
+    const T* const w = static_cast<const T*>(in ? (f < 2 * kDF ? a.w_gate : a.w_up) : a.w_down);
+    const int i = l & 15;
+    const int row = in ? c * 32 + (f / kDF & 1) * 16 + i : (i >> 2) * (kOB * 4) + (f - 4 * kDF) * 4 + (i & 3);
+    const int rows = in ? h : o, cols = in ? d : h;
+    if (kWhole) {
+      // two halves of 4 elements: next to each other, or a block of h apart
+      typedef typename VecOf<T, 4>::type V4;
+      typedef V4 V4U __attribute__((aligned(sizeof(T))));
+      V4 half[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int col = in ? f % kDF * 32 + (l >> 4) * 8 + e * 4 : c * 32 + e * 16 + (l >> 4) * 4;
+        half[e] = *reinterpret_cast<const V4U*>(row < rows && col < cols ? w + (int64_t)row * cols + col
+                                                                        : reinterpret_cast<const T*>(zeros));
+      }
+      v = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      // down: lane quarter q of block b holds columns q kOB 4 + 4 b .. + 3 of y, so
-      // that a lane's blocks are consecutive columns
-      const int i = l & 15, out = (i >> 2) * (kOB * 4) + (f - 4 * kDF) * 4 + (i & 3);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        v[e] = at_or_0<T>(a.w_down, out, c * 32 + (e >> 2) * 16 + (l >> 4) * 4 + (e & 3), o, h);
+        v[e] = at_or_0<T>(w, row, in ? f % kDF * 32 + (l >> 4) * 8 + e : c * 32 + (e >> 2) * 16 + (l >> 4) * 4 + (e & 3),
+                          rows, cols);
     }
     weights[s] = v;
   }
@@ -109,8 +133,7 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
 #pragma unroll
       for (int f = 0; f < kDF; ++f) {
         const int c = f * 32 + q * 8;
-        x[x0][f] = (T)0.0f;
-        if (r < a.n && c < d) x[x0][f] = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + c, d - c);
+        x[x0][f] = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + c, r < a.n ? d - c : 0);
       }
     }
   };
@@ -123,6 +146,16 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
 #pragma unroll
       for (int f = 0; f < kDF; ++f) x[i][f] = next[i][f];
     fetch(r0 + step, next);
+    F res[kRowFrags][kOB / 2];  // on its way while the products run
+    if (a.res)
+#pragma unroll
+      for (int i = 0; i < kRowFrags; ++i)
+#pragma unroll
+        for (int b = 0; b < kOB / 2; ++b) {
+          const int64_t r = r0 + i * 16 + j;
+          const int c = q * (kOB * 4) + b * 8;
+          res[i][b] = load_frag<T, kWhole>(static_cast<const T*>(a.res) + r * a.ldr + c, r < a.n ? o - c : 0);
+        }
     f32x4 y[kRowFrags][kOB];
 #pragma unroll
     for (int i = 0; i < kRowFrags; ++i)
@@ -155,7 +188,7 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float slope;
-            g[i][b][e] = activate(g[i][b][e], a.act, slope) * u[i][b][e];
+            g[i][b][e] = activate<kAct>(g[i][b][e], slope) * u[i][b][e];
           }
         hid[i] = join<T>(g[i][0], g[i][1]);
       }
@@ -177,10 +210,10 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
         Floats<8> v;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = y[i][b + e / 4][e % 4];
-        if (a.b_down) v += load_vec<T, 8, false>(static_cast<const T*>(a.b_down) + c, left);
+        if (a.b_down) v += load_vec<T, 8, kWhole>(static_cast<const T*>(a.b_down) + c, left);
         v = drop_vec<8>(v, a.key, (uint32_t)r, (uint32_t)c);
-        if (a.res) v = load_vec<T, 8, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left) + v;
-        store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + c, v, left);
+        if (a.res) v = __builtin_convertvector(res[i][b / 2], Floats<8>) + v;
+        store_vec<T, 8, kWhole>(static_cast<T*>(a.y) + r * a.ldy + c, v, left);
       }
     }
   }
@@ -206,7 +239,7 @@ __device__ __forceinline__ typename Frag<T>::type read_across(LdsChar* lo, LdsCh
 }
 
 // d and o up to 64, h up to kHB * 128
-template <typename T, int kHB, bool kWhole>
+template <typename T, int kAct, int kHB, bool kWhole>
 __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(FfnNarrowBwd a) {
   typedef typename Frag<T>::type F;
   constexpr int kTile = 64 * 128, kH = kHB * 128;
@@ -216,35 +249,55 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
   const int d = (int)a.d, h = (int)a.h, o = (int)a.o;
   const int l = threadIdx.x & 63, j = l & 15, q = l >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // The weights pass through LDS in tiles of 64 x 64, from which each wave takes its
+  // own: as they lie in memory most of them are needed across their rows.
   // this wave's columns of h: block b's column j
   F wg[kHB][2], wu[kHB][2], wd[kHB][2];
   f32x4 bg[kHB], bu[kHB];
-#pragma unroll
-  for (int b = 0; b < kHB; ++b) {
-    const int col = (wave * kHB + b) * 16 + j;
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-      const int c = f * 32 + q * 8;
-      wg[b][f] = wu[b][f] = (T)0.0f;
-      if (col < h && c < d) {
-        wg[b][f] = load_frag<T, false>(static_cast<const T*>(a.w_gate) + (int64_t)col * d + c, d - c);
-        wu[b][f] = load_frag<T, false>(static_cast<const T*>(a.w_up) + (int64_t)col * d + c, d - c);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) wd[b][f][e] = at_or_0<T>(a.w_down, c + e, col, o, h);
-    }
-    bg[b] = a.b_gate && col < h ? (float)static_cast<const T*>(a.b_gate)[col] : 0.0f;
-    bu[b] = a.b_up && col < h ? (float)static_cast<const T*>(a.b_up)[col] : 0.0f;
-  }
   // what it makes of dx: columns xb * 16 .. + 15 of rows xr * 32 .. + 31
   const int xb = wave & 3, xr = wave >> 2;
   F wx[2][kH / 32];
+  // thread t brings row t / 8, columns (t & 7) 8 .. + 7 of a block's x and dz
+  const int lr = threadIdx.x >> 3, lc = (threadIdx.x & 7) * 8;
+  typedef const __attribute__((address_space(3))) F LdsF;
+  {
+    LdsChar* const t = (LdsChar*)turned[0];  // gate: [kH][64], then up
+    LdsChar* const td = (LdsChar*)turned[1];  // down: [kH / 64][64 of o][64 of h]
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
+    for (int k = 0; k < kH / 64; ++k) {
+      const int row = k * 64 + lr, col = k * 64 + lc;
+      const F g = load_frag<T, kWhole>(static_cast<const T*>(a.w_gate) + (int64_t)row * d + lc, row < h ? d - lc : 0);
+      const F u = load_frag<T, kWhole>(static_cast<const T*>(a.w_up) + (int64_t)row * d + lc, row < h ? d - lc : 0);
+      const F w = load_frag<T, kWhole>(static_cast<const T*>(a.w_down) + (int64_t)lr * h + col, lr < o ? h - col : 0);
+      const int at = row_at(lr, lc / 4) + k * kTile;
+      *(__attribute__((address_space(3))) F*)(t + at) = g;
+      *(__attribute__((address_space(3))) F*)(t + kH * 128 + at) = u;
+      *(__attribute__((address_space(3))) F*)(td + at) = w;
+    }
+    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kH / 32; ++k)
+    for (int b = 0; b < kHB; ++b) {
+      const int col = (wave * kHB + b) * 16 + j;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) wx[s][k][e] = at_or_0<T>(s ? a.w_up : a.w_gate, k * 32 + q * 8 + e, xb * 16 + j, h, d);
+      for (int f = 0; f < 2; ++f) {
+        wg[b][f] = *(LdsF*)(t + row_at(col, f * 8 + q * 2));
+        wu[b][f] = *(LdsF*)(t + kH * 128 + row_at(col, f * 8 + q * 2));
+        const int first = (wave * kHB + b) * 16, row = f * 32 + q * 8 + (j >> 2), unit = (first & 63) / 4 + (j & 3);
+        wd[b][f] = read_across<T>(td + first / 64 * kTile + row_at(row, unit), td + first / 64 * kTile + row_at(row + 4, unit));
+      }
+      bg[b] = a.b_gate ? (float)at_or_0<T>(a.b_gate, 0, col, 1, h) : 0.0f;
+      bu[b] = a.b_up ? (float)at_or_0<T>(a.b_up, 0, col, 1, h) : 0.0f;
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int k = 0; k < kH / 32; ++k) {
+        const int row = k * 32 + q * 8 + (j >> 2), unit = xb * 4 + (j & 3);
+        LdsChar* const from = t + s * kH * 128;
+        wx[s][k] = read_across<T>(from + row_at(row, unit), from + row_at(row + 4, unit));
+      }
+    __syncthreads();
+  }
   f32x4 dwg[kHB][4], dwu[kHB][4], dwd[kHB][4], sg[kHB], su[kHB], sz = 0.0f;
 #pragma unroll
   for (int b = 0; b < kHB; ++b) {
@@ -256,14 +309,11 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones[e] = (T)1.0f;
 
-  // thread t brings row t / 8, columns (t & 7) 8 .. + 7 of a block's x and dz
-  const int lr = threadIdx.x >> 3, lc = (threadIdx.x & 7) * 8;
   F nx, nz;
   auto fetch = [&](int64_t block) {
     const int64_t r = block * 64 + lr;
-    nx = nz = (T)0.0f;
-    if (r < a.n && lc < d) nx = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + lc, d - lc);
-    if (r < a.n && lc < o) nz = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + r * a.lddy + lc, o - lc);
+    nx = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + lc, r < a.n ? d - lc : 0);
+    nz = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + r * a.lddy + lc, r < a.n ? o - lc : 0);
   };
   auto put = [&](int64_t block, int into) {
     // the mask as it was in the forward; the factor of what is kept comes at the end
@@ -280,6 +330,19 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     *reinterpret_cast<F*>(xs[into] + row_at(lr, lc / 4)) = nx;
     *reinterpret_cast<F*>(zs[into] + row_at(lr, lc / 4)) = nz;
   };
+  // places in LDS, up to what does not change a swizzle: rows by 16, chunks of h by 32
+  int along[2], across[4], read_lo[2], read_hi[2];
+#pragma unroll
+  for (int f = 0; f < 2; ++f) along[f] = row_at(j, f * 8 + q * 2);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) across[k] = row_at(q * 4 + (j >> 2), k * 4 + (j & 3));
+  const int across_z = row_at(q * 4 + (j >> 2), (wave & 3) * 4 + (j & 3));  // its columns of dbd
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = q * 8 + (j >> 2), unit = (xr * 2 + i) * 4 + (j & 3);
+    read_lo[i] = turned_at(row, unit);
+    read_hi[i] = turned_at(row + 4, unit);
+  }
   auto dx_of = [&](int64_t block, int from) {
     f32x4 acc[2];
     acc[0] = acc[1] = 0.0f;
@@ -290,15 +353,15 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
       for (int k = 0; k < kH / 32; ++k)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int row = s * kH + k * 32 + q * 8 + (j >> 2), unit = (xr * 2 + i) * 4 + (j & 3);
-          acc[i] = mma(wx[s][k], read_across<T>(t + turned_at(row, unit), t + turned_at(row + 4, unit)), acc[i]);
+          LdsChar* const at = t + (s * kH + k * 32) * 128;
+          acc[i] = mma(wx[s][k], read_across<T>(at + read_lo[i], at + read_hi[i]), acc[i]);
         }
     const int c = xb * 16 + q * 4, left = d - c;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t r = block * 64 + xr * 32 + i * 16 + j;
       if (a.dx && r < a.n && left > 0)
-        store_vec<T, 4, false>(static_cast<T*>(a.dx) + r * a.lddx + c, acc[i] * a.scale, left);
+        store_vec<T, 4, kWhole>(static_cast<T*>(a.dx) + r * a.lddx + c, acc[i] * a.scale, left);
     }
   };
 
@@ -324,13 +387,12 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
         f32x4 vg[2], vu[2], vh[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int row = half * 32 + i * 16 + j;
+          const int row = (half * 32 + i * 16) * 128;
           f32x4 g = bg[b], u = bu[b], dh = 0.0f;
 #pragma unroll
           for (int f = 0; f < 2; ++f) {
-            typedef const __attribute__((address_space(3))) F LdsF;
-            const F ax = *(LdsF*)(x + row_at(row, (f * 32 + q * 8) / 4));
-            const F az = *(LdsF*)(z + row_at(row, (f * 32 + q * 8) / 4));
+            const F ax = *(LdsF*)(x + row + along[f]);
+            const F az = *(LdsF*)(z + row + along[f]);
             g = mma(ax, wg[b][f], g);
             u = mma(ax, wu[b][f], u);
             dh = mma(az, wd[b][f], dh);
@@ -338,7 +400,7 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float slope;
-            const float v = activate(g[e], a.act, slope);
+            const float v = activate<kAct>(g[e], slope);
             vh[i][e] = v * u[e];
             vg[i][e] = dh[e] * (u[e] * slope);
             vu[i][e] = dh[e] * v;
@@ -361,17 +423,18 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         // column 16 k + j, rows half 32 + 4 q .. + 3 and 16 further on
-        const int row = half * 32 + q * 4 + (j >> 2), unit = k * 4 + (j & 3);
-        const F ax = read_across<T>(x + row_at(row, unit), x + row_at(row + 16, unit));
-        const F az = read_across<T>(z + row_at(row, unit), z + row_at(row + 16, unit));
+        const int at = half * 32 * 128 + across[k];
+        const F ax = read_across<T>(x + at, x + at + 16 * 128);
+        const F az = read_across<T>(z + at, z + at + 16 * 128);
 #pragma unroll
         for (int b = 0; b < kHB; ++b) {
           dwg[b][k] = mma(ax, dg[b], dwg[b][k]);
           dwu[b][k] = mma(ax, du[b], dwu[b][k]);
           dwd[b][k] = mma(az, hid[b], dwd[b][k]);
         }
-        if (k == (wave & 3)) sz = mma(az, ones, sz);
       }
+      const int at = half * 32 * 128 + across_z;
+      sz = mma(read_across<T>(z + at, z + at + 16 * 128), ones, sz);
     }
     if (last >= 0) dx_of(last, cur ^ 1);
     last = block;
@@ -413,24 +476,28 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 
 template <typename T>
 int32_t run_narrow(const FfnNarrow& a, int64_t blocks, hipStream_t stream) {
-  const bool whole = a.d % 8 == 0;
-  if (whole)
-    ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, 2, 4, 4, true>), blocks, kNarrowThreads, 0, stream, a);
-  else
-    ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, 2, 4, 4, false>), blocks, kNarrowThreads, 0, stream, a);
-  ABCD_HIP(hipGetLastError());
-  return ABCD_OK;
+  return with_act(a.act, [&](auto act) -> int32_t {
+    constexpr int kAct = decltype(act)::value;
+    if (a.d % 8 == 0 && a.h % 8 == 0 && a.o % 8 == 0)
+      ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, kAct, 2, 4, 4, true>), blocks, kNarrowThreads, 0, stream, a);
+    else
+      ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, kAct, 2, 4, 4, false>), blocks, kNarrowThreads, 0, stream, a);
+    ABCD_HIP(hipGetLastError());
+    return ABCD_OK;
+  });
 }
 
 template <typename T>
 int32_t run_narrow_bwd(const FfnNarrowBwd& a, int64_t blocks, hipStream_t stream) {
-  const bool whole = a.d % 8 == 0 && a.o % 8 == 0;
-  if (whole)
-    ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, 1, true>), blocks, kNarrowBwdThreads, 0, stream, a);
-  else
-    ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, 1, false>), blocks, kNarrowBwdThreads, 0, stream, a);
-  ABCD_HIP(hipGetLastError());
-  return ABCD_OK;
+  return with_act(a.act, [&](auto act) -> int32_t {
+    constexpr int kAct = decltype(act)::value;
+    if (a.d % 8 == 0 && a.h % 8 == 0 && a.o % 8 == 0)
+      ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, true>), blocks, kNarrowBwdThreads, 0, stream, a);
+    else
+      ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, false>), blocks, kNarrowBwdThreads, 0, stream, a);
+    ABCD_HIP(hipGetLastError());
+    return ABCD_OK;
+  });
 }
 
 }  // namespace

@@ -138,10 +138,11 @@ __device__ __forceinline__ uint32_t drop_bits(const DropKey& k, uint32_t row, ui
 template <int N>
 __device__ __forceinline__ Floats<N> drop_vec(Floats<N> v, const DropKey& k, uint32_t row, uint32_t col) {
   if (k.mode == 0) return v;
-  Floats<N> r;
+  Floats<N> r = 0.0f;
+  if (k.mode == 2) return r;
 #pragma unroll
   for (int q = 0; q < N / 4; ++q) {
-    const uint32_t bits = k.mode == 2 ? 0 : drop_bits(k, row, col / 4 + q);
+    const uint32_t bits = drop_bits(k, row, col / 4 + q);
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[4 * q + i] = (bits >> i & 1) ? v[4 * q + i] * k.scale : 0.0f;
   }
