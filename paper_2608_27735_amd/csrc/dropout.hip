@@ -34,8 +34,7 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropArgs a) {
       Floats<N> v = load_vec<T, N, kWhole>(x + c, a.d - c);
       Floats<N> r = 0.0f;
       if (res) r = load_vec<T, N, kWhole>(res + c, a.d - c);
-      v = drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c);
-      store_vec<T, N, kWhole>(y + c, res ? r + v : v, a.d - c);
+      store_vec<T, N, kWhole>(y + c, drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c, r), a.d - c);
     }
   }
 }

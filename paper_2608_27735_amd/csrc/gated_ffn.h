@@ -112,8 +112,9 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_out_kernel(FfnOu
       __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
       const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
       if (r >= a.hidden.len) continue;
-      f32x4 y = drop_vec<4>(p.acc[x][w] + b, a.key, (uint32_t)r, (uint32_t)c);
-      if (a.res) y = load4<T>(a.res, r * a.ldr + c, left) + y;
+      f32x4 y = 0.0f;
+      if (a.res) y = load4<T>(a.res, r * a.ldr + c, left);
+      y = drop_vec<4>(p.acc[x][w] + b, a.key, (uint32_t)r, (uint32_t)c, y);
       store_vec<T, 4, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, (int)(left > 4 ? 4 : left));
     }
   }

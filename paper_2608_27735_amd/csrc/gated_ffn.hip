@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kBlock) void pack_rows_kernel(PackArgs a) {
     for (int c = t * N; c < a.ldd; c += a.lanes * N) {
       Floats<N> v = 0.0f;
       if (c < a.cols) v = load_vec<T, N, false>(s + c, a.cols - c);
-      store_vec<T, N, true>(d + c, drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c), N);
+      store_vec<T, N, true>(d + c, drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c, 0.0f), N);
     }
   }
 }
@@ -140,7 +140,7 @@ bool narrow(const abcd_ffn& f, int64_t n) {
   return f.dtype != ABCD_F32 && f.d <= 64 && f.o <= 64 && f.h <= 128 && n >= 1024;
 }
 constexpr int64_t kCUs = 256;
-int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 127) / 128, 3 * kCUs); }
+int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 255) / 256, 2 * kCUs); }
 int64_t narrow_bwd_blocks(int64_t n) { return std::min<int64_t>((n + 63) / 64, kCUs); }
 int64_t narrow_sums(const abcd_ffn& f) { return 2 * f.h * f.d + f.o * f.h + 2 * f.h + f.o; }
 

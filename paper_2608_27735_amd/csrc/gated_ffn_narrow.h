@@ -69,17 +69,18 @@ __device__ __forceinline__ T at_or_0(const void* m, int row, int col, int rows, 
   return *(in ? static_cast<const T*>(m) + (int64_t)row * cols + col : reinterpret_cast<const T*>(zeros));
 }
 
-constexpr int kNarrowThreads = 256, kNarrowBwdThreads = 512;
+constexpr int kNarrowThreads = 512, kNarrowBwdThreads = 512;
 
 // kWhole: d, h and o are multiples of 8. kDF: contractions of 32 that hold d; kOB: 16-column blocks of o; kHC: 32-column
 // chunks of h
 template <typename T, int kAct, int kDF, int kOB, int kHC, bool kWhole>
-__global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow a) {
+__global__ __launch_bounds__(kNarrowThreads, 4) void ffn_narrow_kernel(FfnNarrow a) {
   typedef typename Frag<T>::type F;
   constexpr int kNarrowWaves = kNarrowThreads / 64, kRowFrags = 2, kRows = kRowFrags * 16;
   constexpr int kChunk = 4 * kDF + kOB;  // fragments of a chunk: gate, up, down
   __shared__ __align__(16) F weights[kHC * kChunk * 64];
   __shared__ __align__(16) float bias[2][kHC * 32];
+  __shared__ __align__(16) float bias_down[kOB * 16];
   const int d = (int)a.d, h = (int)a.h, o = (int)a.o;
   constexpr int kTurns = kHC * kChunk * 64 / kNarrowThreads;
   static_assert(kHC * kChunk * 64 % kNarrowThreads == 0, "every thread sets up as many");
@@ -121,6 +122,9 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
     const T* b = static_cast<const T*>(s < kHC * 32 ? a.b_gate : a.b_up);
     bias[s / (kHC * 32)][c] = b && c < h ? (float)b[c] : 0.0f;
   }
+  if (threadIdx.x < kOB * 16)
+    bias_down[threadIdx.x] =
+        a.b_down && threadIdx.x < a.o ? (float)static_cast<const T*>(a.b_down)[threadIdx.x] : 0.0f;
   __syncthreads();
   const int l = threadIdx.x & 63, j = l & 15, q = l >> 4;
   const int64_t step = (int64_t)gridDim.x * kNarrowWaves * kRows;
@@ -137,15 +141,9 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
       }
     }
   };
-  F next[kRowFrags][kDF];
-  fetch(r0, next);
   for (; r0 < a.n; r0 += step) {
     F x[kRowFrags][kDF];
-#pragma unroll
-    for (int i = 0; i < kRowFrags; ++i)
-#pragma unroll
-      for (int f = 0; f < kDF; ++f) x[i][f] = next[i][f];
-    fetch(r0 + step, next);
+    fetch(r0, x);
     F res[kRowFrags][kOB / 2];  // on its way while the products run
     if (a.res)
 #pragma unroll
@@ -160,7 +158,7 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
 #pragma unroll
     for (int i = 0; i < kRowFrags; ++i)
 #pragma unroll
-      for (int b = 0; b < kOB; ++b) y[i][b] = 0.0f;
+      for (int b = 0; b < kOB; ++b) y[i][b] = *reinterpret_cast<const f32x4*>(&bias_down[q * (kOB * 4) + b * 4]);
     for (int c = 0; c < chunks; ++c) {
       const F* w = weights + c * kChunk * 64 + l;
       f32x4 g[kRowFrags][2], u[kRowFrags][2];
@@ -205,14 +203,17 @@ __global__ __launch_bounds__(kNarrowThreads, 3) void ffn_narrow_kernel(FfnNarrow
       if (r >= a.n) continue;
 #pragma unroll
       for (int b = 0; b < kOB; b += 2) {
+        __builtin_amdgcn_sched_barrier(0);  // one at a time, for the registers' sake
         const int c = q * (kOB * 4) + b * 4, left = o - c;
         if (left <= 0) continue;
         Floats<8> v;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = y[i][b + e / 4][e % 4];
-        if (a.b_down) v += load_vec<T, 8, kWhole>(static_cast<const T*>(a.b_down) + c, left);
-        v = drop_vec<8>(v, a.key, (uint32_t)r, (uint32_t)c);
-        if (a.res) v = __builtin_convertvector(res[i][b / 2], Floats<8>) + v;
+        uint32_t at = (uint32_t)c;
+        asm volatile("" : "+v"(at));  // keeps the generator's first round out of registers between rows
+        Floats<8> add = 0.0f;
+        if (a.res) add = __builtin_convertvector(res[i][b / 2], Floats<8>);
+        v = drop_vec<8>(v, a.key, (uint32_t)r, at, add);
         store_vec<T, 8, kWhole>(static_cast<T*>(a.y) + r * a.ldy + c, v, left);
       }
     }
@@ -239,7 +240,7 @@ __device__ __forceinline__ typename Frag<T>::type read_across(LdsChar* lo, LdsCh
 }
 
 // d and o up to 64, h up to kHB * 128
-template <typename T, int kAct, int kHB, bool kWhole>
+template <typename T, int kAct, int kHB, bool kWhole, bool kDrop>
 __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(FfnNarrowBwd a) {
   typedef typename Frag<T>::type F;
   constexpr int kTile = 64 * 128, kH = kHB * 128;
@@ -315,17 +316,13 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     nx = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + lc, r < a.n ? d - lc : 0);
     nz = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + r * a.lddy + lc, r < a.n ? o - lc : 0);
   };
+  // dz of a block: what the forward kept of dy; the factor comes with the sums, at
+  // the end
   auto put = [&](int64_t block, int into) {
-    // the mask as it was in the forward; the factor of what is kept comes at the end
-    if (a.key.mode != 0) {
-      const uint32_t r = (uint32_t)(block * 64 + lr);
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        const uint32_t bits = a.key.mode == 2 ? 0 : drop_bits(a.key, r, lc / 4 + v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!(bits >> e & 1)) nz[4 * v + e] = (T)0.0f;
-      }
+    if (kDrop) {
+      typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+      const uint4 m = drop_masks(a.key, (uint32_t)(block * 64 + lr), lc);
+      nz = __builtin_bit_cast(F, __builtin_bit_cast(U4, nz) & U4{m.x, m.y, m.z, m.w});
     }
     *reinterpret_cast<F*>(xs[into] + row_at(lr, lc / 4)) = nx;
     *reinterpret_cast<F*>(zs[into] + row_at(lr, lc / 4)) = nz;
@@ -343,105 +340,116 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     read_lo[i] = turned_at(row, unit);
     read_hi[i] = turned_at(row + 4, unit);
   }
-  auto dx_of = [&](int64_t block, int from) {
-    f32x4 acc[2];
-    acc[0] = acc[1] = 0.0f;
-    LdsChar* const t = (LdsChar*)turned[from];
+  f32x4 ax[2];
+  // half of dx of a block whose dg and du lie at t
+  auto dx_half = [&](const LdsChar* t, int half) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int k = 0; k < kH / 32; ++k)
+      for (int k = half * kH / 64; k < (half + 1) * kH / 64; ++k)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          LdsChar* const at = t + (s * kH + k * 32) * 128;
-          acc[i] = mma(wx[s][k], read_across<T>(at + read_lo[i], at + read_hi[i]), acc[i]);
+          LdsChar* const at = const_cast<LdsChar*>(t) + (s * kH + k * 32) * 128;
+          ax[i] = mma(wx[s][k], read_across<T>(at + read_lo[i], at + read_hi[i]), ax[i]);
         }
+  };
+  auto dx_store = [&](int64_t block) {
     const int c = xb * 16 + q * 4, left = d - c;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t r = block * 64 + xr * 32 + i * 16 + j;
-      if (a.dx && r < a.n && left > 0)
-        store_vec<T, 4, kWhole>(static_cast<T*>(a.dx) + r * a.lddx + c, acc[i] * a.scale, left);
+      if (a.dx && r >= 0 && r < a.n && left > 0)
+        store_vec<T, 4, kWhole>(static_cast<T*>(a.dx) + r * a.lddx + c, ax[i] * a.scale, left);
     }
+  };
+  // 32 rows of a block: g, u and dh, from these dg, du and h, which stay in registers
+  // for the weights' gradients; dg and du also go to t
+  auto half_of = [&](LdsChar* x, LdsChar* z, LdsChar* t, int half) {
+    F dg[kHB], du[kHB], hid[kHB];
+#pragma unroll
+    for (int b = 0; b < kHB; ++b) {
+      f32x4 vg[2], vu[2], vh[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = (half * 32 + i * 16) * 128;
+        f32x4 g = bg[b], u = bu[b], dh = 0.0f;
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const F fx = *(LdsF*)(x + row + along[f]);
+          const F fz = *(LdsF*)(z + row + along[f]);
+          g = mma(fx, wg[b][f], g);
+          u = mma(fx, wu[b][f], u);
+          dh = mma(fz, wd[b][f], dh);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float slope;
+          const float v = activate<kAct>(g[e], slope);
+          vh[i][e] = v * u[e];
+          vg[i][e] = dh[e] * (u[e] * slope);
+          vu[i][e] = dh[e] * v;
+        }
+      }
+      dg[b] = join<T>(vg[0], vg[1]);
+      du[b] = join<T>(vu[0], vu[1]);
+      hid[b] = join<T>(vh[0], vh[1]);
+      const int col = (wave * kHB + b) * 16 + j;
+      typedef typename VecOf<T, 4>::type V4;
+      typedef __attribute__((address_space(3))) V4 LdsV4;
+      const int unit = half * 8 + q;
+      *(LdsV4*)(t + turned_at(col, unit)) = __builtin_shufflevector(dg[b], dg[b], 0, 1, 2, 3);
+      *(LdsV4*)(t + turned_at(col, unit + 4)) = __builtin_shufflevector(dg[b], dg[b], 4, 5, 6, 7);
+      *(LdsV4*)(t + turned_at(kH + col, unit)) = __builtin_shufflevector(du[b], du[b], 0, 1, 2, 3);
+      *(LdsV4*)(t + turned_at(kH + col, unit + 4)) = __builtin_shufflevector(du[b], du[b], 4, 5, 6, 7);
+      sg[b] = mma(ones, dg[b], sg[b]);
+      su[b] = mma(ones, du[b], su[b]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // column 16 k + j, rows half 32 + 4 q .. + 3 and 16 further on
+      const int at = half * 32 * 128 + across[k];
+      const F fx = read_across<T>(x + at, x + at + 16 * 128);
+      const F fz = read_across<T>(z + at, z + at + 16 * 128);
+#pragma unroll
+      for (int b = 0; b < kHB; ++b) {
+        dwg[b][k] = mma(fx, dg[b], dwg[b][k]);
+        dwu[b][k] = mma(fx, du[b], dwu[b][k]);
+        dwd[b][k] = mma(fz, hid[b], dwd[b][k]);
+      }
+    }
+    const int at = half * 32 * 128 + across_z;
+    sz = mma(read_across<T>(z + at, z + at + 16 * 128), ones, sz);
+  };
+  // A block: its own two halves, and dx of the one before, whose dg and du are whole.
+  // The buffers do not overlap.
+  auto turn = [&](LdsChar* __restrict__ x, LdsChar* __restrict__ z, LdsChar* __restrict__ t,
+                  const LdsChar* __restrict__ before) {
+    ax[0] = ax[1] = 0.0f;
+    dx_half(before, 0);
+    half_of(x, z, t, 0);
+    dx_half(before, 1);
+    half_of(x, z, t, 1);
   };
 
   const int64_t blocks = (a.n + 63) / 64;
   int64_t block = blockIdx.x, last = -1;
   int cur = 0;
-  if (block < blocks) {
-    fetch(block);
-    put(block, 0);
-  }
+  fetch(block);
+  put(block, 0);
   for (; block < blocks; block += gridDim.x, cur ^= 1) {
     const int64_t next = block + gridDim.x;
     __syncthreads();  // this block's rows are in LDS, and so are the last one's dg and du
-    if (next < blocks) fetch(next);
-    LdsChar* const x = (LdsChar*)xs[cur];
-    LdsChar* const z = (LdsChar*)zs[cur];
-    LdsChar* const t = (LdsChar*)turned[cur];
-#pragma unroll 1
-    for (int half = 0; half < 2; ++half) {  // 32 rows at a time
-      F dg[kHB], du[kHB], hid[kHB];
-#pragma unroll
-      for (int b = 0; b < kHB; ++b) {
-        f32x4 vg[2], vu[2], vh[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int row = (half * 32 + i * 16) * 128;
-          f32x4 g = bg[b], u = bu[b], dh = 0.0f;
-#pragma unroll
-          for (int f = 0; f < 2; ++f) {
-            const F ax = *(LdsF*)(x + row + along[f]);
-            const F az = *(LdsF*)(z + row + along[f]);
-            g = mma(ax, wg[b][f], g);
-            u = mma(ax, wu[b][f], u);
-            dh = mma(az, wd[b][f], dh);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float slope;
-            const float v = activate<kAct>(g[e], slope);
-            vh[i][e] = v * u[e];
-            vg[i][e] = dh[e] * (u[e] * slope);
-            vu[i][e] = dh[e] * v;
-          }
-        }
-        dg[b] = join<T>(vg[0], vg[1]);
-        du[b] = join<T>(vu[0], vu[1]);
-        hid[b] = join<T>(vh[0], vh[1]);
-        const int col = (wave * kHB + b) * 16 + j;
-        typedef typename VecOf<T, 4>::type V4;
-        typedef __attribute__((address_space(3))) V4 LdsV4;
-        const int unit = half * 8 + q;
-        *(LdsV4*)(t + turned_at(col, unit)) = __builtin_shufflevector(dg[b], dg[b], 0, 1, 2, 3);
-        *(LdsV4*)(t + turned_at(col, unit + 4)) = __builtin_shufflevector(dg[b], dg[b], 4, 5, 6, 7);
-        *(LdsV4*)(t + turned_at(kH + col, unit)) = __builtin_shufflevector(du[b], du[b], 0, 1, 2, 3);
-        *(LdsV4*)(t + turned_at(kH + col, unit + 4)) = __builtin_shufflevector(du[b], du[b], 4, 5, 6, 7);
-        sg[b] = mma(ones, dg[b], sg[b]);
-        su[b] = mma(ones, du[b], su[b]);
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // column 16 k + j, rows half 32 + 4 q .. + 3 and 16 further on
-        const int at = half * 32 * 128 + across[k];
-        const F ax = read_across<T>(x + at, x + at + 16 * 128);
-        const F az = read_across<T>(z + at, z + at + 16 * 128);
-#pragma unroll
-        for (int b = 0; b < kHB; ++b) {
-          dwg[b][k] = mma(ax, dg[b], dwg[b][k]);
-          dwu[b][k] = mma(ax, du[b], dwu[b][k]);
-          dwd[b][k] = mma(az, hid[b], dwd[b][k]);
-        }
-      }
-      const int at = half * 32 * 128 + across_z;
-      sz = mma(read_across<T>(z + at, z + at + 16 * 128), ones, sz);
-    }
-    if (last >= 0) dx_of(last, cur ^ 1);
+    fetch(next);      // past the end: zeros
+    turn((LdsChar*)xs[cur], (LdsChar*)zs[cur], (LdsChar*)turned[cur], (LdsChar*)turned[cur ^ 1]);
+    dx_store(last);  // the first turn's is of no block: its rows are below 0
     last = block;
-    if (next < blocks) put(next, cur ^ 1);
+    put(next, cur ^ 1);
   }
   __syncthreads();
-  if (last >= 0) dx_of(last, cur ^ 1);
+  ax[0] = ax[1] = 0.0f;
+  dx_half((LdsChar*)turned[cur ^ 1], 0);
+  dx_half((LdsChar*)turned[cur ^ 1], 1);
+  dx_store(last);
 
   // sums: [dWg h x d][dWu h x d][dWd o x h][dbg h][dbu h][dbd o]
   float* const part = a.part + (int64_t)blockIdx.x * a.sums;
@@ -491,10 +499,20 @@ template <typename T>
 int32_t run_narrow_bwd(const FfnNarrowBwd& a, int64_t blocks, hipStream_t stream) {
   return with_act(a.act, [&](auto act) -> int32_t {
     constexpr int kAct = decltype(act)::value;
-    if (a.d % 8 == 0 && a.h % 8 == 0 && a.o % 8 == 0)
-      ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, true>), blocks, kNarrowBwdThreads, 0, stream, a);
+    const bool whole = a.d % 8 == 0 && a.h % 8 == 0 && a.o % 8 == 0;
+    auto launch = [&](auto drop) {
+      constexpr bool kDrop = decltype(drop)::value;
+      if (whole)
+        ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, true, kDrop>), blocks, kNarrowBwdThreads, 0,
+                    stream, a);
+      else
+        ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, false, kDrop>), blocks, kNarrowBwdThreads, 0,
+                    stream, a);
+    };
+    if (a.key.mode != 0)
+      launch(std::true_type{});
     else
-      ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, false>), blocks, kNarrowBwdThreads, 0, stream, a);
+      launch(std::false_type{});
     ABCD_HIP(hipGetLastError());
     return ABCD_OK;
   });

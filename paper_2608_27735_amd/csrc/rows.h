@@ -116,37 +116,54 @@ inline DropKey drop_key(double p, uint64_t seed, uint64_t offset) {
   return k;
 }
 
-// Which of the elements (row, 4 quad + 0..3) are kept, as bits 0 to 3.
-__device__ __forceinline__ uint32_t drop_bits(const DropKey& k, uint32_t row, uint32_t quad) {
+// Its four words for the elements (row, 4 quad + 0..3).
+__device__ __forceinline__ uint4 drop_words(const DropKey& k, uint32_t row, uint32_t quad) {
+  constexpr int kXor3 = 0x96;
   uint32_t c0 = quad, c1 = row, c2 = k.o0, c3 = k.o1, k0 = k.k0, k1 = k.k1;
 #pragma unroll
   for (int r = 0; r < 7; ++r) {
     const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(b >> 32), c1, k0, kXor3);
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(a >> 32), c3, k1, kXor3);
     c3 = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  return (c0 >= k.below ? 1u : 0u) | (c1 >= k.below ? 2u : 0u) | (c2 >= k.below ? 4u : 0u) |
-         (c3 >= k.below ? 8u : 0u);
+  return make_uint4(c0, c1, c2, c3);
 }
 
-// Dropout of N consecutive elements (a multiple of 4) from column col, a multiple
-// of 4. What is dropped becomes 0, infinities and NaN too.
+// add + dropout of N consecutive elements (a multiple of 4) from column col, a
+// multiple of 4. What is dropped becomes 0, infinities and NaN too.
 template <int N>
-__device__ __forceinline__ Floats<N> drop_vec(Floats<N> v, const DropKey& k, uint32_t row, uint32_t col) {
-  if (k.mode == 0) return v;
-  Floats<N> r = 0.0f;
-  if (k.mode == 2) return r;
+__device__ __forceinline__ Floats<N> drop_vec(Floats<N> v, const DropKey& k, uint32_t row, uint32_t col,
+                                              Floats<N> add) {
+  if (k.mode == 0) return add + v;
+  if (k.mode == 2) return add;
+  Floats<N> r;
 #pragma unroll
   for (int q = 0; q < N / 4; ++q) {
-    const uint32_t bits = drop_bits(k, row, col / 4 + q);
+    const uint4 w = drop_words(k, row, col / 4 + q);
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[4 * q + i] = (bits >> i & 1) ? v[4 * q + i] * k.scale : 0.0f;
+    for (int i = 0; i < 4; ++i)
+      r[4 * q + i] = fmaf(word[i] >= k.below ? v[4 * q + i] : 0.0f, k.scale, add[4 * q + i]);
   }
   return r;
+}
+
+// The same of 8 elements of 16 bits, two a word, without the factor: masks of what is
+// kept.
+__device__ __forceinline__ uint4 drop_masks(const DropKey& k, uint32_t row, uint32_t col) {
+  if (k.mode == 2) return make_uint4(0, 0, 0, 0);
+  uint32_t m[4];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const uint4 w = drop_words(k, row, col / 4 + q);
+    m[2 * q] = (w.x >= k.below ? 0xFFFFu : 0u) | (w.y >= k.below ? 0xFFFF0000u : 0u);
+    m[2 * q + 1] = (w.z >= k.below ? 0xFFFFu : 0u) | (w.w >= k.below ? 0xFFFF0000u : 0u);
+  }
+  return make_uint4(m[0], m[1], m[2], m[3]);
 }
 
 }  // namespace abcd
