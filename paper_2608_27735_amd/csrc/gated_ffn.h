@@ -22,6 +22,7 @@
 
 #include "activation.h"
 #include "gated_ffn_args.h"
+#include "gated_ffn_few.h"
 #include "gemm.h"
 
 namespace abcd {
@@ -275,6 +276,8 @@ int32_t run_dweight(FfnDWeight a, int splits, hipStream_t stream) {
 
 #define ABCD_FFN_KERNELS(NAME, TYPE)                                                                   \
   int32_t ffn_in_##NAME(const FfnIn& a, hipStream_t s) { return run_in<TYPE>(a, s); }                  \
+  int32_t ffn_few_in_##NAME(const FfnIn& a, hipStream_t s) { return run_few_in<TYPE>(a, s); }          \
+  int32_t ffn_few_out_##NAME(const FfnOut& a, hipStream_t s) { return run_few_out<TYPE>(a, s); }       \
   int32_t ffn_out_##NAME(const FfnOut& a, hipStream_t s) { return run_out<TYPE>(a, s); }               \
   int32_t ffn_dhidden_##NAME(const FfnDHidden& a, hipStream_t s) { return run_dhidden<TYPE>(a, s); }   \
   int32_t ffn_dx_##NAME(const FfnDX& a, hipStream_t s) { return run_dx<TYPE>(a, s); }                  \

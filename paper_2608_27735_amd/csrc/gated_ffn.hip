@@ -139,6 +139,8 @@ int splits_down(const abcd_ffn& f, int64_t n) { return splits_for(tiles128(f.o, 
 bool narrow(const abcd_ffn& f, int64_t n) {
   return f.dtype != ABCD_F32 && f.d <= 64 && f.o <= 64 && f.h <= 128 && n >= 1024;
 }
+// Whether the kernels for a few rows take the forward.
+bool few(int64_t n) { return n <= 64; }
 constexpr int64_t kCUs = 256;
 int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 255) / 256, 2 * kCUs); }
 int64_t narrow_bwd_blocks(int64_t n) { return std::min<int64_t>((n + 63) / 64, kCUs); }
@@ -151,6 +153,11 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
   Scratch s{};
   if (!saved && narrow(f, n)) {
     if (backward) s.part = static_cast<float*>(p.take(narrow_bwd_blocks(n) * narrow_sums(f) * sizeof(float)));
+    s.bytes = p.used;
+    return s;
+  }
+  if (!backward && few(n)) {
+    if (!saved) s.hidden = p.take(n * hp * sz);
     s.bytes = p.used;
     return s;
   }
@@ -207,6 +214,13 @@ int32_t gate_up(const abcd_ffn& f, const Scratch& s, Side& w, hipStream_t stream
   return pack(f.dtype, f.h, f.d, f.w_up, f.d, s.wu, w.ld, DropKey{}, stream);
 }
 
+int32_t few_in(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx, void* by_gate, void* by_up, void* hidden,
+               hipStream_t stream) {
+  const FfnIn in{Side{{x, nullptr}, ldx, n}, Side{{f.w_gate, f.w_up}, f.d, f.h}, f.b_gate, f.b_up, hidden, by_gate,
+                 by_up, f.d, f.h, up8(f.h), f.act, 0, 0};
+  return FFN_BY_TYPE(f, ffn_few_in, in, stream);
+}
+
 }  // namespace
 
 bool gated_ffn_keeps(const abcd_ffn& f, int64_t n) { return !narrow(f, n); }
@@ -228,14 +242,18 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
   const Scratch s = layout(f, n, hidden != nullptr, false, workspace);
   if (!hidden) hidden = s.hidden;
   const int64_t hp = up8(f.h);
+  FfnOut out{Side{{hidden, nullptr}, hp, n}, Side{{f.w_down, nullptr}, f.h, f.o}, f.b_down, residual, y, f.h, f.o, ldr,
+             ldy, drop_key(f.p, f.seed, f.offset), 0, 0};
+  if (few(n)) {
+    TRY_STATUS(few_in(f, n, x, ldx, by_gate, by_up, hidden, stream));
+    return FFN_BY_TYPE(f, ffn_few_out, out, stream);
+  }
   Side xs, w;
   TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
   TRY_STATUS(gate_up(f, s, w, stream));
   const FfnIn in{xs, w, f.b_gate, f.b_up, hidden, by_gate, by_up, f.d, f.h, hp, f.act, 0, 0};
   TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
-  TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, w, stream));
-  const FfnOut out{Side{{hidden, nullptr}, hp, n}, w, f.b_down, residual, y, f.h, f.o, ldr, ldy,
-                   drop_key(f.p, f.seed, f.offset), 0, 0};
+  TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, out.w, stream));
   return FFN_BY_TYPE(f, ffn_out, out, stream);
 }
 
@@ -275,7 +293,12 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     } else {
       TRY_STATUS(rows_of(f, dy, n, f.o, lddy, s.dz, dz, stream));
     }
-    if (!hidden) {
+    if (!hidden && few(n)) {
+      TRY_STATUS(few_in(f, n, x, ldx, s.gate, s.up, s.hidden, stream));
+      by_gate = s.gate;
+      by_up = s.up;
+      hidden = s.hidden;
+    } else if (!hidden) {
       const FfnIn in{xs, wgu, f.b_gate, f.b_up, s.hidden, s.gate, s.up, f.d, f.h, hp, f.act, 0, 0};
       TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
       by_gate = s.gate;

@@ -91,6 +91,8 @@ int32_t ffn_narrow_bwd_bf16(const FfnNarrowBwd&, int64_t blocks, hipStream_t);
 
 #define ABCD_FFN_DECLARE(NAME)                                 \
   int32_t ffn_in_##NAME(const FfnIn&, hipStream_t);            \
+  int32_t ffn_few_in_##NAME(const FfnIn&, hipStream_t);        \
+  int32_t ffn_few_out_##NAME(const FfnOut&, hipStream_t);      \
   int32_t ffn_out_##NAME(const FfnOut&, hipStream_t);          \
   int32_t ffn_dhidden_##NAME(const FfnDHidden&, hipStream_t);  \
   int32_t ffn_dx_##NAME(const FfnDX&, hipStream_t);            \
