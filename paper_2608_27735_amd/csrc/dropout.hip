@@ -7,7 +7,7 @@
 // generator in 16-bit types, one in 32), columns along the lanes.
 #include <algorithm>
 
-#include "rows.h"
+#include "load_frag.h"
 
 namespace abcd {
 namespace {
@@ -31,9 +31,11 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropArgs a) {
     const T* res = a.res ? static_cast<const T*>(a.res) + row * a.ldr : nullptr;
     T* y = static_cast<T*>(a.y) + row * a.ldy;
     for (int c = t * N; c < a.d; c += a.lanes * N) {
-      Floats<N> v = load_vec<T, N, kWhole>(x + c, a.d - c);
+      const int64_t below = a.n - 1 - row, left = a.d - c;
+      const Floats<N> v =
+          __builtin_convertvector(load_frag<T, kWhole>(x + c, left, below * a.ldx + left), Floats<N>);
       Floats<N> r = 0.0f;
-      if (res) r = load_vec<T, N, kWhole>(res + c, a.d - c);
+      if (res) r = __builtin_convertvector(load_frag<T, kWhole>(res + c, left, below * a.ldr + left), Floats<N>);
       store_vec<T, N, kWhole>(y + c, drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c, r), a.d - c);
     }
   }

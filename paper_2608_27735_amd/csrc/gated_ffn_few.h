@@ -38,10 +38,12 @@ __device__ __forceinline__ void few_products(f32x4 (&acc)[kX][kSides], const T* 
       const int k = (s0 + t) * kK + q * kPer, left = s0 + t < end ? k_end - k : 0;
 #pragma unroll
       for (int s = 0; s < kSides; ++s)
-        fw[s][t] = load_frag<T, kWhole>(w[s] + (int64_t)(first + j) * ldw + k, first + j < rows ? left : 0);
+        fw[s][t] = load_frag<T, kWhole>(w[s] + (int64_t)(first + j) * ldw + k, first + j < rows ? left : 0,
+                                        (int64_t)(rows - 1 - first - j) * ldw + left);
 #pragma unroll
       for (int i = 0; i < kX; ++i)
-        fx[i][t] = load_frag<T, kWhole>(x + (int64_t)(i * 16 + j) * ldx + k, i * 16 + j < n ? left : 0);
+        fx[i][t] = load_frag<T, kWhole>(x + (int64_t)(i * 16 + j) * ldx + k, i * 16 + j < n ? left : 0,
+                                        (int64_t)(n - 1 - i * 16 - j) * ldx + left);
     }
 #pragma unroll
     for (int t = 0; t < kAhead; ++t)

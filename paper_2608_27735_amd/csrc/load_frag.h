@@ -17,14 +17,32 @@ __device__ __forceinline__ typename Frag<T>::type load_whole(const T* p, bool in
   typedef F FU __attribute__((aligned(sizeof(T))));
   return *reinterpret_cast<const FU*>(in ? p : reinterpret_cast<const T*>(zeros));
 }
-// The same where only n of them may be there (n <= 0: none).
+// The first n elements of v, and zeros.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type keep_first(typename Frag<T>::type v, int n) {
+  typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+  U4 m;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4)
+      m[i] = n > i ? ~0u : 0u;
+    else
+      m[i] = n >= 2 * i + 2 ? ~0u : n == 2 * i + 1 ? 0xFFFFu : 0u;
+  }
+  return __builtin_bit_cast(typename Frag<T>::type, __builtin_bit_cast(U4, v) & m);
+}
+
+// 16 bytes from p of which n elements are wanted (n <= 0: none), the others 0; kWhole:
+// all or none. room: elements from p to the end of the array: where it reaches over 16
+// bytes what lies behind the row is loaded and masked, so that only the array's last
+// elements take single loads.
 template <typename T, bool kWhole>
-__device__ __forceinline__ typename Frag<T>::type load_frag(const T* p, int n) {
-  if (kWhole || n >= kPer16<T> || n <= 0) return load_whole(p, n > 0);
+__device__ __forceinline__ typename Frag<T>::type load_frag(const T* p, int n, int64_t room) {
+  if (kWhole) return load_whole(p, n > 0);
+  if (n >= kPer16<T> || n <= 0 || room >= kPer16<T>) return keep_first<T>(load_whole(p, n > 0), n);
   typename Frag<T>::type v = (T)0.0f;
 #pragma unroll
-  for (int i = 0; i < kPer16<T> - 1; ++i)
-    if (i < n) v[i] = p[i];
+  for (int i = 0; i < kPer16<T> - 1; ++i) v[i] = *(i < n ? p + i : reinterpret_cast<const T*>(zeros));
   return v;
 }
 
