@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kBlock) void pack_rows_kernel(PackArgs a) {
     for (int c = t * N; c < a.ldd; c += a.lanes * N) {
       const int left = a.cols - c;
       const Floats<N> v =
-          __builtin_convertvector(load_frag<T, false>(s + c, left, (a.n - 1 - row) * a.ld + left), Floats<N>);
+          __builtin_convertvector((load_first<T, false>(s + c, left, (a.n - 1 - row) * a.ld + left)), Floats<N>);
       store_vec<T, N, true>(d + c, drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c, 0.0f), N);
     }
   }
@@ -48,8 +48,8 @@ __global__ __launch_bounds__(kBlock) void column_sums_kernel(const void* m, int6
   Floats<N> s = 0.0f;
   if (c < cols)
     for (int64_t row = (int64_t)blockIdx.y * rows + threadIdx.x / lanes; row < n; row += (int64_t)gridDim.y * rows)
-      s += __builtin_convertvector(load_frag<T, false>(static_cast<const T*>(m) + row * ld + c, cols - c,
-                                                       (n - 1 - row) * ld + cols - c),
+      s += __builtin_convertvector((load_first<T, false>(static_cast<const T*>(m) + row * ld + c, cols - c,
+                                                         (n - 1 - row) * ld + cols - c)),
                                    Floats<N>);
 #pragma unroll
   for (int i = 0; i < N; ++i) red[threadIdx.x * N + i] = s[i];

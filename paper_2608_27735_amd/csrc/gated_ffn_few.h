@@ -46,11 +46,18 @@ __device__ __forceinline__ void few_products(f32x4 (&acc)[kX][kSides], const T* 
                                         (int64_t)(n - 1 - i * 16 - j) * ldx + left);
     }
 #pragma unroll
-    for (int t = 0; t < kAhead; ++t)
+    for (int t = 0; t < kAhead; ++t) {
+      // what is not of the contraction has to be zero on both sides
+      const int left = s0 + t < end ? k_end - ((s0 + t) * kK + q * kPer) : 0;
 #pragma unroll
-      for (int i = 0; i < kX; ++i)
+      for (int s = 0; s < kSides; ++s) fw[s][t] = first_of<T, kWhole>(fw[s][t], left);
+#pragma unroll
+      for (int i = 0; i < kX; ++i) {
+        fx[i][t] = first_of<T, kWhole>(fx[i][t], left);
 #pragma unroll
         for (int s = 0; s < kSides; ++s) acc[i][s] = mma(fw[s][t], fx[i][t], acc[i][s]);
+      }
+    }
   }
 }
 

@@ -124,6 +124,10 @@ __global__ __launch_bounds__(kNarrowThreads, 4) void ffn_narrow_kernel(FfnNarrow
   for (; r0 < a.n; r0 += step) {
     F x[kRowFrags][kDF];
     fetch(r0, x);
+#pragma unroll
+    for (int i = 0; i < kRowFrags; ++i)
+#pragma unroll
+      for (int f = 0; f < kDF; ++f) x[i][f] = first_of<T, kWhole>(x[i][f], d - (f * 32 + q * 8));
     F res[kRowFrags][kOB / 2];  // on its way while the products run
     if (a.res)
 #pragma unroll
@@ -248,11 +252,11 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 #pragma unroll
     for (int k = 0; k < kH / 64; ++k) {
       const int row = k * 64 + lr, col = k * 64 + lc;
-      const F g = load_frag<T, kWhole>(static_cast<const T*>(a.w_gate) + (int64_t)row * d + lc, row < h ? d - lc : 0,
+      const F g = load_first<T, kWhole>(static_cast<const T*>(a.w_gate) + (int64_t)row * d + lc, row < h ? d - lc : 0,
                                            (int64_t)(h - 1 - row) * d + d - lc);
-      const F u = load_frag<T, kWhole>(static_cast<const T*>(a.w_up) + (int64_t)row * d + lc, row < h ? d - lc : 0,
+      const F u = load_first<T, kWhole>(static_cast<const T*>(a.w_up) + (int64_t)row * d + lc, row < h ? d - lc : 0,
                                            (int64_t)(h - 1 - row) * d + d - lc);
-      const F w = load_frag<T, kWhole>(static_cast<const T*>(a.w_down) + (int64_t)lr * h + col, lr < o ? h - col : 0,
+      const F w = load_first<T, kWhole>(static_cast<const T*>(a.w_down) + (int64_t)lr * h + col, lr < o ? h - col : 0,
                                            (int64_t)(o - 1 - lr) * h + h - col);
       const int at = row_at(lr, lc / 4) + k * kTile;
       *(__attribute__((address_space(3))) F*)(t + at) = g;
@@ -310,6 +314,8 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
       const uint4 m = drop_masks(a.key, (uint32_t)(block * 64 + lr), lc);
       nz = __builtin_bit_cast(F, __builtin_bit_cast(U4, nz) & U4{m.x, m.y, m.z, m.w});
     }
+    nx = first_of<T, kWhole>(nx, d - lc);
+    nz = first_of<T, kWhole>(nz, o - lc);
     *reinterpret_cast<F*>(xs[into] + row_at(lr, lc / 4)) = nx;
     *reinterpret_cast<F*>(zs[into] + row_at(lr, lc / 4)) = nz;
   };

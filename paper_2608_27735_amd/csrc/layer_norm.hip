@@ -56,13 +56,17 @@ __global__ __launch_bounds__(kBlock) void layer_norm_kernel(NormArgs a) {
   const int64_t step = (int64_t)gridDim.x * kRows;
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G; row < a.n; row += step) {
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    typename Frag<T>::type raw[R];
     Floats<N> v[R];
     float s = 0.0f;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const int c = (j * G + t) * N;
-      v[j] = __builtin_convertvector(load_frag<T, kWhole>(x + c, a.d - c, (a.n - 1 - row) * a.ldx + a.d - c),
-                                     Floats<N>);
+      raw[j] = load_frag<T, kWhole>(x + c, a.d - c, (a.n - 1 - row) * a.ldx + a.d - c);
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      v[j] = __builtin_convertvector((first_of<T, kWhole>(raw[j], a.d - (j * G + t) * N)), Floats<N>);
 #pragma unroll
       for (int i = 0; i < N; ++i) s += v[j][i];
     }
@@ -194,8 +198,9 @@ __global__ __launch_bounds__(kBlock) void layer_norm_bwd_kernel(NormBwdArgs a) {
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-      z[j] = __builtin_convertvector(nx[j], Floats<N>);
-      v[j] = __builtin_convertvector(ndy[j], Floats<N>);
+      const int left = a.d - (j * G + t) * N;
+      z[j] = __builtin_convertvector((first_of<T, kWhole>(nx[j], left)), Floats<N>);
+      v[j] = __builtin_convertvector((first_of<T, kWhole>(ndy[j], left)), Floats<N>);
       add[j] = nadd[j];
     }
     if (kAhead) fetch(row + step);

@@ -6,10 +6,6 @@
 namespace abcd {
 namespace {
 
-// Where loads of what lies outside an array go: under a condition a load would be
-// waited for by itself, at the end of its branch.
-__device__ uint32_t zeros[4];
-
 // 16 bytes from p as they are where `in`, else 0.
 template <typename T>
 __device__ __forceinline__ typename Frag<T>::type load_whole(const T* p, bool in) {
@@ -17,9 +13,26 @@ __device__ __forceinline__ typename Frag<T>::type load_whole(const T* p, bool in
   typedef F FU __attribute__((aligned(sizeof(T))));
   return *reinterpret_cast<const FU*>(in ? p : reinterpret_cast<const T*>(zeros));
 }
-// The first n elements of v, and zeros.
-template <typename T>
-__device__ __forceinline__ typename Frag<T>::type keep_first(typename Frag<T>::type v, int n) {
+// 16 bytes from p of which n elements are wanted (n <= 0: none); kWhole: all or none.
+// The others come as they may (first_of makes zeros of them, once the load has to have
+// arrived anyway: done here it would be waited for at once). room: elements from p to
+// the end of the array: where it reaches over 16 bytes what lies behind the row is
+// loaded too, so that only the array's last elements take single loads.
+template <typename T, bool kWhole>
+__device__ __forceinline__ typename Frag<T>::type load_frag(const T* p, int n, int64_t room) {
+  const bool single = !kWhole && n > 0 && n < kPer16<T> && room < kPer16<T>;
+  typename Frag<T>::type v = load_whole(p, n > 0 && !single);
+  if (single) {
+#pragma unroll
+    for (int i = 0; i < kPer16<T> - 1; ++i) v[i] = *(i < n ? p + i : reinterpret_cast<const T*>(zeros));
+  }
+  return v;
+}
+
+// The first n elements of what load_frag gave, and zeros.
+template <typename T, bool kWhole>
+__device__ __forceinline__ typename Frag<T>::type first_of(typename Frag<T>::type v, int n) {
+  if (kWhole) return v;
   typedef uint32_t U4 __attribute__((ext_vector_type(4)));
   U4 m;
 #pragma unroll
@@ -32,18 +45,10 @@ __device__ __forceinline__ typename Frag<T>::type keep_first(typename Frag<T>::t
   return __builtin_bit_cast(typename Frag<T>::type, __builtin_bit_cast(U4, v) & m);
 }
 
-// 16 bytes from p of which n elements are wanted (n <= 0: none), the others 0; kWhole:
-// all or none. room: elements from p to the end of the array: where it reaches over 16
-// bytes what lies behind the row is loaded and masked, so that only the array's last
-// elements take single loads.
+// Both, for a load that is used at once.
 template <typename T, bool kWhole>
-__device__ __forceinline__ typename Frag<T>::type load_frag(const T* p, int n, int64_t room) {
-  if (kWhole) return load_whole(p, n > 0);
-  if (n >= kPer16<T> || n <= 0 || room >= kPer16<T>) return keep_first<T>(load_whole(p, n > 0), n);
-  typename Frag<T>::type v = (T)0.0f;
-#pragma unroll
-  for (int i = 0; i < kPer16<T> - 1; ++i) v[i] = *(i < n ? p + i : reinterpret_cast<const T*>(zeros));
-  return v;
+__device__ __forceinline__ typename Frag<T>::type load_first(const T* p, int n, int64_t room) {
+  return first_of<T, kWhole>(load_frag<T, kWhole>(p, n, room), n);
 }
 
 }  // namespace

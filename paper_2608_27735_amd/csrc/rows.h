@@ -31,6 +31,12 @@ int32_t with_type(int32_t dtype, F f) {
 inline size_t type_bytes(int32_t dtype) { return dtype == ABCD_F32 ? 4 : 2; }
 inline size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
 
+namespace {
+// Where loads of what lies outside an array go: under a condition a load would be
+// waited for by itself, at the end of its branch.
+__device__ uint32_t zeros[4];
+}  // namespace
+
 // N consecutive elements at p as floats, n of them within the row (the others
 // are 0 and are not read). One load if all are: gfx950 loads a vector from any
 // element's address, so rows of odd widths and strides need no other path.
@@ -40,7 +46,7 @@ __device__ __forceinline__ Floats<N> load_vec(const T* p, int n) {
   if (kWhole || n >= N) return __builtin_convertvector(*reinterpret_cast<const V*>(p), Floats<N>);
   Floats<N> r;
 #pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = i < n ? (float)p[i] : 0.0f;
+  for (int i = 0; i < N; ++i) r[i] = (float)*(i < n ? p + i : reinterpret_cast<const T*>(zeros));
   return r;
 }
 
