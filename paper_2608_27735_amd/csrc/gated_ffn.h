@@ -181,40 +181,63 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dx_kernel(FfnDX 
   }
 }
 
-// Weights' gradients: rows are X's index (of half tx >= tiles_x / 2 with two), the
-// contraction runs over rows [blockIdx.y per, + per).
+// Which product a tile of the weights' gradients belongs to, and its place there.
+__device__ __forceinline__ const FfnDWeight::One& dweight_at(const FfnDWeight& a, int tile, int& tx, int& tw) {
+  int k = 0;
+  while (k + 1 < a.count && tile >= a.one[k + 1].first) ++k;
+  tile_at(tile - a.one[k].first, a.one[k].tiles_x, a.one[k].tiles_w, tx, tw);
+  return a.one[k];
+}
+
 template <typename T, typename Cfg>
 __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dweight_kernel(FfnDWeight a) {
   typedef ProductOf<T, Cfg, false, false, false> P;
   ABCD_TILE_LDS(P);
+  const int b = blockIdx.x, rest = b - a.whole;
+  const int tile = rest < 0 ? xcd_order(b, a.whole) : a.whole + rest / a.splits;
   int tx, tw;
-  tile_of(blockIdx.x, a.halves * a.tiles_x, a.tiles_w, tx, tw);
-  const int half = tx >= a.tiles_x ? 1 : 0;
-  const int64_t ix = (int64_t)(tx - half * a.tiles_x) * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
-  const int64_t k0 = blockIdx.y * a.per, k1 = k0 + a.per < a.n ? k0 + a.per : a.n;
-  Side X = a.x;
-  X.p[0] = a.x.p[half];
+  const FfnDWeight::One& m = dweight_at(a, tile, tx, tw);
+  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
+  int64_t k0 = 0, k1 = a.n;
+  if (rest >= 0) {
+    k0 = rest % a.splits * a.per;
+    k1 = k0 + a.per < a.n ? k0 + a.per : a.n;
+  }
   P p;
-  p.template run<1>(X, a.w, ix, iw, k0, k1, lds0, lds1);
+  p.template run<1>(Side{{m.x, nullptr}, m.ldx, m.rows}, Side{{m.w, nullptr}, m.ldw, m.cols}, ix, iw, k0, k1, lds0,
+                    lds1);
   const int l = threadIdx.x & 63;
-  const int64_t cols = a.w.len, rows = a.x.len;
 #pragma unroll
   for (int w = 0; w < P::FW; ++w) {
-    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4, left = cols - c;
-    if (left <= 0) continue;
-    const int m = (int)(left > 4 ? 4 : left);
+    const int cw = P::unit_w(w) * 16 + (l >> 4) * 4;
+    const int64_t c = iw + cw, left = m.cols - c;
 #pragma unroll
     for (int x = 0; x < P::FX; ++x) {
       __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
-      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
-      if (r >= rows) continue;
-      if (a.part)
-        store_vec<float, 4, false>(a.part + ((blockIdx.y * a.halves + half) * rows + r) * cols + c, p.acc[x][w] * a.scale,
-                                   m);
-      else
-        store_vec<T, 4, false>(static_cast<T*>(half ? a.out1 : a.out0) + r * cols + c, p.acc[x][w] * a.scale, m);
+      const int rx = P::unit_x(x) * 16 + (l & 15);
+      if (rest >= 0)
+        *reinterpret_cast<f32x4*>(a.part + ((int64_t)rest * Cfg::TX + rx) * Cfg::TW + cw) = p.acc[x][w];
+      else if (ix + rx < m.rows && left > 0)
+        store_vec<T, 4, false>(static_cast<T*>(m.out) + (ix + rx) * m.cols + c, p.acc[x][w] * m.scale,
+                               (int)(left > 4 ? 4 : left));
     }
   }
+}
+
+// Tile blockIdx.x of those that were split: the sum of its parts, rows blockIdx.y 4 ..
+// + 3 of it by TW / 4 threads each.
+template <typename T, int TX, int TW>
+__global__ __launch_bounds__(TW) void ffn_dweight_sum_kernel(FfnDWeight a) {
+  int tx, tw;
+  const FfnDWeight::One& m = dweight_at(a, a.whole + blockIdx.x, tx, tw);
+  const int rx = blockIdx.y * 4 + threadIdx.x / (TW / 4), cw = threadIdx.x % (TW / 4) * 4;
+  const int64_t r = (int64_t)tx * TX + rx, c = (int64_t)tw * TW + cw, left = m.cols - c;
+  if (r >= m.rows || left <= 0) return;
+  const float* part = a.part + ((int64_t)blockIdx.x * a.splits * TX + rx) * TW + cw;
+  f32x4 s = 0.0f;
+#pragma unroll 4
+  for (int k = 0; k < a.splits; ++k) s += *reinterpret_cast<const f32x4*>(part + (int64_t)k * TX * TW);
+  store_vec<T, 4, false>(static_cast<T*>(m.out) + r * m.cols + c, s * m.scale, (int)(left > 4 ? 4 : left));
 }
 
 inline int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
@@ -258,18 +281,39 @@ int32_t run_dx(FfnDX a, hipStream_t stream) {
   ABCD_FFN_LAUNCH("ffn_dx", ffn_dx_kernel, a, a.dgu.len, a.d, 1, stream);
   return ABCD_OK;
 }
-template <typename T>
-int32_t run_dweight(FfnDWeight a, int splits, hipStream_t stream) {
-  const bool big = splits == 1 && use_big(a.halves * a.x.len, a.w.len, Big::TW);
-  a.tiles_x = (int)tiles(a.x.len, big ? Big::TX : Small::TX);
-  a.tiles_w = (int)tiles(a.w.len, big ? Big::TW : Small::TW);
-  const dim3 grid(a.halves * a.tiles_x * a.tiles_w, splits);
-  if (big)
-    ABCD_LAUNCH("ffn_dweight", (ffn_dweight_kernel<T, Big>), grid, Big::WX* Big::WW * 64, 0, stream, a);
-  else
-    ABCD_LAUNCH("ffn_dweight", (ffn_dweight_kernel<T, Small>), grid, Small::WX* Small::WW * 64, 0, stream, a);
+template <typename T, typename Cfg>
+int32_t run_dweight_tiles(FfnDWeight a, int slots, hipStream_t stream) {
+  int64_t total = 0;
+  for (int i = 0; i < a.count; ++i) {
+    a.one[i].tiles_x = (int)tiles(a.one[i].rows, Cfg::TX);
+    a.one[i].tiles_w = (int)tiles(a.one[i].cols, Cfg::TW);
+    a.one[i].first = (int)total;
+    total += (int64_t)a.one[i].tiles_x * a.one[i].tiles_w;
+  }
+  a.tiles = (int)total;
+  // As many tiles whole as make full rounds of the GPU; the rows of the others are
+  // split so that they make one more, but for at least 512 rows a part.
+  const int left = a.tiles % slots;
+  a.splits = left == 0 ? 1 : (int)std::min<int64_t>(slots / left, std::max<int64_t>(1, a.n / 512));
+  a.whole = a.splits > 1 ? a.tiles - left : a.tiles;
+  a.per = ((a.n + a.splits - 1) / a.splits + kStep<T> - 1) / kStep<T> * kStep<T>;
+  const int rest = a.tiles - a.whole;
+  ABCD_LAUNCH("ffn_dweight", (ffn_dweight_kernel<T, Cfg>), a.whole + rest * a.splits, Cfg::WX* Cfg::WW * 64, 0, stream,
+              a);
   ABCD_HIP(hipGetLastError());
+  if (rest > 0) {
+    ABCD_LAUNCH("ffn_dweight_sum", (ffn_dweight_sum_kernel<T, Cfg::TX, Cfg::TW>), dim3(rest, Cfg::TX / 4), Cfg::TW, 0,
+                stream, a);
+    ABCD_HIP(hipGetLastError());
+  }
   return ABCD_OK;
+}
+
+template <typename T>
+int32_t run_dweight(const FfnDWeight& a, hipStream_t stream) {
+  int64_t big = 0;
+  for (int i = 0; i < a.count; ++i) big += tiles(a.one[i].rows, Big::TX) * tiles(a.one[i].cols, Big::TW);
+  return big >= 192 ? run_dweight_tiles<T, Big>(a, kBigSlots, stream) : run_dweight_tiles<T, Small>(a, kSmallSlots, stream);
 }
 
 }  // namespace
@@ -281,8 +325,6 @@ int32_t run_dweight(FfnDWeight a, int splits, hipStream_t stream) {
   int32_t ffn_out_##NAME(const FfnOut& a, hipStream_t s) { return run_out<TYPE>(a, s); }               \
   int32_t ffn_dhidden_##NAME(const FfnDHidden& a, hipStream_t s) { return run_dhidden<TYPE>(a, s); }   \
   int32_t ffn_dx_##NAME(const FfnDX& a, hipStream_t s) { return run_dx<TYPE>(a, s); }                  \
-  int32_t ffn_dweight_##NAME(const FfnDWeight& a, int splits, hipStream_t s) {                         \
-    return run_dweight<TYPE>(a, splits, s);                                                            \
-  }
+  int32_t ffn_dweight_##NAME(const FfnDWeight& a, hipStream_t s) { return run_dweight<TYPE>(a, s); }
 
 }  // namespace abcd

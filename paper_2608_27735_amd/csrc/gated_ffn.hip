@@ -127,15 +127,10 @@ struct Scratch {
   size_t bytes;
 };
 
-// How many ways the rows are split for a weight gradient of `tiles` 128 x 128
-// tiles: about two workgroups per CU, each with at least 512 rows.
-int splits_for(int64_t tiles, int64_t n) {
-  const int64_t want = (512 + tiles - 1) / tiles, most = std::max<int64_t>(1, n / 512);
-  return (int)std::min<int64_t>({want, most, 256});
-}
-int64_t tiles128(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128); }
-int splits_gate_up(const abcd_ffn& f, int64_t n) { return splits_for(2 * tiles128(f.h, f.d), n); }
-int splits_down(const abcd_ffn& f, int64_t n) { return splits_for(tiles128(f.o, f.h), n); }
+// Room for the parts of the weights' gradients: no more than run at once, and none
+// where the rows are too few to split.
+size_t dweight_part(int64_t n) { return n < 1024 ? 0 : (size_t)kBigSlots * 256 * 256; }
+static_assert((size_t)kBigSlots * 256 * 256 >= (size_t)kSmallSlots * 128 * 128, "the large tiles' parts are the larger");
 
 // Whether the narrow kernels take the block: what they hold in registers and LDS,
 // in 16-bit types, and rows enough to share the cost of setting the weights up.
@@ -144,7 +139,6 @@ bool narrow(const abcd_ffn& f, int64_t n) {
 }
 // Whether the kernels for a few rows take the forward.
 bool few(int64_t n) { return n <= 64; }
-constexpr int64_t kCUs = 256;
 int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 255) / 256, 2 * kCUs); }
 int64_t narrow_bwd_blocks(int64_t n) { return std::min<int64_t>((n + 63) / 64, kCUs); }
 int64_t narrow_sums(const abcd_ffn& f) { return 2 * f.h * f.d + f.o * f.h + 2 * f.h + f.o; }
@@ -173,10 +167,8 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
     s.dz = p.take(n * op * sz);
     s.gate = p.take(n * hp * sz);
     s.up = p.take(n * hp * sz);
-    size_t part = sum_parts_of(n) * std::max(f.h, f.o);
-    const int sg = splits_gate_up(f, n), sd = splits_down(f, n);
-    if (sg > 1) part = std::max<size_t>(part, (size_t)sg * 2 * f.h * f.d);
-    if (sd > 1) part = std::max<size_t>(part, (size_t)sd * f.h * f.o);
+    size_t part = (size_t)sum_parts_of(n) * std::max(f.h, f.o);
+    part = std::max(part, dweight_part(n));
     s.part = static_cast<float*>(p.take(part * sizeof(float)));
   }
   s.bytes = p.used;
@@ -320,25 +312,16 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     const FfnDX a{dgu, Side{{wgu.p[0], wgu.p[1]}, wgu.ld, f.d}, dx, f.h, f.d, lddx, 0, 0};
     TRY_STATUS(FFN_BY_TYPE(f, ffn_dx, a, stream));
   }
-  auto dweight = [&](Side X, Side W, int halves, void* out0, void* out1, int splits, float factor) -> int32_t {
-    const int64_t rows = (n + splits - 1) / splits, per = (rows + 63) / 64 * 64;
-    FfnDWeight a{X, W, out0, out1, splits > 1 ? s.part : nullptr, factor, n, per, halves, 0, 0};
-    TRY_STATUS(FFN_BY_TYPE(f, ffn_dweight, a, splits, stream));
-    if (splits == 1) return ABCD_OK;
-    SumOuts outs{};
-    outs.add(out0, X.len * W.len);
-    if (halves == 2) outs.add(out1, X.len * W.len);
-    return launch_sum_parts(s.part, splits, outs, f.dtype, stream);
+  FfnDWeight dw{};
+  dw.part = s.part;
+  dw.n = n;
+  auto want = [&](void* out, const void* m, int64_t ld, int64_t rows, const Side& w, int64_t cols, float factor) {
+    if (out) dw.one[dw.count++] = FfnDWeight::One{m, w.p[0], out, ld, rows, w.ld, cols, factor, 0, 0, 0};
   };
-  if (dw_gate || dw_up) {
-    Side X{{dw_gate ? s.gate : s.up, s.up}, hp, f.h};
-    const int halves = dw_gate && dw_up ? 2 : 1;
-    TRY_STATUS(dweight(X, Side{{xs.p[0], nullptr}, xs.ld, f.d}, halves, dw_gate ? dw_gate : dw_up, dw_up,
-                       splits_gate_up(f, n), 1.0f));
-  }
-  if (dw_down)
-    TRY_STATUS(dweight(Side{{dz.p[0], nullptr}, dz.ld, f.o}, Side{{hidden, nullptr}, hp, f.h}, 1, dw_down, nullptr,
-                       splits_down(f, n), scale));
+  want(dw_gate, s.gate, hp, f.h, xs, f.d, 1.0f);
+  want(dw_up, s.up, hp, f.h, xs, f.d, 1.0f);
+  want(dw_down, dz.p[0], dz.ld, f.o, Side{{hidden, nullptr}, hp, 0}, f.h, scale);
+  if (dw.count > 0) TRY_STATUS(FFN_BY_TYPE(f, ffn_dweight, dw, stream));
   if (db_gate) TRY_STATUS(column_sums(f.dtype, n, f.h, s.gate, hp, 1.0f, db_gate, s.part, stream));
   if (db_up) TRY_STATUS(column_sums(f.dtype, n, f.h, s.up, hp, 1.0f, db_up, s.part, stream));
   if (db_down) TRY_STATUS(column_sums(f.dtype, n, f.o, dz.p[0], dz.ld, scale, db_down, s.part, stream));

@@ -53,17 +53,25 @@ struct FfnDX {
   int64_t h, d, lddx;
   int tiles_x, tiles_w;
 };
-// out = X' W over n rows, X of one or two halves; part: [splits][halves][x.len][w.len]
-// fp32 sums over `per` rows each, or NULL for the results themselves
+// The weights' gradients, out = scale X' W over n rows each, their tiles one after the
+// other. The first `whole` of these take a workgroup each, the others one for each of
+// `splits` parts of `per` rows, whose sums go to part: [tiles - whole][splits][tile].
 struct FfnDWeight {
-  Side x, w;
-  void* out0;
-  void* out1;
+  struct One {
+    const void* x;
+    const void* w;
+    void* out;
+    int64_t ldx, rows, ldw, cols;
+    float scale;
+    int tiles_x, tiles_w, first;
+  } one[3];
   float* part;
-  float scale;  // of the sums
   int64_t n, per;
-  int halves, tiles_x, tiles_w;
+  int count, tiles, whole, splits;
 };
+
+// Workgroups that run at once with tiles of 256 x 256, one a CU, and of 128 x 128.
+constexpr int kCUs = 256, kBigSlots = kCUs, kSmallSlots = 2 * kCUs;
 
 // The narrow block, in one launch each way.
 struct FfnNarrow {
@@ -96,7 +104,7 @@ int32_t ffn_narrow_bwd_bf16(const FfnNarrowBwd&, int64_t blocks, hipStream_t);
   int32_t ffn_out_##NAME(const FfnOut&, hipStream_t);          \
   int32_t ffn_dhidden_##NAME(const FfnDHidden&, hipStream_t);  \
   int32_t ffn_dx_##NAME(const FfnDX&, hipStream_t);            \
-  int32_t ffn_dweight_##NAME(const FfnDWeight&, int, hipStream_t);
+  int32_t ffn_dweight_##NAME(const FfnDWeight&, hipStream_t);
 ABCD_FFN_DECLARE(f32)
 ABCD_FFN_DECLARE(f16)
 ABCD_FFN_DECLARE(bf16)

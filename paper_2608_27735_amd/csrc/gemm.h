@@ -160,16 +160,22 @@ __device__ __forceinline__ typename Frag<T>::type read_frag(const LdsChar* lds, 
   }
 }
 
-// The tile that workgroup b of `tiles` takes. Workgroups go round the 8 XCDs, each
-// with an L2 of its own: an XCD takes consecutive tiles, and these go down 8 tiles
-// of X before the next tile of W, so that what runs together on it shares both.
-__device__ __forceinline__ void tile_of(int b, int tiles_x, int tiles_w, int& tx, int& tw) {
-  const int tiles = tiles_x * tiles_w, q = tiles / 8, r = tiles % 8, xcd = b % 8;
-  const int id = xcd * q + (xcd < r ? xcd : r) + b / 8;
-  const int group = id / (8 * tiles_w), g0 = group * 8;
-  const int gx = tiles_x - g0 < 8 ? tiles_x - g0 : 8, in = id - g0 * tiles_w;
+// The place in order of workgroup b of `tiles`. Workgroups go round the 8 XCDs, each
+// with an L2 of its own: an XCD takes consecutive places.
+__device__ __forceinline__ int xcd_order(int b, int tiles) {
+  const int q = tiles / 8, r = tiles % 8, xcd = b % 8;
+  return xcd * q + (xcd < r ? xcd : r) + b / 8;
+}
+// The tile at a place: down 8 tiles of X before the next tile of W, so that what runs
+// together on an XCD shares both.
+__device__ __forceinline__ void tile_at(int place, int tiles_x, int tiles_w, int& tx, int& tw) {
+  const int group = place / (8 * tiles_w), g0 = group * 8;
+  const int gx = tiles_x - g0 < 8 ? tiles_x - g0 : 8, in = place - g0 * tiles_w;
   tx = g0 + in % gx;
   tw = in / gx;
+}
+__device__ __forceinline__ void tile_of(int b, int tiles_x, int tiles_w, int& tx, int& tw) {
+  tile_at(xcd_order(b, tiles_x * tiles_w), tiles_x, tiles_w, tx, tw);
 }
 
 // The accumulators of a wave: fragments x by w of its part of the tile.
