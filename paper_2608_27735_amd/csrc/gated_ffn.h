@@ -29,27 +29,28 @@ namespace abcd {
 namespace {
 
 // Tiles: 256 x 256 by 8 waves, each 128 x 64 of it, where there are enough of
-// them; else 128 x 128 by 4 waves of 64 x 64.
+// them; else 128 x 128 by 4 waves of 64 x 64. For two halves of columns the waves lie
+// the other way, so that each has 64 columns of both and writes whole lines.
 struct Big {
   static constexpr int TX = 256, TW = 256, WX = 2, WW = 4;
+};
+struct BigHalves {
+  static constexpr int TX = 256, TW = 256, WX = 4, WW = 2;
 };
 struct Small {
   static constexpr int TX = 128, TW = 128, WX = 2, WW = 2;
 };
 
+// Of what is left of a row, up to the 8 elements that a lane takes.
+__device__ __forceinline__ int left_of(int64_t n) { return n < 8 ? (int)n : 8; }
+
 template <typename T, typename Cfg, bool kXAlong, bool kWAlong, bool kHalves>
 using ProductOf = Product<T, Cfg::TX, Cfg::TW, Cfg::WX, Cfg::WW, kXAlong, kWAlong, kHalves>;
 
-#define ABCD_TILE_LDS(P)                    \
-  __shared__ __align__(16) char tile0[P::kLdsBytes]; \
-  __shared__ __align__(16) char tile1[P::kLdsBytes]; \
-  LdsChar* const lds0 = (LdsChar*)tile0;    \
-  LdsChar* const lds1 = (LdsChar*)tile1
-
-template <typename T>
-__device__ __forceinline__ f32x4 load4(const void* p, int64_t at, int64_t n) {
-  return load_vec<T, 4, false>(static_cast<const T*>(p) + at, n > 4 ? 4 : (int)n);
-}
+#define ABCD_TILE_LDS(P)                              \
+  __shared__ __align__(16) char tiles_[2 * P::kLdsBytes]; \
+  LdsChar* const lds0 = (LdsChar*)tiles_;             \
+  LdsChar* const lds1 = lds0 + P::kLdsBytes
 
 template <typename T, typename Cfg, int kAct>
 __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn a) {
@@ -60,36 +61,32 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn 
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * (Cfg::TW / 2);
   P p;
   p.template run<1>(a.x, a.w, ix, iw, 0, a.d, lds0, lds1);
-  const int l = threadIdx.x & 63;
+  const int64_t c = iw + P::col_of();
+  const bool inside = c < a.ldh;
+  Floats<8> bg = 0.0f, bu = 0.0f;
+  if (a.bg && c < a.h) bg = load_vec<T, 8, false>(static_cast<const T*>(a.bg) + c, left_of(a.h - c));
+  if (a.bu && c < a.h) bu = load_vec<T, 8, false>(static_cast<const T*>(a.bu) + c, left_of(a.h - c));
+  p.by_rows(lds0, [&](int x, int group, Floats<8> g, Floats<8> u) {
+    const int64_t r = ix + P::row_of(x, group);
+    if (r >= a.x.len || !inside) return;
+    g += bg;
+    u += bu;
+    Floats<8> h, hg, hu;
 #pragma unroll
-  for (int w = 0; w < P::FW / 2; ++w) {
-    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4;
-    if (c >= a.ldh) continue;
-    f32x4 bg = 0.0f, bu = 0.0f;
-    if (a.bg && c < a.h) bg = load4<T>(a.bg, c, a.h - c);
-    if (a.bu && c < a.h) bu = load4<T>(a.bu, c, a.h - c);
-#pragma unroll
-    for (int x = 0; x < P::FX; ++x) {
-      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
-      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
-      if (r >= a.x.len) continue;
-      f32x4 g = p.acc[x][w] + bg, u = p.acc[x][w + P::FW / 2] + bu, h, hg, hu;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
-        float slope;
-        hu[i] = activate<kAct>(g[i], slope);
-        h[i] = hu[i] * u[i];
-        hg[i] = slope * u[i];
-      }
-      const int64_t at = r * a.ldh + c;
-      store_vec<T, 4, true>(static_cast<T*>(a.hidden) + at, h, 4);
-      if (a.by_gate) {
-        store_vec<T, 4, true>(static_cast<T*>(a.by_gate) + at, hg, 4);
-        store_vec<T, 4, true>(static_cast<T*>(a.by_up) + at, hu, 4);
-      }
+    for (int i = 0; i < 8; ++i) {
+      if (c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
+      float slope;
+      hu[i] = activate<kAct>(g[i], slope);
+      h[i] = hu[i] * u[i];
+      hg[i] = slope * u[i];
     }
-  }
+    const int64_t at = r * a.ldh + c;
+    store_vec<T, 8, true>(static_cast<T*>(a.hidden) + at, h, 8);
+    if (a.by_gate) {
+      store_vec<T, 8, true>(static_cast<T*>(a.by_gate) + at, hg, 8);
+      store_vec<T, 8, true>(static_cast<T*>(a.by_up) + at, hu, 8);
+    }
+  });
 }
 
 template <typename T, typename Cfg>
@@ -101,60 +98,57 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_out_kernel(FfnOu
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
   P p;
   p.template run<1>(a.hidden, a.w, ix, iw, 0, a.h, lds0, lds1);
-  const int l = threadIdx.x & 63;
-#pragma unroll
-  for (int w = 0; w < P::FW; ++w) {
-    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4, left = a.o - c;
-    if (left <= 0) continue;
-    f32x4 b = 0.0f;
-    if (a.bias) b = load4<T>(a.bias, c, left);
-#pragma unroll
-    for (int x = 0; x < P::FX; ++x) {
-      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
-      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
-      if (r >= a.hidden.len) continue;
-      f32x4 y = 0.0f;
-      if (a.res) y = load4<T>(a.res, r * a.ldr + c, left);
-      y = drop_vec<4>(p.acc[x][w] + b, a.key, (uint32_t)r, (uint32_t)c, y);
-      store_vec<T, 4, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, (int)(left > 4 ? 4 : left));
-    }
-  }
+  const int64_t c = iw + P::col_of();
+  const int left = left_of(a.o - c);
+  Floats<8> b = 0.0f;
+  if (a.bias && left > 0) b = load_vec<T, 8, false>(static_cast<const T*>(a.bias) + c, left);
+  p.by_rows(lds0, [&](int x, int group, Floats<8> v) {
+    const int64_t r = ix + P::row_of(x, group);
+    if (r >= a.hidden.len || left <= 0) return;
+    Floats<8> y = 0.0f;
+    if (a.res) y = load_vec<T, 8, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left);
+    y = drop_vec<8>(v + b, a.key, (uint32_t)r, (uint32_t)c, y);
+    store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, left);
+  });
 }
 
 template <typename T, typename Cfg>
 __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dhidden_kernel(FfnDHidden a) {
   typedef ProductOf<T, Cfg, true, false, false> P;
+  typedef typename VecOf<T, 8>::type V8;
   ABCD_TILE_LDS(P);
   int tx, tw;
   tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
   P p;
   p.template run<1>(a.dz, a.w, ix, iw, 0, a.o, lds0, lds1);
-  const int l = threadIdx.x & 63;
+  const int64_t c = iw + P::col_of();
+  const bool inside = c < a.ldh;
+  // h's derivatives, 16 rows ahead
+  V8 hg[2][P::kGroups], hu[2][P::kGroups];
+  auto fetch = [&](int x) {
 #pragma unroll
-  for (int w = 0; w < P::FW; ++w) {
-    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4;
-    if (c >= a.ldh) continue;
-#pragma unroll
-    for (int x = 0; x < P::FX; ++x) {
-      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
-      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
-      if (r >= a.dz.len) continue;
-      const int64_t at = r * a.ldh + c;
-      const f32x4 hg = load_vec<T, 4, true>(static_cast<const T*>(a.by_gate) + at, 4);
-      const f32x4 hu = load_vec<T, 4, true>(static_cast<const T*>(a.by_up) + at, 4);
-      f32x4 dg, du;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float dh = p.acc[x][w][i] * a.scale;
-        const bool in = c + i < a.h;
-        dg[i] = in ? dh * hg[i] : 0.0f;
-        du[i] = in ? dh * hu[i] : 0.0f;
-      }
-      store_vec<T, 4, true>(static_cast<T*>(a.dgate) + at, dg, 4);
-      store_vec<T, 4, true>(static_cast<T*>(a.dup) + at, du, 4);
+    for (int g = 0; g < P::kGroups; ++g) {
+      const int64_t r = ix + P::row_of(x, g), at = (r < a.dz.len ? r : ix) * a.ldh + (inside ? c : 0);
+      hg[x & 1][g] = *reinterpret_cast<const V8*>(static_cast<const T*>(a.by_gate) + at);
+      hu[x & 1][g] = *reinterpret_cast<const V8*>(static_cast<const T*>(a.by_up) + at);
     }
-  }
+  };
+  fetch(0);
+  p.by_rows(lds0, [&](int x, int g, Floats<8> dh) {
+    if (g == 0 && x + 1 < P::FX) fetch(x + 1);
+    const int64_t r = ix + P::row_of(x, g);
+    if (r >= a.dz.len || !inside) return;
+    dh *= a.scale;
+    Floats<8> dg = dh * __builtin_convertvector(hg[x & 1][g], Floats<8>);
+    Floats<8> du = dh * __builtin_convertvector(hu[x & 1][g], Floats<8>);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i >= a.h) dg[i] = du[i] = 0.0f;  // the padding, which products read
+    const int64_t at = r * a.ldh + c;
+    store_vec<T, 8, true>(static_cast<T*>(a.dgate) + at, dg, 8);
+    store_vec<T, 8, true>(static_cast<T*>(a.dup) + at, du, 8);
+  });
 }
 
 template <typename T, typename Cfg>
@@ -166,19 +160,12 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dx_kernel(FfnDX 
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
   P p;
   p.template run<2>(a.dgu, a.w, ix, iw, 0, a.h, lds0, lds1);
-  const int l = threadIdx.x & 63;
-#pragma unroll
-  for (int w = 0; w < P::FW; ++w) {
-    const int64_t c = iw + P::unit_w(w) * 16 + (l >> 4) * 4, left = a.d - c;
-    if (left <= 0) continue;
-#pragma unroll
-    for (int x = 0; x < P::FX; ++x) {
-      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
-      const int64_t r = ix + P::unit_x(x) * 16 + (l & 15);
-      if (r < a.dgu.len)
-        store_vec<T, 4, false>(static_cast<T*>(a.dx) + r * a.lddx + c, p.acc[x][w], (int)(left > 4 ? 4 : left));
-    }
-  }
+  const int64_t c = iw + P::col_of();
+  const int left = left_of(a.d - c);
+  p.by_rows(lds0, [&](int x, int group, Floats<8> v) {
+    const int64_t r = ix + P::row_of(x, group);
+    if (r < a.dgu.len && left > 0) store_vec<T, 8, false>(static_cast<T*>(a.dx) + r * a.lddx + c, v, left);
+  });
 }
 
 // Which product a tile of the weights' gradients belongs to, and its place there.
@@ -206,22 +193,15 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dweight_kernel(F
   P p;
   p.template run<1>(Side{{m.x, nullptr}, m.ldx, m.rows}, Side{{m.w, nullptr}, m.ldw, m.cols}, ix, iw, k0, k1, lds0,
                     lds1);
-  const int l = threadIdx.x & 63;
-#pragma unroll
-  for (int w = 0; w < P::FW; ++w) {
-    const int cw = P::unit_w(w) * 16 + (l >> 4) * 4;
-    const int64_t c = iw + cw, left = m.cols - c;
-#pragma unroll
-    for (int x = 0; x < P::FX; ++x) {
-      __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses and values at a time
-      const int rx = P::unit_x(x) * 16 + (l & 15);
-      if (rest >= 0)
-        *reinterpret_cast<f32x4*>(a.part + ((int64_t)rest * Cfg::TX + rx) * Cfg::TW + cw) = p.acc[x][w];
-      else if (ix + rx < m.rows && left > 0)
-        store_vec<T, 4, false>(static_cast<T*>(m.out) + (ix + rx) * m.cols + c, p.acc[x][w] * m.scale,
-                               (int)(left > 4 ? 4 : left));
-    }
-  }
+  const int cw = P::col_of();
+  const int left = left_of(m.cols - (iw + cw));
+  p.by_rows(lds0, [&](int x, int group, Floats<8> v) {
+    const int rx = P::row_of(x, group);
+    if (rest >= 0)
+      store_vec<float, 8, true>(a.part + ((int64_t)rest * Cfg::TX + rx) * Cfg::TW + cw, v, 8);
+    else if (ix + rx < m.rows && left > 0)
+      store_vec<T, 8, false>(static_cast<T*>(m.out) + (ix + rx) * m.cols + iw + cw, v * m.scale, left);
+  });
 }
 
 // Tile blockIdx.x of those that were split: the sum of its parts, rows blockIdx.y 4 ..
@@ -245,7 +225,7 @@ inline int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
 // The big tile where it gives most of the CUs one.
 inline bool use_big(int64_t nx, int64_t nw, int tw) { return tiles(nx, Big::TX) * tiles(nw, tw) >= 192; }
 
-#define ABCD_FFN_LAUNCH(label, kernel, a, nx, nw, half, stream, ...)                                      \
+#define ABCD_FFN_LAUNCH(label, kernel, Big_, a, nx, nw, half, stream, ...)                                \
   do {                                                                                                    \
     const bool big_ = use_big(nx, nw, Big::TW / (half));                                                  \
     a.tiles_x = (int)tiles(nx, big_ ? Big::TX : Small::TX);                                               \
@@ -253,7 +233,7 @@ inline bool use_big(int64_t nx, int64_t nw, int tw) { return tiles(nx, Big::TX) 
     const int64_t grid_ = (int64_t)a.tiles_x * a.tiles_w;                                                 \
     REQUIRE(grid_ < (int64_t(1) << 31), "too many tiles");                                                \
     if (big_)                                                                                             \
-      ABCD_LAUNCH(label, (kernel<T, Big __VA_ARGS__>), grid_, Big::WX* Big::WW * 64, 0, stream, a);       \
+      ABCD_LAUNCH(label, (kernel<T, Big_ __VA_ARGS__>), grid_, Big::WX* Big::WW * 64, 0, stream, a);      \
     else                                                                                                  \
       ABCD_LAUNCH(label, (kernel<T, Small __VA_ARGS__>), grid_, Small::WX* Small::WW * 64, 0, stream, a); \
     ABCD_HIP(hipGetLastError());                                                                          \
@@ -262,23 +242,23 @@ inline bool use_big(int64_t nx, int64_t nw, int tw) { return tiles(nx, Big::TX) 
 template <typename T>
 int32_t run_in(FfnIn a, hipStream_t stream) {
   return with_act(a.act, [&](auto act) -> int32_t {
-    ABCD_FFN_LAUNCH("ffn_in", ffn_in_kernel, a, a.x.len, a.h, 2, stream, , decltype(act)::value);
+    ABCD_FFN_LAUNCH("ffn_in", ffn_in_kernel, BigHalves, a, a.x.len, a.h, 2, stream, , decltype(act)::value);
     return ABCD_OK;
   });
 }
 template <typename T>
 int32_t run_out(FfnOut a, hipStream_t stream) {
-  ABCD_FFN_LAUNCH("ffn_out", ffn_out_kernel, a, a.hidden.len, a.o, 1, stream);
+  ABCD_FFN_LAUNCH("ffn_out", ffn_out_kernel, Big, a, a.hidden.len, a.o, 1, stream);
   return ABCD_OK;
 }
 template <typename T>
 int32_t run_dhidden(FfnDHidden a, hipStream_t stream) {
-  ABCD_FFN_LAUNCH("ffn_dhidden", ffn_dhidden_kernel, a, a.dz.len, a.h, 1, stream);
+  ABCD_FFN_LAUNCH("ffn_dhidden", ffn_dhidden_kernel, Big, a, a.dz.len, a.h, 1, stream);
   return ABCD_OK;
 }
 template <typename T>
 int32_t run_dx(FfnDX a, hipStream_t stream) {
-  ABCD_FFN_LAUNCH("ffn_dx", ffn_dx_kernel, a, a.dgu.len, a.d, 1, stream);
+  ABCD_FFN_LAUNCH("ffn_dx", ffn_dx_kernel, Big, a, a.dgu.len, a.d, 1, stream);
   return ABCD_OK;
 }
 template <typename T, typename Cfg>

@@ -211,6 +211,50 @@ struct Product {
     }
   }
 
+  // The results by rows: f(x, row, col, v) with 8 consecutive columns col.. of row `row`
+  // of the tile, eight or more lanes next to each other in a row; with halves f(x, row,
+  // col, v, v2), the same columns of both. kGroups calls for each x. The accumulators
+  // pass through LDS 16 rows at a time, each wave by itself: stored as the lanes hold
+  // them, 4 columns of each of 16 rows, they would take twice the instructions and touch
+  // lines a quarter at a time (an epilogue that reads two arrays and writes two took 64
+  // us of a tile's 118).
+  static constexpr int kLanes = kHalves ? FW : 2 * FW;  // lanes of a row
+  static constexpr int kGroups = 16 * kLanes / 64;
+  __device__ __forceinline__ static int row_of(int x, int group) {
+    return unit_x(x) * 16 + group * (64 / kLanes) + (threadIdx.x & 63) / kLanes;
+  }
+  __device__ __forceinline__ static int col_of() {
+    return (threadIdx.x >> 6) % kWW * (kLanes * 8) + (threadIdx.x & 63) % kLanes * 8;
+  }
+  template <typename Fn>
+  __device__ __forceinline__ void by_rows(LdsChar* lds, const Fn& f) {
+    constexpr int kPitch = FW * 64 + 16;
+    static_assert(kWX * kWW * 16 * kPitch <= 2 * kLdsBytes, "the waves' rows fit in the tiles' LDS");
+    typedef __attribute__((address_space(3))) f32x4 LdsF4;
+    const int l = threadIdx.x & 63;
+    LdsChar* const buf = lds + (threadIdx.x >> 6) * 16 * kPitch;
+    __syncthreads();  // nothing reads the tiles any more
+#pragma unroll
+    for (int x = 0; x < FX; ++x) {
+#pragma unroll
+      for (int w = 0; w < FW; ++w) *(LdsF4*)(buf + (l & 15) * kPitch + w * 64 + (l >> 4) * 16) = acc[x][w];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        LdsChar* const at = buf + (g * (64 / kLanes) + l / kLanes) * kPitch + l % kLanes * 32;
+        Floats<8> v[2];
+#pragma unroll
+        for (int k = 0; k < (kHalves ? 2 : 1); ++k) {
+          const f32x4 lo = *(LdsF4*)(at + k * FW * 32), hi = *(LdsF4*)(at + k * FW * 32 + 16);
+          v[k] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        if constexpr (kHalves)
+          f(x, g, v[0], v[1]);
+        else
+          f(x, g, v[0]);
+      }
+    }
+  }
+
   // acc = sum over the segments' contractions [kbeg, kend) of X and W at the tile's
   // first indexes ix, iw. lds0, lds1: kLdsBytes each.
   template <int kSegments>
