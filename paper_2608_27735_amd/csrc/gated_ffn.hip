@@ -35,31 +35,44 @@ __global__ __launch_bounds__(kBlock) void pack_rows_kernel(PackArgs a) {
   }
 }
 
-// part[blockIdx.y][c] = sum over rows blockIdx.y, + gridDim.y rows.. of m[row][c],
-// times scale.
-// `lanes` threads along a row, the workgroup's other threads on other rows.
+// Column sums of up to three matrices of n rows (blockIdx.z): part[blockIdx.y][first + c]
+// = scale times the sum over rows blockIdx.y, + gridDim.y rows.. of m[row][c]. `lanes`
+// threads along a row, the workgroup's other threads on other rows.
+struct ColumnSums {
+  struct One {
+    const void* m;
+    int64_t ld, first;
+    int cols, lanes;
+    float scale;
+  } one[3];
+  float* part;
+  int64_t n, cols;  // of all together
+};
 template <typename T>
-__global__ __launch_bounds__(kBlock) void column_sums_kernel(const void* m, int64_t ld, int64_t n, int cols,
-                                                             int lanes, float scale, float* part) {
+__global__ __launch_bounds__(kBlock) void column_sums_kernel(ColumnSums a) {
   constexpr int N = kPer16<T>;
   __shared__ float red[kBlock * N];
-  const int t = threadIdx.x & (lanes - 1), rows = kBlock / lanes;
-  const int c = ((int)blockIdx.x * lanes + t) * N;
+  const ColumnSums::One m = a.one[blockIdx.z];
+  const int t = threadIdx.x & (m.lanes - 1), rows = kBlock / m.lanes;
+  const int c = ((int)blockIdx.x * m.lanes + t) * N;
+  if ((int)blockIdx.x * m.lanes * N >= m.cols) return;
   Floats<N> s = 0.0f;
-  if (c < cols)
-    for (int64_t row = (int64_t)blockIdx.y * rows + threadIdx.x / lanes; row < n; row += (int64_t)gridDim.y * rows)
-      s += __builtin_convertvector((load_first<T, false>(static_cast<const T*>(m) + row * ld + c, cols - c,
-                                                         (n - 1 - row) * ld + cols - c)),
+  if (c < m.cols) {
+#pragma unroll 4
+    for (int64_t row = (int64_t)blockIdx.y * rows + threadIdx.x / m.lanes; row < a.n; row += (int64_t)gridDim.y * rows)
+      s += __builtin_convertvector((load_first<T, false>(static_cast<const T*>(m.m) + row * m.ld + c, m.cols - c,
+                                                         (a.n - 1 - row) * m.ld + m.cols - c)),
                                    Floats<N>);
+  }
 #pragma unroll
   for (int i = 0; i < N; ++i) red[threadIdx.x * N + i] = s[i];
   __syncthreads();
-  for (int i = threadIdx.x; i < lanes * N; i += kBlock) {
-    const int64_t at = (int64_t)blockIdx.x * lanes * N + i;
-    if (at >= cols) break;
+  for (int i = threadIdx.x; i < m.lanes * N; i += kBlock) {
+    const int64_t at = (int64_t)blockIdx.x * m.lanes * N + i;
+    if (at >= m.cols) break;
     float v = 0.0f;
-    for (int r = 0; r < rows; ++r) v += red[r * lanes * N + i];
-    part[(int64_t)blockIdx.y * cols + at] = v * scale;
+    for (int r = 0; r < rows; ++r) v += red[r * m.lanes * N + i];
+    a.part[(int64_t)blockIdx.y * a.cols + m.first + at] = v * m.scale;
   }
 }
 
@@ -82,23 +95,6 @@ int32_t pack(int32_t dtype, int64_t n, int64_t cols, const void* src, int64_t ld
     ABCD_HIP(hipGetLastError());
     return ABCD_OK;
   });
-}
-
-// out[c] = scale times the sum over the rows of m, rounded to dtype.
-int32_t column_sums(int32_t dtype, int64_t n, int64_t cols, const void* m, int64_t ld, float scale, void* out,
-                    float* part, hipStream_t stream) {
-  const int64_t parts = sum_parts_of(n);
-  TRY_STATUS(with_type(dtype, [&](auto z) -> int32_t {
-    typedef decltype(z) T;
-    const int nvec = (int)((cols + kPer16<T> - 1) / kPer16<T>), lanes = std::min(lanes_for(nvec), 64);
-    ABCD_LAUNCH("column_sums", (column_sums_kernel<T>), dim3((nvec + lanes - 1) / lanes, parts), kBlock, 0, stream,
-                m, ld, n, (int)cols, lanes, scale, part);
-    ABCD_HIP(hipGetLastError());
-    return ABCD_OK;
-  }));
-  SumOuts outs{};
-  outs.add(out, cols);
-  return launch_sum_parts(part, parts, outs, dtype, stream);
 }
 
 int64_t up8(int64_t v) { return (v + 7) & ~int64_t(7); }
@@ -167,7 +163,7 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
     s.dz = p.take(n * op * sz);
     s.gate = p.take(n * hp * sz);
     s.up = p.take(n * hp * sz);
-    size_t part = (size_t)sum_parts_of(n) * std::max(f.h, f.o);
+    size_t part = (size_t)sum_parts_of(n) * (2 * f.h + f.o);
     part = std::max(part, dweight_part(n));
     s.part = static_cast<float*>(p.take(part * sizeof(float)));
   }
@@ -322,9 +318,33 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
   want(dw_up, s.up, hp, f.h, xs, f.d, 1.0f);
   want(dw_down, dz.p[0], dz.ld, f.o, Side{{hidden, nullptr}, hp, 0}, f.h, scale);
   if (dw.count > 0) TRY_STATUS(FFN_BY_TYPE(f, ffn_dweight, dw, stream));
-  if (db_gate) TRY_STATUS(column_sums(f.dtype, n, f.h, s.gate, hp, 1.0f, db_gate, s.part, stream));
-  if (db_up) TRY_STATUS(column_sums(f.dtype, n, f.h, s.up, hp, 1.0f, db_up, s.part, stream));
-  if (db_down) TRY_STATUS(column_sums(f.dtype, n, f.o, dz.p[0], dz.ld, scale, db_down, s.part, stream));
+  ColumnSums cs{};
+  cs.part = s.part;
+  cs.n = n;
+  SumOuts outs{};
+  const int per16 = 16 / (int)type_bytes(f.dtype);
+  int64_t widest = 0;
+  auto sums = [&](void* out, const void* m, int64_t ld, int64_t cols, float factor) {
+    if (!out) return;
+    const int lanes = std::min(lanes_for((int)((cols + per16 - 1) / per16)), 64);
+    cs.one[outs.count] = ColumnSums::One{m, ld, cs.cols, (int)cols, lanes, factor};
+    outs.add(out, cols);
+    cs.cols += cols;
+    widest = std::max<int64_t>(widest, (cols + lanes * per16 - 1) / (lanes * per16));
+  };
+  sums(db_gate, s.gate, hp, f.h, 1.0f);
+  sums(db_up, s.up, hp, f.h, 1.0f);
+  sums(db_down, dz.p[0], dz.ld, f.o, scale);
+  if (outs.count > 0) {
+    const int64_t parts = sum_parts_of(n);
+    TRY_STATUS(with_type(f.dtype, [&](auto z) -> int32_t {
+      ABCD_LAUNCH("column_sums", (column_sums_kernel<decltype(z)>), dim3(widest, parts, outs.count), kBlock, 0, stream,
+                  cs);
+      ABCD_HIP(hipGetLastError());
+      return ABCD_OK;
+    }));
+    TRY_STATUS(launch_sum_parts(s.part, parts, outs, f.dtype, stream));
+  }
   return ABCD_OK;
 }
 
