@@ -47,10 +47,9 @@ __device__ __forceinline__ int left_of(int64_t n) { return n < 8 ? (int)n : 8; }
 template <typename T, typename Cfg, bool kXAlong, bool kWAlong, bool kHalves>
 using ProductOf = Product<T, Cfg::TX, Cfg::TW, Cfg::WX, Cfg::WW, kXAlong, kWAlong, kHalves>;
 
-#define ABCD_TILE_LDS(P)                              \
-  __shared__ __align__(16) char tiles_[2 * P::kLdsBytes]; \
-  LdsChar* const lds0 = (LdsChar*)tiles_;             \
-  LdsChar* const lds1 = lds0 + P::kLdsBytes
+#define ABCD_TILE_LDS(P)                            \
+  __shared__ __align__(16) char tiles_[P::kLdsBytes]; \
+  LdsChar* const lds = (LdsChar*)tiles_
 
 template <typename T, typename Cfg, int kAct>
 __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn a) {
@@ -60,13 +59,13 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn 
   tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * (Cfg::TW / 2);
   P p;
-  p.template run<1>(a.x, a.w, ix, iw, 0, a.d, lds0, lds1);
+  p.template run<1>(a.x, a.w, ix, iw, 0, a.d, lds);
   const int64_t c = iw + P::col_of();
   const bool inside = c < a.ldh;
   Floats<8> bg = 0.0f, bu = 0.0f;
   if (a.bg && c < a.h) bg = load_vec<T, 8, false>(static_cast<const T*>(a.bg) + c, left_of(a.h - c));
   if (a.bu && c < a.h) bu = load_vec<T, 8, false>(static_cast<const T*>(a.bu) + c, left_of(a.h - c));
-  p.by_rows(lds0, [&](int x, int group, Floats<8> g, Floats<8> u) {
+  p.by_rows(lds, [&](int x, int group, Floats<8> g, Floats<8> u) {
     const int64_t r = ix + P::row_of(x, group);
     if (r >= a.x.len || !inside) return;
     g += bg;
@@ -97,12 +96,12 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_out_kernel(FfnOu
   tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
   P p;
-  p.template run<1>(a.hidden, a.w, ix, iw, 0, a.h, lds0, lds1);
+  p.template run<1>(a.hidden, a.w, ix, iw, 0, a.h, lds);
   const int64_t c = iw + P::col_of();
   const int left = left_of(a.o - c);
   Floats<8> b = 0.0f;
   if (a.bias && left > 0) b = load_vec<T, 8, false>(static_cast<const T*>(a.bias) + c, left);
-  p.by_rows(lds0, [&](int x, int group, Floats<8> v) {
+  p.by_rows(lds, [&](int x, int group, Floats<8> v) {
     const int64_t r = ix + P::row_of(x, group);
     if (r >= a.hidden.len || left <= 0) return;
     Floats<8> y = 0.0f;
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dhidden_kernel(F
   tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
   P p;
-  p.template run<1>(a.dz, a.w, ix, iw, 0, a.o, lds0, lds1);
+  p.template run<1>(a.dz, a.w, ix, iw, 0, a.o, lds);
   const int64_t c = iw + P::col_of();
   const bool inside = c < a.ldh;
   // h's derivatives, 16 rows ahead
@@ -135,7 +134,7 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dhidden_kernel(F
     }
   };
   fetch(0);
-  p.by_rows(lds0, [&](int x, int g, Floats<8> dh) {
+  p.by_rows(lds, [&](int x, int g, Floats<8> dh) {
     if (g == 0 && x + 1 < P::FX) fetch(x + 1);
     const int64_t r = ix + P::row_of(x, g);
     if (r >= a.dz.len || !inside) return;
@@ -159,10 +158,10 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dx_kernel(FfnDX 
   tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
   P p;
-  p.template run<2>(a.dgu, a.w, ix, iw, 0, a.h, lds0, lds1);
+  p.template run<2>(a.dgu, a.w, ix, iw, 0, a.h, lds);
   const int64_t c = iw + P::col_of();
   const int left = left_of(a.d - c);
-  p.by_rows(lds0, [&](int x, int group, Floats<8> v) {
+  p.by_rows(lds, [&](int x, int group, Floats<8> v) {
     const int64_t r = ix + P::row_of(x, group);
     if (r < a.dgu.len && left > 0) store_vec<T, 8, false>(static_cast<T*>(a.dx) + r * a.lddx + c, v, left);
   });
@@ -191,11 +190,10 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dweight_kernel(F
     k1 = k0 + a.per < a.n ? k0 + a.per : a.n;
   }
   P p;
-  p.template run<1>(Side{{m.x, nullptr}, m.ldx, m.rows}, Side{{m.w, nullptr}, m.ldw, m.cols}, ix, iw, k0, k1, lds0,
-                    lds1);
+  p.template run<1>(Side{{m.x, nullptr}, m.ldx, m.rows}, Side{{m.w, nullptr}, m.ldw, m.cols}, ix, iw, k0, k1, lds);
   const int cw = P::col_of();
   const int left = left_of(m.cols - (iw + cw));
-  p.by_rows(lds0, [&](int x, int group, Floats<8> v) {
+  p.by_rows(lds, [&](int x, int group, Floats<8> v) {
     const int rx = P::row_of(x, group);
     if (rest >= 0)
       store_vec<float, 8, true>(a.part + ((int64_t)rest * Cfg::TX + rx) * Cfg::TW + cw, v, 8);
@@ -222,19 +220,24 @@ __global__ __launch_bounds__(TW) void ffn_dweight_sum_kernel(FfnDWeight a) {
 
 inline int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
 
-// The big tile where it gives most of the CUs one.
-inline bool use_big(int64_t nx, int64_t nw, int tw) { return tiles(nx, Big::TX) * tiles(nw, tw) >= 192; }
+// The big tile where it gives most of the CUs one. (fp32, whose parts are
+// made on the way to LDS, has the small one only.)
+template <typename T>
+bool use_big(int64_t nx, int64_t nw, int tw) {
+  return sizeof(T) == 2 && tiles(nx, Big::TX) * tiles(nw, tw) >= 192;
+}
 
 #define ABCD_FFN_LAUNCH(label, kernel, Big_, a, nx, nw, half, stream, ...)                                \
   do {                                                                                                    \
-    const bool big_ = use_big(nx, nw, Big::TW / (half));                                                  \
+    const bool big_ = use_big<T>(nx, nw, Big::TW / (half));                                               \
     a.tiles_x = (int)tiles(nx, big_ ? Big::TX : Small::TX);                                               \
     a.tiles_w = (int)tiles(nw, (big_ ? Big::TW : Small::TW) / (half));                                    \
     const int64_t grid_ = (int64_t)a.tiles_x * a.tiles_w;                                                 \
     REQUIRE(grid_ < (int64_t(1) << 31), "too many tiles");                                                \
-    if (big_)                                                                                             \
-      ABCD_LAUNCH(label, (kernel<T, Big_ __VA_ARGS__>), grid_, Big::WX* Big::WW * 64, 0, stream, a);      \
-    else                                                                                                  \
+    if constexpr (sizeof(T) == 2)                                                                         \
+      if (big_)                                                                                           \
+        ABCD_LAUNCH(label, (kernel<T, Big_ __VA_ARGS__>), grid_, Big::WX* Big::WW * 64, 0, stream, a);      \
+    if (!big_)                                                                                            \
       ABCD_LAUNCH(label, (kernel<T, Small __VA_ARGS__>), grid_, Small::WX* Small::WW * 64, 0, stream, a); \
     ABCD_HIP(hipGetLastError());                                                                          \
   } while (0)
@@ -293,7 +296,9 @@ template <typename T>
 int32_t run_dweight(const FfnDWeight& a, hipStream_t stream) {
   int64_t big = 0;
   for (int i = 0; i < a.count; ++i) big += tiles(a.one[i].rows, Big::TX) * tiles(a.one[i].cols, Big::TW);
-  return big >= 192 ? run_dweight_tiles<T, Big>(a, kBigSlots, stream) : run_dweight_tiles<T, Small>(a, kSmallSlots, stream);
+  if constexpr (sizeof(T) == 2)
+    if (big >= 192) return run_dweight_tiles<T, Big>(a, kBigSlots, stream);
+  return run_dweight_tiles<T, Small>(a, kSmallSlots, stream);
 }
 
 }  // namespace

@@ -214,16 +214,6 @@ __device__ __forceinline__ int turned_at(int row, int unit) {
   return row * 128 + ((unit ^ (((row & 3) << 2) | ((row >> 2) & 3))) * 8);
 }
 
-template <typename T>
-__device__ __forceinline__ typename Frag<T>::type read_across(LdsChar* lo, LdsChar* hi) {
-  typedef short s16x4 __attribute__((ext_vector_type(4)));
-  typedef short s16x8 __attribute__((ext_vector_type(8)));
-  typedef __attribute__((address_space(3))) s16x4 LdsS4;
-  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)lo);
-  const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)hi);
-  return __builtin_bit_cast(typename Frag<T>::type, (s16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
 // d and o up to 64, h up to kHB * 128
 template <typename T, int kAct, int kHB, bool kWhole, bool kDrop>
 __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(FfnNarrowBwd a) {

@@ -17,13 +17,17 @@
 //   the loads fetch the chunk that belongs at their place, and the fragments'
 //   16-byte reads meet no bank twice.
 // - LDS, across: rows of one contraction index, whose unit u of 16 elements lies
-//   at place u ^ across_swizzle(k). In 16 bits ds_read_b64_tr_b16 hands each lane
-//   four contraction indexes of its column; in 32 bits the lanes read 4 bytes.
+//   at place u ^ across_swizzle(k); ds_read_b64_tr_b16 hands each lane four
+//   contraction indexes of its column.
 // - Fragments are 16 x 16, with W as the matrix instruction's first operand, so
 //   that a lane holds four consecutive columns of one row of the result: stores of
 //   four elements, and one block of dropout's generator for them.
-// - fp32 uses the same bytes with v_mfma_f32_16x16x4_f32 four times per 16 bytes;
-//   the contraction's indexes are taken in another order on both sides alike.
+// - fp32: every number is the sum of three of 8 bits each, cut off one after the
+//   other (exact), and a product the six products of parts that are not below its last
+//   bit, on the same matrix instructions with fp32 sums: 96 cycles of a SIMD for what
+//   v_mfma_f32_16x16x4_f32 takes 256 for, at a relative error of a product of 2^-24.
+//   The parts are made on the way from memory to LDS, through registers. An infinity
+//   among the operands gives NaN.
 #pragma once
 
 #include "gated_ffn_args.h"
@@ -57,11 +61,10 @@ __device__ __forceinline__ f32x4 mma(Frag<float>::type w, Frag<float>::type x, f
 typedef __attribute__((address_space(3))) void LdsVoid;
 typedef __attribute__((address_space(3))) char LdsChar;
 
-__device__ __forceinline__ int across_swizzle16(int k) { return (k & 3) | ((k >> 1) & 4); }
-__device__ __forceinline__ int across_swizzle32(int k) { return (k >> 2) & 3; }
+__device__ __forceinline__ int across_swizzle(int k) { return (k & 3) | ((k >> 1) & 4); }
 
 // Where this thread's loads of a step come from, as byte offsets from the tile's
-// first element.
+// first element (16-bit types).
 template <typename T, int TILE, bool kAlong, int NT>
 struct TileLoads {
   static constexpr int kLoads = TILE * kStepBytes / 16 / NT;
@@ -76,12 +79,11 @@ struct TileLoads {
       for (int i = 0; i < kLoads; ++i)
         off[i] = (uint32_t)((i * (NT / 8) + (tid >> 3)) * (int)(ld * sizeof(T)) + chunk * 16);
     } else {
-      constexpr int kRowChunks = TILE * (int)sizeof(T) / 16, kUnitChunks = (int)sizeof(T);
+      constexpr int kRowChunks = TILE * (int)sizeof(T) / 16;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int q = i * NT + tid, k = q / kRowChunks, at = q % kRowChunks;
-        const int sw = sizeof(T) == 2 ? across_swizzle16(k) : across_swizzle32(k);
-        off[i] = (uint32_t)(k * (int)(ld * sizeof(T)) + (((at / kUnitChunks) ^ sw) * kUnitChunks + at % kUnitChunks) * 16);
+        off[i] = (uint32_t)(k * (int)(ld * sizeof(T)) + (((at >> 1) ^ across_swizzle(k)) * 2 + (at & 1)) * 16);
       }
     }
   }
@@ -128,7 +130,19 @@ __device__ __forceinline__ void load_tile(const TileLoads<T, TILE, kAlong, NT>& 
   }
 }
 
-// Fragment f (16 indexes from unit u0 + f) of half kk of the step.
+// 16 indexes of one contraction row's units each, four contraction indexes from each
+// of two places: a fragment across.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type read_across(LdsChar* lo, LdsChar* hi) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) s16x4 LdsS4;
+  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)lo);
+  const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)hi);
+  return __builtin_bit_cast(typename Frag<T>::type, (s16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Fragment `unit` (16 indexes) of half kk of the step.
 template <typename T, int TILE, bool kAlong>
 __device__ __forceinline__ typename Frag<T>::type read_frag(const LdsChar* lds, int unit, int kk) {
   typedef typename Frag<T>::type F;
@@ -138,26 +152,9 @@ __device__ __forceinline__ typename Frag<T>::type read_frag(const LdsChar* lds, 
     return *reinterpret_cast<const __attribute__((address_space(3))) F*>(lds + row * kStepBytes + ((c ^ (l & 7)) * 16));
   }
   constexpr int kRowBytes = TILE * (int)sizeof(T);
-  if constexpr (sizeof(T) == 2) {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
-    typedef __attribute__((address_space(3))) s16x4 LdsS4;
-    const int k = kk * 32 + (l >> 4) * 8 + ((l & 15) >> 2);
-    LdsChar* at = const_cast<LdsChar*>(lds) + k * kRowBytes + ((unit ^ across_swizzle16(k)) * 32) + (l & 3) * 8;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)at);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)(at + 4 * kRowBytes));
-    const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(F, v);
-  } else {
-    F v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int k = kk * 16 + (l >> 4) * 4 + e;
-      v[e] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(
-          lds + k * kRowBytes + ((unit ^ across_swizzle32(k)) * 64) + (l & 15) * 4);
-    }
-    return v;
-  }
+  const int k = kk * 32 + (l >> 4) * 8 + ((l & 15) >> 2);
+  LdsChar* at = const_cast<LdsChar*>(lds) + k * kRowBytes + ((unit ^ across_swizzle(k)) * 32) + (l & 3) * 8;
+  return read_across<T>(at, at + 4 * kRowBytes);
 }
 
 // The place in order of workgroup b of `tiles`. Workgroups go round the 8 XCDs, each
@@ -180,12 +177,18 @@ __device__ __forceinline__ void tile_of(int b, int tiles_x, int tiles_w, int& tx
 
 // The accumulators of a wave: fragments x by w of its part of the tile.
 // Waves: kWX along X, the others along W.
-template <typename T, int TX, int TW, int kWX, int kWW, bool kXAlong, bool kWAlong, bool kHalves>
-struct Product {
+template <int TX, int TW, int kWX, int kWW, bool kHalves>
+struct Accumulators {
   static constexpr int NT = kWX * kWW * 64;
   static constexpr int FX = TX / kWX / 16, FW = TW / kWW / 16;
-  static constexpr int kLdsBytes = (TX + TW) * kStepBytes;
   f32x4 acc[FX][FW];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int x = 0; x < FX; ++x)
+#pragma unroll
+      for (int w = 0; w < FW; ++w) acc[x][w] = 0.0f;
+  }
 
   // The unit of 16 that fragment w of this wave takes of the tile; with halves the
   // first FW / 2 lie in the first one and the others at the same place of the second.
@@ -196,24 +199,9 @@ struct Product {
   }
   __device__ __forceinline__ static int unit_x(int x) { return (threadIdx.x >> 6) / kWW * FX + x; }
 
-  __device__ __forceinline__ void step(const LdsChar* lds) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      typename Frag<T>::type fx[FX], fw[FW];
-#pragma unroll
-      for (int w = 0; w < FW; ++w) fw[w] = read_frag<T, TW, kWAlong>(lds + TX * kStepBytes, unit_w(w), kk);
-#pragma unroll
-      for (int x = 0; x < FX; ++x) fx[x] = read_frag<T, TX, kXAlong>(lds, unit_x(x), kk);
-#pragma unroll
-      for (int x = 0; x < FX; ++x)
-#pragma unroll
-        for (int w = 0; w < FW; ++w) acc[x][w] = mma(fw[w], fx[x], acc[x][w]);
-    }
-  }
-
-  // The results by rows: f(x, row, col, v) with 8 consecutive columns col.. of row `row`
-  // of the tile, eight or more lanes next to each other in a row; with halves f(x, row,
-  // col, v, v2), the same columns of both. kGroups calls for each x. The accumulators
+  // The results by rows: f(x, group, v) with 8 consecutive columns, col_of().., of row
+  // row_of(x, group) of the tile, eight or more lanes next to each other in a row; with
+  // halves f(x, group, v, v2), the same columns of both. The accumulators
   // pass through LDS 16 rows at a time, each wave by itself: stored as the lanes hold
   // them, 4 columns of each of 16 rows, they would take twice the instructions and touch
   // lines a quarter at a time (an epilogue that reads two arrays and writes two took 64
@@ -226,10 +214,9 @@ struct Product {
   __device__ __forceinline__ static int col_of() {
     return (threadIdx.x >> 6) % kWW * (kLanes * 8) + (threadIdx.x & 63) % kLanes * 8;
   }
+  static constexpr int kPitch = FW * 64 + 16, kRowsBytes = kWX * kWW * 16 * kPitch;  // of LDS
   template <typename Fn>
   __device__ __forceinline__ void by_rows(LdsChar* lds, const Fn& f) {
-    constexpr int kPitch = FW * 64 + 16;
-    static_assert(kWX * kWW * 16 * kPitch <= 2 * kLdsBytes, "the waves' rows fit in the tiles' LDS");
     typedef __attribute__((address_space(3))) f32x4 LdsF4;
     const int l = threadIdx.x & 63;
     LdsChar* const buf = lds + (threadIdx.x >> 6) * 16 * kPitch;
@@ -255,15 +242,38 @@ struct Product {
     }
   }
 
+};
+
+// 16-bit types.
+template <typename T, int TX, int TW, int kWX, int kWW, bool kXAlong, bool kWAlong, bool kHalves>
+struct Product : Accumulators<TX, TW, kWX, kWW, kHalves> {
+  typedef Accumulators<TX, TW, kWX, kWW, kHalves> Base;
+  using Base::acc, Base::FW, Base::FX, Base::NT, Base::unit_w, Base::unit_x;
+  static constexpr int kStageBytes = (TX + TW) * kStepBytes, kLdsBytes = 2 * kStageBytes;
+  static_assert(Base::kRowsBytes <= kLdsBytes, "the waves' rows fit in the tiles' LDS");
+
+  __device__ __forceinline__ void step(const LdsChar* lds) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      typename Frag<T>::type fx[FX], fw[FW];
+#pragma unroll
+      for (int w = 0; w < FW; ++w) fw[w] = read_frag<T, TW, kWAlong>(lds + TX * kStepBytes, unit_w(w), kk);
+#pragma unroll
+      for (int x = 0; x < FX; ++x) fx[x] = read_frag<T, TX, kXAlong>(lds, unit_x(x), kk);
+#pragma unroll
+      for (int x = 0; x < FX; ++x)
+#pragma unroll
+        for (int w = 0; w < FW; ++w) acc[x][w] = mma(fw[w], fx[x], acc[x][w]);
+    }
+  }
+
   // acc = sum over the segments' contractions [kbeg, kend) of X and W at the tile's
-  // first indexes ix, iw. lds0, lds1: kLdsBytes each.
+  // first indexes ix, iw. lds: kLdsBytes.
   template <int kSegments>
   __device__ __forceinline__ void run(const Side& X, const Side& W, int64_t ix, int64_t iw, int64_t kbeg, int64_t kend,
-                                      LdsChar* lds0, LdsChar* lds1) {
-#pragma unroll
-    for (int x = 0; x < FX; ++x)
-#pragma unroll
-      for (int w = 0; w < FW; ++w) acc[x][w] = 0.0f;
+                                      LdsChar* lds) {
+    this->clear();
+    LdsChar *lds0 = lds, *lds1 = lds + kStageBytes;
     TileLoads<T, TX, kXAlong, NT> lx;
     TileLoads<T, TW, kWAlong, NT> lw;
     lx.init(X.ld);
@@ -294,6 +304,159 @@ struct Product {
                                        const LdsChar* __restrict__ from) {
     if (more) fetch(next, into);
     step(from);
+  }
+};
+
+// ------------------------------------------------------------------ fp32
+
+// Three bf16 whose sum is v, cut off one after the other: 8 bits each, of two numbers
+// a word.
+struct Parts {
+  uint32_t p[3];
+};
+__device__ __forceinline__ Parts parts_of(float a, float b) {
+  Parts r;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+    r.p[i] = __builtin_amdgcn_perm(ub, ua, 0x07060302);  // the upper halves
+    if (i < 2) {
+      a -= __uint_as_float(ua & 0xFFFF0000u);
+      b -= __uint_as_float(ub & 0xFFFF0000u);
+    }
+  }
+  return r;
+}
+
+// One side's loads of a step of 32, 16 bytes (4 numbers) each, and where their parts go
+// in LDS: planes of TILE x 64 bytes. Along: rows of 32 elements whose 16-byte chunk c
+// lies at place c ^ ((row >> 1) & 3); across: as in 16 bits.
+template <int TILE, bool kAlong, int NT, bool kHalves>
+struct PartLoads {
+  static constexpr int kLoads = TILE * 32 / 4 / NT, kPlane = TILE * 64;
+  uint32_t off[kLoads];
+  int at[kLoads];
+  f32x4 v[kLoads];
+
+  __device__ __forceinline__ void init(int64_t ld) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int q = i * NT + threadIdx.x;
+      if (kAlong) {
+        const int row = q >> 3, c = q & 7, from = kHalves && i >= kLoads / 2 ? row - TILE / 2 : row;
+        off[i] = (uint32_t)(from * (int)(ld * 4) + c * 16);
+        at[i] = row * 64 + (((c >> 1) ^ ((row >> 1) & 3)) * 16) + (c & 1) * 8;
+      } else {
+        const int k = q / (TILE / 4), c = q % (TILE / 4);
+        off[i] = (uint32_t)(k * (int)(ld * 4) + c * 16);
+        at[i] = k * (TILE * 2) + (((c >> 2) ^ across_swizzle(k)) * 32) + (c & 3) * 8;
+      }
+    }
+  }
+
+  // (arguments as load_tile's)
+  __device__ __forceinline__ void fetch(const void* p, const void* p2, int64_t ld, int64_t len, int64_t i0, int64_t k0,
+                                        int64_t kn) {
+    constexpr int kRows = kHalves ? TILE / 2 : TILE;
+    const int64_t first = kAlong ? i0 * ld + k0 : k0 * ld + i0, left = len - i0;
+    const int rows = (int)(left < kRows ? left : kRows);
+    const int ks = (int)(kn - k0 < 32 ? kn - k0 : 32);
+    const uint32_t bytes = kAlong ? (uint32_t)((rows - 1) * (int)(ld * 4) + ((ks * 4 + 15) & ~15))
+                                  : (uint32_t)((ks - 1) * (int)(ld * 4) + ((rows * 4 + 15) & ~15));
+    const bool tail = kAlong && (int)(threadIdx.x & 7) * 4 >= ks;  // past the contraction's end
+    auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(static_cast<const float*>(p) + first), 0, bytes,
+                                                  0x00020000);
+    auto rsrc2 = rsrc;
+    if (kHalves)
+      rsrc2 = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(static_cast<const float*>(p2) + first), 0, bytes,
+                                                0x00020000);
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      v[i] = __builtin_bit_cast(f32x4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(
+                                           kHalves && i >= kLoads / 2 ? rsrc2 : rsrc, tail ? 0x80000000u : off[i], 0, 0));
+  }
+
+  __device__ __forceinline__ void put(LdsChar* lds) const {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) u32x2 LdsU2;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const Parts a = parts_of(v[i][0], v[i][1]), b = parts_of(v[i][2], v[i][3]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) *(LdsU2*)(lds + k * kPlane + at[i]) = u32x2{a.p[k], b.p[k]};
+    }
+  }
+};
+
+template <int TILE, bool kAlong>
+__device__ __forceinline__ Frag<__bf16>::type read_part(const LdsChar* lds, int unit) {
+  typedef Frag<__bf16>::type F;
+  const int l = threadIdx.x & 63;
+  if (kAlong) {
+    const int row = unit * 16 + (l & 15);
+    return *reinterpret_cast<const __attribute__((address_space(3))) F*>(lds + row * 64 +
+                                                                          (((l >> 4) ^ ((row >> 1) & 3)) * 16));
+  }
+  const int k = (l >> 4) * 8 + ((l & 15) >> 2);
+  LdsChar* at = const_cast<LdsChar*>(lds) + k * (TILE * 2) + ((unit ^ across_swizzle(k)) * 32) + (l & 3) * 8;
+  return read_across<__bf16>(at, at + 4 * (TILE * 2));
+}
+
+template <int TX, int TW, int kWX, int kWW, bool kXAlong, bool kWAlong, bool kHalves>
+struct Product<float, TX, TW, kWX, kWW, kXAlong, kWAlong, kHalves> : Accumulators<TX, TW, kWX, kWW, kHalves> {
+  typedef Accumulators<TX, TW, kWX, kWW, kHalves> Base;
+  using Base::acc, Base::FW, Base::FX, Base::NT, Base::unit_w, Base::unit_x;
+  typedef Frag<__bf16>::type F;
+  static constexpr int kXBytes = 3 * TX * 64;
+  static constexpr int kLdsBytes = kXBytes + 3 * TW * 64;
+  static_assert(Base::kRowsBytes <= kLdsBytes, "the waves' rows fit in the tiles' LDS");
+
+  __device__ __forceinline__ void step(const LdsChar* lds) {
+    F w[3][FW];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int i = 0; i < FW; ++i) w[k][i] = read_part<TW, kWAlong>(lds + kXBytes + k * TW * 64, unit_w(i));
+#pragma unroll
+    for (int x = 0; x < FX; ++x) {
+      F f[3];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) f[k] = read_part<TX, kXAlong>(lds + k * TX * 64, unit_x(x));
+      // the smallest products first
+#pragma unroll
+      for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+        for (int k = sum; k >= 0; --k)
+#pragma unroll
+          for (int i = 0; i < FW; ++i) acc[x][i] = mma(w[k][i], f[sum - k], acc[x][i]);
+    }
+  }
+
+  template <int kSegments>
+  __device__ __forceinline__ void run(const Side& X, const Side& W, int64_t ix, int64_t iw, int64_t kbeg, int64_t kend,
+                                      LdsChar* lds) {
+    this->clear();
+    PartLoads<TX, kXAlong, NT, false> lx;
+    PartLoads<TW, kWAlong, NT, kHalves> lw;
+    lx.init(X.ld);
+    lw.init(W.ld);
+    const int per = (int)((kend - kbeg + 31) / 32), steps = per * kSegments;
+    auto fetch = [&](int s) {
+      const int seg = kSegments > 1 && s >= per ? 1 : 0;
+      const int64_t k0 = kbeg + (int64_t)(s - seg * per) * 32;
+      lx.fetch(X.p[seg], nullptr, X.ld, X.len, ix, k0, kend);
+      lw.fetch(W.p[kHalves ? 0 : seg], W.p[1], W.ld, W.len, iw, k0, kend);
+    };
+    if (steps > 0) fetch(0);
+    for (int s = 0; s < steps; ++s) {
+      __syncthreads();  // nothing reads the last step's parts any more
+      lx.put(lds);
+      lw.put(lds + kXBytes);
+      if (s + 1 < steps) fetch(s + 1);
+      __syncthreads();
+      step(lds);
+    }
   }
 };
 
