@@ -513,7 +513,7 @@ ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, c
  * render_fwd, loss_l1, zero_fill, bwd_order, render_bwd, project_bwd, adam,
  * render_cache, cache_rect_init, layer_norm, layer_norm_bwd, layer_norm_cols,
  * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
- * ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out). */
+ * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

@@ -24,6 +24,7 @@
 #include "gated_ffn_args.h"
 #include "gated_ffn_few.h"
 #include "gemm.h"
+#include "load_frag.h"
 
 namespace abcd {
 namespace {
@@ -51,120 +52,240 @@ using ProductOf = Product<T, Cfg::TX, Cfg::TW, Cfg::WX, Cfg::WW, kXAlong, kWAlon
   __shared__ __align__(16) char tiles_[P::kLdsBytes]; \
   LdsChar* const lds = (LdsChar*)tiles_
 
-template <typename T, typename Cfg, int kAct>
-__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_in_kernel(FfnIn a) {
-  typedef ProductOf<T, Cfg, true, true, true> P;
-  ABCD_TILE_LDS(P);
-  int tx, tw;
-  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
-  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * (Cfg::TW / 2);
-  P p;
-  p.template run<1>(a.x, a.w, ix, iw, 0, a.d, lds);
-  const int64_t c = iw + P::col_of();
-  const bool inside = c < a.ldh;
-  Floats<8> bg = 0.0f, bu = 0.0f;
-  if (a.bg && c < a.h) bg = load_vec<T, 8, false>(static_cast<const T*>(a.bg) + c, left_of(a.h - c));
-  if (a.bu && c < a.h) bu = load_vec<T, 8, false>(static_cast<const T*>(a.bu) + c, left_of(a.h - c));
-  p.by_rows(lds, [&](int x, int group, Floats<8> g, Floats<8> u) {
-    const int64_t r = ix + P::row_of(x, group);
-    if (r >= a.x.len || !inside) return;
-    g += bg;
-    u += bu;
+template <typename T>
+using V8 = typename VecOf<T, 8>::type;
+
+// 8 elements from p as they are, n of them there (others 0).
+template <typename T>
+__device__ __forceinline__ V8<T> load8(const void* p, int64_t at, int n) {
+  typedef V8<T> V8U __attribute__((aligned(sizeof(T))));
+  const T* const q = static_cast<const T*>(p) + at;
+  if (n >= 8) return *reinterpret_cast<const V8U*>(q);
+  V8<T> v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = *(i < n ? q + i : reinterpret_cast<const T*>(zeros));
+  return v;
+}
+
+// What becomes of each product's sums, 8 consecutive columns of a row at a time:
+// column(c) is what a lane keeps of its columns c.., ahead(column, row) what it loads of
+// a row before the sums are there, and put(column, row, ahead, sums) writes. Columns from
+// end() on do not exist.
+template <typename T, int kAct>
+struct InEnd {
+  static constexpr bool kXAlong = true, kWAlong = true, kHalves = true;
+  static constexpr int kSegments = 1;
+  typedef BigHalves Large;
+  FfnIn a;
+  __device__ const Side& x() const { return a.x; }
+  __device__ const Side& w() const { return a.w; }
+  __host__ __device__ int64_t rows() const { return a.x.len; }
+  __host__ __device__ int64_t cols() const { return a.h; }
+  __host__ __device__ int64_t end() const { return a.ldh; }
+  __host__ __device__ int64_t length() const { return a.d; }
+  struct Column {
+    int64_t c;
+    Floats<8> bg, bu;
+  };
+  struct Ahead {};
+  __device__ __forceinline__ Column column(int64_t c) const {
+    Column k{c, 0.0f, 0.0f};
+    if (a.bg && c < a.h) k.bg = load_vec<T, 8, false>(static_cast<const T*>(a.bg) + c, left_of(a.h - c));
+    if (a.bu && c < a.h) k.bu = load_vec<T, 8, false>(static_cast<const T*>(a.bu) + c, left_of(a.h - c));
+    return k;
+  }
+  __device__ __forceinline__ Ahead ahead(const Column&, int64_t) const { return Ahead{}; }
+  __device__ __forceinline__ void put(const Column& k, int64_t r, const Ahead&, Floats<8> g, Floats<8> u) const {
+    g += k.bg;
+    u += k.bu;
     Floats<8> h, hg, hu;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
+      if (k.c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
       float slope;
       hu[i] = activate<kAct>(g[i], slope);
       h[i] = hu[i] * u[i];
       hg[i] = slope * u[i];
     }
-    const int64_t at = r * a.ldh + c;
+    const int64_t at = r * a.ldh + k.c;
     store_vec<T, 8, true>(static_cast<T*>(a.hidden) + at, h, 8);
     if (a.by_gate) {
       store_vec<T, 8, true>(static_cast<T*>(a.by_gate) + at, hg, 8);
       store_vec<T, 8, true>(static_cast<T*>(a.by_up) + at, hu, 8);
     }
-  });
-}
+  }
+};
 
-template <typename T, typename Cfg>
-__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_out_kernel(FfnOut a) {
-  typedef ProductOf<T, Cfg, true, true, false> P;
-  ABCD_TILE_LDS(P);
-  int tx, tw;
-  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
-  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
-  P p;
-  p.template run<1>(a.hidden, a.w, ix, iw, 0, a.h, lds);
-  const int64_t c = iw + P::col_of();
-  const int left = left_of(a.o - c);
-  Floats<8> b = 0.0f;
-  if (a.bias && left > 0) b = load_vec<T, 8, false>(static_cast<const T*>(a.bias) + c, left);
-  p.by_rows(lds, [&](int x, int group, Floats<8> v) {
-    const int64_t r = ix + P::row_of(x, group);
-    if (r >= a.hidden.len || left <= 0) return;
-    Floats<8> y = 0.0f;
-    if (a.res) y = load_vec<T, 8, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left);
-    y = drop_vec<8>(v + b, a.key, (uint32_t)r, (uint32_t)c, y);
-    store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, left);
-  });
-}
-
-template <typename T, typename Cfg>
-__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dhidden_kernel(FfnDHidden a) {
-  typedef ProductOf<T, Cfg, true, false, false> P;
-  typedef typename VecOf<T, 8>::type V8;
-  ABCD_TILE_LDS(P);
-  int tx, tw;
-  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
-  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
-  P p;
-  p.template run<1>(a.dz, a.w, ix, iw, 0, a.o, lds);
-  const int64_t c = iw + P::col_of();
-  const bool inside = c < a.ldh;
-  // h's derivatives, 16 rows ahead
-  V8 hg[2][P::kGroups], hu[2][P::kGroups];
-  auto fetch = [&](int x) {
-#pragma unroll
-    for (int g = 0; g < P::kGroups; ++g) {
-      const int64_t r = ix + P::row_of(x, g), at = (r < a.dz.len ? r : ix) * a.ldh + (inside ? c : 0);
-      hg[x & 1][g] = *reinterpret_cast<const V8*>(static_cast<const T*>(a.by_gate) + at);
-      hu[x & 1][g] = *reinterpret_cast<const V8*>(static_cast<const T*>(a.by_up) + at);
-    }
+template <typename T>
+struct OutEnd {
+  static constexpr bool kXAlong = true, kWAlong = true, kHalves = false;
+  static constexpr int kSegments = 1;
+  typedef Big Large;
+  FfnOut a;
+  __device__ const Side& x() const { return a.hidden; }
+  __device__ const Side& w() const { return a.w; }
+  __host__ __device__ int64_t rows() const { return a.hidden.len; }
+  __host__ __device__ int64_t cols() const { return a.o; }
+  __host__ __device__ int64_t end() const { return a.o; }
+  __host__ __device__ int64_t length() const { return a.h; }
+  struct Column {
+    int64_t c;
+    int left;
+    Floats<8> b;
   };
-  fetch(0);
-  p.by_rows(lds, [&](int x, int g, Floats<8> dh) {
-    if (g == 0 && x + 1 < P::FX) fetch(x + 1);
-    const int64_t r = ix + P::row_of(x, g);
-    if (r >= a.dz.len || !inside) return;
+  struct Ahead {
+    V8<T> res;
+  };
+  __device__ __forceinline__ Column column(int64_t c) const {
+    Column k{c, left_of(a.o - c), 0.0f};
+    if (a.bias && k.left > 0) k.b = load_vec<T, 8, false>(static_cast<const T*>(a.bias) + c, k.left);
+    return k;
+  }
+  __device__ __forceinline__ Ahead ahead(const Column& k, int64_t r) const {
+    return Ahead{load8<T>(a.res, r * a.ldr + k.c, a.res ? k.left : 0)};
+  }
+  __device__ __forceinline__ void put(const Column& k, int64_t r, const Ahead& f, Floats<8> v) const {
+    v = drop_vec<8>(v + k.b, a.key, (uint32_t)r, (uint32_t)k.c, __builtin_convertvector(f.res, Floats<8>));
+    store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + k.c, v, k.left);
+  }
+};
+
+template <typename T>
+struct DHiddenEnd {
+  static constexpr bool kXAlong = true, kWAlong = false, kHalves = false;
+  static constexpr int kSegments = 1;
+  typedef Big Large;
+  FfnDHidden a;
+  __device__ const Side& x() const { return a.dz; }
+  __device__ const Side& w() const { return a.w; }
+  __host__ __device__ int64_t rows() const { return a.dz.len; }
+  __host__ __device__ int64_t cols() const { return a.h; }
+  __host__ __device__ int64_t end() const { return a.ldh; }
+  __host__ __device__ int64_t length() const { return a.o; }
+  struct Column {
+    int64_t c;
+  };
+  struct Ahead {
+    V8<T> hg, hu;
+  };
+  __device__ __forceinline__ Column column(int64_t c) const { return Column{c}; }
+  __device__ __forceinline__ Ahead ahead(const Column& k, int64_t r) const {
+    const int64_t at = r * a.ldh + (k.c < a.ldh ? k.c : 0);
+    return Ahead{*reinterpret_cast<const V8<T>*>(static_cast<const T*>(a.by_gate) + at),
+                 *reinterpret_cast<const V8<T>*>(static_cast<const T*>(a.by_up) + at)};
+  }
+  __device__ __forceinline__ void put(const Column& k, int64_t r, const Ahead& f, Floats<8> dh) const {
     dh *= a.scale;
-    Floats<8> dg = dh * __builtin_convertvector(hg[x & 1][g], Floats<8>);
-    Floats<8> du = dh * __builtin_convertvector(hu[x & 1][g], Floats<8>);
+    Floats<8> dg = dh * __builtin_convertvector(f.hg, Floats<8>), du = dh * __builtin_convertvector(f.hu, Floats<8>);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i >= a.h) dg[i] = du[i] = 0.0f;  // the padding, which products read
-    const int64_t at = r * a.ldh + c;
+      if (k.c + i >= a.h) dg[i] = du[i] = 0.0f;  // the padding, which products read
+    const int64_t at = r * a.ldh + k.c;
     store_vec<T, 8, true>(static_cast<T*>(a.dgate) + at, dg, 8);
     store_vec<T, 8, true>(static_cast<T*>(a.dup) + at, du, 8);
-  });
+  }
+};
+
+template <typename T>
+struct DXEnd {
+  static constexpr bool kXAlong = true, kWAlong = false, kHalves = false;
+  static constexpr int kSegments = 2;
+  typedef Big Large;
+  FfnDX a;
+  __device__ const Side& x() const { return a.dgu; }
+  __device__ const Side& w() const { return a.w; }
+  __host__ __device__ int64_t rows() const { return a.dgu.len; }
+  __host__ __device__ int64_t cols() const { return a.d; }
+  __host__ __device__ int64_t end() const { return a.d; }
+  __host__ __device__ int64_t length() const { return a.h; }
+  struct Column {
+    int64_t c;
+  };
+  struct Ahead {};
+  __device__ __forceinline__ Column column(int64_t c) const { return Column{c}; }
+  __device__ __forceinline__ Ahead ahead(const Column&, int64_t) const { return Ahead{}; }
+  __device__ __forceinline__ void put(const Column& k, int64_t r, const Ahead&, Floats<8> v) const {
+    store_vec<T, 8, false>(static_cast<T*>(a.dx) + r * a.lddx + k.c, v, left_of(a.d - k.c));
+  }
+};
+
+template <typename T, typename Cfg, typename End, bool kSplit>
+__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_product_kernel(End e) {
+  typedef ProductOf<T, Cfg, End::kXAlong, End::kWAlong, End::kHalves> P;
+  ABCD_TILE_LDS(P);
+  const Tiling& t = e.a.t;
+  int tx, tw;
+  tile_of(blockIdx.x, t.tiles_x, t.tiles_w, tx, tw);
+  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * (End::kHalves ? Cfg::TW / 2 : Cfg::TW);
+  int begin = 0, end = End::kSegments * steps_of<T>(e.length());
+  if (kSplit) {
+    begin = blockIdx.y * t.steps;
+    end = min(end, begin + t.steps);
+  }
+  P p;
+  p.template run<End::kSegments>(e.x(), e.w(), ix, iw, e.length(), begin, end, lds);
+  const int64_t c = iw + P::col_of(), rows = e.rows();
+  if constexpr (kSplit) {
+    const int64_t pitch = (e.cols() + 7) & ~int64_t(7);
+    auto at = [&](int half, int64_t r) {
+      return t.part + (((int64_t)blockIdx.y * (End::kHalves ? 2 : 1) + half) * rows + r) * pitch + c;
+    };
+    if constexpr (End::kHalves)
+      p.by_rows(lds, [&](int x, int g, Floats<8> v, Floats<8> v2) {
+        const int64_t r = ix + P::row_of(x, g);
+        if (r >= rows || c >= pitch) return;
+        store_vec<float, 8, true>(at(0, r), v, 8);
+        store_vec<float, 8, true>(at(1, r), v2, 8);
+      });
+    else
+      p.by_rows(lds, [&](int x, int g, Floats<8> v) {
+        const int64_t r = ix + P::row_of(x, g);
+        if (r < rows && c < pitch) store_vec<float, 8, true>(at(0, r), v, 8);
+      });
+  } else {
+    const bool inside = c < e.end();
+    const typename End::Column col = e.column(c);
+    typename End::Ahead ahead[2][P::kGroups];
+    auto fetch = [&](int x) {  // 16 rows ahead
+#pragma unroll
+      for (int g = 0; g < P::kGroups; ++g) {
+        const int64_t r = ix + P::row_of(x, g);
+        ahead[x & 1][g] = e.ahead(col, r < rows ? r : ix);
+      }
+    };
+    fetch(0);
+    auto put = [&](int x, int g, auto... v) {
+      if (g == 0 && x + 1 < P::FX) fetch(x + 1);
+      const int64_t r = ix + P::row_of(x, g);
+      if (r < rows && inside) e.put(col, r, ahead[x & 1][g], v...);
+    };
+    p.by_rows(lds, put);
+  }
 }
 
-template <typename T, typename Cfg>
-__global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dx_kernel(FfnDX a) {
-  typedef ProductOf<T, Cfg, true, false, false> P;
-  ABCD_TILE_LDS(P);
-  int tx, tw;
-  tile_of(blockIdx.x, a.tiles_x, a.tiles_w, tx, tw);
-  const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
-  P p;
-  p.template run<2>(a.dgu, a.w, ix, iw, 0, a.h, lds);
-  const int64_t c = iw + P::col_of();
-  const int left = left_of(a.d - c);
-  p.by_rows(lds, [&](int x, int group, Floats<8> v) {
-    const int64_t r = ix + P::row_of(x, group);
-    if (r < a.dgu.len && left > 0) store_vec<T, 8, false>(static_cast<T*>(a.dx) + r * a.lddx + c, v, left);
-  });
+// The parts of a split contraction added up in order, and what becomes of the sums: a
+// thread for 8 columns of a row.
+template <typename End>
+__global__ __launch_bounds__(kBlock) void ffn_join_kernel(End e) {
+  const int64_t pitch = (e.cols() + 7) & ~int64_t(7), rows = e.rows(), vecs = pitch / 8;
+  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (i >= rows * vecs) return;
+  const int64_t r = i / vecs, c = i % vecs * 8;
+  const typename End::Column col = e.column(c);
+  const typename End::Ahead ahead = e.ahead(col, r);
+  Floats<8> v[End::kHalves ? 2 : 1];
+#pragma unroll
+  for (int k = 0; k < (End::kHalves ? 2 : 1); ++k) {
+    const float* p = e.a.t.part + (k * rows + r) * pitch + c;
+    v[k] = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < e.a.t.splits; ++s)
+      v[k] += load_vec<float, 8, true>(p + (int64_t)s * (End::kHalves ? 2 : 1) * rows * pitch, 8);
+  }
+  if constexpr (End::kHalves)
+    e.put(col, r, ahead, v[0], v[1]);
+  else
+    e.put(col, r, ahead, v[0]);
 }
 
 // Which product a tile of the weights' gradients belongs to, and its place there.
@@ -184,13 +305,14 @@ __global__ __launch_bounds__(Cfg::WX* Cfg::WW * 64, 2) void ffn_dweight_kernel(F
   int tx, tw;
   const FfnDWeight::One& m = dweight_at(a, tile, tx, tw);
   const int64_t ix = (int64_t)tx * Cfg::TX, iw = (int64_t)tw * Cfg::TW;
-  int64_t k0 = 0, k1 = a.n;
+  int begin = 0, end = steps_of<T>(a.n);
   if (rest >= 0) {
-    k0 = rest % a.splits * a.per;
-    k1 = k0 + a.per < a.n ? k0 + a.per : a.n;
+    begin = rest % a.splits * a.steps;
+    end = min(end, begin + a.steps);
   }
   P p;
-  p.template run<1>(Side{{m.x, nullptr}, m.ldx, m.rows}, Side{{m.w, nullptr}, m.ldw, m.cols}, ix, iw, k0, k1, lds);
+  p.template run<1>(Side{{m.x, nullptr}, m.ldx, m.rows}, Side{{m.w, nullptr}, m.ldw, m.cols}, ix, iw, a.n, begin, end,
+                    lds);
   const int cw = P::col_of();
   const int left = left_of(m.cols - (iw + cw));
   p.by_rows(lds, [&](int x, int group, Floats<8> v) {
@@ -220,50 +342,68 @@ __global__ __launch_bounds__(TW) void ffn_dweight_sum_kernel(FfnDWeight a) {
 
 inline int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
 
-// The big tile where it gives most of the CUs one. (fp32, whose parts are
-// made on the way to LDS, has the small one only.)
-template <typename T>
-bool use_big(int64_t nx, int64_t nw, int tw) {
-  return sizeof(T) == 2 && tiles(nx, Big::TX) * tiles(nw, tw) >= 192;
+// The large tile where it gives most of the CUs one (fp32, whose parts are made on the
+// way to LDS, has the small one only); a split contraction where the small ones leave
+// half of the workgroups idle.
+template <typename T, typename End>
+int32_t run_product(const char* label, End e, hipStream_t stream) {
+  constexpr int kHalf = End::kHalves ? 2 : 1;
+  Tiling& t = e.a.t;
+  auto deal = [&](auto cfg) -> int64_t {
+    typedef decltype(cfg) Cfg;
+    t.tiles_x = (int)tiles(e.rows(), Cfg::TX);
+    t.tiles_w = (int)tiles(e.cols(), Cfg::TW / kHalf);
+    return (int64_t)t.tiles_x * t.tiles_w;
+  };
+  t.splits = 1;
+  if constexpr (sizeof(T) == 2) {
+    typedef typename End::Large L;
+    const int64_t grid = deal(L{});
+    if (grid >= 192) {
+      REQUIRE(grid < (int64_t(1) << 31), "too many tiles");
+      ABCD_LAUNCH(label, (ffn_product_kernel<T, L, End, false>), grid, L::WX* L::WW * 64, 0, stream, e);
+      ABCD_HIP(hipGetLastError());
+      return ABCD_OK;
+    }
+  }
+  const int64_t grid = deal(Small{});
+  REQUIRE(grid < (int64_t(1) << 31), "too many tiles");
+  const int steps = End::kSegments * steps_of<T>(e.length());
+  t.splits = product_splits(e.rows(), e.cols(), kHalf, steps);
+  if (t.splits == 1) {
+    ABCD_LAUNCH(label, (ffn_product_kernel<T, Small, End, false>), grid, Small::WX* Small::WW * 64, 0, stream, e);
+    ABCD_HIP(hipGetLastError());
+    return ABCD_OK;
+  }
+  t.steps = (steps + t.splits - 1) / t.splits;
+  ABCD_LAUNCH(label, (ffn_product_kernel<T, Small, End, true>), dim3(grid, t.splits), Small::WX* Small::WW * 64, 0,
+              stream, e);
+  ABCD_HIP(hipGetLastError());
+  const int64_t vecs = e.rows() * ((e.cols() + 7) / 8);
+  ABCD_LAUNCH("ffn_join", (ffn_join_kernel<End>), (vecs + kBlock - 1) / kBlock, kBlock, 0, stream, e);
+  ABCD_HIP(hipGetLastError());
+  return ABCD_OK;
 }
 
-#define ABCD_FFN_LAUNCH(label, kernel, Big_, a, nx, nw, half, stream, ...)                                \
-  do {                                                                                                    \
-    const bool big_ = use_big<T>(nx, nw, Big::TW / (half));                                               \
-    a.tiles_x = (int)tiles(nx, big_ ? Big::TX : Small::TX);                                               \
-    a.tiles_w = (int)tiles(nw, (big_ ? Big::TW : Small::TW) / (half));                                    \
-    const int64_t grid_ = (int64_t)a.tiles_x * a.tiles_w;                                                 \
-    REQUIRE(grid_ < (int64_t(1) << 31), "too many tiles");                                                \
-    if constexpr (sizeof(T) == 2)                                                                         \
-      if (big_)                                                                                           \
-        ABCD_LAUNCH(label, (kernel<T, Big_ __VA_ARGS__>), grid_, Big::WX* Big::WW * 64, 0, stream, a);      \
-    if (!big_)                                                                                            \
-      ABCD_LAUNCH(label, (kernel<T, Small __VA_ARGS__>), grid_, Small::WX* Small::WW * 64, 0, stream, a); \
-    ABCD_HIP(hipGetLastError());                                                                          \
-  } while (0)
-
 template <typename T>
-int32_t run_in(FfnIn a, hipStream_t stream) {
+int32_t run_in(const FfnIn& a, hipStream_t stream) {
   return with_act(a.act, [&](auto act) -> int32_t {
-    ABCD_FFN_LAUNCH("ffn_in", ffn_in_kernel, BigHalves, a, a.x.len, a.h, 2, stream, , decltype(act)::value);
-    return ABCD_OK;
+    return run_product<T>("ffn_in", InEnd<T, decltype(act)::value>{a}, stream);
   });
 }
 template <typename T>
-int32_t run_out(FfnOut a, hipStream_t stream) {
-  ABCD_FFN_LAUNCH("ffn_out", ffn_out_kernel, Big, a, a.hidden.len, a.o, 1, stream);
-  return ABCD_OK;
+int32_t run_out(const FfnOut& a, hipStream_t stream) {
+  return run_product<T>("ffn_out", OutEnd<T>{a}, stream);
 }
 template <typename T>
-int32_t run_dhidden(FfnDHidden a, hipStream_t stream) {
-  ABCD_FFN_LAUNCH("ffn_dhidden", ffn_dhidden_kernel, Big, a, a.dz.len, a.h, 1, stream);
-  return ABCD_OK;
+int32_t run_dhidden(const FfnDHidden& a, hipStream_t stream) {
+  return run_product<T>("ffn_dhidden", DHiddenEnd<T>{a}, stream);
 }
 template <typename T>
-int32_t run_dx(FfnDX a, hipStream_t stream) {
-  ABCD_FFN_LAUNCH("ffn_dx", ffn_dx_kernel, Big, a, a.dgu.len, a.d, 1, stream);
-  return ABCD_OK;
+int32_t run_dx(const FfnDX& a, hipStream_t stream) {
+  return run_product<T>("ffn_dx", DXEnd<T>{a}, stream);
 }
+
 template <typename T, typename Cfg>
 int32_t run_dweight_tiles(FfnDWeight a, int slots, hipStream_t stream) {
   int64_t total = 0;
@@ -279,7 +419,7 @@ int32_t run_dweight_tiles(FfnDWeight a, int slots, hipStream_t stream) {
   const int left = a.tiles % slots;
   a.splits = left == 0 ? 1 : (int)std::min<int64_t>(slots / left, std::max<int64_t>(1, a.n / 512));
   a.whole = a.splits > 1 ? a.tiles - left : a.tiles;
-  a.per = ((a.n + a.splits - 1) / a.splits + kStep<T> - 1) / kStep<T> * kStep<T>;
+  a.steps = (steps_of<T>(a.n) + a.splits - 1) / a.splits;
   const int rest = a.tiles - a.whole;
   ABCD_LAUNCH("ffn_dweight", (ffn_dweight_kernel<T, Cfg>), a.whole + rest * a.splits, Cfg::WX* Cfg::WW * 64, 0, stream,
               a);

@@ -159,14 +159,19 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
   s.wu = p.take(f.h * dp * sz);
   s.wd = p.take(f.o * hp * sz);
   if (!saved) s.hidden = p.take(n * hp * sz);
+  const int64_t step = kStepBytes / (int64_t)sz;
+  auto steps = [&](int64_t kn) { return (kn + step - 1) / step; };
+  size_t part = 0;
+  if (!backward || !saved) part = product_part(n, f.h, 2, steps(f.d));
+  if (!backward) part = std::max(part, product_part(n, f.o, 1, steps(f.h)));
   if (backward) {
     s.dz = p.take(n * op * sz);
     s.gate = p.take(n * hp * sz);
     s.up = p.take(n * hp * sz);
-    size_t part = (size_t)sum_parts_of(n) * (2 * f.h + f.o);
-    part = std::max(part, dweight_part(n));
-    s.part = static_cast<float*>(p.take(part * sizeof(float)));
+    part = std::max({part, product_part(n, f.h, 1, steps(f.o)), product_part(n, f.d, 1, 2 * steps(f.h)),
+                     (size_t)sum_parts_of(n) * (2 * f.h + f.o), dweight_part(n)});
   }
+  s.part = static_cast<float*>(p.take(part * sizeof(float)));
   s.bytes = p.used;
   return s;
 }
@@ -208,7 +213,7 @@ int32_t gate_up(const abcd_ffn& f, const Scratch& s, Side& w, hipStream_t stream
 int32_t few_in(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx, void* by_gate, void* by_up, void* hidden,
                hipStream_t stream) {
   const FfnIn in{Side{{x, nullptr}, ldx, n}, Side{{f.w_gate, f.w_up}, f.d, f.h}, f.b_gate, f.b_up, hidden, by_gate,
-                 by_up, f.d, f.h, up8(f.h), f.act, 0, 0};
+                 by_up, f.d, f.h, up8(f.h), f.act, Tiling{}};
   return FFN_BY_TYPE(f, ffn_few_in, in, stream);
 }
 
@@ -234,7 +239,7 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
   if (!hidden) hidden = s.hidden;
   const int64_t hp = up8(f.h);
   FfnOut out{Side{{hidden, nullptr}, hp, n}, Side{{f.w_down, nullptr}, f.h, f.o}, f.b_down, residual, y, f.h, f.o, ldr,
-             ldy, drop_key(f.p, f.seed, f.offset), 0, 0};
+             ldy, drop_key(f.p, f.seed, f.offset), Tiling{s.part, 0, 0, 1, 0}};
   if (few(n)) {
     TRY_STATUS(few_in(f, n, x, ldx, by_gate, by_up, hidden, stream));
     return FFN_BY_TYPE(f, ffn_few_out, out, stream);
@@ -242,7 +247,7 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
   Side xs, w;
   TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
   TRY_STATUS(gate_up(f, s, w, stream));
-  const FfnIn in{xs, w, f.b_gate, f.b_up, hidden, by_gate, by_up, f.d, f.h, hp, f.act, 0, 0};
+  const FfnIn in{xs, w, f.b_gate, f.b_up, hidden, by_gate, by_up, f.d, f.h, hp, f.act, Tiling{s.part, 0, 0, 1, 0}};
   TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
   TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, out.w, stream));
   return FFN_BY_TYPE(f, ffn_out, out, stream);
@@ -290,7 +295,7 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
       by_up = s.up;
       hidden = s.hidden;
     } else if (!hidden) {
-      const FfnIn in{xs, wgu, f.b_gate, f.b_up, s.hidden, s.gate, s.up, f.d, f.h, hp, f.act, 0, 0};
+      const FfnIn in{xs, wgu, f.b_gate, f.b_up, s.hidden, s.gate, s.up, f.d, f.h, hp, f.act, Tiling{s.part, 0, 0, 1, 0}};
       TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
       by_gate = s.gate;
       by_up = s.up;
@@ -300,12 +305,12 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
   // W side across: its index is h, the contraction o
   const bool inner = dx || dw_gate || dw_up || db_gate || db_up;
   if (n > 0 && inner) {
-    const FfnDHidden dh{dz, Side{{wd.p[0], nullptr}, wd.ld, f.h}, by_gate, by_up, s.gate, s.up, f.o, f.h, hp, scale, 0, 0};
+    const FfnDHidden dh{dz, Side{{wd.p[0], nullptr}, wd.ld, f.h}, by_gate, by_up, s.gate, s.up, f.o, f.h, hp, scale, Tiling{s.part, 0, 0, 1, 0}};
     TRY_STATUS(FFN_BY_TYPE(f, ffn_dhidden, dh, stream));
   }
   const Side dgu{{s.gate, s.up}, hp, n};
   if (n > 0 && dx) {
-    const FfnDX a{dgu, Side{{wgu.p[0], wgu.p[1]}, wgu.ld, f.d}, dx, f.h, f.d, lddx, 0, 0};
+    const FfnDX a{dgu, Side{{wgu.p[0], wgu.p[1]}, wgu.ld, f.d}, dx, f.h, f.d, lddx, Tiling{s.part, 0, 0, 1, 0}};
     TRY_STATUS(FFN_BY_TYPE(f, ffn_dx, a, stream));
   }
   FfnDWeight dw{};

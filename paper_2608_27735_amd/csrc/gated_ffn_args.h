@@ -15,6 +15,14 @@ struct Side {
   int64_t len;  // of the index that is not contracted (of each half)
 };
 
+// How a product is dealt out: tiles, and (with few of them) parts of the contraction
+// of `steps` steps each, whose sums go to part: [splits][halves][rows][columns up to a
+// multiple of 8].
+struct Tiling {
+  float* part;
+  int tiles_x, tiles_w, splits, steps;
+};
+
 // hidden and its derivatives by gate and up: [n][ldh], columns [h, ldh) zero;
 // by_gate NULL: only hidden
 struct FfnIn {
@@ -25,7 +33,8 @@ struct FfnIn {
   void* by_gate;
   void* by_up;
   int64_t d, h, ldh;
-  int act, tiles_x, tiles_w;
+  int act;
+  Tiling t;
 };
 struct FfnOut {
   Side hidden, w;
@@ -34,7 +43,7 @@ struct FfnOut {
   void* y;
   int64_t h, o, ldr, ldy;
   DropKey key;
-  int tiles_x, tiles_w;
+  Tiling t;
 };
 // dgate and dup may be by_gate and by_up themselves
 struct FfnDHidden {
@@ -45,17 +54,17 @@ struct FfnDHidden {
   void* dup;
   int64_t o, h, ldh;
   float scale;  // of dz
-  int tiles_x, tiles_w;
+  Tiling t;
 };
 struct FfnDX {
   Side dgu, w;
   void* dx;
   int64_t h, d, lddx;
-  int tiles_x, tiles_w;
+  Tiling t;
 };
 // The weights' gradients, out = scale X' W over n rows each, their tiles one after the
 // other. The first `whole` of these take a workgroup each, the others one for each of
-// `splits` parts of `per` rows, whose sums go to part: [tiles - whole][splits][tile].
+// `splits` parts of the rows, whose sums go to part: [tiles - whole][splits][tile].
 struct FfnDWeight {
   struct One {
     const void* x;
@@ -66,12 +75,30 @@ struct FfnDWeight {
     int tiles_x, tiles_w, first;
   } one[3];
   float* part;
-  int64_t n, per;
-  int count, tiles, whole, splits;
+  int64_t n;
+  int count, tiles, whole, splits, steps;
 };
 
 // Workgroups that run at once with tiles of 256 x 256, one a CU, and of 128 x 128.
 constexpr int kCUs = 256, kBigSlots = kCUs, kSmallSlots = 2 * kCUs;
+
+// Floats of the parts that a product of rows x cols (of `halves` of them) over
+// `steps` steps writes, 0 if its contraction is not split: it is where its tiles of
+// 128 x 128 leave half of the workgroups that fit idle, into at least four steps each.
+inline int64_t product_tiles(int64_t rows, int64_t cols, int halves) {
+  return (rows + 127) / 128 * ((halves * cols + 127) / 128);
+}
+inline int product_splits(int64_t rows, int64_t cols, int halves, int64_t steps) {
+  const int64_t tiles = product_tiles(rows, cols, halves);
+  if (tiles == 0 || 2 * tiles > kSmallSlots || steps < 8) return 1;
+  int64_t s = kSmallSlots / tiles;
+  s = s < steps / 4 ? s : steps / 4;
+  return (int)(s < 32 ? s : 32);
+}
+inline size_t product_part(int64_t rows, int64_t cols, int halves, int64_t steps) {
+  const int s = product_splits(rows, cols, halves, steps);
+  return s == 1 ? 0 : (size_t)s * halves * rows * ((cols + 7) & ~int64_t(7));
+}
 
 // The narrow block, in one launch each way.
 struct FfnNarrow {

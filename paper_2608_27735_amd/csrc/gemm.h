@@ -39,6 +39,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kStepBytes = 128;
 template <typename T>
 constexpr int kStep = kStepBytes / (int)sizeof(T);
+template <typename T>
+__host__ __device__ inline int steps_of(int64_t kn) {
+  return (int)((kn + kStep<T> - 1) / kStep<T>);
+}
 
 // 16 bytes of a lane: 8 elements of 16 bits, or 4 of 32.
 template <typename T>
@@ -267,29 +271,30 @@ struct Product : Accumulators<TX, TW, kWX, kWW, kHalves> {
     }
   }
 
-  // acc = sum over the segments' contractions [kbeg, kend) of X and W at the tile's
-  // first indexes ix, iw. lds: kLdsBytes.
+  // acc = the sum over steps [begin, end) of X and W at the tile's first indexes ix, iw:
+  // kSegments contractions of length kn one after the other, each in steps_of(kn) steps.
+  // lds: kLdsBytes.
   template <int kSegments>
-  __device__ __forceinline__ void run(const Side& X, const Side& W, int64_t ix, int64_t iw, int64_t kbeg, int64_t kend,
-                                      LdsChar* lds) {
+  __device__ __forceinline__ void run(const Side& X, const Side& W, int64_t ix, int64_t iw, int64_t kn, int begin,
+                                      int end, LdsChar* lds) {
     this->clear();
     LdsChar *lds0 = lds, *lds1 = lds + kStageBytes;
     TileLoads<T, TX, kXAlong, NT> lx;
     TileLoads<T, TW, kWAlong, NT> lw;
     lx.init(X.ld);
     lw.init(W.ld);
-    const int per = (int)((kend - kbeg + kStep<T> - 1) / kStep<T>), steps = per * kSegments;
+    const int per = steps_of<T>(kn);
     auto fetch = [&](int s, LdsChar* lds) {
       const int seg = kSegments > 1 && s >= per ? 1 : 0;
-      const int64_t k0 = kbeg + (int64_t)(s - seg * per) * kStep<T>;
-      load_tile<T, TX, kXAlong, NT, false>(lx, lds, X.p[seg], nullptr, X.ld, X.len, ix, k0, kend);
+      const int64_t k0 = (int64_t)(s - seg * per) * kStep<T>;
+      load_tile<T, TX, kXAlong, NT, false>(lx, lds, X.p[seg], nullptr, X.ld, X.len, ix, k0, kn);
       load_tile<T, TW, kWAlong, NT, kHalves>(lw, lds + TX * kStepBytes, W.p[kHalves ? 0 : seg], W.p[1], W.ld, W.len, iw,
-                                            k0, kend);
+                                            k0, kn);
     };
-    if (steps > 0) fetch(0, lds0);
-    for (int s = 0; s < steps; ++s) {
+    if (begin < end) fetch(begin, lds0);
+    for (int s = begin; s < end; ++s) {
       __syncthreads();  // step s has arrived, and nothing reads the other buffer any more
-      turn(fetch, s + 1, s + 1 < steps, lds1, lds0);
+      turn(fetch, s + 1, s + 1 < end, lds1, lds0);
       LdsChar* const t = lds0;
       lds0 = lds1;
       lds1 = t;
@@ -434,26 +439,26 @@ struct Product<float, TX, TW, kWX, kWW, kXAlong, kWAlong, kHalves> : Accumulator
   }
 
   template <int kSegments>
-  __device__ __forceinline__ void run(const Side& X, const Side& W, int64_t ix, int64_t iw, int64_t kbeg, int64_t kend,
-                                      LdsChar* lds) {
+  __device__ __forceinline__ void run(const Side& X, const Side& W, int64_t ix, int64_t iw, int64_t kn, int begin,
+                                      int end, LdsChar* lds) {
     this->clear();
     PartLoads<TX, kXAlong, NT, false> lx;
     PartLoads<TW, kWAlong, NT, kHalves> lw;
     lx.init(X.ld);
     lw.init(W.ld);
-    const int per = (int)((kend - kbeg + 31) / 32), steps = per * kSegments;
+    const int per = steps_of<float>(kn);
     auto fetch = [&](int s) {
       const int seg = kSegments > 1 && s >= per ? 1 : 0;
-      const int64_t k0 = kbeg + (int64_t)(s - seg * per) * 32;
-      lx.fetch(X.p[seg], nullptr, X.ld, X.len, ix, k0, kend);
-      lw.fetch(W.p[kHalves ? 0 : seg], W.p[1], W.ld, W.len, iw, k0, kend);
+      const int64_t k0 = (int64_t)(s - seg * per) * 32;
+      lx.fetch(X.p[seg], nullptr, X.ld, X.len, ix, k0, kn);
+      lw.fetch(W.p[kHalves ? 0 : seg], W.p[1], W.ld, W.len, iw, k0, kn);
     };
-    if (steps > 0) fetch(0);
-    for (int s = 0; s < steps; ++s) {
+    if (begin < end) fetch(begin);
+    for (int s = begin; s < end; ++s) {
       __syncthreads();  // nothing reads the last step's parts any more
       lx.put(lds);
       lw.put(lds + kXBytes);
-      if (s + 1 < steps) fetch(s + 1);
+      if (s + 1 < end) fetch(s + 1);
       __syncthreads();
       step(lds);
     }
