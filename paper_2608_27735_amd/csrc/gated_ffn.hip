@@ -128,14 +128,21 @@ struct Scratch {
 size_t dweight_part(int64_t n) { return n < 1024 ? 0 : (size_t)kBigSlots * 256 * 256; }
 static_assert((size_t)kBigSlots * 256 * 256 >= (size_t)kSmallSlots * 128 * 128, "the large tiles' parts are the larger");
 
-// Whether the narrow kernels take the block: what they hold in registers and LDS,
-// in 16-bit types, and rows enough to share the cost of setting the weights up.
+// Whether the narrow kernels take the block, both ways or the forward alone: what they
+// hold in registers and LDS, in 16-bit types, and rows enough to share the cost of
+// setting the weights up.
 bool narrow(const abcd_ffn& f, int64_t n) {
-  return f.dtype != ABCD_F32 && f.d <= 64 && f.o <= 64 && f.h <= 128 && n >= 1024;
+  return f.dtype != ABCD_F32 && narrow_shape(f.d, f.h, f.o) == 1 && n >= 1024;
+}
+bool narrow_forward(const abcd_ffn& f, int64_t n) {
+  const int shape = f.dtype == ABCD_F32 ? 0 : narrow_shape(f.d, f.h, f.o);
+  return shape == 1 ? n >= 1024 : shape > 1 && n >= 4096;
 }
 // Whether the kernels for a few rows take the forward.
 bool few(int64_t n) { return n <= 64; }
-int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 255) / 256, 2 * kCUs); }
+int64_t narrow_blocks(const abcd_ffn& f, int64_t n) {
+  return std::min<int64_t>((n + 255) / 256, (narrow_shape(f.d, f.h, f.o) == 1 ? 2 : 1) * kCUs);
+}
 int64_t narrow_bwd_blocks(int64_t n) { return std::min<int64_t>((n + 63) / 64, kCUs); }
 int64_t narrow_sums(const abcd_ffn& f) { return 2 * f.h * f.d + f.o * f.h + 2 * f.h + f.o; }
 
@@ -144,7 +151,7 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
   const int64_t dp = up8(f.d), hp = up8(f.h), op = up8(f.o);
   Pieces p{static_cast<char*>(workspace)};
   Scratch s{};
-  if (!saved && narrow(f, n)) {
+  if (!saved && (backward ? narrow(f, n) : narrow_forward(f, n))) {
     if (backward) s.part = static_cast<float*>(p.take(narrow_bwd_blocks(n) * narrow_sums(f) * sizeof(float)));
     s.bytes = p.used;
     return s;
@@ -229,11 +236,11 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
                          int64_t ldr, void* y, int64_t ldy, void* by_gate, void* by_up, void* hidden, void* workspace,
                          hipStream_t stream) {
   if (n == 0) return ABCD_OK;
-  if (!hidden && narrow(f, n)) {
+  if (!hidden && narrow_forward(f, n)) {
     const FfnNarrow a{x, f.w_gate, f.w_up, f.w_down, f.b_gate, f.b_up, f.b_down, residual, y, n, f.d, f.h, f.o,
                       ldx, ldr, ldy, drop_key(f.p, f.seed, f.offset), f.act};
-    return f.dtype == ABCD_F16 ? ffn_narrow_f16(a, narrow_blocks(n), stream)
-                               : ffn_narrow_bf16(a, narrow_blocks(n), stream);
+    return f.dtype == ABCD_F16 ? ffn_narrow_f16(a, narrow_blocks(f, n), stream)
+                               : ffn_narrow_bf16(a, narrow_blocks(f, n), stream);
   }
   const Scratch s = layout(f, n, hidden != nullptr, false, workspace);
   if (!hidden) hidden = s.hidden;

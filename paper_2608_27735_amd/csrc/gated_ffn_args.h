@@ -100,7 +100,13 @@ inline size_t product_part(int64_t rows, int64_t cols, int halves, int64_t steps
   return s == 1 ? 0 : (size_t)s * halves * rows * ((cols + 7) & ~int64_t(7));
 }
 
-// The narrow block, in one launch each way.
+// The narrow block, in one launch each way. Which of the forward's compiled shapes
+// holds it, 0 if none: with its weights in 48, 144, 120 or 144 KB of LDS.
+inline int narrow_shape(int64_t d, int64_t h, int64_t o) {
+  if (d <= 64 && o <= 64 && h <= 384) return h <= 128 ? 1 : 2;
+  if (d <= 128 && o <= 128 && h <= 192) return o <= 64 ? 3 : 4;
+  return 0;
+}
 struct FfnNarrow {
   const void *x, *w_gate, *w_up, *w_down, *b_gate, *b_up, *b_down;
   const void* res;

@@ -53,7 +53,7 @@ constexpr int kNarrowThreads = 512, kNarrowBwdThreads = 512;
 // kWhole: d, h and o are multiples of 8. kDF: contractions of 32 that hold d; kOB: 16-column blocks of o; kHC: 32-column
 // chunks of h
 template <typename T, int kAct, int kDF, int kOB, int kHC, bool kWhole>
-__global__ __launch_bounds__(kNarrowThreads, 4) void ffn_narrow_kernel(FfnNarrow a) {
+__global__ __launch_bounds__(kNarrowThreads, (kHC * (4 * kDF + kOB) <= 72 ? 4 : 2)) void ffn_narrow_kernel(FfnNarrow a) {
   typedef typename Frag<T>::type F;
   constexpr int kNarrowWaves = kNarrowThreads / 64, kRowFrags = 2, kRows = kRowFrags * 16;
   constexpr int kChunk = 4 * kDF + kOB;  // fragments of a chunk: gate, up, down
@@ -464,16 +464,32 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     }
 }
 
+// The smallest of the compiled shapes that holds the block (narrow_shape), with two
+// workgroups a CU or, from 72 KB of weights on, one.
 template <typename T>
 int32_t run_narrow(const FfnNarrow& a, int64_t blocks, hipStream_t stream) {
   return with_act(a.act, [&](auto act) -> int32_t {
-    constexpr int kAct = decltype(act)::value;
-    if (a.d % 8 == 0 && a.h % 8 == 0 && a.o % 8 == 0)
-      ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, kAct, 2, 4, 4, true>), blocks, kNarrowThreads, 0, stream, a);
-    else
-      ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, kAct, 2, 4, 4, false>), blocks, kNarrowThreads, 0, stream, a);
-    ABCD_HIP(hipGetLastError());
-    return ABCD_OK;
+    auto launch = [&](auto df, auto ob, auto hc) -> int32_t {
+      constexpr int kAct = decltype(act)::value, kDF = decltype(df)::value, kOB = decltype(ob)::value,
+                    kHC = decltype(hc)::value;
+      if (a.d % 8 == 0 && a.h % 8 == 0 && a.o % 8 == 0)
+        ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, kAct, kDF, kOB, kHC, true>), blocks, kNarrowThreads, 0, stream, a);
+      else
+        ABCD_LAUNCH("ffn_narrow", (ffn_narrow_kernel<T, kAct, kDF, kOB, kHC, false>), blocks, kNarrowThreads, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      return ABCD_OK;
+    };
+    std::integral_constant<int, 2> i2;
+    std::integral_constant<int, 4> i4;
+    std::integral_constant<int, 6> i6;
+    std::integral_constant<int, 8> i8;
+    std::integral_constant<int, 12> i12;
+    switch (narrow_shape(a.d, a.h, a.o)) {
+      case 1: return launch(i2, i4, i4);
+      case 2: return launch(i2, i4, i12);
+      case 3: return launch(i4, i4, i6);
+      default: return launch(i4, i8, i6);
+    }
   });
 }
 
