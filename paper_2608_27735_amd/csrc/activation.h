@@ -14,7 +14,10 @@ __device__ __forceinline__ float sigmoid(float g) {
 
 // a(g) and a'(g). The activation is a template argument of the kernels: with a
 // branch at every element no two elements' exponentials overlap.
-template <int kAct>
+// kShort: for what is rounded to 16 bits, the error function by Abramowitz and Stegun's
+// 7.1.26, within 1.5e-7 of it: a polynomial of 1 / (1 + p |x|) times the exponential
+// that the derivative needs too.
+template <int kAct, bool kShort>
 __device__ __forceinline__ float activate(float g, float& slope) {
   if (kAct == ABCD_ACT_SILU) {
     const float s = sigmoid(g), v = g * s;
@@ -22,8 +25,19 @@ __device__ __forceinline__ float activate(float g, float& slope) {
     return v;
   }
   if (kAct == ABCD_ACT_GELU) {
-    const float c = 0.5f + 0.5f * erff(0.70710678118654752f * g);
-    slope = c + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
+    const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);  // e^(-g^2 / 2)
+    float c;  // the normal distribution
+    if (kShort) {
+      const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.0f));
+      float s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+      s = fmaf(t, s, 0.5f * 1.421413741f);
+      s = fmaf(t, s, 0.5f * -0.284496736f);
+      s = fmaf(t, s, 0.5f * 0.254829592f) * t * e;
+      c = g < 0.0f ? s : 1.0f - s;
+    } else {
+      c = 0.5f + 0.5f * erff(0.70710678118654752f * g);
+    }
+    slope = fmaf(g * 0.39894228040143268f, e, c);
     return g * c;
   }
   slope = g > 0.0f ? 1.0f : 0.0f;

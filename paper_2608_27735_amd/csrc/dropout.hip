@@ -31,11 +31,11 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropArgs a) {
     const T* res = a.res ? static_cast<const T*>(a.res) + row * a.ldr : nullptr;
     T* y = static_cast<T*>(a.y) + row * a.ldy;
     for (int c = t * N; c < a.d; c += a.lanes * N) {
-      const int64_t below = a.n - 1 - row, left = a.d - c;
+      const int left = a.d - c;
       // (what lies behind the row is not stored)
-      const typename Frag<T>::type v = load_frag<T, kWhole>(x + c, left, below * a.ldx + left);
+      const typename Frag<T>::type v = load_frag<T, kWhole>(x + c, left, room_of(a.n, row, a.ldx, left));
       Floats<N> r = 0.0f;
-      if (res) r = __builtin_convertvector((load_frag<T, kWhole>(res + c, left, below * a.ldr + left)), Floats<N>);
+      if (res) r = __builtin_convertvector((load_frag<T, kWhole>(res + c, left, room_of(a.n, row, a.ldr, left))), Floats<N>);
       store_vec<T, N, kWhole>(y + c, drop_vec<N>(__builtin_convertvector(v, Floats<N>), a.key, (uint32_t)row, (uint32_t)c, r), a.d - c);
     }
   }

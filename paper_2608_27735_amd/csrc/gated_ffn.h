@@ -103,7 +103,7 @@ struct InEnd {
     for (int i = 0; i < 8; ++i) {
       if (k.c + i >= a.h) g[i] = u[i] = 0.0f;  // the padding, which products read
       float slope;
-      hu[i] = activate<kAct>(g[i], slope);
+      hu[i] = activate<kAct, sizeof(T) == 2>(g[i], slope);
       h[i] = hu[i] * u[i];
       hg[i] = slope * u[i];
     }

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kBlock) void pack_rows_kernel(PackArgs a) {
     for (int c = t * N; c < a.ldd; c += a.lanes * N) {
       const int left = a.cols - c;
       const Floats<N> v =
-          __builtin_convertvector((load_first<T, false>(s + c, left, (a.n - 1 - row) * a.ld + left)), Floats<N>);
+          __builtin_convertvector((load_first<T, false>(s + c, left, room_of(a.n, row, a.ld, left))), Floats<N>);
       store_vec<T, N, true>(d + c, drop_vec<N>(v, a.key, (uint32_t)row, (uint32_t)c, 0.0f), N);
     }
   }
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kBlock) void column_sums_kernel(ColumnSums a) {
 #pragma unroll 4
     for (int64_t row = (int64_t)blockIdx.y * rows + threadIdx.x / m.lanes; row < a.n; row += (int64_t)gridDim.y * rows)
       s += __builtin_convertvector((load_first<T, false>(static_cast<const T*>(m.m) + row * m.ld + c, m.cols - c,
-                                                         (a.n - 1 - row) * m.ld + m.cols - c)),
+                                                         room_of(a.n, row, m.ld, m.cols - c))),
                                    Floats<N>);
   }
 #pragma unroll

@@ -39,11 +39,11 @@ __device__ __forceinline__ void few_products(f32x4 (&acc)[kX][kSides], const T* 
 #pragma unroll
       for (int s = 0; s < kSides; ++s)
         fw[s][t] = load_frag<T, kWhole>(w[s] + (int64_t)(first + j) * ldw + k, first + j < rows ? left : 0,
-                                        (int64_t)(rows - 1 - first - j) * ldw + left);
+                                        room_of(rows, first + j, ldw, left));
 #pragma unroll
       for (int i = 0; i < kX; ++i)
         fx[i][t] = load_frag<T, kWhole>(x + (int64_t)(i * 16 + j) * ldx + k, i * 16 + j < n ? left : 0,
-                                        (int64_t)(n - 1 - i * 16 - j) * ldx + left);
+                                        room_of(n, i * 16 + j, ldx, left));
     }
 #pragma unroll
     for (int t = 0; t < kAhead; ++t) {
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kFewInWaves * 64) void ffn_few_in_kernel(FfnIn a) {
     const bool in = c + i < a.h;  // else padding, which products read
     const float g = in ? sum[0][i] : 0.0f, u = in ? sum[1][i] : 0.0f;
     float slope;
-    hu[i] = activate<kAct>(g, slope);
+    hu[i] = activate<kAct, sizeof(T) == 2>(g, slope);
     h[i] = hu[i] * u;
     hg[i] = slope * u;
   }

@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kNarrowThreads, (kHC * (4 * kDF + kOB) <= 72 ? 4 : 
       for (int f = 0; f < kDF; ++f) {
         const int c = f * 32 + q * 8;
         x[x0][f] = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + c, r < a.n ? d - c : 0,
-                                        (a.n - 1 - r) * a.ldx + d - c);
+                                        room_of(a.n, r, a.ldx, d - c));
       }
     }
   };
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kNarrowThreads, (kHC * (4 * kDF + kOB) <= 72 ? 4 : 
           const int64_t r = r0 + i * 16 + j;
           const int c = q * (kOB * 4) + b * 8;
           res[i][b] = load_frag<T, kWhole>(static_cast<const T*>(a.res) + r * a.ldr + c, r < a.n ? o - c : 0,
-                                           (a.n - 1 - r) * a.ldr + o - c);
+                                           room_of(a.n, r, a.ldr, o - c));
         }
     f32x4 y[kRowFrags][kOB];
 #pragma unroll
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kNarrowThreads, (kHC * (4 * kDF + kOB) <= 72 ? 4 : 
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float slope;
-            g[i][b][e] = activate<kAct>(g[i][b][e], slope) * u[i][b][e];
+            g[i][b][e] = activate<kAct, true>(g[i][b][e], slope) * u[i][b][e];
           }
         hid[i] = join<T>(g[i][0], g[i][1]);
       }
@@ -243,11 +243,11 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     for (int k = 0; k < kH / 64; ++k) {
       const int row = k * 64 + lr, col = k * 64 + lc;
       const F g = load_first<T, kWhole>(static_cast<const T*>(a.w_gate) + (int64_t)row * d + lc, row < h ? d - lc : 0,
-                                           (int64_t)(h - 1 - row) * d + d - lc);
+                                           room_of(h, row, d, d - lc));
       const F u = load_first<T, kWhole>(static_cast<const T*>(a.w_up) + (int64_t)row * d + lc, row < h ? d - lc : 0,
-                                           (int64_t)(h - 1 - row) * d + d - lc);
+                                           room_of(h, row, d, d - lc));
       const F w = load_first<T, kWhole>(static_cast<const T*>(a.w_down) + (int64_t)lr * h + col, lr < o ? h - col : 0,
-                                           (int64_t)(o - 1 - lr) * h + h - col);
+                                           room_of(o, lr, h, h - col));
       const int at = row_at(lr, lc / 4) + k * kTile;
       *(__attribute__((address_space(3))) F*)(t + at) = g;
       *(__attribute__((address_space(3))) F*)(t + kH * 128 + at) = u;
@@ -292,9 +292,9 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
   auto fetch = [&](int64_t block) {
     const int64_t r = block * 64 + lr;
     nx = load_frag<T, kWhole>(static_cast<const T*>(a.x) + r * a.ldx + lc, r < a.n ? d - lc : 0,
-                              (a.n - 1 - r) * a.ldx + d - lc);
+                              room_of(a.n, r, a.ldx, d - lc));
     nz = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + r * a.lddy + lc, r < a.n ? o - lc : 0,
-                              (a.n - 1 - r) * a.lddy + o - lc);
+                              room_of(a.n, r, a.lddy, o - lc));
   };
   // dz of a block: what the forward kept of dy; the factor comes with the sums, at
   // the end
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float slope;
-          const float v = activate<kAct>(g[e], slope);
+          const float v = activate<kAct, true>(g[e], slope);
           vh[i][e] = v * u[e];
           vg[i][e] = dh[e] * (u[e] * slope);
           vu[i][e] = dh[e] * v;

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kBlock) void layer_norm_kernel(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const int c = (j * G + t) * N;
-      raw[j] = load_frag<T, kWhole>(x + c, a.d - c, (a.n - 1 - row) * a.ldx + a.d - c);
+      raw[j] = load_frag<T, kWhole>(x + c, a.d - c, room_of(a.n, row, a.ldx, a.d - c));
     }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -176,14 +176,13 @@ __global__ __launch_bounds__(kBlock) void layer_norm_bwd_kernel(NormBwdArgs a) {
   float nmean, nrstd;
   auto fetch = [&](int64_t row) {
     const bool in = row < a.n;
-    const int64_t below = a.n - 1 - row;  // rows behind this one
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const int c = (j * G + t) * N, left = in ? a.d - c : 0;
-      nx[j] = load_frag<T, kWhole>(static_cast<const T*>(a.x) + row * a.ldx + c, left, below * a.ldx + left);
-      ndy[j] = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + row * a.lddy + c, left, below * a.lddy + left);
+      nx[j] = load_frag<T, kWhole>(static_cast<const T*>(a.x) + row * a.ldx + c, left, room_of(a.n, row, a.ldx, left));
+      ndy[j] = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + row * a.lddy + c, left, room_of(a.n, row, a.lddy, left));
       nadd[j] = load_frag<T, kWhole>(static_cast<const T*>(a.add) + row * a.ldadd + c, a.add ? left : 0,
-                                     below * a.ldadd + left);
+                                     room_of(a.n, row, a.ldadd, left));
     }
     nmean = in ? a.mean[row] : 0.0f;
     nrstd = in ? a.rstd[row] : 0.0f;
