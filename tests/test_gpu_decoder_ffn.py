@@ -117,6 +117,51 @@ def test_few_rows(api, n, d, h, o):
     run(api, n, d, h, o, torch.float32, "silu", True, 0.0)
 
 
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,d,h,o", [
+    (137, 1024, 520, 72), (70, 600, 2100, 90), (65, 4000, 40, 9), (200, 33, 3001, 17), (300, 515, 1300, 260)])
+def test_few_tiles_and_long_sums(api, dtype, n, d, h, o):
+    """Products whose few tiles have their sums' terms split among workgroups."""
+    run(api, n, d, h, o, dtype, "silu", True, 0.1)
+    run(api, n, d, h, o, dtype, "gelu", False, 0.0, pad=3, skip=1)
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n,d,h,o", [
+    (4096, 64, 384, 64), (4111, 1, 129, 1), (5000, 59, 200, 33), (4097, 65, 192, 64), (6001, 127, 1, 3),
+    (5003, 96, 176, 18), (4500, 128, 192, 128), (4100, 64, 100, 65), (4129, 101, 190, 127), (70001, 72, 130, 70)])
+def test_narrow_forward(api, dtype, n, d, h, o):
+    """Blocks whose forward alone is one launch."""
+    for act, bias, p, pad, skip in [("silu", True, 0.1, 0, 0), ("gelu", False, 0.0, 5, 1), ("relu", True, 1.0, 8, 8)]:
+        say("narrow forward", n, d, h, o, dtype, act, p, pad, skip)
+        x, w, res = rand(1, n, d, dtype, pad, skip), weights(10, d, h, o, dtype, bias), rand(2, n, o, dtype, skip, pad)
+        keep = R.keep_mask(n, o, p, 5, 9) if 0.0 < p < 1.0 else torch.full((n, o), p < 1.0)
+        ref = R.ffn(R.d64(x), {k: R.d64(v) for k, v in w.items()}, act, R.UNIT[dtype], R.d64(res), keep, p)
+        wide = torch.full((n, o + 9), 7.0, dtype=dtype, device="cuda")
+        api.gated_ffn(x, w, act, residual=res, p=p, seed=5, offset=9, out=wide[:, 4:4 + o])
+        check("y", wide[:, 4:4 + o], ref["y"])
+        assert (wide[:, :4] == 7).all() and (wide[:, 4 + o:] == 7).all()
+
+
+def test_gelu_far_out(api):
+    """Where the normal distribution is all but 0 or 1: the block of one input, with
+    gates from -12 to 12, against the formula."""
+    g = torch.linspace(-12.0, 12.0, 4801)
+    one = torch.ones(1, 1, device="cuda")
+    for dtype in DT:
+        x = g.to(dtype).cuda()[:, None]
+        w = dict(w_gate=one.to(dtype), w_up=torch.zeros_like(one).to(dtype), w_down=one.to(dtype),
+                 b_gate=torch.zeros(1, dtype=dtype, device="cuda"), b_up=torch.ones(1, dtype=dtype, device="cuda"),
+                 b_down=torch.zeros(1, dtype=dtype, device="cuda"))
+        want = R.act(R.d64(x), "gelu")[0]
+        for rows in (x, x[:40], x[:500]):
+            y = R.d64(api.gated_ffn(rows, w, "gelu")["y"])
+            ref = want[:rows.shape[0]]
+            # two roundings to the type; 1.5e-7 |g| / 2 (the polynomial's) or fp32 roundings of g
+            tol = 2.0 * R.UNIT[dtype] * ref.abs() + 4 * R.TINY[dtype] + 3e-7 * R.d64(rows).abs()
+            assert ((y - ref).abs() <= tol).all(), (dtype, rows.shape, ((y - ref).abs() - tol).max())
+
+
 def test_no_rows(api):
     w = weights(1, 16, 24, 8, torch.float32, True)
     x, dy = torch.empty(0, 16, device="cuda"), torch.empty(0, 8, device="cuda")
