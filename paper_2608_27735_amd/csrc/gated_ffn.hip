@@ -119,7 +119,7 @@ struct Pieces {
 
 struct Scratch {
   void *x, *wg, *wu, *wd, *dz, *gate, *up, *hidden;
-  float* part;
+  float *part, *dx_part;
   size_t bytes;
 };
 
@@ -131,13 +131,11 @@ static_assert((size_t)kBigSlots * 256 * 256 >= (size_t)kSmallSlots * 128 * 128, 
 // Whether the narrow kernels take the block, both ways or the forward alone: what they
 // hold in registers and LDS, in 16-bit types, and rows enough to share the cost of
 // setting the weights up.
-bool narrow(const abcd_ffn& f, int64_t n) {
-  return f.dtype != ABCD_F32 && narrow_shape(f.d, f.h, f.o) == 1 && n >= 1024;
-}
 bool narrow_forward(const abcd_ffn& f, int64_t n) {
   const int shape = f.dtype == ABCD_F32 ? 0 : narrow_shape(f.d, f.h, f.o);
   return shape == 1 ? n >= 1024 : shape > 1 && n >= 4096;
 }
+bool narrow(const abcd_ffn& f, int64_t n) { return narrow_forward(f, n) && narrow_shape(f.d, f.h, f.o) <= 2; }
 // Whether the kernels for a few rows take the forward.
 bool few(int64_t n) { return n <= 64; }
 int64_t narrow_blocks(const abcd_ffn& f, int64_t n) {
@@ -152,7 +150,10 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
   Pieces p{static_cast<char*>(workspace)};
   Scratch s{};
   if (!saved && (backward ? narrow(f, n) : narrow_forward(f, n))) {
-    if (backward) s.part = static_cast<float*>(p.take(narrow_bwd_blocks(n) * narrow_sums(f) * sizeof(float)));
+    if (backward) {
+      s.part = static_cast<float*>(p.take(narrow_bwd_blocks(n) * narrow_groups(f.h) * narrow_sums(f) * sizeof(float)));
+      if (f.h > 128) s.dx_part = static_cast<float*>(p.take(n * up8(f.d) * sizeof(float)));
+    }
     s.bytes = p.used;
     return s;
   }
@@ -273,9 +274,14 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
   mask.scale = 1.0f;
   if (!hidden && narrow(f, n)) {
     const int64_t blocks = narrow_bwd_blocks(n);
-    const FfnNarrowBwd a{x, dy, f.w_gate, f.w_up, f.w_down, f.b_gate, f.b_up, dx, s.part, n, f.d, f.h, f.o,
-                         ldx, lddy, lddx, narrow_sums(f), mask, scale, f.act};
-    TRY_STATUS(f.dtype == ABCD_F16 ? ffn_narrow_bwd_f16(a, blocks, stream) : ffn_narrow_bwd_bf16(a, blocks, stream));
+    const int64_t sz = (int64_t)type_bytes(f.dtype);
+    auto from = [&](const void* p, int64_t e) { return p ? static_cast<const char*>(p) + e * sz : nullptr; };
+    for (int64_t c = 0; c < f.h; c += 128) {
+      const FfnNarrowBwd a{x, dy, from(f.w_gate, c * f.d), from(f.w_up, c * f.d), from(f.w_down, c), from(f.b_gate, c),
+                           from(f.b_up, c), dx, s.part, s.dx_part, n, f.d, std::min<int64_t>(f.h - c, 128), f.o, f.h,
+                           c, ldx, lddy, lddx, up8(f.d), narrow_sums(f), c + 128 >= f.h, mask, scale, f.act};
+      TRY_STATUS(f.dtype == ABCD_F16 ? ffn_narrow_bwd_f16(a, blocks, stream) : ffn_narrow_bwd_bf16(a, blocks, stream));
+    }
     SumOuts outs{};
     outs.add(dw_gate, f.h * f.d);
     outs.add(dw_up, f.h * f.d);
@@ -283,7 +289,7 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     outs.add(db_gate, f.h);
     outs.add(db_up, f.h);
     outs.add(db_down, f.o);
-    return launch_sum_parts(s.part, blocks, outs, f.dtype, stream);
+    return launch_sum_parts(s.part, blocks * narrow_groups(f.h), outs, f.dtype, stream);
   }
   Side xs{}, wgu{}, wd{}, dz{};
   if (n > 0) {

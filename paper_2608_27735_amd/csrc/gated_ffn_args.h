@@ -115,16 +115,22 @@ struct FfnNarrow {
   DropKey key;
   int act;
 };
-// part: [workgroups][sums], the sums laid out as dWg, dWu, dWd, dbg, dbu, dbd
+// The backward of columns first .. first + h - 1 of an h of ldd (whose pointers are moved
+// to them; ldd is also w_down's row stride). part: [workgroups][narrow_groups][sums], the
+// sums laid out as dWg, dWu, dWd, dbg, dbu, dbd of all of h. dx_part: dx so far, rows of
+// ldp; the last columns' launch writes dx.
 struct FfnNarrowBwd {
   const void *x, *dy, *w_gate, *w_up, *w_down, *b_gate, *b_up;
   void* dx;  // may be NULL
-  float* part;
-  int64_t n, d, h, o, ldx, lddy, lddx, sums;
+  float *part, *dx_part;
+  int64_t n, d, h, o, ldd, first, ldx, lddy, lddx, ldp, sums;
+  bool last;
   DropKey key;
   float scale;  // of what the forward kept
   int act;
 };
+// How many groups of its waves share a block's rows.
+inline int narrow_groups(int64_t h) { return h <= 64 ? 2 : 1; }
 int32_t ffn_narrow_f16(const FfnNarrow&, int64_t blocks, hipStream_t);
 int32_t ffn_narrow_bf16(const FfnNarrow&, int64_t blocks, hipStream_t);
 int32_t ffn_narrow_bwd_f16(const FfnNarrowBwd&, int64_t blocks, hipStream_t);

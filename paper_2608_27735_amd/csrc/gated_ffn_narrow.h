@@ -13,10 +13,10 @@
 // fragment order, loaded once per workgroup, and for every 32 columns of h the
 // wave makes g and u, h from them, and adds h's part of y.
 //
-// Backward: a workgroup takes 64 rows at a time, and each of its 8 waves kHB x 16
-// columns of h for all of them, so that its part of the weights stays in its
-// registers, and so do its parts of dWg, dWu and dWd over all rows that the
-// workgroup takes. g, u, dh, dg, du and h are made again in registers; only dg and
+// Backward: a workgroup takes 64 rows at a time, and each of its 8 waves 16 columns
+// of h, so that its part of the weights stays in its registers, and so do its parts of
+// dWg, dWu and dWd over all rows that the workgroup takes. An h of more than 128
+// columns takes a launch for each 128, which pass dx on in fp32. g, u, dh, dg, du and h are made again in registers; only dg and
 // du go through LDS, to the waves that make dx, one round later. x and dz are read
 // from LDS along for g, u and dh, and across (ds_read_b64_tr_b16) for the weights'
 // gradients. The biases' gradients are products with ones. Workgroups write their
@@ -214,11 +214,13 @@ __device__ __forceinline__ int turned_at(int row, int unit) {
   return row * 128 + ((unit ^ (((row & 3) << 2) | ((row >> 2) & 3))) * 8);
 }
 
-// d and o up to 64, h up to kHB * 128
-template <typename T, int kAct, int kHB, bool kWhole, bool kDrop>
+// d and o up to 64. kGroups: 1: h up to 128, each wave all 64 rows; 2: h up to 64, four
+// waves the first 32 rows and four the others, with sums of their own. kMore: the launch
+// takes up to 128 columns of an h with more.
+template <typename T, int kAct, int kGroups, bool kMore, bool kWhole, bool kDrop>
 __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(FfnNarrowBwd a) {
   typedef typename Frag<T>::type F;
-  constexpr int kTile = 64 * 128, kH = kHB * 128;
+  constexpr int kTile = 64 * 128, kH = 128 / kGroups;
   __shared__ __align__(16) char xs[2][kTile];        // [64 rows][64 columns]
   __shared__ __align__(16) char zs[2][kTile];
   __shared__ __align__(16) char turned[2][2 * kH * 128];  // [dg, then du: column of h][64 rows]
@@ -227,9 +229,9 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // The weights pass through LDS in tiles of 64 x 64, from which each wave takes its
   // own: as they lie in memory most of them are needed across their rows.
-  // this wave's columns of h: block b's column j
-  F wg[kHB][2], wu[kHB][2], wd[kHB][2];
-  f32x4 bg[kHB], bu[kHB];
+  const int group = wave / (8 / kGroups), first = wave % (8 / kGroups) * 16, col = first + j;  // its columns of h
+  F wg[2], wu[2], wd[2];
+  f32x4 bg, bu;
   // what it makes of dx: columns xb * 16 .. + 15 of rows xr * 32 .. + 31
   const int xb = wave & 3, xr = wave >> 2;
   F wx[2][kH / 32];
@@ -246,8 +248,8 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
                                            room_of(h, row, d, d - lc));
       const F u = load_first<T, kWhole>(static_cast<const T*>(a.w_up) + (int64_t)row * d + lc, row < h ? d - lc : 0,
                                            room_of(h, row, d, d - lc));
-      const F w = load_first<T, kWhole>(static_cast<const T*>(a.w_down) + (int64_t)lr * h + col, lr < o ? h - col : 0,
-                                           room_of(o, lr, h, h - col));
+      const F w = load_first<T, kWhole>(static_cast<const T*>(a.w_down) + (int64_t)lr * a.ldd + col, lr < o ? h - col : 0,
+                                           room_of(o, lr, a.ldd, h - col));
       const int at = row_at(lr, lc / 4) + k * kTile;
       *(__attribute__((address_space(3))) F*)(t + at) = g;
       *(__attribute__((address_space(3))) F*)(t + kH * 128 + at) = u;
@@ -255,18 +257,14 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     }
     __syncthreads();
 #pragma unroll
-    for (int b = 0; b < kHB; ++b) {
-      const int col = (wave * kHB + b) * 16 + j;
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        wg[b][f] = *(LdsF*)(t + row_at(col, f * 8 + q * 2));
-        wu[b][f] = *(LdsF*)(t + kH * 128 + row_at(col, f * 8 + q * 2));
-        const int first = (wave * kHB + b) * 16, row = f * 32 + q * 8 + (j >> 2), unit = (first & 63) / 4 + (j & 3);
-        wd[b][f] = read_across<T>(td + first / 64 * kTile + row_at(row, unit), td + first / 64 * kTile + row_at(row + 4, unit));
-      }
-      bg[b] = a.b_gate ? (float)at_or_0<T>(a.b_gate, 0, col, 1, h) : 0.0f;
-      bu[b] = a.b_up ? (float)at_or_0<T>(a.b_up, 0, col, 1, h) : 0.0f;
+    for (int f = 0; f < 2; ++f) {
+      wg[f] = *(LdsF*)(t + row_at(col, f * 8 + q * 2));
+      wu[f] = *(LdsF*)(t + kH * 128 + row_at(col, f * 8 + q * 2));
+      const int row = f * 32 + q * 8 + (j >> 2), unit = (first & 63) / 4 + (j & 3);
+      wd[f] = read_across<T>(td + first / 64 * kTile + row_at(row, unit), td + first / 64 * kTile + row_at(row + 4, unit));
     }
+    bg = a.b_gate ? (float)at_or_0<T>(a.b_gate, 0, col, 1, h) : 0.0f;
+    bu = a.b_up ? (float)at_or_0<T>(a.b_up, 0, col, 1, h) : 0.0f;
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -277,13 +275,9 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
       }
     __syncthreads();
   }
-  f32x4 dwg[kHB][4], dwu[kHB][4], dwd[kHB][4], sg[kHB], su[kHB], sz = 0.0f;
+  f32x4 dwg[4], dwu[4], dwd[4], sg = 0.0f, su = 0.0f, sz = 0.0f;
 #pragma unroll
-  for (int b = 0; b < kHB; ++b) {
-    sg[b] = su[b] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) dwg[b][k] = dwu[b][k] = dwd[b][k] = 0.0f;
-  }
+  for (int k = 0; k < 4; ++k) dwg[k] = dwu[k] = dwd[k] = 0.0f;
   F ones;
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones[e] = (T)1.0f;
@@ -322,7 +316,18 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     read_lo[i] = turned_at(row, unit);
     read_hi[i] = turned_at(row + 4, unit);
   }
-  f32x4 ax[2];
+  f32x4 ax[2], px[2];
+  // px: what the columns of h before this launch's made of dx
+  auto dx_fetch = [&](int64_t block) {
+    if (!kMore) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t r = block * 64 + xr * 32 + i * 16 + j;
+      const int c = xb * 16 + q * 4;
+      const bool in = a.dx && a.first > 0 && r >= 0 && r < a.n && c < d;
+      px[i] = *reinterpret_cast<const f32x4*>(in ? a.dx_part + r * a.ldp + c : reinterpret_cast<const float*>(zeros));
+    }
+  };
   // half of dx of a block whose dg and du lie at t
   auto dx_half = [&](const LdsChar* t, int half) {
 #pragma unroll
@@ -340,64 +345,59 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t r = block * 64 + xr * 32 + i * 16 + j;
-      if (a.dx && r >= 0 && r < a.n && left > 0)
-        store_vec<T, 4, kWhole>(static_cast<T*>(a.dx) + r * a.lddx + c, ax[i] * a.scale, left);
+      if (kMore) ax[i] += px[i];
+      if (a.dx && r >= 0 && r < a.n && left > 0) {
+        if (kMore && !a.last)
+          *reinterpret_cast<f32x4*>(a.dx_part + r * a.ldp + c) = ax[i];
+        else
+          store_vec<T, 4, kWhole>(static_cast<T*>(a.dx) + r * a.lddx + c, ax[i] * a.scale, left);
+      }
     }
   };
   // 32 rows of a block: g, u and dh, from these dg, du and h, which stay in registers
   // for the weights' gradients; dg and du also go to t
   auto half_of = [&](LdsChar* x, LdsChar* z, LdsChar* t, int half) {
-    F dg[kHB], du[kHB], hid[kHB];
+    f32x4 vg[2], vu[2], vh[2];
 #pragma unroll
-    for (int b = 0; b < kHB; ++b) {
-      f32x4 vg[2], vu[2], vh[2];
+    for (int i = 0; i < 2; ++i) {
+      const int row = (half * 32 + i * 16) * 128;
+      f32x4 g = bg, u = bu, dh = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = (half * 32 + i * 16) * 128;
-        f32x4 g = bg[b], u = bu[b], dh = 0.0f;
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          const F fx = *(LdsF*)(x + row + along[f]);
-          const F fz = *(LdsF*)(z + row + along[f]);
-          g = mma(fx, wg[b][f], g);
-          u = mma(fx, wu[b][f], u);
-          dh = mma(fz, wd[b][f], dh);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float slope;
-          const float v = activate<kAct, true>(g[e], slope);
-          vh[i][e] = v * u[e];
-          vg[i][e] = dh[e] * (u[e] * slope);
-          vu[i][e] = dh[e] * v;
-        }
+      for (int f = 0; f < 2; ++f) {
+        const F fx = *(LdsF*)(x + row + along[f]);
+        const F fz = *(LdsF*)(z + row + along[f]);
+        g = mma(fx, wg[f], g);
+        u = mma(fx, wu[f], u);
+        dh = mma(fz, wd[f], dh);
       }
-      dg[b] = join<T>(vg[0], vg[1]);
-      du[b] = join<T>(vu[0], vu[1]);
-      hid[b] = join<T>(vh[0], vh[1]);
-      const int col = (wave * kHB + b) * 16 + j;
-      typedef typename VecOf<T, 4>::type V4;
-      typedef __attribute__((address_space(3))) V4 LdsV4;
-      const int unit = half * 8 + q;
-      *(LdsV4*)(t + turned_at(col, unit)) = __builtin_shufflevector(dg[b], dg[b], 0, 1, 2, 3);
-      *(LdsV4*)(t + turned_at(col, unit + 4)) = __builtin_shufflevector(dg[b], dg[b], 4, 5, 6, 7);
-      *(LdsV4*)(t + turned_at(kH + col, unit)) = __builtin_shufflevector(du[b], du[b], 0, 1, 2, 3);
-      *(LdsV4*)(t + turned_at(kH + col, unit + 4)) = __builtin_shufflevector(du[b], du[b], 4, 5, 6, 7);
-      sg[b] = mma(ones, dg[b], sg[b]);
-      su[b] = mma(ones, du[b], su[b]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float slope;
+        const float v = activate<kAct, true>(g[e], slope);
+        vh[i][e] = v * u[e];
+        vg[i][e] = dh[e] * (u[e] * slope);
+        vu[i][e] = dh[e] * v;
+      }
     }
+    const F dg = join<T>(vg[0], vg[1]), du = join<T>(vu[0], vu[1]), hid = join<T>(vh[0], vh[1]);
+    typedef typename VecOf<T, 4>::type V4;
+    typedef __attribute__((address_space(3))) V4 LdsV4;
+    const int unit = half * 8 + q;
+    *(LdsV4*)(t + turned_at(col, unit)) = __builtin_shufflevector(dg, dg, 0, 1, 2, 3);
+    *(LdsV4*)(t + turned_at(col, unit + 4)) = __builtin_shufflevector(dg, dg, 4, 5, 6, 7);
+    *(LdsV4*)(t + turned_at(kH + col, unit)) = __builtin_shufflevector(du, du, 0, 1, 2, 3);
+    *(LdsV4*)(t + turned_at(kH + col, unit + 4)) = __builtin_shufflevector(du, du, 4, 5, 6, 7);
+    sg = mma(ones, dg, sg);
+    su = mma(ones, du, su);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       // column 16 k + j, rows half 32 + 4 q .. + 3 and 16 further on
       const int at = half * 32 * 128 + across[k];
       const F fx = read_across<T>(x + at, x + at + 16 * 128);
       const F fz = read_across<T>(z + at, z + at + 16 * 128);
-#pragma unroll
-      for (int b = 0; b < kHB; ++b) {
-        dwg[b][k] = mma(fx, dg[b], dwg[b][k]);
-        dwu[b][k] = mma(fx, du[b], dwu[b][k]);
-        dwd[b][k] = mma(fz, hid[b], dwd[b][k]);
-      }
+      dwg[k] = mma(fx, dg, dwg[k]);
+      dwu[k] = mma(fx, du, dwu[k]);
+      dwd[k] = mma(fz, hid, dwd[k]);
     }
     const int at = half * 32 * 128 + across_z;
     sz = mma(read_across<T>(z + at, z + at + 16 * 128), ones, sz);
@@ -408,9 +408,9 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
                   const LdsChar* __restrict__ before) {
     ax[0] = ax[1] = 0.0f;
     dx_half(before, 0);
-    half_of(x, z, t, 0);
+    if (kGroups == 1) half_of(x, z, t, 0);
     dx_half(before, 1);
-    half_of(x, z, t, 1);
+    half_of(x, z, t, kGroups == 1 ? 1 : group);
   };
 
   const int64_t blocks = (a.n + 63) / 64;
@@ -422,45 +422,44 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
     const int64_t next = block + gridDim.x;
     __syncthreads();  // this block's rows are in LDS, and so are the last one's dg and du
     fetch(next);      // past the end: zeros
+    dx_fetch(last);
     turn((LdsChar*)xs[cur], (LdsChar*)zs[cur], (LdsChar*)turned[cur], (LdsChar*)turned[cur ^ 1]);
     dx_store(last);  // the first turn's is of no block: its rows are below 0
     last = block;
     put(next, cur ^ 1);
   }
   __syncthreads();
+  dx_fetch(last);
   ax[0] = ax[1] = 0.0f;
   dx_half((LdsChar*)turned[cur ^ 1], 0);
   dx_half((LdsChar*)turned[cur ^ 1], 1);
   dx_store(last);
 
-  // sums: [dWg h x d][dWu h x d][dWd o x h][dbg h][dbu h][dbd o]
-  float* const part = a.part + (int64_t)blockIdx.x * a.sums;
-  const int64_t up = (int64_t)h * d, down = 2 * up, biases = down + (int64_t)o * h;
-#pragma unroll
-  for (int b = 0; b < kHB; ++b) {
-    const int col = (wave * kHB + b) * 16 + j;
-    if (col >= h) continue;
+  // sums: [dWg h x d][dWu h x d][dWd o x h][dbg h][dbu h][dbd o], of all of h
+  float* const part = a.part + ((int64_t)blockIdx.x * kGroups + group) * a.sums;
+  const int64_t up = a.ldd * d, down = 2 * up, biases = down + a.ldd * o, at = a.first + col;
+  if (col < h) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int c = k * 16 + q * 4 + e;
         if (c < d) {
-          part[(int64_t)col * d + c] = dwg[b][k][e] * a.scale;
-          part[up + (int64_t)col * d + c] = dwu[b][k][e] * a.scale;
+          part[at * d + c] = dwg[k][e] * a.scale;
+          part[up + at * d + c] = dwu[k][e] * a.scale;
         }
-        if (c < o) part[down + (int64_t)c * h + col] = dwd[b][k][e] * a.scale;
+        if (c < o) part[down + c * a.ldd + at] = dwd[k][e] * a.scale;
       }
     if (q == 0) {
-      part[biases + col] = sg[b][0] * a.scale;
-      part[biases + h + col] = su[b][0] * a.scale;
+      part[biases + at] = sg[0] * a.scale;
+      part[biases + a.ldd + at] = su[0] * a.scale;
     }
   }
-  if (wave < 4 && j == 0)
+  if ((kGroups == 2 || wave < 4) && j == 0 && a.first == 0)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int c = wave * 16 + q * 4 + e;
-      if (c < o) part[biases + 2 * h + c] = sz[e] * a.scale;
+      const int c = (wave & 3) * 16 + q * 4 + e;
+      if (c < o) part[biases + 2 * a.ldd + c] = sz[e] * a.scale;
     }
 }
 
@@ -498,19 +497,28 @@ int32_t run_narrow_bwd(const FfnNarrowBwd& a, int64_t blocks, hipStream_t stream
   return with_act(a.act, [&](auto act) -> int32_t {
     constexpr int kAct = decltype(act)::value;
     const bool whole = a.d % 8 == 0 && a.h % 8 == 0 && a.o % 8 == 0;
-    auto launch = [&](auto drop) {
-      constexpr bool kDrop = decltype(drop)::value;
+    auto launch = [&](auto groups, auto more, auto drop) {
+      constexpr int kGroups = decltype(groups)::value;
+      constexpr bool kMore = decltype(more)::value, kDrop = decltype(drop)::value;
       if (whole)
-        ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, true, kDrop>), blocks, kNarrowBwdThreads, 0,
-                    stream, a);
+        ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, kGroups, kMore, true, kDrop>), blocks,
+                    kNarrowBwdThreads, 0, stream, a);
       else
-        ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, 1, false, kDrop>), blocks, kNarrowBwdThreads, 0,
-                    stream, a);
+        ABCD_LAUNCH("ffn_narrow_bwd", (ffn_narrow_bwd_kernel<T, kAct, kGroups, kMore, false, kDrop>), blocks,
+                    kNarrowBwdThreads, 0, stream, a);
+    };
+    auto of = [&](auto drop) {
+      if (a.ldd > 128)
+        launch(std::integral_constant<int, 1>{}, std::true_type{}, drop);
+      else if (narrow_groups(a.ldd) == 1)
+        launch(std::integral_constant<int, 1>{}, std::false_type{}, drop);
+      else
+        launch(std::integral_constant<int, 2>{}, std::false_type{}, drop);
     };
     if (a.key.mode != 0)
-      launch(std::true_type{});
+      of(std::true_type{});
     else
-      launch(std::false_type{});
+      of(std::false_type{});
     ABCD_HIP(hipGetLastError());
     return ABCD_OK;
   });

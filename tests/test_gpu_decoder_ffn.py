@@ -86,6 +86,16 @@ def test_narrow_rows(api, dtype, n, d, h, o):
     run(api, n, d, h, o, dtype, "relu", True, 1.0)
 
 
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n,d,h,o", [
+    (4096, 64, 256, 64), (4097, 59, 129, 33), (5000, 8, 384, 16), (4200, 33, 300, 64), (20011, 64, 136, 40),
+    (1024, 64, 64, 64), (1031, 63, 63, 63), (40001, 17, 24, 64)])
+def test_narrow_rows_of_other_hidden_widths(api, dtype, n, d, h, o):
+    """Launches for parts of h, and waves that share a block's rows."""
+    run(api, n, d, h, o, dtype, "silu", True, 0.1)
+    run(api, n, d, h, o, dtype, "gelu", False, 0.0, pad=5, skip=1)
+
+
 def test_narrow_kernels_agree_with_the_products(api):
     """The same block by the tiled products (what the forward keeps is given)."""
     n, d, h, o = 5000, 64, 128, 64
