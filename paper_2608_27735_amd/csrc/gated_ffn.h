@@ -342,9 +342,14 @@ __global__ __launch_bounds__(TW) void ffn_dweight_sum_kernel(FfnDWeight a) {
 
 inline int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
 
-// The large tile where it gives most of the CUs one (fp32, whose parts are made on the
-// way to LDS, has the small one only); a split contraction where the small ones leave
-// half of the workgroups idle.
+// The large tile (in 16-bit types: fp32's parts are made on the way to LDS, which has
+// room for the small one) where it gives most of the CUs one. A CU holds two of the
+// small workgroups but one large, whose end nothing overlaps: after a short contraction,
+// or where half of a large tile would lie outside, the small ones win (bf16, 300,000
+// rows, K = 128: h Wd' 57 against 95 us, dh 72 against 87; 65,536 rows, K = 1024: 66
+// against 55). Not in the first product, whose small tiles have 64 columns of a side
+// (the same rows, K = 64 to 192: 5 to 15 percent slower). A split contraction where
+// the small ones leave half of the workgroups idle.
 template <typename T, typename End>
 int32_t run_product(const char* label, End e, hipStream_t stream) {
   constexpr int kHalf = End::kHalves ? 2 : 1;
@@ -356,10 +361,11 @@ int32_t run_product(const char* label, End e, hipStream_t stream) {
     return (int64_t)t.tiles_x * t.tiles_w;
   };
   t.splits = 1;
+  const int steps = End::kSegments * steps_of<T>(e.length());
   if constexpr (sizeof(T) == 2) {
     typedef typename End::Large L;
     const int64_t grid = deal(L{});
-    if (grid >= 192) {
+    if (grid >= 192 && (End::kHalves || (steps > 8 && e.cols() > Small::TW))) {
       REQUIRE(grid < (int64_t(1) << 31), "too many tiles");
       ABCD_LAUNCH(label, (ffn_product_kernel<T, L, End, false>), grid, L::WX* L::WW * 64, 0, stream, e);
       ABCD_HIP(hipGetLastError());
@@ -368,7 +374,6 @@ int32_t run_product(const char* label, End e, hipStream_t stream) {
   }
   const int64_t grid = deal(Small{});
   REQUIRE(grid < (int64_t(1) << 31), "too many tiles");
-  const int steps = End::kSegments * steps_of<T>(e.length());
   t.splits = product_splits(e.rows(), e.cols(), kHalf, steps);
   if (t.splits == 1) {
     ABCD_LAUNCH(label, (ffn_product_kernel<T, Small, End, false>), grid, Small::WX* Small::WW * 64, 0, stream, e);
