@@ -7,23 +7,29 @@
 namespace abcd {
 namespace {
 
-// Copies rows of `cols` elements into rows of ldd, the rest of each zeroed, with
-// dropout where the key says so: what a product reads has to start on 16 bytes,
-// its rows a multiple of that apart, with zeros up to it.
-struct PackArgs {
-  const void* src;
-  void* dst;
-  int64_t ld, ldd, n;
-  int cols, lanes;
-  DropKey key;
+// Copies of up to five arrays in one launch, each rows of `cols` elements into rows of
+// ldd, the rest of each zeroed, with dropout where the key says so: what a product
+// reads has to start on 16 bytes, its rows a multiple of that apart, with zeros up to it.
+struct Packs {
+  struct One {
+    const void* src;
+    void* dst;
+    int64_t ld, ldd, n;
+    int cols, lanes, first, blocks;
+    DropKey key;
+  } one[5];
+  int count = 0, blocks = 0;
 };
 
 template <typename T>
-__global__ __launch_bounds__(kBlock) void pack_rows_kernel(PackArgs a) {
+__global__ __launch_bounds__(kBlock) void pack_rows_kernel(Packs packs) {
   constexpr int N = kPer16<T>;
+  int k = 0;
+  while (k + 1 < packs.count && (int)blockIdx.x >= packs.one[k + 1].first) ++k;
+  const Packs::One& a = packs.one[k];
   const int t = threadIdx.x & (a.lanes - 1), rows = kBlock / a.lanes;
-  for (int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / a.lanes; row < a.n;
-       row += (int64_t)gridDim.x * rows) {
+  for (int64_t row = (int64_t)((int)blockIdx.x - a.first) * rows + threadIdx.x / a.lanes; row < a.n;
+       row += (int64_t)a.blocks * rows) {
     const T* s = static_cast<const T*>(a.src) + row * a.ld;
     T* d = static_cast<T*>(a.dst) + row * a.ldd;
     for (int c = t * N; c < a.ldd; c += a.lanes * N) {
@@ -84,14 +90,19 @@ int lanes_for(int nvec) {
 
 int64_t sum_parts_of(int64_t n) { return std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, 256)); }
 
-int32_t pack(int32_t dtype, int64_t n, int64_t cols, const void* src, int64_t ld, void* dst, int64_t ldd,
-             const DropKey& key, hipStream_t stream) {
+void add_pack(Packs& p, int32_t dtype, int64_t n, int64_t cols, const void* src, int64_t ld, void* dst, int64_t ldd,
+              const DropKey& key) {
+  const int lanes = lanes_for((int)(ldd * (int64_t)type_bytes(dtype) / 16));
+  const int64_t rows = kBlock / lanes;
+  const int blocks = (int)std::min<int64_t>((n + rows - 1) / rows, 1 << 20);
+  p.one[p.count++] = Packs::One{src, dst, ld, ldd, n, (int)cols, lanes, p.blocks, blocks, key};
+  p.blocks += blocks;
+}
+
+int32_t launch(const Packs& p, int32_t dtype, hipStream_t stream) {
+  if (p.blocks == 0) return ABCD_OK;
   return with_type(dtype, [&](auto z) -> int32_t {
-    typedef decltype(z) T;
-    PackArgs a{src, dst, ld, ldd, n, (int)cols, lanes_for((int)(ldd / kPer16<T>)), key};
-    const int64_t rows = kBlock / a.lanes;
-    ABCD_LAUNCH("pack_rows", (pack_rows_kernel<T>), std::min<int64_t>((n + rows - 1) / rows, 1 << 20), kBlock, 0,
-                stream, a);
+    ABCD_LAUNCH("pack_rows", (pack_rows_kernel<decltype(z)>), p.blocks, kBlock, 0, stream, p);
     ABCD_HIP(hipGetLastError());
     return ABCD_OK;
   });
@@ -189,33 +200,20 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
    : (f).dtype == ABCD_F16 ? fn##_f16(__VA_ARGS__)              \
                            : fn##_bf16(__VA_ARGS__))
 
-// A weight as products read it: itself or its copy.
-int32_t weight(const abcd_ffn& f, const void* w, int64_t rows, int64_t cols, void* copy, Side& s,
-               hipStream_t stream) {
-  s = Side{{w, nullptr}, cols, rows};
-  if (direct(f.dtype, w, cols, cols)) return ABCD_OK;
-  s.p[0] = copy;
-  s.ld = up8(cols);
-  return pack(f.dtype, rows, cols, w, cols, copy, s.ld, DropKey{}, stream);
-}
-
-int32_t rows_of(const abcd_ffn& f, const void* m, int64_t n, int64_t cols, int64_t ld, void* copy, Side& s,
-                hipStream_t stream) {
-  s = Side{{m, nullptr}, ld, n};
-  if (direct(f.dtype, m, cols, ld)) return ABCD_OK;
-  s.p[0] = copy;
-  s.ld = up8(cols);
-  return pack(f.dtype, n, cols, m, ld, copy, s.ld, DropKey{}, stream);
+// n rows of `cols` elements as products read them: themselves or a copy.
+Side side_of(Packs& p, const abcd_ffn& f, const void* m, int64_t n, int64_t cols, int64_t ld, void* copy) {
+  if (direct(f.dtype, m, cols, ld)) return Side{{m, nullptr}, ld, n};
+  add_pack(p, f.dtype, n, cols, m, ld, copy, up8(cols), DropKey{});
+  return Side{{copy, nullptr}, up8(cols), n};
 }
 
 // Both projections as one side of two halves; their copies are laid out alike.
-int32_t gate_up(const abcd_ffn& f, const Scratch& s, Side& w, hipStream_t stream) {
-  const bool both = direct(f.dtype, f.w_gate, f.d, f.d) && direct(f.dtype, f.w_up, f.d, f.d);
-  w = Side{{f.w_gate, f.w_up}, f.d, f.h};
-  if (both) return ABCD_OK;
-  w = Side{{s.wg, s.wu}, up8(f.d), f.h};
-  TRY_STATUS(pack(f.dtype, f.h, f.d, f.w_gate, f.d, s.wg, w.ld, DropKey{}, stream));
-  return pack(f.dtype, f.h, f.d, f.w_up, f.d, s.wu, w.ld, DropKey{}, stream);
+Side gate_up(Packs& p, const abcd_ffn& f, const Scratch& s) {
+  if (direct(f.dtype, f.w_gate, f.d, f.d) && direct(f.dtype, f.w_up, f.d, f.d))
+    return Side{{f.w_gate, f.w_up}, f.d, f.h};
+  add_pack(p, f.dtype, f.h, f.d, f.w_gate, f.d, s.wg, up8(f.d), DropKey{});
+  add_pack(p, f.dtype, f.h, f.d, f.w_up, f.d, s.wu, up8(f.d), DropKey{});
+  return Side{{s.wg, s.wu}, up8(f.d), f.h};
 }
 
 int32_t few_in(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx, void* by_gate, void* by_up, void* hidden,
@@ -252,12 +250,12 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
     TRY_STATUS(few_in(f, n, x, ldx, by_gate, by_up, hidden, stream));
     return FFN_BY_TYPE(f, ffn_few_out, out, stream);
   }
-  Side xs, w;
-  TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
-  TRY_STATUS(gate_up(f, s, w, stream));
+  Packs copies;
+  const Side xs = side_of(copies, f, x, n, f.d, ldx, s.x), w = gate_up(copies, f, s);
+  out.w = side_of(copies, f, f.w_down, f.o, f.h, f.h, s.wd);
+  TRY_STATUS(launch(copies, f.dtype, stream));
   const FfnIn in{xs, w, f.b_gate, f.b_up, hidden, by_gate, by_up, f.d, f.h, hp, f.act, Tiling{s.part, 0, 0, 1, 0}};
   TRY_STATUS(FFN_BY_TYPE(f, ffn_in, in, stream));
-  TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, out.w, stream));
   return FFN_BY_TYPE(f, ffn_out, out, stream);
 }
 
@@ -293,15 +291,17 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
   }
   Side xs{}, wgu{}, wd{}, dz{};
   if (n > 0) {
-    TRY_STATUS(rows_of(f, x, n, f.d, ldx, s.x, xs, stream));
-    TRY_STATUS(gate_up(f, s, wgu, stream));
-    TRY_STATUS(weight(f, f.w_down, f.o, f.h, s.wd, wd, stream));
+    Packs copies;
+    xs = side_of(copies, f, x, n, f.d, ldx, s.x);
+    wgu = gate_up(copies, f, s);
+    wd = side_of(copies, f, f.w_down, f.o, f.h, f.h, s.wd);
     if (f.p > 0.0) {
       dz = Side{{s.dz, nullptr}, up8(f.o), n};
-      TRY_STATUS(pack(f.dtype, n, f.o, dy, lddy, s.dz, dz.ld, mask, stream));
+      add_pack(copies, f.dtype, n, f.o, dy, lddy, s.dz, dz.ld, mask);
     } else {
-      TRY_STATUS(rows_of(f, dy, n, f.o, lddy, s.dz, dz, stream));
+      dz = side_of(copies, f, dy, n, f.o, lddy, s.dz);
     }
+    TRY_STATUS(launch(copies, f.dtype, stream));
     if (!hidden && few(n)) {
       TRY_STATUS(few_in(f, n, x, ldx, s.gate, s.up, s.hidden, stream));
       by_gate = s.gate;
