@@ -459,7 +459,8 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
  * ABCD_ACT_SILU g sigmoid(g), ABCD_ACT_GELU g Phi(g) (Phi the normal distribution,
  * by the error function), ABCD_ACT_RELU max(g, 0). Products and act are computed
  * in fp32; h, its derivatives by the pre-activations and the gradients that
- * reach these are rounded to dtype where they are stored between products. */
+ * reach these are rounded to dtype where they are stored between products. In float32 a
+ * row of x or dy with an infinity gives NaN where the sum would be infinite. */
 enum { ABCD_ACT_SILU = 0, ABCD_ACT_GELU = 1, ABCD_ACT_RELU = 2 };
 typedef struct abcd_ffn {
   int32_t dtype, act;
@@ -480,7 +481,8 @@ ABCD_API int32_t abcd_gated_ffn_keeps(const abcd_ffn* ffn /* host */, int64_t n,
  * aligned, that receive for the backward h's derivatives by the two
  * pre-activations and h itself (columns past h: zeros). workspace: at least
  * abcd_gated_ffn_workspace_size(ffn, n, saved) bytes (saved: 1 if by_gate, by_up
- * and hidden are given, else 0), 256-byte aligned. */
+ * and hidden are given, else 0), 256-byte aligned. With and without these the sums may
+ * be taken in another order. */
 ABCD_API int32_t abcd_gated_ffn_workspace_size(const abcd_ffn* ffn /* host */, int64_t n,
                                                int32_t saved, size_t* bytes);
 ABCD_API int32_t abcd_gated_ffn(const abcd_ffn* ffn /* host */, int64_t n, const void* x,
@@ -492,7 +494,8 @@ ABCD_API int32_t abcd_gated_ffn(const abcd_ffn* ffn /* host */, int64_t n, const
  * itself) and of every weight and bias, written, of dtype, laid out as what they
  * belong to; each may be NULL, then not computed. by_gate, by_up, hidden: the
  * forward's, or all NULL: then they are computed again from x (one product more, and no
- * memory held between the passes). p, seed and offset are the forward's. */
+ * memory held between the passes). p, seed and offset are the forward's. No output may
+ * overlap an input. */
 ABCD_API int32_t abcd_gated_ffn_bwd_workspace_size(const abcd_ffn* ffn /* host */, int64_t n,
                                                    int32_t saved, size_t* bytes);
 ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, const void* dy,

@@ -280,6 +280,29 @@ def test_on_a_side_stream_and_in_a_graph(api):
         assert all(torch.equal(out[k], want[k]) for k in want), i
 
 
+@pytest.mark.parametrize("d,h,o", [(67, 40, 45), (40, 72, 48), (48, 256, 64), (128, 150, 128)])
+def test_offsets_past_32_bits(api, d, h, o):
+    """Rows so far apart that the last lie more than 2^31 elements (2^32 bytes) in."""
+    n, ld = 4400, 1 << 19
+    for dtype in (torch.bfloat16, torch.float32):
+        say("far apart", n, d, h, o, dtype)
+        wide, into = (torch.empty((n, ld), dtype=dtype, device="cuda") for _ in range(2))
+        x, y, w = wide[:, 8:8 + d], into[:, 16:16 + o], weights(4, d, h, o, dtype, True)
+        x.copy_(rand(1, n, d, dtype))
+        near = x.clone()
+        y.copy_(rand(2, n, o, dtype))
+        res = y.clone()
+        want = api.gated_ffn(near, w, residual=res, p=0.2, seed=1)["y"]
+        api.gated_ffn(x, w, residual=y, p=0.2, seed=1, out=y)
+        assert torch.equal(y, want)
+        b = api.gated_ffn_bwd(res, near, w, p=0.2, seed=1)
+        y.copy_(res)
+        g = {k: torch.empty_like(v) for k, v in w.items()}
+        dx = into[:, 256:256 + d]
+        api.gated_ffn_bwd(y, x, w, p=0.2, seed=1, grads={**g, "x": dx})
+        assert torch.equal(dx, b["x"]) and all(torch.equal(g[k], b[k]) for k in g)
+
+
 def test_refusals(api):
     n, d, h, o = 8, 16, 24, 12
     w, x = weights(4, d, h, o, torch.float32, True), rand(1, n, d, torch.float32)

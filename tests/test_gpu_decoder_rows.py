@@ -257,3 +257,21 @@ def test_refusals(api):
         with pytest.raises((ValueError, api.AbcdError)):
             call()
             print("not refused:", i)
+
+
+def test_offsets_past_32_bits(api):
+    """Rows so far apart that the last lie more than 2^31 elements (2^32 bytes) in."""
+    n, d, ld = 2300, 67, 1 << 20
+    for dtype in (torch.bfloat16, torch.float32):
+        wide, into = (torch.empty((n, ld), dtype=dtype, device="cuda") for _ in range(2))
+        x, y = wide[:, 5:5 + d], into[:, 3:3 + d]
+        x.copy_(rand(1, n, d, dtype))
+        near, dy = x.clone(), rand(2, n, d, dtype)
+        f, g = api.layer_norm(x, out=y), api.layer_norm(near)
+        assert torch.equal(y, g["y"]) and torch.equal(f["mean"], g["mean"])
+        w = rand(3, 1, d, dtype)[0].contiguous()
+        a = api.layer_norm_bwd(dy, x, g["mean"], g["rstd"], w, add=x)
+        b = api.layer_norm_bwd(dy, near, g["mean"], g["rstd"], w, add=near)
+        assert all(torch.equal(a[k], b[k]) for k in a if a[k] is not None)
+        api.dropout(x, 0.3, 1, 2, residual=x, out=y)
+        assert torch.equal(y, api.dropout(near, 0.3, 1, 2, residual=near))
