@@ -14,9 +14,14 @@ __device__ __forceinline__ float sigmoid(float g) {
 
 // a(g) and a'(g). The activation is a template argument of the kernels: with a
 // branch at every element no two elements' exponentials overlap.
-// kShort: for what is rounded to 16 bits, the error function by Abramowitz and Stegun's
-// 7.1.26, within 1.5e-7 of it: a polynomial of 1 / (1 + p |x|) times the exponential
-// that the derivative needs too.
+// The normal distribution below 0 is e^(-g^2 / 2) times a smooth function of |g|, and
+// the derivative needs the exponential anyway; the other factor is t Q(t), with t =
+// 1 / (1 + p |g|) in (0, 1]. kShort, for what is rounded to 16 bits: Abramowitz and
+// Stegun's 7.1.26, the distribution within 1e-7. Else Q of degree 9, fitted to the scaled
+// complementary error function with the least relative error, 3.3e-8 (4e-7 with the
+// roundings of fp32), so that the tail keeps its digits. The first product of 65,536 rows
+// of 96 x 256 in fp32 takes 73 us, with erff 80; a step of 1M rows of 64 x 128 x 64 in
+// bfloat16 429, with erff 527.
 template <int kAct, bool kShort>
 __device__ __forceinline__ float activate(float g, float& slope) {
   if (kAct == ABCD_ACT_SILU) {
@@ -25,18 +30,27 @@ __device__ __forceinline__ float activate(float g, float& slope) {
     return v;
   }
   if (kAct == ABCD_ACT_GELU) {
-    const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);  // e^(-g^2 / 2)
-    float c;  // the normal distribution
+    const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
+    float s;
     if (kShort) {
       const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.0f));
-      float s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+      s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
       s = fmaf(t, s, 0.5f * 1.421413741f);
       s = fmaf(t, s, 0.5f * -0.284496736f);
       s = fmaf(t, s, 0.5f * 0.254829592f) * t * e;
-      c = g < 0.0f ? s : 1.0f - s;
     } else {
-      c = 0.5f + 0.5f * erff(0.70710678118654752f * g);
+      const float t = __builtin_amdgcn_rcpf(fmaf(0.31819805f, fabsf(g), 1.0f));
+      s = fmaf(t, -0.02069551f, 0.095343746f);
+      s = fmaf(t, s, -0.15029088f);
+      s = fmaf(t, s, 0.07120013f);
+      s = fmaf(t, s, -0.011178771f);
+      s = fmaf(t, s, 0.05997515f);
+      s = fmaf(t, s, 0.08762608f);
+      s = fmaf(t, s, 0.11413582f);
+      s = fmaf(t, s, 0.12694158f);
+      s = fmaf(t, s, 0.12694266f) * t * e;
     }
+    const float c = g < 0.0f ? s : 1.0f - s;  // the normal distribution
     slope = fmaf(g * 0.39894228040143268f, e, c);
     return g * c;
   }
