@@ -143,12 +143,29 @@ struct NormBwdArgs {
   const void* w;
   const void* add;
   void* dx;
-  float* part;  // [gridDim.x][2][d]: the workgroups' sums of dy z and of dy; NULL: not wanted
+  float* part;  // [gridDim.x][2][d]: the workgroups' sums of dy z and of dy
+  void *dw, *db;  // what they add up to; NULL: not wanted
   int64_t lddy, ldx, ldadd, lddx, n;
   int d;
   int wf32;
   float inv_d;
 };
+
+// A workgroup's (of `parts`) sums of N columns: a part, or, where there is but one, the
+// result.
+template <typename T, int N, bool kWhole>
+__device__ __forceinline__ void put_sums(const NormBwdArgs& a, int which, int parts, int at, int c, Floats<N> v) {
+  if (parts > 1) {
+    store_vec<float, N, kWhole>(a.part + ((int64_t)at * 2 + which) * a.d + c, v, a.d - c);
+    return;
+  }
+  void* const out = which ? a.db : a.dw;
+  if (!out) return;
+  if (a.wf32)
+    store_vec<float, N, kWhole>(static_cast<float*>(out) + c, v, a.d - c);
+  else
+    store_vec<T, N, kWhole>(static_cast<T*>(out) + c, v, a.d - c);
+}
 
 template <typename T, int G, int R, bool kWhole>
 __global__ __launch_bounds__(kBlock) void layer_norm_bwd_kernel(NormBwdArgs a) {
@@ -230,15 +247,14 @@ __global__ __launch_bounds__(kBlock) void layer_norm_bwd_kernel(NormBwdArgs a) {
       }
     }
   }
-  if (!a.part) return;
-  float* part = a.part + (int64_t)blockIdx.x * 2 * a.d;
+  if (!a.dw && !a.db) return;
   if (G > 64) {
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       const int c = (j * G + t) * N;
       if (c >= a.d) continue;
-      store_vec<float, N, kWhole>(part + c, dw[j], a.d - c);
-      store_vec<float, N, kWhole>(part + a.d + c, db[j], a.d - c);
+      put_sums<T, N, kWhole>(a, 0, gridDim.x, blockIdx.x, c, dw[j]);
+      put_sums<T, N, kWhole>(a, 1, gridDim.x, blockIdx.x, c, db[j]);
     }
     return;
   }
@@ -259,7 +275,7 @@ __global__ __launch_bounds__(kBlock) void layer_norm_bwd_kernel(NormBwdArgs a) {
     for (int c = threadIdx.x; c < a.d; c += kBlock) {
       float e = 0.0f;
       for (int w = 0; w < kWaves; ++w) e += cols[w][c];
-      part[which * a.d + c] = e;
+      put_sums<T, 1, true>(a, which, gridDim.x, blockIdx.x, c, Floats<1>(e));
     }
     __syncthreads();
   }
@@ -314,9 +330,8 @@ __global__ __launch_bounds__(kBlock) void layer_norm_cols_kernel(NormBwdArgs a) 
     dw += v * z;
     db += v;
   }
-  float* part = a.part + (int64_t)blockIdx.y * 2 * a.d;
-  store_vec<float, N, kWhole>(part + c, dw, left);
-  store_vec<float, N, kWhole>(part + a.d + c, db, left);
+  put_sums<T, N, kWhole>(a, 0, gridDim.y, blockIdx.y, (int)c, dw);
+  put_sums<T, N, kWhole>(a, 1, gridDim.y, blockIdx.y, (int)c, db);
 }
 
 // Rows of G lanes by R vectors that a kernel is compiled for; f(G, R) with the
@@ -340,11 +355,13 @@ bool with_shape(int nvec, bool few, F f) {
 
 // Workgroups of the backward, each with its own column sums: these are 8 bytes a
 // column written and read, so there are no more of them than what a workgroup reads
-// of its rows outweighs by far, but one for every CU.
+// of its rows outweighs by far, but one for every CU. What one workgroup does in two
+// turns it does alone, and saves the second launch (16 x 224 in float16: 18.4 us with the
+// call's host time, with two workgroups and their sum 21.4).
 int64_t bwd_blocks(int64_t n, int nvec, int64_t item) {
   const int64_t rows = nvec <= 8 ? 32 : nvec <= 16 ? 16 : nvec <= 32 ? 8 : nvec <= 128 ? 4 : 1;
   const int64_t most = std::max<int64_t>(256, std::min<int64_t>(n * item / 24, nvec <= 128 ? 1024 : 512));
-  return std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, most));
+  return n <= 2 * rows ? 1 : std::min<int64_t>((n + rows - 1) / rows, most);
 }
 
 }  // namespace
@@ -390,9 +407,9 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
                               const void* weight, const void* add, int64_t ldadd, void* dx, int64_t lddx,
                               void* dweight, void* dbias, void* workspace, hipStream_t stream) {
   const bool wf32 = wdtype == ABCD_F32;
-  float* part = dweight || dbias ? static_cast<float*>(workspace) : nullptr;
-  const NormBwdArgs a{dy,   x,   mean,  rstd, weight, add,    dx, part, lddy, ldx,
-                      ldadd, lddx, n, (int)d, wf32 && dtype != ABCD_F32, 1.0f / (float)d};
+  float* part = static_cast<float*>(workspace);
+  const NormBwdArgs a{dy,  x,     mean, rstd, weight, add,  dx, part, dweight, dbias, lddy,
+                      ldx, ldadd, lddx, n, (int)d, wf32 && dtype != ABCD_F32, 1.0f / (float)d};
   int64_t blocks = 0;
   if (n > 0)
     TRY_STATUS(with_type(dtype, [&](auto zero) -> int32_t {
@@ -415,7 +432,7 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
           else
             ABCD_LAUNCH("layer_norm_bwd", (layer_norm_bwd_wide_kernel<T, false>), rows, kBlock, 0, stream, a);
         }
-        if (part) {
+        if (dweight || dbias) {
           const dim3 grid((nvec + kBlock - 1) / kBlock, blocks);
           if (whole)
             ABCD_LAUNCH("layer_norm_cols", (layer_norm_cols_kernel<T, true>), grid, kBlock, 0, stream, a);
@@ -426,7 +443,7 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
       ABCD_HIP(hipGetLastError());
       return ABCD_OK;
     }));
-  if (dweight || dbias) {
+  if ((dweight || dbias) && blocks != 1) {
     const int32_t to = wf32 ? ABCD_F32 : dtype;
     SumOuts outs{};
     outs.add(dweight, d);
