@@ -473,7 +473,7 @@ typedef struct abcd_ffn {
 
 /* *keeps = 1 if a training step does best to let the forward keep by_gate, by_up and
  * hidden for the backward, 0 if the backward makes them again faster than it would
- * read them (narrow blocks of many rows). Either way both are correct. */
+ * read them (narrow blocks). Either way both are correct. */
 ABCD_API int32_t abcd_gated_ffn_keeps(const abcd_ffn* ffn /* host */, int64_t n, int32_t* keeps);
 
 /* Forward. residual (may be NULL) and y: [n][o], y may be residual itself. by_gate,

@@ -561,7 +561,7 @@ def gated_ffn(x, params, act="silu", residual=None, p=0.0, seed=0, offset=0, sav
 
     Returns dict(y [n, o], saved): with save=True what gated_ffn_bwd takes of
     this pass, else None; None too where the backward makes it again faster than
-    it would read it (narrow blocks of many rows). out may be residual."""
+    it would read it (narrow blocks). out may be residual."""
     f, ldx = _ffn(x, params, act, p, seed, offset)
     n, dev = x.shape[0], x.device
     ldr = 0 if residual is None else _rows(residual, "residual", x, (n, f.o))

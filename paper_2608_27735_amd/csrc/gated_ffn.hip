@@ -139,16 +139,25 @@ struct Scratch {
 size_t dweight_part(int64_t n) { return n < 1024 ? 0 : (size_t)kBigSlots * 256 * 256; }
 static_assert((size_t)kBigSlots * 256 * 256 >= (size_t)kSmallSlots * 128 * 128, "the large tiles' parts are the larger");
 
-// Whether the narrow kernels take the block, both ways or the forward alone: what they
-// hold in registers and LDS, in 16-bit types, and rows enough to share the cost of
-// setting the weights up.
+// Whether the kernels for a few rows take the first products. They read x again for
+// every 16 columns of h, so that many rows of a wide block leave it to the tiles: bf16,
+// 64 x 512 x 1,376 x 512 18 against 25 us, 64 x 1,024 x 2,816 x 1,024 25 either way, 64 x
+// 2,048 x 5,632 x 2,048 55 against 35; fp32, 32 rows of the second 33 against 37, 48 rows
+// 44 against 39.
+bool few(const abcd_ffn& f, int64_t n) {
+  return n <= 16 || (n <= 64 && (n + 15) / 16 * (2 * f.h * f.d + f.o * f.h) * (int64_t)type_bytes(f.dtype) <= 80 << 20);
+}
+// Whether the narrow kernels do, in 16-bit types, of what they hold in registers and LDS.
+// Both ways they win from the first row on, with fewer launches (64 x 128 x 64, forward
+// and backward: one row 49 against 68 us, 100 rows 48 against 73, 16,000 42 against 60; of 384 hidden units,
+// 8,000 rows lose, 94 against 80, and 32,000 win, 103 against 120). The forwards of the
+// larger shapes have their setting up to make good: 128 x 192 x 128, 32,000 rows 22
+// against 20 us, 64,000 25 against 32.
 bool narrow_forward(const abcd_ffn& f, int64_t n) {
   const int shape = f.dtype == ABCD_F32 ? 0 : narrow_shape(f.d, f.h, f.o);
-  return shape == 1 ? n >= 1024 : shape > 1 && n >= 4096;
+  return shape > 0 && (shape <= 2 || n >= 40000);
 }
 bool narrow(const abcd_ffn& f, int64_t n) { return narrow_forward(f, n) && narrow_shape(f.d, f.h, f.o) <= 2; }
-// Whether the kernels for a few rows take the forward.
-bool few(int64_t n) { return n <= 64; }
 int64_t narrow_blocks(const abcd_ffn& f, int64_t n) {
   return std::min<int64_t>((n + 255) / 256, (narrow_shape(f.d, f.h, f.o) == 1 ? 2 : 1) * kCUs);
 }
@@ -168,7 +177,7 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
     s.bytes = p.used;
     return s;
   }
-  if (!backward && few(n)) {
+  if (!backward && few(f, n)) {
     if (!saved) s.hidden = p.take(n * hp * sz);
     s.bytes = p.used;
     return s;
@@ -246,7 +255,7 @@ int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ld
   const int64_t hp = up8(f.h);
   FfnOut out{Side{{hidden, nullptr}, hp, n}, Side{{f.w_down, nullptr}, f.h, f.o}, f.b_down, residual, y, f.h, f.o, ldr,
              ldy, drop_key(f.p, f.seed, f.offset), Tiling{s.part, 0, 0, 1, 0}};
-  if (few(n)) {
+  if (few(f, n)) {
     TRY_STATUS(few_in(f, n, x, ldx, by_gate, by_up, hidden, stream));
     return FFN_BY_TYPE(f, ffn_few_out, out, stream);
   }
@@ -302,7 +311,7 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
       dz = side_of(copies, f, dy, n, f.o, lddy, s.dz);
     }
     TRY_STATUS(launch(copies, f.dtype, stream));
-    if (!hidden && few(n)) {
+    if (!hidden && few(f, n)) {
       TRY_STATUS(few_in(f, n, x, ldx, s.gate, s.up, s.hidden, stream));
       by_gate = s.gate;
       by_up = s.up;

@@ -21,6 +21,13 @@
 // from LDS along for g, u and dh, and across (ds_read_b64_tr_b16) for the weights'
 // gradients. The biases' gradients are products with ones. Workgroups write their
 // sums in fp32, and a second launch adds these in a fixed order.
+//
+// 1M rows of 64 x 128 x 64 in bf16, dropout and biases: forward 106 us (256 MB), backward
+// 220 (384 MB). Neither memory nor the matrix instructions (a quarter and 40 percent
+// busy) bound them but issue: the forward's vector instructions (activation, generator,
+// conversions) at four waves a SIMD, the backward's chain of LDS, products, activation
+// and products at the two waves that its registers leave room for. By the tiled products
+// the step takes 2,100 us: g, u, h and their gradients through memory.
 #pragma once
 
 #include <algorithm>
@@ -464,7 +471,9 @@ __global__ __launch_bounds__(kNarrowBwdThreads, 2) void ffn_narrow_bwd_kernel(Ff
 }
 
 // The smallest of the compiled shapes that holds the block (narrow_shape), with two
-// workgroups a CU or, from 72 KB of weights on, one.
+// workgroups a CU or, from 72 KB of weights on, one. By the tiled products the larger
+// shapes take two to four times as long: 1M rows of 64 x 384 x 64 724 against 200 us,
+// 300,000 of 128 x 192 x 128 183 against 78 (20,000 rows: 20 against 22).
 template <typename T>
 int32_t run_narrow(const FfnNarrow& a, int64_t blocks, hipStream_t stream) {
   return with_act(a.act, [&](auto act) -> int32_t {

@@ -27,7 +27,13 @@
 //   bit, on the same matrix instructions with fp32 sums: 96 cycles of a SIMD for what
 //   v_mfma_f32_16x16x4_f32 takes 256 for, at a relative error of a product of 2^-24.
 //   The parts are made on the way from memory to LDS, through registers. An infinity
-//   among the operands gives NaN.
+//   among the operands gives NaN. (137 x 1,696 x 3,208 x 63, forward and backward: 151 us,
+//   with the fp32 instruction, and no split contractions, 615.)
+//
+// What the matrix instructions' rate bounds runs at 1.15 to 1.3 PFLOP/s in bf16, a large
+// library product at 1.35: two 256 x 256 tiles of 64 contraction indexes fill the LDS of
+// a CU, which so holds one workgroup of 8 waves, and nothing overlaps its first loads and
+// its last stores.
 #pragma once
 
 #include "gated_ffn_args.h"

@@ -9,8 +9,9 @@ namespace {
 constexpr int kPartWaves = 16;
 
 // Column c of the parts belongs to the output whose range holds it; out[i] = sum
-// over p of part[p][c]: 64 columns per workgroup, the parts dealt to its 16 waves,
-// whose sums LDS joins.
+// over p of part[p][c]: 64 columns per workgroup, the parts dealt to its 16 waves with
+// eight loads in flight each, whose sums LDS joins. 256 parts of 24,896 columns (25 MB):
+// 6 us; a launch of little work 4.5.
 template <typename T>
 __global__ __launch_bounds__(kPartWaves* kWave) void sum_parts_kernel(const float* part, int64_t parts,
                                                                      SumOuts outs) {

@@ -139,7 +139,8 @@ def test_few_tiles_and_long_sums(api, dtype, n, d, h, o):
 @pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
 @pytest.mark.parametrize("n,d,h,o", [
     (4096, 64, 384, 64), (4111, 1, 129, 1), (5000, 59, 200, 33), (4097, 65, 192, 64), (6001, 127, 1, 3),
-    (5003, 96, 176, 18), (4500, 128, 192, 128), (4100, 64, 100, 65), (4129, 101, 190, 127), (70001, 72, 130, 70)])
+    (5003, 96, 176, 18), (4500, 128, 192, 128), (4100, 64, 100, 65), (4129, 101, 190, 127), (70001, 72, 130, 70),
+    (40003, 96, 176, 18), (40000, 128, 192, 128), (50001, 101, 190, 127), (40961, 65, 192, 64)])
 def test_narrow_forward(api, dtype, n, d, h, o):
     """Blocks whose forward alone is one launch."""
     for act, bias, p, pad, skip in [("silu", True, 0.1, 0, 0), ("gelu", False, 0.0, 5, 1), ("relu", True, 1.0, 8, 8)]:
@@ -151,6 +152,12 @@ def test_narrow_forward(api, dtype, n, d, h, o):
         api.gated_ffn(x, w, act, residual=res, p=p, seed=5, offset=9, out=wide[:, 4:4 + o])
         check("y", wide[:, 4:4 + o], ref["y"])
         assert (wide[:, :4] == 7).all() and (wide[:, 4 + o:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+def test_few_rows_of_wide_blocks(api, dtype):
+    run(api, 40, 1500, 6000, 900, dtype, "silu", True, 0.1)
+    run(api, 7, 1500, 6000, 900, dtype, "gelu", False, 0.0, pad=3, skip=1)
 
 
 def test_gelu_far_out(api):
