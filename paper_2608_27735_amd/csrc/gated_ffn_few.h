@@ -1,12 +1,12 @@
 // gated_ffn_few.h -- the gated feed-forward block of a few rows (single tokens and
 // small batches), forward.
 //
-// The weights are read once and bound it. A workgroup takes 16 columns of the
+// The weights are read once and bound it. A workgroup takes 16 or 8 columns of the
 // result and all rows; its waves divide the contraction, each with many loads of
 // 16 bytes in flight straight into the matrix instructions' operands, and LDS joins
 // their sums. No operand needs an alignment beyond its elements'. One row of 2,048 x
-// 5,632 x 2,048 in bf16: 13 us for the projections (46 MB, 3.5 TB/s) and 10 for the way
-// down (23 MB), 21.6 together where launches overlap; the tiled products take 75.
+// 5,632 x 2,048 in bf16: 13 us for the projections (46 MB, 3.5 TB/s) and 8.7 for the way
+// down (23 MB, 2.6 TB/s); the tiled products take 75 together.
 #pragma once
 
 #include "activation.h"
@@ -116,16 +116,20 @@ __global__ __launch_bounds__(kFewInWaves * 64) void ffn_few_in_kernel(FfnIn a) {
   }
 }
 
+// 8 columns a workgroup, the other half of the matrix instructions empty, where that
+// still is no more than one for a CU: 5,632 x 2,048 in bf16 11.0 us instead of 12.4 (with
+// 4 columns 14.5), 2,816 x 1,024 7.4 instead of 8.2.
 template <typename T, int kX, bool kWhole>
 __global__ __launch_bounds__(kFewOutWaves * 64) void ffn_few_out_kernel(FfnOut a) {
   f32x4 acc[kX][1], sum[1];
-  const int first = blockIdx.x * 16, n = (int)a.hidden.len;
+  const int columns = (int64_t)gridDim.x * 8 >= a.o ? 8 : 16;
+  const int first = blockIdx.x * columns, end = min((int)a.o, first + columns), n = (int)a.hidden.len;
   const T* const w[1] = {static_cast<const T*>(a.w.p[0])};
   few_products<T, kX, 1, kFewOutWaves, kWhole>(acc, static_cast<const T*>(a.hidden.p[0]), a.hidden.ld, n, w, a.w.ld,
-                                               first, (int)a.o, (int)a.h);
+                                               first, end, (int)a.h);
   if (!few_join<kX, 1, kFewOutWaves>(acc, sum)) return;
   const int l = threadIdx.x & 63, r = (threadIdx.x >> 6) * 16 + (l & 15), c = first + (l >> 4) * 4;
-  const int left = (int)a.o - c;
+  const int left = end - c;
   if (r >= n || left <= 0) return;
   if (a.bias) sum[0] += load_vec<T, 4, false>(static_cast<const T*>(a.bias) + c, left);
   f32x4 y = 0.0f;
@@ -161,7 +165,7 @@ template <typename T>
 int32_t run_few_out(const FfnOut& a, hipStream_t stream) {
   return with_rows(a.hidden.len, [&](auto rows) -> int32_t {
     constexpr int kX = decltype(rows)::value;
-    const int64_t grid = (a.o + 15) / 16;
+    const int64_t grid = (a.o + 7) / 8 <= kCUs ? (a.o + 7) / 8 : (a.o + 15) / 16;
     if (a.h % kPer16<T> == 0)
       ABCD_LAUNCH("ffn_few_out", (ffn_few_out_kernel<T, kX, true>), grid, kFewOutWaves * 64, 0, stream, a);
     else

@@ -158,6 +158,8 @@ def test_narrow_forward(api, dtype, n, d, h, o):
 def test_few_rows_of_wide_blocks(api, dtype):
     run(api, 40, 1500, 6000, 900, dtype, "silu", True, 0.1)
     run(api, 7, 1500, 6000, 900, dtype, "gelu", False, 0.0, pad=3, skip=1)
+    run(api, 16, 300, 700, 2047, dtype, "silu", True, 0.1)
+    run(api, 3, 300, 701, 2050, dtype, "silu", True, 0.1, pad=3, skip=1)
 
 
 def test_gelu_far_out(api):
