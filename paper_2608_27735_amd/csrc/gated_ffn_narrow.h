@@ -23,10 +23,11 @@
 // sums in fp32, and a second launch adds these in a fixed order.
 //
 // 1M rows of 64 x 128 x 64 in bf16, dropout and biases: forward 106 us (256 MB), backward
-// 220 (384 MB). Neither memory nor the matrix instructions (a quarter and 40 percent
-// busy) bound them but issue: the forward's vector instructions (activation, generator,
-// conversions) at four waves a SIMD, the backward's chain of LDS, products, activation
-// and products at the two waves that its registers leave room for. By the tiled products
+// 220 (384 MB). Neither memory nor the matrix instructions (20 and 29 percent busy) bound
+// them but issue: the forward's vector instructions (activation, generator, conversions;
+// 63 percent busy) at four waves a SIMD, the backward's chain of LDS, products,
+// activation and products at the two waves that its registers leave room for (vector
+// instructions 46 percent busy, LDS about as much). By the tiled products
 // the step takes 2,100 us: g, u, h and their gradients through memory.
 #pragma once
 
@@ -57,8 +58,9 @@ __device__ __forceinline__ T at_or_0(const void* m, int row, int col, int rows, 
 
 constexpr int kNarrowThreads = 512, kNarrowBwdThreads = 512;
 
-// kWhole: d, h and o are multiples of 8. kDF: contractions of 32 that hold d; kOB: 16-column blocks of o; kHC: 32-column
-// chunks of h
+// kWhole: d, h and o are multiples of 8. kDF: contractions of 32 that hold d; kOB:
+// 16-column blocks of o; kHC: 32-column chunks of h. Registers for the waves whose
+// workgroups' weights fit a CU's LDS: two of the smallest shape, one of the others.
 template <typename T, int kAct, int kDF, int kOB, int kHC, bool kWhole>
 __global__ __launch_bounds__(kNarrowThreads, (kHC * (4 * kDF + kOB) <= 72 ? 4 : 2)) void ffn_narrow_kernel(FfnNarrow a) {
   typedef typename Frag<T>::type F;
