@@ -236,8 +236,9 @@ int32_t few_in(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx, void* b
 
 bool gated_ffn_keeps(const abcd_ffn& f, int64_t n) { return !narrow(f, n); }
 
+// Never 0, also of a call that needs none: which those are is not the caller's to know.
 size_t gated_ffn_workspace_bytes(const abcd_ffn& f, int64_t n, bool saved, bool backward) {
-  return layout(f, n, saved, backward, nullptr).bytes;
+  return std::max<size_t>(256, layout(f, n, saved, backward, nullptr).bytes);
 }
 
 int32_t launch_gated_ffn(const abcd_ffn& f, int64_t n, const void* x, int64_t ldx, const void* residual,
