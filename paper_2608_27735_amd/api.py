@@ -383,6 +383,11 @@ def _param_dtype(x, weight, bias):
     return wt
 
 
+def _new(x, size):
+    """An array of x's type beside x (empty_like is half of what torch.empty takes)."""
+    return torch.empty_like(x) if x.shape == size and x.is_contiguous() else x.new_empty(size)
+
+
 def _workspace(workspace, need, device):
     if workspace is None:
         return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
@@ -405,16 +410,15 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, mean=None, rstd=No
     _vector(weight, "weight", d, wt, dev)
     _vector(bias, "bias", d, wt, dev)
     if out is None:
-        out, ldy = torch.empty(size, dtype=x.dtype, device=dev), d
+        out, ldy = _new(x, size), d
     else:
         ldy = _rows(out, "out", x, size)
-    if mean is None and rstd is None:
-        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=dev).unbind(0)
-    else:
-        mean = torch.empty(n, dtype=torch.float32, device=dev) if mean is None else mean
-        rstd = torch.empty(n, dtype=torch.float32, device=dev) if rstd is None else rstd
-        _vector(mean, "mean", n, torch.float32, dev)
-        _vector(rstd, "rstd", n, torch.float32, dev)
+    _vector(mean, "mean", n, torch.float32, dev)
+    _vector(rstd, "rstd", n, torch.float32, dev)
+    if mean is None:
+        mean = torch.empty(n, dtype=torch.float32, device=dev)
+    if rstd is None:
+        rstd = torch.empty(n, dtype=torch.float32, device=dev)
     check(_lib.load().abcd_layer_norm(code, n, d, x.data_ptr(), ldx, _DTYPES[wt], _ptr(weight),
                                       _ptr(bias), eps, out.data_ptr(), ldy,
                                       mean.data_ptr(), rstd.data_ptr(), _stream()))
@@ -447,8 +451,11 @@ def layer_norm_bwd(dy, x, mean, rstd, weight=None, add=None, wdtype=None, worksp
         raise ValueError(f"wdtype must be {x.dtype} or float32, got {wdtype}")
     _vector(weight, "weight", d, wdtype, dev)
     if grads is None:
-        dx, lddx = torch.empty(size, dtype=x.dtype, device=dev), d
-        dw, db = torch.empty((2, d), dtype=wdtype, device=dev).unbind(0)
+        dx, lddx = _new(x, size), d
+        if weight is not None:
+            dw, db = torch.empty_like(weight), torch.empty_like(weight)
+        else:
+            dw, db = torch.empty((2, d), dtype=wdtype, device=dev).unbind(0)
         grads = dict(x=dx, weight=dw, bias=db)
     else:
         dx, dw, db = grads.get("x"), grads.get("weight"), grads.get("bias")
@@ -485,7 +492,7 @@ def dropout(x, p, seed, offset=0, residual=None, out=None):
     p, seed, offset = _drop_args(p, seed, offset)
     ldr = 0 if residual is None else _rows(residual, "residual", x, size)
     if out is None:
-        out, ldy = torch.empty(size, dtype=x.dtype, device=x.device), size[1]
+        out, ldy = _new(x, size), size[1]
     else:
         ldy = _rows(out, "out", x, size)
     check(_lib.load().abcd_dropout(code, size[0], size[1], x.data_ptr(), ldx, _ptr(residual), ldr,
@@ -566,7 +573,7 @@ def gated_ffn(x, params, act="silu", residual=None, p=0.0, seed=0, offset=0, sav
     n, dev = x.shape[0], x.device
     ldr = 0 if residual is None else _rows(residual, "residual", x, (n, f.o))
     if out is None:
-        out, ldy = torch.empty((n, f.o), dtype=x.dtype, device=dev), f.o
+        out, ldy = _new(x, (n, f.o)), f.o
     else:
         ldy = _rows(out, "out", x, (n, f.o))
     lib = _lib.load()
@@ -577,7 +584,8 @@ def gated_ffn(x, params, act="silu", residual=None, p=0.0, seed=0, offset=0, sav
         save = keeps.value != 0
     if save:
         hp = (f.h + 7) // 8 * 8
-        saved = {k: torch.empty((n, hp), dtype=x.dtype, device=dev) for k in FFN_SAVED}
+        kept = _new(x, (n, hp))
+        saved = dict(zip(FFN_SAVED, (kept, torch.empty_like(kept), torch.empty_like(kept))))
     sz = C.c_size_t(0)
     check(lib.abcd_gated_ffn_workspace_size(C.byref(f), n, 1 if save else 0, C.byref(sz)))
     workspace = _workspace(workspace, sz.value, dev)
@@ -600,7 +608,7 @@ def gated_ffn_bwd(dy, x, params, act="silu", saved=None, p=0.0, seed=0, offset=0
     if grads is None:
         grads = {k: torch.empty_like(params[k]) for k in FFN_WEIGHTS + FFN_BIASES
                  if params.get(k) is not None}
-        grads["x"] = torch.empty((n, d), dtype=x.dtype, device=dev)
+        grads["x"] = _new(x, (n, d))
     for k, shape in (("w_gate", (f.h, d)), ("w_up", (f.h, d)), ("w_down", (f.o, f.h)),
                      ("b_gate", (f.h,)), ("b_up", (f.h,)), ("b_down", (f.o,))):
         t = grads.get(k)
