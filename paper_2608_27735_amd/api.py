@@ -510,6 +510,7 @@ _ACTS = {"silu": 0, "gelu": 1, "relu": 2}  # ABCD_ACT_*
 FFN_WEIGHTS = ("w_gate", "w_up", "w_down")
 FFN_BIASES = ("b_gate", "b_up", "b_down")
 FFN_SAVED = ("by_gate", "by_up", "hidden")
+_FFN_PARAMS = frozenset(FFN_WEIGHTS + FFN_BIASES)
 
 
 def _ffn(x, params, act, p, seed, offset):
@@ -519,28 +520,30 @@ def _ffn(x, params, act, p, seed, offset):
     d, dtype, dev = x.shape[1], x.dtype, x.device
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)}, got {act!r}")
+    if not params.keys() <= _FFN_PARAMS:
+        raise ValueError(f"unknown parameters {sorted(params.keys() - _FFN_PARAMS)}")
+    get = params.get
     for k in FFN_WEIGHTS:
-        if params.get(k) is None:
-            raise ValueError(f"{k} is required")
-        if params[k].dim() != 2 or params[k].shape[0] == 0:
-            raise ValueError(f"{k} must be a matrix with rows, got {tuple(params[k].shape)}")
-    h, o = params["w_gate"].shape[0], params["w_down"].shape[0]
-    shapes = dict(w_gate=(h, d), w_up=(h, d), w_down=(o, h), b_gate=(h,), b_up=(h,), b_down=(o,))
-    ptrs = dict.fromkeys(shapes)
-    for k, t in params.items():
-        if k not in shapes:
-            raise ValueError(f"unknown parameter {k!r}")
+        t = get(k)
         if t is None:
+            raise ValueError(f"{k} is required")
+        if t.dim() != 2 or t.shape[0] == 0:
+            raise ValueError(f"{k} must be a matrix with rows, got {tuple(t.shape)}")
+    h, o = params["w_gate"].shape[0], params["w_down"].shape[0]
+    ptrs = []
+    for k, shape in (("w_gate", (h, d)), ("w_up", (h, d)), ("w_down", (o, h)),
+                     ("b_gate", (h,)), ("b_up", (h,)), ("b_down", (o,))):
+        t = get(k)
+        if t is None:
+            ptrs.append(None)
             continue
         if t.dtype != dtype or t.device != dev:
             raise ValueError(f"{k} must be {dtype} on {dev}, got {t.dtype} on {t.device}")
-        if t.shape != shapes[k] or not t.is_contiguous():
-            raise ValueError(f"{k} must be contiguous with shape {shapes[k]}, "
-                             f"got {tuple(t.shape)}")
-        ptrs[k] = t.data_ptr()
+        if t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{k} must be contiguous with shape {shape}, got {tuple(t.shape)}")
+        ptrs.append(t.data_ptr())
     p, seed, offset = _drop_args(p, seed, offset)
-    return _lib.abcd_ffn(code, _ACTS[act], d, h, o, ptrs["w_gate"], ptrs["w_up"], ptrs["w_down"],
-                         ptrs["b_gate"], ptrs["b_up"], ptrs["b_down"], p, seed, offset), ldx
+    return _lib.abcd_ffn(code, _ACTS[act], d, h, o, *ptrs, p, seed, offset), ldx
 
 
 def _saved_ptrs(saved, n, h, like):
@@ -605,18 +608,20 @@ def gated_ffn_bwd(dy, x, params, act="silu", saved=None, p=0.0, seed=0, offset=0
     n, d = x.shape
     dev = x.device
     lddy = _rows(dy, "dy", x, (n, f.o))
-    if grads is None:
+    if grads is None:  # laid out as the parameters, which _ffn has checked
         grads = {k: torch.empty_like(params[k]) for k in FFN_WEIGHTS + FFN_BIASES
                  if params.get(k) is not None}
-        grads["x"] = _new(x, (n, d))
-    for k, shape in (("w_gate", (f.h, d)), ("w_up", (f.h, d)), ("w_down", (f.o, f.h)),
-                     ("b_gate", (f.h,)), ("b_up", (f.h,)), ("b_down", (f.o,))):
-        t = grads.get(k)
-        if t is not None and (t.dtype != x.dtype or t.device != dev or tuple(t.shape) != shape
-                              or not t.is_contiguous()):
-            raise ValueError(f"grads[{k}] must be contiguous {x.dtype} on {dev} with shape {shape}")
-    dx = grads.get("x")
-    lddx = 0 if dx is None else _rows(dx, "grads[x]", x, (n, d))
+        dx, lddx = _new(x, (n, d)), d
+        grads["x"] = dx
+    else:
+        for k, shape in (("w_gate", (f.h, d)), ("w_up", (f.h, d)), ("w_down", (f.o, f.h)),
+                         ("b_gate", (f.h,)), ("b_up", (f.h,)), ("b_down", (f.o,))):
+            t = grads.get(k)
+            if t is not None and (t.dtype != x.dtype or t.device != dev or t.shape != shape
+                                  or not t.is_contiguous()):
+                raise ValueError(f"grads[{k}] must be contiguous {x.dtype} on {dev} with shape {shape}")
+        dx = grads.get("x")
+        lddx = 0 if dx is None else _rows(dx, "grads[x]", x, (n, d))
     lib = _lib.load()
     sz = C.c_size_t(0)
     check(lib.abcd_gated_ffn_bwd_workspace_size(C.byref(f), n, 0 if saved is None else 1,
