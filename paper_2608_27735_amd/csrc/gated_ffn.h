@@ -379,7 +379,7 @@ int32_t run_product(const char* label, End e, hipStream_t stream) {
   }
   const int64_t grid = deal(Small{});
   REQUIRE(grid < (int64_t(1) << 31), "too many tiles");
-  t.splits = product_splits(e.rows(), e.cols(), kHalf, steps);
+  t.splits = product_splits(sizeof(T), e.rows(), e.cols(), kHalf, steps);
   if (t.splits == 1) {
     ABCD_LAUNCH(label, (ffn_product_kernel<T, Small, End, false>), grid, Small::WX* Small::WW * 64, 0, stream, e);
     ABCD_HIP(hipGetLastError());
@@ -425,9 +425,9 @@ int32_t run_dweight_tiles(FfnDWeight a, int slots, hipStream_t stream) {
   }
   a.tiles = (int)total;
   // As many tiles whole as make full rounds of the GPU; the rows of the others are
-  // split so that they make one more, but for at least 512 rows a part.
+  // split so that they make one more.
   const int left = a.tiles % slots;
-  a.splits = left == 0 ? 1 : (int)std::min<int64_t>(slots / left, std::max<int64_t>(1, a.n / 512));
+  a.splits = left == 0 ? 1 : (int)std::min<int64_t>(slots / left, dweight_splits(steps_of<T>(a.n)));
   a.whole = a.splits > 1 ? a.tiles - left : a.tiles;
   a.steps = (steps_of<T>(a.n) + a.splits - 1) / a.splits;
   const int rest = a.tiles - a.whole;

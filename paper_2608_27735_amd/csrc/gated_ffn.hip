@@ -134,10 +134,17 @@ struct Scratch {
   size_t bytes;
 };
 
-// Room for the parts of the weights' gradients: no more than run at once, and none
-// where the rows are too few to split.
-size_t dweight_part(int64_t n) { return n < 1024 ? 0 : (size_t)kBigSlots * 256 * 256; }
-static_assert((size_t)kBigSlots * 256 * 256 >= (size_t)kSmallSlots * 128 * 128, "the large tiles' parts are the larger");
+// Room for the parts of the weights' gradients, none where the rows are too few to
+// split: no more of them than run at once, and of a few tiles no more than their splits.
+size_t dweight_part(const abcd_ffn& f, int64_t steps) {
+  const int64_t splits = dweight_splits(steps);
+  if (splits == 1) return 0;
+  auto room = [&](int64_t tile, int64_t slots) {
+    auto of = [&](int64_t rows, int64_t cols) { return (rows + tile - 1) / tile * ((cols + tile - 1) / tile); };
+    return (size_t)std::min(slots, (2 * of(f.h, f.d) + of(f.o, f.h)) * splits) * tile * tile;
+  };
+  return std::max(room(256, kBigSlots), room(128, kSmallSlots));
+}
 
 // Whether the kernels for a few rows take the first products. They read x again for
 // every 16 columns of h, so that many rows of a wide block leave it to the tiles: bf16,
@@ -190,14 +197,14 @@ Scratch layout(const abcd_ffn& f, int64_t n, bool saved, bool backward, void* wo
   const int64_t step = kStepBytes / (int64_t)sz;
   auto steps = [&](int64_t kn) { return (kn + step - 1) / step; };
   size_t part = 0;
-  if (!backward || !saved) part = product_part(n, f.h, 2, steps(f.d));
-  if (!backward) part = std::max(part, product_part(n, f.o, 1, steps(f.h)));
+  if (!backward || !saved) part = product_part(sz, n, f.h, 2, steps(f.d));
+  if (!backward) part = std::max(part, product_part(sz, n, f.o, 1, steps(f.h)));
   if (backward) {
     s.dz = p.take(n * op * sz);
     s.gate = p.take(n * hp * sz);
     s.up = p.take(n * hp * sz);
-    part = std::max({part, product_part(n, f.h, 1, steps(f.o)), product_part(n, f.d, 1, 2 * steps(f.h)),
-                     (size_t)sum_parts_of(n) * (2 * f.h + f.o), dweight_part(n)});
+    part = std::max({part, product_part(sz, n, f.h, 1, steps(f.o)), product_part(sz, n, f.d, 1, 2 * steps(f.h)),
+                     (size_t)sum_parts_of(n) * (2 * f.h + f.o), dweight_part(f, steps(n))});
   }
   s.part = static_cast<float*>(p.take(part * sizeof(float)));
   s.bytes = p.used;

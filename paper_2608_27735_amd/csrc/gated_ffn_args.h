@@ -84,21 +84,29 @@ constexpr int kCUs = 256, kBigSlots = kCUs, kSmallSlots = 2 * kCUs;
 
 // Floats of the parts that a product of rows x cols (of `halves` of them) over
 // `steps` steps writes, 0 if its contraction is not split: it is where its tiles of
-// 128 x 128 leave half of the workgroups that fit idle, into at least four steps each.
+// 128 x 128 leave half of the workgroups that fit idle, into at least four steps each,
+// and from 8 steps on in fp32, which take 1.9 us each, and 12 in 16-bit types, whose 1 us
+// pays for the second launch later (forward and backward, bf16, 1,000 x 512 x 2,816 x 512:
+// 99 us, from 8 on 109; fp32, 3,000 x 64 x 128 x 64: 76, from 12 on 80).
 inline int64_t product_tiles(int64_t rows, int64_t cols, int halves) {
   return (rows + 127) / 128 * ((halves * cols + 127) / 128);
 }
-inline int product_splits(int64_t rows, int64_t cols, int halves, int64_t steps) {
+inline int product_splits(size_t item, int64_t rows, int64_t cols, int halves, int64_t steps) {
   const int64_t tiles = product_tiles(rows, cols, halves);
-  if (tiles == 0 || 2 * tiles > kSmallSlots || steps < 8) return 1;
+  if (tiles == 0 || 2 * tiles > kSmallSlots || steps < (item == 2 ? 12 : 8)) return 1;
   int64_t s = kSmallSlots / tiles;
   s = s < steps / 4 ? s : steps / 4;
   return (int)(s < 32 ? s : 32);
 }
-inline size_t product_part(int64_t rows, int64_t cols, int halves, int64_t steps) {
-  const int s = product_splits(rows, cols, halves, steps);
+inline size_t product_part(size_t item, int64_t rows, int64_t cols, int halves, int64_t steps) {
+  const int s = product_splits(item, rows, cols, halves, steps);
   return s == 1 ? 0 : (size_t)s * halves * rows * ((cols + 7) & ~int64_t(7));
 }
+
+// Into how many parts the rows of a tile of the weights' gradients may be split: of four
+// steps each, and from 16 on, as adding them up is a launch (fp32, 3,000 x 64 x 128 x 64:
+// 15 and 7 us, of 512 rows each 37 and 6).
+inline int64_t dweight_splits(int64_t steps) { return steps < 16 ? 1 : steps / 4; }
 
 // The narrow block. Which of the forward's compiled shapes holds it, 0 if none: with
 // its weights in 48, 144, 120 or 144 KB of LDS.
