@@ -426,19 +426,20 @@ int32_t launch_layer_norm_bwd(int32_t dtype, int64_t n, int64_t d, const void* d
           ABCD_LAUNCH("layer_norm_bwd", (layer_norm_bwd_kernel<T, G, R, false>), blocks, kBlock, 0, stream, a);
       });
       if (!held) {
-        if (dx) {
-          const int64_t rows = std::min<int64_t>(n, 2048);
-          if (whole)
-            ABCD_LAUNCH("layer_norm_bwd", (layer_norm_bwd_wide_kernel<T, true>), rows, kBlock, 0, stream, a);
-          else
-            ABCD_LAUNCH("layer_norm_bwd", (layer_norm_bwd_wide_kernel<T, false>), rows, kBlock, 0, stream, a);
-        }
+        // the column sums first: dx may be dy
         if (dweight || dbias) {
           const dim3 grid((nvec + kBlock - 1) / kBlock, blocks);
           if (whole)
             ABCD_LAUNCH("layer_norm_cols", (layer_norm_cols_kernel<T, true>), grid, kBlock, 0, stream, a);
           else
             ABCD_LAUNCH("layer_norm_cols", (layer_norm_cols_kernel<T, false>), grid, kBlock, 0, stream, a);
+        }
+        if (dx) {
+          const int64_t rows = std::min<int64_t>(n, 2048);
+          if (whole)
+            ABCD_LAUNCH("layer_norm_bwd", (layer_norm_bwd_wide_kernel<T, true>), rows, kBlock, 0, stream, a);
+          else
+            ABCD_LAUNCH("layer_norm_bwd", (layer_norm_bwd_wide_kernel<T, false>), rows, kBlock, 0, stream, a);
         }
       }
       ABCD_HIP(hipGetLastError());

@@ -275,3 +275,20 @@ def test_offsets_past_32_bits(api):
         assert all(torch.equal(a[k], b[k]) for k in a if a[k] is not None)
         api.dropout(x, 0.3, 1, 2, residual=x, out=y)
         assert torch.equal(y, api.dropout(near, 0.3, 1, 2, residual=near))
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,d", [(1, 8200), (3, 20001), (40, 8200), (5, 4100), (50, 300), (9, 1500)])
+def test_layer_norm_gradients_in_place(api, dtype, n, d):
+    """dx written over dy, or over what is added to it, with every gradient wanted."""
+    say("in place", dtype, n, d)
+    x, dy, add = (rand(i, n, d, dtype) for i in (1, 2, 4))
+    w = rand(3, 1, d, dtype)[0]
+    f = api.layer_norm(x, w)
+    for aa in (None, add):
+        want = api.layer_norm_bwd(dy, x, f["mean"], f["rstd"], w, add=aa)
+        for into in ("dy", "add")[:1 if aa is None else 2]:
+            over = dict(dy=dy.clone(), add=None if aa is None else aa.clone())
+            grads = dict(x=over[into], weight=torch.empty_like(w), bias=torch.empty_like(w))
+            api.layer_norm_bwd(over["dy"], x, f["mean"], f["rstd"], w, add=over["add"], grads=grads)
+            assert all(torch.equal(grads[k], want[k]) for k in want), into
