@@ -291,7 +291,8 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
     const int64_t blocks = narrow_bwd_blocks(n);
     const int64_t sz = (int64_t)type_bytes(f.dtype);
     auto from = [&](const void* p, int64_t e) { return p ? static_cast<const char*>(p) + e * sz : nullptr; };
-    for (int64_t c = 0; c < f.h; c += 128) {
+    // no rows: no parts either, whose sums are zeros
+    for (int64_t c = 0; n > 0 && c < f.h; c += 128) {
       const FfnNarrowBwd a{x, dy, from(f.w_gate, c * f.d), from(f.w_up, c * f.d), from(f.w_down, c), from(f.b_gate, c),
                            from(f.b_up, c), dx, s.part, s.dx_part, n, f.d, std::min<int64_t>(f.h - c, 128), f.o, f.h,
                            c, ldx, lddy, lddx, up8(f.d), narrow_sums(f), c + 128 >= f.h, mask, scale, f.act};

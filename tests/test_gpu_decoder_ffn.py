@@ -344,3 +344,18 @@ def test_refusals(api):
         with pytest.raises((ValueError, api.AbcdError)):
             call()
             print("not refused:", i)
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("d,h,o", [(16, 24, 8), (64, 64, 64), (64, 128, 64), (59, 129, 33), (64, 384, 64), (128, 192, 128)])
+def test_no_rows_of_any_block(api, dtype, d, h, o):
+    w = weights(1, d, h, o, dtype, True)
+    x, dy = torch.empty(0, d, dtype=dtype, device="cuda"), torch.empty(0, o, dtype=dtype, device="cuda")
+    for p in (0.0, 0.1):
+        say("no rows", dtype, d, h, o, p)
+        f = api.gated_ffn(x, w, p=p, save=True)
+        assert f["y"].shape == (0, o)
+        for saved in (f["saved"], None):
+            g = api.gated_ffn_bwd(dy, x, w, saved=saved, p=p)
+            assert set(g) == set(w) | {"x"} and g["x"].shape == (0, d)
+            assert all((v == 0).all() for v in g.values())
