@@ -457,8 +457,8 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
  * output: w_gate and w_up [h][d], w_down [o][h]; biases [h], [h], [o], each may be
  * NULL (0). Dropout as in abcd_dropout over y's n rows (p = 0: none). act:
  * ABCD_ACT_SILU g sigmoid(g), ABCD_ACT_GELU g Phi(g) (Phi the normal distribution,
- * by the error function), ABCD_ACT_RELU max(g, 0). Products and act are computed
- * in fp32; h, its derivatives by the pre-activations and the gradients that
+ * by the error function), ABCD_ACT_RELU max(g, 0); of a NaN each gives NaN, as value
+ * and as derivative. Products and act are computed in fp32; h, its derivatives by the pre-activations and the gradients that
  * reach these are rounded to dtype where they are stored between products. In float32 a
  * row of x or dy with an infinity gives NaN where the sum would be infinite. */
 enum { ABCD_ACT_SILU = 0, ABCD_ACT_GELU = 1, ABCD_ACT_RELU = 2 };

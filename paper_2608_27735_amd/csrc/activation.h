@@ -54,8 +54,9 @@ __device__ __forceinline__ float activate(float g, float& slope) {
     slope = fmaf(g * 0.39894228040143268f, e, c);
     return g * c;
   }
-  slope = g > 0.0f ? 1.0f : 0.0f;
-  return fmaxf(g, 0.0f);
+  const float v = g < 0.0f ? 0.0f : g;  // a NaN stays one, and so does its slope
+  slope = g > 0.0f ? 1.0f : v;
+  return v;
 }
 
 // Calls f with act as a constant.

@@ -359,3 +359,26 @@ def test_no_rows_of_any_block(api, dtype, d, h, o):
             g = api.gated_ffn_bwd(dy, x, w, saved=saved, p=p)
             assert set(g) == set(w) | {"x"} and g["x"].shape == (0, d)
             assert all((v == 0).all() for v in g.values())
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("n,d,h,o", [(3, 40, 72, 24), (90, 80, 136, 70), (200, 40, 72, 24), (40000, 96, 130, 18)])
+def test_nan_among_the_weights_shows(api, dtype, act, n, d, h, o):
+    """A NaN of the gate alone reaches y and every gradient that its unit of h enters."""
+    say("nan", dtype, act, n, d, h, o)
+    nan, unit = float("nan"), 5
+    x, dy = rand(1, n, d, dtype), rand(2, n, o, dtype)
+    for where in ("w_gate", "b_gate"):
+        w = weights(10, d, h, o, dtype, True)
+        w[where][unit if where == "b_gate" else (unit, 3)] = nan
+        f = api.gated_ffn(x, w, act, save=True)
+        assert f["y"].isnan().all() and api.gated_ffn(x, w, act)["y"].isnan().all()
+        for saved in (f["saved"], None):
+            g = api.gated_ffn_bwd(dy, x, w, act, saved=saved)
+            assert g["x"].isnan().all() and g["w_down"][:, unit].isnan().all()
+            others = torch.arange(h, device="cuda") != unit
+            for k in ("gate", "up"):
+                assert g["w_" + k][unit].isnan().all() and g["b_" + k][unit].isnan()
+                assert g["w_" + k][others].isfinite().all() and g["b_" + k][others].isfinite().all()
+            assert g["w_down"][:, others].isfinite().all() and g["b_down"].isfinite().all()
