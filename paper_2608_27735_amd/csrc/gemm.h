@@ -22,13 +22,15 @@
 // - Fragments are 16 x 16, with W as the matrix instruction's first operand, so
 //   that a lane holds four consecutive columns of one row of the result: stores of
 //   four elements, and one block of dropout's generator for them.
-// - fp32: every number is the sum of three of 8 bits each, cut off one after the
-//   other (exact), and a product the six products of parts that are not below its last
-//   bit, on the same matrix instructions with fp32 sums: 96 cycles of a SIMD for what
-//   v_mfma_f32_16x16x4_f32 takes 256 for, at a relative error of a product of 2^-24.
-//   The parts are made on the way from memory to LDS, through registers. An infinity
-//   among the operands gives NaN. (137 x 1,696 x 3,208 x 63, forward and backward: 151 us,
-//   with the fp32 instruction, and no split contractions, 615.)
+// - fp32: every number is the sum of three of 8 bits each, the second and third of
+//   what rounding left (exact down to 2^-110, where the third part's bits end), and a
+//   product the six products of parts that are not below its last bit, on the same matrix
+//   instructions with fp32 sums: 96 cycles of a SIMD for what v_mfma_f32_16x16x4_f32
+//   takes 256 for. The parts left out are at most 2^-24 of a product, to either side; the
+//   instruction's own sum is within an ulp and leans down by 0.1 of one. The parts are
+//   made on the way from memory to LDS, through registers. An infinity among the operands
+//   gives NaN. (137 x 1,696 x 3,208 x 63, forward and backward: 151 us, with the fp32
+//   instruction, and no split contractions, 615.)
 //
 // What the matrix instructions' rate bounds runs at 1.15 to 1.3 PFLOP/s in bf16, a large
 // library product at 1.35: two 256 x 256 tiles of 64 contraction indexes fill the LDS of
@@ -320,20 +322,24 @@ struct Product : Accumulators<TX, TW, kWX, kWW, kHalves> {
 
 // ------------------------------------------------------------------ fp32
 
-// Three bf16 whose sum is v, cut off one after the other: 8 bits each, of two numbers
-// a word.
+// Three bf16 whose sum is v, of two numbers a word: each what is left, rounded to
+// nearest, so that what is left is signed and at most half of the part's last bit. (The
+// first not past the largest bf16: a v up to 2^-9 above it would round to infinity.)
 struct Parts {
   uint32_t p[3];
 };
 __device__ __forceinline__ Parts parts_of(float a, float b) {
+  typedef VecOf<__bf16, 2>::type B2;
+  constexpr float kMost = 0x1.FEp127f;
   Parts r;
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
-    r.p[i] = __builtin_amdgcn_perm(ub, ua, 0x07060302);  // the upper halves
+    Floats<2> v = {a, b};
+    if (i == 0) v = {__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost)};
+    r.p[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, B2));
     if (i < 2) {
-      a -= __uint_as_float(ua & 0xFFFF0000u);
-      b -= __uint_as_float(ub & 0xFFFF0000u);
+      a -= __uint_as_float(r.p[i] << 16);
+      b -= __uint_as_float(r.p[i] & 0xFFFF0000u);
     }
   }
   return r;

@@ -382,3 +382,28 @@ def test_nan_among_the_weights_shows(api, dtype, act, n, d, h, o):
                 assert g["w_" + k][unit].isnan().all() and g["b_" + k][unit].isnan()
                 assert g["w_" + k][others].isfinite().all() and g["b_" + k][others].isfinite().all()
             assert g["w_down"][:, others].isfinite().all() and g["b_down"].isfinite().all()
+
+
+def test_products_of_single_numbers_in_float32(api):
+    """Every product of two numbers of 24 bits by itself: h of one input through ReLU
+    and a unit matrix. Of nine products of parts six are made; the others are at most
+    2^-24, to either side. The matrix instruction's last sum is off by less than an ulp
+    (2 x 2^-24 of 1) and those before it by 2^-7 of that; it leans down by 0.21 x 2^-24
+    where no product is left out (24 by 8 bits)."""
+    top = 2.0 - 2.0 ** -23
+    edge = [1.0 + s * 2.0 ** -e + t * 2.0 ** -23 for e in (6, 7, 8, 9, 15, 16, 17) for s in (1, 3) for t in (-1, 0, 1)]
+    edge += [1.0, top, top / 2, 1.0 + 2.0 ** -23, 4.0 / 3.0, 1.6, 1.0 + 255.0 * 2.0 ** -8]
+    gen = torch.Generator().manual_seed(11)
+    a, b = ((1.0 + torch.rand(k, generator=gen, dtype=R.F64)).float() for k in (1000, 128))
+    a[:len(edge)] = torch.tensor(edge)
+    b[:len(edge)] = torch.tensor(edge)
+    h = len(b)
+    for sa, sb in ((1.0, 1.0), (2.0 ** 127, 2.0 ** -3), (2.0 ** -3, 2.0 ** 127), (2.0 ** -60, 2.0 ** 20)):
+        x, wg = (a.double() * sa).float()[:, None].cuda(), (b.double() * sb).float()[:, None].cuda()
+        w = dict(w_gate=wg, w_up=torch.zeros_like(wg), w_down=torch.eye(h, device="cuda"), b_up=torch.ones(h, device="cuda"))
+        y = R.d64(api.gated_ffn(x, w, "relu")["y"])
+        ref = R.d64(x) * R.d64(wg).T
+        off = (y - ref) / ref * 2.0 ** 24
+        say("single products", sa, sb, "largest", off.abs().max().item(), "mean", off[len(edge):, len(edge):].mean().item())
+        assert off.abs().max() <= 3.1
+        assert off[len(edge):, len(edge):].mean().abs() <= 0.3
