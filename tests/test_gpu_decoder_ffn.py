@@ -2,6 +2,8 @@
 definition. Tolerances: one rounding of the output, six standard deviations of
 what rounding the stored intermediates leaves, and fp32 roundings of the sums'
 terms (16 of their magnitude)."""
+import math
+
 import pytest
 import torch
 
@@ -407,3 +409,23 @@ def test_products_of_single_numbers_in_float32(api):
         say("single products", sa, sb, "largest", off.abs().max().item(), "mean", off[len(edge):, len(edge):].mean().item())
         assert off.abs().max() <= 3.1
         assert off[len(edge):, len(edge):].mean().abs() <= 0.3
+
+
+def gelu_far_below(api, dtype, share):
+    """y of the block of one input with gates from -12 to 0 (2e-32, above the 2^-110
+    from which products of fp32 have all their digits), within `share` of GELU."""
+    x = torch.linspace(-12.0, -2.0 ** -10, 4801).to(dtype).cuda()[:, None]
+    one = torch.ones(1, 1, dtype=dtype, device="cuda")
+    w = dict(w_gate=one, w_up=torch.zeros_like(one), w_down=one, b_up=one[0])
+    ref = 0.5 * R.d64(x) * torch.special.erfc(-R.d64(x) / math.sqrt(2.0))
+    for rows in (4801, 40):
+        y = R.d64(api.gated_ffn(x[:rows], w, "gelu")["y"])
+        off = (y - ref[:rows]).abs() - share * ref[:rows].abs() - R.TINY[dtype]
+        say("gelu far below", dtype, rows, ((y - ref[:rows]) / ref[:rows]).abs().max().item())
+        assert (off <= 0).all(), (rows, x[off.argmax()].item())
+
+
+def test_gelu_keeps_its_digits_far_below_zero(api):
+    """16 roundings of fp32: the reciprocal's by the derivative of the fit 8, its other
+    steps 5, exponential and products 3."""
+    gelu_far_below(api, torch.float32, 16 * R.E32)
