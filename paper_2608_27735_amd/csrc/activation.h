@@ -30,12 +30,12 @@ __device__ __forceinline__ float bell(float g) {
 // branch at every element no two elements' exponentials overlap.
 // The normal distribution below 0 is e^(-g^2 / 2) times a smooth function of |g|, and
 // the derivative needs the exponential anyway; the other factor is t Q(t), with t =
-// 1 / (1 + p |g|) in (0, 1]. kShort, for what is rounded to 16 bits: Abramowitz and
-// Stegun's 7.1.26, the distribution within 1e-7. Else Q of degree 9, fitted to the scaled
-// complementary error function with the least relative error, 3.3e-8 (with the
-// roundings of fp32 3.2e-7, measured from g = -12 on), so that the tail keeps its digits. The first product of 65,536 rows
+// 1 / (1 + p |g|) in (0, 1], fitted to the scaled complementary error function with the
+// least relative error, so that the tail keeps its digits: Q of degree 5, 4.8e-6, for
+// what is rounded to 16 bits (kShort); else of degree 9, 3.3e-8 (with the
+// roundings of fp32 3.2e-7, measured from g = -12 on). The first product of 65,536 rows
 // of 96 x 256 in fp32 takes 73 us, with erff 80; a step of 1M rows of 64 x 128 x 64 in
-// bfloat16 429, with erff 527.
+// bfloat16 404, with erff 527.
 template <int kAct, bool kShort>
 __device__ __forceinline__ float activate(float g, float& slope) {
   if (kAct == ABCD_ACT_SILU) {
@@ -47,11 +47,12 @@ __device__ __forceinline__ float activate(float g, float& slope) {
     const float e = kShort ? __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g) : bell(g);
     float s;
     if (kShort) {
-      const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.0f));
-      s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-      s = fmaf(t, s, 0.5f * 1.421413741f);
-      s = fmaf(t, s, 0.5f * -0.284496736f);
-      s = fmaf(t, s, 0.5f * 0.254829592f) * t * e;
+      const float t = __builtin_amdgcn_rcpf(fmaf(0.31f, fabsf(g), 1.0f));
+      s = fmaf(t, -0.07391444f, 0.18040521f);
+      s = fmaf(t, s, 0.01579695f);
+      s = fmaf(t, s, 0.1334017f);
+      s = fmaf(t, s, 0.12044814f);
+      s = fmaf(t, s, 0.123860106f) * t * e;
     } else {
       const float t = __builtin_amdgcn_rcpf(fmaf(0.31819805f, fabsf(g), 1.0f));
       s = fmaf(t, -0.02069551f, 0.095343746f);

@@ -429,3 +429,9 @@ def test_gelu_keeps_its_digits_far_below_zero(api):
     """16 roundings of fp32: the reciprocal's by the derivative of the fit 8, its other
     steps 5, exponential and products 3."""
     gelu_far_below(api, torch.float32, 16 * R.E32)
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+def test_gelu_keeps_its_digits_far_below_zero_in_16_bits(api, dtype):
+    """The rounding of h, 4.8e-6 of the fit and the exponential's arithmetic."""
+    gelu_far_below(api, dtype, R.UNIT[dtype] + 6e-6)
