@@ -21,10 +21,11 @@ namespace abcd {
 namespace {
 
 // sum / d, rounded once or nearly so (a constant row has to give its own value:
-// what its mean is off by, rstd multiplies by up to 1 / sqrt(eps)).
+// what its mean is off by, rstd multiplies by up to 1 / sqrt(eps)). An infinite sum
+// leaves nothing to correct.
 __device__ __forceinline__ float mean_of(float sum, float d, float inv_d) {
   const float m = sum * inv_d;
-  return fmaf(fmaf(-m, d, sum), inv_d, m);
+  return __builtin_isinf(m) ? m : fmaf(fmaf(-m, d, sum), inv_d, m);
 }
 
 struct NormArgs {

@@ -292,3 +292,16 @@ def test_layer_norm_gradients_in_place(api, dtype, n, d):
             grads = dict(x=over[into], weight=torch.empty_like(w), bias=torch.empty_like(w))
             api.layer_norm_bwd(over["dy"], x, f["mean"], f["rstd"], w, add=over["add"], grads=grads)
             assert all(torch.equal(grads[k], want[k]) for k in want), into
+
+
+def test_layer_norm_statistics_of_infinite_rows(api):
+    """The mean of a row with an infinity is that infinity, with both NaN."""
+    inf = float("inf")
+    for dtype in DT:
+        for d in (40, 4100, 20001):
+            x = rand(1, 6, d, dtype)
+            x[1, 3], x[2, d - 1], x[3, 0], x[3, 5], x[4, 7] = inf, -inf, inf, -inf, float("nan")
+            f = api.layer_norm(x)
+            assert f["mean"][1] == inf and f["mean"][2] == -inf and f["mean"][3:5].isnan().all()
+            assert f["rstd"][1:5].isnan().all() and f["y"][1:5].isnan().all()
+            assert f["mean"][[0, 5]].isfinite().all() and f["y"][[0, 5]].isfinite().all()
