@@ -28,6 +28,12 @@ __device__ __forceinline__ float mean_of(float sum, float d, float inv_d) {
   return __builtin_isinf(m) ? m : fmaf(fmaf(-m, d, sum), inv_d, m);
 }
 
+// 1 / sqrt(v), also where v is subnormal, of which the instruction makes an infinity.
+__device__ __forceinline__ float rsqrt_of(float v) {
+  const bool small = v < 0x1p-126f;
+  return __builtin_amdgcn_rsqf(small ? v * 0x1p24f : v) * (small ? 0x1p12f : 1.0f);
+}
+
 struct NormArgs {
   const void* x;
   const void* w;
@@ -84,7 +90,7 @@ __global__ __launch_bounds__(kBlock) void layer_norm_kernel(NormArgs a) {
         s += e * e;
       }
     }
-    const float rstd = __builtin_amdgcn_rsqf(row_sum<G>(s, red[1]) * a.inv_d + a.eps);
+    const float rstd = rsqrt_of(row_sum<G>(s, red[1]) * a.inv_d + a.eps);
     T* y = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -122,7 +128,7 @@ __global__ __launch_bounds__(kBlock) void layer_norm_wide_kernel(NormArgs a) {
         s += e * e;
       }
     }
-    const float rstd = __builtin_amdgcn_rsqf(row_sum<kBlock>(s, red[1]) * a.inv_d + a.eps);
+    const float rstd = rsqrt_of(row_sum<kBlock>(s, red[1]) * a.inv_d + a.eps);
     T* y = static_cast<T*>(a.y) + row * a.ldy;
     for (int c = threadIdx.x * N; c < a.d; c += kBlock * N) {
       Floats<N> v = (load_vec<T, N, kWhole>(x + c, a.d - c) - mean) * rstd;

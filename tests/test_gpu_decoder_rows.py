@@ -305,3 +305,17 @@ def test_layer_norm_statistics_of_infinite_rows(api):
             assert f["mean"][1] == inf and f["mean"][2] == -inf and f["mean"][3:5].isnan().all()
             assert f["rstd"][1:5].isnan().all() and f["y"][1:5].isnan().all()
             assert f["mean"][[0, 5]].isfinite().all() and f["y"][[0, 5]].isfinite().all()
+
+
+def test_layer_norm_of_tiny_rows(api):
+    """With eps = 0 or a subnormal one the variance may be subnormal."""
+    n, d, scale = 20, 96, 2.0 ** -66
+    x = rand(1, n, d, torch.float32, scale=scale)
+    for eps in (0.0, 2.0 ** -131):
+        f = api.layer_norm(x, eps=eps)
+        y, mean, rstd, mag = R.layer_norm(R.d64(x), None, None, eps)
+        # every square and sum below 2^-126 is off by half of 2^-149 at most
+        var = R.d64(x).var(1, unbiased=False)
+        off = 4 * 2.0 ** -150 / (var + eps)
+        assert ((R.d64(f["rstd"]) - rstd).abs() <= rstd * (16 * R.E32 + off)).all()
+        assert ((R.d64(f["y"]) - y).abs() <= mag * (16 * R.E32 + off[:, None])).all()
