@@ -435,3 +435,24 @@ def test_gelu_keeps_its_digits_far_below_zero(api):
 def test_gelu_keeps_its_digits_far_below_zero_in_16_bits(api, dtype):
     """The rounding of h, 4.8e-6 of the fit and the exponential's arithmetic."""
     gelu_far_below(api, dtype, R.UNIT[dtype] + 6e-6)
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n,d,h,o", [
+    (1024, 64, 128, 64), (1025, 1, 1, 1), (3000, 59, 127, 61), (1500, 16, 129, 16), (20011, 64, 128, 64),
+    (4096, 64, 256, 64), (5000, 8, 384, 16), (4200, 33, 300, 64), (1031, 63, 63, 63)])
+def test_narrow_rows_with_relu(api, dtype, n, d, h, o):
+    run(api, n, d, h, o, dtype, "relu", True, 0.1)
+    run(api, n, d, h, o, dtype, "relu", False, 0.0, pad=5, skip=1)
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n,d,h,o", [
+    (4111, 1, 129, 1), (4096, 64, 384, 64), (70001, 72, 130, 70), (40003, 96, 176, 18), (40000, 128, 192, 128)])
+def test_narrow_forward_with_relu(api, dtype, n, d, h, o):
+    for bias, p, pad, skip in [(True, 0.1, 0, 0), (False, 0.0, 5, 1)]:
+        say("narrow forward, relu", n, d, h, o, dtype, p, pad, skip)
+        x, w, res = rand(1, n, d, dtype, pad, skip), weights(10, d, h, o, dtype, bias), rand(2, n, o, dtype, skip, pad)
+        keep = R.keep_mask(n, o, p, 5, 9) if p > 0.0 else torch.ones(n, o, dtype=torch.bool)
+        ref = R.ffn(R.d64(x), {k: R.d64(v) for k, v in w.items()}, "relu", R.UNIT[dtype], R.d64(res), keep, p)
+        check("y", api.gated_ffn(x, w, "relu", residual=res, p=p, seed=5, offset=9)["y"], ref["y"])
