@@ -133,3 +133,40 @@ def test_reference_ffn_gradients_are_its_forwards(name):
     got = R.ffn(x, w, name, 0.0, None, keep, 0.25, dy)
     for k in want:
         assert torch.allclose(got[k][0], want[k], rtol=1e-10, atol=1e-12), k
+
+
+def test_reference_generator_published_words():
+    """Known answers published with the generator (4x32, 7 rounds): the words for
+    counter 0 under key 0, and, as rows and offsets are counters too, for the digits of
+    pi in both."""
+    def words(quad, row, seed, offset):
+        kept = []
+        for j in range(4):  # the threshold at which a word is just kept, bit by bit
+            at = 0
+            for bit in range(31, -1, -1):
+                p = (at + (1 << bit)) / 2.0 ** 32
+                if _mask_row(quad, row, p, seed, offset)[j]:
+                    at += 1 << bit
+            kept.append(at)
+        return kept
+
+    assert words(0, 0, 0, 0) == [0x5F6FB709, 0x0D893F64, 0x4F121F81, 0x4F730A48]
+    small = words(0, 3, (5 << 32) + 7, (9 << 32) + 11)
+    assert small == _philox7([0, 3, 11, 9], [7, 5])
+    assert _philox7([0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344], [0xA4093822, 0x299F31D0]) == \
+        [0x4DFCCABA, 0x190A87F0, 0xC47362BA, 0xB6B5242A]
+
+
+def _mask_row(quad, row, p, seed, offset):
+    return R.keep_mask(row + 1, 4 * quad + 4, p, seed, offset)[row, 4 * quad:]
+
+
+def _philox7(c, k):
+    """The generator in plain integers; the last case above pins it to the published
+    words of a counter and key that no mask's row reaches."""
+    for _ in range(7):
+        h0, l0 = divmod(0xD2511F53 * c[0], 1 << 32)
+        h1, l1 = divmod(0xCD9E8D57 * c[2], 1 << 32)
+        c = [h1 ^ c[1] ^ k[0], l1, h0 ^ c[3] ^ k[1], l0]
+        k = [(k[0] + 0x9E3779B9) % (1 << 32), (k[1] + 0xBB67AE85) % (1 << 32)]
+    return c
