@@ -58,6 +58,7 @@ class FeatureDecoder:
         self.m = {k: torch.zeros_like(v) for k, v in self.params.items()}
         self.v = {k: torch.zeros_like(v) for k, v in self.params.items()}
         self.t = 0
+        self._kept = None
 
     def _views(self, flat):
         views, at = {}, 0
@@ -73,7 +74,7 @@ class FeatureDecoder:
 
     def forward(self, train=True):
         """SH coefficients [n, (sh_degree + 1)^2, 3] in fp32. train: dropout, and
-        what backward() needs is kept; every call has a mask of its own."""
+        what backward() needs is kept; every such call has a mask of its own."""
         w = self._views(self.flat.to(self.dtype))
         x = self.features.to(self.dtype)
         p = self.p if train else 0.0
@@ -84,11 +85,15 @@ class FeatureDecoder:
                            offset=offset, save=train)
         n2 = api.layer_norm(f1["y"], w["norm2_weight"], w["norm2_bias"])
         f2 = api.gated_ffn(n2["y"], self._ffn(w, 2), self.act, save=train)
-        self._kept = (w, x, n1, f1, n2, f2, p, offset) if train else None
+        if train:
+            self._kept = (w, x, n1, f1, n2, f2, p, offset)
         return f2["y"].float().view(-1, self.nc, 3)
 
     def backward(self, d_sh):
-        """Gradients of features and weights from the SH coefficients' gradient."""
+        """Gradients of features and weights from the gradient of the SH coefficients
+        that the last forward() with train=True gave; once for each of these."""
+        if self._kept is None:
+            raise ValueError("backward() needs a forward() with train=True before it")
         w, x, n1, f1, n2, f2, p, offset = self._kept
         self._kept = None
         d = d_sh.reshape(x.shape[0], -1).to(self.dtype)

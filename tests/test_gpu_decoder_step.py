@@ -63,3 +63,19 @@ def test_decoder_trains_through_the_step(decoder):
     print(f"  L1 loss {first:.4f} -> {last:.4f}")
     assert last < 0.5 * first
     assert torch.equal(params["sh"], stored)  # the caller's parameters are not written
+
+
+def test_a_forward_without_training_keeps_what_training_needs(decoder):
+    """A look at the colours between a training forward and its backward changes
+    neither; a backward without a forward is refused."""
+    d_sh = torch.randn(50, 4, 3, generator=torch.Generator().manual_seed(2)).cuda()
+    a, b = (decoder.FeatureDecoder(50, width=24, hidden=32, sh_degree=1, p=0.2, seed=3) for _ in range(2))
+    with pytest.raises(ValueError):
+        a.backward(d_sh)
+    want, got = a.forward(), b.forward()
+    b.forward(train=False)
+    assert torch.equal(want, got)
+    want, got = a.backward(d_sh), b.backward(d_sh)
+    assert all(torch.equal(want[k], got[k]) for k in want)
+    with pytest.raises(ValueError):
+        a.backward(d_sh)
