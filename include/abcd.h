@@ -457,10 +457,16 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
  * output: w_gate and w_up [h][d], w_down [o][h]; biases [h], [h], [o], each may be
  * NULL (0). Dropout as in abcd_dropout over y's n rows (p = 0: none). act:
  * ABCD_ACT_SILU g sigmoid(g), ABCD_ACT_GELU g Phi(g) (Phi the normal distribution,
- * by the error function), ABCD_ACT_RELU max(g, 0); of a NaN each gives NaN, as value
- * and as derivative. Products and act are computed in fp32; h, its derivatives by the pre-activations and the gradients that
- * reach these are rounded to dtype where they are stored between products. In float32 a
- * row of x or dy with an infinity gives NaN where the sum would be infinite. */
+ * by the error function; in 16-bit types within 5e-6 of its size), ABCD_ACT_RELU
+ * max(g, 0); of a NaN each gives NaN, as value and as derivative. Products and act are
+ * computed in fp32. h, its derivatives by the pre-activations and the gradients that
+ * reach these are rounded to dtype where they go from one product to the next, in
+ * memory or in registers, and the weights' and biases' gradients are sums of what was
+ * rounded. In float16 this bounds their range too: beyond 65,504 they are infinities,
+ * below 2^-25 zeros, whatever y and the weights' gradients come to, so that a loss is
+ * scaled as float16 training does. In float32 a product may give NaN where an infinity
+ * among what it multiplies (x, dy, a weight, h) would make it infinite, and numbers below
+ * 2^-110 have fewer digits in it. */
 enum { ABCD_ACT_SILU = 0, ABCD_ACT_GELU = 1, ABCD_ACT_RELU = 2 };
 typedef struct abcd_ffn {
   int32_t dtype, act;

@@ -436,7 +436,8 @@ def layer_norm_bwd(dy, x, mean, rstd, weight=None, add=None, wdtype=None, worksp
     """Gradients of layer_norm: dict(x, weight, bias). mean and rstd are the
     forward's; add [n, d] is added to x's gradient (a residual path's). weight
     and bias gradients have weight's type (wdtype without a weight). grads: a
-    dict of tensors to write into, where a None leaves that gradient out."""
+    dict of tensors to write into, where a None leaves that gradient out; x's may be
+    dy or add itself."""
     code = _dtype_of(x, "x")
     ldx = _rows(x, "x")
     size, dev = x.shape, x.device
@@ -567,7 +568,9 @@ def gated_ffn(x, params, act="silu", residual=None, p=0.0, seed=0, offset=0, sav
     row stride): residual + dropout(h w_down' + b_down) with
     h = act(x w_gate' + b_gate) * (x w_up' + b_up). params: dict(w_gate [h, d],
     w_up [h, d], w_down [o, h][, b_gate [h], b_up [h], b_down [o]]) of x's type.
-    act: "silu", "gelu" or "relu". Dropout as in dropout().
+    act: "silu", "gelu" or "relu". Dropout as in dropout(). h, and in the backward the
+    gradients that reach it, are rounded to x's type between products: in float16
+    they overflow beyond 65,504 and vanish below 2^-25.
 
     Returns dict(y [n, o], saved): with save=True what gated_ffn_bwd takes of
     this pass, else None; None too where the backward makes it again faster than
@@ -603,7 +606,8 @@ def gated_ffn_bwd(dy, x, params, act="silu", saved=None, p=0.0, seed=0, offset=0
     """Gradients of gated_ffn for dy [n, o]: dict(x, w_gate, w_up, w_down[, and
     the biases that params has]); the residual's is dy itself. saved: the
     forward's, or None to compute it again. p, seed and offset are the forward's.
-    grads: a dict of tensors to write into, where a missing one is left out."""
+    grads: a dict of tensors to write into, where a missing one is left out; none may
+    overlap an input."""
     f, ldx = _ffn(x, params, act, p, seed, offset)
     n, d = x.shape
     dev = x.device

@@ -17,10 +17,10 @@
 // instead of two or three, and the backward evaluates no activation. dz is dy with
 // zeros, exact; its factor 1 / (1 - p) is applied to the products' fp32 sums.
 //
-// 8,192 rows of 2,048 x 5,632 x 2,048 in bf16, forward and backward: 1,520 us, 1.12
-// PFLOP/s. First product 337 us (1,121 TFLOP/s, with three arrays of 92 MB written), down
-// 162 (1,167), dh 212 (891: two such arrays read and two written), dx 292 (1,294), the
-// three weights' gradients 468 and 14 for the sums of split tiles (1,176).
+// 8,192 rows of 2,048 x 5,632 x 2,048 in bf16, forward and backward: 1,524 us, 1.12
+// PFLOP/s. First product 341 us (1,108 TFLOP/s, with three arrays of 92 MB written), down
+// 163 (1,159), dh 215 (879: two such arrays read and two written), dx 298 (1,268), the
+// three weights' gradients 477 and 12 for the sums of split tiles (1,159).
 #pragma once
 
 #include <algorithm>

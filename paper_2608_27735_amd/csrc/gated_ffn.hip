@@ -148,9 +148,9 @@ size_t dweight_part(const abcd_ffn& f, int64_t steps) {
 
 // Whether the kernels for a few rows take the first products. They read x again for
 // every 16 columns of h, so that many rows of a wide block leave it to the tiles: bf16,
-// 64 x 512 x 1,376 x 512 18 against 25 us, 64 x 1,024 x 2,816 x 1,024 25 either way, 64 x
-// 2,048 x 5,632 x 2,048 55 against 35; fp32, 32 rows of the second 33 against 37, 48 rows
-// 44 against 39.
+// 64 x 512 x 1,376 x 512 16 against 19 us, 64 x 1,024 x 2,816 x 1,024 24 either way, 64 x
+// 2,048 x 5,632 x 2,048 52 against 35; fp32, 32 rows of the second 30 against 37, 48 rows
+// 41 against 38.
 bool few(const abcd_ffn& f, int64_t n) {
   return n <= 16 || (n <= 64 && (n + 15) / 16 * (2 * f.h * f.d + f.o * f.h) * (int64_t)type_bytes(f.dtype) <= 80 << 20);
 }

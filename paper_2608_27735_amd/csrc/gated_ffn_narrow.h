@@ -22,8 +22,8 @@
 // gradients. The biases' gradients are products with ones. Workgroups write their
 // sums in fp32, and a second launch adds these in a fixed order.
 //
-// 1M rows of 64 x 128 x 64 in bf16, dropout and biases: forward 106 us (256 MB), backward
-// 220 (384 MB). Neither memory nor the matrix instructions (20 and 29 percent busy) bound
+// 1M rows of 64 x 128 x 64 in bf16, dropout and biases: forward 100 us (256 MB), backward
+// 210 (384 MB). Neither memory nor the matrix instructions (20 and 29 percent busy) bound
 // them but issue: the forward's vector instructions (activation, generator, conversions;
 // 63 percent busy) at four waves a SIMD, the backward's chain of LDS, products,
 // activation and products at the two waves that its registers leave room for (vector

@@ -29,10 +29,10 @@
 //   takes 256 for. The parts left out are at most 2^-24 of a product, to either side; the
 //   instruction's own sum is within an ulp and leans down by 0.1 of one. The parts are
 //   made on the way from memory to LDS, through registers. An infinity among the operands
-//   gives NaN. (137 x 1,696 x 3,208 x 63, forward and backward: 151 us, with the fp32
+//   gives NaN. (137 x 1,696 x 3,208 x 63, forward and backward: 147 us, with the fp32
 //   instruction, and no split contractions, 615.)
 //
-// What the matrix instructions' rate bounds runs at 1.15 to 1.3 PFLOP/s in bf16, a large
+// What the matrix instructions' rate bounds runs at 1.1 to 1.3 PFLOP/s in bf16, a large
 // library product at 1.35: two 256 x 256 tiles of 64 contraction indexes fill the LDS of
 // a CU, which so holds one workgroup of 8 waves, and nothing overlaps its first loads and
 // its last stores.
