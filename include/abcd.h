@@ -512,6 +512,52 @@ ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, c
                                     hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Operators around the decoder's blocks, for the same rows and element types. */
+
+/* Features that rows share: y[i] = scale table[index[i]] for n indexes (index_bits:
+ * 32 or 64, signed) into a table of m rows (1 <= m <= ABCD_MAX_GAUSSIANS, type tdtype:
+ * dtype or ABCD_F32). An index outside [0, m), as of a place of a batch that holds
+ * nothing, gives a row of zeros. y may not overlap the table. */
+ABCD_API int32_t abcd_embed(int32_t dtype, int64_t n, int64_t m, int64_t d, int32_t tdtype,
+                            const void* table, int64_t ldt, int32_t index_bits, const void* index,
+                            float scale, void* y, int64_t ldy, hipStream_t stream);
+
+/* The n positions by index: order[n] (positions; of equal indexes in order, those
+ * outside the table last), rows[n] (their indexes, m for those outside the table) and
+ * ranges[m][2] (where row r's positions begin and end in order; 0, 0 for a row with none). A
+ * set of indexes that does not change is sorted once for all its gradients. workspace: at
+ * least abcd_embed_sort_workspace_size bytes, 256-byte aligned. */
+ABCD_API int32_t abcd_embed_sort_workspace_size(int64_t n, int64_t m, size_t* bytes);
+ABCD_API int32_t abcd_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* index,
+                                 int32_t* order, int32_t* rows, int32_t* ranges, void* workspace,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* The table's gradient: dtable[r] = scale times the sum of dy[i] over the i with index
+ * r, zeros for a row with none (written, not added to; type wdtype: dtype or ABCD_F32; ldt
+ * elements between its rows). order, rows and ranges: abcd_embed_sort's, of the same n and
+ * m, unchanged (they are not checked). workspace: at least abcd_embed_bwd_workspace_size
+ * bytes, 256-byte aligned. */
+ABCD_API int32_t abcd_embed_bwd_workspace_size(int64_t n, int64_t d, size_t* bytes);
+ABCD_API int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy,
+                                int64_t lddy, const int32_t* order, const int32_t* rows,
+                                const int32_t* ranges, float scale, int32_t wdtype, void* dtable,
+                                int64_t ldt, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Checkpoints of activations in 8 bits. Of every ABCD_PACK8_BLOCK consecutive elements
+ * of a row (the last block may have fewer), with 2^e the largest power of two that does
+ * not exceed the largest finite magnitude (e at least -120):
+ *   q = rint(x 2^(6 - e)) between -127 and 127, which stands for q 2^(e - 6);
+ * an infinity or a NaN is q = -128 and comes back as NaN. q: [n][blocks][32] (elements past
+ * the row's end 0), 16-byte aligned; e: [n][blocks], the byte e + 127; blocks = (d + 31) / 32.
+ * What was packed and unpacked packs to the same again. abcd_unpack8 writes dtype, which
+ * is the packed one's: its numbers hold q 2^(e - 6) exactly. */
+#define ABCD_PACK8_BLOCK 32
+ABCD_API int32_t abcd_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx,
+                            int8_t* q, uint8_t* e, hipStream_t stream);
+ABCD_API int32_t abcd_unpack8(int32_t dtype, int64_t n, int64_t d, const int8_t* q,
+                              const uint8_t* e, void* y, int64_t ldy, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Helpers. abcd_last_error: message of the last failure on this thread.
  * abcd_timing_*: optional per-kernel HIP-event timing of every launch made by
  * this thread (off by default; enabling it adds two event records per launch
@@ -522,7 +568,9 @@ ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, c
  * render_fwd, loss_l1, zero_fill, bwd_order, render_bwd, project_bwd, adam,
  * render_cache, cache_rect_init, layer_norm, layer_norm_bwd, layer_norm_cols,
  * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
- * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out). */
+ * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out,
+ * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_none, embed_bwd,
+ * embed_join, pack8, unpack8). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

@@ -89,6 +89,14 @@ SIGNATURES = {
     "abcd_gated_ffn": (_I32, [_FFN, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _SZ, _P]),
     "abcd_gated_ffn_bwd": (_I32, [_FFN, _I64, _P, _I64, _P, _I64] + [_P] * 4 + [_I64] + [_P] * 7 +
                            [_SZ, _P]),
+    "abcd_embed": (_I32, [_I32, _I64, _I64, _I64, _I32, _P, _I64, _I32, _P, C.c_float, _P, _I64, _P]),
+    "abcd_embed_sort_workspace_size": (_I32, [_I64, _I64, C.POINTER(_SZ)]),
+    "abcd_embed_sort": (_I32, [_I64, _I64, _I32] + [_P] * 5 + [_SZ, _P]),
+    "abcd_embed_bwd_workspace_size": (_I32, [_I64, _I64, C.POINTER(_SZ)]),
+    "abcd_embed_bwd": (_I32, [_I32, _I64, _I64, _I64, _P, _I64, _P, _P, _P, C.c_float, _I32, _P, _I64,
+                              _P, _SZ, _P]),
+    "abcd_pack8": (_I32, [_I32, _I64, _I64, _P, _I64, _P, _P, _P]),
+    "abcd_unpack8": (_I32, [_I32, _I64, _I64, _P, _P, _P, _I64, _P]),
     "abcd_last_error": (C.c_char_p, []),
     "abcd_version": (C.c_char_p, []),
     "abcd_status_string": (C.c_char_p, [_I32]),

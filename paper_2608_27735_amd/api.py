@@ -5,6 +5,7 @@ their device pointers and the current HIP stream are passed to libabcd.so,
 and every step runs in the library's kernels. There is no CPU fallback.
 """
 import ctypes as C
+from typing import NamedTuple
 
 import torch
 
@@ -638,6 +639,182 @@ def gated_ffn_bwd(dy, x, params, act="silu", saved=None, p=0.0, seed=0, offset=0
     return grads
 
 
+# -------------------------------------------------- decoder: shared features
+
+def _here(t, name):
+    """A kernel runs on the current device's stream."""
+    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+
+
+class Sorted(NamedTuple):
+    """What embed_sort gives: positions by index, and where each table row's are."""
+    order: torch.Tensor   # int32 [n]
+    rows: torch.Tensor    # int32 [n]: their indexes, m for those outside the table
+    ranges: torch.Tensor  # int32 [m, 2]
+
+
+def _index(index, device):
+    """Bits of a contiguous vector of indexes."""
+    if index.dtype != torch.int64 and index.dtype != torch.int32:
+        raise ValueError(f"index must be int32 or int64, got {index.dtype}")
+    if index.device != device or not index.is_cuda:
+        raise ValueError(f"index must be on {device}, got {index.device}")
+    if index.dim() != 1 or not index.is_contiguous():
+        raise ValueError(f"index must be a contiguous vector, got shape {tuple(index.shape)}")
+    return 64 if index.dtype == torch.int64 else 32
+
+
+def _table_rows(m, name):
+    if m < 1:
+        raise ValueError(f"{name} must have rows")
+    return m
+
+
+def embed(table, index, scale=1.0, dtype=None, out=None):
+    """Rows of table [m, d] by index [n] (int32 or int64), scaled: y[i] = scale
+    table[index[i]]. An index outside [0, m) gives a row of zeros. dtype: y's, the
+    table's or, of a float32 table, a shorter one."""
+    tcode = _dtype_of(table, "table")
+    _here(table, "table")
+    ldt = _rows(table, "table")
+    m, d = table.shape
+    _table_rows(m, "table")
+    bits = _index(index, table.device)
+    n = index.shape[0]
+    if out is None:
+        out = torch.empty((n, d), dtype=dtype or table.dtype, device=table.device)
+    elif (dtype is not None and out.dtype != dtype) or out.device != table.device:
+        raise ValueError(f"out must be {dtype or out.dtype} on {table.device}")
+    code = _dtype_of(out, "out")
+    ldy = _rows(out, "out", shape=(n, d))
+    if tcode != code and tcode != 0:
+        raise ValueError(f"table must be {out.dtype} or float32, got {table.dtype}")
+    check(_lib.load().abcd_embed(code, n, m, d, tcode, table.data_ptr(), ldt, bits, index.data_ptr(),
+                                 float(scale), out.data_ptr(), ldy, _stream()))
+    return out
+
+
+def embed_sort(index, m, workspace=None):
+    """The positions of index [n] (int32 or int64) by index, for the gradients of a
+    table of m rows: what embed_bwd takes. Indexes that do not change need it once."""
+    m = _table_rows(int(m), "a table")
+    _here(index, "index")
+    bits = _index(index, index.device)
+    n, dev = index.shape[0], index.device
+    order, rows = torch.empty((2, n), dtype=torch.int32, device=dev).unbind(0)
+    ranges = torch.empty((m, 2), dtype=torch.int32, device=dev)
+    lib = _lib.load()
+    sz = C.c_size_t(0)
+    check(lib.abcd_embed_sort_workspace_size(n, m, C.byref(sz)))
+    workspace = _workspace(workspace, sz.value, dev)
+    check(lib.abcd_embed_sort(n, m, bits, index.data_ptr(), order.data_ptr(), rows.data_ptr(),
+                              ranges.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()))
+    return Sorted(order, rows, ranges)
+
+
+def embed_bwd(dy, index, m, scale=1.0, wdtype=None, out=None, workspace=None):
+    """Gradient [m, d] of embed's table for dy [n, d]: row r gets scale times the sum of
+    dy[i] over the i with index[i] = r, in their order; a row without any zeros. index: the
+    forward's, or what embed_sort made of it. wdtype: the gradient's type, dy's or
+    float32."""
+    code = _dtype_of(dy, "dy")
+    _here(dy, "dy")
+    lddy = _rows(dy, "dy")
+    (n, d), dev = dy.shape, dy.device
+    m = _table_rows(int(m), "a table")
+    if not isinstance(index, Sorted):
+        if index.shape != (n,):
+            raise ValueError(f"index has shape {tuple(index.shape)}, expected ({n},)")
+        _index(index, dev)
+        index = embed_sort(index, m)
+    for t, name, shape in ((index.order, "order", (n,)), (index.rows, "rows", (n,)),
+                           (index.ranges, "ranges", (m, 2))):
+        if t.dtype != torch.int32 or t.device != dev or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous int32 on {dev} with shape {shape}, "
+                             f"got {t.dtype} of {tuple(t.shape)}")
+    if out is None:
+        out = torch.empty((m, d), dtype=wdtype or dy.dtype, device=dev)
+    elif (wdtype is not None and out.dtype != wdtype) or out.device != dev:
+        raise ValueError(f"out must be {wdtype or out.dtype} on {dev}")
+    wcode = _dtype_of(out, "out")
+    if wcode != code and wcode != 0:
+        raise ValueError(f"the gradient must be {dy.dtype} or float32, got {out.dtype}")
+    ldt = _rows(out, "out", shape=(m, d))
+    lib = _lib.load()
+    sz = C.c_size_t(0)
+    check(lib.abcd_embed_bwd_workspace_size(n, d, C.byref(sz)))
+    workspace = _workspace(workspace, sz.value, dev)
+    check(lib.abcd_embed_bwd(code, n, m, d, dy.data_ptr(), lddy, index.order.data_ptr(),
+                             index.rows.data_ptr(), index.ranges.data_ptr(), float(scale), wcode,
+                             out.data_ptr(), ldt, workspace.data_ptr(), workspace.numel(), _stream()))
+    return out
+
+
+# ------------------------------------------------------ decoder: checkpoints
+
+class Packed8(NamedTuple):
+    """Rows as pack8 keeps them."""
+    q: torch.Tensor   # int8 [n, 32 blocks]
+    e: torch.Tensor   # uint8 [n, blocks]
+    width: int
+    dtype: torch.dtype
+
+    @property
+    def shape(self):
+        return torch.Size((self.q.shape[0], self.width))
+
+
+def _packed(p, name):
+    """Checks a checkpoint; returns its rows' number."""
+    n, blocks = p.q.shape[0], (p.width + 31) // 32
+    if p.dtype not in _DTYPES or p.width < 1:
+        raise ValueError(f"{name} must hold rows of float32, float16 or bfloat16")
+    for t, k, dtype, shape in ((p.q, "q", torch.int8, (n, 32 * blocks)), (p.e, "e", torch.uint8, (n, blocks))):
+        if not t.is_cuda or t.dtype != dtype or t.device != p.q.device or t.shape != shape \
+                or not t.is_contiguous():
+            raise ValueError(f"{name}.{k} must be a contiguous {dtype} GPU tensor of shape {shape}, "
+                             f"got {t.dtype} of {tuple(t.shape)}")
+    return n
+
+
+def pack8(x, out=None):
+    """An 8-bit checkpoint of x [n, d] (float32, float16 or bfloat16; any row stride):
+    blocks of 32 elements with one power-of-two scale each (see abcd_pack8). An element is
+    off by at most 1/128 of its block's largest magnitude, those next to that by at most
+    1/64; an infinity or a NaN comes back as NaN. out: a checkpoint of x's shape and
+    type to write into."""
+    code = _dtype_of(x, "x")
+    _here(x, "x")
+    ldx = _rows(x, "x")
+    n, d = x.shape
+    if out is None:
+        blocks = (d + 31) // 32
+        out = Packed8(torch.empty((n, 32 * blocks), dtype=torch.int8, device=x.device),
+                      torch.empty((n, blocks), dtype=torch.uint8, device=x.device), d, x.dtype)
+    else:
+        _packed(out, "out")
+        if out.shape != x.shape or out.dtype != x.dtype or out.q.device != x.device:
+            raise ValueError(f"out must be a checkpoint of {x.dtype} rows of shape {tuple(x.shape)} on {x.device}")
+    check(_lib.load().abcd_pack8(code, n, d, x.data_ptr(), ldx, out.q.data_ptr(), out.e.data_ptr(),
+                                 _stream()))
+    return out
+
+
+def unpack8(packed, out=None):
+    """The rows [n, d] that an 8-bit checkpoint stands for, in the type it was made of."""
+    n, d = _packed(packed, "packed"), packed.width
+    _here(packed.q, "packed")
+    if out is None:
+        out = torch.empty((n, d), dtype=packed.dtype, device=packed.q.device)
+    elif out.dtype != packed.dtype or out.device != packed.q.device:
+        raise ValueError(f"out must be {packed.dtype} on {packed.q.device}, got {out.dtype} on {out.device}")
+    ldy = _rows(out, "out", shape=(n, d))
+    check(_lib.load().abcd_unpack8(_DTYPES[packed.dtype], n, d, packed.q.data_ptr(), packed.e.data_ptr(),
+                                   out.data_ptr(), ldy, _stream()))
+    return out
+
+
 # ---------------------------------------------------------------- collapse
 
 def composite_cache(images, order, n_front, F=None, B=None, accumulate=False, rects=None,
@@ -732,4 +909,5 @@ __all__ = ["AbcdError", "project", "bin_sort", "bin_sort_workspace_size", "rende
            "timing_enable", "timing_reset", "timing_read", "version", "n_tiles", "adam_step",
            "render_cache", "stage_cached", "make_split", "split_workspace_size", "intersections",
            "render_bwd_noalloc", "layer_norm", "layer_norm_bwd", "layer_norm_bwd_workspace_size",
-           "dropout", "dropout_bwd", "gated_ffn", "gated_ffn_bwd"]
+           "dropout", "dropout_bwd", "gated_ffn", "gated_ffn_bwd", "embed", "embed_sort",
+           "embed_bwd", "Sorted", "pack8", "unpack8", "Packed8"]

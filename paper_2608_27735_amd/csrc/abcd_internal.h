@@ -372,6 +372,24 @@ int32_t launch_gated_ffn_bwd(const abcd_ffn& f, int64_t n, const void* dy, int64
                              const void* hidden, void* dx, int64_t lddx, void* dw_gate,
                              void* dw_up, void* dw_down, void* db_gate, void* db_up, void* db_down,
                              void* workspace, hipStream_t stream);
+// embed.hip
+int32_t launch_embed(int32_t dtype, int64_t n, int64_t m, int64_t d, int32_t tdtype,
+                     const void* table, int64_t ldt, int32_t index_bits, const void* index,
+                     float scale, void* y, int64_t ldy, hipStream_t stream);
+size_t embed_sort_workspace_bytes(int64_t n, int64_t m);
+int32_t launch_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* index,
+                          int32_t* order, int32_t* rows, int32_t* ranges, void* workspace,
+                          hipStream_t stream);
+size_t embed_bwd_workspace_bytes(int64_t n, int64_t d);
+int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy,
+                         int64_t lddy, const int32_t* order, const int32_t* rows,
+                         const int32_t* ranges, float scale, int32_t wdtype, void* dtable,
+                         int64_t ldt, void* workspace, hipStream_t stream);
+// pack8.hip
+int32_t launch_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx, int8_t* q,
+                     uint8_t* e, hipStream_t stream);
+int32_t launch_unpack8(int32_t dtype, int64_t n, int64_t d, const int8_t* q, const uint8_t* e,
+                       void* y, int64_t ldy, hipStream_t stream);
 // reduce.hip: out[i][c - begin[i]] = sum over p of part[p][c], rounded to dtype, for
 // the columns c of [begin[i], begin[i + 1]); an output may be NULL. begin[count]:
 // columns of a part. No parts: zeros.

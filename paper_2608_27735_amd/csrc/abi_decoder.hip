@@ -73,6 +73,27 @@ int32_t check_saved(const void* by_gate, const void* by_up, const void* hidden) 
   return ABCD_OK;
 }
 
+int32_t check_index(int32_t bits, const void* index, int64_t n) {
+  REQUIRE(bits == 32 || bits == 64, "indexes of %d bits", bits);
+  if (n == 0) return ABCD_OK;
+  REQUIRE(index != nullptr, "index is NULL");
+  REQUIRE((reinterpret_cast<uintptr_t>(index) & (bits / 8 - 1)) == 0, "index is not aligned to its elements");
+  return ABCD_OK;
+}
+
+int32_t check_table_rows(int64_t n, int64_t m) {
+  REQUIRE(n >= 0 && n <= ABCD_MAX_GAUSSIANS, "n = %lld out of range", (long long)n);
+  REQUIRE(m >= 1 && m <= ABCD_MAX_GAUSSIANS, "a table of %lld rows", (long long)m);
+  return ABCD_OK;
+}
+
+int32_t check_ints(const char* name, const void* p, size_t align, int64_t n) {
+  if (n == 0) return ABCD_OK;
+  REQUIRE(p != nullptr && (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0, "%s must be non-NULL and %zu-byte aligned",
+          name, align);
+  return ABCD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -184,6 +205,75 @@ int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t
   TRY_STATUS(check_matrix("y", y, dtype, n, d, ldy, false));
   REQUIRE(p >= 0.0 && p <= 1.0, "p must be in [0, 1]");
   return launch_dropout(dtype, n, d, x, ldx, residual, ldr, y, ldy, p, seed, offset, stream);
+}
+
+int32_t abcd_embed(int32_t dtype, int64_t n, int64_t m, int64_t d, int32_t tdtype, const void* table, int64_t ldt,
+                   int32_t index_bits, const void* index, float scale, void* y, int64_t ldy, hipStream_t stream) {
+  TRY_STATUS(check_rows(dtype, n, d));
+  TRY_STATUS(check_table_rows(n, m));
+  TRY_STATUS(check_wdtype(dtype, tdtype));
+  TRY_STATUS(check_matrix("table", table, tdtype, m, d, ldt, false));
+  TRY_STATUS(check_index(index_bits, index, n));
+  TRY_STATUS(check_matrix("y", y, dtype, n, d, ldy, false));
+  return launch_embed(dtype, n, m, d, tdtype, table, ldt, index_bits, index, scale, y, ldy, stream);
+}
+
+int32_t abcd_embed_sort_workspace_size(int64_t n, int64_t m, size_t* bytes) {
+  TRY_STATUS(check_table_rows(n, m));
+  REQUIRE(bytes != nullptr, "bytes is NULL");
+  *bytes = embed_sort_workspace_bytes(n, m);
+  return ABCD_OK;
+}
+
+int32_t abcd_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* index, int32_t* order, int32_t* rows,
+                        int32_t* ranges, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  TRY_STATUS(check_table_rows(n, m));
+  TRY_STATUS(check_index(index_bits, index, n));
+  TRY_STATUS(check_ints("order", order, 4, n));
+  TRY_STATUS(check_ints("rows", rows, 4, n));
+  TRY_STATUS(check_ints("ranges", ranges, 8, m));
+  TRY_STATUS(check_workspace(workspace, ws_bytes, embed_sort_workspace_bytes(n, m)));
+  return launch_embed_sort(n, m, index_bits, index, order, rows, ranges, workspace, stream);
+}
+
+int32_t abcd_embed_bwd_workspace_size(int64_t n, int64_t d, size_t* bytes) {
+  TRY_STATUS(check_rows(ABCD_F32, n, d));
+  REQUIRE(bytes != nullptr, "bytes is NULL");
+  *bytes = embed_bwd_workspace_bytes(n, d);
+  return ABCD_OK;
+}
+
+int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy, int64_t lddy,
+                       const int32_t* order, const int32_t* rows, const int32_t* ranges, float scale, int32_t wdtype,
+                       void* dtable, int64_t ldt, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  TRY_STATUS(check_rows(dtype, n, d));
+  TRY_STATUS(check_table_rows(n, m));
+  TRY_STATUS(check_matrix("dy", dy, dtype, n, d, lddy, false));
+  TRY_STATUS(check_ints("order", order, 4, n));
+  TRY_STATUS(check_ints("rows", rows, 4, n));
+  TRY_STATUS(check_ints("ranges", ranges, 8, m));
+  TRY_STATUS(check_wdtype(dtype, wdtype));
+  TRY_STATUS(check_matrix("dtable", dtable, wdtype, m, d, ldt, false));
+  TRY_STATUS(check_workspace(workspace, ws_bytes, embed_bwd_workspace_bytes(n, d)));
+  return launch_embed_bwd(dtype, n, m, d, dy, lddy, order, rows, ranges, scale, wdtype, dtable, ldt, workspace, stream);
+}
+
+int32_t abcd_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx, int8_t* q, uint8_t* e,
+                   hipStream_t stream) {
+  TRY_STATUS(check_rows(dtype, n, d));
+  TRY_STATUS(check_matrix("x", x, dtype, n, d, ldx, false));
+  TRY_STATUS(check_ints("q", q, 16, n));
+  TRY_STATUS(check_ints("e", e, 1, n));
+  return launch_pack8(dtype, n, d, x, ldx, q, e, stream);
+}
+
+int32_t abcd_unpack8(int32_t dtype, int64_t n, int64_t d, const int8_t* q, const uint8_t* e, void* y, int64_t ldy,
+                     hipStream_t stream) {
+  TRY_STATUS(check_rows(dtype, n, d));
+  TRY_STATUS(check_ints("q", q, 16, n));
+  TRY_STATUS(check_ints("e", e, 1, n));
+  TRY_STATUS(check_matrix("y", y, dtype, n, d, ldy, false));
+  return launch_unpack8(dtype, n, d, q, e, y, ldy, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,496 @@
+// embed.hip -- rows of a table by index, scaled, and the table's gradient by sorted
+// indexes.
+//
+// y[i] = scale table[index[i]]; dtable[r] = scale times the sum of dy[i] over the i whose
+// index is r, in the order of i. An index outside the table gives a row of zeros and has
+// no gradient.
+//
+// The sort: positions by index, equal ones in order (stable, least digit first), with
+// counts of every digit by parts of kSortPart keys, their prefix sums, and a scatter whose
+// ranks come from ballots: three launches for each digit of up to kSortBits bits, and no
+// atomics on memory. ranges[r] is where row r's positions begin and end in that order.
+//
+// The gradient: rows of up to kRun positions are added up by the lanes that write them;
+// of longer ones (a feature that thousands share, a frequent token) every chunk of kRun
+// positions in order gives a partial sum in fp32, and a workgroup for each such row adds
+// these. Either way the order of the sums is fixed by the indexes alone.
+#include <algorithm>
+
+#include "load_frag.h"
+
+namespace abcd {
+namespace {
+
+constexpr int kSortItems = 16, kSortPart = kBlock * kSortItems, kSortBits = 10;
+constexpr int kRun = 64;
+
+// ------------------------------------------------------------------ lookup
+
+struct EmbedArgs {
+  const void* table;
+  const void* index;
+  void* y;
+  int64_t ldt, ldy, n, m;
+  int d, lanes;  // lanes: threads along a row, a power of two up to kBlock
+  int tf32;
+  float scale;
+};
+
+template <typename T, typename I, bool kWhole>
+__global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a) {
+  constexpr int N = kPer16<T>, kAhead = 4;
+  const int t = threadIdx.x & (a.lanes - 1), rows = kBlock / a.lanes;
+  const int64_t step = (int64_t)gridDim.x * rows;
+  for (int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / a.lanes; row < a.n; row += kAhead * step) {
+    int64_t from[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t r = row + u * step;
+      const int64_t i = r < a.n ? (int64_t)static_cast<const I*>(a.index)[r] : -1;
+      from[u] = i >= 0 && i < a.m ? i : -1;
+    }
+    for (int c = t * N; c < a.d; c += a.lanes * N) {
+      Floats<N> v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        v[u] = 0.0f;
+        if (from[u] >= 0) v[u] = load_param<T, N, kWhole>(a.table, from[u] * a.ldt + c, a.d - c, a.tf32);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int64_t r = row + u * step;
+        if (r < a.n) store_vec<T, N, kWhole>(static_cast<T*>(a.y) + r * a.ldy + c, v[u] * a.scale, a.d - c);
+      }
+    }
+  }
+}
+
+// -------------------------------------------------------------------- sort
+
+struct SortArgs {
+  const void* index;
+  const uint32_t *keys_in, *vals_in;
+  uint32_t *keys_out, *vals_out;
+  uint32_t* counts;  // [digit][part]: how many; from the scan on, how many before
+  uint32_t* totals;  // [digit]
+  int2* ranges;
+  int64_t n;
+  int32_t m;
+  int parts, shift, bits;
+};
+
+// Key i: its row, those outside the table behind all rows.
+template <typename I>
+__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i) {
+  if (a.keys_in) return a.keys_in[i];
+  const int64_t k = (int64_t)static_cast<const I*>(a.index)[i];
+  return (uint32_t)(k >= 0 && k < a.m ? k : a.m);
+}
+
+// Counts of a part's digits; with the first digit, rows without positions are marked too.
+template <typename I>
+__global__ __launch_bounds__(kBlock) void embed_count_kernel(SortArgs a) {
+  __shared__ uint32_t count[1 << kSortBits];
+  const int digits = 1 << a.bits;
+  if (!a.keys_in)
+    for (int64_t r = (int64_t)blockIdx.x * kBlock + threadIdx.x; r < a.m; r += (int64_t)gridDim.x * kBlock)
+      a.ranges[r] = make_int2(0, 0);
+  if ((int)blockIdx.x >= a.parts) return;
+  for (int i = threadIdx.x; i < digits; i += kBlock) count[i] = 0;
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * kSortPart;
+#pragma unroll 4
+  for (int k = 0; k < kSortItems; ++k) {
+    const int64_t i = first + k * kBlock + threadIdx.x;
+    if (i < a.n) atomicAdd(&count[(sort_key<I>(a, i) >> a.shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < digits; i += kBlock) a.counts[(int64_t)i * a.parts + blockIdx.x] = count[i];
+}
+
+// Sum over the lanes before this one; total: over all.
+__device__ __forceinline__ uint32_t wave_before(uint32_t v, uint32_t& total) {
+  uint32_t s = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t u = (uint32_t)__shfl_up((int)s, d, 64);
+    if ((int)(threadIdx.x & 63) >= d) s += u;
+  }
+  total = (uint32_t)__shfl((int)s, 63, 64);
+  return s - v;
+}
+
+// A wave for each digit: its counts become the counts before each part.
+__global__ __launch_bounds__(kWave) void embed_scan_kernel(SortArgs a) {
+  uint32_t* const c = a.counts + (int64_t)blockIdx.x * a.parts;
+  uint32_t before = 0;
+  for (int p = 0; p < a.parts; p += kWave) {
+    const int i = p + (int)threadIdx.x;
+    uint32_t all;
+    const uint32_t own = i < a.parts ? c[i] : 0, at = wave_before(own, all);
+    if (i < a.parts) c[i] = before + at;
+    before += all;
+  }
+  if (threadIdx.x == 0) a.totals[blockIdx.x] = before;
+}
+
+// Every wave ranks its quarter of the part in order, 64 keys at a time: lanes with the
+// same digit find each other by ballots.
+template <typename I>
+__global__ __launch_bounds__(kBlock) void embed_scatter_kernel(SortArgs a) {
+  constexpr int kWaves = kBlock / kWave, kTurns = kSortPart / kBlock;
+  __shared__ uint32_t at[kWaves][1 << kSortBits];  // by wave: counts, then next places
+  __shared__ uint32_t sums[kWaves];
+  const int digits = 1 << a.bits, w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+  for (int i = threadIdx.x; i < kWaves << kSortBits; i += kBlock) (&at[0][0])[i] = 0;
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * kSortPart + w * (kSortPart / kWaves) + l;
+  uint32_t key[kTurns], place[kTurns];
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) key[k] = first + k * kWave < a.n ? sort_key<I>(a, first + k * kWave) : 0u;
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    const bool in = first + k * kWave < a.n;
+    const uint32_t d = (key[k] >> a.shift) & (uint32_t)(digits - 1);
+    uint64_t same = __ballot(in);
+    for (int b = 0; b < a.bits; ++b) {
+      const uint64_t set = __ballot((d >> b) & 1u);
+      same &= (d >> b) & 1u ? set : ~set;
+    }
+    const uint32_t before = (uint32_t)__popcll(same & ((1ull << l) - 1ull));
+    uint32_t start = 0;
+    const int leader = in ? __ffsll((unsigned long long)same) - 1 : l;
+    if (in && l == leader) start = atomicAdd(&at[w][d], (uint32_t)__popcll(same));
+    place[k] = (uint32_t)__shfl((int)start, leader, 64) + before;
+  }
+  __syncthreads();
+  // where each wave's keys of a digit go: behind all smaller digits, the parts before
+  // this one and the waves before this one
+  uint32_t run = 0;
+  for (int i0 = 0; i0 < digits; i0 += kBlock) {
+    const int i = i0 + (int)threadIdx.x;
+    uint32_t all;
+    const uint32_t own = i < digits ? a.totals[i] : 0;
+    uint32_t before = wave_before(own, all);
+    if (l == 0) sums[w] = all;
+    __syncthreads();
+    for (int v = 0; v < kWaves; ++v) {
+      if (v < w) before += sums[v];
+    }
+    const uint32_t round = sums[0] + sums[1] + sums[2] + sums[3];
+    if (i < digits) {
+      uint32_t next = run + before + a.counts[(int64_t)i * a.parts + blockIdx.x];
+      for (int v = 0; v < kWaves; ++v) {
+        const uint32_t c = at[v][i];
+        at[v][i] = next;
+        next += c;
+      }
+    }
+    run += round;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    const int64_t i = first + k * kWave;
+    if (i >= a.n) continue;
+    const uint32_t to = at[w][(key[k] >> a.shift) & (uint32_t)(digits - 1)] + place[k];
+    a.keys_out[to] = key[k];
+    a.vals_out[to] = a.vals_in ? a.vals_in[i] : (uint32_t)i;
+  }
+}
+
+__global__ __launch_bounds__(kBlock) void embed_ranges_kernel(SortArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (i >= a.n) return;
+  const uint32_t k = a.keys_in[i];
+  if (k >= (uint32_t)a.m) return;
+  if (i == 0 || a.keys_in[i - 1] != k) a.ranges[k].x = (int)i;
+  if (i == a.n - 1 || a.keys_in[i + 1] != k) a.ranges[k].y = (int)(i + 1);
+}
+
+// ---------------------------------------------------------------- gradient
+
+struct EmbedBwdArgs {
+  const void* dy;
+  const int32_t* order;
+  const int32_t* rows;  // of the sorted positions
+  const int2* ranges;
+  void* dtable;
+  float* part;       // [chunk][2][pitch]: of the long row that reaches into a chunk, and of the one that begins there
+  int* owners;       // how many long rows there are, then in which chunk each begins
+  int64_t lddy, ldt, n, m, pitch;
+  int d, lanes, row_blocks;
+  int wf32;
+  float scale;
+};
+
+template <typename T, int N, bool kWhole>
+__device__ __forceinline__ void put_row(const EmbedBwdArgs& a, int64_t r, int c, Floats<N> v) {
+  v *= a.scale;
+  if (a.wf32)
+    store_vec<float, N, kWhole>(static_cast<float*>(a.dtable) + r * a.ldt + c, v, a.d - c);
+  else
+    store_vec<T, N, kWhole>(static_cast<T*>(a.dtable) + r * a.ldt + c, v, a.d - c);
+}
+
+// The sum of columns c.. of dy over positions [from, to) of the order.
+template <typename T, int N, bool kWhole>
+__device__ __forceinline__ Floats<N> sum_run(const EmbedBwdArgs& a, int from, int to, int c) {
+  constexpr int kAhead = 8;
+  Floats<N> s = 0.0f;
+  for (int p = from; p < to; p += kAhead) {
+    typename Frag<T>::type v[kAhead];
+    int64_t at[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) at[u] = a.order[p + u < to ? p + u : from];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int left = p + u < to ? a.d - c : 0;
+      v[u] = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + at[u] * a.lddy + c, left,
+                                  room_of(a.n, at[u], a.lddy, left));
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      s += __builtin_convertvector((first_of<T, kWhole>(v[u], p + u < to ? a.d - c : 0)), Floats<N>);
+  }
+  return s;
+}
+
+__global__ void embed_none_kernel(int* owners) { owners[0] = 0; }
+
+// Workgroups below row_blocks: rows of the table with up to kRun positions. The others:
+// chunks of the order, of which they take what belongs to longer rows. blockIdx.y: blocks
+// of kBlock vectors of columns at most.
+template <typename T, bool kWhole>
+__global__ __launch_bounds__(kBlock) void embed_bwd_kernel(EmbedBwdArgs a) {
+  constexpr int N = kPer16<T>;
+  const int rows = kBlock / a.lanes, c = ((int)blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1))) * N;
+  if (c >= a.d) return;
+  if ((int)blockIdx.x < a.row_blocks) {
+    const int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / a.lanes;
+    if (r >= a.m) return;
+    const int2 at = a.ranges[r];
+    if (at.y - at.x > kRun) return;
+    put_row<T, N, kWhole>(a, r, c, sum_run<T, N, kWhole>(a, at.x, at.y, c));
+    return;
+  }
+  const int64_t chunk = (int64_t)((int)blockIdx.x - a.row_blocks) * rows + threadIdx.x / a.lanes, begin = chunk * kRun;
+  if (begin >= a.n) return;
+  const int64_t end = begin + kRun < a.n ? begin + kRun : a.n;
+  // a row of more than kRun positions that has any here has the first or the last one
+  const int first_row = a.rows[begin], last_row = a.rows[end - 1];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int r = k == 0 ? first_row : last_row;
+    if (r >= a.m || (k == 1 && last_row == first_row)) continue;
+    const int2 at = a.ranges[r];
+    if (at.y - at.x <= kRun) continue;
+    const int which = at.x >= begin ? 1 : 0;
+    const Floats<N> s = sum_run<T, N, kWhole>(a, max(at.x, (int)begin), min(at.y, (int)end), c);
+    store_vec<float, N, true>(a.part + (chunk * 2 + which) * a.pitch + c, s, N);
+    if (which == 1 && c == 0) a.owners[1 + atomicAdd(a.owners, 1)] = (int)chunk;
+  }
+}
+
+constexpr int kJoinWaves = 16;
+
+// Rows of more than kRun positions: 64 columns a workgroup, the chunks dealt to its
+// waves. (Which workgroup takes which row depends on the order of the atomics above; the sums do not.)
+template <typename T>
+__global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedBwdArgs a) {
+  __shared__ float red[kJoinWaves][kWave];
+  const int w = threadIdx.x / kWave, l = threadIdx.x % kWave, c = (int)blockIdx.y * kWave + l;
+  const int count = a.owners[0];
+  for (int i = blockIdx.x; i < count; i += gridDim.x) {
+    const int64_t first = a.owners[1 + i];
+    // the row that begins in this chunk and goes on behind it has the chunk's last position
+    const int64_t end = (first + 1) * kRun < a.n ? (first + 1) * kRun : a.n;
+    const int r = a.rows[end - 1];
+    const int64_t last = (a.ranges[r].y - 1) / kRun;
+    float s = 0.0f;
+    if (c < a.d) {
+      if (w == 0) s = a.part[(first * 2 + 1) * a.pitch + c];
+      int64_t k = first + 1 + w;
+      for (; k + 7 * kJoinWaves <= last; k += 8 * kJoinWaves) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = a.part[(k + u * kJoinWaves) * 2 * a.pitch + c];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += v[u];
+      }
+      for (; k <= last; k += kJoinWaves) s += a.part[k * 2 * a.pitch + c];
+    }
+    red[w][l] = s;
+    __syncthreads();
+    if (w == 0 && c < a.d) {
+      for (int v = 1; v < kJoinWaves; ++v) s += red[v][l];
+      put_row<T, 1, true>(a, r, c, Floats<1>(s));
+    }
+    __syncthreads();
+  }
+}
+
+// --------------------------------------------------------------- launching
+
+int bits_of(int64_t v) {
+  int b = 1;
+  while (v >> b) ++b;
+  return b;
+}
+
+// Hands out a workspace in 256-byte pieces; with no base it only adds up.
+struct Pieces {
+  char* base;
+  size_t used = 0;
+  void* take(size_t bytes) {
+    char* p = base ? base + used : nullptr;
+    used += align256(bytes);
+    return p;
+  }
+};
+
+struct SortScratch {
+  uint32_t *keys, *vals, *counts, *totals;
+  size_t bytes;
+  int passes, bits;
+  int64_t parts;
+};
+SortScratch sort_layout(int64_t n, int64_t m, void* workspace) {
+  SortScratch s{};
+  const int bits = bits_of(m);
+  s.passes = (bits + kSortBits - 1) / kSortBits;
+  s.bits = (bits + s.passes - 1) / s.passes;
+  s.parts = (n + kSortPart - 1) / kSortPart;
+  Pieces p{static_cast<char*>(workspace)};
+  s.keys = static_cast<uint32_t*>(p.take(n * sizeof(uint32_t)));
+  s.vals = static_cast<uint32_t*>(p.take(n * sizeof(uint32_t)));
+  s.counts = static_cast<uint32_t*>(p.take(((size_t)s.parts << s.bits) * sizeof(uint32_t)));
+  s.totals = static_cast<uint32_t*>(p.take(sizeof(uint32_t) << s.bits));
+  s.bytes = p.used;
+  return s;
+}
+
+int64_t embed_chunks(int64_t n) { return (n + kRun - 1) / kRun; }
+int64_t embed_pitch(int64_t d) { return (d + 7) & ~int64_t(7); }
+
+// Calls f with a value of the index type.
+template <typename F>
+int32_t with_index(int32_t bits, F f) {
+  return bits == 64 ? f(int64_t(0)) : f(int32_t(0));
+}
+
+// Threads along a row of nvec vectors.
+int embed_lanes(int nvec) {
+  int l = 1;
+  while (l < kWave && l < nvec) l *= 2;
+  return l;
+}
+
+}  // namespace
+
+int32_t launch_embed(int32_t dtype, int64_t n, int64_t m, int64_t d, int32_t tdtype, const void* table, int64_t ldt,
+                     int32_t index_bits, const void* index, float scale, void* y, int64_t ldy, hipStream_t stream) {
+  if (n == 0) return ABCD_OK;
+  EmbedArgs a{table, index, y, ldt, ldy, n, m, (int)d, 0, tdtype == ABCD_F32 && dtype != ABCD_F32, scale};
+  return with_type(dtype, [&](auto z) -> int32_t {
+    return with_index(index_bits, [&](auto zi) -> int32_t {
+      typedef decltype(z) T;
+      typedef decltype(zi) I;
+      a.lanes = embed_lanes((int)((d + kPer16<T> - 1) / kPer16<T>));
+      const int64_t rows = kBlock / a.lanes, blocks = std::min<int64_t>((n + 4 * rows - 1) / (4 * rows), 1 << 20);
+      if (d % kPer16<T> == 0)
+        ABCD_LAUNCH("embed", (embed_kernel<T, I, true>), blocks, kBlock, 0, stream, a);
+      else
+        ABCD_LAUNCH("embed", (embed_kernel<T, I, false>), blocks, kBlock, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      return ABCD_OK;
+    });
+  });
+}
+
+size_t embed_sort_workspace_bytes(int64_t n, int64_t m) { return std::max<size_t>(256, sort_layout(n, m, nullptr).bytes); }
+
+int32_t launch_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* index, int32_t* order, int32_t* rows,
+                          int32_t* ranges, void* workspace, hipStream_t stream) {
+  const SortScratch s = sort_layout(n, m, workspace);
+  SortArgs a{};
+  a.index = index;
+  a.counts = s.counts;
+  a.totals = s.totals;
+  a.ranges = reinterpret_cast<int2*>(ranges);
+  a.n = n;
+  a.m = (int32_t)m;
+  a.parts = (int)s.parts;
+  a.bits = s.bits;
+  return with_index(index_bits, [&](auto zi) -> int32_t {
+    typedef decltype(zi) I;
+    // of no positions only the rows' ranges are written
+    for (int pass = 0; pass < (n > 0 ? s.passes : 1); ++pass) {
+      // two places take turns so that the last pass writes the result
+      const bool own = (s.passes - 1 - pass) & 1;
+      a.shift = pass * s.bits;
+      a.keys_in = pass == 0 ? nullptr : a.keys_out;
+      a.vals_in = pass == 0 ? nullptr : a.vals_out;
+      a.keys_out = own ? s.keys : reinterpret_cast<uint32_t*>(rows);
+      a.vals_out = own ? s.vals : reinterpret_cast<uint32_t*>(order);
+      const int64_t zero = pass == 0 ? std::min<int64_t>((m + kBlock - 1) / kBlock, 2048) : 0;
+      ABCD_LAUNCH("embed_count", (embed_count_kernel<I>), std::max<int64_t>(s.parts, zero), kBlock, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      if (n == 0) return ABCD_OK;
+      ABCD_LAUNCH("embed_scan", embed_scan_kernel, 1 << s.bits, kWave, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      ABCD_LAUNCH("embed_scatter", (embed_scatter_kernel<I>), s.parts, kBlock, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      if (pass == s.passes - 1) {
+        a.keys_in = a.keys_out;
+        ABCD_LAUNCH("embed_ranges", embed_ranges_kernel, (n + kBlock - 1) / kBlock, kBlock, 0, stream, a);
+        ABCD_HIP(hipGetLastError());
+      }
+    }
+    return ABCD_OK;
+  });
+}
+
+size_t embed_bwd_workspace_bytes(int64_t n, int64_t d) {
+  Pieces p{nullptr};
+  p.take((size_t)embed_chunks(n) * 2 * embed_pitch(d) * sizeof(float));
+  p.take((1 + (size_t)embed_chunks(n)) * sizeof(int));
+  return p.used;
+}
+
+int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy, int64_t lddy,
+                         const int32_t* order, const int32_t* rows_of, const int32_t* ranges, float scale, int32_t wdtype, void* dtable, int64_t ldt, void* workspace, hipStream_t stream) {
+  if (m == 0) return ABCD_OK;
+  Pieces p{static_cast<char*>(workspace)};
+  const int64_t pitch = embed_pitch(d), chunks = embed_chunks(n);
+  float* const part = static_cast<float*>(p.take((size_t)chunks * 2 * pitch * sizeof(float)));
+  int* const owners = static_cast<int*>(p.take((1 + (size_t)chunks) * sizeof(int)));
+  EmbedBwdArgs a{dy, order, rows_of, reinterpret_cast<const int2*>(ranges), dtable, part, owners, lddy, ldt, n, m, pitch,
+                 (int)d, 0, 0, wdtype == ABCD_F32 && dtype != ABCD_F32, scale};
+  return with_type(dtype, [&](auto z) -> int32_t {
+    typedef decltype(z) T;
+    const int nvec = (int)((d + kPer16<T> - 1) / kPer16<T>);
+    a.lanes = embed_lanes(nvec);
+    const int64_t rows = kBlock / a.lanes;
+    a.row_blocks = (int)((m + rows - 1) / rows);
+    const int64_t blocks = a.row_blocks + (chunks + rows - 1) / rows;
+    REQUIRE(blocks < (int64_t(1) << 31), "too many rows");
+    ABCD_LAUNCH("embed_none", embed_none_kernel, 1, 1, 0, stream, owners);
+    ABCD_HIP(hipGetLastError());
+    const dim3 grid(blocks, (nvec + a.lanes - 1) / a.lanes);
+    if (d % kPer16<T> == 0)
+      ABCD_LAUNCH("embed_bwd", (embed_bwd_kernel<T, true>), grid, kBlock, 0, stream, a);
+    else
+      ABCD_LAUNCH("embed_bwd", (embed_bwd_kernel<T, false>), grid, kBlock, 0, stream, a);
+    ABCD_HIP(hipGetLastError());
+    if (n > kRun) {
+      const int64_t most = std::min<int64_t>(chunks, 256);
+      ABCD_LAUNCH("embed_join", (embed_join_kernel<T>), dim3(most, (d + kWave - 1) / kWave), kJoinWaves * kWave, 0, stream,
+                  a);
+      ABCD_HIP(hipGetLastError());
+    }
+    return ABCD_OK;
+  });
+}
+
+}  // namespace abcd

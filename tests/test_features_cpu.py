@@ -1,0 +1,101 @@
+"""The entry points of the operators around a decoder's blocks refuse bad
+arguments on the host, before any HIP call, and the float64 definitions of
+their tests agree with differences."""
+import ctypes as C
+import os
+
+import pytest
+import torch
+
+import decoder_ref as D
+import features_ref as R
+
+FAKE = 0x1000  # never dereferenced: every call below fails validation first
+F32, F16, BF16 = 0, 1, 2
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2608_27735_amd import _lib
+    if not os.path.exists(_lib.LIB_PATH):
+        from paper_2608_27735_amd import build
+        build.build()
+    return _lib.load()
+
+
+def refuse(base, call, cases):
+    for i, v in cases:
+        a = list(base)
+        a[i] = v
+        assert call(*a) == 1, (i, v)
+
+
+def test_embed_refuses(lib):
+    base = [F16, 4, 5, 8, F16, FAKE, 8, 32, FAKE, 1.0, FAKE, 8, None]
+    refuse(base, lib.abcd_embed,
+           [(0, 3), (1, -1), (1, (1 << 30) + 1), (2, 0), (2, (1 << 30) + 1), (3, 0), (3, 65537), (4, BF16),
+            (5, None), (5, FAKE + 1), (6, 7), (7, 16), (8, None), (8, FAKE + 2), (10, None), (10, FAKE + 1), (11, 7)])
+    base[7] = 64
+    refuse(base, lib.abcd_embed, [(8, FAKE + 4)])
+
+
+def test_embed_sort_refuses(lib):
+    need = C.c_size_t(0)
+    assert lib.abcd_embed_sort_workspace_size(4, 5, C.byref(need)) == 0 and need.value >= 4 * 4 * 2
+    refuse([4, 5, C.byref(need)], lib.abcd_embed_sort_workspace_size, [(0, -1), (1, 0), (1, (1 << 30) + 1), (2, None)])
+    base = [4, 5, 32, FAKE, FAKE, FAKE, FAKE, FAKE, need.value, None]
+    refuse(base, lib.abcd_embed_sort,
+           [(0, -1), (1, 0), (2, 8), (3, None), (3, FAKE + 2), (4, None), (4, FAKE + 2), (5, None), (5, FAKE + 2),
+            (6, None), (6, FAKE + 4), (7, None), (7, FAKE + 16), (8, need.value - 1)])
+
+
+def test_embed_bwd_refuses(lib):
+    need = C.c_size_t(0)
+    assert lib.abcd_embed_bwd_workspace_size(4, 8, C.byref(need)) == 0 and need.value >= 2 * 8 * 4
+    refuse([4, 8, C.byref(need)], lib.abcd_embed_bwd_workspace_size, [(0, -1), (1, 0), (1, 65537), (2, None)])
+    base = [BF16, 4, 5, 8, FAKE, 8, FAKE, FAKE, FAKE, 1.0, F32, FAKE, 8, FAKE, need.value, None]
+    refuse(base, lib.abcd_embed_bwd,
+           [(0, 7), (1, -1), (2, 0), (3, 0), (4, None), (4, FAKE + 1), (5, 7), (6, None), (6, FAKE + 1), (7, None),
+            (8, None), (8, FAKE + 4), (10, F16), (11, None), (11, FAKE + 2), (12, 7), (13, None), (13, FAKE + 8),
+            (14, need.value - 1)])
+
+
+def test_pack8_refuses(lib):
+    base = [F16, 4, 8, FAKE, 8, FAKE, FAKE, None]
+    refuse(base, lib.abcd_pack8, [(0, 3), (1, -1), (2, 0), (2, 65537), (3, None), (3, FAKE + 1), (4, 7), (5, None),
+                                  (5, FAKE + 8), (6, None)])
+    base = [F32, 4, 8, FAKE, FAKE, FAKE, 8, None]
+    refuse(base, lib.abcd_unpack8, [(0, 3), (1, -1), (2, 0), (3, None), (3, FAKE + 8), (4, None), (5, None),
+                                    (5, FAKE + 2), (6, 7)])
+
+
+def test_python_refuses_what_is_not_on_the_gpu():
+    from paper_2608_27735_amd import api
+    x, i = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: api.embed(x, i), lambda: api.embed_sort(i, 4), lambda: api.embed_bwd(x, i, 4),
+                 lambda: api.embed_sort(i, 0), lambda: api.pack8(x),
+                 lambda: api.unpack8(api.Packed8(torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8),
+                                                 8, torch.float32))):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_reference_embed_gradient_is_its_forwards():
+    g = torch.Generator().manual_seed(0)
+    t = torch.randn(5, 3, generator=g, dtype=D.F64).requires_grad_()
+    dy = torch.randn(9, 3, generator=g, dtype=D.F64)
+    index = torch.tensor([0, 4, 4, -1, 2, 5, 0, 4, 2])
+    inside = (index >= 0) & (index < 5)
+    want, = torch.autograd.grad((t[index[inside]] * 1.5 * dy[inside]).sum(), t)
+    assert torch.allclose(R.embed_bwd(dy, index, 5, 1.5)[0], want, rtol=1e-12)
+    assert torch.allclose(R.embed(t.detach(), index, 1.5)[inside], t.detach()[index[inside]] * 1.5, rtol=1e-12)
+
+
+def test_reference_checkpoint_keeps_within_its_step():
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(7, 70, generator=g, dtype=D.F64) * torch.exp(3 * torch.randn(7, 70, generator=g, dtype=D.F64))
+    y, e = R.pack8(x)
+    top = torch.stack([x[:, b:b + 32].abs().amax(1) for b in (0, 32, 64)], 1)
+    err = torch.stack([(y - x)[:, b:b + 32].abs().amax(1) for b in (0, 32, 64)], 1)
+    assert (err <= top / 64).all() and (err <= 2.0 ** (e.to(D.F64) - 127 - 6)).all()
+    assert torch.equal(R.pack8(y)[0], y)  # what was kept once is kept

@@ -1,0 +1,223 @@
+"""Shared features and 8-bit checkpoints against float64 definitions, at the
+sizes, indexes, strides and values where they can go wrong. A lookup is one
+product in fp32 and one rounding; a gradient is a sum in fp32 of up to 64 terms
+one after the other, of partial sums in the order of their chunks, and one
+product; a checkpoint holds exactly what its definition says."""
+import math
+
+import pytest
+import torch
+
+import decoder_ref as D
+import features_ref as R
+
+pytestmark = pytest.mark.gpu
+
+DT = [torch.float32, torch.float16, torch.bfloat16]
+IDS = ["f32", "f16", "bf16"]
+
+
+def say(*a):
+    print("[case]", *a, flush=True)
+
+
+@pytest.fixture(scope="module")
+def api():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2608_27735_amd import api
+    return api
+
+
+def rand(seed, n, d, dtype, pad=0, skip=0, scale=1.0, shift=0.0):
+    """An n x d matrix on the GPU, `pad` elements between its rows, `skip`
+    elements into its allocation; NaN around it."""
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(n, d, generator=g) * scale + shift).to(dtype)
+    buf = torch.full((skip + n * (d + pad),), float("nan"), dtype=dtype, device="cuda")
+    v = buf[skip:].view(n, d + pad)[:, :d]
+    v.copy_(x)
+    return v
+
+
+def indices(seed, n, m, how):
+    g = torch.Generator().manual_seed(seed)
+    if how == "one":
+        return torch.full((n,), m // 2, dtype=torch.int64)
+    if how == "none":
+        return torch.randint(0, 2, (n,), generator=g) * (m + 7) - 3  # -3 or m + 4: outside
+    i = torch.randint(0, m, (n,), generator=g)
+    if how == "hot":  # one row has a third of all, and some places are empty
+        i[torch.rand(n, generator=g) < 0.33] = m - 1
+        i[torch.rand(n, generator=g) < 0.1] = -1
+        i[torch.rand(n, generator=g) < 0.05] = m
+    if how == "runs":
+        i = i.sort()[0]
+    return i
+
+
+SHAPES = [(1, 1, 1), (1, 7, 64), (5, 3, 7), (63, 64, 16), (64, 1, 8), (65, 2, 129), (129, 40, 59), (700, 1023, 33),
+          (1000, 1024, 64), (4097, 5, 100), (3000, 70000, 5), (900, 300, 2053)]
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,m,d", SHAPES)
+def test_embed_both_ways(api, dtype, n, m, d):
+    for k, how in enumerate(("uniform", "hot", "runs", "one", "none")):
+        wide, pad, skip = k % 2 == 0, (0, 3, 0, 1, 5)[k], (0, 1, 3, 0, 0)[k]
+        tdtype = torch.float32 if k in (1, 2) else dtype
+        scale = (1.0, math.sqrt(d), -0.25, 3.0, 1.0)[k]
+        say("embed", dtype, n, m, d, how, wide, pad, skip, tdtype)
+        index = indices(n + k, n, m, how)
+        gi = (index if wide else index.int()).cuda()
+        table = rand(1, m, d, tdtype, pad, skip)
+        y = api.embed(table, gi, scale, dtype=dtype)
+        s32 = float(torch.tensor(scale, dtype=torch.float32))
+        want = R.embed(D.d64(table), index, s32)
+        assert y.dtype == dtype and y.shape == (n, d)
+        D.close("y", y, want, want.abs(), k=1.0)
+        dy = rand(2, n, d, dtype, pad, skip)
+        ref, mag = R.embed_bwd(D.d64(dy), index, m, s32)
+        # at most 64 sums in order, n / 64 / 16 partial ones a wave, 16 waves and the product
+        terms = 64.0 + n / 1024 + 18
+        got = api.embed_bwd(dy, gi, m, scale, wdtype=tdtype)
+        assert got.dtype == tdtype and got.shape == (m, d)
+        D.close("dtable", got, ref, mag, k=terms)
+        kept = api.embed_sort(gi, m)
+        for _ in range(2):  # the same result again, from the same plan
+            assert torch.equal(api.embed_bwd(dy, kept, m, scale, wdtype=tdtype), got)
+        out = rand(3, m, d, tdtype, 3, 1)
+        assert api.embed_bwd(dy, kept, m, scale, out=out) is out and torch.equal(out, got)
+
+
+@pytest.mark.parametrize("n,m", [(1, 1), (4096, 1), (4097, 1023), (5000, 1024), (70000, 99), (20000, 1048576),
+                                 (300000, 3000000)])
+def test_sorted_positions(api, n, m):
+    for how in ("uniform", "hot", "none"):
+        say("embed_sort", n, m, how)
+        index = indices(n, n, m, how)
+        s = api.embed_sort(index.cuda(), m)
+        key = torch.where((index >= 0) & (index < m), index, torch.tensor(m))
+        rows, order = key.sort(stable=True)
+        assert torch.equal(s.order.cpu().long(), order) and torch.equal(s.rows.cpu().long(), rows)
+        count = torch.bincount(rows, minlength=m + 1)[:m]
+        begin = torch.cumsum(count, 0) - count
+        want = torch.where(count > 0, begin, 0)
+        assert torch.equal(s.ranges[:, 0].cpu().long(), want) and torch.equal(s.ranges[:, 1].cpu().long(), want + count)
+
+
+def test_embed_of_no_positions(api):
+    table = rand(1, 4, 9, torch.float16)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert api.embed(table, none).shape == (0, 9)
+    g = api.embed_bwd(torch.zeros(0, 9, dtype=torch.float16, device="cuda"), none, 4)
+    assert g.shape == (4, 9) and (g == 0).all()
+
+
+def test_embed_keeps_infinities_to_their_rows(api):
+    """What one row's gradient holds reaches no other row, nor does a row that no place names."""
+    dy = torch.ones(200, 40, device="cuda")
+    index = (torch.arange(200) % 3).cuda()
+    dy[4], dy[199] = math.inf, math.nan  # rows 1 and 1
+    index[199] = -1
+    got = api.embed_bwd(dy, index, 4)
+    assert (got[0] == 67).all() and (got[1] == math.inf).all() and (got[2] == 66).all() and (got[3] == 0).all()
+    table = torch.full((3, 40), math.nan, device="cuda")
+    table[1] = 2.0
+    assert (api.embed(table, torch.tensor([1, -1, 3, 1], device="cuda")) ==
+            torch.tensor([2.0, 0, 0, 2.0], device="cuda")[:, None]).all()
+
+
+def test_embed_far_rows(api):
+    """Rows more than 2^31 elements apart, of table and gradient."""
+    ld, m = (1 << 30) + 16, 3
+    buf = torch.empty(2 * ld + 64, dtype=torch.bfloat16, device="cuda")
+    far = buf.as_strided((m, 64), (ld, 1))
+    far.copy_(rand(1, m, 64, torch.bfloat16))
+    index = torch.tensor([2, 0, 1, 2, 2], device="cuda")
+    assert torch.equal(api.embed(far, index), far[index])
+    dy = rand(2, 5, 64, torch.bfloat16)
+    want = api.embed_bwd(dy, index, m)
+    assert torch.equal(api.embed_bwd(dy, index, m, out=far), want)
+    dfar = buf.as_strided((3, 64), (ld, 1))
+    dfar.copy_(dy[:3])
+    assert torch.equal(api.embed_bwd(dfar, index[:3], m), api.embed_bwd(dy[:3].contiguous(), index[:3], m))
+
+
+def test_embed_refuses(api):
+    t, i = torch.zeros(4, 8, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    bad = [lambda: api.embed(t.double(), i), lambda: api.embed(t, i.float()), lambda: api.embed(t, i.cpu()),
+           lambda: api.embed(t, i[:, None]), lambda: api.embed(t, torch.zeros(6, dtype=torch.int64, device="cuda")[::2]),
+           lambda: api.embed(t[:0], i), lambda: api.embed(t.t(), i), lambda: api.embed(t.half(), i, dtype=torch.float32),
+           lambda: api.embed(t, i, out=torch.zeros(2, 8, device="cuda")),
+           lambda: api.embed(t, i, dtype=torch.float16, out=torch.zeros(3, 8, device="cuda")),
+           lambda: api.embed_sort(i, 0), lambda: api.embed_sort(i[:, None], 4),
+           lambda: api.embed_bwd(t, i, 4), lambda: api.embed_bwd(t[:3], api.embed_sort(i, 5), 4),
+           lambda: api.embed_bwd(t, api.embed_sort(i, 4), 4), lambda: api.embed_bwd(t[:3].half(), i, 4, wdtype=torch.bfloat16),
+           lambda: api.embed_bwd(t[:3], i, 4, out=torch.zeros(3, 8, device="cuda"))]
+    for k, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            print("accepted", k)
+    with pytest.raises(api.AbcdError):
+        api.embed_sort(i, 4, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+
+
+# ------------------------------------------------------------- checkpoints
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,d", [(1, 1), (3, 7), (37, 31), (5, 32), (70, 33), (9, 59), (300, 64), (4, 129), (3, 2048),
+                                 (2, 4100)])
+def test_checkpoint_holds_its_definition(api, dtype, n, d):
+    for pad, skip, spread in ((0, 0, 0.5), (3, 1, 6.0)):
+        say("pack8", dtype, n, d, pad, skip)
+        g = torch.Generator().manual_seed(n + d)
+        x = rand(n, n, d, dtype, pad, skip)
+        x.copy_((D.d64(x) * torch.exp(spread * torch.randn(n, d, generator=g, dtype=D.F64)).clamp(max=1e3)).to(dtype))
+        p = api.pack8(x)
+        want, e = R.pack8(D.d64(x))
+        assert p.shape == (n, d) and p.dtype == dtype
+        assert torch.equal(p.e.cpu(), e)
+        y = api.unpack8(p)
+        assert torch.equal(D.d64(y), want)
+        assert (p.q.view(n, -1)[:, d:] == 0).all()  # behind the row's end
+        again = api.pack8(y)
+        assert torch.equal(D.d64(api.unpack8(again)), want)
+        out = rand(1, n, d, dtype, 5, 1)
+        assert api.unpack8(api.pack8(x, out=p), out=out) is out and torch.equal(out, y)
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+def test_checkpoint_of_extremes(api, dtype):
+    """The type's largest, smallest and subnormal numbers, zeros, halves between two
+    steps, and infinities and NaN, which stay where they are."""
+    info = torch.finfo(dtype)
+    x = torch.zeros(9, 64, dtype=dtype)
+    x[0, :2] = torch.tensor([info.max, -info.max])
+    x[1, :2] = torch.tensor([info.tiny, -info.tiny / 2])
+    x[2, 5] = info.smallest_normal * info.eps
+    x[3] = torch.linspace(-2, 2, 64)
+    x[4] = torch.tensor([127.5, 126.5, 0.5, 1.5, 2.5, -0.5, -1.5, 64] * 8)
+    x[5, 3], x[5, 40], x[5, 41] = math.inf, -math.inf, 3.0
+    x[6] = math.nan
+    x[7, 0], x[7, 1] = info.max, info.tiny
+    x = x.cuda()
+    p = api.pack8(x)
+    want, e = R.pack8(D.d64(x))
+    assert torch.equal(p.e.cpu(), e)
+    y = D.d64(api.unpack8(p))
+    assert torch.equal(y.nan_to_num(-1e30), want.nan_to_num(-1e30)) and torch.equal(y.isnan(), want.isnan())
+
+
+def test_checkpoint_refuses(api):
+    x = torch.zeros(4, 40, device="cuda")
+    p = api.pack8(x)
+    bad = [lambda: api.pack8(x.double()), lambda: api.pack8(x[0]), lambda: api.pack8(x.t()),
+           lambda: api.pack8(x.half(), out=p), lambda: api.pack8(x[:3], out=p),
+           lambda: api.unpack8(p._replace(width=65)), lambda: api.unpack8(p._replace(width=32)),
+           lambda: api.unpack8(p._replace(q=p.q[:, :32])), lambda: api.unpack8(p._replace(e=p.e.cpu())),
+           lambda: api.unpack8(p._replace(dtype=torch.float64)), lambda: api.unpack8(p, out=x.half()),
+           lambda: api.unpack8(p, out=x[:, :39])]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    assert api.unpack8(api.pack8(x[:0])).shape == (0, 40)
