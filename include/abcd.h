@@ -543,6 +543,50 @@ ABCD_API int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, 
                                 const int32_t* ranges, float scale, int32_t wdtype, void* dtable,
                                 int64_t ldt, void* workspace, size_t ws_bytes, hipStream_t stream);
 
+/* The joint between two blocks: a block's result f, normed, gated and scaled, goes
+ * onto the residual path x, and the next block takes that normed:
+ *   t = post(f);  y = x + scale gate t;  z = pre(y)
+ * post and pre are each ABCD_NORM_NONE (t = f; no z), ABCD_NORM_LAYER, (v - mean) rstd
+ * weight + bias with mean and rstd as in abcd_layer_norm, or ABCD_NORM_RMS, v rstd weight
+ * with rstd = 1 / sqrt(mean(v^2) + eps). Weights, biases and scale (d elements of type
+ * wdtype: dtype or ABCD_F32) may be NULL, then 1 and 0; they go with the norm that has them
+ * (no bias with ABCD_NORM_RMS). gate: ABCD_GATE_NONE (1), ABCD_GATE_ROW, one number a row
+ * (row r's at gate + r ldg), or ABCD_GATE_ELEMENT, [n][d]; of dtype, taken as it is. */
+enum { ABCD_NORM_NONE = 0, ABCD_NORM_LAYER = 1, ABCD_NORM_RMS = 2 };
+enum { ABCD_GATE_NONE = 0, ABCD_GATE_ROW = 1, ABCD_GATE_ELEMENT = 2 };
+typedef struct abcd_joint {
+  int32_t dtype, wdtype;
+  int32_t post, pre, gate;
+  float eps;
+  int64_t d;
+  const void *post_weight, *post_bias, *pre_weight, *pre_bias, *scale;
+} abcd_joint;
+
+/* Forward. z is the norm of y before y is rounded; z is NULL if and only if pre is
+ * ABCD_NORM_NONE. The statistics (fp32, n each; means of layer norms only) may be NULL, then not
+ * written; the backward needs them. No output may overlap an input. */
+ABCD_API int32_t abcd_residual_norm(const abcd_joint* joint /* host */, int64_t n, const void* f,
+                                    int64_t ldf, const void* x, int64_t ldx, const void* gate,
+                                    int64_t ldg, void* y, int64_t ldy, void* z, int64_t ldz,
+                                    float* post_mean, float* post_rstd, float* pre_mean,
+                                    float* pre_rstd, hipStream_t stream);
+
+/* Backward, from the gradients dz of z (NULL if and only if there is no z) and dy that
+ * reaches y by other paths (NULL: none, with a z only); y and the statistics are the forward's:
+ * gradients of x, f, gate (laid out as the gate is) and of the parameters (sums over the
+ * rows, type wdtype), written, not added to; each may be NULL, then not computed, and is
+ * NULL where there is no such gate or norm (dscale may be given without a scale). workspace: at
+ * least abcd_residual_norm_bwd_workspace_size bytes, 256-byte aligned. No output may overlap an input. */
+ABCD_API int32_t abcd_residual_norm_bwd_workspace_size(const abcd_joint* joint /* host */,
+                                                       int64_t n, size_t* bytes);
+ABCD_API int32_t abcd_residual_norm_bwd(
+    const abcd_joint* joint /* host */, int64_t n, const void* dz, int64_t lddz, const void* dy,
+    int64_t lddy, const void* f, int64_t ldf, const void* y, int64_t ldy, const void* gate,
+    int64_t ldg, const float* post_mean, const float* post_rstd, const float* pre_mean,
+    const float* pre_rstd, void* dx, int64_t lddx, void* df, int64_t lddf, void* dgate, int64_t lddg,
+    void* dpost_weight, void* dpost_bias, void* dpre_weight, void* dpre_bias, void* dscale,
+    void* workspace, size_t ws_bytes, hipStream_t stream);
+
 /* Checkpoints of activations in 8 bits. Of every ABCD_PACK8_BLOCK consecutive elements
  * of a row (the last block may have fewer), with 2^e the largest power of two that does
  * not exceed the largest finite magnitude (e at least -120):
@@ -570,7 +614,7 @@ ABCD_API int32_t abcd_unpack8(int32_t dtype, int64_t n, int64_t d, const int8_t*
  * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
  * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out,
  * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_none, embed_bwd,
- * embed_join, pack8, unpack8). */
+ * embed_join, pack8, unpack8, residual_norm, residual_norm_bwd, residual_norm_sums). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

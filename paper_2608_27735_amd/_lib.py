@@ -50,10 +50,18 @@ class abcd_ffn(C.Structure):
                 ("offset", C.c_uint64)]
 
 
+class abcd_joint(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("wdtype", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32),
+                ("gate", C.c_int32), ("eps", C.c_float), ("d", C.c_int64), ("post_weight", C.c_void_p),
+                ("post_bias", C.c_void_p), ("pre_weight", C.c_void_p), ("pre_bias", C.c_void_p),
+                ("scale", C.c_void_p)]
+
+
 _P = C.c_void_p  # device pointers travel as integers
 _I32, _I64, _SZ = C.c_int32, C.c_int64, C.c_size_t
 _CAM, _PRM = C.POINTER(abcd_camera), C.POINTER(abcd_raster_params)
 _FFN = C.POINTER(abcd_ffn)
+_JOINT = C.POINTER(abcd_joint)
 
 # name -> (restype, argtypes); mirrors include/abcd.h
 SIGNATURES = {
@@ -95,6 +103,10 @@ SIGNATURES = {
     "abcd_embed_bwd_workspace_size": (_I32, [_I64, _I64, C.POINTER(_SZ)]),
     "abcd_embed_bwd": (_I32, [_I32, _I64, _I64, _I64, _P, _I64, _P, _P, _P, C.c_float, _I32, _P, _I64,
                               _P, _SZ, _P]),
+    "abcd_residual_norm": (_I32, [_JOINT, _I64] + [_P, _I64] * 5 + [_P] * 5),
+    "abcd_residual_norm_bwd_workspace_size": (_I32, [_JOINT, _I64, C.POINTER(_SZ)]),
+    "abcd_residual_norm_bwd": (_I32, [_JOINT, _I64] + [_P, _I64] * 5 + [_P] * 4 + [_P, _I64] * 3 + [_P] * 6 +
+                               [_SZ, _P]),
     "abcd_pack8": (_I32, [_I32, _I64, _I64, _P, _I64, _P, _P, _P]),
     "abcd_unpack8": (_I32, [_I32, _I64, _I64, _P, _P, _P, _I64, _P]),
     "abcd_last_error": (C.c_char_p, []),

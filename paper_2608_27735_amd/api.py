@@ -751,6 +751,128 @@ def embed_bwd(dy, index, m, scale=1.0, wdtype=None, out=None, workspace=None):
     return out
 
 
+# ------------------------------------------------- decoder: between two blocks
+
+_NORMS = {None: 0, "layer": 1, "rms": 2}  # ABCD_NORM_*
+JOINT_PARAMS = ("post_weight", "post_bias", "pre_weight", "pre_bias", "scale")
+JOINT_STATS = ("post_mean", "post_rstd", "pre_mean", "pre_rstd")
+
+
+def _joint(f, post, pre, params, gate, eps):
+    """The joint's description for the library, checked against f [n, d], and the
+    distances between f's and the gate's rows."""
+    code = _dtype_of(f, "f")
+    _here(f, "f")
+    ldf = _rows(f, "f")
+    (n, d), dev = f.shape, f.device
+    for k, v in (("post", post), ("pre", pre)):
+        if v not in _NORMS:
+            raise ValueError(f"{k} must be None, 'layer' or 'rms', got {v!r}")
+    params = params or {}
+    if not params.keys() <= set(JOINT_PARAMS):
+        raise ValueError(f"unknown parameters {sorted(params.keys() - set(JOINT_PARAMS))}")
+    given = [t for t in map(params.get, JOINT_PARAMS) if t is not None]
+    wdtype = _param_dtype(f, given[0], None) if given else f.dtype
+    ptrs = []
+    for k in JOINT_PARAMS:
+        t = params.get(k)
+        _vector(t, k, d, wdtype, dev)
+        kind = dict(post=post, pre=pre).get(k.split("_")[0], "layer")
+        if t is not None and (kind is None or (kind == "rms" and k.endswith("bias"))):
+            raise ValueError(f"{k} given, but no norm that has one")
+        ptrs.append(_ptr(t))
+    mode, ldg = 0, 0
+    if gate is not None:
+        if gate.dim() != 2 or gate.shape[0] != n or gate.shape[1] not in (1, d):
+            raise ValueError(f"gate has shape {tuple(gate.shape)}, expected ({n}, 1) or ({n}, {d})")
+        ldg = _rows(gate, "gate", f)
+        mode = 2 if gate.shape[1] == d else 1
+    j = _lib.abcd_joint(code, _DTYPES[wdtype], _NORMS[post], _NORMS[pre], mode, float(eps), d, *ptrs)
+    return j, wdtype, ldf, ldg
+
+
+def residual_norm(f, x, post=None, pre=None, params=None, gate=None, eps=1e-5, out=None, z=None):
+    """The joint between two blocks, of the first one's result f and the residual path x
+    [n, d]: y = x + scale gate post(f), z = pre(y). post and pre: "layer", "rms" or
+    None (post: f itself; pre: no z). params: dict of any of post_weight, post_bias, pre_weight,
+    pre_bias, scale, each [d], of f's type or float32 (a missing one is 1 or 0). gate:
+    [n, d], or [n, 1] for one number a row. Returns dict(y, z, post_mean, post_rstd, pre_mean,
+    pre_rstd): the norms' float32 statistics, None where there are none (an RMS norm has
+    no mean). out, z: tensors for y and z, which may not overlap an input."""
+    joint, _, ldf, ldg = _joint(f, post, pre, params, gate, eps)
+    size, dev = f.shape, f.device
+    n, d = size
+    ldx = _rows(x, "x", f, size)
+    y, ldy = (_new(f, size), d) if out is None else (out, _rows(out, "out", f, size))
+    ldz = 0
+    if pre is None:
+        if z is not None:
+            raise ValueError("z given, but no norm after the joint")
+    elif z is None:
+        z, ldz = _new(f, size), d
+    else:
+        ldz = _rows(z, "z", f, size)
+    names = [k for k, kind in zip(JOINT_STATS, (post, post, pre, pre))
+             if kind == "layer" or (kind == "rms" and k.endswith("rstd"))]
+    r = dict.fromkeys(JOINT_STATS)
+    if names:
+        r.update(zip(names, torch.empty((len(names), n), dtype=torch.float32, device=dev).unbind(0)))
+    check(_lib.load().abcd_residual_norm(
+        C.byref(joint), n, f.data_ptr(), ldf, x.data_ptr(), ldx, _ptr(gate), ldg, y.data_ptr(), ldy,
+        _ptr(z), ldz, *[_ptr(r[k]) for k in JOINT_STATS], _stream()))
+    r["y"], r["z"] = y, z
+    return r
+
+
+def residual_norm_bwd(dz, dy, f, kept, post=None, pre=None, params=None, gate=None, grads=None,
+                      workspace=None):
+    """Gradients of residual_norm from those of z (dz, None without a z) and of y by other
+    paths (dy, None for none): dict(x, f[, gate] and those of params). kept: the forward's
+    dict (its y and statistics are read). grads: a dict of tensors to write into, where a
+    missing one is left out; none may overlap an input."""
+    joint, wdtype, ldf, ldg = _joint(f, post, pre, params, gate, 0.0)
+    size, dev = f.shape, f.device
+    n, d = size
+    if (dz is None) != (pre is None):
+        raise ValueError("dz goes with a norm after the joint")
+    if dz is None and dy is None:
+        raise ValueError("dy is required without dz")
+    lddz = 0 if dz is None else _rows(dz, "dz", f, size)
+    lddy = 0 if dy is None else _rows(dy, "dy", f, size)
+    y = kept["y"] if pre is not None else None
+    ldy = 0 if y is None else _rows(y, "y", f, size)
+    for k, kind in zip(JOINT_STATS, (post, post, pre, pre)):
+        if kind == "layer" or (kind == "rms" and k.endswith("rstd")):
+            if kept[k] is None:
+                raise ValueError(f"{k} is required")
+            _vector(kept[k], k, n, torch.float32, dev)
+    if grads is None:
+        grads = dict(x=_new(f, size), f=_new(f, size))
+        if gate is not None:
+            grads["gate"] = torch.empty(gate.shape, dtype=f.dtype, device=dev)
+        for k, t in (params or {}).items():
+            if t is not None:
+                grads[k] = torch.empty_like(t)
+    else:
+        for k in JOINT_PARAMS:
+            _vector(grads.get(k), f"grads[{k}]", d, wdtype, dev)
+    dx, df, dg = grads.get("x"), grads.get("f"), grads.get("gate")
+    lddx = 0 if dx is None else _rows(dx, "grads[x]", f, size)
+    lddf = 0 if df is None else _rows(df, "grads[f]", f, size)
+    if dg is not None and gate is None:
+        raise ValueError("grads[gate] given, but no gate")
+    lddg = 0 if dg is None else _rows(dg, "grads[gate]", f, gate.shape)
+    lib = _lib.load()
+    sz = C.c_size_t(0)
+    check(lib.abcd_residual_norm_bwd_workspace_size(C.byref(joint), n, C.byref(sz)))
+    workspace = _workspace(workspace, sz.value, dev)
+    check(lib.abcd_residual_norm_bwd(
+        C.byref(joint), n, _ptr(dz), lddz, _ptr(dy), lddy, f.data_ptr(), ldf, _ptr(y), ldy, _ptr(gate),
+        ldg, *[_ptr(kept[k]) for k in JOINT_STATS], _ptr(dx), lddx, _ptr(df), lddf, _ptr(dg), lddg,
+        *[_ptr(grads.get(k)) for k in JOINT_PARAMS], workspace.data_ptr(), workspace.numel(), _stream()))
+    return grads
+
+
 # ------------------------------------------------------ decoder: checkpoints
 
 class Packed8(NamedTuple):
@@ -910,4 +1032,4 @@ __all__ = ["AbcdError", "project", "bin_sort", "bin_sort_workspace_size", "rende
            "render_cache", "stage_cached", "make_split", "split_workspace_size", "intersections",
            "render_bwd_noalloc", "layer_norm", "layer_norm_bwd", "layer_norm_bwd_workspace_size",
            "dropout", "dropout_bwd", "gated_ffn", "gated_ffn_bwd", "embed", "embed_sort",
-           "embed_bwd", "Sorted", "pack8", "unpack8", "Packed8"]
+           "embed_bwd", "Sorted", "residual_norm", "residual_norm_bwd", "pack8", "unpack8", "Packed8"]

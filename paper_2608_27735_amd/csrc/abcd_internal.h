@@ -385,6 +385,21 @@ int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const v
                          int64_t lddy, const int32_t* order, const int32_t* rows,
                          const int32_t* ranges, float scale, int32_t wdtype, void* dtable,
                          int64_t ldt, void* workspace, hipStream_t stream);
+// residual_norm.hip
+size_t residual_norm_bwd_workspace_bytes(const abcd_joint& j, int64_t n);
+int32_t launch_residual_norm(const abcd_joint& j, int64_t n, const void* f, int64_t ldf,
+                             const void* x, int64_t ldx, const void* gate, int64_t ldg, void* y,
+                             int64_t ldy, void* z, int64_t ldz, float* post_mean, float* post_rstd,
+                             float* pre_mean, float* pre_rstd, hipStream_t stream);
+int32_t launch_residual_norm_bwd(const abcd_joint& j, int64_t n, const void* dz, int64_t lddz,
+                                 const void* dy, int64_t lddy, const void* f, int64_t ldf,
+                                 const void* y, int64_t ldy, const void* gate, int64_t ldg,
+                                 const float* post_mean, const float* post_rstd,
+                                 const float* pre_mean, const float* pre_rstd, void* dx,
+                                 int64_t lddx, void* df, int64_t lddf, void* dgate, int64_t lddg,
+                                 void* dpost_weight, void* dpost_bias, void* dpre_weight,
+                                 void* dpre_bias, void* dscale, void* workspace,
+                                 hipStream_t stream);
 // pack8.hip
 int32_t launch_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx, int8_t* q,
                      uint8_t* e, hipStream_t stream);

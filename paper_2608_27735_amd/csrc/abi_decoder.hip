@@ -94,6 +94,31 @@ int32_t check_ints(const char* name, const void* p, size_t align, int64_t n) {
   return ABCD_OK;
 }
 
+int32_t check_joint(const abcd_joint* joint, int64_t n) {
+  REQUIRE(joint != nullptr, "joint is NULL");
+  const abcd_joint& j = *joint;
+  TRY_STATUS(check_rows(j.dtype, n, j.d));
+  TRY_STATUS(check_wdtype(j.dtype, j.wdtype));
+  for (int32_t k : {j.post, j.pre})
+    REQUIRE(k == ABCD_NORM_NONE || k == ABCD_NORM_LAYER || k == ABCD_NORM_RMS, "unknown norm %d", k);
+  REQUIRE(j.gate == ABCD_GATE_NONE || j.gate == ABCD_GATE_ROW || j.gate == ABCD_GATE_ELEMENT, "unknown gate %d", j.gate);
+  REQUIRE((j.post != ABCD_NORM_NONE || !j.post_weight) && (j.post == ABCD_NORM_LAYER || !j.post_bias) &&
+              (j.pre != ABCD_NORM_NONE || !j.pre_weight) && (j.pre == ABCD_NORM_LAYER || !j.pre_bias),
+          "a parameter of no norm");
+  for (const void* p : {j.post_weight, j.post_bias, j.pre_weight, j.pre_bias, j.scale})
+    TRY_STATUS(check_vector("a parameter", p, j.wdtype));
+  REQUIRE(j.eps >= 0.0f && std::isfinite(j.eps), "eps must be finite and >= 0");
+  return ABCD_OK;
+}
+
+int32_t check_gate(const char* name, const abcd_joint& j, const void* gate, int64_t n, int64_t ldg, bool optional) {
+  if (j.gate == ABCD_GATE_NONE) {
+    REQUIRE(gate == nullptr, "%s without a gate", name);
+    return ABCD_OK;
+  }
+  return check_matrix(name, gate, j.dtype, n, j.gate == ABCD_GATE_ROW ? 1 : j.d, ldg, optional);
+}
+
 }  // namespace
 
 extern "C" {
@@ -256,6 +281,71 @@ int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const voi
   TRY_STATUS(check_matrix("dtable", dtable, wdtype, m, d, ldt, false));
   TRY_STATUS(check_workspace(workspace, ws_bytes, embed_bwd_workspace_bytes(n, d)));
   return launch_embed_bwd(dtype, n, m, d, dy, lddy, order, rows, ranges, scale, wdtype, dtable, ldt, workspace, stream);
+}
+
+int32_t abcd_residual_norm(const abcd_joint* joint, int64_t n, const void* f, int64_t ldf, const void* x, int64_t ldx,
+                           const void* gate, int64_t ldg, void* y, int64_t ldy, void* z, int64_t ldz, float* post_mean,
+                           float* post_rstd, float* pre_mean, float* pre_rstd, hipStream_t stream) {
+  TRY_STATUS(check_joint(joint, n));
+  const abcd_joint& j = *joint;
+  TRY_STATUS(check_matrix("f", f, j.dtype, n, j.d, ldf, false));
+  TRY_STATUS(check_matrix("x", x, j.dtype, n, j.d, ldx, false));
+  TRY_STATUS(check_gate("gate", j, gate, n, ldg, false));
+  TRY_STATUS(check_matrix("y", y, j.dtype, n, j.d, ldy, false));
+  if (j.pre == ABCD_NORM_NONE)
+    REQUIRE(z == nullptr, "z without a norm");
+  else
+    TRY_STATUS(check_matrix("z", z, j.dtype, n, j.d, ldz, false));
+  for (const float* p : {post_mean, post_rstd, pre_mean, pre_rstd}) TRY_STATUS(check_vector("a statistic", p, ABCD_F32));
+  return launch_residual_norm(j, n, f, ldf, x, ldx, gate, ldg, y, ldy, z, ldz,
+                              j.post == ABCD_NORM_LAYER ? post_mean : nullptr, post_rstd,
+                              j.pre == ABCD_NORM_LAYER ? pre_mean : nullptr, pre_rstd, stream);
+}
+
+int32_t abcd_residual_norm_bwd_workspace_size(const abcd_joint* joint, int64_t n, size_t* bytes) {
+  TRY_STATUS(check_joint(joint, n));
+  REQUIRE(bytes != nullptr, "bytes is NULL");
+  *bytes = residual_norm_bwd_workspace_bytes(*joint, n);
+  return ABCD_OK;
+}
+
+int32_t abcd_residual_norm_bwd(const abcd_joint* joint, int64_t n, const void* dz, int64_t lddz, const void* dy,
+                               int64_t lddy, const void* f, int64_t ldf, const void* y, int64_t ldy, const void* gate,
+                               int64_t ldg, const float* post_mean, const float* post_rstd, const float* pre_mean,
+                               const float* pre_rstd, void* dx, int64_t lddx, void* df, int64_t lddf, void* dgate,
+                               int64_t lddg, void* dpost_weight, void* dpost_bias, void* dpre_weight, void* dpre_bias,
+                               void* dscale, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  TRY_STATUS(check_joint(joint, n));
+  const abcd_joint& j = *joint;
+  const bool post = j.post != ABCD_NORM_NONE, pre = j.pre != ABCD_NORM_NONE;
+  if (pre) {
+    TRY_STATUS(check_matrix("dz", dz, j.dtype, n, j.d, lddz, false));
+    TRY_STATUS(check_matrix("y", y, j.dtype, n, j.d, ldy, false));
+  } else {
+    REQUIRE(dz == nullptr, "dz without a norm");
+  }
+  TRY_STATUS(check_matrix("dy", dy, j.dtype, n, j.d, lddy, pre));
+  TRY_STATUS(check_matrix("f", f, j.dtype, n, j.d, ldf, false));
+  TRY_STATUS(check_gate("gate", j, gate, n, ldg, false));
+  REQUIRE(n == 0 || ((!post || post_rstd) && (!pre || pre_rstd) && (j.post != ABCD_NORM_LAYER || post_mean) &&
+                     (j.pre != ABCD_NORM_LAYER || pre_mean)),
+          "a statistic is NULL");
+  for (const float* p : {post_mean, post_rstd, pre_mean, pre_rstd}) TRY_STATUS(check_vector("a statistic", p, ABCD_F32));
+  TRY_STATUS(check_matrix("dx", dx, j.dtype, n, j.d, lddx, true));
+  TRY_STATUS(check_matrix("df", df, j.dtype, n, j.d, lddf, true));
+  TRY_STATUS(check_gate("dgate", j, dgate, n, lddg, true));
+  REQUIRE((post || !dpost_weight) && (j.post == ABCD_NORM_LAYER || !dpost_bias) && (pre || !dpre_weight) &&
+              (j.pre == ABCD_NORM_LAYER || !dpre_bias),
+          "a gradient of no norm's parameter");
+  bool sums = false;
+  for (const void* p : {dpost_weight, dpost_bias, dpre_weight, dpre_bias, dscale}) {
+    TRY_STATUS(check_vector("a gradient", p, j.wdtype));
+    sums = sums || p;
+  }
+  if (sums) TRY_STATUS(check_workspace(workspace, ws_bytes, residual_norm_bwd_workspace_bytes(j, n)));
+  return launch_residual_norm_bwd(j, n, dz, lddz, dy, lddy, f, ldf, y, ldy, gate, ldg, post_mean, post_rstd, pre_mean,
+                                  pre_rstd, dx, lddx, df, lddf, dgate, lddg, dpost_weight, dpost_bias, dpre_weight,
+                                  dpre_bias, dscale, workspace, stream);
 }
 
 int32_t abcd_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx, int8_t* q, uint8_t* e,

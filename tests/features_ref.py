@@ -39,3 +39,80 @@ def pack8(x):
             out[i, b:b + 32] = torch.where(finite, q * 2.0 ** (k - 6), math.nan)
             e[i, b // 32] = k + 127
     return out, e
+
+
+# ------------------------------------------------------ between two blocks
+
+def _stats(v, kind, eps):
+    d = v.shape[1]
+    mean = v.sum(1) / d if kind == "layer" else torch.zeros(len(v), dtype=F64)
+    e = v - mean[:, None]
+    return mean, 1.0 / torch.sqrt((e * e).sum(1) / d + eps)
+
+
+def residual_norm(f, x, post, pre, p, gate, eps):
+    """name -> (value, magnitude of the terms behind it: an fp32 evaluation is off by some
+    roundings of that)."""
+    one, out = torch.ones(f.shape[1], dtype=F64), {}
+
+    def norm(v, mag, k, kind):
+        # mag: of v's terms. An error of a mean, or of a variance, reaches the whole row.
+        mean, rstd = _stats(v, kind, eps)
+        m = mag.sum(1) / v.shape[1]
+        out[k + "_rstd"] = (rstd, rstd * (1 + m * rstd) ** 2)
+        if kind == "layer":
+            out[k + "_mean"] = (mean, m)
+        else:
+            m = torch.zeros_like(m)
+        w, b = p.get(k + "_weight", one), p.get(k + "_bias")
+        y = (v - mean[:, None]) * rstd[:, None] * w
+        top = (mag + m[:, None]) * rstd[:, None] * (1 + (mag.sum(1) / v.shape[1] * rstd)[:, None]) ** 2 * w.abs()
+        return (y, top) if b is None else (y + b, top + b.abs())
+
+    t, mt = (f, f.abs()) if post is None else norm(f, f.abs(), "post", post)
+    factor = p.get("scale", one) * (1.0 if gate is None else gate)
+    y, my = x + factor * t, x.abs() + factor.abs() * mt
+    out["y"] = (y, my)
+    if pre is not None:
+        out["z"] = norm(y, my, "pre", pre)
+    return out
+
+
+def _norm_bwd(u, mu, v, mean, rstd, kind):
+    """Gradient through a norm of v from that of its normalised rows, u; mu: magnitude behind u."""
+    d = v.shape[1]
+    h = (v - mean[:, None]) * rstd[:, None]
+    hm = (v.abs() + mean.abs()[:, None]) * rstd[:, None]
+    g = u - h * ((u * h).sum(1) / d)[:, None]
+    m = mu + hm * ((mu * hm).sum(1) / d)[:, None]
+    if kind == "layer":
+        g, m = g - (u.sum(1) / d)[:, None], m + (mu.sum(1) / d)[:, None]
+    return g * rstd[:, None], m * rstd[:, None], h, hm
+
+
+def residual_norm_bwd(dz, dy, f, y, stats, post, pre, p, gate):
+    one, zero, out = torch.ones(f.shape[1], dtype=F64), torch.zeros(len(f), dtype=F64), {}
+    g = torch.zeros_like(f) if dy is None else dy
+    mg = g.abs()
+    stat = lambda k: stats[k] if stats.get(k) is not None else zero
+    if pre is not None:
+        u = dz * p.get("pre_weight", one)
+        add, m, h, hm = _norm_bwd(u, u.abs(), y, stat("pre_mean"), stats["pre_rstd"], pre)
+        g, mg = g + add, mg + m
+        out["pre_weight"], out["pre_bias"] = ((dz * h).sum(0), (dz.abs() * hm).sum(0)), (dz.sum(0), dz.abs().sum(0))
+    out["x"] = (g, mg)
+    s, w, b = p.get("scale", one), p.get("post_weight", one), p.get("post_bias", 0 * one)
+    k = torch.ones_like(f) if gate is None else gate.expand_as(f)
+    dt, mdt = g * k * s, mg * (k * s).abs()
+    if post is None:
+        h, hm = f, f.abs()
+        out["f"] = (dt, mdt)
+    else:
+        df, m, h, hm = _norm_bwd(dt * w, mdt * w.abs(), f, stat("post_mean"), stats["post_rstd"], post)
+        out["f"] = (df, m)
+        out["post_weight"], out["post_bias"] = ((dt * h).sum(0), (mdt * hm).sum(0)), (dt.sum(0), mdt.sum(0))
+    t, mt = h * w + b, hm * w.abs() + b.abs()
+    out["scale"] = ((g * k * t).sum(0), (mg * k.abs() * mt).sum(0))
+    by, mby = g * s * t, mg * s.abs() * mt
+    out["gate"] = (by, mby) if gate is None or gate.shape == f.shape else (by.sum(1, keepdim=True), mby.sum(1, keepdim=True))
+    return out

@@ -99,3 +99,70 @@ def test_reference_checkpoint_keeps_within_its_step():
     err = torch.stack([(y - x)[:, b:b + 32].abs().amax(1) for b in (0, 32, 64)], 1)
     assert (err <= top / 64).all() and (err <= 2.0 ** (e.to(D.F64) - 127 - 6)).all()
     assert torch.equal(R.pack8(y)[0], y)  # what was kept once is kept
+
+
+def joint(**kw):
+    from paper_2608_27735_amd import _lib
+    j = dict(dtype=F16, wdtype=F16, post=1, pre=2, gate=1, eps=1e-5, d=8, post_weight=FAKE, post_bias=FAKE,
+             pre_weight=FAKE, pre_bias=None, scale=FAKE)
+    j.update(kw)
+    return _lib.abcd_joint(*j.values())
+
+
+BAD_JOINTS = [dict(dtype=3), dict(wdtype=BF16), dict(post=3), dict(post=-1), dict(pre=3), dict(gate=3), dict(eps=-1.0),
+              dict(eps=float("nan")), dict(eps=float("inf")), dict(d=0), dict(d=65537), dict(post=0), dict(post=2),
+              dict(pre=0), dict(pre_bias=FAKE), dict(scale=FAKE + 1), dict(post_weight=FAKE + 1)]
+
+
+def test_residual_norm_refuses(lib):
+    j = joint()
+    base = [C.byref(j), 4, FAKE, 8, FAKE, 8, FAKE, 1, FAKE, 8, FAKE, 8, FAKE, FAKE, FAKE, FAKE, None]
+    refuse(base, lib.abcd_residual_norm,
+           [(0, None), (1, -1), (1, (1 << 30) + 1), (2, None), (2, FAKE + 1), (3, 7), (4, None), (5, 7), (6, None),
+            (6, FAKE + 1), (7, 0), (8, None), (9, 7), (10, None), (11, 7), (12, FAKE + 2), (15, FAKE + 1)])
+    refuse(base, lib.abcd_residual_norm, [(0, C.byref(joint(**kw))) for kw in BAD_JOINTS])
+    # an element's gate has rows as wide as f's; no gate and no norm after it take no array
+    refuse(base, lib.abcd_residual_norm, [(0, C.byref(joint(gate=2))), (0, C.byref(joint(gate=0))),
+                                          (0, C.byref(joint(pre=0, pre_weight=None)))])
+
+
+def test_residual_norm_bwd_refuses(lib):
+    j, need = joint(), C.c_size_t(0)
+    assert lib.abcd_residual_norm_bwd_workspace_size(C.byref(j), 4, C.byref(need)) == 0 and need.value >= 4 * 8 * 4
+    refuse([C.byref(j), 4, C.byref(need)], lib.abcd_residual_norm_bwd_workspace_size,
+           [(0, None), (1, -1), (2, None)] + [(0, C.byref(joint(**kw))) for kw in BAD_JOINTS])
+    base = [C.byref(j), 4, FAKE, 8, FAKE, 8, FAKE, 8, FAKE, 8, FAKE, 1, FAKE, FAKE, None, FAKE, FAKE, 8, FAKE, 8, FAKE, 1,
+            FAKE, FAKE, FAKE, None, FAKE, FAKE, need.value, None]
+    refuse(base, lib.abcd_residual_norm_bwd,
+           [(0, None), (1, -1), (2, None), (2, FAKE + 1), (3, 7), (4, FAKE + 1), (5, 7), (6, None), (7, 7), (8, None),
+            (9, 7), (10, None), (11, 0), (12, None), (13, None), (15, None), (15, FAKE + 2), (16, FAKE + 1), (17, 7),
+            (18, FAKE + 1), (19, 7), (20, FAKE + 1), (21, 0), (22, FAKE + 1), (25, FAKE), (26, FAKE + 1), (27, None),
+            (27, FAKE + 8), (28, need.value - 1)])
+    refuse(base, lib.abcd_residual_norm_bwd, [(0, C.byref(joint(**kw))) for kw in BAD_JOINTS])
+    base[0] = C.byref(joint(pre=0, pre_weight=None))
+    refuse(base, lib.abcd_residual_norm_bwd, [(24, FAKE)])
+    base[2], base[24] = None, None
+    refuse(base, lib.abcd_residual_norm_bwd, [(4, None)])
+
+
+@pytest.mark.parametrize("post,pre,gate", [("layer", "layer", "row"), ("rms", "rms", "full"), (None, "layer", "none"),
+                                           ("rms", None, "row"), (None, "rms", "full"), ("layer", None, "none")])
+def test_reference_joint_gradient_is_its_forwards(post, pre, gate):
+    g = torch.Generator().manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=g, dtype=D.F64).requires_grad_()
+    n, d = 5, 9
+    f, x = rand(n, d), rand(n, d)
+    p = {k: rand(d) for k in ("post_weight", "post_bias", "pre_weight", "pre_bias", "scale")
+         if not (k.startswith("post") and post is None) and not (k.startswith("pre") and pre is None)
+         and not (k == "post_bias" and post == "rms") and not (k == "pre_bias" and pre == "rms")}
+    gt = dict(none=None, row=rand(n, 1), full=rand(n, d))[gate]
+    r = R.residual_norm(f, x, post, pre, p, gt, 1e-5)
+    dy, dz = rand(n, d).detach(), rand(n, d).detach() if pre else None
+    loss = (r["y"][0] * dy).sum() + ((r["z"][0] * dz).sum() if pre else 0)
+    leaves = dict(f=f, x=x, **p, **({"gate": gt} if gt is not None else {}))
+    want = dict(zip(leaves, torch.autograd.grad(loss, list(leaves.values()))))
+    det = lambda t: None if t is None else t.detach()
+    stats = {k: det(r[k][0]) for k in ("post_mean", "post_rstd", "pre_mean", "pre_rstd") if k in r}
+    got = R.residual_norm_bwd(dz, dy, det(f), det(r["y"][0]), stats, post, pre, {k: det(v) for k, v in p.items()}, det(gt))
+    for k, v in want.items():
+        assert torch.allclose(got[k][0], v, rtol=1e-9, atol=1e-11), k
