@@ -459,7 +459,7 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
  * ABCD_ACT_SILU g sigmoid(g), ABCD_ACT_GELU g Phi(g) (Phi the normal distribution,
  * by the error function; in 16-bit types within 5e-6 of its size), ABCD_ACT_RELU
  * max(g, 0); of a NaN each gives NaN, as value and as derivative. Products and act are
- * computed in fp32. h, its derivatives by the pre-activations and the gradients that
+ * computed in fp32. (ABCD_ACT_SIGMOID and ABCD_ACT_NONE are a linear layer's.) h, its derivatives by the pre-activations and the gradients that
  * reach these are rounded to dtype where they go from one product to the next, in
  * memory or in registers, and the weights' and biases' gradients are sums of what was
  * rounded. In float16 this bounds their range too: beyond 65,504 they are infinities,
@@ -467,7 +467,7 @@ ABCD_API int32_t abcd_dropout(int32_t dtype, int64_t n, int64_t d, const void* x
  * scaled as float16 training does. In float32 a product may give NaN where an infinity
  * among what it multiplies (x, dy, a weight, h) would make it infinite, and numbers below
  * 2^-110 have fewer digits in it. */
-enum { ABCD_ACT_SILU = 0, ABCD_ACT_GELU = 1, ABCD_ACT_RELU = 2 };
+enum { ABCD_ACT_SILU = 0, ABCD_ACT_GELU = 1, ABCD_ACT_RELU = 2, ABCD_ACT_SIGMOID = 3, ABCD_ACT_NONE = 4 };
 typedef struct abcd_ffn {
   int32_t dtype, act;
   int64_t d, h, o;
@@ -601,6 +601,38 @@ ABCD_API int32_t abcd_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, 
 ABCD_API int32_t abcd_unpack8(int32_t dtype, int64_t n, int64_t d, const int8_t* q,
                               const uint8_t* e, void* y, int64_t ldy, hipStream_t stream);
 
+/* Linear layer of rows x[n][i]: y = residual + act(x w' + b), [n][o]. w: [o][i],
+ * contiguous, one row per output; b [o] may be NULL (0). act: those of the gated block, as
+ * it computes them, ABCD_ACT_SIGMOID 1 / (1 + e^-z) or ABCD_ACT_NONE. Products, act and sums in
+ * fp32, with the gated block's limits in float32. */
+typedef struct abcd_layer {
+  int32_t dtype, act;
+  int64_t i, o;
+  const void *w, *b;
+} abcd_layer;
+
+/* Forward. residual (may be NULL), and y, which may be residual itself. slope: NULL, or
+ * [n][(o + 7) / 8 * 8] of dtype, 16-byte aligned, that receives for the backward act's
+ * derivative (columns past o: zeros; with ABCD_ACT_NONE nothing is written). workspace: at least
+ * abcd_linear_workspace_size bytes, 256-byte aligned. */
+ABCD_API int32_t abcd_linear_workspace_size(const abcd_layer* layer /* host */, int64_t n, size_t* bytes);
+ABCD_API int32_t abcd_linear(const abcd_layer* layer /* host */, int64_t n, const void* x, int64_t ldx,
+                             const void* residual, int64_t ldr, void* y, int64_t ldy, void* slope,
+                             void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Backward, with dz = dy act'(x w' + b): dx = dz w, dw = dz' x, db = the sum of dz's rows
+ * (the residual's gradient is dy itself); written, of dtype, laid out as what they belong to;
+ * each may be NULL, then not computed. dz is rounded to dtype for all three. x: the forward's
+ * rows, or NULL and q and e, an 8-bit checkpoint of them (abcd_pack8), whose numbers are then x,
+ * in the slopes too where these are made again. slope: the forward's, or NULL: made again
+ * from x, w and b. workspace: at least abcd_linear_bwd_workspace_size bytes, 256-byte
+ * aligned. No output may overlap an input. */
+ABCD_API int32_t abcd_linear_bwd_workspace_size(const abcd_layer* layer /* host */, int64_t n, size_t* bytes);
+ABCD_API int32_t abcd_linear_bwd(const abcd_layer* layer /* host */, int64_t n, const void* dy, int64_t lddy,
+                                 const void* x, int64_t ldx, const int8_t* q, const uint8_t* e,
+                                 const void* slope, void* dx, int64_t lddx, void* dw, void* db,
+                                 void* workspace, size_t ws_bytes, hipStream_t stream);
+
 /* ------------------------------------------------------------------------ */
 /* Helpers. abcd_last_error: message of the last failure on this thread.
  * abcd_timing_*: optional per-kernel HIP-event timing of every launch made by
@@ -614,7 +646,8 @@ ABCD_API int32_t abcd_unpack8(int32_t dtype, int64_t n, int64_t d, const int8_t*
  * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
  * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out,
  * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_none, embed_bwd,
- * embed_join, pack8, unpack8, residual_norm, residual_norm_bwd, residual_norm_sums). */
+ * embed_join, pack8, unpack8, residual_norm, residual_norm_bwd, residual_norm_sums,
+ * linear_out, linear_few, linear_dz, linear_dx, linear_slope). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

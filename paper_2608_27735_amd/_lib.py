@@ -57,11 +57,17 @@ class abcd_joint(C.Structure):
                 ("scale", C.c_void_p)]
 
 
+class abcd_layer(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("i", C.c_int64), ("o", C.c_int64),
+                ("w", C.c_void_p), ("b", C.c_void_p)]
+
+
 _P = C.c_void_p  # device pointers travel as integers
 _I32, _I64, _SZ = C.c_int32, C.c_int64, C.c_size_t
 _CAM, _PRM = C.POINTER(abcd_camera), C.POINTER(abcd_raster_params)
 _FFN = C.POINTER(abcd_ffn)
 _JOINT = C.POINTER(abcd_joint)
+_LAYER = C.POINTER(abcd_layer)
 
 # name -> (restype, argtypes); mirrors include/abcd.h
 SIGNATURES = {
@@ -107,6 +113,10 @@ SIGNATURES = {
     "abcd_residual_norm_bwd_workspace_size": (_I32, [_JOINT, _I64, C.POINTER(_SZ)]),
     "abcd_residual_norm_bwd": (_I32, [_JOINT, _I64] + [_P, _I64] * 5 + [_P] * 4 + [_P, _I64] * 3 + [_P] * 6 +
                                [_SZ, _P]),
+    "abcd_linear_workspace_size": (_I32, [_LAYER, _I64, C.POINTER(_SZ)]),
+    "abcd_linear_bwd_workspace_size": (_I32, [_LAYER, _I64, C.POINTER(_SZ)]),
+    "abcd_linear": (_I32, [_LAYER, _I64] + [_P, _I64] * 3 + [_P, _P, _SZ, _P]),
+    "abcd_linear_bwd": (_I32, [_LAYER, _I64, _P, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P, _P, _P, _SZ, _P]),
     "abcd_pack8": (_I32, [_I32, _I64, _I64, _P, _I64, _P, _P, _P]),
     "abcd_unpack8": (_I32, [_I32, _I64, _I64, _P, _P, _P, _I64, _P]),
     "abcd_last_error": (C.c_char_p, []),

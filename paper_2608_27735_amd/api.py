@@ -937,6 +937,105 @@ def unpack8(packed, out=None):
     return out
 
 
+# ----------------------------------------------------- decoder: linear layer
+
+_LINEAR_ACTS = {**_ACTS, "sigmoid": 3, None: 4}
+
+
+def _layer(x, w, b, act):
+    """The layer's description for the library, checked against x's rows (a tensor or a
+    checkpoint of one)."""
+    code = _DTYPES.get(x.dtype)
+    if code is None:
+        raise ValueError(f"x must be float32, float16 or bfloat16, got {x.dtype}")
+    dev = x.q.device if isinstance(x, Packed8) else x.device
+    if act not in _LINEAR_ACTS:
+        raise ValueError(f"act must be None or one of {sorted(_LINEAR_ACTS.keys() - {None})}, got {act!r}")
+    d = x.shape[1]
+    if w.dim() != 2 or w.shape[0] == 0 or w.shape[1] != d or not w.is_contiguous():
+        raise ValueError(f"w must be a contiguous matrix of rows of {d}, got {tuple(w.shape)}")
+    if w.dtype != x.dtype or w.device != dev:
+        raise ValueError(f"w must be {x.dtype} on {dev}, got {w.dtype} on {w.device}")
+    o = w.shape[0]
+    _vector(b, "b", o, x.dtype, dev)
+    return _lib.abcd_layer(code, _LINEAR_ACTS[act], d, o, w.data_ptr(), _ptr(b)), dev
+
+
+def _slope(saved, n, o, dtype, dev):
+    op = (o + 7) // 8 * 8
+    if saved.dtype != dtype or saved.device != dev or not saved.is_contiguous() or saved.shape != (n, op):
+        raise ValueError(f"saved must be a contiguous {dtype} tensor of shape ({n}, {op}) on {dev}")
+    return saved.data_ptr()
+
+
+def linear(x, w, b=None, act=None, residual=None, save=False, out=None, workspace=None):
+    """Linear layer of x [n, i] (float32, float16 or bfloat16; any row stride): y =
+    residual + act(x w' + b) for w [o, i] and b [o] of x's type. act: None, "silu", "gelu",
+    "relu" or "sigmoid". Returns dict(y [n, o], saved): with save=True and an act its
+    derivative, for linear_bwd (which makes it again without), else None. out may be
+    residual."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a matrix of rows")
+    _here(x, "x")
+    layer, dev = _layer(x, w, b, act)
+    ldx = _rows(x, "x")
+    n, o = x.shape[0], layer.o
+    ldr = 0 if residual is None else _rows(residual, "residual", x, (n, o))
+    out, ldy = (_new(x, (n, o)), o) if out is None else (out, _rows(out, "out", x, (n, o)))
+    saved = _new(x, (n, (o + 7) // 8 * 8)) if save and act is not None else None
+    lib = _lib.load()
+    sz = C.c_size_t(0)
+    check(lib.abcd_linear_workspace_size(C.byref(layer), n, C.byref(sz)))
+    workspace = _workspace(workspace, sz.value, dev)
+    check(lib.abcd_linear(C.byref(layer), n, x.data_ptr(), ldx, _ptr(residual), ldr, out.data_ptr(), ldy,
+                          _ptr(saved), workspace.data_ptr(), workspace.numel(), _stream()))
+    return dict(y=out, saved=saved)
+
+
+def linear_bwd(dy, x, w, b=None, act=None, saved=None, grads=None, workspace=None):
+    """Gradients of linear for dy [n, o]: dict(x, w[, b]); the residual's is dy itself. x:
+    the forward's rows, or what pack8 made of them, which then stands for x. saved: the
+    forward's, or None to make act's derivative again. grads: a dict of tensors to write
+    into, where a missing one is left out; none may overlap an input."""
+    packed = isinstance(x, Packed8)
+    if packed:
+        _packed(x, "x")
+        _here(x.q, "x")
+    else:
+        _dtype_of(x, "x")
+        _here(x, "x")
+        if x.dim() != 2:
+            raise ValueError("x must be a matrix of rows")
+    layer, dev = _layer(x, w, b, act)
+    n, d = x.shape
+    o, dtype = layer.o, x.dtype
+    ldx = 0 if packed else _rows(x, "x")
+    if dy.dtype != dtype or dy.device != dev:
+        raise ValueError(f"dy must be {dtype} on {dev}, got {dy.dtype} on {dy.device}")
+    lddy = _rows(dy, "dy", shape=(n, o))
+    slope = None if saved is None or act is None else _slope(saved, n, o, dtype, dev)
+    if grads is None:
+        grads = dict(x=torch.empty((n, d), dtype=dtype, device=dev), w=torch.empty_like(w))
+        if b is not None:
+            grads["b"] = torch.empty_like(b)
+    else:
+        t = grads.get("w")
+        if t is not None and (t.dtype != dtype or t.device != dev or t.shape != w.shape or not t.is_contiguous()):
+            raise ValueError(f"grads[w] must be contiguous {dtype} on {dev} with shape {tuple(w.shape)}")
+        _vector(grads.get("b"), "grads[b]", o, dtype, dev)
+    dx = grads.get("x")
+    lddx = 0 if dx is None else _rows(dx, "grads[x]", dy, (n, d))
+    lib = _lib.load()
+    sz = C.c_size_t(0)
+    check(lib.abcd_linear_bwd_workspace_size(C.byref(layer), n, C.byref(sz)))
+    workspace = _workspace(workspace, sz.value, dev)
+    check(lib.abcd_linear_bwd(
+        C.byref(layer), n, dy.data_ptr(), lddy, None if packed else x.data_ptr(), ldx,
+        x.q.data_ptr() if packed else None, x.e.data_ptr() if packed else None, slope, _ptr(dx), lddx,
+        _ptr(grads.get("w")), _ptr(grads.get("b")), workspace.data_ptr(), workspace.numel(), _stream()))
+    return grads
+
+
 # ---------------------------------------------------------------- collapse
 
 def composite_cache(images, order, n_front, F=None, B=None, accumulate=False, rects=None,
@@ -1032,4 +1131,4 @@ __all__ = ["AbcdError", "project", "bin_sort", "bin_sort_workspace_size", "rende
            "render_cache", "stage_cached", "make_split", "split_workspace_size", "intersections",
            "render_bwd_noalloc", "layer_norm", "layer_norm_bwd", "layer_norm_bwd_workspace_size",
            "dropout", "dropout_bwd", "gated_ffn", "gated_ffn_bwd", "embed", "embed_sort",
-           "embed_bwd", "Sorted", "residual_norm", "residual_norm_bwd", "pack8", "unpack8", "Packed8"]
+           "embed_bwd", "Sorted", "residual_norm", "residual_norm_bwd", "linear", "linear_bwd", "pack8", "unpack8", "Packed8"]

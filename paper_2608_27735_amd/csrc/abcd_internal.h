@@ -400,6 +400,15 @@ int32_t launch_residual_norm_bwd(const abcd_joint& j, int64_t n, const void* dz,
                                  void* dpost_weight, void* dpost_bias, void* dpre_weight,
                                  void* dpre_bias, void* dscale, void* workspace,
                                  hipStream_t stream);
+// linear.hip
+size_t linear_workspace_bytes(const abcd_layer& l, int64_t n, bool backward);
+int32_t launch_linear(const abcd_layer& l, int64_t n, const void* x, int64_t ldx,
+                      const void* residual, int64_t ldr, void* y, int64_t ldy, void* slope,
+                      void* workspace, hipStream_t stream);
+int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_t lddy,
+                          const void* x, int64_t ldx, const int8_t* q, const uint8_t* e,
+                          const void* slope, void* dx, int64_t lddx, void* dw, void* db,
+                          void* workspace, hipStream_t stream);
 // pack8.hip
 int32_t launch_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx, int8_t* q,
                      uint8_t* e, hipStream_t stream);

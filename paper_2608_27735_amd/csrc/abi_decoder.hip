@@ -111,6 +111,23 @@ int32_t check_joint(const abcd_joint* joint, int64_t n) {
   return ABCD_OK;
 }
 
+int32_t check_layer(const abcd_layer* layer, int64_t n) {
+  REQUIRE(layer != nullptr, "layer is NULL");
+  const abcd_layer& l = *layer;
+  TRY_STATUS(check_rows(l.dtype, n, l.i));
+  TRY_STATUS(check_rows(l.dtype, n, l.o));
+  REQUIRE(l.act >= ABCD_ACT_SILU && l.act <= ABCD_ACT_NONE, "unknown act %d", l.act);
+  return ABCD_OK;
+}
+
+int32_t check_layer_weights(const abcd_layer& l, const void* slope) {
+  REQUIRE(l.w != nullptr, "w is NULL");
+  TRY_STATUS(check_vector("w", l.w, l.dtype));
+  TRY_STATUS(check_vector("b", l.b, l.dtype));
+  REQUIRE((reinterpret_cast<uintptr_t>(slope) & 15) == 0, "slope must be 16-byte aligned");
+  return ABCD_OK;
+}
+
 int32_t check_gate(const char* name, const abcd_joint& j, const void* gate, int64_t n, int64_t ldg, bool optional) {
   if (j.gate == ABCD_GATE_NONE) {
     REQUIRE(gate == nullptr, "%s without a gate", name);
@@ -346,6 +363,51 @@ int32_t abcd_residual_norm_bwd(const abcd_joint* joint, int64_t n, const void* d
   return launch_residual_norm_bwd(j, n, dz, lddz, dy, lddy, f, ldf, y, ldy, gate, ldg, post_mean, post_rstd, pre_mean,
                                   pre_rstd, dx, lddx, df, lddf, dgate, lddg, dpost_weight, dpost_bias, dpre_weight,
                                   dpre_bias, dscale, workspace, stream);
+}
+
+int32_t abcd_linear_workspace_size(const abcd_layer* layer, int64_t n, size_t* bytes) {
+  TRY_STATUS(check_layer(layer, n));
+  REQUIRE(bytes != nullptr, "bytes is NULL");
+  *bytes = linear_workspace_bytes(*layer, n, false);
+  return ABCD_OK;
+}
+
+int32_t abcd_linear_bwd_workspace_size(const abcd_layer* layer, int64_t n, size_t* bytes) {
+  TRY_STATUS(check_layer(layer, n));
+  REQUIRE(bytes != nullptr, "bytes is NULL");
+  *bytes = linear_workspace_bytes(*layer, n, true);
+  return ABCD_OK;
+}
+
+int32_t abcd_linear(const abcd_layer* layer, int64_t n, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                    void* y, int64_t ldy, void* slope, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  TRY_STATUS(check_layer(layer, n));
+  const abcd_layer& l = *layer;
+  TRY_STATUS(check_layer_weights(l, slope));
+  TRY_STATUS(check_matrix("x", x, l.dtype, n, l.i, ldx, false));
+  TRY_STATUS(check_matrix("residual", residual, l.dtype, n, l.o, ldr, true));
+  TRY_STATUS(check_matrix("y", y, l.dtype, n, l.o, ldy, false));
+  if (n > 0) TRY_STATUS(check_workspace(workspace, ws_bytes, linear_workspace_bytes(l, n, false)));
+  return launch_linear(l, n, x, ldx, residual, ldr, y, ldy, slope, workspace, stream);
+}
+
+int32_t abcd_linear_bwd(const abcd_layer* layer, int64_t n, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                        const int8_t* q, const uint8_t* e, const void* slope, void* dx, int64_t lddx, void* dw, void* db,
+                        void* workspace, size_t ws_bytes, hipStream_t stream) {
+  TRY_STATUS(check_layer(layer, n));
+  const abcd_layer& l = *layer;
+  TRY_STATUS(check_layer_weights(l, slope));
+  TRY_STATUS(check_matrix("dy", dy, l.dtype, n, l.o, lddy, false));
+  REQUIRE((q == nullptr) == (e == nullptr) && (n == 0 || (x == nullptr) != (q == nullptr)), "either x, or q and e");
+  if (q)
+    TRY_STATUS(check_ints("q", q, 16, n));
+  else
+    TRY_STATUS(check_matrix("x", x, l.dtype, n, l.i, ldx, false));
+  TRY_STATUS(check_matrix("dx", dx, l.dtype, n, l.i, lddx, true));
+  TRY_STATUS(check_vector("dw", dw, l.dtype));
+  TRY_STATUS(check_vector("db", db, l.dtype));
+  TRY_STATUS(check_workspace(workspace, ws_bytes, linear_workspace_bytes(l, n, true)));
+  return launch_linear_bwd(l, n, dy, lddy, x, ldx, q, e, slope, dx, lddx, dw, db, workspace, stream);
 }
 
 int32_t abcd_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t ldx, int8_t* q, uint8_t* e,

@@ -1,4 +1,4 @@
-// activation.h -- the gated block's activations and their derivatives.
+// activation.h -- the decoder's activations and their derivatives.
 #pragma once
 
 #include <type_traits>
@@ -38,6 +38,15 @@ __device__ __forceinline__ float bell(float g) {
 // 386, with erff 456.
 template <int kAct, bool kShort>
 __device__ __forceinline__ float activate(float g, float& slope) {
+  if (kAct == ABCD_ACT_NONE) {
+    slope = 1.0f;
+    return g;
+  }
+  if (kAct == ABCD_ACT_SIGMOID) {
+    const float s = sigmoid(g);
+    slope = s * sigmoid(-g);  // 1 - s would lose the digits of its tail
+    return s;
+  }
   if (kAct == ABCD_ACT_SILU) {
     const float s = sigmoid(g), v = g * s;
     slope = fmaf(v, 1.0f - s, s);
@@ -74,12 +83,18 @@ __device__ __forceinline__ float activate(float g, float& slope) {
   return v;
 }
 
-// Calls f with act as a constant.
+// Calls f with act as a constant: of the gated block, and of a linear layer.
 template <typename F>
 int32_t with_act(int act, F f) {
   if (act == ABCD_ACT_SILU) return f(std::integral_constant<int, ABCD_ACT_SILU>{});
   if (act == ABCD_ACT_GELU) return f(std::integral_constant<int, ABCD_ACT_GELU>{});
   return f(std::integral_constant<int, ABCD_ACT_RELU>{});
+}
+template <typename F>
+int32_t with_any_act(int act, F f) {
+  if (act == ABCD_ACT_NONE) return f(std::integral_constant<int, ABCD_ACT_NONE>{});
+  if (act == ABCD_ACT_SIGMOID) return f(std::integral_constant<int, ABCD_ACT_SIGMOID>{});
+  return with_act(act, f);
 }
 
 }  // namespace abcd

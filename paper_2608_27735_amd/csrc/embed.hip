@@ -16,7 +16,7 @@
 // these. Either way the order of the sums is fixed by the indexes alone.
 #include <algorithm>
 
-#include "load_frag.h"
+#include "sides.h"
 
 namespace abcd {
 namespace {
@@ -337,17 +337,6 @@ int bits_of(int64_t v) {
   while (v >> b) ++b;
   return b;
 }
-
-// Hands out a workspace in 256-byte pieces; with no base it only adds up.
-struct Pieces {
-  char* base;
-  size_t used = 0;
-  void* take(size_t bytes) {
-    char* p = base ? base + used : nullptr;
-    used += align256(bytes);
-    return p;
-  }
-};
 
 struct SortScratch {
   uint32_t *keys, *vals, *counts, *totals;

@@ -1,0 +1,218 @@
+// linear.h -- the linear layer's kernels, for one element type (linear_f32.hip,
+// linear_f16.hip and linear_bf16.hip each compile them for theirs).
+//
+//   z = x w' + b, y = res + act(z); dz = dy act'(z), dx = dz w, dw = dz' x, db = sum dz
+// Products accumulate in fp32, and bias, activation and residual are applied to the
+// accumulators. The backward has act'(z) from the forward, rounded to the element type,
+// or makes z again, and rounds dz to the element type, as the matrix cores read it, for both
+// products and the bias's sum.
+#pragma once
+
+#include "activation.h"
+#include "gated_ffn_few.h"
+#include "linear_args.h"
+#include "product.h"
+
+namespace abcd {
+namespace {
+
+template <typename T, int kAct>
+struct LinearOutEnd {
+  static constexpr bool kXAlong = true, kWAlong = true, kHalves = false;
+  static constexpr int kSegments = 1;
+  typedef Big Large;
+  LinearOut a;
+  __device__ const Side& x() const { return a.x; }
+  __device__ const Side& w() const { return a.w; }
+  __host__ __device__ int64_t rows() const { return a.x.len; }
+  __host__ __device__ int64_t cols() const { return a.o; }
+  __host__ __device__ int64_t end() const { return a.slope ? a.ldslope : a.o; }
+  __host__ __device__ int64_t length() const { return a.i; }
+  struct Column {
+    int64_t c;
+    int left;
+    Floats<8> b;
+  };
+  struct Ahead {
+    V8<T> res;
+  };
+  __device__ __forceinline__ Column column(int64_t c) const {
+    Column k{c, left_of(a.o - c), 0.0f};
+    if (a.bias && k.left > 0) k.b = load_vec<T, 8, false>(static_cast<const T*>(a.bias) + c, k.left);
+    return k;
+  }
+  __device__ __forceinline__ Ahead ahead(const Column& k, int64_t r) const {
+    return Ahead{load8<T>(a.res, r * a.ldr + k.c, a.res ? k.left : 0)};
+  }
+  __device__ __forceinline__ void put(const Column& k, int64_t r, const Ahead& f, Floats<8> v) const {
+    v += k.b;
+    Floats<8> y, s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float slope;
+      y[e] = activate<kAct, sizeof(T) == 2>(v[e], slope);
+      s[e] = e < k.left ? slope : 0.0f;
+    }
+    if (a.res) y += __builtin_convertvector(f.res, Floats<8>);
+    store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + k.c, y, k.left);
+    if (kAct != ABCD_ACT_NONE && a.slope) store_vec<T, 8, true>(static_cast<T*>(a.slope) + r * a.ldslope + k.c, s, 8);
+  }
+};
+
+template <typename T, int kAct>
+struct LinearDzEnd {
+  static constexpr bool kXAlong = true, kWAlong = true, kHalves = false;
+  static constexpr int kSegments = 1;
+  typedef Big Large;
+  LinearDz a;
+  __device__ const Side& x() const { return a.x; }
+  __device__ const Side& w() const { return a.w; }
+  __host__ __device__ int64_t rows() const { return a.x.len; }
+  __host__ __device__ int64_t cols() const { return a.o; }
+  __host__ __device__ int64_t end() const { return a.lddz; }
+  __host__ __device__ int64_t length() const { return a.i; }
+  typedef typename LinearOutEnd<T, kAct>::Column Column;
+  struct Ahead {
+    V8<T> dy;
+  };
+  __device__ __forceinline__ Column column(int64_t c) const {
+    Column k{c, left_of(a.o - c), 0.0f};
+    if (a.bias && k.left > 0) k.b = load_vec<T, 8, false>(static_cast<const T*>(a.bias) + c, k.left);
+    return k;
+  }
+  __device__ __forceinline__ Ahead ahead(const Column& k, int64_t r) const {
+    return Ahead{load8<T>(a.dy, r * a.lddy + k.c, k.left)};
+  }
+  __device__ __forceinline__ void put(const Column& k, int64_t r, const Ahead& f, Floats<8> v) const {
+    v += k.b;
+    const Floats<8> dy = __builtin_convertvector(f.dy, Floats<8>);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float slope;
+      activate<kAct, sizeof(T) == 2>(v[e], slope);
+      v[e] = e < k.left ? dy[e] * slope : 0.0f;
+    }
+    store_vec<T, 8, true>(static_cast<T*>(a.dz) + r * a.lddz + k.c, v, 8);
+  }
+};
+
+template <typename T>
+struct LinearDxEnd {
+  static constexpr bool kXAlong = true, kWAlong = false, kHalves = false;
+  static constexpr int kSegments = 1;
+  typedef Big Large;
+  LinearDx a;
+  __device__ const Side& x() const { return a.dz; }
+  __device__ const Side& w() const { return a.w; }
+  __host__ __device__ int64_t rows() const { return a.dz.len; }
+  __host__ __device__ int64_t cols() const { return a.i; }
+  __host__ __device__ int64_t end() const { return a.i; }
+  __host__ __device__ int64_t length() const { return a.o; }
+  struct Column {
+    int64_t c;
+  };
+  struct Ahead {};
+  __device__ __forceinline__ Column column(int64_t c) const { return Column{c}; }
+  __device__ __forceinline__ Ahead ahead(const Column&, int64_t) const { return Ahead{}; }
+  __device__ __forceinline__ void put(const Column& k, int64_t r, const Ahead&, Floats<8> v) const {
+    store_vec<T, 8, false>(static_cast<T*>(a.dx) + r * a.lddx + k.c, v, left_of(a.i - k.c));
+  }
+};
+
+// Few rows: the weights are read once and bound it (gated_ffn_few.h).
+template <typename T, int kAct, int kX, bool kWhole>
+__global__ __launch_bounds__(kFewOutWaves * 64) void linear_few_kernel(LinearOut a) {
+  f32x4 acc[kX][1], sum[1];
+  const int columns = (int64_t)gridDim.x * 8 >= a.o ? 8 : 16;
+  const int first = blockIdx.x * columns, end = min((int)a.o, first + columns), n = (int)a.x.len;
+  const T* const w[1] = {static_cast<const T*>(a.w.p[0])};
+  few_products<T, kX, 1, kFewOutWaves, kWhole>(acc, static_cast<const T*>(a.x.p[0]), a.x.ld, n, w, a.w.ld, first, end,
+                                               (int)a.i);
+  if (!few_join<kX, 1, kFewOutWaves>(acc, sum)) return;
+  const int l = threadIdx.x & 63, r = (threadIdx.x >> 6) * 16 + (l & 15), c = first + (l >> 4) * 4;
+  const int left = end - c;
+  if (r >= n || left <= 0) return;
+  if (a.bias) sum[0] += load_vec<T, 4, false>(static_cast<const T*>(a.bias) + c, left);
+  f32x4 y, s;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float slope;
+    y[e] = activate<kAct, sizeof(T) == 2>(sum[0][e], slope);
+    s[e] = e < left ? slope : 0.0f;
+  }
+  if (a.res) y += load_vec<T, 4, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left);
+  store_vec<T, 4, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, left);
+  if (kAct != ABCD_ACT_NONE && a.slope) {
+    T* const to = static_cast<T*>(a.slope) + r * a.ldslope;
+    store_vec<T, 4, true>(to + c, s, 4);
+    // the columns past o that this lane's four do not reach
+    if (a.o - c <= 4 && c + 4 < a.ldslope) store_vec<T, 4, true>(to + c + 4, Floats<4>(0.0f), 4);
+  }
+}
+
+// dz = dy slope: a thread for 8 columns of a row.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void linear_slope_kernel(LinearSlope a) {
+  const int64_t vecs = a.lddz / 8, total = a.n * vecs;
+  for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < total; k += (int64_t)gridDim.x * kBlock) {
+    const int64_t r = k / vecs, c = k % vecs * 8;
+    const Floats<8> dy = __builtin_convertvector(load8<T>(a.dy, r * a.lddy + c, left_of(a.o - c)), Floats<8>);
+    const Floats<8> s = load_vec<T, 8, true>(static_cast<const T*>(a.slope) + r * a.ldslope + c, 8);
+    Floats<8> v = dy * s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < a.o ? v[e] : 0.0f;
+    store_vec<T, 8, true>(static_cast<T*>(a.dz) + r * a.lddz + c, v, 8);
+  }
+}
+
+template <typename T>
+int32_t run_linear_out(const LinearOut& a, hipStream_t stream) {
+  return with_any_act(a.act, [&](auto act) -> int32_t {
+    return run_product<T>("linear_out", LinearOutEnd<T, decltype(act)::value>{a}, stream);
+  });
+}
+template <typename T>
+int32_t run_linear_dz(const LinearDz& a, hipStream_t stream) {
+  return with_any_act(a.act, [&](auto act) -> int32_t {
+    return run_product<T>("linear_dz", LinearDzEnd<T, decltype(act)::value>{a}, stream);
+  });
+}
+template <typename T>
+int32_t run_linear_dx(const LinearDx& a, hipStream_t stream) {
+  return run_product<T>("linear_dx", LinearDxEnd<T>{a}, stream);
+}
+
+template <typename T>
+int32_t run_linear_few(const LinearOut& a, hipStream_t stream) {
+  return with_any_act(a.act, [&](auto act) -> int32_t {
+    return with_rows(a.x.len, [&](auto rows) -> int32_t {
+      constexpr int kAct = decltype(act)::value, kX = decltype(rows)::value;
+      const int64_t grid = (a.o + 7) / 8 <= kCUs ? (a.o + 7) / 8 : (a.o + 15) / 16;
+      if (a.i % kPer16<T> == 0)
+        ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, true>), grid, kFewOutWaves * 64, 0, stream, a);
+      else
+        ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, false>), grid, kFewOutWaves * 64, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      return ABCD_OK;
+    });
+  });
+}
+
+template <typename T>
+int32_t run_linear_slope(const LinearSlope& a, hipStream_t stream) {
+  const int64_t blocks = std::min<int64_t>((a.n * (a.lddz / 8) + kBlock - 1) / kBlock, 1 << 16);
+  ABCD_LAUNCH("linear_slope", (linear_slope_kernel<T>), blocks, kBlock, 0, stream, a);
+  ABCD_HIP(hipGetLastError());
+  return ABCD_OK;
+}
+
+}  // namespace
+
+#define ABCD_LINEAR_KERNELS(NAME, TYPE)                                                                    \
+  int32_t linear_out_##NAME(const LinearOut& a, hipStream_t s) { return run_linear_out<TYPE>(a, s); }      \
+  int32_t linear_few_##NAME(const LinearOut& a, hipStream_t s) { return run_linear_few<TYPE>(a, s); }      \
+  int32_t linear_dz_##NAME(const LinearDz& a, hipStream_t s) { return run_linear_dz<TYPE>(a, s); }         \
+  int32_t linear_dx_##NAME(const LinearDx& a, hipStream_t s) { return run_linear_dx<TYPE>(a, s); }         \
+  int32_t linear_slope_##NAME(const LinearSlope& a, hipStream_t s) { return run_linear_slope<TYPE>(a, s); }
+
+}  // namespace abcd

@@ -1,0 +1,128 @@
+// linear.hip -- the linear layer: how a call becomes products (linear.h), copies of what
+// 16-byte loads cannot take, and column sums.
+#include <algorithm>
+
+#include "linear_args.h"
+#include "sides.h"
+
+namespace abcd {
+namespace {
+
+#define LINEAR_BY_TYPE(l, fn, ...)                              \
+  ((l).dtype == ABCD_F32   ? fn##_f32(__VA_ARGS__)              \
+   : (l).dtype == ABCD_F16 ? fn##_f16(__VA_ARGS__)              \
+                           : fn##_bf16(__VA_ARGS__))
+
+// Whether the kernel for a few rows takes the forward: it reads x again for every 16
+// columns of y.
+bool few(const abcd_layer& l, int64_t n) {
+  return n <= 16 || (n <= 64 && (n + 15) / 16 * l.o * l.i * (int64_t)type_bytes(l.dtype) <= 80 << 20);
+}
+
+// Room for the parts of the weights' gradient, none where the rows are too few to split: no
+// more of them than run at once, and of a few tiles no more than their splits.
+size_t dweight_part(const abcd_layer& l, int64_t steps) {
+  const int64_t splits = dweight_splits(steps);
+  if (splits == 1) return 0;
+  auto room = [&](int64_t tile, int64_t slots) {
+    return (size_t)std::min(slots, (l.o + tile - 1) / tile * ((l.i + tile - 1) / tile) * splits) * tile * tile;
+  };
+  return std::max(room(256, kBigSlots), room(128, kSmallSlots));
+}
+
+struct Scratch {
+  void *x, *w, *dz;
+  float* part;
+  size_t bytes;
+};
+
+Scratch layout(const abcd_layer& l, int64_t n, bool backward, void* workspace) {
+  const size_t sz = type_bytes(l.dtype);
+  const int64_t step = kStepBytes / (int64_t)sz;
+  auto steps = [&](int64_t kn) { return (kn + step - 1) / step; };
+  Pieces p{static_cast<char*>(workspace)};
+  Scratch s{};
+  if (!backward && few(l, n)) return s;
+  s.x = p.take(n * up8(l.i) * sz);
+  s.w = p.take(l.o * up8(l.i) * sz);
+  size_t part = product_part(sz, n, l.o, 1, steps(l.i));
+  if (backward) {
+    s.dz = p.take(n * up8(l.o) * sz);
+    part = std::max({part, product_part(sz, n, l.i, 1, steps(l.o)), (size_t)(sum_parts_of(n) * l.o),
+                     dweight_part(l, steps(n))});
+  }
+  s.part = static_cast<float*>(p.take(part * sizeof(float)));
+  s.bytes = p.used;
+  return s;
+}
+
+}  // namespace
+
+// Never 0, also of a call that needs none: which those are is not the caller's to know.
+size_t linear_workspace_bytes(const abcd_layer& l, int64_t n, bool backward) {
+  return std::max<size_t>(256, layout(l, n, backward, nullptr).bytes);
+}
+
+int32_t launch_linear(const abcd_layer& l, int64_t n, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                      void* y, int64_t ldy, void* slope, void* workspace, hipStream_t stream) {
+  if (n == 0) return ABCD_OK;
+  const Scratch s = layout(l, n, false, workspace);
+  LinearOut out{Side{{x, nullptr}, ldx, n}, Side{{l.w, nullptr}, l.i, l.o}, l.b, residual, y,
+                l.act == ABCD_ACT_NONE ? nullptr : slope, l.i, l.o, ldr, ldy, up8(l.o), l.act, Tiling{s.part, 0, 0, 1, 0}};
+  if (few(l, n)) return LINEAR_BY_TYPE(l, linear_few, out, stream);
+  Packs copies;
+  out.x = side_of(copies, l.dtype, x, n, l.i, ldx, s.x);
+  out.w = side_of(copies, l.dtype, l.w, l.o, l.i, l.i, s.w);
+  TRY_STATUS(launch(copies, l.dtype, stream));
+  return LINEAR_BY_TYPE(l, linear_out, out, stream);
+}
+
+int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                          const int8_t* q, const uint8_t* e, const void* slope, void* dx, int64_t lddx, void* dw, void* db,
+                          void* workspace, hipStream_t stream) {
+  const Scratch s = layout(l, n, true, workspace);
+  const bool again = l.act != ABCD_ACT_NONE && !slope;
+  Side xs{}, w{}, dz{};
+  if (n > 0) {
+    Packs copies;
+    if (again || dw) {
+      if (q) {
+        // a checkpoint's rows up to a multiple of 8: zeros behind their end
+        TRY_STATUS(launch_unpack8(l.dtype, n, up8(l.i), q, e, s.x, up8(l.i), stream));
+        xs = Side{{s.x, nullptr}, up8(l.i), n};
+      } else {
+        xs = side_of(copies, l.dtype, x, n, l.i, ldx, s.x);
+      }
+    }
+    if (again || dx) w = side_of(copies, l.dtype, l.w, l.o, l.i, l.i, s.w);
+    if (l.act == ABCD_ACT_NONE)
+      dz = side_of(copies, l.dtype, dy, n, l.o, lddy, s.dz);
+    else
+      dz = Side{{s.dz, nullptr}, up8(l.o), n};
+    TRY_STATUS(launch(copies, l.dtype, stream));
+    if (again) {
+      const LinearDz a{xs, w, l.b, dy, s.dz, l.i, l.o, lddy, dz.ld, l.act, Tiling{s.part, 0, 0, 1, 0}};
+      TRY_STATUS(LINEAR_BY_TYPE(l, linear_dz, a, stream));
+    } else if (slope) {
+      const LinearSlope a{dy, slope, s.dz, n, l.o, lddy, up8(l.o), dz.ld};
+      TRY_STATUS(LINEAR_BY_TYPE(l, linear_slope, a, stream));
+    }
+    if (dx) {
+      // W across: its index is i, the contraction o
+      const LinearDx a{dz, Side{{w.p[0], nullptr}, w.ld, l.i}, dx, l.o, l.i, lddx, Tiling{s.part, 0, 0, 1, 0}};
+      TRY_STATUS(LINEAR_BY_TYPE(l, linear_dx, a, stream));
+    }
+  }
+  if (dw) {
+    FfnDWeight a{};
+    a.part = s.part;
+    a.n = n;
+    a.one[a.count++] = FfnDWeight::One{dz.p[0], xs.p[0], dw, dz.ld, l.o, xs.ld, l.i, 1.0f, 0, 0, 0};
+    TRY_STATUS(LINEAR_BY_TYPE(l, ffn_dweight, a, stream));
+  }
+  SumCall sums{l.dtype, n, s.part};
+  sums.add(db, dz.p[0], dz.ld, l.o, 1.0f);
+  return sums.launch(stream);
+}
+
+}  // namespace abcd

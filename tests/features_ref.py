@@ -4,7 +4,7 @@ import math
 
 import torch
 
-from decoder_ref import E32, F64
+from decoder_ref import E32, F64, act as _decoder_act
 
 
 def embed(table, index, scale):
@@ -116,3 +116,44 @@ def residual_norm_bwd(dz, dy, f, y, stats, post, pre, p, gate):
     by, mby = g * s * t, mg * s.abs() * mt
     out["gate"] = (by, mby) if gate is None or gate.shape == f.shape else (by.sum(1, keepdim=True), mby.sum(1, keepdim=True))
     return out
+
+
+# ------------------------------------------------------------ linear layer
+
+def act(z, name):
+    """An activation, its derivative, and a bound of the second one's size."""
+    if name is None:
+        return z, torch.ones_like(z), 0.0
+    if name == "sigmoid":
+        s = torch.special.expit(z)
+        return s, s * torch.special.expit(-z), 0.1
+    a, da = _decoder_act(z, name)
+    return a, da, dict(silu=0.5, gelu=0.8, relu=0.0)[name]
+
+
+def linear(x, w, b, name, res):
+    """y and the magnitude behind it."""
+    z, mz = x @ w.T, x.abs() @ w.abs().T
+    if b is not None:
+        z, mz = z + b, mz + b.abs()
+    a, da, _ = act(z, name)
+    m = mz if name is None else 1.1 * mz + a.abs()  # no act here has a slope above 1.13
+    return (a, m) if res is None else (a + res, m + res.abs())
+
+
+def linear_bwd(dy, x, w, b, name, u, kept):
+    """name -> (value, magnitude of the fp32 sums' terms, standard deviation that rounding
+    dz, and the slopes where these are kept, to unit u leaves, to first order)."""
+    z, mz = x @ w.T, x.abs() @ w.abs().T
+    if b is not None:
+        z, mz = z + b, mz + b.abs()
+    _, da, bend = act(z, name)
+    dz = dy * da
+    sdz = torch.zeros_like(dz)
+    if name is not None:
+        sdz = u * dz.abs() * (2 if kept else 1) + 16 * E32 * dy.abs() * (da.abs() + bend * mz)
+    if name == "relu":  # its slope jumps where the fp32 sum may have either sign
+        sdz = sdz + torch.where(z.abs() <= 16 * E32 * mz, dy.abs(), torch.zeros_like(z))
+    return dict(x=(dz @ w, dz.abs() @ w.abs(), (sdz ** 2 @ w ** 2).sqrt()),
+                w=(dz.T @ x, dz.abs().T @ x.abs(), ((sdz ** 2).T @ x ** 2).sqrt()),
+                b=(dz.sum(0), dz.abs().sum(0), (sdz ** 2).sum(0).sqrt()))

@@ -166,3 +166,56 @@ def test_reference_joint_gradient_is_its_forwards(post, pre, gate):
     got = R.residual_norm_bwd(dz, dy, det(f), det(r["y"][0]), stats, post, pre, {k: det(v) for k, v in p.items()}, det(gt))
     for k, v in want.items():
         assert torch.allclose(got[k][0], v, rtol=1e-9, atol=1e-11), k
+
+
+def layer(**kw):
+    from paper_2608_27735_amd import _lib
+    l = dict(dtype=F16, act=3, i=8, o=5, w=FAKE, b=FAKE)
+    l.update(kw)
+    return _lib.abcd_layer(*l.values())
+
+
+BAD_LAYERS = [dict(dtype=3), dict(act=5), dict(act=-1), dict(i=0), dict(i=65537), dict(o=0), dict(o=65537)]
+
+
+def test_linear_refuses(lib):
+    l, need = layer(), C.c_size_t(0)
+    for size in (lib.abcd_linear_workspace_size, lib.abcd_linear_bwd_workspace_size):
+        assert size(C.byref(l), 4, C.byref(need)) == 0 and need.value >= 256
+        refuse([C.byref(l), 4, C.byref(need)], size,
+               [(0, None), (1, -1), (1, (1 << 30) + 1), (2, None)] + [(0, C.byref(layer(**kw))) for kw in BAD_LAYERS])
+    lib.abcd_linear_workspace_size(C.byref(l), 400, C.byref(need))
+    base = [C.byref(l), 400, FAKE, 8, FAKE, 5, FAKE, 5, FAKE, FAKE, need.value, None]
+    bad = BAD_LAYERS + [dict(w=None), dict(w=FAKE + 1), dict(b=FAKE + 1)]
+    refuse(base, lib.abcd_linear,
+           [(0, C.byref(layer(**kw))) for kw in bad] +
+           [(0, None), (1, -1), (2, None), (2, FAKE + 1), (3, 7), (4, FAKE + 1), (5, 4), (6, None), (7, 4), (8, FAKE + 8),
+            (9, None), (9, FAKE + 16), (10, need.value - 1)])
+    lib.abcd_linear_bwd_workspace_size(C.byref(l), 400, C.byref(need))
+    base = [C.byref(l), 400, FAKE, 5, FAKE, 8, None, None, FAKE, FAKE, 8, FAKE, FAKE, FAKE, need.value, None]
+    refuse(base, lib.abcd_linear_bwd,
+           [(0, C.byref(layer(**kw))) for kw in bad] +
+           [(0, None), (1, -1), (2, None), (2, FAKE + 1), (3, 4), (4, None), (4, FAKE + 1), (5, 7), (6, FAKE), (7, FAKE),
+            (8, FAKE + 8), (9, FAKE + 1), (10, 7), (11, FAKE + 1), (12, FAKE + 1), (13, None), (13, FAKE + 16),
+            (14, need.value - 1)])
+    base[4], base[6], base[7] = None, FAKE, FAKE
+    refuse(base, lib.abcd_linear_bwd, [(4, FAKE), (6, FAKE + 8), (6, None), (7, None)])
+
+
+def test_the_gated_block_refuses_a_layers_activations(lib):
+    from paper_2608_27735_amd import _lib
+    for a in (3, 4):
+        f = _lib.abcd_ffn(F16, a, 8, 8, 8, FAKE, FAKE, FAKE, None, None, None, 0.0, 0, 0)
+        assert lib.abcd_gated_ffn_workspace_size(C.byref(f), 4, 0, C.byref(C.c_size_t(0))) == 1
+
+
+@pytest.mark.parametrize("name", [None, "silu", "gelu", "relu", "sigmoid"])
+def test_reference_linear_gradient_is_its_forwards(name):
+    g = torch.Generator().manual_seed(5)
+    x, w, b, res, dy = (torch.randn(*s, generator=g, dtype=D.F64).requires_grad_()
+                        for s in ((6, 4), (3, 4), (3,), (6, 3), (6, 3)))
+    y, _ = R.linear(x, w, b, name, res)
+    want = torch.autograd.grad((y * dy.detach()).sum(), (x, w, b))
+    got = R.linear_bwd(*(t.detach() for t in (dy, x, w, b)), name, 0.0, False)
+    for k, v in zip(("x", "w", "b"), want):
+        assert torch.allclose(got[k][0], v, rtol=1e-9, atol=1e-11), k
