@@ -612,8 +612,8 @@ typedef struct abcd_layer {
 } abcd_layer;
 
 /* Forward. residual (may be NULL), and y, which may be residual itself. slope: NULL, or
- * [n][(o + 7) / 8 * 8] of dtype, 16-byte aligned, that receives for the backward act's
- * derivative (columns past o: zeros; with ABCD_ACT_NONE nothing is written). workspace: at least
+ * [n][(o + 7) / 8 * 8], 16-byte aligned, that receives for the backward act's derivative (in
+ * ABCD_F32 of that type, else in ABCD_F16; columns past o: zeros; with ABCD_ACT_NONE nothing is written). workspace: at least
  * abcd_linear_workspace_size bytes, 256-byte aligned. */
 ABCD_API int32_t abcd_linear_workspace_size(const abcd_layer* layer /* host */, int64_t n, size_t* bytes);
 ABCD_API int32_t abcd_linear(const abcd_layer* layer /* host */, int64_t n, const void* x, int64_t ldx,
@@ -622,7 +622,8 @@ ABCD_API int32_t abcd_linear(const abcd_layer* layer /* host */, int64_t n, cons
 
 /* Backward, with dz = dy act'(x w' + b): dx = dz w, dw = dz' x, db = the sum of dz's rows
  * (the residual's gradient is dy itself); written, of dtype, laid out as what they belong to;
- * each may be NULL, then not computed. dz is rounded to dtype for all three. x: the forward's
+ * each may be NULL, then not computed. Both products take dz rounded to dtype, and db may sum it
+ * rounded or not. x: the forward's
  * rows, or NULL and q and e, an 8-bit checkpoint of them (abcd_pack8), whose numbers are then x,
  * in the slopes too where these are made again. slope: the forward's, or NULL: made again
  * from x, w and b. workspace: at least abcd_linear_bwd_workspace_size bytes, 256-byte
@@ -647,7 +648,8 @@ ABCD_API int32_t abcd_linear_bwd(const abcd_layer* layer /* host */, int64_t n, 
  * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out,
  * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_none, embed_bwd,
  * embed_join, pack8, unpack8, residual_norm, residual_norm_bwd, residual_norm_sums,
- * linear_out, linear_few, linear_dz, linear_dx, linear_slope). */
+ * linear_out, linear_few, linear_dz, linear_dx, linear_slope, linear_narrow,
+ * linear_narrow_bwd). */
 ABCD_API const char* abcd_last_error(void);
 ABCD_API const char* abcd_version(void);
 ABCD_API const char* abcd_status_string(int32_t status);

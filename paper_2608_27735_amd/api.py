@@ -961,8 +961,12 @@ def _layer(x, w, b, act):
     return _lib.abcd_layer(code, _LINEAR_ACTS[act], d, o, w.data_ptr(), _ptr(b)), dev
 
 
+def _slope_dtype(dtype):
+    return dtype if dtype == torch.float32 else torch.float16
+
+
 def _slope(saved, n, o, dtype, dev):
-    op = (o + 7) // 8 * 8
+    op, dtype = (o + 7) // 8 * 8, _slope_dtype(dtype)
     if saved.dtype != dtype or saved.device != dev or not saved.is_contiguous() or saved.shape != (n, op):
         raise ValueError(f"saved must be a contiguous {dtype} tensor of shape ({n}, {op}) on {dev}")
     return saved.data_ptr()
@@ -982,7 +986,9 @@ def linear(x, w, b=None, act=None, residual=None, save=False, out=None, workspac
     n, o = x.shape[0], layer.o
     ldr = 0 if residual is None else _rows(residual, "residual", x, (n, o))
     out, ldy = (_new(x, (n, o)), o) if out is None else (out, _rows(out, "out", x, (n, o)))
-    saved = _new(x, (n, (o + 7) // 8 * 8)) if save and act is not None else None
+    saved = None
+    if save and act is not None:
+        saved = torch.empty((n, (o + 7) // 8 * 8), dtype=_slope_dtype(x.dtype), device=dev)
     lib = _lib.load()
     sz = C.c_size_t(0)
     check(lib.abcd_linear_workspace_size(C.byref(layer), n, C.byref(sz)))

@@ -3,9 +3,8 @@
 //
 //   z = x w' + b, y = res + act(z); dz = dy act'(z), dx = dz w, dw = dz' x, db = sum dz
 // Products accumulate in fp32, and bias, activation and residual are applied to the
-// accumulators. The backward has act'(z) from the forward, rounded to the element type,
-// or makes z again, and rounds dz to the element type, as the matrix cores read it, for both
-// products and the bias's sum.
+// accumulators. The backward has act'(z) from the forward (SlopeOf) or makes z again, and
+// rounds dz to the element type, as the matrix cores read it, for both products.
 #pragma once
 
 #include "activation.h"
@@ -55,7 +54,7 @@ struct LinearOutEnd {
     }
     if (a.res) y += __builtin_convertvector(f.res, Floats<8>);
     store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + k.c, y, k.left);
-    if (kAct != ABCD_ACT_NONE && a.slope) store_vec<T, 8, true>(static_cast<T*>(a.slope) + r * a.ldslope + k.c, s, 8);
+    if (kAct != ABCD_ACT_NONE && a.slope) store_vec<SlopeOf<T>, 8, true>(static_cast<SlopeOf<T>*>(a.slope) + r * a.ldslope + k.c, s, 8);
   }
 };
 
@@ -143,25 +142,41 @@ __global__ __launch_bounds__(kFewOutWaves * 64) void linear_few_kernel(LinearOut
   if (a.res) y += load_vec<T, 4, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left);
   store_vec<T, 4, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, left);
   if (kAct != ABCD_ACT_NONE && a.slope) {
-    T* const to = static_cast<T*>(a.slope) + r * a.ldslope;
-    store_vec<T, 4, true>(to + c, s, 4);
+    SlopeOf<T>* const to = static_cast<SlopeOf<T>*>(a.slope) + r * a.ldslope;
+    store_vec<SlopeOf<T>, 4, true>(to + c, s, 4);
     // the columns past o that this lane's four do not reach
-    if (a.o - c <= 4 && c + 4 < a.ldslope) store_vec<T, 4, true>(to + c + 4, Floats<4>(0.0f), 4);
+    if (a.o - c <= 4 && c + 4 < a.ldslope) store_vec<SlopeOf<T>, 4, true>(to + c + 4, Floats<4>(0.0f), 4);
   }
 }
 
-// dz = dy slope: a thread for 8 columns of a row.
+// dz = dy slope, and the sums of its rows: a thread for 8 columns, `lanes` of them next to
+// each other, of rows blockIdx.y, + gridDim.y rows..
 template <typename T>
 __global__ __launch_bounds__(kBlock) void linear_slope_kernel(LinearSlope a) {
-  const int64_t vecs = a.lddz / 8, total = a.n * vecs;
-  for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < total; k += (int64_t)gridDim.x * kBlock) {
-    const int64_t r = k / vecs, c = k % vecs * 8;
-    const Floats<8> dy = __builtin_convertvector(load8<T>(a.dy, r * a.lddy + c, left_of(a.o - c)), Floats<8>);
-    const Floats<8> s = load_vec<T, 8, true>(static_cast<const T*>(a.slope) + r * a.ldslope + c, 8);
-    Floats<8> v = dy * s;
+  __shared__ float red[kBlock * 8];
+  const int t = threadIdx.x & (a.lanes - 1), rows = kBlock / a.lanes;
+  const int64_t c = ((int64_t)blockIdx.x * a.lanes + t) * 8;
+  Floats<8> sum = 0.0f;
+  if (c < a.lddz)
+#pragma unroll 4
+    for (int64_t r = (int64_t)blockIdx.y * rows + threadIdx.x / a.lanes; r < a.n; r += (int64_t)gridDim.y * rows) {
+      const Floats<8> dy = __builtin_convertvector(load8<T>(a.dy, r * a.lddy + c, left_of(a.o - c)), Floats<8>);
+      Floats<8> v = dy * load_vec<SlopeOf<T>, 8, true>(static_cast<const SlopeOf<T>*>(a.slope) + r * a.ldslope + c, 8);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c + e < a.o ? v[e] : 0.0f;
-    store_vec<T, 8, true>(static_cast<T*>(a.dz) + r * a.lddz + c, v, 8);
+      for (int e = 0; e < 8; ++e) v[e] = c + e < a.o ? v[e] : 0.0f;
+      store_vec<T, 8, true>(static_cast<T*>(a.dz) + r * a.lddz + c, v, 8);
+      sum += v;
+    }
+  if (!a.part) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) red[threadIdx.x * 8 + e] = sum[e];
+  __syncthreads();
+  for (int k = threadIdx.x; k < a.lanes * 8; k += kBlock) {
+    const int64_t at = (int64_t)blockIdx.x * a.lanes * 8 + k;
+    if (at >= a.o) break;
+    float v = 0.0f;
+    for (int r = 0; r < rows; ++r) v += red[r * a.lanes * 8 + k];
+    a.part[(int64_t)blockIdx.y * a.o + at] = v;
   }
 }
 
@@ -199,9 +214,9 @@ int32_t run_linear_few(const LinearOut& a, hipStream_t stream) {
 }
 
 template <typename T>
-int32_t run_linear_slope(const LinearSlope& a, hipStream_t stream) {
-  const int64_t blocks = std::min<int64_t>((a.n * (a.lddz / 8) + kBlock - 1) / kBlock, 1 << 16);
-  ABCD_LAUNCH("linear_slope", (linear_slope_kernel<T>), blocks, kBlock, 0, stream, a);
+int32_t run_linear_slope(const LinearSlope& a, int64_t parts, hipStream_t stream) {
+  const dim3 grid((a.lddz / 8 + a.lanes - 1) / a.lanes, parts);
+  ABCD_LAUNCH("linear_slope", (linear_slope_kernel<T>), grid, kBlock, 0, stream, a);
   ABCD_HIP(hipGetLastError());
   return ABCD_OK;
 }
@@ -213,6 +228,8 @@ int32_t run_linear_slope(const LinearSlope& a, hipStream_t stream) {
   int32_t linear_few_##NAME(const LinearOut& a, hipStream_t s) { return run_linear_few<TYPE>(a, s); }      \
   int32_t linear_dz_##NAME(const LinearDz& a, hipStream_t s) { return run_linear_dz<TYPE>(a, s); }         \
   int32_t linear_dx_##NAME(const LinearDx& a, hipStream_t s) { return run_linear_dx<TYPE>(a, s); }         \
-  int32_t linear_slope_##NAME(const LinearSlope& a, hipStream_t s) { return run_linear_slope<TYPE>(a, s); }
+  int32_t linear_slope_##NAME(const LinearSlope& a, int64_t parts, hipStream_t s) {                          \
+    return run_linear_slope<TYPE>(a, parts, s);                                                            \
+  }
 
 }  // namespace abcd

@@ -30,9 +30,15 @@ size_t dweight_part(const abcd_layer& l, int64_t steps) {
   return std::max(room(256, kBigSlots), room(128, kSmallSlots));
 }
 
+// Whether the narrow kernels do, in 16-bit types.
+bool narrow(const abcd_layer& l, int64_t n) { return l.dtype != ABCD_F32 && narrow_layer(l.i, l.o) && n > 64; }
+bool narrow_bwd(const abcd_layer& l, int64_t n) { return l.dtype != ABCD_F32 && narrow_layer_bwd(l.i, l.o) && n > 0; }
+int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 127) / 128, 4 * kCUs); }
+int64_t narrow_bwd_blocks(int64_t n) { return std::min<int64_t>((n + 127) / 128, 2 * kCUs); }
+
 struct Scratch {
   void *x, *w, *dz;
-  float* part;
+  float *part, *sums;
   size_t bytes;
 };
 
@@ -42,7 +48,12 @@ Scratch layout(const abcd_layer& l, int64_t n, bool backward, void* workspace) {
   auto steps = [&](int64_t kn) { return (kn + step - 1) / step; };
   Pieces p{static_cast<char*>(workspace)};
   Scratch s{};
-  if (!backward && few(l, n)) return s;
+  if (!backward && (few(l, n) || narrow(l, n))) return s;
+  if (backward && narrow_bwd(l, n)) {
+    s.part = static_cast<float*>(p.take(narrow_bwd_blocks(n) * (l.o * l.i + l.o) * sizeof(float)));
+    s.bytes = p.used;
+    return s;
+  }
   s.x = p.take(n * up8(l.i) * sz);
   s.w = p.take(l.o * up8(l.i) * sz);
   size_t part = product_part(sz, n, l.o, 1, steps(l.i));
@@ -50,6 +61,7 @@ Scratch layout(const abcd_layer& l, int64_t n, bool backward, void* workspace) {
     s.dz = p.take(n * up8(l.o) * sz);
     part = std::max({part, product_part(sz, n, l.i, 1, steps(l.o)), (size_t)(sum_parts_of(n) * l.o),
                      dweight_part(l, steps(n))});
+    s.sums = static_cast<float*>(p.take(sum_parts_of(n) * l.o * sizeof(float)));
   }
   s.part = static_cast<float*>(p.take(part * sizeof(float)));
   s.bytes = p.used;
@@ -69,6 +81,10 @@ int32_t launch_linear(const abcd_layer& l, int64_t n, const void* x, int64_t ldx
   const Scratch s = layout(l, n, false, workspace);
   LinearOut out{Side{{x, nullptr}, ldx, n}, Side{{l.w, nullptr}, l.i, l.o}, l.b, residual, y,
                 l.act == ABCD_ACT_NONE ? nullptr : slope, l.i, l.o, ldr, ldy, up8(l.o), l.act, Tiling{s.part, 0, 0, 1, 0}};
+  if (narrow(l, n)) {
+    const LinearNarrow a{x, l.w, l.b, residual, y, out.slope, n, l.i, l.o, ldx, ldr, ldy, out.ldslope, l.act};
+    return l.dtype == ABCD_F16 ? linear_narrow_f16(a, narrow_blocks(n), stream) : linear_narrow_bf16(a, narrow_blocks(n), stream);
+  }
   if (few(l, n)) return LINEAR_BY_TYPE(l, linear_few, out, stream);
   Packs copies;
   out.x = side_of(copies, l.dtype, x, n, l.i, ldx, s.x);
@@ -81,6 +97,18 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
                           const int8_t* q, const uint8_t* e, const void* slope, void* dx, int64_t lddx, void* dw, void* db,
                           void* workspace, hipStream_t stream) {
   const Scratch s = layout(l, n, true, workspace);
+  if (l.act == ABCD_ACT_NONE) slope = nullptr;
+  if (narrow_bwd(l, n)) {
+    const LinearNarrowBwd a{x, q, e, dy, slope, l.w, l.b, dx, dw || db ? s.part : nullptr, n, l.i, l.o, ldx, lddy, up8(l.o),
+                            lddx, l.act};
+    const int64_t blocks = narrow_bwd_blocks(n);
+    TRY_STATUS(l.dtype == ABCD_F16 ? linear_narrow_bwd_f16(a, blocks, stream) : linear_narrow_bwd_bf16(a, blocks, stream));
+    if (!a.part) return ABCD_OK;
+    SumOuts outs{};
+    outs.add(dw, l.o * l.i);
+    outs.add(db, l.o);
+    return launch_sum_parts(s.part, blocks, outs, l.dtype, stream);
+  }
   const bool again = l.act != ABCD_ACT_NONE && !slope;
   Side xs{}, w{}, dz{};
   if (n > 0) {
@@ -104,8 +132,9 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
       const LinearDz a{xs, w, l.b, dy, s.dz, l.i, l.o, lddy, dz.ld, l.act, Tiling{s.part, 0, 0, 1, 0}};
       TRY_STATUS(LINEAR_BY_TYPE(l, linear_dz, a, stream));
     } else if (slope) {
-      const LinearSlope a{dy, slope, s.dz, n, l.o, lddy, up8(l.o), dz.ld};
-      TRY_STATUS(LINEAR_BY_TYPE(l, linear_slope, a, stream));
+      const int lanes = std::min(lanes_for((int)(dz.ld / 8)), 64);
+      const LinearSlope a{dy, slope, s.dz, db ? s.sums : nullptr, n, l.o, lddy, up8(l.o), dz.ld, lanes};
+      TRY_STATUS(LINEAR_BY_TYPE(l, linear_slope, a, sum_parts_of(n), stream));
     }
     if (dx) {
       // W across: its index is i, the contraction o
@@ -119,6 +148,11 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
     a.n = n;
     a.one[a.count++] = FfnDWeight::One{dz.p[0], xs.p[0], dw, dz.ld, l.o, xs.ld, l.i, 1.0f, 0, 0, 0};
     TRY_STATUS(LINEAR_BY_TYPE(l, ffn_dweight, a, stream));
+  }
+  if (slope && db && n > 0) {
+    SumOuts outs{};
+    outs.add(db, l.o);
+    return launch_sum_parts(s.sums, sum_parts_of(n), outs, l.dtype, stream);
   }
   SumCall sums{l.dtype, n, s.part};
   sums.add(db, dz.p[0], dz.ld, l.o, 1.0f);

@@ -216,6 +216,6 @@ def test_reference_linear_gradient_is_its_forwards(name):
                         for s in ((6, 4), (3, 4), (3,), (6, 3), (6, 3)))
     y, _ = R.linear(x, w, b, name, res)
     want = torch.autograd.grad((y * dy.detach()).sum(), (x, w, b))
-    got = R.linear_bwd(*(t.detach() for t in (dy, x, w, b)), name, 0.0, False)
+    got = R.linear_bwd(*(t.detach() for t in (dy, x, w, b)), name, 0.0, 0.0)
     for k, v in zip(("x", "w", "b"), want):
         assert torch.allclose(got[k][0], v, rtol=1e-9, atol=1e-11), k

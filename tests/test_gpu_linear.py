@@ -29,6 +29,7 @@ def run(api, n, i, o, dtype, act, bias=True, res=True, pad=0, skip=0):
     r = rand(4, n, o, dtype, skip, pad) if res else None
     dy = rand(5, n, o, dtype, pad, 2 * skip)
     x64, w64, b64, dy64, u = D.d64(x), D.d64(w), D.d64(b), D.d64(dy), D.UNIT[dtype]
+    us = 0.0 if act is None else D.UNIT[torch.float32 if dtype == torch.float32 else torch.float16]  # the slopes'
     f = api.linear(x, w, b, act, residual=r, save=True)
     y, my = R.linear(x64, w64, b64, act, D.d64(r))
     D.close("y", f["y"], y, my)
@@ -44,19 +45,19 @@ def run(api, n, i, o, dtype, act, bias=True, res=True, pad=0, skip=0):
         for k, v in got.items():
             D.close(what + " d" + k, v, ref[k][0], ref[k][1], extra=6 * ref[k][2])
 
-    check(api.linear_bwd(dy, x, w, b, act), R.linear_bwd(dy64, x64, w64, b64, act, u, False), "made again")
+    check(api.linear_bwd(dy, x, w, b, act), R.linear_bwd(dy64, x64, w64, b64, act, u, 0.0), "made again")
     kept = api.linear_bwd(dy, x, w, b, act, saved=f["saved"])
-    check(kept, R.linear_bwd(dy64, x64, w64, b64, act, u, act is not None), "kept")
+    check(kept, R.linear_bwd(dy64, x64, w64, b64, act, u, us), "kept")
     packed = api.pack8(x)
     x8 = D.d64(api.unpack8(packed))
     eight = api.linear_bwd(dy, packed, w, b, act)
-    check(eight, R.linear_bwd(dy64, x8, w64, b64, act, u, False), "8 bits")
+    check(eight, R.linear_bwd(dy64, x8, w64, b64, act, u, 0.0), "8 bits")
     if act is not None:
         got = api.linear_bwd(dy, packed, w, b, act, saved=f["saved"])
         assert torch.equal(got["x"], kept["x"])  # x is in the weights' gradient only
         z = x64 @ w64.T + (0 if b is None else b64)
         dz = dy64 * R.act(z, act)[1]
-        sdz = 2 * u * dz.abs() + 16 * D.E32 * dy64.abs() * (1 + x64.abs() @ w64.abs().T)
+        sdz = (u + us) * dz.abs() + us * 2.0 ** -14 * dy64.abs() + 16 * D.E32 * dy64.abs() * (1 + x64.abs() @ w64.abs().T)
         if act == "relu":
             sdz = sdz + torch.where(z.abs() <= 16 * D.E32 * (x64.abs() @ w64.abs().T + 1), dy64.abs(), torch.zeros_like(z))
         D.close("8 bits, kept dw", got["w"], dz.T @ x8, dz.abs().T @ x8.abs(), extra=6 * ((sdz ** 2).T @ x8 ** 2).sqrt())
