@@ -21,8 +21,9 @@
 namespace abcd {
 namespace {
 
-constexpr int kSortItems = 16, kSortPart = kBlock * kSortItems, kSortBits = 10;
+constexpr int kSortItems = 8, kSortPart = kBlock * kSortItems, kSortBits = 10;
 constexpr int kRun = 64;
+constexpr int kRowTurns = 4;
 
 // ------------------------------------------------------------------ lookup
 
@@ -98,12 +99,13 @@ __global__ __launch_bounds__(kBlock) void embed_count_kernel(SortArgs a) {
   if ((int)blockIdx.x >= a.parts) return;
   for (int i = threadIdx.x; i < digits; i += kBlock) count[i] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kSortPart;
-#pragma unroll 4
-  for (int k = 0; k < kSortItems; ++k) {
-    const int64_t i = first + k * kBlock + threadIdx.x;
-    if (i < a.n) atomicAdd(&count[(sort_key<I>(a, i) >> a.shift) & (digits - 1)], 1u);
-  }
+  const int64_t first = (int64_t)blockIdx.x * kSortPart + threadIdx.x;
+  uint32_t key[kSortItems];
+#pragma unroll
+  for (int k = 0; k < kSortItems; ++k) key[k] = first + k * kBlock < a.n ? sort_key<I>(a, first + k * kBlock) : 0u;
+#pragma unroll
+  for (int k = 0; k < kSortItems; ++k)
+    if (first + k * kBlock < a.n) atomicAdd(&count[(key[k] >> a.shift) & (digits - 1)], 1u);
   __syncthreads();
   for (int i = threadIdx.x; i < digits; i += kBlock) a.counts[(int64_t)i * a.parts + blockIdx.x] = count[i];
 }
@@ -122,80 +124,218 @@ __device__ __forceinline__ uint32_t wave_before(uint32_t v, uint32_t& total) {
 
 // A wave for each digit: its counts become the counts before each part.
 __global__ __launch_bounds__(kWave) void embed_scan_kernel(SortArgs a) {
+  constexpr int kAhead = 4;
   uint32_t* const c = a.counts + (int64_t)blockIdx.x * a.parts;
   uint32_t before = 0;
-  for (int p = 0; p < a.parts; p += kWave) {
-    const int i = p + (int)threadIdx.x;
-    uint32_t all;
-    const uint32_t own = i < a.parts ? c[i] : 0, at = wave_before(own, all);
-    if (i < a.parts) c[i] = before + at;
-    before += all;
+  for (int p = 0; p < a.parts; p += kAhead * kWave) {
+    uint32_t own[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = p + u * kWave + (int)threadIdx.x;
+      own[u] = i < a.parts ? c[i] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = p + u * kWave + (int)threadIdx.x;
+      uint32_t all;
+      const uint32_t at = wave_before(own[u], all);
+      if (i < a.parts) c[i] = before + at;
+      before += all;
+    }
   }
   if (threadIdx.x == 0) a.totals[blockIdx.x] = before;
 }
 
+// Lanes of the wave whose digit of up to kBits bits equals this one's, among those `in`.
+template <int kBits>
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, bool in) {
+  constexpr int kAndEqual = 0x90;  // a & ~(b ^ c)
+  const uint64_t there = __ballot(in);
+  uint32_t lo = (uint32_t)there, hi = (uint32_t)(there >> 32);
+#pragma unroll
+  for (int b = 0; b < kBits; ++b) {
+    const uint32_t m = (uint32_t)((int32_t)(d << (31 - b)) >> 31);
+    const uint64_t set = __ballot(m != 0);
+    lo = __builtin_amdgcn_bitop3_b32(lo, (uint32_t)set, m, kAndEqual);
+    hi = __builtin_amdgcn_bitop3_b32(hi, (uint32_t)(set >> 32), m, kAndEqual);
+  }
+  return (uint64_t)hi << 32 | lo;
+}
+
 // Every wave ranks its quarter of the part in order, 64 keys at a time: lanes with the
-// same digit find each other by ballots.
+// same digit find each other by ballots. The part is then ordered in LDS, so that keys of a
+// digit leave next to each other.
 template <typename I>
 __global__ __launch_bounds__(kBlock) void embed_scatter_kernel(SortArgs a) {
-  constexpr int kWaves = kBlock / kWave, kTurns = kSortPart / kBlock;
-  __shared__ uint32_t at[kWaves][1 << kSortBits];  // by wave: counts, then next places
-  __shared__ uint32_t sums[kWaves];
+  constexpr int kWaves = kBlock / kWave, kTurns = kSortPart / kBlock, kPer = (1 << kSortBits) / kBlock;
+  __shared__ uint32_t at[kWaves][1 << kSortBits];  // by wave: counts, then places in the part
+  __shared__ uint32_t to[1 << kSortBits];          // of a digit: where its first key goes, less its place in the part
+  __shared__ uint32_t keys[kSortPart], vals[kSortPart];
+  __shared__ uint32_t sums[2][kWaves];
   const int digits = 1 << a.bits, w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+  // parts whose keys end up next to each other are one XCD's, whose L2 joins their lines
+  const int part = xcd_order(blockIdx.x, a.parts);
+  const int64_t first = (int64_t)part * kSortPart + w * (kSortPart / kWaves) + l;
+  uint32_t key[kTurns], val[kTurns], place[kTurns], total[kPer], before_part[kPer];
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    const int64_t i = first + k * kWave;
+    key[k] = i < a.n ? sort_key<I>(a, i) : 0u;
+    val[k] = a.vals_in && i < a.n ? a.vals_in[i] : (uint32_t)i;
+  }
+  const int per = max(digits / kBlock, 1), digit = (int)threadIdx.x * per;  // a thread's digits
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const bool there = k < per && digit + k < digits;
+    total[k] = there ? a.totals[digit + k] : 0u;
+    before_part[k] = there ? a.counts[(int64_t)(digit + k) * a.parts + part] : 0u;
+  }
   for (int i = threadIdx.x; i < kWaves << kSortBits; i += kBlock) (&at[0][0])[i] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kSortPart + w * (kSortPart / kWaves) + l;
-  uint32_t key[kTurns], place[kTurns];
-#pragma unroll
-  for (int k = 0; k < kTurns; ++k) key[k] = first + k * kWave < a.n ? sort_key<I>(a, first + k * kWave) : 0u;
 #pragma unroll
   for (int k = 0; k < kTurns; ++k) {
     const bool in = first + k * kWave < a.n;
     const uint32_t d = (key[k] >> a.shift) & (uint32_t)(digits - 1);
-    uint64_t same = __ballot(in);
-    for (int b = 0; b < a.bits; ++b) {
-      const uint64_t set = __ballot((d >> b) & 1u);
-      same &= (d >> b) & 1u ? set : ~set;
-    }
-    const uint32_t before = (uint32_t)__popcll(same & ((1ull << l) - 1ull));
+    const uint64_t same = same_digit<kSortBits>(d, in);
     uint32_t start = 0;
     const int leader = in ? __ffsll((unsigned long long)same) - 1 : l;
     if (in && l == leader) start = atomicAdd(&at[w][d], (uint32_t)__popcll(same));
-    place[k] = (uint32_t)__shfl((int)start, leader, 64) + before;
+    place[k] = (uint32_t)__shfl((int)start, leader, 64) + (uint32_t)__popcll(same & ((1ull << l) - 1ull));
   }
   __syncthreads();
-  // where each wave's keys of a digit go: behind all smaller digits, the parts before
-  // this one and the waves before this one
-  uint32_t run = 0;
-  for (int i0 = 0; i0 < digits; i0 += kBlock) {
-    const int i = i0 + (int)threadIdx.x;
-    uint32_t all;
-    const uint32_t own = i < digits ? a.totals[i] : 0;
-    uint32_t before = wave_before(own, all);
-    if (l == 0) sums[w] = all;
-    __syncthreads();
-    for (int v = 0; v < kWaves; ++v) {
-      if (v < w) before += sums[v];
-    }
-    const uint32_t round = sums[0] + sums[1] + sums[2] + sums[3];
-    if (i < digits) {
-      uint32_t next = run + before + a.counts[(int64_t)i * a.parts + blockIdx.x];
-      for (int v = 0; v < kWaves; ++v) {
-        const uint32_t c = at[v][i];
-        at[v][i] = next;
-        next += c;
-      }
-    }
-    run += round;
-    __syncthreads();
+  // a digit's keys go behind all smaller digits and the parts before this one; in the part
+  // behind its smaller digits, wave by wave
+  uint32_t sum = 0, own = 0, all;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    sum += total[k];
+    if (k < per && digit + k < digits)
+      for (int v = 0; v < kWaves; ++v) own += at[v][digit + k];
+  }
+  uint32_t before = wave_before(sum, all);
+  if (l == 0) sums[0][w] = all;
+  uint32_t here = wave_before(own, all);
+  if (l == 0) sums[1][w] = all;
+  __syncthreads();
+  for (int v = 0; v < w; ++v) {
+    before += sums[0][v];
+    here += sums[1][v];
   }
 #pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (k < per && digit + k < digits) {
+      to[digit + k] = before + before_part[k] - here;
+      for (int v = 0; v < kWaves; ++v) {
+        const uint32_t c = at[v][digit + k];
+        at[v][digit + k] = here;
+        here += c;
+      }
+    }
+    before += total[k];
+  }
+  __syncthreads();
+#pragma unroll
   for (int k = 0; k < kTurns; ++k) {
-    const int64_t i = first + k * kWave;
-    if (i >= a.n) continue;
-    const uint32_t to = at[w][(key[k] >> a.shift) & (uint32_t)(digits - 1)] + place[k];
-    a.keys_out[to] = key[k];
-    a.vals_out[to] = a.vals_in ? a.vals_in[i] : (uint32_t)i;
+    if (first + k * kWave >= a.n) continue;
+    const uint32_t slot = at[w][(key[k] >> a.shift) & (uint32_t)(digits - 1)] + place[k];
+    keys[slot] = key[k];
+    vals[slot] = val[k];
+  }
+  __syncthreads();
+  const int64_t left = a.n - (int64_t)part * kSortPart;
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    const int slot = k * kBlock + (int)threadIdx.x;
+    if (slot >= left) continue;
+    const uint32_t v = keys[slot], place_of = to[(v >> a.shift) & (uint32_t)(digits - 1)] + (uint32_t)slot;
+    a.keys_out[place_of] = v;
+    a.vals_out[place_of] = vals[slot];
+  }
+}
+
+// Few positions: one workgroup sorts them in LDS, digits of up to kFewBits bits, and marks
+// the rows that have any (embed_count's workgroups have marked all as empty).
+constexpr int kFewWaves = 16, kFewTurns = 8, kFewMost = kFewWaves * kWave * kFewTurns, kFewBits = 8;
+template <typename I>
+__global__ __launch_bounds__(kFewWaves* kWave) void embed_few_kernel(SortArgs a) {
+  constexpr int kThreads = kFewWaves * kWave;
+  __shared__ uint32_t keys[kFewMost];
+  __shared__ uint16_t vals[kFewMost];
+  __shared__ uint32_t at[1 << kFewBits][kFewWaves + 1];  // by digit and wave: counts, then next places
+  __shared__ uint32_t sums[kFewWaves];
+  const int n = (int)a.n, w = threadIdx.x / kWave, l = threadIdx.x % kWave, digits = 1 << a.bits;
+  // a wave's keys are consecutive: as many turns as it takes
+  const int turns = (n + kThreads - 1) / kThreads, first = w * turns * kWave + l;
+  uint32_t key[kFewTurns], val[kFewTurns], place[kFewTurns];
+#pragma unroll
+  for (int k = 0; k < kFewTurns; ++k) {
+    const int i = first + k * kWave;
+    val[k] = (uint32_t)i;
+    key[k] = k < turns && i < n ? sort_key<I>(a, i) : 0u;
+  }
+  for (int shift = 0; shift < a.shift; shift += a.bits) {
+    for (int i = threadIdx.x; i < digits * (kFewWaves + 1); i += kThreads) (&at[0][0])[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kFewTurns; ++k) {
+      if (k >= turns) break;
+      const bool in = first + k * kWave < n;
+      const uint32_t d = (key[k] >> shift) & (uint32_t)(digits - 1);
+      const uint64_t same = same_digit<kFewBits>(d, in);
+      uint32_t start = 0;
+      const int leader = in ? __ffsll((unsigned long long)same) - 1 : l;
+      if (in && l == leader) start = atomicAdd(&at[d][w], (uint32_t)__popcll(same));
+      place[k] = (uint32_t)__shfl((int)start, leader, 64) + (uint32_t)__popcll(same & ((1ull << l) - 1ull));
+    }
+    __syncthreads();
+    // counts by digit, then wave, become places: kPer of them next to each other a thread
+    constexpr int kPer = (kFewWaves << kFewBits) / kThreads;
+    const int per = digits * kFewWaves / kThreads > 0 ? digits * kFewWaves / kThreads : 1;
+    const bool takes = (int)threadIdx.x * per < digits * kFewWaves;
+    uint32_t own[kPer], total = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int e = (int)threadIdx.x * per + k;
+      own[k] = takes && k < per ? at[e / kFewWaves][e % kFewWaves] : 0u;
+      total += own[k];
+    }
+    uint32_t all;
+    uint32_t before = wave_before(total, all);
+    if (l == 0) sums[w] = all;
+    __syncthreads();
+    for (int v = 0; v < w; ++v) before += sums[v];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int e = (int)threadIdx.x * per + k;
+      if (takes && k < per) at[e / kFewWaves][e % kFewWaves] = before;
+      before += own[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kFewTurns; ++k) {
+      if (k >= turns || first + k * kWave >= n) break;
+      const uint32_t to = at[(key[k] >> shift) & (uint32_t)(digits - 1)][w] + place[k];
+      keys[to] = key[k];
+      vals[to] = (uint16_t)val[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kFewTurns; ++k) {
+      const int i = first + k * kWave;
+      if (k >= turns || i >= n) break;
+      key[k] = keys[i];
+      val[k] = vals[i];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kFewTurns; ++k) {
+    const int i = first + k * kWave;
+    if (k >= turns || i >= n) break;
+    a.keys_out[i] = key[k];
+    a.vals_out[i] = val[k];
+    if (key[k] >= (uint32_t)a.m) continue;
+    if (i == 0 || keys[i - 1] != key[k]) a.ranges[key[k]].x = i;
+    if (i == n - 1 || keys[i + 1] != key[k]) a.ranges[key[k]].y = i + 1;
   }
 }
 
@@ -217,9 +357,8 @@ struct EmbedBwdArgs {
   const int2* ranges;
   void* dtable;
   float* part;       // [chunk][2][pitch]: of the long row that reaches into a chunk, and of the one that begins there
-  int* owners;       // how many long rows there are, then in which chunk each begins
   int64_t lddy, ldt, n, m, pitch;
-  int d, lanes, row_blocks;
+  int d, lanes, row_blocks, turns;  // turns: rows of the table that a group of lanes takes
   int wf32;
   float scale;
 };
@@ -256,8 +395,6 @@ __device__ __forceinline__ Floats<N> sum_run(const EmbedBwdArgs& a, int from, in
   return s;
 }
 
-__global__ void embed_none_kernel(int* owners) { owners[0] = 0; }
-
 // Workgroups below row_blocks: rows of the table with up to kRun positions. The others:
 // chunks of the order, of which they take what belongs to longer rows. blockIdx.y: blocks
 // of kBlock vectors of columns at most.
@@ -267,11 +404,20 @@ __global__ __launch_bounds__(kBlock) void embed_bwd_kernel(EmbedBwdArgs a) {
   const int rows = kBlock / a.lanes, c = ((int)blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1))) * N;
   if (c >= a.d) return;
   if ((int)blockIdx.x < a.row_blocks) {
-    const int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / a.lanes;
-    if (r >= a.m) return;
-    const int2 at = a.ranges[r];
-    if (at.y - at.x > kRun) return;
-    put_row<T, N, kWhole>(a, r, c, sum_run<T, N, kWhole>(a, at.x, at.y, c));
+    int64_t r = (int64_t)blockIdx.x * rows * a.turns + threadIdx.x / a.lanes;
+    if (a.turns == 1) {
+      if (r >= a.m) return;
+      const int2 at = a.ranges[r];
+      if (at.y - at.x > kRun) return;
+      put_row<T, N, kWhole>(a, r, c, sum_run<T, N, kWhole>(a, at.x, at.y, c));
+      return;
+    }
+    int2 at[kRowTurns];
+#pragma unroll
+    for (int k = 0; k < kRowTurns; ++k) at[k] = r + k * rows < a.m ? a.ranges[r + k * rows] : make_int2(0, kRun + 1);
+#pragma unroll
+    for (int k = 0; k < kRowTurns; ++k, r += rows)
+      if (at[k].y - at[k].x <= kRun) put_row<T, N, kWhole>(a, r, c, sum_run<T, N, kWhole>(a, at[k].x, at[k].y, c));
     return;
   }
   const int64_t chunk = (int64_t)((int)blockIdx.x - a.row_blocks) * rows + threadIdx.x / a.lanes, begin = chunk * kRun;
@@ -288,25 +434,33 @@ __global__ __launch_bounds__(kBlock) void embed_bwd_kernel(EmbedBwdArgs a) {
     const int which = at.x >= begin ? 1 : 0;
     const Floats<N> s = sum_run<T, N, kWhole>(a, max(at.x, (int)begin), min(at.y, (int)end), c);
     store_vec<float, N, true>(a.part + (chunk * 2 + which) * a.pitch + c, s, N);
-    if (which == 1 && c == 0) a.owners[1 + atomicAdd(a.owners, 1)] = (int)chunk;
   }
 }
 
 constexpr int kJoinWaves = 16;
 
-// Rows of more than kRun positions: 64 columns a workgroup, the chunks dealt to its
-// waves. (Which workgroup takes which row depends on the order of the atomics above; the sums do not.)
+// Rows of more than kRun positions that begin in one of 64 chunks: 64 columns a workgroup,
+// the chunks that a row reaches dealt to its waves.
 template <typename T>
 __global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedBwdArgs a) {
   __shared__ float red[kJoinWaves][kWave];
   const int w = threadIdx.x / kWave, l = threadIdx.x % kWave, c = (int)blockIdx.y * kWave + l;
-  const int count = a.owners[0];
-  for (int i = blockIdx.x; i < count; i += gridDim.x) {
-    const int64_t first = a.owners[1 + i];
-    // the row that begins in this chunk and goes on behind it has the chunk's last position
-    const int64_t end = (first + 1) * kRun < a.n ? (first + 1) * kRun : a.n;
-    const int r = a.rows[end - 1];
-    const int64_t last = (a.ranges[r].y - 1) / kRun;
+  // a row that begins in a chunk and goes on behind it has the chunk's last position
+  const int64_t chunk = (int64_t)blockIdx.x * kWave + l, behind = (chunk + 1) * kRun;
+  int row = a.m, end = 0;
+  bool begins = false;
+  if (behind < a.n) {
+    row = a.rows[behind - 1];
+    if (row < a.m) {
+      const int2 at = a.ranges[row];
+      end = at.y;
+      begins = at.y - at.x > kRun && at.x >= chunk * kRun;
+    }
+  }
+  for (uint64_t left = __ballot(begins); left; left &= left - 1) {
+    const int own = __ffsll((unsigned long long)left) - 1;
+    const int r = __shfl(row, own, 64);
+    const int64_t first = (int64_t)blockIdx.x * kWave + own, last = (__shfl(end, own, 64) - 1) / kRun;
     float s = 0.0f;
     if (c < a.d) {
       if (w == 0) s = a.part[(first * 2 + 1) * a.pitch + c];
@@ -413,8 +567,23 @@ int32_t launch_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* 
   a.bits = s.bits;
   return with_index(index_bits, [&](auto zi) -> int32_t {
     typedef decltype(zi) I;
-    // of no positions only the rows' ranges are written
-    for (int pass = 0; pass < (n > 0 ? s.passes : 1); ++pass) {
+    if (n <= kFewMost) {
+      const int bits = bits_of(m);
+      const int64_t zero = std::min<int64_t>((m + kBlock - 1) / kBlock, 2048);
+      a.parts = 0;  // all that this does is mark the rows
+      ABCD_LAUNCH("embed_count", (embed_count_kernel<I>), zero, kBlock, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      if (n == 0) return ABCD_OK;
+      const int passes = (bits + kFewBits - 1) / kFewBits;
+      a.bits = (bits + passes - 1) / passes;
+      a.shift = passes * a.bits;
+      a.keys_out = reinterpret_cast<uint32_t*>(rows);
+      a.vals_out = reinterpret_cast<uint32_t*>(order);
+      ABCD_LAUNCH("embed_few", (embed_few_kernel<I>), 1, kFewWaves * kWave, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      return ABCD_OK;
+    }
+    for (int pass = 0; pass < s.passes; ++pass) {
       // two places take turns so that the last pass writes the result
       const bool own = (s.passes - 1 - pass) & 1;
       a.shift = pass * s.bits;
@@ -425,7 +594,6 @@ int32_t launch_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* 
       const int64_t zero = pass == 0 ? std::min<int64_t>((m + kBlock - 1) / kBlock, 2048) : 0;
       ABCD_LAUNCH("embed_count", (embed_count_kernel<I>), std::max<int64_t>(s.parts, zero), kBlock, 0, stream, a);
       ABCD_HIP(hipGetLastError());
-      if (n == 0) return ABCD_OK;
       ABCD_LAUNCH("embed_scan", embed_scan_kernel, 1 << s.bits, kWave, 0, stream, a);
       ABCD_HIP(hipGetLastError());
       ABCD_LAUNCH("embed_scatter", (embed_scatter_kernel<I>), s.parts, kBlock, 0, stream, a);
@@ -443,8 +611,7 @@ int32_t launch_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* 
 size_t embed_bwd_workspace_bytes(int64_t n, int64_t d) {
   Pieces p{nullptr};
   p.take((size_t)embed_chunks(n) * 2 * embed_pitch(d) * sizeof(float));
-  p.take((1 + (size_t)embed_chunks(n)) * sizeof(int));
-  return p.used;
+  return std::max<size_t>(256, p.used);
 }
 
 int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy, int64_t lddy,
@@ -453,19 +620,18 @@ int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const v
   Pieces p{static_cast<char*>(workspace)};
   const int64_t pitch = embed_pitch(d), chunks = embed_chunks(n);
   float* const part = static_cast<float*>(p.take((size_t)chunks * 2 * pitch * sizeof(float)));
-  int* const owners = static_cast<int*>(p.take((1 + (size_t)chunks) * sizeof(int)));
-  EmbedBwdArgs a{dy, order, rows_of, reinterpret_cast<const int2*>(ranges), dtable, part, owners, lddy, ldt, n, m, pitch,
-                 (int)d, 0, 0, wdtype == ABCD_F32 && dtype != ABCD_F32, scale};
+  EmbedBwdArgs a{dy, order, rows_of, reinterpret_cast<const int2*>(ranges), dtable, part, lddy, ldt, n, m, pitch,
+                 (int)d, 0, 0, 1, wdtype == ABCD_F32 && dtype != ABCD_F32, scale};
   return with_type(dtype, [&](auto z) -> int32_t {
     typedef decltype(z) T;
     const int nvec = (int)((d + kPer16<T> - 1) / kPer16<T>);
     a.lanes = embed_lanes(nvec);
     const int64_t rows = kBlock / a.lanes;
-    a.row_blocks = (int)((m + rows - 1) / rows);
+    // where most rows are empty, and long, a wave looks at several of them at once
+    a.turns = n < m && nvec >= kWave ? kRowTurns : 1;
+    a.row_blocks = (int)((m + rows * a.turns - 1) / (rows * a.turns));
     const int64_t blocks = a.row_blocks + (chunks + rows - 1) / rows;
     REQUIRE(blocks < (int64_t(1) << 31), "too many rows");
-    ABCD_LAUNCH("embed_none", embed_none_kernel, 1, 1, 0, stream, owners);
-    ABCD_HIP(hipGetLastError());
     const dim3 grid(blocks, (nvec + a.lanes - 1) / a.lanes);
     if (d % kPer16<T> == 0)
       ABCD_LAUNCH("embed_bwd", (embed_bwd_kernel<T, true>), grid, kBlock, 0, stream, a);
@@ -473,9 +639,8 @@ int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const v
       ABCD_LAUNCH("embed_bwd", (embed_bwd_kernel<T, false>), grid, kBlock, 0, stream, a);
     ABCD_HIP(hipGetLastError());
     if (n > kRun) {
-      const int64_t most = std::min<int64_t>(chunks, 256);
-      ABCD_LAUNCH("embed_join", (embed_join_kernel<T>), dim3(most, (d + kWave - 1) / kWave), kJoinWaves * kWave, 0, stream,
-                  a);
+      const dim3 joins((chunks + kWave - 1) / kWave, (d + kWave - 1) / kWave);
+      ABCD_LAUNCH("embed_join", (embed_join_kernel<T>), joins, kJoinWaves * kWave, 0, stream, a);
       ABCD_HIP(hipGetLastError());
     }
     return ABCD_OK;
