@@ -756,6 +756,15 @@ def embed_bwd(dy, index, m, scale=1.0, wdtype=None, out=None, workspace=None):
 _NORMS = {None: 0, "layer": 1, "rms": 2}  # ABCD_NORM_*
 JOINT_PARAMS = ("post_weight", "post_bias", "pre_weight", "pre_bias", "scale")
 JOINT_STATS = ("post_mean", "post_rstd", "pre_mean", "pre_rstd")
+_JOINT_SET = frozenset(JOINT_PARAMS)
+# the statistics that a pair of norms has
+_JOINT_HAS = {(a, b): tuple(k for k, kind in zip(JOINT_STATS, (a, a, b, b))
+                            if kind == "layer" or (kind == "rms" and k.endswith("rstd")))
+              for a in _NORMS for b in _NORMS}
+# the parameters that norms of these kinds do not have
+_JOINT_LACKS = {(a, b): tuple(k for k, kind in zip(JOINT_PARAMS, (a, a, b, b, "layer"))
+                              if kind is None or (kind == "rms" and k.endswith("bias")))
+                for a in _NORMS for b in _NORMS}
 
 
 def _joint(f, post, pre, params, gate, eps):
@@ -765,22 +774,22 @@ def _joint(f, post, pre, params, gate, eps):
     _here(f, "f")
     ldf = _rows(f, "f")
     (n, d), dev = f.shape, f.device
-    for k, v in (("post", post), ("pre", pre)):
-        if v not in _NORMS:
-            raise ValueError(f"{k} must be None, 'layer' or 'rms', got {v!r}")
-    params = params or {}
-    if not params.keys() <= set(JOINT_PARAMS):
-        raise ValueError(f"unknown parameters {sorted(params.keys() - set(JOINT_PARAMS))}")
-    given = [t for t in map(params.get, JOINT_PARAMS) if t is not None]
-    wdtype = _param_dtype(f, given[0], None) if given else f.dtype
-    ptrs = []
-    for k in JOINT_PARAMS:
-        t = params.get(k)
-        _vector(t, k, d, wdtype, dev)
-        kind = dict(post=post, pre=pre).get(k.split("_")[0], "layer")
-        if t is not None and (kind is None or (kind == "rms" and k.endswith("bias"))):
-            raise ValueError(f"{k} given, but no norm that has one")
-        ptrs.append(_ptr(t))
+    if post not in _NORMS or pre not in _NORMS:
+        raise ValueError(f"post and pre must be None, 'layer' or 'rms', got {post!r} and {pre!r}")
+    wdtype, ptrs = f.dtype, (None,) * 5
+    if params:
+        if not params.keys() <= _JOINT_SET:
+            raise ValueError(f"unknown parameters {sorted(params.keys() - _JOINT_SET)}")
+        for k in _JOINT_LACKS[post, pre]:
+            if params.get(k) is not None:
+                raise ValueError(f"{k} given, but no norm that has one")
+        given = [params.get(k) for k in JOINT_PARAMS]
+        wdtype = next((t.dtype for t in given if t is not None), wdtype)
+        if wdtype != f.dtype and wdtype != torch.float32:
+            raise ValueError(f"parameters must be {f.dtype} or float32, got {wdtype}")
+        for k, t in zip(JOINT_PARAMS, given):
+            _vector(t, k, d, wdtype, dev)
+        ptrs = [_ptr(t) for t in given]
     mode, ldg = 0, 0
     if gate is not None:
         if gate.dim() != 2 or gate.shape[0] != n or gate.shape[1] not in (1, d):
@@ -812,8 +821,7 @@ def residual_norm(f, x, post=None, pre=None, params=None, gate=None, eps=1e-5, o
         z, ldz = _new(f, size), d
     else:
         ldz = _rows(z, "z", f, size)
-    names = [k for k, kind in zip(JOINT_STATS, (post, post, pre, pre))
-             if kind == "layer" or (kind == "rms" and k.endswith("rstd"))]
+    names = _JOINT_HAS[post, pre]
     r = dict.fromkeys(JOINT_STATS)
     if names:
         r.update(zip(names, torch.empty((len(names), n), dtype=torch.float32, device=dev).unbind(0)))
@@ -841,11 +849,10 @@ def residual_norm_bwd(dz, dy, f, kept, post=None, pre=None, params=None, gate=No
     lddy = 0 if dy is None else _rows(dy, "dy", f, size)
     y = kept["y"] if pre is not None else None
     ldy = 0 if y is None else _rows(y, "y", f, size)
-    for k, kind in zip(JOINT_STATS, (post, post, pre, pre)):
-        if kind == "layer" or (kind == "rms" and k.endswith("rstd")):
-            if kept[k] is None:
-                raise ValueError(f"{k} is required")
-            _vector(kept[k], k, n, torch.float32, dev)
+    for k in _JOINT_HAS[post, pre]:
+        if kept[k] is None:
+            raise ValueError(f"{k} is required")
+        _vector(kept[k], k, n, torch.float32, dev)
     if grads is None:
         grads = dict(x=_new(f, size), f=_new(f, size))
         if gate is not None:

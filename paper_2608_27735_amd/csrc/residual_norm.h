@@ -26,28 +26,35 @@
 namespace abcd {
 namespace {
 
+// Threads of a workgroup: forward, and backward, where fewer workgroups of more waves leave
+// fewer column sums to be added up.
 template <int G>
 constexpr int kJointThreads = G > kBlock ? G : kBlock;
+template <int G>
+constexpr int kJointBwdThreads = G > 512 ? G : 512;
 
 // Sums of K values over the G lanes of a row, returned to each. `turn` alternates
 // between the two halves of red, so that a wave that writes one again has met the
 // other's barrier, behind all reads.
+constexpr int kJointWaves = 16;  // of a workgroup at most
 template <int G, int K>
-__device__ __forceinline__ void joint_sums(float (&v)[K], float (*red)[K][G / 64 + 1], int& turn) {
+__device__ __forceinline__ void joint_sums(float (&v)[K], float (*red)[K][kJointWaves], int& turn) {
 #pragma unroll
   for (int k = 0; k < K; ++k) v[k] = lanes_sum<(G <= 64 ? G : 64)>(v[k]);
   if (G <= 64) return;
-  float(&r)[K][G / 64 + 1] = red[turn & 1];
+  constexpr int kOf = G > 64 ? G / 64 : 1;  // waves of a row
+  float(&r)[K][kJointWaves] = red[turn & 1];
   ++turn;
+  const int wave = threadIdx.x >> 6, first = wave / kOf * kOf;
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
-    for (int k = 0; k < K; ++k) r[k][threadIdx.x >> 6] = v[k];
+    for (int k = 0; k < K; ++k) r[k][wave] = v[k];
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     float s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < G / 64; ++w) s += r[k][w];
+    for (int w = 0; w < kOf; ++w) s += r[k][first + w];
     v[k] = s;
   }
 }
@@ -80,92 +87,64 @@ __device__ __forceinline__ Floats<N> joint_load(const void* p, int64_t row, int6
       (load_first<T, kWhole>(static_cast<const T*>(p) + row * ld + c, left, room_of(a.n, row, ld, left))), Floats<N>);
 }
 
-// Mean (0 of an RMS norm) and 1 / sd of the row whose columns the lanes hold.
-template <int G, int R, int N>
-__device__ __forceinline__ void joint_stats(const JointArgs& a, const Floats<N> (&v)[R], int t, int kind,
-                                            float (*red)[1][G / 64 + 1], int& turn, float& mean, float& rstd) {
+// Mean (0 of an RMS norm) and 1 / sd of the row whose columns c.. a lane holds.
+template <int G, int N>
+__device__ __forceinline__ void joint_stats(const JointArgs& a, Floats<N> v, int c, int kind, float (*red)[1][kJointWaves],
+                                            int& turn, float& mean, float& rstd) {
   float s[1];
   mean = 0.0f;
   if (kind == ABCD_NORM_LAYER) {
     s[0] = 0.0f;
 #pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-      for (int i = 0; i < N; ++i) s[0] += (j * G + t) * N + i < a.d ? v[j][i] : 0.0f;
+    for (int i = 0; i < N; ++i) s[0] += c + i < a.d ? v[i] : 0.0f;
     joint_sums<G, 1>(s, red, turn);
     mean = joint_mean(s[0], (float)a.d, a.inv_d);
   }
   s[0] = 0.0f;
 #pragma unroll
-  for (int j = 0; j < R; ++j)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float e = (j * G + t) * N + i < a.d ? v[j][i] - mean : 0.0f;
-      s[0] += e * e;
-    }
+  for (int i = 0; i < N; ++i) {
+    const float e = c + i < a.d ? v[i] - mean : 0.0f;
+    s[0] += e * e;
+  }
   joint_sums<G, 1>(s, red, turn);
   rstd = joint_rsqrt(s[0] * a.inv_d + a.eps);
 }
 
-template <typename T, int G, int R, bool kWhole>
+template <typename T, int G, bool kWhole>
 __global__ __launch_bounds__(kJointThreads<G>) void residual_norm_kernel(JointArgs a) {
   constexpr int N = kPer16<T>, kRows = kJointThreads<G> / G;
-  __shared__ float red[2][1][G / 64 + 1];
+  __shared__ float red[2][1][kJointWaves];
   int turn = 0;
-  const int t = threadIdx.x % G;
-  Floats<N> wp[R], bp[R], wn[R], bn[R], sc[R];
-#pragma unroll
-  for (int j = 0; j < R; ++j) {
-    const int c = (j * G + t) * N;
-    wp[j] = joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f);
-    bp[j] = joint_param<T, N, kWhole>(a, a.post_b, c, 0.0f);
-    wn[j] = joint_param<T, N, kWhole>(a, a.pre_w, c, 1.0f);
-    bn[j] = joint_param<T, N, kWhole>(a, a.pre_b, c, 0.0f);
-    sc[j] = joint_param<T, N, kWhole>(a, a.scale, c, 1.0f);
-  }
+  const int t = threadIdx.x % G, c = t * N;
+  const bool inside = c < a.d;
+  const Floats<N> wp = joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f), bp = joint_param<T, N, kWhole>(a, a.post_b, c, 0.0f);
+  const Floats<N> wn = joint_param<T, N, kWhole>(a, a.pre_w, c, 1.0f), bn = joint_param<T, N, kWhole>(a, a.pre_b, c, 0.0f);
+  const Floats<N> sc = joint_param<T, N, kWhole>(a, a.scale, c, 1.0f);
   const int64_t step = (int64_t)gridDim.x * kRows;
+  const int sub = G >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G;
   // Every lane of a row takes part in its sums: rows past the end are worked on as zeros.
   for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += step) {
-    const int64_t row = first + threadIdx.x / G;
+    const int64_t row = first + sub;
     const bool in = row < a.n;
-    Floats<N> v[R], x[R], g[R];
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int c = (j * G + t) * N;
-      v[j] = joint_load<T, N, kWhole>(a.f, row, a.ldf, c, a);
-      x[j] = joint_load<T, N, kWhole>(a.x, row, a.ldx, c, a);
-      g[j] = 1.0f;
-      if (a.gate_mode == 2) g[j] = joint_load<T, N, kWhole>(a.gate, row, a.ldg, c, a);
-    }
-    if (a.gate_mode == 1) {
-      const float one = in ? (float)static_cast<const T*>(a.gate)[row * a.ldg] : 0.0f;
-#pragma unroll
-      for (int j = 0; j < R; ++j) g[j] = one;
-    }
+    Floats<N> v = joint_load<T, N, kWhole>(a.f, row, a.ldf, c, a), x = joint_load<T, N, kWhole>(a.x, row, a.ldx, c, a);
+    Floats<N> g = 1.0f;
+    if (a.gate_mode == 2) g = joint_load<T, N, kWhole>(a.gate, row, a.ldg, c, a);
+    if (a.gate_mode == 1) g = in ? (float)static_cast<const T*>(a.gate)[row * a.ldg] : 0.0f;
     float mean, rstd;
     if (a.post != ABCD_NORM_NONE) {
-      joint_stats<G, R, N>(a, v, t, a.post, red, turn, mean, rstd);
-#pragma unroll
-      for (int j = 0; j < R; ++j) v[j] = (v[j] - mean) * rstd * wp[j] + bp[j];
+      joint_stats<G, N>(a, v, c, a.post, red, turn, mean, rstd);
+      v = (v - mean) * rstd * wp + bp;
       if (t == 0 && in) {
         if (a.post_mean) a.post_mean[row] = mean;
         if (a.post_rstd) a.post_rstd[row] = rstd;
       }
     }
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int c = (j * G + t) * N;
-      v[j] = x[j] + sc[j] * (g[j] * v[j]);
-      if (in && c < a.d) store_vec<T, N, kWhole>(static_cast<T*>(a.y) + row * a.ldy + c, v[j], a.d - c);
-    }
+    v = x + sc * (g * v);
+    if (in && inside) store_vec<T, N, kWhole>(static_cast<T*>(a.y) + row * a.ldy + c, v, a.d - c);
     if (a.pre != ABCD_NORM_NONE) {
-      joint_stats<G, R, N>(a, v, t, a.pre, red, turn, mean, rstd);
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        const int c = (j * G + t) * N;
-        if (in && c < a.d)
-          store_vec<T, N, kWhole>(static_cast<T*>(a.z) + row * a.ldz + c, (v[j] - mean) * rstd * wn[j] + bn[j], a.d - c);
-      }
+      joint_stats<G, N>(a, v, c, a.pre, red, turn, mean, rstd);
+      if (in && inside)
+        store_vec<T, N, kWhole>(static_cast<T*>(a.z) + row * a.ldz + c, (v - mean) * rstd * wn + bn, a.d - c);
       if (t == 0 && in) {
         if (a.pre_mean) a.pre_mean[row] = mean;
         if (a.pre_rstd) a.pre_rstd[row] = rstd;
@@ -180,7 +159,7 @@ constexpr int kWide = 1024;  // threads of a row too long for registers
 template <typename T, bool kWhole>
 __global__ __launch_bounds__(kWide) void residual_norm_wide_kernel(JointArgs a) {
   constexpr int N = kPer16<T>;
-  __shared__ float red[2][1][kWide / 64 + 1];
+  __shared__ float red[2][1][kJointWaves];
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     // the sum over the row of f(its columns c..)
@@ -255,157 +234,159 @@ __device__ __forceinline__ void put_params(const JointArgs& a, int c, Floats<N> 
   put(a.dpre_b, db);
 }
 
-template <typename T, int G, int R, bool kWhole>
-__global__ __launch_bounds__(kJointThreads<G>) void residual_norm_bwd_kernel(JointArgs a) {
-  constexpr int N = kPer16<T>, kThreads = kJointThreads<G>, kRows = kThreads / G, kWaves = kThreads / 64;
-  __shared__ float red2[2][2][G / 64 + 1], red3[2][3][G / 64 + 1];
-  __shared__ float cols[G <= 64 ? kWaves : 1][G <= 64 ? G * R * N : 1];
+// Rows of G lanes, one vector each. The parameters lie in LDS, in fp32, which leaves registers
+// for the next row's values, on their way while one is worked on, and for four waves a SIMD
+// (8,192 x 4,096 in bf16 with a gate an element: 249 us without either; values that spill are
+// dear: 65,536 x 1,024 159 us, with 16 registers in memory 290).
+template <typename T, int G, bool kWhole>
+__global__ __launch_bounds__(kJointBwdThreads<G>, 4) void residual_norm_bwd_kernel(JointArgs a) {
+  constexpr int N = kPer16<T>, kThreads = kJointBwdThreads<G>, kRows = kThreads / G, kWaves = kThreads / 64;
+  constexpr int kGroups = G <= 64 ? kWaves : kRows;  // that hold sums of the same columns
+  typedef typename Frag<T>::type F;
+  __shared__ float red2[2][2][kJointWaves], red3[2][3][kJointWaves];
+  __shared__ __align__(16) float params[4][G * N];  // post's weight and bias, pre's weight, scale
+  __shared__ float cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? G * N : 1];
   int turn2 = 0, turn3 = 0;
-  const int t = threadIdx.x % G;
-  const bool has_pre = a.pre != ABCD_NORM_NONE, has_post = a.post != ABCD_NORM_NONE;
-  Floats<N> wp[R], bp[R], wn[R], sc[R], s1[R], s0[R], dw[R], db[R];
-#pragma unroll
-  for (int j = 0; j < R; ++j) {
-    const int c = (j * G + t) * N;
-    wp[j] = joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f);
-    bp[j] = joint_param<T, N, kWhole>(a, a.post_b, c, 0.0f);
-    wn[j] = joint_param<T, N, kWhole>(a, a.pre_w, c, 1.0f);
-    sc[j] = joint_param<T, N, kWhole>(a, a.scale, c, 1.0f);
-    s1[j] = s0[j] = dw[j] = db[j] = 0.0f;
+  const int t = threadIdx.x % G, c = t * N;
+  const bool has_pre = a.pre != ABCD_NORM_NONE, has_post = a.post != ABCD_NORM_NONE, inside = c < a.d;
+  if ((int)threadIdx.x < G) {
+    store_vec<float, N, true>(&params[0][c], joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f), N);
+    store_vec<float, N, true>(&params[1][c], joint_param<T, N, kWhole>(a, a.post_b, c, 0.0f), N);
+    store_vec<float, N, true>(&params[2][c], joint_param<T, N, kWhole>(a, a.pre_w, c, 1.0f), N);
+    store_vec<float, N, true>(&params[3][c], joint_param<T, N, kWhole>(a, a.scale, c, 1.0f), N);
   }
-  const int64_t step = (int64_t)gridDim.x * kRows;
-  for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += step) {
-    const int64_t row = first + threadIdx.x / G;
+  __syncthreads();
+  auto param = [&](int k) { return *reinterpret_cast<const Floats<N>*>(&params[k][c]); };
+  Floats<N> s1 = 0.0f, s0 = 0.0f, dw = 0.0f, db = 0.0f;
+  F ndy, ndz, ny, nf;
+  float nmean, nrstd, npm, npr, none;
+  auto load = [&](const void* p, int64_t row, int64_t ld, bool wanted) {
+    const int left = row < a.n && wanted ? a.d - c : 0;
+    return load_frag<T, kWhole>(static_cast<const T*>(p) + row * ld + c, left, room_of(a.n, row, ld, left));
+  };
+  auto fetch = [&](int64_t row) {
     const bool in = row < a.n;
-    Floats<N> g[R], h[R], v[R], f[R], gate[R];
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int c = (j * G + t) * N;
-      g[j] = v[j] = h[j] = 0.0f;
-      if (a.dy) g[j] = joint_load<T, N, kWhole>(a.dy, row, a.lddy, c, a);
-      if (has_pre) {
-        v[j] = joint_load<T, N, kWhole>(a.dz, row, a.lddz, c, a);
-        h[j] = joint_load<T, N, kWhole>(a.y, row, a.ldy, c, a);
-      }
-      f[j] = joint_load<T, N, kWhole>(a.f, row, a.ldf, c, a);
-      gate[j] = 1.0f;
-      if (a.gate_mode == 2) gate[j] = joint_load<T, N, kWhole>(a.gate, row, a.ldg, c, a);
-    }
-    float one = 1.0f;
-    if (a.gate_mode == 1) one = in ? (float)static_cast<const T*>(a.gate)[row * a.ldg] : 0.0f;
+    ndy = load(a.dy, row, a.lddy, a.dy != nullptr);
+    ndz = load(a.dz, row, a.lddz, has_pre);
+    ny = load(a.y, row, a.ldy, has_pre);
+    nf = load(a.f, row, a.ldf, true);
+    nmean = in && a.pre == ABCD_NORM_LAYER ? a.pre_mean[row] : 0.0f;
+    nrstd = in && has_pre ? a.pre_rstd[row] : 0.0f;
+    npm = in && a.post == ABCD_NORM_LAYER ? a.post_mean[row] : 0.0f;
+    npr = in && has_post ? a.post_rstd[row] : 1.0f;
+    none = a.gate_mode == 1 && in ? (float)static_cast<const T*>(a.gate)[row * a.ldg] : 1.0f;
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t first = (int64_t)blockIdx.x * kRows;
+  constexpr bool kAhead = G > 64;  // short rows have waves enough without, and need their registers
+  // (of whole waves the row is a scalar, and so are its addresses)
+  const int sub = G >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G;
+  if (kAhead) fetch(first + sub);
+  for (; first < a.n; first += step) {
+    const int64_t row = first + sub;
+    const bool in = row < a.n && inside;
+    if (!kAhead) fetch(row);
+    const float mean = nmean, rstd = nrstd, pm = npm, pr = npr, one = none;
+    auto value = [&](F v) { return __builtin_convertvector((first_of<T, kWhole>(v, a.d - c)), Floats<N>); };
+    Floats<N> g = value(ndy), v = value(ndz), h = value(ny);
+    const F rf = nf, rg = load(a.gate, row, a.ldg, a.gate_mode == 2);  // the gate is needed last
+    if (kAhead) fetch(row + step);
     if (has_pre) {
-      const float mean = in && a.pre == ABCD_NORM_LAYER ? a.pre_mean[row] : 0.0f, rstd = in ? a.pre_rstd[row] : 0.0f;
       float s[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int j = 0; j < R; ++j) {
-        const int c = (j * G + t) * N;
+      for (int i = 0; i < N; ++i) h[i] = c + i < a.d ? (h[i] - mean) * rstd : 0.0f;
+      dw += v * h;
+      db += v;
+      v *= param(2);
 #pragma unroll
-        for (int i = 0; i < N; ++i) h[j][i] = c + i < a.d ? (h[j][i] - mean) * rstd : 0.0f;
-        dw[j] += v[j] * h[j];
-        db[j] += v[j];
-        v[j] *= wn[j];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          s[0] += v[j][i];
-          s[1] += v[j][i] * h[j][i];
-        }
+      for (int i = 0; i < N; ++i) {
+        s[0] += v[i];
+        s[1] += v[i] * h[i];
       }
       joint_sums<G, 2>(s, red2, turn2);
       const float c1 = a.pre == ABCD_NORM_LAYER ? s[0] * a.inv_d : 0.0f, c2 = s[1] * a.inv_d;
-#pragma unroll
-      for (int j = 0; j < R; ++j) g[j] += rstd * (v[j] - c1 - h[j] * c2);
+      g += rstd * (v - c1 - h * c2);
     }
-    const float pm = in && a.post == ABCD_NORM_LAYER ? a.post_mean[row] : 0.0f, pr = has_post && in ? a.post_rstd[row] : 1.0f;
+    if (a.dx && in) store_vec<T, N, kWhole>(static_cast<T*>(a.dx) + row * a.lddx + c, g, a.d - c);
+    Floats<N> f = value(rf);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool there = row < a.n && c + i < a.d;
+      f[i] = there ? (f[i] - pm) * pr : 0.0f;
+      g[i] = there ? g[i] : 0.0f;
+    }
+    const Floats<N> wp = param(0), sc = param(3);
+    const Floats<N> by = g * sc * (f * wp + param(1));  // the gate's
+    if (a.dgate && a.gate_mode == 2 && in) store_vec<T, N, kWhole>(static_cast<T*>(a.dgate) + row * a.lddg + c, by, a.d - c);
+    if (a.gate_mode == 2)
+      g *= value(rg);
+    else
+      g *= one;
+    s1 += g * f;
+    s0 += g;
+    g *= sc * wp;
     float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int c = (j * G + t) * N;
-      if (a.dx && in && c < a.d) store_vec<T, N, kWhole>(static_cast<T*>(a.dx) + row * a.lddx + c, g[j], a.d - c);
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const bool there = in && c + i < a.d;
-        f[j][i] = there ? (f[j][i] - pm) * pr : 0.0f;
-        g[j][i] = there ? g[j][i] : 0.0f;
-      }
-      if (a.gate_mode == 1) gate[j] = one;
-      const Floats<N> by = g[j] * sc[j] * (f[j] * wp[j] + bp[j]);  // the gate's
-      if (a.dgate && a.gate_mode == 2 && in && c < a.d)
-        store_vec<T, N, kWhole>(static_cast<T*>(a.dgate) + row * a.lddg + c, by, a.d - c);
-      g[j] *= gate[j];
-      s1[j] += g[j] * f[j];
-      s0[j] += g[j];
-      g[j] *= sc[j] * wp[j];
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        s[0] += g[j][i];
-        s[1] += g[j][i] * f[j][i];
-        s[2] += by[i];
-      }
+    for (int i = 0; i < N; ++i) {
+      s[0] += g[i];
+      s[1] += g[i] * f[i];
+      s[2] += by[i];
     }
     if (has_post || a.gate_mode == 1) joint_sums<G, 3>(s, red3, turn3);
-    if (a.dgate && a.gate_mode == 1 && in && t == 0) static_cast<T*>(a.dgate)[row * a.lddg] = (T)s[2];
-    if (a.df) {
+    if (a.dgate && a.gate_mode == 1 && row < a.n && t == 0) static_cast<T*>(a.dgate)[row * a.lddg] = (T)s[2];
+    if (a.df && in) {
       const float c1 = a.post == ABCD_NORM_LAYER ? s[0] * a.inv_d : 0.0f, c2 = has_post ? s[1] * a.inv_d : 0.0f;
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        const int c = (j * G + t) * N;
-        if (in && c < a.d)
-          store_vec<T, N, kWhole>(static_cast<T*>(a.df) + row * a.lddf + c, pr * (g[j] - c1 - f[j] * c2), a.d - c);
-      }
+      store_vec<T, N, kWhole>(static_cast<T*>(a.df) + row * a.lddf + c, pr * (g - c1 - f * c2), a.d - c);
     }
   }
   if (!a.part && gridDim.x > 1) return;  // no parameter's gradient is wanted
-  if (G > 64) {
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int c = (j * G + t) * N;
-      if (c >= a.d) continue;
-      if (gridDim.x == 1) {
-        put_params<T, N, kWhole>(a, c, s1[j], s0[j], dw[j], db[j]);
-        continue;
-      }
-      float* const p = a.part + (int64_t)blockIdx.x * 4 * a.pitch + c;
-      store_vec<float, N, true>(p, s1[j], N);
-      store_vec<float, N, true>(p + a.pitch, s0[j], N);
-      store_vec<float, N, true>(p + 2 * a.pitch, dw[j], N);
-      store_vec<float, N, true>(p + 3 * a.pitch, db[j], N);
+  if (kGroups == 1) {
+    if (!inside) return;
+    if (gridDim.x == 1) {
+      put_params<T, N, kWhole>(a, c, s1, s0, dw, db);
+      return;
     }
+    float* const p = a.part + (int64_t)blockIdx.x * 4 * a.pitch + c;
+    store_vec<float, N, true>(p, s1, N);
+    store_vec<float, N, true>(p + a.pitch, s0, N);
+    store_vec<float, N, true>(p + 2 * a.pitch, dw, N);
+    store_vec<float, N, true>(p + 3 * a.pitch, db, N);
     return;
   }
-  // the wave's groups added across the lanes, then the waves' sums through LDS
-  constexpr int kTurns = (G * R * N + kThreads - 1) / kThreads;
+  // a wave's rows added across the lanes, then the groups' sums through LDS
+  constexpr int kTurns = (G * N + kThreads - 1) / kThreads;
   float own[4][kTurns];
 #pragma unroll
   for (int which = 0; which < 4; ++which) {
+    const Floats<N> v = which == 0 ? s1 : which == 1 ? s0 : which == 2 ? dw : db;
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const Floats<N> v = which == 0 ? s1[j] : which == 1 ? s0[j] : which == 2 ? dw[j] : db[j];
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float e = v[i];
-        for (int off = G; off < 64; off *= 2) e += __shfl_xor(e, off, 64);
-        if ((threadIdx.x & 63) < G) cols[threadIdx.x >> 6][(j * G + t) * N + i] = e;
-      }
+    for (int i = 0; i < N; ++i) {
+      float e = v[i];
+      for (int off = G; off < 64; off *= 2) e += __shfl_xor(e, off, 64);
+      if (G > 64)
+        cols[threadIdx.x / G][c + i] = e;
+      else if ((threadIdx.x & 63) < G)
+        cols[threadIdx.x >> 6][c + i] = e;
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kTurns; ++k) {
-      const int c = k * kThreads + threadIdx.x;
+      const int at = k * kThreads + threadIdx.x;
       own[which][k] = 0.0f;
-      if (c < a.d && c < G * R * N)
-        for (int w = 0; w < kWaves; ++w) own[which][k] += cols[w][c];
+      if (at < a.d && at < G * N)
+        for (int w = 0; w < kGroups; ++w) own[which][k] += cols[w][at];
     }
     __syncthreads();
   }
 #pragma unroll
   for (int k = 0; k < kTurns; ++k) {
-    const int c = k * kThreads + threadIdx.x;
-    if (c >= a.d) continue;
+    const int at = k * kThreads + threadIdx.x;
+    if (at >= a.d) continue;
     if (gridDim.x == 1)
-      put_params<T, 1, true>(a, c, Floats<1>(own[0][k]), Floats<1>(own[1][k]), Floats<1>(own[2][k]), Floats<1>(own[3][k]));
+      put_params<T, 1, true>(a, at, Floats<1>(own[0][k]), Floats<1>(own[1][k]), Floats<1>(own[2][k]), Floats<1>(own[3][k]));
     else
 #pragma unroll
-      for (int which = 0; which < 4; ++which) a.part[((int64_t)blockIdx.x * 4 + which) * a.pitch + c] = own[which][k];
+      for (int which = 0; which < 4; ++which) a.part[((int64_t)blockIdx.x * 4 + which) * a.pitch + at] = own[which][k];
   }
 }
 
@@ -413,7 +394,7 @@ __global__ __launch_bounds__(kJointThreads<G>) void residual_norm_bwd_kernel(Joi
 template <typename T, bool kWhole>
 __global__ __launch_bounds__(kWide) void residual_norm_bwd_wide_kernel(JointArgs a) {
   constexpr int N = kPer16<T>;
-  __shared__ float red2[2][2][kWide / 64 + 1], red3[2][3][kWide / 64 + 1];
+  __shared__ float red2[2][2][kJointWaves], red3[2][3][kJointWaves];
   int turn2 = 0, turn3 = 0;
   const bool has_pre = a.pre != ABCD_NORM_NONE, has_post = a.post != ABCD_NORM_NONE;
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
@@ -495,45 +476,50 @@ __global__ __launch_bounds__(kWide) void residual_norm_bwd_wide_kernel(JointArgs
   }
 }
 
-// The workgroups' column sums added up in order: 64 columns a workgroup, the parts dealt
-// to its waves.
-constexpr int kJointPartWaves = 16;
+// The workgroups' column sums added up in order: 16 columns of all four a workgroup, the parts
+// dealt to its waves (256 parts of 1,001 columns: with 64 columns a workgroup 10.6 us).
+constexpr int kJointPartWaves = 16, kJointPartCols = 16;
 template <typename T>
 __global__ __launch_bounds__(kJointPartWaves* kWave) void residual_norm_sums_kernel(JointArgs a, int64_t parts) {
-  __shared__ float red[kJointPartWaves][4][kWave];
-  const int w = threadIdx.x / kWave, l = threadIdx.x % kWave, c = (int)blockIdx.x * kWave + l;
-  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (c < a.d)
-#pragma unroll 4
-    for (int64_t p = w; p < parts; p += kJointPartWaves)
+  __shared__ float red[kJointPartWaves][kWave];
+  const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+  const int which = l / kJointPartCols, first = (int)blockIdx.x * kJointPartCols, c = first + l % kJointPartCols;
+  float s = 0.0f;
+  if (c < a.d) {
+    int64_t p = w;
+    for (; p + 7 * kJointPartWaves < parts; p += 8 * kJointPartWaves) {
+      float v[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) s[k] += a.part[(p * 4 + k) * a.pitch + c];
+      for (int u = 0; u < 8; ++u) v[u] = a.part[((p + u * kJointPartWaves) * 4 + which) * a.pitch + c];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) red[w][k][l] = s[k];
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; p < parts; p += kJointPartWaves) s += a.part[(p * 4 + which) * a.pitch + c];
+  }
+  red[w][l] = s;
   __syncthreads();
-  if (w != 0 || c >= a.d) return;
-  for (int v = 1; v < kJointPartWaves; ++v)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s[k] += red[v][k][l];
-  put_params<T, 1, true>(a, c, Floats<1>(s[0]), Floats<1>(s[1]), Floats<1>(s[2]), Floats<1>(s[3]));
+  if (w == 0) {
+    for (int v = 1; v < kJointPartWaves; ++v) s += red[v][l];
+    red[0][l] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x < kJointPartCols)  // (put_params leaves out what lies past the row's end)
+    put_params<T, 1, true>(a, first + l, Floats<1>(red[0][l]), Floats<1>(red[0][kJointPartCols + l]),
+                           Floats<1>(red[0][2 * kJointPartCols + l]), Floats<1>(red[0][3 * kJointPartCols + l]));
 }
 
-// Rows of G lanes by R vectors that a kernel is compiled for; f(shape) with the
-// smallest that holds nvec, and false if none does.
-template <int G, int R>
-struct JointShape {
-  static constexpr int g = G, r = R;
-};
+// Lanes of a row that a kernel is compiled for; f with the fewest that hold nvec vectors, and
+// false if none do.
 template <typename F>
-bool with_joint_shape(int nvec, F f) {
-  if (nvec <= 8) return f(JointShape<8, 1>{}), true;
-  if (nvec <= 16) return f(JointShape<16, 1>{}), true;
-  if (nvec <= 32) return f(JointShape<32, 1>{}), true;
-  if (nvec <= 64) return f(JointShape<64, 1>{}), true;
-  if (nvec <= 128) return f(JointShape<64, 2>{}), true;
-  if (nvec <= 256) return f(JointShape<256, 1>{}), true;
-  if (nvec <= 512) return f(JointShape<512, 1>{}), true;
-  if (nvec <= 1024) return f(JointShape<1024, 1>{}), true;
+bool with_joint_lanes(int nvec, F f) {
+  if (nvec <= 8) return f(std::integral_constant<int, 8>{}), true;
+  if (nvec <= 16) return f(std::integral_constant<int, 16>{}), true;
+  if (nvec <= 32) return f(std::integral_constant<int, 32>{}), true;
+  if (nvec <= 64) return f(std::integral_constant<int, 64>{}), true;
+  if (nvec <= 128) return f(std::integral_constant<int, 128>{}), true;
+  if (nvec <= 256) return f(std::integral_constant<int, 256>{}), true;
+  if (nvec <= 512) return f(std::integral_constant<int, 512>{}), true;
+  if (nvec <= 1024) return f(std::integral_constant<int, 1024>{}), true;
   return false;
 }
 
@@ -541,13 +527,13 @@ template <typename T>
 int32_t run_joint(const JointArgs& a, hipStream_t stream) {
   const int nvec = (int)((a.d + kPer16<T> - 1) / kPer16<T>);
   const bool whole = a.d % kPer16<T> == 0;
-  const bool held = with_joint_shape(nvec, [&](auto shape) {
-    constexpr int G = decltype(shape)::g, R = decltype(shape)::r, kThreads = kJointThreads<G>;
+  const bool held = with_joint_lanes(nvec, [&](auto lanes) {
+    constexpr int G = decltype(lanes)::value, kThreads = kJointThreads<G>;
     const int64_t rows = kThreads / G, blocks = std::min<int64_t>((a.n + rows - 1) / rows, G > 64 ? 4096 : 2048);
     if (whole)
-      ABCD_LAUNCH("residual_norm", (residual_norm_kernel<T, G, R, true>), blocks, kThreads, 0, stream, a);
+      ABCD_LAUNCH("residual_norm", (residual_norm_kernel<T, G, true>), blocks, kThreads, 0, stream, a);
     else
-      ABCD_LAUNCH("residual_norm", (residual_norm_kernel<T, G, R, false>), blocks, kThreads, 0, stream, a);
+      ABCD_LAUNCH("residual_norm", (residual_norm_kernel<T, G, false>), blocks, kThreads, 0, stream, a);
   });
   if (!held) {
     const int64_t blocks = std::min<int64_t>(a.n, 1024);
@@ -566,12 +552,12 @@ int32_t run_joint_bwd(const JointArgs& a, int64_t blocks, hipStream_t stream) {
   const bool whole = a.d % kPer16<T> == 0;
   bool summed = blocks == 1;
   if (a.n > 0) {
-    const bool held = with_joint_shape(nvec, [&](auto shape) {
-      constexpr int G = decltype(shape)::g, R = decltype(shape)::r, kThreads = kJointThreads<G>;
+    const bool held = with_joint_lanes(nvec, [&](auto lanes) {
+      constexpr int G = decltype(lanes)::value, kThreads = kJointBwdThreads<G>;
       if (whole)
-        ABCD_LAUNCH("residual_norm_bwd", (residual_norm_bwd_kernel<T, G, R, true>), blocks, kThreads, 0, stream, a);
+        ABCD_LAUNCH("residual_norm_bwd", (residual_norm_bwd_kernel<T, G, true>), blocks, kThreads, 0, stream, a);
       else
-        ABCD_LAUNCH("residual_norm_bwd", (residual_norm_bwd_kernel<T, G, R, false>), blocks, kThreads, 0, stream, a);
+        ABCD_LAUNCH("residual_norm_bwd", (residual_norm_bwd_kernel<T, G, false>), blocks, kThreads, 0, stream, a);
     });
     if (!held) {
       summed = false;
@@ -583,8 +569,8 @@ int32_t run_joint_bwd(const JointArgs& a, int64_t blocks, hipStream_t stream) {
     ABCD_HIP(hipGetLastError());
   }
   if (a.part && (!summed || a.n == 0)) {
-    ABCD_LAUNCH("residual_norm_sums", (residual_norm_sums_kernel<T>), (a.d + kWave - 1) / kWave, kJointPartWaves * kWave, 0,
-                stream, a, a.n == 0 ? 0 : blocks);
+    ABCD_LAUNCH("residual_norm_sums", (residual_norm_sums_kernel<T>), (a.d + kJointPartCols - 1) / kJointPartCols,
+                kJointPartWaves * kWave, 0, stream, a, a.n == 0 ? 0 : blocks);
     ABCD_HIP(hipGetLastError());
   }
   return ABCD_OK;
