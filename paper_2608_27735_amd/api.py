@@ -999,9 +999,10 @@ def linear(x, w, b=None, act=None, residual=None, save=False, out=None, workspac
     lib = _lib.load()
     sz = C.c_size_t(0)
     check(lib.abcd_linear_workspace_size(C.byref(layer), n, C.byref(sz)))
-    workspace = _workspace(workspace, sz.value, dev)
+    if workspace is not None or sz.value > 0:
+        workspace = _workspace(workspace, sz.value, dev)
     check(lib.abcd_linear(C.byref(layer), n, x.data_ptr(), ldx, _ptr(residual), ldr, out.data_ptr(), ldy,
-                          _ptr(saved), workspace.data_ptr(), workspace.numel(), _stream()))
+                          _ptr(saved), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
     return dict(y=out, saved=saved)
 
 

@@ -387,7 +387,8 @@ int32_t abcd_linear(const abcd_layer* layer, int64_t n, const void* x, int64_t l
   TRY_STATUS(check_matrix("x", x, l.dtype, n, l.i, ldx, false));
   TRY_STATUS(check_matrix("residual", residual, l.dtype, n, l.o, ldr, true));
   TRY_STATUS(check_matrix("y", y, l.dtype, n, l.o, ldy, false));
-  if (n > 0) TRY_STATUS(check_workspace(workspace, ws_bytes, linear_workspace_bytes(l, n, false)));
+  const size_t need = linear_workspace_bytes(l, n, false);
+  if (n > 0 && need > 0) TRY_STATUS(check_workspace(workspace, ws_bytes, need));
   return launch_linear(l, n, x, ldx, residual, ldr, y, ldy, slope, workspace, stream);
 }
 
@@ -406,7 +407,8 @@ int32_t abcd_linear_bwd(const abcd_layer* layer, int64_t n, const void* dy, int6
   TRY_STATUS(check_matrix("dx", dx, l.dtype, n, l.i, lddx, true));
   TRY_STATUS(check_vector("dw", dw, l.dtype));
   TRY_STATUS(check_vector("db", db, l.dtype));
-  TRY_STATUS(check_workspace(workspace, ws_bytes, linear_workspace_bytes(l, n, true)));
+  const size_t need = linear_workspace_bytes(l, n, true);
+  if (need > 0) TRY_STATUS(check_workspace(workspace, ws_bytes, need));
   return launch_linear_bwd(l, n, dy, lddy, x, ldx, q, e, slope, dx, lddx, dw, db, workspace, stream);
 }
 

@@ -10,7 +10,7 @@
 #include "activation.h"
 #include "gated_ffn_few.h"
 #include "linear_args.h"
-#include "product.h"
+#include "dweight.h"
 
 namespace abcd {
 namespace {
@@ -118,16 +118,18 @@ struct LinearDxEnd {
   }
 };
 
-// Few rows: the weights are read once and bound it (gated_ffn_few.h).
-template <typename T, int kAct, int kX, bool kWhole>
-__global__ __launch_bounds__(kFewOutWaves * 64) void linear_few_kernel(LinearOut a) {
+// Few rows: the weights are read once and bound it (gated_ffn_few.h). 8 waves a workgroup where
+// rows of the weights are short, else 16 (one row in bf16, weights from memory: 2,048 to 5,632
+// 8.6 against 10.7 us, 512 to 1,376 4.3 against 5.3, but 5,632 to 2,048 10.2 against 10.0 and
+// 33 rows of 2,048 to 2,048 12.7 against 10.4).
+template <typename T, int kAct, int kX, int kWaves, bool kWhole>
+__global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, int columns) {
   f32x4 acc[kX][1], sum[1];
-  const int columns = (int64_t)gridDim.x * 8 >= a.o ? 8 : 16;
   const int first = blockIdx.x * columns, end = min((int)a.o, first + columns), n = (int)a.x.len;
   const T* const w[1] = {static_cast<const T*>(a.w.p[0])};
-  few_products<T, kX, 1, kFewOutWaves, kWhole>(acc, static_cast<const T*>(a.x.p[0]), a.x.ld, n, w, a.w.ld, first, end,
+  few_products<T, kX, 1, kWaves, kWhole>(acc, static_cast<const T*>(a.x.p[0]), a.x.ld, n, w, a.w.ld, first, end,
                                                (int)a.i);
-  if (!few_join<kX, 1, kFewOutWaves>(acc, sum)) return;
+  if (!few_join<kX, 1, kWaves>(acc, sum)) return;
   const int l = threadIdx.x & 63, r = (threadIdx.x >> 6) * 16 + (l & 15), c = first + (l >> 4) * 4;
   const int left = end - c;
   if (r >= n || left <= 0) return;
@@ -202,11 +204,19 @@ int32_t run_linear_few(const LinearOut& a, hipStream_t stream) {
   return with_any_act(a.act, [&](auto act) -> int32_t {
     return with_rows(a.x.len, [&](auto rows) -> int32_t {
       constexpr int kAct = decltype(act)::value, kX = decltype(rows)::value;
-      const int64_t grid = (a.o + 7) / 8 <= kCUs ? (a.o + 7) / 8 : (a.o + 15) / 16;
-      if (a.i % kPer16<T> == 0)
-        ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, true>), grid, kFewOutWaves * 64, 0, stream, a);
+      const int columns = (a.o + 7) / 8 <= kCUs ? 8 : 16;
+      const int64_t grid = (a.o + columns - 1) / columns;
+      auto launch = [&](auto waves) {
+        constexpr int kWaves = decltype(waves)::value;
+        if (a.i % kPer16<T> == 0)
+          ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, kWaves, true>), grid, kWaves * 64, 0, stream, a, columns);
+        else
+          ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, kWaves, false>), grid, kWaves * 64, 0, stream, a, columns);
+      };
+      if (kX == 1 && a.i * (int64_t)sizeof(T) <= 4096)
+        launch(std::integral_constant<int, kX == 1 ? 8 : 16>{});
       else
-        ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, false>), grid, kFewOutWaves * 64, 0, stream, a);
+        launch(std::integral_constant<int, 16>{});
       ABCD_HIP(hipGetLastError());
       return ABCD_OK;
     });
@@ -224,6 +234,7 @@ int32_t run_linear_slope(const LinearSlope& a, int64_t parts, hipStream_t stream
 }  // namespace
 
 #define ABCD_LINEAR_KERNELS(NAME, TYPE)                                                                    \
+  int32_t linear_dw_##NAME(const FfnDWeight& a, hipStream_t s) { return run_dweight<TYPE, true>(a, s); }   \
   int32_t linear_out_##NAME(const LinearOut& a, hipStream_t s) { return run_linear_out<TYPE>(a, s); }      \
   int32_t linear_few_##NAME(const LinearOut& a, hipStream_t s) { return run_linear_few<TYPE>(a, s); }      \
   int32_t linear_dz_##NAME(const LinearDz& a, hipStream_t s) { return run_linear_dz<TYPE>(a, s); }         \

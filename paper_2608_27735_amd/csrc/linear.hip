@@ -30,8 +30,15 @@ size_t dweight_part(const abcd_layer& l, int64_t steps) {
   return std::max(room(256, kBigSlots), room(128, kSmallSlots));
 }
 
-// Whether the narrow kernels do, in 16-bit types.
-bool narrow(const abcd_layer& l, int64_t n) { return l.dtype != ABCD_F32 && narrow_layer(l.i, l.o) && n > 64; }
+// Whether the narrow kernels do, in 16-bit types: wherever they hold the layer (bf16, SiLU,
+// forward of 300,000 x 100 to 200 67 us, by the tiles 112, 1M x 130 to 20 101 against 324, 1,000 x 64
+// to 64 9.8 against 11.0; backward of 20,000 x 64 to 64 18 against 31, 1,000 x 61 to 127 27.6 against
+// 32.2), but forward not of long rows that are no whole vectors, whose weights take a load an
+// element (300,000 x 200 to 100 80 against 71, 20,000 18 against 12).
+bool narrow(const abcd_layer& l, int64_t n) {
+  return l.dtype != ABCD_F32 && narrow_layer(l.i, l.o) && n > 64 &&
+         (l.i <= 128 || l.o <= 64 || (l.i % 8 == 0 && l.o % 8 == 0));
+}
 bool narrow_bwd(const abcd_layer& l, int64_t n) { return l.dtype != ABCD_F32 && narrow_layer_bwd(l.i, l.o) && n > 0; }
 int64_t narrow_blocks(int64_t n) { return std::min<int64_t>((n + 127) / 128, 4 * kCUs); }
 int64_t narrow_bwd_blocks(int64_t n) { return std::min<int64_t>((n + 127) / 128, 2 * kCUs); }
@@ -70,9 +77,8 @@ Scratch layout(const abcd_layer& l, int64_t n, bool backward, void* workspace) {
 
 }  // namespace
 
-// Never 0, also of a call that needs none: which those are is not the caller's to know.
 size_t linear_workspace_bytes(const abcd_layer& l, int64_t n, bool backward) {
-  return std::max<size_t>(256, layout(l, n, backward, nullptr).bytes);
+  return layout(l, n, backward, nullptr).bytes;
 }
 
 int32_t launch_linear(const abcd_layer& l, int64_t n, const void* x, int64_t ldx, const void* residual, int64_t ldr,
@@ -147,7 +153,7 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
     a.part = s.part;
     a.n = n;
     a.one[a.count++] = FfnDWeight::One{dz.p[0], xs.p[0], dw, dz.ld, l.o, xs.ld, l.i, 1.0f, 0, 0, 0};
-    TRY_STATUS(LINEAR_BY_TYPE(l, ffn_dweight, a, stream));
+    TRY_STATUS(LINEAR_BY_TYPE(l, linear_dw, a, stream));
   }
   if (slope && db && n > 0) {
     SumOuts outs{};

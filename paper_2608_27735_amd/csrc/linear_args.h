@@ -69,8 +69,8 @@ struct LinearNarrowBwd {
   int64_t n, i, o, ldx, lddy, ldslope, lddx;
   int act;
 };
-inline bool narrow_layer(int64_t i, int64_t o) { return i <= 128 && o <= 128; }
-inline bool narrow_layer_bwd(int64_t i, int64_t o) { return narrow_layer(i, o) && (i <= 64 || o <= 64); }
+inline bool narrow_layer(int64_t i, int64_t o) { return i <= 256 && o <= 256 && (i <= 128 || o <= 128); }
+inline bool narrow_layer_bwd(int64_t i, int64_t o) { return i <= 128 && o <= 128 && (i <= 64 || o <= 64); }
 int32_t linear_narrow_f16(const LinearNarrow&, int64_t blocks, hipStream_t);
 int32_t linear_narrow_bf16(const LinearNarrow&, int64_t blocks, hipStream_t);
 int32_t linear_narrow_bwd_f16(const LinearNarrowBwd&, int64_t blocks, hipStream_t);
@@ -81,6 +81,7 @@ int32_t linear_narrow_bwd_bf16(const LinearNarrowBwd&, int64_t blocks, hipStream
   int32_t linear_few_##NAME(const LinearOut&, hipStream_t);     \
   int32_t linear_dz_##NAME(const LinearDz&, hipStream_t);       \
   int32_t linear_dx_##NAME(const LinearDx&, hipStream_t);       \
+  int32_t linear_dw_##NAME(const FfnDWeight&, hipStream_t);     \
   int32_t linear_slope_##NAME(const LinearSlope&, int64_t parts, hipStream_t);
 ABCD_LINEAR_DECLARE(f32)
 ABCD_LINEAR_DECLARE(f16)

@@ -391,6 +391,9 @@ int32_t run_linear_narrow(const LinearNarrow& a, int64_t blocks, hipStream_t str
     std::integral_constant<int, 2> i2;
     std::integral_constant<int, 4> i4;
     std::integral_constant<int, 8> i8;
+    std::integral_constant<int, 16> i16;
+    if (a.o > 128) return launch(i4, i16);
+    if (a.i > 128) return a.o > 64 ? launch(i8, i8) : launch(i8, i4);
     if (a.o > 64) return launch(i4, i8);
     return a.i > 64 ? launch(i4, i4) : launch(i2, i4);
   });

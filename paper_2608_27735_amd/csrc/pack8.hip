@@ -96,8 +96,11 @@ __global__ __launch_bounds__(kBlock) void unpack8_kernel(PackArgs a) {
   }
 }
 
-// Threads along a row of nvec vectors: as many as leave the fewest idle in its last round.
-int row_lanes(int nvec, int least) {
+// Threads along a row of nvec vectors: as many as leave the fewest idle in its last round;
+// eight at least where the row has them, so that a wave's accesses cover lines.
+int row_lanes(int nvec) {
+  int least = 1;
+  while (least < 8 && least < nvec) least *= 2;
   int best = 1 << 30, lanes = least;
   for (int l = least; l <= kBlock; l *= 2) {
     const int used = (nvec + l - 1) / l * l;
@@ -114,7 +117,7 @@ int32_t launch_pack8(int32_t dtype, int64_t n, int64_t d, const void* x, int64_t
   PackArgs a{x, nullptr, q, e, ldx, n, (int)d, (int)pack_blocks(d), 0};
   return with_type(dtype, [&](auto z) -> int32_t {
     typedef decltype(z) T;
-    a.lanes = row_lanes(a.blocks * kPackBlock / kPer16<T>, 8);
+    a.lanes = std::max(row_lanes(a.blocks * kPackBlock / kPer16<T>), 8);  // those of a block at least
     const int64_t rows = kBlock / a.lanes, blocks = std::min<int64_t>((n + rows - 1) / rows, 1 << 20);
     if (d % kPer16<T> == 0)
       ABCD_LAUNCH("pack8", (pack8_kernel<T, true>), blocks, kBlock, 0, stream, a);
@@ -131,7 +134,7 @@ int32_t launch_unpack8(int32_t dtype, int64_t n, int64_t d, const int8_t* q, con
   PackArgs a{nullptr, y, const_cast<int8_t*>(q), const_cast<uint8_t*>(e), ldy, n, (int)d, (int)pack_blocks(d), 0};
   return with_type(dtype, [&](auto z) -> int32_t {
     typedef decltype(z) T;
-    a.lanes = row_lanes((int)((d + kPer16<T> - 1) / kPer16<T>), 1);
+    a.lanes = row_lanes((int)((d + kPer16<T> - 1) / kPer16<T>));
     const int64_t rows = kBlock / a.lanes, blocks = std::min<int64_t>((n + rows - 1) / rows, 1 << 20);
     if (d % kPer16<T> == 0)
       ABCD_LAUNCH("unpack8", (unpack8_kernel<T, true>), blocks, kBlock, 0, stream, a);

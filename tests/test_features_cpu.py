@@ -180,17 +180,20 @@ BAD_LAYERS = [dict(dtype=3), dict(act=5), dict(act=-1), dict(i=0), dict(i=65537)
 
 def test_linear_refuses(lib):
     l, need = layer(), C.c_size_t(0)
+    assert lib.abcd_linear_workspace_size(C.byref(l), 4, C.byref(need)) == 0 and need.value == 0  # of a few rows
     for size in (lib.abcd_linear_workspace_size, lib.abcd_linear_bwd_workspace_size):
-        assert size(C.byref(l), 4, C.byref(need)) == 0 and need.value >= 256
+        assert size(C.byref(layer(i=300)), 400, C.byref(need)) == 0 and need.value >= 400
         refuse([C.byref(l), 4, C.byref(need)], size,
                [(0, None), (1, -1), (1, (1 << 30) + 1), (2, None)] + [(0, C.byref(layer(**kw))) for kw in BAD_LAYERS])
+    l = layer(i=300)
     lib.abcd_linear_workspace_size(C.byref(l), 400, C.byref(need))
-    base = [C.byref(l), 400, FAKE, 8, FAKE, 5, FAKE, 5, FAKE, FAKE, need.value, None]
+    base = [C.byref(l), 400, FAKE, 300, FAKE, 5, FAKE, 5, FAKE, FAKE, need.value, None]
     bad = BAD_LAYERS + [dict(w=None), dict(w=FAKE + 1), dict(b=FAKE + 1)]
     refuse(base, lib.abcd_linear,
            [(0, C.byref(layer(**kw))) for kw in bad] +
-           [(0, None), (1, -1), (2, None), (2, FAKE + 1), (3, 7), (4, FAKE + 1), (5, 4), (6, None), (7, 4), (8, FAKE + 8),
+           [(0, None), (1, -1), (2, None), (2, FAKE + 1), (3, 299), (4, FAKE + 1), (5, 4), (6, None), (7, 4), (8, FAKE + 8),
             (9, None), (9, FAKE + 16), (10, need.value - 1)])
+    l = layer()
     lib.abcd_linear_bwd_workspace_size(C.byref(l), 400, C.byref(need))
     base = [C.byref(l), 400, FAKE, 5, FAKE, 8, None, None, FAKE, FAKE, 8, FAKE, FAKE, FAKE, need.value, None]
     refuse(base, lib.abcd_linear_bwd,

@@ -92,7 +92,8 @@ def test_large_tiles_and_split_rows(api, dtype):
 @pytest.mark.parametrize("dtype", DT, ids=IDS)
 @pytest.mark.parametrize("n,i,o", [
     (1024, 64, 64), (1025, 1, 1), (2049, 7, 5), (2049, 33, 48), (3000, 59, 61), (1500, 16, 128), (1500, 128, 16), (20011, 64, 64),
-    (70001, 24, 50), (4099, 128, 64), (4100, 64, 128), (5001, 121, 63), (3001, 128, 128), (2500, 96, 59)])
+    (70001, 24, 50), (4099, 128, 64), (4100, 64, 128), (5001, 121, 63), (3001, 128, 128), (2500, 96, 59),
+    (1003, 256, 128), (1500, 200, 72), (900, 131, 63), (1001, 250, 3), (777, 64, 256), (1200, 127, 201), (65, 17, 129)])
 def test_narrow_rows(api, dtype, n, i, o):
     run(api, n, i, o, dtype, "silu")
     run(api, n, i, o, dtype, None, bias=False, res=False, pad=5, skip=1)
@@ -193,7 +194,7 @@ def test_linear_refuses(api):
     for call in bad:
         with pytest.raises(ValueError):
             call()
-    many = torch.zeros(400, 16, device="cuda")
+    many = torch.zeros(400, 16, device="cuda")  # (of few rows none is needed)
     with pytest.raises(api.AbcdError):
         api.linear(many, w, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
     with pytest.raises(api.AbcdError):
