@@ -612,8 +612,9 @@ typedef struct abcd_layer {
 } abcd_layer;
 
 /* Forward. residual (may be NULL), and y, which may be residual itself. slope: NULL, or
- * [n][(o + 7) / 8 * 8], 16-byte aligned, that receives for the backward act's derivative (in
- * ABCD_F32 of that type, else in ABCD_F16; columns past o: zeros; with ABCD_ACT_NONE nothing is written). workspace: at least
+ * [n][(o + 7) / 8 * 8], 16-byte aligned, that receives for the backward act's derivative (floats
+ * with ABCD_F32, else a code of 16 bits, 30,800 times the slope's root; columns past o: zeros; with
+ * ABCD_ACT_NONE nothing is written). workspace: at least
  * abcd_linear_workspace_size bytes, 256-byte aligned; NULL where that is 0. */
 ABCD_API int32_t abcd_linear_workspace_size(const abcd_layer* layer /* host */, int64_t n, size_t* bytes);
 ABCD_API int32_t abcd_linear(const abcd_layer* layer /* host */, int64_t n, const void* x, int64_t ldx,

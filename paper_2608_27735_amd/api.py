@@ -723,16 +723,17 @@ def embed_bwd(dy, index, m, scale=1.0, wdtype=None, out=None, workspace=None):
     lddy = _rows(dy, "dy")
     (n, d), dev = dy.shape, dy.device
     m = _table_rows(int(m), "a table")
-    if not isinstance(index, Sorted):
+    if isinstance(index, Sorted):
+        for t, name, shape in ((index.order, "order", (n,)), (index.rows, "rows", (n,)),
+                               (index.ranges, "ranges", (m, 2))):
+            if t.dtype != torch.int32 or t.device != dev or t.shape != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous int32 on {dev} with shape {shape}, "
+                                 f"got {t.dtype} of {tuple(t.shape)}")
+        plan = [t.data_ptr() for t in index]
+    else:
         if index.shape != (n,):
             raise ValueError(f"index has shape {tuple(index.shape)}, expected ({n},)")
-        _index(index, dev)
-        index = embed_sort(index, m)
-    for t, name, shape in ((index.order, "order", (n,)), (index.rows, "rows", (n,)),
-                           (index.ranges, "ranges", (m, 2))):
-        if t.dtype != torch.int32 or t.device != dev or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous int32 on {dev} with shape {shape}, "
-                             f"got {t.dtype} of {tuple(t.shape)}")
+        bits, plan = _index(index, dev), None
     if out is None:
         out = torch.empty((m, d), dtype=wdtype or dy.dtype, device=dev)
     elif (wdtype is not None and out.dtype != wdtype) or out.device != dev:
@@ -744,9 +745,18 @@ def embed_bwd(dy, index, m, scale=1.0, wdtype=None, out=None, workspace=None):
     lib = _lib.load()
     sz = C.c_size_t(0)
     check(lib.abcd_embed_bwd_workspace_size(n, d, C.byref(sz)))
-    workspace = _workspace(workspace, sz.value, dev)
-    check(lib.abcd_embed_bwd(code, n, m, d, dy.data_ptr(), lddy, index.order.data_ptr(),
-                             index.rows.data_ptr(), index.ranges.data_ptr(), float(scale), wcode,
+    need = sz.value
+    if plan is None:
+        # the sort and its result beside each other (one array takes less of the host's time)
+        check(lib.abcd_embed_sort_workspace_size(n, m, C.byref(sz)))
+        up = (4 * n + 255) & ~255
+        kept = torch.empty(2 * up + ((8 * m + 255) & ~255) + sz.value, dtype=torch.uint8, device=dev)
+        at = kept.data_ptr()
+        plan = (at, at + up, at + 2 * up)
+        ws = at + kept.numel() - sz.value
+        check(lib.abcd_embed_sort(n, m, bits, index.data_ptr(), *plan, ws, sz.value, _stream()))
+    workspace = _workspace(workspace, need, dev)
+    check(lib.abcd_embed_bwd(code, n, m, d, dy.data_ptr(), lddy, *plan, float(scale), wcode,
                              out.data_ptr(), ldt, workspace.data_ptr(), workspace.numel(), _stream()))
     return out
 
@@ -969,7 +979,7 @@ def _layer(x, w, b, act):
 
 
 def _slope_dtype(dtype):
-    return dtype if dtype == torch.float32 else torch.float16
+    return dtype if dtype == torch.float32 else torch.int16
 
 
 def _slope(saved, n, o, dtype, dev):

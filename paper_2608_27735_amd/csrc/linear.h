@@ -54,7 +54,7 @@ struct LinearOutEnd {
     }
     if (a.res) y += __builtin_convertvector(f.res, Floats<8>);
     store_vec<T, 8, false>(static_cast<T*>(a.y) + r * a.ldy + k.c, y, k.left);
-    if (kAct != ABCD_ACT_NONE && a.slope) store_vec<SlopeOf<T>, 8, true>(static_cast<SlopeOf<T>*>(a.slope) + r * a.ldslope + k.c, s, 8);
+    if (kAct != ABCD_ACT_NONE && a.slope) store_slopes<8>(static_cast<SlopeOf<T>*>(a.slope) + r * a.ldslope + k.c, s);
   }
 };
 
@@ -145,9 +145,9 @@ __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, in
   store_vec<T, 4, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, left);
   if (kAct != ABCD_ACT_NONE && a.slope) {
     SlopeOf<T>* const to = static_cast<SlopeOf<T>*>(a.slope) + r * a.ldslope;
-    store_vec<SlopeOf<T>, 4, true>(to + c, s, 4);
+    store_slopes<4>(to + c, s);
     // the columns past o that this lane's four do not reach
-    if (a.o - c <= 4 && c + 4 < a.ldslope) store_vec<SlopeOf<T>, 4, true>(to + c + 4, Floats<4>(0.0f), 4);
+    if (a.o - c <= 4 && c + 4 < a.ldslope) store_slopes<4>(to + c + 4, Floats<4>(0.0f));
   }
 }
 
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kBlock) void linear_slope_kernel(LinearSlope a) {
 #pragma unroll 4
     for (int64_t r = (int64_t)blockIdx.y * rows + threadIdx.x / a.lanes; r < a.n; r += (int64_t)gridDim.y * rows) {
       const Floats<8> dy = __builtin_convertvector(load8<T>(a.dy, r * a.lddy + c, left_of(a.o - c)), Floats<8>);
-      Floats<8> v = dy * load_vec<SlopeOf<T>, 8, true>(static_cast<const SlopeOf<T>*>(a.slope) + r * a.ldslope + c, 8);
+      Floats<8> v = dy * load_slopes<8>(static_cast<const SlopeOf<T>*>(a.slope) + r * a.ldslope + c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = c + e < a.o ? v[e] : 0.0f;
       store_vec<T, 8, true>(static_cast<T*>(a.dz) + r * a.lddz + c, v, 8);

@@ -6,11 +6,46 @@
 
 namespace abcd {
 
-// What a forward keeps of act's derivative: in 16-bit types float16 whatever these are, as it
-// lies between -0.13 and 1.13 (below 2^-14 with fewer digits): kept in bfloat16 its rounding
-// would be as large as dz's.
+// What a forward keeps of act's derivative: float in fp32; in 16-bit types, as it lies between
+// -0.13 and 1.13, a code of 16 bits: 30,800 times its root, with its sign. A step of that is
+// 2^-14 of a slope of 1 and 2^-12 of one of 0.02, where float16 has 2^-11 of any: kept in
+// the rows' type its rounding would be as large as dz's. -32768 is a NaN.
 template <typename T>
-using SlopeOf = std::conditional_t<sizeof(T) == 4, float, _Float16>;
+using SlopeOf = std::conditional_t<sizeof(T) == 4, float, int16_t>;
+constexpr float kSlopeUnit = 30800.0f;
+template <int N>
+__device__ __forceinline__ void store_slopes(float* p, Floats<N> s) {
+  store_vec<float, N, true>(p, s, N);
+}
+template <int N>
+__device__ __forceinline__ void store_slopes(int16_t* p, Floats<N> s) {
+  typedef typename VecOf<int16_t, N>::type V;
+  V q;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float r = __builtin_rintf(__builtin_amdgcn_sqrtf(fabsf(s[i])) * kSlopeUnit);
+    q[i] = s[i] == s[i] ? (int16_t)(int)copysignf(r, s[i]) : (int16_t)-32768;
+  }
+  *reinterpret_cast<V*>(p) = q;
+}
+template <int N>
+__device__ __forceinline__ Floats<N> slopes_of(typename VecOf<int16_t, N>::type q) {
+  Floats<N> s;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float v = (float)q[i];
+    s[i] = q[i] == -32768 ? __builtin_nanf("") : v * fabsf(v) * (1.0f / (kSlopeUnit * kSlopeUnit));
+  }
+  return s;
+}
+template <int N>
+__device__ __forceinline__ Floats<N> load_slopes(const float* p) {
+  return load_vec<float, N, true>(p, N);
+}
+template <int N>
+__device__ __forceinline__ Floats<N> load_slopes(const int16_t* p) {
+  return slopes_of<N>(*reinterpret_cast<const typename VecOf<int16_t, N>::type*>(p));
+}
 
 // y = res + act(x w' + bias); slope: act's derivative, [n][ldslope], columns past o zeros.
 struct LinearOut {

@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 16 ? 4 : 2) void 
           store_vec<T, 8, kWhole>(static_cast<T*>(a.y) + r * a.ldy + c, y, left);
         }
         if (kAct != ABCD_ACT_NONE && a.slope && c < a.ldslope)
-          store_vec<_Float16, 8, true>(static_cast<_Float16*>(a.slope) + r * a.ldslope + c, s, 8);
+          store_slopes<8>(static_cast<int16_t*>(a.slope) + r * a.ldslope + c, s);
       }
     }
   }
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
   }
   // what is on its way: x (or the 8-bit one: two words and an exponent), dy, the slopes
   F nx[2][kDF], ny[2][kOF];
-  VecOf<_Float16, 8>::type ns[2][kOF];
+  VecOf<int16_t, 8>::type ns[2][kOF];
   const int blocks8 = (i + kPackBlock - 1) / kPackBlock;
   auto fetch = [&](int64_t from) {
 #pragma unroll
@@ -217,9 +217,9 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
         const int c = b * 32 + q * 8, left = in ? o - c : 0;
         ny[k][b] = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + r * a.lddy + c, left, room_of(a.n, r, a.lddy, left));
         if (kMode == kLinearKept) {
-          typedef VecOf<_Float16, 8>::type H;
-          ns[k][b] = *reinterpret_cast<const H*>(in && c < a.ldslope ? static_cast<const _Float16*>(a.slope) + r * a.ldslope + c
-                                                                    : reinterpret_cast<const _Float16*>(zeros));
+          typedef VecOf<int16_t, 8>::type H;
+          ns[k][b] = *reinterpret_cast<const H*>(in && c < a.ldslope ? static_cast<const int16_t*>(a.slope) + r * a.ldslope + c
+                                                                    : reinterpret_cast<const int16_t*>(zeros));
         }
       }
     }
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
 #pragma unroll
       for (int b = 0; b < kOF; ++b) {
         dy[k][b] = first_of<T, kWhole>(ny[k][b], o - (b * 32 + q * 8));
-        if (kMode == kLinearKept) slope[k][b] = __builtin_convertvector(ns[k][b], Floats<8>);
+        if (kMode == kLinearKept) slope[k][b] = slopes_of<8>(ns[k][b]);
       }
     }
     if (kEarly) fetch(r0 + step);  // past the end: zeros

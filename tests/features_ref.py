@@ -151,7 +151,7 @@ def linear_bwd(dy, x, w, b, name, u, kept):
     dz = dy * da
     sdz = torch.zeros_like(dz)
     if name is not None:
-        sdz = u * dz.abs() + kept * (dz.abs() + 2.0 ** -14 * dy.abs()) + 16 * E32 * dy.abs() * (da.abs() + bend * mz)
+        sdz = u * dz.abs() + kept * (dz.abs() + 2.0 ** -8 * dy.abs()) + 16 * E32 * dy.abs() * (da.abs() + bend * mz)
     if name == "relu":  # its slope jumps where the fp32 sum may have either sign
         sdz = sdz + torch.where(z.abs() <= 16 * E32 * mz, dy.abs(), torch.zeros_like(z))
     return dict(x=(dz @ w, dz.abs() @ w.abs(), (sdz ** 2 @ w ** 2).sqrt()),

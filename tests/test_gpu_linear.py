@@ -29,7 +29,9 @@ def run(api, n, i, o, dtype, act, bias=True, res=True, pad=0, skip=0):
     r = rand(4, n, o, dtype, skip, pad) if res else None
     dy = rand(5, n, o, dtype, pad, 2 * skip)
     x64, w64, b64, dy64, u = D.d64(x), D.d64(w), D.d64(b), D.d64(dy), D.UNIT[dtype]
-    us = 0.0 if act is None else D.UNIT[torch.float32 if dtype == torch.float32 else torch.float16]  # the slopes'
+    # the slopes': half a step of their root's code is 1 / (30,800 root) of a slope, below 2^-11
+    # of it above 2^-7 and, further down, below 2^-11 of it and 2^-19 together
+    us = 0.0 if act is None else D.UNIT[torch.float32 if dtype == torch.float32 else torch.float16]
     f = api.linear(x, w, b, act, residual=r, save=True)
     y, my = R.linear(x64, w64, b64, act, D.d64(r))
     D.close("y", f["y"], y, my)
@@ -57,7 +59,7 @@ def run(api, n, i, o, dtype, act, bias=True, res=True, pad=0, skip=0):
         assert torch.equal(got["x"], kept["x"])  # x is in the weights' gradient only
         z = x64 @ w64.T + (0 if b is None else b64)
         dz = dy64 * R.act(z, act)[1]
-        sdz = (u + us) * dz.abs() + us * 2.0 ** -14 * dy64.abs() + 16 * D.E32 * dy64.abs() * (1 + x64.abs() @ w64.abs().T)
+        sdz = (u + us) * dz.abs() + us * 2.0 ** -8 * dy64.abs() + 16 * D.E32 * dy64.abs() * (1 + x64.abs() @ w64.abs().T)
         if act == "relu":
             sdz = sdz + torch.where(z.abs() <= 16 * D.E32 * (x64.abs() @ w64.abs().T + 1), dy64.abs(), torch.zeros_like(z))
         D.close("8 bits, kept dw", got["w"], dz.T @ x8, dz.abs().T @ x8.abs(), extra=6 * ((sdz ** 2).T @ x8 ** 2).sqrt())
