@@ -19,6 +19,7 @@ template <typename T, int kAct>
 struct LinearOutEnd {
   static constexpr bool kXAlong = true, kWAlong = true, kHalves = false;
   static constexpr int kSegments = 1;
+  static constexpr bool kByRounds = true;
   typedef Big Large;
   LinearOut a;
   __device__ const Side& x() const { return a.x; }
@@ -62,6 +63,7 @@ template <typename T, int kAct>
 struct LinearDzEnd {
   static constexpr bool kXAlong = true, kWAlong = true, kHalves = false;
   static constexpr int kSegments = 1;
+  static constexpr bool kByRounds = true;
   typedef Big Large;
   LinearDz a;
   __device__ const Side& x() const { return a.x; }
@@ -99,6 +101,7 @@ template <typename T>
 struct LinearDxEnd {
   static constexpr bool kXAlong = true, kWAlong = false, kHalves = false;
   static constexpr int kSegments = 1;
+  static constexpr bool kByRounds = true;
   typedef Big Large;
   LinearDx a;
   __device__ const Side& x() const { return a.dz; }
