@@ -516,7 +516,7 @@ ABCD_API int32_t abcd_gated_ffn_bwd(const abcd_ffn* ffn /* host */, int64_t n, c
 
 /* Features that rows share: y[i] = scale table[index[i]] for n indexes (index_bits:
  * 32 or 64, signed) into a table of m rows (1 <= m <= ABCD_MAX_GAUSSIANS, type tdtype:
- * dtype or ABCD_F32). An index outside [0, m), as of a place of a batch that holds
+ * dtype or ABCD_F32; scale finite). An index outside [0, m), as of a place of a batch that holds
  * nothing, gives a row of zeros. y may not overlap the table. */
 ABCD_API int32_t abcd_embed(int32_t dtype, int64_t n, int64_t m, int64_t d, int32_t tdtype,
                             const void* table, int64_t ldt, int32_t index_bits, const void* index,
@@ -535,7 +535,7 @@ ABCD_API int32_t abcd_embed_sort(int64_t n, int64_t m, int32_t index_bits, const
 /* The table's gradient: dtable[r] = scale times the sum of dy[i] over the i with index
  * r, zeros for a row with none (written, not added to; type wdtype: dtype or ABCD_F32; ldt
  * elements between its rows). order, rows and ranges: abcd_embed_sort's, of the same n and
- * m, unchanged (they are not checked). workspace: at least abcd_embed_bwd_workspace_size
+ * m, unchanged (what they hold is not checked on the host; with others the result is wrong). workspace: at least abcd_embed_bwd_workspace_size
  * bytes, 256-byte aligned. */
 ABCD_API int32_t abcd_embed_bwd_workspace_size(int64_t n, int64_t d, size_t* bytes);
 ABCD_API int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy,
@@ -611,7 +611,7 @@ typedef struct abcd_layer {
   const void *w, *b;
 } abcd_layer;
 
-/* Forward. residual (may be NULL), and y, which may be residual itself. slope: NULL, or
+/* Forward. residual (may be NULL), and y, which may be residual itself but may not overlap x. slope: NULL, or
  * [n][(o + 7) / 8 * 8], 16-byte aligned, that receives for the backward act's derivative (floats
  * with ABCD_F32, else a code of 16 bits, 30,800 times the slope's root; columns past o: zeros; with
  * ABCD_ACT_NONE nothing is written). workspace: at least

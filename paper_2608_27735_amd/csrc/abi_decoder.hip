@@ -256,6 +256,7 @@ int32_t abcd_embed(int32_t dtype, int64_t n, int64_t m, int64_t d, int32_t tdtyp
   TRY_STATUS(check_wdtype(dtype, tdtype));
   TRY_STATUS(check_matrix("table", table, tdtype, m, d, ldt, false));
   TRY_STATUS(check_index(index_bits, index, n));
+  REQUIRE(std::isfinite(scale), "scale must be finite");
   TRY_STATUS(check_matrix("y", y, dtype, n, d, ldy, false));
   return launch_embed(dtype, n, m, d, tdtype, table, ldt, index_bits, index, scale, y, ldy, stream);
 }
@@ -294,6 +295,7 @@ int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const voi
   TRY_STATUS(check_ints("order", order, 4, n));
   TRY_STATUS(check_ints("rows", rows, 4, n));
   TRY_STATUS(check_ints("ranges", ranges, 8, m));
+  REQUIRE(std::isfinite(scale), "scale must be finite");
   TRY_STATUS(check_wdtype(dtype, wdtype));
   TRY_STATUS(check_matrix("dtable", dtable, wdtype, m, d, ldt, false));
   TRY_STATUS(check_workspace(workspace, ws_bytes, embed_bwd_workspace_bytes(n, d)));

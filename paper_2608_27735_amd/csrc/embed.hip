@@ -372,6 +372,13 @@ __device__ __forceinline__ void put_row(const EmbedBwdArgs& a, int64_t r, int c,
     store_vec<T, N, kWhole>(static_cast<T*>(a.dtable) + r * a.ldt + c, v, a.d - c);
 }
 
+// Where a row's positions are. What the caller has kept of the sort is not checked on the
+// host: whatever it holds, no access leaves the arrays.
+__device__ __forceinline__ int2 range_of(const EmbedBwdArgs& a, int64_t r) {
+  const int2 at = a.ranges[r];
+  return make_int2(max(at.x, 0), max(min(at.y, (int)a.n), 0));
+}
+
 // The sum of columns c.. of dy over positions [from, to) of the order.
 template <typename T, int N, bool kWhole>
 __device__ __forceinline__ Floats<N> sum_run(const EmbedBwdArgs& a, int from, int to, int c) {
@@ -384,13 +391,13 @@ __device__ __forceinline__ Floats<N> sum_run(const EmbedBwdArgs& a, int from, in
     for (int u = 0; u < kAhead; ++u) at[u] = a.order[p + u < to ? p + u : from];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int left = p + u < to ? a.d - c : 0;
+      const int left = p + u < to && (uint64_t)at[u] < (uint64_t)a.n ? a.d - c : 0;
       v[u] = load_frag<T, kWhole>(static_cast<const T*>(a.dy) + at[u] * a.lddy + c, left,
                                   room_of(a.n, at[u], a.lddy, left));
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      s += __builtin_convertvector((first_of<T, kWhole>(v[u], p + u < to ? a.d - c : 0)), Floats<N>);
+      s += __builtin_convertvector((first_of<T, kWhole>(v[u], a.d - c)), Floats<N>);
   }
   return s;
 }
@@ -404,20 +411,21 @@ __global__ __launch_bounds__(kBlock) void embed_bwd_kernel(EmbedBwdArgs a) {
   const int rows = kBlock / a.lanes, c = ((int)blockIdx.y * a.lanes + (threadIdx.x & (a.lanes - 1))) * N;
   if (c >= a.d) return;
   if ((int)blockIdx.x < a.row_blocks) {
-    int64_t r = (int64_t)blockIdx.x * rows * a.turns + threadIdx.x / a.lanes;
-    if (a.turns == 1) {
-      if (r >= a.m) return;
-      const int2 at = a.ranges[r];
-      if (at.y - at.x > kRun) return;
-      put_row<T, N, kWhole>(a, r, c, sum_run<T, N, kWhole>(a, at.x, at.y, c));
-      return;
+    const int64_t step = (int64_t)a.row_blocks * rows * a.turns;
+    for (int64_t r = (int64_t)blockIdx.x * rows * a.turns + threadIdx.x / a.lanes; r < a.m; r += step) {
+      if (a.turns == 1) {
+        const int2 at = range_of(a, r);
+        if (at.y - at.x <= kRun) put_row<T, N, kWhole>(a, r, c, sum_run<T, N, kWhole>(a, at.x, at.y, c));
+        continue;
+      }
+      int2 at[kRowTurns];
+#pragma unroll
+      for (int k = 0; k < kRowTurns; ++k) at[k] = r + k * rows < a.m ? range_of(a, r + k * rows) : make_int2(0, kRun + 1);
+#pragma unroll
+      for (int k = 0; k < kRowTurns; ++k)
+        if (at[k].y - at[k].x <= kRun)
+          put_row<T, N, kWhole>(a, r + k * rows, c, sum_run<T, N, kWhole>(a, at[k].x, at[k].y, c));
     }
-    int2 at[kRowTurns];
-#pragma unroll
-    for (int k = 0; k < kRowTurns; ++k) at[k] = r + k * rows < a.m ? a.ranges[r + k * rows] : make_int2(0, kRun + 1);
-#pragma unroll
-    for (int k = 0; k < kRowTurns; ++k, r += rows)
-      if (at[k].y - at[k].x <= kRun) put_row<T, N, kWhole>(a, r, c, sum_run<T, N, kWhole>(a, at[k].x, at[k].y, c));
     return;
   }
   const int64_t chunk = (int64_t)((int)blockIdx.x - a.row_blocks) * rows + threadIdx.x / a.lanes, begin = chunk * kRun;
@@ -428,8 +436,8 @@ __global__ __launch_bounds__(kBlock) void embed_bwd_kernel(EmbedBwdArgs a) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int r = k == 0 ? first_row : last_row;
-    if (r >= a.m || (k == 1 && last_row == first_row)) continue;
-    const int2 at = a.ranges[r];
+    if ((uint32_t)r >= (uint32_t)a.m || (k == 1 && last_row == first_row)) continue;
+    const int2 at = range_of(a, r);
     if (at.y - at.x <= kRun) continue;
     const int which = at.x >= begin ? 1 : 0;
     const Floats<N> s = sum_run<T, N, kWhole>(a, max(at.x, (int)begin), min(at.y, (int)end), c);
@@ -451,8 +459,8 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedBwdA
   bool begins = false;
   if (behind < a.n) {
     row = a.rows[behind - 1];
-    if (row < a.m) {
-      const int2 at = a.ranges[row];
+    if ((uint32_t)row < (uint32_t)a.m) {
+      const int2 at = range_of(a, row);
       end = at.y;
       begins = at.y - at.x > kRun && at.x >= chunk * kRun;
     }
@@ -629,9 +637,8 @@ int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const v
     const int64_t rows = kBlock / a.lanes;
     // where most rows are empty, and long, a wave looks at several of them at once
     a.turns = n < m && nvec >= kWave ? kRowTurns : 1;
-    a.row_blocks = (int)((m + rows * a.turns - 1) / (rows * a.turns));
+    a.row_blocks = (int)std::min<int64_t>((m + rows * a.turns - 1) / (rows * a.turns), 1 << 18);
     const int64_t blocks = a.row_blocks + (chunks + rows - 1) / rows;
-    REQUIRE(blocks < (int64_t(1) << 31), "too many rows");
     const dim3 grid(blocks, (nvec + a.lanes - 1) / a.lanes);
     if (d % kPer16<T> == 0)
       ABCD_LAUNCH("embed_bwd", (embed_bwd_kernel<T, true>), grid, kBlock, 0, stream, a);

@@ -34,7 +34,7 @@ def test_embed_refuses(lib):
     base = [F16, 4, 5, 8, F16, FAKE, 8, 32, FAKE, 1.0, FAKE, 8, None]
     refuse(base, lib.abcd_embed,
            [(0, 3), (1, -1), (1, (1 << 30) + 1), (2, 0), (2, (1 << 30) + 1), (3, 0), (3, 65537), (4, BF16),
-            (5, None), (5, FAKE + 1), (6, 7), (7, 16), (8, None), (8, FAKE + 2), (10, None), (10, FAKE + 1), (11, 7)])
+            (5, None), (5, FAKE + 1), (6, 7), (7, 16), (8, None), (8, FAKE + 2), (9, float("inf")), (9, float("nan")), (10, None), (10, FAKE + 1), (11, 7)])
     base[7] = 64
     refuse(base, lib.abcd_embed, [(8, FAKE + 4)])
 
@@ -56,7 +56,7 @@ def test_embed_bwd_refuses(lib):
     base = [BF16, 4, 5, 8, FAKE, 8, FAKE, FAKE, FAKE, 1.0, F32, FAKE, 8, FAKE, need.value, None]
     refuse(base, lib.abcd_embed_bwd,
            [(0, 7), (1, -1), (2, 0), (3, 0), (4, None), (4, FAKE + 1), (5, 7), (6, None), (6, FAKE + 1), (7, None),
-            (8, None), (8, FAKE + 4), (10, F16), (11, None), (11, FAKE + 2), (12, 7), (13, None), (13, FAKE + 8),
+            (8, None), (8, FAKE + 4), (9, float("inf")), (9, float("nan")), (10, F16), (11, None), (11, FAKE + 2), (12, 7), (13, None), (13, FAKE + 8),
             (14, need.value - 1)])
 
 

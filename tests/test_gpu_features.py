@@ -143,6 +143,33 @@ def test_embed_far_rows(api):
     assert torch.equal(api.embed_bwd(dfar, index[:3], m), api.embed_bwd(dy[:3].contiguous(), index[:3], m))
 
 
+def test_gradient_of_many_rows(api):
+    """More rows than workgroups, most of them without a position."""
+    m, d = 2200000, 256
+    index = torch.tensor([0, m - 1, 5, m - 1, 2099999, 1048576, 5, m // 2], device="cuda")
+    dy = rand(1, 8, d, torch.bfloat16)
+    got = api.embed_bwd(dy, index, m)
+    want, mag = R.embed_bwd(D.d64(dy), torch.tensor([0, 1, 2, 1, 3, 4, 2, 5]), 6, 1.0)
+    D.close("rows", got[torch.tensor([0, m - 1, 5, 2099999, 1048576, m // 2], device="cuda")], want, mag, k=2.0)
+    got[index] = 0
+    assert not got.any()
+
+
+def test_a_plan_of_other_indexes_stays_inside(api):
+    """A kept sort that does not belong to the call gives wrong sums, and reads and writes
+    nothing outside its arrays: what lies around the gradient is left as it was."""
+    n, m, d = 300, 40, 24
+    dy = rand(1, n, d, torch.float32)
+    g = torch.Generator().manual_seed(2)
+    odd = lambda *s: torch.randint(-(1 << 31), 1 << 31, s, generator=g).int().cuda()
+    room = torch.full((m + 8, d), 7.0, device="cuda")
+    for k in range(4):
+        s = api.embed_sort(torch.randint(0, m, (n,), generator=g).cuda(), m)
+        s = api.Sorted(odd(n) if k in (0, 3) else s.order, odd(n) if k in (1, 3) else s.rows, odd(m, 2) if k in (2, 3) else s.ranges)
+        api.embed_bwd(dy, s, m, out=room[4:-4])
+        assert (room[:4] == 7).all() and (room[-4:] == 7).all()
+
+
 def test_embed_refuses(api):
     t, i = torch.zeros(4, 8, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
     bad = [lambda: api.embed(t.double(), i), lambda: api.embed(t, i.float()), lambda: api.embed(t, i.cpu()),
