@@ -35,12 +35,20 @@ constexpr int kLinearKept = 5;  // an "act" whose slope is read
 // (with all of a quarter's blocks consecutive 1M x 64 to 128 forward takes 173 us).
 __device__ __forceinline__ int column_of(int b, int r) { return (b >> 1) * 32 + (r >> 2) * 8 + (b & 1) * 4 + (r & 3); }
 
+// Which of x's columns quarter q of contraction f of 32 begins at: those of rows in memory lie
+// 64 bytes of a row next to each other; of an 8-bit checkpoint a quarter has kDF 8 bytes, which
+// it so loads at once.
+template <int kDF>
+__device__ __forceinline__ int column_along(int f, int q, bool packed) {
+  return packed ? (q * kDF + f) * 8 : f * 32 + q * 8;
+}
+
 // Fragment f of the weights for z: block f / kDF of 16 columns of z, contraction f % kDF of
 // 32.
 template <typename T, int kDF, bool kWhole>
-__device__ __forceinline__ typename Frag<T>::type weights_along(const void* w, int f, int rows, int cols) {
+__device__ __forceinline__ typename Frag<T>::type weights_along(const void* w, int f, int rows, int cols, bool packed) {
   const int l = threadIdx.x & 63, j = l & 15;
-  const int row = column_of(f / kDF, j), col = f % kDF * 32 + (l >> 4) * 8;
+  const int row = column_of(f / kDF, j), col = column_along<kDF>(f % kDF, l >> 4, packed);
   const T* const p = static_cast<const T*>(w) + (int64_t)row * cols + col;
   if (kWhole) return load_whole(p, row < rows && col < cols);
   typename Frag<T>::type v;
@@ -81,7 +89,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 16 ? 4 : 2) void 
   const int i = (int)a.i, o = (int)a.o;
   const int l = threadIdx.x & 63, j = l & 15, q = l >> 4, wave = threadIdx.x >> 6;
 #pragma unroll 2
-  for (int f = wave; f < kFrags; f += kNarrowLayerWaves) weights[f * 64 + l] = weights_along<T, kDF, kWhole>(a.w, f, o, i);
+  for (int f = wave; f < kFrags; f += kNarrowLayerWaves) weights[f * 64 + l] = weights_along<T, kDF, kWhole>(a.w, f, o, i, false);
   if (threadIdx.x < kOB * 16)
     bias[threadIdx.x] = a.bias && (int)threadIdx.x < o ? (float)static_cast<const T*>(a.bias)[threadIdx.x] : 0.0f;
   __syncthreads();
@@ -172,7 +180,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
   const int l = threadIdx.x & 63, j = l & 15, q = l >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int f = wave; f < kFrags; f += kNarrowLayerWaves) {
-    if (kAgain) along[f * 64 + l] = weights_along<T, kDF, kWhole>(a.w, f, o, i);
+    if (kAgain) along[f * 64 + l] = weights_along<T, kDF, kWhole>(a.w, f, o, i, a.q != nullptr);
     across[f * 64 + l] = weights_across<T, kOF>(a.w, f, o, i);
   }
   __syncthreads();
@@ -185,7 +193,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
 #pragma unroll
     for (int k = 0; k < kIB; ++k) dw[b][k] = 0.0f;
   }
-  // what is on its way: x (or the 8-bit one: two words and an exponent), dy, the slopes
+  // what is on its way: x (or the 8-bit one: kDF / 2 vectors and then an exponent), dy, the slopes
   F nx[2][kDF], ny[2][kOF];
   VecOf<int16_t, 8>::type ns[2][kOF];
   const int blocks8 = (i + kPackBlock - 1) / kPackBlock;
@@ -195,16 +203,14 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
       const int64_t r = from + k * 16 + j;
       const bool in = r < a.n;
       if (a.q) {
+        const bool there = in && q * kDF * 8 < blocks8 * kPackBlock;
+        const char* const from = reinterpret_cast<const char*>(a.q) + r * blocks8 * kPackBlock + q * kDF * 8;
 #pragma unroll
-        for (int f = 0; f < kDF; ++f) {
-          typedef VecOf<uint32_t, 2>::type U2;
-          typedef VecOf<uint32_t, 4>::type U4;
-          const bool there = in && f < blocks8;
-          const U2 v = *reinterpret_cast<const U2*>(
-              there ? reinterpret_cast<const char*>(a.q) + (r * blocks8 + f) * kPackBlock + q * 8 : reinterpret_cast<const char*>(zeros));
-          const uint8_t e = *(there ? a.e + r * blocks8 + f : reinterpret_cast<const uint8_t*>(zeros));
-          nx[k][f] = __builtin_bit_cast(F, (U4){v[0], v[1], (uint32_t)e, 0u});
-        }
+        for (int f = 0; f < kDF / 2; ++f)
+          nx[k][f] = *reinterpret_cast<const F*>(there ? from + f * 16 : reinterpret_cast<const char*>(zeros));
+        const uint8_t e = *(there ? a.e + r * blocks8 + q * kDF / 4 : reinterpret_cast<const uint8_t*>(zeros));
+        typedef VecOf<uint32_t, 4>::type U4;
+        nx[k][kDF / 2] = __builtin_bit_cast(F, (U4){(uint32_t)e, 0u, 0u, 0u});
       } else {
 #pragma unroll
         for (int f = 0; f < kDF; ++f) {
@@ -232,17 +238,18 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
     Floats<8> slope[2][kOF];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
+      typedef VecOf<uint32_t, 4>::type U4;
+      // (outside the array the exponent is 0: the least one's unit, of numbers that are 0)
+      const float unit = packed_unit(max(__builtin_bit_cast(U4, nx[k][kDF / 2])[0], (uint32_t)kPackLeast));
 #pragma unroll
       for (int f = 0; f < kDF; ++f) {
         if (a.q) {
-          typedef VecOf<uint32_t, 4>::type U4;
-          const U4 v = __builtin_bit_cast(U4, nx[k][f]);
-          // (outside the array the exponent is 0: the least one's unit, of numbers that are 0)
-          x[k][f] = __builtin_convertvector(unpack_8(v[0], v[1], packed_unit(max(v[2], (uint32_t)kPackLeast))), F);
+          const U4 v = __builtin_bit_cast(U4, nx[k][f / 2]);
+          x[k][f] = __builtin_convertvector(unpack_8(v[f % 2 * 2], v[f % 2 * 2 + 1], unit), F);
         } else {
           x[k][f] = first_of<T, kWhole>(nx[k][f], i - (f * 32 + q * 8));
         }
-        *(LdsF*)(xs + turned_row<kXBytes>(k * 16 + j, (f * 4 + q) * 2)) = x[k][f];
+        *(LdsF*)(xs + turned_row<kXBytes>(k * 16 + j, column_along<kDF>(f, q, a.q != nullptr) / 4)) = x[k][f];
       }
 #pragma unroll
       for (int b = 0; b < kOF; ++b) {
