@@ -49,28 +49,38 @@ __global__ __launch_bounds__(kBlock) void pack8_kernel(PackArgs a) {
     const T* x = static_cast<const T*>(a.x) + row * a.ld;
     for (int c = t * N; c < pitch; c += a.lanes * N) {
       const int left = a.d - c;
-      const Floats<N> v =
-          __builtin_convertvector((load_first<T, kWhole>(x + c, left, room_of(a.n, row, a.ld, left))), Floats<N>);
+      const typename Frag<T>::type raw = load_first<T, kWhole>(x + c, left, room_of(a.n, row, a.ld, left));
+      const Floats<N> v = __builtin_convertvector(raw, Floats<N>);
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-        top = max(top, m < 0x7F800000u ? m : 0u);
+      for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      const bool finite = top < 0x7F800000u;
+      // infinities and NaN, which no block's exponent takes part of, for all lanes of a wave
+      if (__builtin_expect(__any(!finite), 0)) {
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+          top = max(top, m < 0x7F800000u ? m : 0u);
+        }
       }
       const uint32_t e = max(lanes_max<kLanes>(top) >> 23, (uint32_t)kPackLeast);
-      const float up = __uint_as_float((127 + 127 + 6 - e) << 23);
-      uint32_t words[N / 4];
+      // rint(v 2^(6 - e)) as the low bits of a sum with 1.5 x 2^23; cut off at 127 steps before
+      const float up = __uint_as_float((127 + 127 + 6 - e) << 23), most = 127.0f * packed_unit(e);
+      uint32_t q[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float s = __builtin_rintf(v[i] * up);
-        int q = (int)__builtin_amdgcn_fmed3f(s, -127.0f, 127.0f);
-        if ((__float_as_uint(v[i]) & 0x7F800000u) == 0x7F800000u) q = -128;
-        words[i / 4] = i % 4 == 0 ? (uint32_t)(q & 255) : words[i / 4] | (uint32_t)(q & 255) << (i % 4 * 8);
+      for (int i = 0; i < N; ++i) q[i] = __float_as_uint(fmaf(__builtin_amdgcn_fmed3f(v[i], -most, most), up, 12582912.0f));
+      if (__builtin_expect(__any(!finite), 0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if ((__float_as_uint(v[i]) & 0x7F800000u) == 0x7F800000u) q[i] = 0x80;
       }
       typedef typename VecOf<uint32_t, N / 4>::type Words;
       Words w;
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) w[i] = words[i];
+      for (int i = 0; i < N / 4; ++i)
+        w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0C0C0400u),
+                                     __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0C0C0400u), 0x05040100u);
       *reinterpret_cast<Words*>(a.q + row * pitch + c) = w;
       if (t % kLanes == 0) a.e[row * a.blocks + c / kPackBlock] = (uint8_t)e;
     }

@@ -476,25 +476,29 @@ __global__ __launch_bounds__(kWide) void residual_norm_bwd_wide_kernel(JointArgs
   }
 }
 
-// The workgroups' column sums added up in order: 16 columns of all four a workgroup, the parts
-// dealt to its waves (256 parts of 1,001 columns: with 64 columns a workgroup 10.6 us).
-constexpr int kJointPartWaves = 16, kJointPartCols = 16;
+// The workgroups' column sums added up in order: 32 columns (128 bytes) of all four a workgroup,
+// the parts dealt to its waves (256 parts of 1,001 columns: 4.2 us, with 64 columns of one
+// sum after the other 10.6).
+constexpr int kJointPartWaves = 16, kJointPartCols = 32;
 template <typename T>
 __global__ __launch_bounds__(kJointPartWaves* kWave) void residual_norm_sums_kernel(JointArgs a, int64_t parts) {
-  __shared__ float red[kJointPartWaves][kWave];
+  typedef VecOf<float, 2>::type F2;
+  constexpr int kLanes = kJointPartCols / 2;
+  __shared__ F2 red[kJointPartWaves][kWave];
   const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
-  const int which = l / kJointPartCols, first = (int)blockIdx.x * kJointPartCols, c = first + l % kJointPartCols;
-  float s = 0.0f;
+  const int first = (int)blockIdx.x * kJointPartCols, c = first + l % kLanes * 2;
+  const float* const from = a.part + l / kLanes * a.pitch + c;  // (rows of parts are whole vectors)
+  F2 s = 0.0f;
   if (c < a.d) {
     int64_t p = w;
     for (; p + 7 * kJointPartWaves < parts; p += 8 * kJointPartWaves) {
-      float v[8];
+      F2 v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = a.part[((p + u * kJointPartWaves) * 4 + which) * a.pitch + c];
+      for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const F2*>(from + (p + u * kJointPartWaves) * 4 * a.pitch);
 #pragma unroll
       for (int u = 0; u < 8; ++u) s += v[u];
     }
-    for (; p < parts; p += kJointPartWaves) s += a.part[(p * 4 + which) * a.pitch + c];
+    for (; p < parts; p += kJointPartWaves) s += *reinterpret_cast<const F2*>(from + p * 4 * a.pitch);
   }
   red[w][l] = s;
   __syncthreads();
@@ -503,9 +507,10 @@ __global__ __launch_bounds__(kJointPartWaves* kWave) void residual_norm_sums_ker
     red[0][l] = s;
   }
   __syncthreads();
-  if (threadIdx.x < kJointPartCols)  // (put_params leaves out what lies past the row's end)
-    put_params<T, 1, true>(a, first + l, Floats<1>(red[0][l]), Floats<1>(red[0][kJointPartCols + l]),
-                           Floats<1>(red[0][2 * kJointPartCols + l]), Floats<1>(red[0][3 * kJointPartCols + l]));
+  if (threadIdx.x < kJointPartCols) {  // (put_params leaves out what lies past the row's end)
+    auto sum = [&](int which) { return Floats<1>(red[0][which * kLanes + threadIdx.x / 2][threadIdx.x % 2]); };
+    put_params<T, 1, true>(a, first + (int)threadIdx.x, sum(0), sum(1), sum(2), sum(3));
+  }
 }
 
 // Lanes of a row that a kernel is compiled for; f with the fewest that hold nvec vectors, and
