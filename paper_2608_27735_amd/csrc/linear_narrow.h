@@ -14,6 +14,11 @@
 // sums stay in the wave's registers over all its rows, as do the bias's, of dz before it is
 // rounded. The workgroup's four waves add their sums up in LDS, and a second launch adds the
 // workgroups' in a fixed order.
+//
+// 1M x 64 to 64 in bf16: forward with SiLU and a residual 75 us (384 MB, 5.1 TB/s), backward 84
+// without an activation (384 MB), 94 with SiLU and 104 with GELU, of an 8-bit checkpoint 74, 88
+// and 100 (322 MB): two waves a SIMD, by their registers, wait for loads, products and LDS in turn,
+// vector instructions 45 percent busy. 128 to 64: 100 and 180; one wave a SIMD, as two spill.
 #pragma once
 
 #include <algorithm>
