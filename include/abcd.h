@@ -543,6 +543,13 @@ ABCD_API int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, 
                                 const int32_t* ranges, float scale, int32_t wdtype, void* dtable,
                                 int64_t ldt, void* workspace, size_t ws_bytes, hipStream_t stream);
 
+/* The same gradient from the indexes themselves, for up to ABCD_EMBED_FEW positions: one
+ * launch, without a sort or a workspace. */
+#define ABCD_EMBED_FEW 64
+ABCD_API int32_t abcd_embed_bwd_few(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy,
+                                    int64_t lddy, int32_t index_bits, const void* index, float scale,
+                                    int32_t wdtype, void* dtable, int64_t ldt, hipStream_t stream);
+
 /* The joint between two blocks: a block's result f, normed, gated and scaled, goes
  * onto the residual path x, and the next block takes that normed:
  *   t = post(f);  y = x + scale gate t;  z = pre(y)
@@ -647,7 +654,7 @@ ABCD_API int32_t abcd_linear_bwd(const abcd_layer* layer /* host */, int64_t n, 
  * render_cache, cache_rect_init, layer_norm, layer_norm_bwd, layer_norm_cols,
  * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
  * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out,
- * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_few, embed_bwd,
+ * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_few, embed_bwd, embed_bwd_few,
  * embed_join, pack8, unpack8, residual_norm, residual_norm_bwd, residual_norm_sums,
  * linear_out, linear_few, linear_dz, linear_dx, linear_slope, linear_narrow,
  * linear_narrow_bwd). */

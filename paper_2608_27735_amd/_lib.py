@@ -30,6 +30,7 @@ class abcd_raster_params(C.Structure):
 
 
 ADAM_MAX_GROUPS = 8
+EMBED_FEW = 64  # ABCD_EMBED_FEW
 
 
 class abcd_adam_group(C.Structure):
@@ -109,6 +110,8 @@ SIGNATURES = {
     "abcd_embed_bwd_workspace_size": (_I32, [_I64, _I64, C.POINTER(_SZ)]),
     "abcd_embed_bwd": (_I32, [_I32, _I64, _I64, _I64, _P, _I64, _P, _P, _P, C.c_float, _I32, _P, _I64,
                               _P, _SZ, _P]),
+    "abcd_embed_bwd_few": (_I32, [_I32, _I64, _I64, _I64, _P, _I64, _I32, _P, C.c_float, _I32, _P, _I64,
+                                  _P]),
     "abcd_residual_norm": (_I32, [_JOINT, _I64] + [_P, _I64] * 5 + [_P] * 5),
     "abcd_residual_norm_bwd_workspace_size": (_I32, [_JOINT, _I64, C.POINTER(_SZ)]),
     "abcd_residual_norm_bwd": (_I32, [_JOINT, _I64] + [_P, _I64] * 5 + [_P] * 4 + [_P, _I64] * 3 + [_P] * 6 +

@@ -743,6 +743,10 @@ def embed_bwd(dy, index, m, scale=1.0, wdtype=None, out=None, workspace=None):
         raise ValueError(f"the gradient must be {dy.dtype} or float32, got {out.dtype}")
     ldt = _rows(out, "out", shape=(m, d))
     lib = _lib.load()
+    if plan is None and n <= _lib.EMBED_FEW:
+        check(lib.abcd_embed_bwd_few(code, n, m, d, dy.data_ptr(), lddy, bits, index.data_ptr(), float(scale),
+                                     wcode, out.data_ptr(), ldt, _stream()))
+        return out
     sz = C.c_size_t(0)
     check(lib.abcd_embed_bwd_workspace_size(n, d, C.byref(sz)))
     need = sz.value

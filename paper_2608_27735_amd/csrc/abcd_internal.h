@@ -385,6 +385,9 @@ int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const v
                          int64_t lddy, const int32_t* order, const int32_t* rows,
                          const int32_t* ranges, float scale, int32_t wdtype, void* dtable,
                          int64_t ldt, void* workspace, hipStream_t stream);
+int32_t launch_embed_bwd_few(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy,
+                             int64_t lddy, int32_t index_bits, const void* index, float scale,
+                             int32_t wdtype, void* dtable, int64_t ldt, hipStream_t stream);
 // residual_norm.hip
 size_t residual_norm_bwd_workspace_bytes(const abcd_joint& j, int64_t n);
 int32_t launch_residual_norm(const abcd_joint& j, int64_t n, const void* f, int64_t ldf,

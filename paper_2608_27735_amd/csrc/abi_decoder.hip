@@ -302,6 +302,20 @@ int32_t abcd_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const voi
   return launch_embed_bwd(dtype, n, m, d, dy, lddy, order, rows, ranges, scale, wdtype, dtable, ldt, workspace, stream);
 }
 
+int32_t abcd_embed_bwd_few(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy, int64_t lddy,
+                           int32_t index_bits, const void* index, float scale, int32_t wdtype, void* dtable, int64_t ldt,
+                           hipStream_t stream) {
+  TRY_STATUS(check_rows(dtype, n, d));
+  TRY_STATUS(check_table_rows(n, m));
+  REQUIRE(n <= ABCD_EMBED_FEW, "%lld positions, more than %d", (long long)n, ABCD_EMBED_FEW);
+  TRY_STATUS(check_matrix("dy", dy, dtype, n, d, lddy, false));
+  TRY_STATUS(check_index(index_bits, index, n));
+  REQUIRE(std::isfinite(scale), "scale must be finite");
+  TRY_STATUS(check_wdtype(dtype, wdtype));
+  TRY_STATUS(check_matrix("dtable", dtable, wdtype, m, d, ldt, false));
+  return launch_embed_bwd_few(dtype, n, m, d, dy, lddy, index_bits, index, scale, wdtype, dtable, ldt, stream);
+}
+
 int32_t abcd_residual_norm(const abcd_joint* joint, int64_t n, const void* f, int64_t ldf, const void* x, int64_t ldx,
                            const void* gate, int64_t ldg, void* y, int64_t ldy, void* z, int64_t ldz, float* post_mean,
                            float* post_rstd, float* pre_mean, float* pre_rstd, hipStream_t stream) {

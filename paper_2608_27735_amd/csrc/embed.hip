@@ -501,6 +501,49 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedBwdA
   }
 }
 
+// Up to a wave's lanes of positions, without a sort: every wave has all indexes, and finds by a
+// ballot those that name one of the rows it writes.
+struct EmbedFewArgs {
+  const void* dy;
+  const void* index;
+  void* dtable;
+  int64_t lddy, ldt, n, m;
+  int d, lanes, wf32;
+  float scale;
+};
+template <typename T, typename I, bool kWhole>
+__global__ __launch_bounds__(kBlock) void embed_bwd_few_kernel(EmbedFewArgs a) {
+  constexpr int N = kPer16<T>, kAhead = 8;
+  const int l = threadIdx.x % kWave, t = l & (a.lanes - 1), rows = kWave / a.lanes;
+  const int c = ((int)blockIdx.y * a.lanes + t) * N;
+  const int64_t index = l < a.n ? (int64_t)static_cast<const I*>(a.index)[l] : -1;
+  const int64_t step = (int64_t)gridDim.x * (kBlock / kWave) * rows;
+  for (int64_t r0 = ((int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave) * rows; r0 < a.m; r0 += step) {
+    const int64_t row = r0 + l / a.lanes;
+    Floats<N> s = 0.0f;
+    uint64_t left = __ballot(index >= r0 && index < r0 + rows);
+    while (left) {
+      Floats<N> v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {  // positions in their order
+        const int p = left ? __ffsll((unsigned long long)left) - 1 : 0;
+        const bool mine = left && r0 + (__shfl((int)(index - r0), p, kWave)) == row;
+        left &= left - 1;
+        v[u] = 0.0f;
+        if (mine && c < a.d) v[u] = load_vec<T, N, kWhole>(static_cast<const T*>(a.dy) + p * a.lddy + c, a.d - c);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s += v[u];
+    }
+    if (row >= a.m || c >= a.d) continue;
+    s *= a.scale;
+    if (a.wf32)
+      store_vec<float, N, kWhole>(static_cast<float*>(a.dtable) + row * a.ldt + c, s, a.d - c);
+    else
+      store_vec<T, N, kWhole>(static_cast<T*>(a.dtable) + row * a.ldt + c, s, a.d - c);
+  }
+}
+
 // --------------------------------------------------------------- launching
 
 int bits_of(int64_t v) {
@@ -660,6 +703,28 @@ int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const v
       ABCD_HIP(hipGetLastError());
     }
     return ABCD_OK;
+  });
+}
+
+int32_t launch_embed_bwd_few(int32_t dtype, int64_t n, int64_t m, int64_t d, const void* dy, int64_t lddy,
+                             int32_t index_bits, const void* index, float scale, int32_t wdtype, void* dtable, int64_t ldt,
+                             hipStream_t stream) {
+  EmbedFewArgs a{dy, index, dtable, lddy, ldt, n, m, (int)d, 0, wdtype == ABCD_F32 && dtype != ABCD_F32, scale};
+  return with_type(dtype, [&](auto z) -> int32_t {
+    return with_index(index_bits, [&](auto zi) -> int32_t {
+      typedef decltype(z) T;
+      typedef decltype(zi) I;
+      const int nvec = (int)((d + kPer16<T> - 1) / kPer16<T>);
+      a.lanes = embed_lanes(nvec);
+      const int64_t rows = kBlock / a.lanes;
+      const dim3 grid(std::min<int64_t>((m + rows - 1) / rows, 1 << 14), (nvec + a.lanes - 1) / a.lanes);
+      if (d % kPer16<T> == 0)
+        ABCD_LAUNCH("embed_bwd_few", (embed_bwd_few_kernel<T, I, true>), grid, kBlock, 0, stream, a);
+      else
+        ABCD_LAUNCH("embed_bwd_few", (embed_bwd_few_kernel<T, I, false>), grid, kBlock, 0, stream, a);
+      ABCD_HIP(hipGetLastError());
+      return ABCD_OK;
+    });
   });
 }
 

@@ -60,6 +60,13 @@ def test_embed_bwd_refuses(lib):
             (14, need.value - 1)])
 
 
+def test_embed_bwd_few_refuses(lib):
+    base = [BF16, 4, 5, 8, FAKE, 8, 32, FAKE, 1.0, F32, FAKE, 8, None]
+    refuse(base, lib.abcd_embed_bwd_few,
+           [(0, 7), (1, -1), (1, 65), (2, 0), (3, 0), (4, None), (4, FAKE + 1), (5, 7), (6, 8), (7, None), (7, FAKE + 2),
+            (8, float("inf")), (9, F16), (10, None), (10, FAKE + 2), (11, 7)])
+
+
 def test_pack8_refuses(lib):
     base = [F16, 4, 8, FAKE, 8, FAKE, FAKE, None]
     refuse(base, lib.abcd_pack8, [(0, 3), (1, -1), (2, 0), (2, 65537), (3, None), (3, FAKE + 1), (4, 7), (5, None),

@@ -55,7 +55,7 @@ def indices(seed, n, m, how):
     return i
 
 
-SHAPES = [(1, 1, 1), (1, 7, 64), (5, 3, 7), (63, 64, 16), (64, 1, 8), (65, 2, 129), (129, 40, 59), (700, 1023, 33),
+SHAPES = [(1, 1, 1), (1, 7, 64), (7, 100000, 24), (64, 5000, 600), (50, 40, 5), (5, 3, 7), (63, 64, 16), (64, 1, 8), (65, 2, 129), (129, 40, 59), (700, 1023, 33),
           (1000, 1024, 64), (4097, 5, 100), (3000, 70000, 5), (900, 300, 2053)]
 
 
@@ -83,7 +83,7 @@ def test_embed_both_ways(api, dtype, n, m, d):
         assert got.dtype == tdtype and got.shape == (m, d)
         D.close("dtable", got, ref, mag, k=terms)
         kept = api.embed_sort(gi, m)
-        for _ in range(2):  # the same result again, from the same plan
+        for _ in range(2):  # the same result again, from the same plan (few positions add up alike either way)
             assert torch.equal(api.embed_bwd(dy, kept, m, scale, wdtype=tdtype), got)
         out = rand(3, m, d, tdtype, 3, 1)
         assert api.embed_bwd(dy, kept, m, scale, out=out) is out and torch.equal(out, got)
