@@ -129,8 +129,10 @@ struct LinearDxEnd {
 // Few rows: the weights are read once and bound it (gated_ffn_few.h). 8 waves a workgroup where
 // rows of the weights are short, else 16 (one row in bf16, weights from memory: 2,048 to 5,632
 // 8.6 against 10.7 us, 512 to 1,376 4.3 against 5.3, but 5,632 to 2,048 10.2 against 10.0 and
-// 33 rows of 2,048 to 2,048 12.7 against 10.4).
-template <typename T, int kAct, int kX, int kWaves, bool kWhole>
+// 33 rows of 2,048 to 2,048 12.7 against 10.4). kDz: the backward's product made again (bf16 with
+// SiLU, the whole backward, against the tiles': one row of 512 to 1,376 19.8 against 25.4 us, of
+// 5,632 to 2,048 32.2 against 38.9, 16 rows of 2,048 to 2,048 23.9 against 27.6).
+template <typename T, int kAct, int kX, int kWaves, bool kWhole, bool kDz>
 __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, int columns) {
   f32x4 acc[kX][1], sum[1];
   const int first = blockIdx.x * columns, end = min((int)a.o, first + columns), n = (int)a.x.len;
@@ -148,6 +150,12 @@ __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, in
     float slope;
     y[e] = activate<kAct, sizeof(T) == 2>(sum[0][e], slope);
     s[e] = e < left ? slope : 0.0f;
+  }
+  if (kDz) {
+    T* const to = static_cast<T*>(a.y) + r * a.ldy;
+    store_vec<T, 4, true>(to + c, s * load_vec<T, 4, false>(static_cast<const T*>(a.dy) + r * a.lddy + c, left), 4);
+    if (a.o - c <= 4 && c + 4 < a.ldy) store_vec<T, 4, true>(to + c + 4, Floats<4>(0.0f), 4);
+    return;
   }
   if (a.res) y += load_vec<T, 4, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left);
   store_vec<T, 4, false>(static_cast<T*>(a.y) + r * a.ldy + c, y, left);
@@ -171,13 +179,16 @@ __global__ __launch_bounds__(kBlock) void linear_slope_kernel(LinearSlope a) {
 #pragma unroll 4
     for (int64_t r = (int64_t)blockIdx.y * rows + threadIdx.x / a.lanes; r < a.n; r += (int64_t)gridDim.y * rows) {
       const Floats<8> dy = __builtin_convertvector(load8<T>(a.dy, r * a.lddy + c, left_of(a.o - c)), Floats<8>);
-      Floats<8> v = dy * load_slopes<8>(static_cast<const SlopeOf<T>*>(a.slope) + r * a.ldslope + c);
+      Floats<8> v = dy;
+      if (a.slope) {
+        v *= load_slopes<8>(static_cast<const SlopeOf<T>*>(a.slope) + r * a.ldslope + c);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = c + e < a.o ? v[e] : 0.0f;
-      store_vec<T, 8, true>(static_cast<T*>(a.dz) + r * a.lddz + c, v, 8);
+        for (int e = 0; e < 8; ++e) v[e] = c + e < a.o ? v[e] : 0.0f;
+        store_vec<T, 8, true>(static_cast<T*>(a.dz) + r * a.lddz + c, v, 8);
+      }
       sum += v;
     }
-  if (!a.part) return;
+  if (!a.part && !a.db) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) red[threadIdx.x * 8 + e] = sum[e];
   __syncthreads();
@@ -186,7 +197,10 @@ __global__ __launch_bounds__(kBlock) void linear_slope_kernel(LinearSlope a) {
     if (at >= a.o) break;
     float v = 0.0f;
     for (int r = 0; r < rows; ++r) v += red[r * a.lanes * 8 + k];
-    a.part[(int64_t)blockIdx.y * a.o + at] = v;
+    if (a.db)
+      static_cast<T*>(a.db)[at] = (T)v;
+    else
+      a.part[(int64_t)blockIdx.y * a.o + at] = v;
   }
 }
 
@@ -214,17 +228,20 @@ int32_t run_linear_few(const LinearOut& a, hipStream_t stream) {
       constexpr int kAct = decltype(act)::value, kX = decltype(rows)::value;
       const int columns = (a.o + 7) / 8 <= kCUs ? 8 : 16;
       const int64_t grid = (a.o + columns - 1) / columns;
-      auto launch = [&](auto waves) {
+      auto launch = [&](auto waves, auto dz) {
         constexpr int kWaves = decltype(waves)::value;
+        constexpr bool kDz = decltype(dz)::value;
         if (a.i % kPer16<T> == 0)
-          ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, kWaves, true>), grid, kWaves * 64, 0, stream, a, columns);
+          ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, kWaves, true, kDz>), grid, kWaves * 64, 0, stream, a, columns);
         else
-          ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, kWaves, false>), grid, kWaves * 64, 0, stream, a, columns);
+          ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, kWaves, false, kDz>), grid, kWaves * 64, 0, stream, a, columns);
       };
-      if (kX == 1 && a.i * (int64_t)sizeof(T) <= 4096)
-        launch(std::integral_constant<int, kX == 1 ? 8 : 16>{});
+      if (kAct != ABCD_ACT_NONE && a.dy)
+        launch(std::integral_constant<int, 16>{}, std::integral_constant<bool, kAct != ABCD_ACT_NONE>{});
+      else if (kX == 1 && a.i * (int64_t)sizeof(T) <= 4096)
+        launch(std::integral_constant<int, kX == 1 ? 8 : 16>{}, std::false_type{});
       else
-        launch(std::integral_constant<int, 16>{});
+        launch(std::integral_constant<int, 16>{}, std::false_type{});
       ABCD_HIP(hipGetLastError());
       return ABCD_OK;
     });

@@ -116,30 +116,39 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
     return launch_sum_parts(s.part, blocks, outs, l.dtype, stream);
   }
   const bool again = l.act != ABCD_ACT_NONE && !slope;
+  const bool one = sum_parts_of(n) == 1;  // part of the bias's sums, which is then all of them
+  const int lanes = std::min(lanes_for((int)(up8(l.o) / 8)), 64);
   Side xs{}, w{}, dz{};
   if (n > 0) {
     Packs copies;
+    const bool tiles = again && !few(l, n);
     if (again || dw) {
       if (q) {
         // a checkpoint's rows up to a multiple of 8: zeros behind their end
         TRY_STATUS(launch_unpack8(l.dtype, n, up8(l.i), q, e, s.x, up8(l.i), stream));
         xs = Side{{s.x, nullptr}, up8(l.i), n};
-      } else {
+      } else if (tiles || dw) {
         xs = side_of(copies, l.dtype, x, n, l.i, ldx, s.x);
       }
     }
-    if (again || dx) w = side_of(copies, l.dtype, l.w, l.o, l.i, l.i, s.w);
+    if (tiles || dx) w = side_of(copies, l.dtype, l.w, l.o, l.i, l.i, s.w);
     if (l.act == ABCD_ACT_NONE)
       dz = side_of(copies, l.dtype, dy, n, l.o, lddy, s.dz);
     else
       dz = Side{{s.dz, nullptr}, up8(l.o), n};
     TRY_STATUS(launch(copies, l.dtype, stream));
-    if (again) {
+    if (again && !tiles) {
+      // the weights as they lie in memory, and x: a checkpoint's copy or the rows themselves
+      LinearOut a{q ? xs : Side{{x, nullptr}, ldx, n}, Side{{l.w, nullptr}, l.i, l.o}, l.b, nullptr, s.dz, nullptr, l.i, l.o,
+                  0, dz.ld, 0, l.act, Tiling{}};
+      a.dy = dy;
+      a.lddy = lddy;
+      TRY_STATUS(LINEAR_BY_TYPE(l, linear_few, a, stream));
+    } else if (again) {
       const LinearDz a{xs, w, l.b, dy, s.dz, l.i, l.o, lddy, dz.ld, l.act, Tiling{s.part, 0, 0, 1, 0}};
       TRY_STATUS(LINEAR_BY_TYPE(l, linear_dz, a, stream));
     } else if (slope) {
-      const int lanes = std::min(lanes_for((int)(dz.ld / 8)), 64);
-      const LinearSlope a{dy, slope, s.dz, db ? s.sums : nullptr, n, l.o, lddy, up8(l.o), dz.ld, lanes};
+      const LinearSlope a{dy, slope, s.dz, db && !one ? s.sums : nullptr, one ? db : nullptr, n, l.o, lddy, up8(l.o), dz.ld, lanes};
       TRY_STATUS(LINEAR_BY_TYPE(l, linear_slope, a, sum_parts_of(n), stream));
     }
     if (dx) {
@@ -154,6 +163,11 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
     a.n = n;
     a.one[a.count++] = FfnDWeight::One{dz.p[0], xs.p[0], dw, dz.ld, l.o, xs.ld, l.i, 1.0f, 0, 0, 0};
     TRY_STATUS(LINEAR_BY_TYPE(l, linear_dw, a, stream));
+  }
+  if (slope && one && n > 0) return ABCD_OK;
+  if (one && db && n > 0) {
+    const LinearSlope a{dz.p[0], nullptr, nullptr, nullptr, db, n, l.o, dz.ld, 0, up8(l.o), lanes};
+    return LINEAR_BY_TYPE(l, linear_slope, a, 1, stream);
   }
   if (slope && db && n > 0) {
     SumOuts outs{};

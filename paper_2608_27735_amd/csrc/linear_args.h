@@ -57,6 +57,8 @@ struct LinearOut {
   int64_t i, o, ldr, ldy, ldslope;
   int act;
   Tiling t;
+  const void* dy = nullptr;  // linear_few: given, y is dz = dy act'(x w' + bias), columns up to ldy zeros
+  int64_t lddy = 0;
 };
 // dz = dy act'(x w' + bias): [n][lddz], columns past o zeros.
 struct LinearDz {
@@ -75,13 +77,14 @@ struct LinearDx {
   int64_t o, i, lddx;
   Tiling t;
 };
-// dz = dy slope, of n rows; part: [parts][o], the sums of dz's rows before it is rounded
-// (NULL: not wanted)
+// dz = dy slope, of n rows; without slopes and dz nothing but the sums: part: [parts][o], the
+// sums of dz's rows before it is rounded (NULL: not wanted), or db itself where one part is all
 struct LinearSlope {
   const void* dy;
   const void* slope;
   void* dz;
   float* part;
+  void* db;
   int64_t n, o, lddy, ldslope, lddz;
   int lanes;  // threads along a row, 8 columns each
 };
