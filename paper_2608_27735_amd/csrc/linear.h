@@ -128,10 +128,10 @@ struct LinearDxEnd {
 
 // Few rows: the weights are read once and bound it (gated_ffn_few.h). 8 waves a workgroup where
 // rows of the weights are short, else 16 (one row in bf16, weights from memory: 2,048 to 5,632
-// 8.6 against 10.7 us, 512 to 1,376 4.3 against 5.3, but 5,632 to 2,048 10.2 against 10.0 and
+// 7.6 against 10.0 us, 512 to 1,376 4.3 against 5.3, but 5,632 to 2,048 10.2 against 10.1 and
 // 33 rows of 2,048 to 2,048 12.7 against 10.4). kDz: the backward's product made again (bf16 with
-// SiLU, the whole backward, against the tiles': one row of 512 to 1,376 19.8 against 25.4 us, of
-// 5,632 to 2,048 32.2 against 38.9, 16 rows of 2,048 to 2,048 23.9 against 27.6).
+// SiLU, the whole backward, against the tiles': one row of 512 to 1,376 18.4 against 25.4 us, of
+// 5,632 to 2,048 31.8 against 38.9, 16 rows of 2,048 to 2,048 22.6 against 27.6).
 template <typename T, int kAct, int kX, int kWaves, bool kWhole, bool kDz>
 __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, int columns) {
   f32x4 acc[kX][1], sum[1];
@@ -221,12 +221,26 @@ int32_t run_linear_dx(const LinearDx& a, hipStream_t stream) {
   return run_product<T>("linear_dx", LinearDxEnd<T>{a}, stream);
 }
 
+// Columns a workgroup: those that leave a CU the fewest in turn, one more counted for what each
+// workgroup costs (one row in bf16, weights from memory, 8, 12 and 16: 2,048 to 5,632 8.6, 7.6 and
+// 8.6 us; 4,096 to 4,096 11.4, 12.2 and 9.8; 2,048 to 2,048 5.1, 5.3 and 5.5; 4 of them 11.9, 16.2
+// and 6.1).
+inline int few_columns(int64_t o) {
+  int best = 0;
+  int64_t least = 0;
+  for (int columns : {16, 12, 8}) {
+    const int64_t takes = ((o + columns - 1) / columns + kCUs - 1) / kCUs * (columns + 1);
+    if (best == 0 || takes < least) best = columns, least = takes;
+  }
+  return best;
+}
+
 template <typename T>
 int32_t run_linear_few(const LinearOut& a, hipStream_t stream) {
   return with_any_act(a.act, [&](auto act) -> int32_t {
     return with_rows(a.x.len, [&](auto rows) -> int32_t {
       constexpr int kAct = decltype(act)::value, kX = decltype(rows)::value;
-      const int columns = (a.o + 7) / 8 <= kCUs ? 8 : 16;
+      const int columns = few_columns(a.o);
       const int64_t grid = (a.o + columns - 1) / columns;
       auto launch = [&](auto waves, auto dz) {
         constexpr int kWaves = decltype(waves)::value;
@@ -236,12 +250,16 @@ int32_t run_linear_few(const LinearOut& a, hipStream_t stream) {
         else
           ABCD_LAUNCH("linear_few", (linear_few_kernel<T, kAct, kX, kWaves, false, kDz>), grid, kWaves * 64, 0, stream, a, columns);
       };
+      auto by_waves = [&](auto dz) {
+        if (kX == 1 && a.i * (int64_t)sizeof(T) <= 4096)
+          launch(std::integral_constant<int, kX == 1 ? 8 : 16>{}, dz);
+        else
+          launch(std::integral_constant<int, 16>{}, dz);
+      };
       if (kAct != ABCD_ACT_NONE && a.dy)
-        launch(std::integral_constant<int, 16>{}, std::integral_constant<bool, kAct != ABCD_ACT_NONE>{});
-      else if (kX == 1 && a.i * (int64_t)sizeof(T) <= 4096)
-        launch(std::integral_constant<int, kX == 1 ? 8 : 16>{}, std::false_type{});
+        by_waves(std::integral_constant<bool, kAct != ABCD_ACT_NONE>{});
       else
-        launch(std::integral_constant<int, 16>{}, std::false_type{});
+        by_waves(std::false_type{});
       ABCD_HIP(hipGetLastError());
       return ABCD_OK;
     });

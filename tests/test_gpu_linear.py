@@ -110,6 +110,13 @@ def test_few_rows(api, n, i, o):
 
 
 @pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,i,o", [(1, 40, 2101), (17, 72, 2049), (3, 33, 4999), (16, 8, 6145)])
+def test_few_rows_of_many_columns(api, dtype, n, i, o):
+    run(api, n, i, o, dtype, "gelu")
+    run(api, n, i, o, dtype, None, pad=3, skip=1)
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
 @pytest.mark.parametrize("n,i,o", [(137, 1024, 520), (70, 600, 2100), (65, 4000, 9), (200, 33, 3001), (300, 2515, 260)])
 def test_few_tiles_and_long_sums(api, dtype, n, i, o):
     run(api, n, i, o, dtype, "silu")
