@@ -654,7 +654,7 @@ ABCD_API int32_t abcd_linear_bwd(const abcd_layer* layer /* host */, int64_t n, 
  * render_cache, cache_rect_init, layer_norm, layer_norm_bwd, layer_norm_cols,
  * sum_parts, dropout, pack_rows, column_sums, ffn_in, ffn_out, ffn_dhidden, ffn_dx,
  * ffn_join, ffn_dweight, ffn_dweight_sum, ffn_narrow, ffn_narrow_bwd, ffn_few_in, ffn_few_out,
- * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_few, embed_bwd, embed_bwd_few,
+ * embed, embed_count, embed_scan, embed_scatter, embed_ranges, embed_rank, embed_bwd, embed_bwd_few,
  * embed_join, pack8, unpack8, residual_norm, residual_norm_bwd, residual_norm_sums,
  * linear_out, linear_few, linear_dz, linear_dx, linear_slope, linear_narrow,
  * linear_narrow_bwd). */

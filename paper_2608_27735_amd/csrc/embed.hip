@@ -8,7 +8,7 @@
 // The sort: positions by index, equal ones in order (stable, least digit first), with
 // counts of every digit by parts of kSortPart keys, their prefix sums, and a scatter whose
 // ranks come from ballots: three launches for each digit of up to kSortBits bits, and no
-// atomics on memory. ranges[r] is where row r's positions begin and end in that order.
+// atomics on memory; of few positions all pairs compared in one launch. ranges[r] is where row r's positions begin and end in that order.
 //
 // The gradient: rows of up to kRun positions are added up by the lanes that write them;
 // of longer ones (a feature that thousands share, a frequent token) every chunk of kRun
@@ -20,7 +20,7 @@
 // written). Gradient of the same in fp32: sums 57 us (285 MB, 5.0 TB/s), and 54 for the sort
 // in seven launches, of which the scatters are 12 and 10 and the others 4 to 8, near what a
 // launch takes. 8,192 positions of 2,048 in bf16 into 32,000 rows: 32 us (the gradient's 131 MB
-// written), the sort 24 in two launches, waiting in one workgroup.
+// written), the sort 13 in two launches.
 #include <algorithm>
 
 #include "sides.h"
@@ -261,91 +261,90 @@ __global__ __launch_bounds__(kBlock) void embed_scatter_kernel(SortArgs a) {
   }
 }
 
-// Few positions: one workgroup sorts them in LDS, digits of up to kFewBits bits, and marks
-// the rows that have any (embed_count's workgroups have marked all as empty). 8,192: 20 us, by
-// the launches for many 52; with its loops rolled up 22.
-constexpr int kFewWaves = 16, kFewTurns = 8, kFewMost = kFewWaves * kWave * kFewTurns, kFewBits = 8;
-template <typename I>
-__global__ __launch_bounds__(kFewWaves* kWave) void embed_few_kernel(SortArgs a) {
-  constexpr int kThreads = kFewWaves * kWave;
-  __shared__ uint32_t keys[kFewMost];
-  __shared__ uint16_t vals[kFewMost];
-  __shared__ uint32_t at[1 << kFewBits][kFewWaves + 1];  // by digit and wave: counts, then next places
-  __shared__ uint32_t sums[kFewWaves];
-  const int n = (int)a.n, w = threadIdx.x / kWave, l = threadIdx.x % kWave, digits = 1 << a.bits;
-  // a wave's keys are consecutive: as many turns as it takes
-  const int turns = (n + kThreads - 1) / kThreads, first = w * turns * kWave + l;
-  uint32_t key[kFewTurns], val[kFewTurns], place[kFewTurns];
+// Few positions: place of key i is the number of keys below it and of equal ones before it. A
+// workgroup has kRankKeys keys, one a lane and twice in each wave, and half a wave compares them
+// with a part of all keys, read from LDS: a subtraction whose borrow is counted and whose zeros
+// are the equal ones. Keys with no equal one before or behind them begin or end their row
+// (embed_count's workgroups have marked all rows as empty).
+//
+// Five instructions for two comparisons bound it: both launches take 6.3 us for 1,000 positions,
+// 12.8 for 8,192 (one workgroup that sorts digits of 8 bits in LDS 9.5 and 22, of 1M rows 12.4 and
+// 34; ballots counted by the scalar unit 7.9 and 22), and by the launches for many 8,193 take 16 with
+// 1,000 rows, 27 with 32,000 and 39 with 1M.
+constexpr int kRankKeys = 32, kRankWaves = 16, kRankMost = 8192;
+template <typename I, int kTurns>
+__global__ __launch_bounds__(kRankWaves* kWave) void embed_rank_kernel(SortArgs a) {
+  constexpr int kPart = kTurns * kRankKeys;  // keys of half a wave
+  constexpr uint32_t kNone = 0xffffffffu;    // neither below nor equal to any
+  __shared__ __align__(16) uint32_t keys[kRankWaves * 2 * kPart];
+  __shared__ int places[kRankWaves][kRankKeys], alike[kRankWaves][kRankKeys];
+  const int n = (int)a.n, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = threadIdx.x % kWave;
+  const int first = blockIdx.x * kRankKeys, mine = first + l % kRankKeys;
 #pragma unroll
-  for (int k = 0; k < kFewTurns; ++k) {
-    const int i = first + k * kWave;
-    val[k] = (uint32_t)i;
-    key[k] = k < turns && i < n ? sort_key<I>(a, i) : 0u;
+  for (int k = 0; k < kTurns; ++k) {  // a wave's own part
+    const int i = w * 2 * kPart + k * kWave + l;
+    keys[i] = i < n ? sort_key<I>(a, i) : kNone;
   }
-  for (int shift = 0; shift < a.shift; shift += a.bits) {
-    for (int i = threadIdx.x; i < digits * (kFewWaves + 1); i += kThreads) (&at[0][0])[i] = 0;
-    __syncthreads();
+  const uint32_t own = mine < n ? sort_key<I>(a, mine) : kNone;
+  __syncthreads();
+  const int begin = w * 2 * kPart + l / kRankKeys * kPart;  // of the half wave's part
+  int place = 0, equal = 0;  // equal: bit 0 before it, bit 1 behind it
+  // count keys from `from` on, which lie all in front or all behind; in front the order is turned
+  // round by `flip`, what is below then being above
+  auto compare = [&](int from, auto count, auto front, uint32_t flip) {
+    const uint32_t o = own ^ flip;
+    uint32_t least = kNone;
+    int below = 0;
+#pragma unroll 4
+    for (int t = 0; t < decltype(count)::value; t += 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(keys + from + t);
 #pragma unroll
-    for (int k = 0; k < kFewTurns; ++k) {
-      if (k >= turns) break;
-      const bool in = first + k * kWave < n;
-      const uint32_t d = (key[k] >> shift) & (uint32_t)(digits - 1);
-      const uint64_t same = same_digit<kFewBits>(d, in);
-      uint32_t start = 0;
-      const int leader = in ? __ffsll((unsigned long long)same) - 1 : l;
-      if (in && l == leader) start = atomicAdd(&at[d][w], (uint32_t)__popcll(same));
-      place[k] = (uint32_t)__shfl((int)start, leader, 64) + (uint32_t)__popcll(same & ((1ull << l) - 1ull));
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t other = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
+        uint32_t d;  // (own - other is ~other - ~own)
+        below += decltype(front)::value ? __builtin_usub_overflow(own, other, &d) : __builtin_usub_overflow(other ^ flip, o, &d);
+        least = min(least, d);
+      }
     }
-    __syncthreads();
-    // counts by digit, then wave, become places: kPer of them next to each other a thread
-    constexpr int kPer = (kFewWaves << kFewBits) / kThreads;
-    const int per = digits * kFewWaves / kThreads > 0 ? digits * kFewWaves / kThreads : 1;
-    const bool takes = (int)threadIdx.x * per < digits * kFewWaves;
-    uint32_t own[kPer], total = 0;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int e = (int)threadIdx.x * per + k;
-      own[k] = takes && k < per ? at[e / kFewWaves][e % kFewWaves] : 0u;
-      total += own[k];
-    }
-    uint32_t all;
-    uint32_t before = wave_before(total, all);
-    if (l == 0) sums[w] = all;
-    __syncthreads();
-    for (int v = 0; v < w; ++v) before += sums[v];
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int e = (int)threadIdx.x * per + k;
-      if (takes && k < per) at[e / kFewWaves][e % kFewWaves] = before;
-      before += own[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kFewTurns; ++k) {
-      if (k >= turns || first + k * kWave >= n) break;
-      const uint32_t to = at[(key[k] >> shift) & (uint32_t)(digits - 1)][w] + place[k];
-      keys[to] = key[k];
-      vals[to] = (uint16_t)val[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kFewTurns; ++k) {
-      const int i = first + k * kWave;
-      if (k >= turns || i >= n) break;
-      key[k] = keys[i];
-      val[k] = vals[i];
+    place += flip ? decltype(count)::value - below : below;
+    if (least == 0) equal |= flip ? 1 : 2;
+  };
+  if (first >= (w + 1) * 2 * kPart) {
+    compare(begin, std::integral_constant<int, kPart>{}, std::true_type{}, ~0u);
+  } else if (first < w * 2 * kPart) {
+    compare(begin, std::integral_constant<int, kPart>{}, std::false_type{}, 0u);
+  } else {
+    for (int from = begin; from < begin + kPart; from += kRankKeys) {
+      if (from != first) {
+        compare(from, std::integral_constant<int, kRankKeys>{}, std::false_type{}, from < first ? ~0u : 0u);
+        continue;
+      }
+      for (int t = 0; t < kRankKeys; ++t) {
+        const uint32_t other = keys[from + t];
+        place += other < own || (other == own && from + t < mine);
+        if (other == own && from + t != mine) equal |= from + t < mine ? 1 : 2;
+      }
     }
   }
-#pragma unroll
-  for (int k = 0; k < kFewTurns; ++k) {
-    const int i = first + k * kWave;
-    if (k >= turns || i >= n) break;
-    a.keys_out[i] = key[k];
-    a.vals_out[i] = val[k];
-    if (key[k] >= (uint32_t)a.m) continue;
-    if (i == 0 || keys[i - 1] != key[k]) a.ranges[key[k]].x = i;
-    if (i == n - 1 || keys[i + 1] != key[k]) a.ranges[key[k]].y = i + 1;
+  place += __shfl_xor(place, kRankKeys, kWave);
+  equal |= __shfl_xor(equal, kRankKeys, kWave);
+  if (l < kRankKeys) {
+    places[w][l] = place;
+    alike[w][l] = equal;
   }
+  __syncthreads();
+  if ((int)threadIdx.x >= kRankKeys || mine >= n) return;
+  place = equal = 0;
+#pragma unroll
+  for (int v = 0; v < kRankWaves; ++v) {
+    place += places[v][l];
+    equal |= alike[v][l];
+  }
+  a.keys_out[place] = own;
+  a.vals_out[place] = (uint32_t)mine;
+  if (own >= (uint32_t)a.m) return;
+  if (!(equal & 1)) a.ranges[own].x = place;
+  if (!(equal & 2)) a.ranges[own].y = place + 1;
 }
 
 __global__ __launch_bounds__(kBlock) void embed_ranges_kernel(SortArgs a) {
@@ -502,7 +501,9 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedBwdA
 }
 
 // Up to a wave's lanes of positions, without a sort: every wave has all indexes, and finds by a
-// ballot those that name one of the rows it writes.
+// ballot those that name one of the rows it writes. The table's bytes or the launch bound it: 4
+// positions of 24,402 x 40 in fp16 9.1 us a call (with a sort 26), 64 of 1M x 64 in bf16 19.5 (41),
+// 64 that all name one of 16 rows of 2,048 15.4.
 struct EmbedFewArgs {
   const void* dy;
   const void* index;
@@ -627,19 +628,28 @@ int32_t launch_embed_sort(int64_t n, int64_t m, int32_t index_bits, const void* 
   a.bits = s.bits;
   return with_index(index_bits, [&](auto zi) -> int32_t {
     typedef decltype(zi) I;
-    if (n <= kFewMost) {
-      const int bits = bits_of(m);
+    if (n <= kRankMost) {
       const int64_t zero = std::min<int64_t>((m + kBlock - 1) / kBlock, 2048);
       a.parts = 0;  // all that this does is mark the rows
       ABCD_LAUNCH("embed_count", (embed_count_kernel<I>), zero, kBlock, 0, stream, a);
       ABCD_HIP(hipGetLastError());
       if (n == 0) return ABCD_OK;
-      const int passes = (bits + kFewBits - 1) / kFewBits;
-      a.bits = (bits + passes - 1) / passes;
-      a.shift = passes * a.bits;
       a.keys_out = reinterpret_cast<uint32_t*>(rows);
       a.vals_out = reinterpret_cast<uint32_t*>(order);
-      ABCD_LAUNCH("embed_few", (embed_few_kernel<I>), 1, kFewWaves * kWave, 0, stream, a);
+      const int64_t grid = (n + kRankKeys - 1) / kRankKeys;
+      auto rank = [&](auto turns) {
+        ABCD_LAUNCH("embed_rank", (embed_rank_kernel<I, decltype(turns)::value>), grid, kRankWaves * kWave, 0, stream, a);
+      };
+      constexpr int kTurn = kRankWaves * kWave;  // keys
+      static_assert(8 * kTurn == kRankMost);
+      if (n <= kTurn)
+        rank(std::integral_constant<int, 1>{});
+      else if (n <= 2 * kTurn)
+        rank(std::integral_constant<int, 2>{});
+      else if (n <= 4 * kTurn)
+        rank(std::integral_constant<int, 4>{});
+      else
+        rank(std::integral_constant<int, 8>{});
       ABCD_HIP(hipGetLastError());
       return ABCD_OK;
     }

@@ -105,6 +105,12 @@ def test_sorted_positions(api, n, m):
         assert torch.equal(s.ranges[:, 0].cpu().long(), want) and torch.equal(s.ranges[:, 1].cpu().long(), want + count)
 
 
+@pytest.mark.parametrize("n", [31, 65, 1024, 1025, 2049, 4100, 8192, 8193, 16383, 16384, 16385])
+@pytest.mark.parametrize("m", [1, 60, 32000])
+def test_sorts_of_few_positions(api, n, m):
+    test_sorted_positions(api, n, m)
+
+
 def test_embed_of_no_positions(api):
     table = rand(1, 4, 9, torch.float16)
     none = torch.zeros(0, dtype=torch.int32, device="cuda")
