@@ -168,8 +168,9 @@ __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, in
 }
 
 // dz = dy slope, and the sums of its rows: a thread for 8 columns, `lanes` of them next to
-// each other, of rows blockIdx.y, + gridDim.y rows..
-template <typename T>
+// each other, of rows blockIdx.y, + gridDim.y rows.. Without slopes only the sums. (8,192 x 2,048 in
+// bf16 20.6 us; with the choice inside the loop, which keeps the loads apart, 25.3.)
+template <typename T, bool kSlope>
 __global__ __launch_bounds__(kBlock) void linear_slope_kernel(LinearSlope a) {
   __shared__ float red[kBlock * 8];
   const int t = threadIdx.x & (a.lanes - 1), rows = kBlock / a.lanes;
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(kBlock) void linear_slope_kernel(LinearSlope a) {
     for (int64_t r = (int64_t)blockIdx.y * rows + threadIdx.x / a.lanes; r < a.n; r += (int64_t)gridDim.y * rows) {
       const Floats<8> dy = __builtin_convertvector(load8<T>(a.dy, r * a.lddy + c, left_of(a.o - c)), Floats<8>);
       Floats<8> v = dy;
-      if (a.slope) {
+      if (kSlope) {
         v *= load_slopes<8>(static_cast<const SlopeOf<T>*>(a.slope) + r * a.ldslope + c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = c + e < a.o ? v[e] : 0.0f;
@@ -269,7 +270,10 @@ int32_t run_linear_few(const LinearOut& a, hipStream_t stream) {
 template <typename T>
 int32_t run_linear_slope(const LinearSlope& a, int64_t parts, hipStream_t stream) {
   const dim3 grid((a.lddz / 8 + a.lanes - 1) / a.lanes, parts);
-  ABCD_LAUNCH("linear_slope", (linear_slope_kernel<T>), grid, kBlock, 0, stream, a);
+  if (a.slope)
+    ABCD_LAUNCH("linear_slope", (linear_slope_kernel<T, true>), grid, kBlock, 0, stream, a);
+  else
+    ABCD_LAUNCH("linear_slope", (linear_slope_kernel<T, false>), grid, kBlock, 0, stream, a);
   ABCD_HIP(hipGetLastError());
   return ABCD_OK;
 }
