@@ -177,6 +177,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
   constexpr int kWaveBytes = 32 * (kXBytes + kZBytes), kSums = kOB * 16 * kIB * 16;
   constexpr bool kAgain = kMode != ABCD_ACT_NONE && kMode != kLinearKept;  // z is needed
   constexpr bool kEarly = kFrags <= 8 && kWhole;  // where the registers suffice
+  constexpr bool kLargest = !std::is_same<T, _Float16>::value;
   constexpr int kPool = kNarrowLayerWaves * kWaveBytes > kSums * 4 ? kNarrowLayerWaves * kWaveBytes : kSums * 4;
   __shared__ __align__(16) F along[kAgain ? kFrags * 64 : 1];
   __shared__ __align__(16) F across[kFrags * 64];
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(kNarrowLayerThreads, kDF * kOB <= 8 ? 2 : 1) void l
       for (int f = 0; f < kDF; ++f) {
         if (a.q) {
           const U4 v = __builtin_bit_cast(U4, nx[k][f / 2]);
-          x[k][f] = __builtin_convertvector(unpack_8(v[f % 2 * 2], v[f % 2 * 2 + 1], unit), F);
+          x[k][f] = __builtin_convertvector(unpack_8<kLargest>(v[f % 2 * 2], v[f % 2 * 2 + 1], unit), F);
         } else {
           x[k][f] = first_of<T, kWhole>(nx[k][f], i - (f * 32 + q * 8));
         }

@@ -20,7 +20,10 @@ __device__ __forceinline__ float unpacked(uint32_t word, int i, float unit) {
 }
 
 // Two words' eight. q + 128 is what an unsigned byte's conversion takes, and q unit =
-// (q + 128) unit - 128 unit is exact; what is not finite is found for a wave's lanes together.
+// (q + 128) unit - 128 unit is exact, but of the largest exponent, where 128 unit is an
+// infinity (kLargest: a type that has it, as float16 does not). That, and what is not finite,
+// is found for a wave's lanes together.
+template <bool kLargest>
 __device__ __forceinline__ Floats<8> unpack_8(uint32_t lo, uint32_t hi, float unit) {
   const uint32_t u[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
   const float off = -128.0f * unit;
@@ -28,10 +31,13 @@ __device__ __forceinline__ Floats<8> unpack_8(uint32_t lo, uint32_t hi, float un
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = fmaf((float)(u[i / 4] >> (8 * (i % 4)) & 255u), unit, off);
   const uint32_t zero = ((u[0] - 0x01010101u) & ~u[0]) | ((u[1] - 0x01010101u) & ~u[1]);  // of a byte 0 the top bit
-  if (__builtin_expect(__any((int)(zero & 0x80808080u)), 0)) {
+  if (__builtin_expect(__any((zero & 0x80808080u) != 0 || (kLargest && unit >= 0x1p121f)), 0)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if ((u[i / 4] >> (8 * (i % 4)) & 255u) == 0) v[i] = __builtin_nanf("");
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t b = u[i / 4] >> (8 * (i % 4)) & 255u;
+      if (kLargest) v[i] = ((float)b - 128.0f) * unit;
+      if (b == 0) v[i] = __builtin_nanf("");
+    }
   }
   return v;
 }

@@ -208,3 +208,26 @@ def test_linear_refuses(api):
         api.linear(many, w, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
     with pytest.raises(api.AbcdError):
         api.linear_bwd(dy, x, w, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("act", [None, "relu"])
+@pytest.mark.parametrize("n,i,o", [(40, 64, 64), (300, 70, 24), (5, 33, 9), (70, 128, 60), (90, 40, 300)])
+def test_checkpoint_of_the_largest_numbers(api, dtype, act, n, i, o):
+    """A block whose exponent is the type's largest stands for the same numbers in the layer's
+    gradients as unpacked. (One number of that size a row, so that no sum leaves the type, and
+    the sign of z, which ReLU's slope goes by, is that of its product.)"""
+    x = rand(1, n, i, dtype)
+    x[:, 5] = torch.finfo(dtype).max * (1.0 - 2.0 * (torch.arange(n) % 2)).cuda()
+    w = rand(2, o, i, dtype, scale=i ** -0.5).contiguous()
+    w[:, 5] = torch.where(w[:, 5] < 0, -0.25, 0.25)
+    dy = (2.0 ** -10 * (1 + (torch.arange(n * o) * 7 % 3).view(n, o))).to(dtype).cuda()
+    packed = api.pack8(x)
+    rows = api.unpack8(packed)
+    assert torch.isfinite(rows).all() and (rows[:, 5].abs() > 0.98 * torch.finfo(dtype).max).all()
+    got, want = api.linear_bwd(dy, packed, w, act=act), api.linear_bwd(dy, rows, w, act=act)
+    x8, w64, dy64 = D.d64(rows), D.d64(w), D.d64(dy)
+    assert torch.equal(got["x"], want["x"])
+    dz = dy64 if act is None else dy64 * ((x8 @ w64.T) > 0)
+    D.close("dw", got["w"], dz.T @ x8, dz.abs().T @ x8.abs())
+    D.close("dx", got["x"], dz @ w64, dz.abs() @ w64.abs())
