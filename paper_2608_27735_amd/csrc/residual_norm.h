@@ -232,7 +232,10 @@ __device__ __forceinline__ void put_params(const JointArgs& a, int c, Floats<N> 
   const Floats<N> sc = joint_param<T, N, kWhole>(a, a.scale, c, 1.0f);
   put(a.dpost_w, sc * s1);
   put(a.dpost_b, sc * s0);
-  put(a.dscale, joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f) * s1 + joint_param<T, N, kWhole>(a, a.post_b, c, 0.0f) * s0);
+  // (without a bias S0 does not count, not even an infinite one, which 0 would make a NaN)
+  Floats<N> ds = joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f) * s1;
+  if (a.post_b) ds += joint_param<T, N, kWhole>(a, a.post_b, c, 0.0f) * s0;
+  put(a.dscale, ds);
   put(a.dpre_w, dw);
   put(a.dpre_b, db);
 }

@@ -179,3 +179,22 @@ def test_joint_refuses(api):
         api.residual_norm(f, x, post="rms", eps=-1.0)
     with pytest.raises(api.AbcdError):
         bwd(workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("post", [None, "rms", "layer"])
+@pytest.mark.parametrize("n,d", [(5, 64), (3000, 64), (40, 1001), (5, 20001)])
+def test_scale_gradient_of_infinite_rows(api, dtype, post, n, d):
+    """An infinity in dy makes scale's gradient of its column that infinity, not a NaN, where
+    the norm has no bias to multiply it with."""
+    f, x, p, _ = make(n, d, dtype, post, None, "none")
+    p.pop("post_bias", None)
+    call = dict(post=post, params=p)
+    r = api.residual_norm(f, x, **call)
+    dy = rand(12, n, d, dtype)
+    dy[3, 7], dy[n - 1, d - 2] = math.inf, -math.inf
+    got = api.residual_norm_bwd(None, dy, f, r, grads=dict(scale=torch.empty_like(p["scale"])), **call)["scale"]
+    stats = {k: D.d64(r[k]) for k in ("post_mean", "post_rstd") if r[k] is not None}
+    want, mag = R.residual_norm_bwd(None, D.d64(dy), D.d64(f), None, stats, post, None, {k: D.d64(v) for k, v in p.items()}, None)["scale"]
+    assert want.isinf().sum() == 2 and not want.isnan().any()
+    D.close("scale", got, want, mag, k=K)
