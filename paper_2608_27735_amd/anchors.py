@@ -8,8 +8,9 @@ feed-forward block,
     y = x + s g layer_norm(ffn(layer_norm(x))),  z = layer_norm(y)
     sh = z w_out' + b_out
 and the step renders with these SH coefficients. Features and weights are kept in
-fp32 for Adam; the operators run in `dtype`. With checkpoints8 the linear layers'
-inputs are kept for the backward pass in 8 bits. Run as a program it fits the
+fp32 for Adam; the operators run in `dtype`. With checkpoints8 the first and the last
+linear layer's inputs are kept for the backward pass in 8 bits (x itself, the gate's
+input, is needed there by the norm and kept as it is). Run as a program it fits the
 colours of a small synthetic scene:
     python -m paper_2608_27735_amd.anchors
 """
@@ -98,7 +99,8 @@ class AnchorDecoder:
         j = api.residual_norm(f["y"], x, gate=gate, **self._joint(w))
         sh = api.linear(j["z"], w["w_out"], w["b_out"])["y"]
         if train:
-            self._kept = (w, keep(e), x, keep(x) if self.checkpoints8 else x, gate, n, f, j, keep(j["z"]))
+            z = keep(j.pop("z"))  # all that the backward pass needs of j are y and the statistics
+            self._kept = (w, keep(e), x, gate, n, f, j, z)
         return sh.float().view(-1, self.nc, 3)
 
     def backward(self, d_sh):
@@ -106,13 +108,13 @@ class AnchorDecoder:
         that the last forward() with train=True gave; once for each of these."""
         if self._kept is None:
             raise ValueError("backward() needs a forward() with train=True before it")
-        w, e, x, x_kept, gate, n, f, j, z = self._kept
+        w, e, x, gate, n, f, j, z = self._kept
         self._kept = None
         d = d_sh.reshape(gate.shape[0], -1).to(self.dtype)
         out = api.linear_bwd(d, z, w["w_out"], w["b_out"])
         gj = api.residual_norm_bwd(out["x"], None, f["y"], j, gate=gate, **self._joint(w))
         # x's gradient comes by the residual path, through the gate and through the block
-        gg = api.linear_bwd(gj["gate"], x_kept, w["w_gate"], w["b_gate"], "sigmoid")
+        gg = api.linear_bwd(gj["gate"], x, w["w_gate"], w["b_gate"], "sigmoid")
         gf = api.gated_ffn_bwd(gj["f"], n["y"], self._ffn(w), self.act, saved=f["saved"])
         gn = api.layer_norm_bwd(gf["x"], x, n["mean"], n["rstd"], w["norm_weight"], add=gj["x"])
         dx = gn["x"].add_(gg["x"])

@@ -162,3 +162,37 @@ def test_on_another_stream_and_from_a_graph(anchors, n, m, width):
         assert all(torch.equal(a, b) for a, b in zip(eager, want[0][k]))
         for i in range(2):
             assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i][k])), (k, i)
+
+
+def test_checkpoints_take_less_memory(anchors):
+    """What a forward keeps for training: with 8-bit checkpoints the rows of features and the
+    last layer's input lie in 8 bits and an exponent for 32, and nothing is kept beside that."""
+    n, fw, width = 1000, 48, 80
+
+    def kept(checkpoints8):
+        dec = make(anchors, n, 11, feature_width=fw, width=width, checkpoints8=checkpoints8)
+        dec.forward()
+        found, todo = {}, [dec._kept]
+        while todo:
+            v = todo.pop()
+            if isinstance(v, torch.Tensor):
+                s = v.untyped_storage()
+                found[s.data_ptr()] = s.nbytes()
+            elif isinstance(v, dict):
+                todo += v.values()
+            elif isinstance(v, (list, tuple)):
+                todo += v
+        return sum(found.values())
+
+    bits16, bits8 = 2 * (fw + width) * n, sum(33 * ((d + 31) // 32) for d in (fw, width)) * n
+    assert kept(False) - kept(True) == bits16 - bits8
+
+
+def test_only_what_a_checkpoint_holds_is_rounded(anchors):
+    """The gate's weights have the gradient of x itself, which is there in full."""
+    d_sh = torch.randn(70, 4, 3, generator=torch.Generator().manual_seed(2)).cuda()
+    a, b = (make(anchors, checkpoints8=k) for k in (True, False))
+    got, want = ({k: v.clone() for k, v in dec._views(dec.backward(d_sh)["weights"]).items()} for dec in (a, b)
+                 if dec.forward() is not None)
+    assert all(torch.equal(got[k], want[k]) for k in want if k not in ("w_in", "b_in", "w_out"))
+    assert not torch.equal(got["w_out"], want["w_out"])  # z is one of the checkpoints
