@@ -101,7 +101,7 @@ class AnchorDecoder:
         if train:
             z = keep(j.pop("z"))  # all that the backward pass needs of j are y and the statistics
             self._kept = (w, keep(e), x, gate, n, f, j, z)
-        return sh.float().view(-1, self.nc, 3)
+        return sh.float().view(len(self.index), self.nc, 3)
 
     def backward(self, d_sh):
         """Gradients of features and weights from the gradient of the SH coefficients
@@ -110,7 +110,7 @@ class AnchorDecoder:
             raise ValueError("backward() needs a forward() with train=True before it")
         w, e, x, gate, n, f, j, z = self._kept
         self._kept = None
-        d = d_sh.reshape(gate.shape[0], -1).to(self.dtype)
+        d = d_sh.reshape(len(self.index), 3 * self.nc).to(self.dtype)
         out = api.linear_bwd(d, z, w["w_out"], w["b_out"])
         gj = api.residual_norm_bwd(out["x"], None, f["y"], j, gate=gate, **self._joint(w))
         # x's gradient comes by the residual path, through the gate and through the block

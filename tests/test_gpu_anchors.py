@@ -196,3 +196,11 @@ def test_only_what_a_checkpoint_holds_is_rounded(anchors):
                  if dec.forward() is not None)
     assert all(torch.equal(got[k], want[k]) for k in want if k not in ("w_in", "b_in", "w_out"))
     assert not torch.equal(got["w_out"], want["w_out"])  # z is one of the checkpoints
+
+
+def test_decoder_of_no_gaussians(anchors):
+    dec = anchors.AnchorDecoder(torch.zeros(0, dtype=torch.int32, device="cuda"), 5, feature_width=12, width=20, hidden=28, sh_degree=1)
+    sh = dec.forward()
+    assert sh.shape == (0, 4, 3)
+    g = dec.backward(sh)
+    assert all((v == 0).all() for v in g.values())
