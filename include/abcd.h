@@ -630,8 +630,8 @@ ABCD_API int32_t abcd_linear(const abcd_layer* layer /* host */, int64_t n, cons
 
 /* Backward, with dz = dy act'(x w' + b): dx = dz w, dw = dz' x, db = the sum of dz's rows
  * (the residual's gradient is dy itself); written, of dtype, laid out as what they belong to;
- * each may be NULL, then not computed. Both products take dz rounded to dtype, and db may sum it
- * rounded or not. x: the forward's
+ * each may be NULL, then not computed. Both products take dz rounded to dtype; db sums it as
+ * it was before that, or rounded where the slopes of many rows of a wide layer are made again. x: the forward's
  * rows, or NULL and q and e, an 8-bit checkpoint of them (abcd_pack8), whose numbers are then x,
  * in the slopes too where these are made again. slope: the forward's, or NULL: made again
  * from x, w and b. workspace: at least abcd_linear_bwd_workspace_size bytes, 256-byte

@@ -129,9 +129,10 @@ struct LinearDxEnd {
 // Few rows: the weights are read once and bound it (gated_ffn_few.h). 8 waves a workgroup where
 // rows of the weights are short, else 16 (one row in bf16, weights from memory: 2,048 to 5,632
 // 7.6 against 10.0 us, 512 to 1,376 4.3 against 5.3, but 5,632 to 2,048 10.2 against 10.1 and
-// 33 rows of 2,048 to 2,048 12.7 against 10.4). kDz: the backward's product made again (bf16 with
-// SiLU, the whole backward, against the tiles': one row of 512 to 1,376 18.4 against 25.4 us, of
-// 5,632 to 2,048 31.8 against 38.9, 16 rows of 2,048 to 2,048 22.6 against 27.6).
+// 33 rows of 2,048 to 2,048 12.7 against 10.4). kDz: the backward's product made again, and
+// the bias's sums (bf16 with SiLU, the whole backward replayed from a graph, against the tiles': one
+// row of 512 to 1,376 16.5 against 23.9 us, of 5,632 to 2,048 31.5 against 38.2, 16 rows of 2,048 to
+// 2,048 21.4 against 28.0, 32 27.3 against 28.9).
 template <typename T, int kAct, int kX, int kWaves, bool kWhole, bool kDz>
 __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, int columns) {
   f32x4 acc[kX][1], sum[1];
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, in
   if (!few_join<kX, 1, kWaves>(acc, sum)) return;
   const int l = threadIdx.x & 63, r = (threadIdx.x >> 6) * 16 + (l & 15), c = first + (l >> 4) * 4;
   const int left = end - c;
-  if (r >= n || left <= 0) return;
+  if (left <= 0 || (!kDz && r >= n)) return;
   if (a.bias) sum[0] += load_vec<T, 4, false>(static_cast<const T*>(a.bias) + c, left);
   f32x4 y, s;
 #pragma unroll
@@ -152,9 +153,23 @@ __global__ __launch_bounds__(kWaves * 64) void linear_few_kernel(LinearOut a, in
     s[e] = e < left ? slope : 0.0f;
   }
   if (kDz) {
-    T* const to = static_cast<T*>(a.y) + r * a.ldy;
-    store_vec<T, 4, true>(to + c, s * load_vec<T, 4, false>(static_cast<const T*>(a.dy) + r * a.lddy + c, left), 4);
-    if (a.o - c <= 4 && c + 4 < a.ldy) store_vec<T, 4, true>(to + c + 4, Floats<4>(0.0f), 4);
+    f32x4 dz = 0.0f;
+    if (r < n) {
+      T* const to = static_cast<T*>(a.y) + r * a.ldy;
+      dz = s * load_vec<T, 4, false>(static_cast<const T*>(a.dy) + r * a.lddy + c, left);
+      store_vec<T, 4, true>(to + c, dz, 4);
+      if (a.o - c <= 4 && c + 4 < a.ldy) store_vec<T, 4, true>(to + c + 4, Floats<4>(0.0f), 4);
+    }
+    // the bias's sums, of dz before it is rounded: of these 16 rows
+    if (a.db || a.part) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dz[e] = lanes_sum<16>(dz[e]);
+      if ((l & 15) != 0) return;
+      if (a.db)
+        store_vec<T, 4, false>(static_cast<T*>(a.db) + c, dz, left);
+      else
+        store_vec<float, 4, false>(a.part + (threadIdx.x >> 6) * a.o + c, dz, left);
+    }
     return;
   }
   if (a.res) y += load_vec<T, 4, false>(static_cast<const T*>(a.res) + r * a.ldr + c, left);

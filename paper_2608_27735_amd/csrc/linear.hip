@@ -68,7 +68,7 @@ Scratch layout(const abcd_layer& l, int64_t n, bool backward, void* workspace) {
     s.dz = p.take(n * up8(l.o) * sz);
     part = std::max({part, product_part(sz, n, l.i, 1, steps(l.o)), (size_t)(sum_parts_of(n) * l.o),
                      dweight_part(l, steps(n))});
-    s.sums = static_cast<float*>(p.take(sum_parts_of(n) * l.o * sizeof(float)));
+    s.sums = static_cast<float*>(p.take(std::max(sum_parts_of(n), few(l, n) ? few_parts(n) : 0) * l.o * sizeof(float)));
   }
   s.part = static_cast<float*>(p.take(part * sizeof(float)));
   s.bytes = p.used;
@@ -116,6 +116,11 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
     return launch_sum_parts(s.part, blocks, outs, l.dtype, stream);
   }
   const bool again = l.act != ABCD_ACT_NONE && !slope;
+  auto sum_up = [&](int64_t parts) -> int32_t {
+    SumOuts outs{};
+    outs.add(db, l.o);
+    return launch_sum_parts(s.sums, parts, outs, l.dtype, stream);
+  };
   const bool one = sum_parts_of(n) == 1;  // part of the bias's sums, which is then all of them
   const int lanes = std::min(lanes_for((int)(up8(l.o) / 8)), 64);
   Side xs{}, w{}, dz{};
@@ -143,6 +148,10 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
                   0, dz.ld, 0, l.act, Tiling{}};
       a.dy = dy;
       a.lddy = lddy;
+      if (db && few_parts(n) == 1)
+        a.db = db;
+      else if (db)
+        a.part = s.sums;
       TRY_STATUS(LINEAR_BY_TYPE(l, linear_few, a, stream));
     } else if (again) {
       const LinearDz a{xs, w, l.b, dy, s.dz, l.i, l.o, lddy, dz.ld, l.act, Tiling{s.part, 0, 0, 1, 0}};
@@ -164,15 +173,12 @@ int32_t launch_linear_bwd(const abcd_layer& l, int64_t n, const void* dy, int64_
     a.one[a.count++] = FfnDWeight::One{dz.p[0], xs.p[0], dw, dz.ld, l.o, xs.ld, l.i, 1.0f, 0, 0, 0};
     TRY_STATUS(LINEAR_BY_TYPE(l, linear_dw, a, stream));
   }
-  if (slope && one && n > 0) return ABCD_OK;
-  if (one && db && n > 0) {
+  if (!db) return ABCD_OK;
+  if (n > 0 && again && few(l, n)) return few_parts(n) == 1 ? ABCD_OK : sum_up(few_parts(n));
+  if (n > 0 && slope) return one ? ABCD_OK : sum_up(sum_parts_of(n));
+  if (n > 0 && one) {
     const LinearSlope a{dz.p[0], nullptr, nullptr, nullptr, db, n, l.o, dz.ld, 0, up8(l.o), lanes};
     return LINEAR_BY_TYPE(l, linear_slope, a, 1, stream);
-  }
-  if (slope && db && n > 0) {
-    SumOuts outs{};
-    outs.add(db, l.o);
-    return launch_sum_parts(s.sums, sum_parts_of(n), outs, l.dtype, stream);
   }
   SumCall sums{l.dtype, n, s.part};
   sums.add(db, dz.p[0], dz.ld, l.o, 1.0f);

@@ -59,7 +59,12 @@ struct LinearOut {
   Tiling t;
   const void* dy = nullptr;  // linear_few: given, y is dz = dy act'(x w' + bias), columns up to ldy zeros
   int64_t lddy = 0;
+  // the sums of dz's rows: db itself of up to 16 rows, else part: [few_parts(n)][o], of 16 rows each
+  // (both NULL: not wanted)
+  void* db = nullptr;
+  float* part = nullptr;
 };
+inline int64_t few_parts(int64_t n) { return n <= 16 ? 1 : n <= 32 ? 2 : 4; }
 // dz = dy act'(x w' + bias): [n][lddz], columns past o zeros.
 struct LinearDz {
   Side x, w;

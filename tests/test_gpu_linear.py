@@ -231,3 +231,20 @@ def test_checkpoint_of_the_largest_numbers(api, dtype, act, n, i, o):
     dz = dy64 if act is None else dy64 * ((x8 @ w64.T) > 0)
     D.close("dw", got["w"], dz.T @ x8, dz.abs().T @ x8.abs())
     D.close("dx", got["x"], dz @ w64, dz.abs() @ w64.abs())
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("act", ["silu", "sigmoid", "relu"])
+@pytest.mark.parametrize("n,i,o", [(1, 512, 1376), (2, 300, 1001), (16, 512, 1376), (17, 200, 333), (31, 512, 1376), (33, 300, 1001),
+                                   (48, 512, 1376), (64, 300, 2050)])
+def test_bias_gradient_of_few_rows(api, dtype, act, n, i, o):
+    """Where the slopes of a few rows are made again the bias's gradient is the sum of dz before it
+    is rounded, as it is with slopes that were kept: nothing but its own rounding, and the fp32 sums'."""
+    x, w, b, dy = rand(1, n, i, dtype), rand(2, o, i, dtype, scale=i ** -0.5).contiguous(), rand(3, 1, o, dtype)[0], rand(4, n, o, dtype)
+    for rows in (x, api.pack8(x)):
+        x64 = D.d64(rows if rows is x else api.unpack8(rows))
+        ref, mag, sd = R.linear_bwd(D.d64(dy), x64, D.d64(w), D.d64(b), act, 0.0, 0.0)["b"]
+        whole = api.linear_bwd(dy, rows, w, b, act)
+        D.close("db", whole["b"], ref, mag, extra=6 * sd)
+        alone = api.linear_bwd(dy, rows, w, b, act, grads=dict(b=torch.full_like(b, math.nan)))["b"]
+        assert torch.equal(alone, whole["b"])
