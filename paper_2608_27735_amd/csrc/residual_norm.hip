@@ -11,13 +11,16 @@ namespace {
 // Workgroups of the backward, each with its own column sums: one for every CU; of one or two
 // long rows at a time two, where their parameters' LDS has room for that (16,384 x 2,048 in
 // bf16 100 against 119 us, 8,192 x 4,096 140 against 150; 65,536 x 1,024 167 against 159, 1M x 64
-// in fp32 308 against 292).
+// in fp32 308 against 292). A single one, which leaves out the second launch, where it takes all
+// rows at once: two turns of it cost more than that launch saves (bf16, with parameters, two
+// turns against two workgroups and the launch: 4 x 2,048 12.2 against 10.4 us, 2 x 20,000 40 against
+// 22, 8 x 1,024 10.1 against 9.9, but 128 x 64 10.1 against 10.4 and 2 x 4,096 8.7 against 9.1).
 int64_t joint_blocks(const abcd_joint& j, int64_t n) {
   const int64_t item = (int64_t)type_bytes(j.dtype), nvec = (j.d * item + 15) / 16;
   int64_t rows = 64;  // that a workgroup takes at a time: 512 threads, 8 or more a row
   while (rows > 1 && nvec * rows > 512) rows /= 2;
   const int64_t most = rows <= 2 && nvec <= 512 ? 2 * kCUs : kCUs;
-  return n <= 2 * rows ? 1 : std::min<int64_t>((n + rows - 1) / rows, most);
+  return n <= rows ? 1 : std::min<int64_t>((n + rows - 1) / rows, most);
 }
 
 int64_t joint_pitch(int64_t d) { return (d + 7) & ~int64_t(7); }

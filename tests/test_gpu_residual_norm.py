@@ -198,3 +198,11 @@ def test_scale_gradient_of_infinite_rows(api, dtype, post, n, d):
     want, mag = R.residual_norm_bwd(None, D.d64(dy), D.d64(f), None, stats, post, None, {k: D.d64(v) for k, v in p.items()}, None)["scale"]
     assert want.isinf().sum() == 2 and not want.isnan().any()
     D.close("scale", got, want, mag, k=K)
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,d", [(17000, 40), (2100, 700), (1100, 2048), (600, 4096), (300, 8200)])
+def test_joint_rows_in_turns(api, dtype, n, d):
+    """More rows than all workgroups take at once, at every way of holding a row."""
+    say("joint", dtype, n, d)
+    check(api, n, d, dtype, "layer", "layer", "full")
