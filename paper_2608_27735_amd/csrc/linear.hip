@@ -13,10 +13,15 @@ namespace {
    : (l).dtype == ABCD_F16 ? fn##_f16(__VA_ARGS__)              \
                            : fn##_bf16(__VA_ARGS__))
 
-// Whether the kernel for a few rows takes the forward: it reads x again for every 16
-// columns of y.
+// Whether the kernel for a few rows takes the forward: of up to 64, whose four products of 16 are
+// made from one load of the weights, while the tiles' more even work does not pay for their second
+// launch (bf16 with SiLU, weights from memory, by the bytes of weights for each 16 rows: 16 rows of
+// 2,048 to 2,048, 8 MB, 5.6 against 9.6 us; 32 of 2,048 to 2,048, 16 MB, 8.8 against 10.0; 64 of 2,048
+// to 2,048, 32 MB, 11.4 against 11.2; 64 of 2,048 to 4,096, 64 MB, 12.7 against 14.5; 32 of 4,096 to 4,096,
+// 64 MB, 16.7 against 16.0; 64 of 4,096 to 2,560, 80 MB, 20.0 against 16.1; 32 of 8,192 to 8,192, 256
+// MB, 55 against 33). Up to 16 always: they need no workspace (but 8,192 to 8,192 41 against 32).
 bool few(const abcd_layer& l, int64_t n) {
-  return n <= 16 || (n <= 64 && (n + 15) / 16 * l.o * l.i * (int64_t)type_bytes(l.dtype) <= 80 << 20);
+  return n <= 16 || (n <= 64 && (n + 15) / 16 * l.o * l.i * (int64_t)type_bytes(l.dtype) <= 64 << 20);
 }
 
 // Room for the parts of the weights' gradient, none where the rows are too few to split: no
