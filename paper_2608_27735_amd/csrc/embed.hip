@@ -697,7 +697,10 @@ int32_t launch_embed_bwd(int32_t dtype, int64_t n, int64_t m, int64_t d, const v
     const int nvec = (int)((d + kPer16<T> - 1) / kPer16<T>);
     a.lanes = embed_lanes(nvec);
     const int64_t rows = kBlock / a.lanes;
-    // where most rows are empty, and long, a wave looks at several of them at once
+    // where most rows are empty, and long, a wave looks at several of them at once (bf16, sums alone,
+    // one row at a time against four: 8,192 of 32,000 x 2,048 47 against 36 us, x 512 17.1 against 15.1,
+    // but x 256 11.4 against 12.4; 100,000 of 32,000 x 2,048 125 against 131. Short rows of a large
+    // table would gain too, 20,000 of 1M x 64 41 against 31, which this rule leaves out)
     a.turns = n < m && nvec >= kWave ? kRowTurns : 1;
     a.row_blocks = (int)std::min<int64_t>((m + rows * a.turns - 1) / (rows * a.turns), 1 << 18);
     const int64_t blocks = a.row_blocks + (chunks + rows - 1) / rows;
