@@ -254,3 +254,42 @@ def test_checkpoint_refuses(api):
         with pytest.raises(ValueError):
             call()
     assert api.unpack8(api.pack8(x[:0])).shape == (0, 40)
+
+
+# ------------------------- the gradient by a kept sort, which few positions take too
+
+def test_sorted_gradient_of_many_rows(api):
+    """More rows than workgroups, most of them without a position."""
+    m, d = 2200000, 256
+    index = torch.tensor([0, m - 1, 5, m - 1, 2099999, 1048576, 5, m // 2], device="cuda")
+    dy = rand(1, 8, d, torch.bfloat16)
+    got = api.embed_bwd(dy, api.embed_sort(index, m), m)
+    assert torch.equal(got, api.embed_bwd(dy, index, m))
+    got[index] = 0
+    assert not got.any()
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+def test_sorted_gradient_of_far_rows(api, dtype):
+    """Rows more than 2^31 elements apart, of the gradient's table, one of them a row of
+    many positions, and of dy."""
+    ld, m, n = (1 << 30) + 16, 3, 500
+    far = torch.empty(2 * ld + 64, dtype=dtype, device="cuda").as_strided((m, 64), (ld, 1))
+    index = torch.full((n,), 2)
+    index[::7], index[3] = 0, -1
+    dy = rand(1, n, 64, dtype)
+    plan = api.embed_sort(index.cuda(), m)
+    want, mag = R.embed_bwd(D.d64(dy), index, m, 0.5)
+    assert api.embed_bwd(dy, plan, m, 0.5, out=far) is far
+    D.close("far table", far, want, mag, k=64.0 + 18 + n / 1024)  # as in test_embed_both_ways
+    far.copy_(dy[:3])
+    few = torch.tensor([2, 2, 0], device="cuda")
+    assert torch.equal(api.embed_bwd(far, api.embed_sort(few, m), m), api.embed_bwd(dy[:3].contiguous(), few, m))
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("n,m,d", [(900, 3000, 1030), (500, 700, 512), (1300, 2001, 4099)])
+def test_sorted_gradient_of_wide_rows(api, dtype, n, m, d):
+    """Fewer positions than rows, of many vectors: a wave looks at four rows at once, and
+    leaves those of many positions to the sums of parts."""
+    test_embed_both_ways(api, dtype, n, m, d)
