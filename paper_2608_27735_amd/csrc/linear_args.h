@@ -7,9 +7,11 @@
 namespace abcd {
 
 // What a forward keeps of act's derivative: float in fp32; in 16-bit types, as it lies between
-// -0.13 and 1.13, a code of 16 bits: 30,800 times its root, with its sign. A step of that is
-// 2^-14 of a slope of 1 and 2^-12 of one of 0.02, where float16 has 2^-11 of any: kept in
-// the rows' type its rounding would be as large as dz's. -32768 is a NaN.
+// -0.13 and 1.13, a code of 16 bits: 30,800 times its root, with its sign. A slope s is so off by
+// up to sqrt(s) / 30,800, half a step: 2^-15 of a slope of 1, 2^-12 of one of 0.02 and 2^-11, which
+// float16's half a step is of any, of one of 0.0044; of smaller ones (sigmoid's beyond 5.4, the
+// others' tails) it is more, 2^-10 at 0.001 and 2^-5 at 10^-6, and float16's less. Kept in the
+// rows' type its rounding would be as large as dz's. -32768 is a NaN.
 template <typename T>
 using SlopeOf = std::conditional_t<sizeof(T) == 4, float, int16_t>;
 constexpr float kSlopeUnit = 30800.0f;

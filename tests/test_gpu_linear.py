@@ -248,3 +248,20 @@ def test_bias_gradient_of_few_rows(api, dtype, act, n, i, o):
         D.close("db", whole["b"], ref, mag, extra=6 * sd)
         alone = api.linear_bwd(dy, rows, w, b, act, grads=dict(b=torch.full_like(b, math.nan)))["b"]
         assert torch.equal(alone, whole["b"])
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+@pytest.mark.parametrize("n,i", [(16, 64), (200, 64), (200, 300)])
+def test_kept_slopes_of_a_tail(api, dtype, n, i):
+    """The code of a kept slope s holds its root in steps of 1 / 30,800, so that s is off by no
+    more than sqrt(s) / 30,800 and a quarter of a step squared. With w the identity and dy ones dx
+    is s, rounded once as dz and unchanged by the product with ones and zeros."""
+    x = torch.linspace(-12.0, -4.0, n * i).view(n, i).to(dtype).cuda()
+    w, dy = torch.eye(i, dtype=dtype, device="cuda"), torch.ones(n, i, dtype=dtype, device="cuda")
+    saved = api.linear(x, w, act="sigmoid", save=True)["saved"]
+    s = R.act(D.d64(x), "sigmoid")[1]
+    got = D.d64(api.linear_bwd(dy, x, w, act="sigmoid", saved=saved)["x"])
+    # and in fp32 by the exponent rounded at a z of 12, and 12 more for exponentials, reciprocals and product
+    code = s.sqrt() / 30800 + 0.25 / 30800 ** 2 + 24 * D.E32 * s
+    u = D.UNIT[dtype]
+    assert ((got - s).abs() <= u * s + D.TINY[dtype] + (1 + u) * code).all()
