@@ -265,3 +265,42 @@ def test_kept_slopes_of_a_tail(api, dtype, n, i):
     code = s.sqrt() / 30800 + 0.25 / 30800 ** 2 + 24 * D.E32 * s
     u = D.UNIT[dtype]
     assert ((got - s).abs() <= u * s + D.TINY[dtype] + (1 + u) * code).all()
+
+
+@pytest.mark.parametrize("n,i,o", [(40, 64, 64), (3000, 64, 64), (300, 200, 300)])
+def test_not_finite_rows_of_float32(api, n, i, o):
+    test_not_finite_rows_stay_by_themselves(api, torch.float32, n, i, o)
+
+
+def test_far_rows_of_float32(api):
+    test_far_rows(api, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+def test_weight_gradient_of_large_tiles(api, dtype):
+    """260 tiles of 256 x 256: a round of the GPU, and four whose rows are split into parts
+    that the kernel for many of them adds up; the last tile of each side is not whole."""
+    n, i, o = 8200, 256 * 13 - 8, 256 * 20 - 24
+    say("dw", n, i, o, dtype)
+    x, dy = rand(1, n, i, dtype), rand(2, n, o, dtype)
+    w = torch.zeros(o, i, dtype=dtype, device="cuda")
+    dw = torch.full_like(w, math.nan)
+    api.linear_bwd(dy, x, w, grads=dict(w=dw))
+    # a row of every tile, and the last ones; fp32 sums of 8,200 terms: 128 indexes a step, one
+    # product's sum after the other (257 of 32 terms), or parts of fewer and their sum
+    rows = torch.tensor([256 * k + 37 * k % 256 for k in range(19)] + [256 * 19 + 5, o - 1])
+    dy64, x64 = D.d64(dy[:, rows.cuda()]), D.d64(x)
+    D.close("dw", dw[rows.cuda()], dy64.T @ x64, dy64.abs().T @ x64.abs(), k=300.0)
+
+
+@pytest.mark.parametrize("dtype", DT[1:], ids=IDS[1:])
+def test_layer_of_small_tiles_by_rounds(api, dtype):
+    """288 large tiles, whose second round would be nearly empty: the small ones take it."""
+    n, i, o = 6000, 3000, 3000
+    say("linear", n, i, o, dtype)
+    x, w, b, r = rand(1, n, i, dtype), rand(2, o, i, dtype, scale=i ** -0.5).contiguous(), rand(3, 1, o, dtype)[0], rand(4, n, o, dtype)
+    y = api.linear(x, w, b, "silu", residual=r)["y"]
+    rows = torch.tensor([0, 127, 128, 255, 2999, 5887, 5888, 5999])
+    at = rows.cuda()
+    ref, mag = R.linear(D.d64(x[at]), D.d64(w), D.d64(b), "silu", D.d64(r[at]))
+    D.close("y", y[at], ref, mag, k=110.0)  # 94 products' sums one after the other, the bias, act and residual
