@@ -342,6 +342,9 @@ __global__ __launch_bounds__(kJointBwdThreads<G>, 4) void residual_norm_bwd_kern
     if (a.dgate && a.gate_mode == 1 && row < a.n && t == 0) static_cast<T*>(a.dgate)[row * a.lddg] = (T)s[2];
     if (a.df && in) {
       const float c1 = a.post == ABCD_NORM_LAYER ? s[0] * a.inv_d : 0.0f, c2 = has_post ? s[1] * a.inv_d : 0.0f;
+      // without a norm c2 is 0, which an infinity or a NaN of f has to leave so (with one it is a NaN then)
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] = __builtin_amdgcn_fmed3f(f[i], -__FLT_MAX__, __FLT_MAX__);
       store_vec<T, N, kWhole>(static_cast<T*>(a.df) + row * a.lddf + c, pr * (g - c1 - f * c2), a.d - c);
     }
   }
@@ -471,13 +474,13 @@ __global__ __launch_bounds__(kWide) void residual_norm_bwd_wide_kernel(JointArgs
     joint_sums<kWide, 3>(s3, red3, turn3);
     if (a.dgate && a.gate_mode == 1 && threadIdx.x == 0) static_cast<T*>(a.dgate)[row * a.lddg] = (T)s3[2];
     if (!a.df) continue;
-    const float c3 = a.post == ABCD_NORM_LAYER ? s3[0] * a.inv_d : 0.0f, c4 = has_post ? s3[1] * a.inv_d : 0.0f;
+    const float c3 = a.post == ABCD_NORM_LAYER ? s3[0] * a.inv_d : 0.0f, c4 = s3[1] * a.inv_d;
     for (int c = threadIdx.x * N; c < a.d; c += kWide * N) {
       Floats<N> dz, h;
-      const Floats<N> g = grad(c, dz, h) * gate_at(c) * joint_param<T, N, kWhole>(a, a.scale, c, 1.0f) *
-                          joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f);
-      const Floats<N> f = hat(joint_load<T, N, kWhole>(a.f, row, a.ldf, c, a), pm, pr, c);
-      store_vec<T, N, kWhole>(static_cast<T*>(a.df) + row * a.lddf + c, pr * (g - c3 - f * c4), a.d - c);
+      Floats<N> g = grad(c, dz, h) * gate_at(c) * joint_param<T, N, kWhole>(a, a.scale, c, 1.0f) *
+                    joint_param<T, N, kWhole>(a, a.post_w, c, 1.0f);
+      if (has_post) g = pr * (g - c3 - hat(joint_load<T, N, kWhole>(a.f, row, a.ldf, c, a), pm, pr, c) * c4);
+      store_vec<T, N, kWhole>(static_cast<T*>(a.df) + row * a.lddf + c, g, a.d - c);
     }
   }
 }

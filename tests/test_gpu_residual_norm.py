@@ -206,3 +206,21 @@ def test_joint_rows_in_turns(api, dtype, n, d):
     """More rows than all workgroups take at once, at every way of holding a row."""
     say("joint", dtype, n, d)
     check(api, n, d, dtype, "layer", "layer", "full")
+
+
+@pytest.mark.parametrize("dtype", DT, ids=IDS)
+@pytest.mark.parametrize("gate", ["none", "row", "full"])
+@pytest.mark.parametrize("n,d", [(6, 64), (9, 1001), (5, 20001)])
+def test_gradients_of_infinite_rows_without_norms(api, dtype, gate, n, d):
+    """Without a norm f has no part in its own gradient nor in x's: an infinity or a NaN in it
+    leaves both as they are."""
+    f, x, p, g = make(n, d, dtype, None, None, gate)
+    f[1, 3], f[2], f[3, d - 1] = math.inf, math.nan, -math.inf
+    call = dict(params=p, gate=g)
+    r = api.residual_norm(f, x, **call)
+    dy = rand(12, n, d, dtype)
+    got = api.residual_norm_bwd(None, dy, f, r, **call)
+    want = R.residual_norm_bwd(None, D.d64(dy), D.d64(f), None, {}, None, None, {k: D.d64(v) for k, v in p.items()}, D.d64(g))
+    assert torch.isfinite(want["f"][0]).all()
+    for k in ("x", "f"):
+        D.close(k, got[k], want[k][0], want[k][1], k=K)
