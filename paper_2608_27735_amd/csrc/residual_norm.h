@@ -17,7 +17,7 @@
 // rows that a workgroup takes, and a second launch adds the workgroups' in a fixed order.
 // Rows too long for a workgroup's registers are read again (the wide kernels).
 //
-// 1M x 64 in bf16 with a gate a row, forward 110 us (530 MB, 4.8 TB/s), backward 164; 8,192 x 4,096
+// 1M x 64 in bf16 with a gate a row, forward 110 us (530 MB, 4.8 TB/s), backward 158; 8,192 x 4,096
 // with a gate an element, backward 115 us and 8 for the column sums (537 MB, 4.7 TB/s).
 #pragma once
 
