@@ -29,7 +29,8 @@ class AnchorDecoder:
     def __init__(self, index, m, feature_width=32, width=64, hidden=128, sh_degree=3, features=None,
                  dtype=torch.bfloat16, act="silu", checkpoints8=False, seed=0):
         dev = index.device
-        self.index, self.m, self.dtype, self.act = index, int(m), dtype, act
+        # a copy: what embed_sort makes of it below belongs to these anchors
+        self.index, self.m, self.dtype, self.act = index.clone(), int(m), dtype, act
         self.checkpoints8 = bool(checkpoints8)
         self.scale = float(feature_width) ** 0.5
         self.nc = (sh_degree + 1) ** 2
@@ -60,7 +61,7 @@ class AnchorDecoder:
         if self.features.shape != (self.m, feature_width):
             raise ValueError(f"features must have shape ({self.m}, {feature_width})")
         # anchors do not change: their positions are sorted once for all steps
-        self.sorted = api.embed_sort(index, self.m)
+        self.sorted = api.embed_sort(self.index, self.m)
         self.params = dict(features=self.features, weights=self.flat)
         self.grads = {k: torch.zeros_like(v) for k, v in self.params.items()}
         self._grad = self._views(self.grads["weights"])

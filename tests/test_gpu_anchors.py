@@ -204,3 +204,15 @@ def test_decoder_of_no_gaussians(anchors):
     assert sh.shape == (0, 4, 3)
     g = dec.backward(sh)
     assert all((v == 0).all() for v in g.values())
+
+
+def test_anchors_are_those_at_construction(anchors):
+    """A caller's later change of index reaches neither the lookup nor the gradient's sort."""
+    d_sh = torch.randn(70, 4, 3, generator=torch.Generator().manual_seed(2)).cuda()
+    index = (torch.arange(70) * 3 % 11).cuda()
+    kw = dict(feature_width=12, width=20, hidden=28, sh_degree=1, seed=4)
+    a, b = (anchors.AnchorDecoder(i, 11, **kw) for i in (index, index.clone()))
+    index.fill_(0)
+    assert torch.equal(a.forward(), b.forward())
+    got, want = a.backward(d_sh), b.backward(d_sh)
+    assert all(torch.equal(got[k], want[k]) for k in want)
